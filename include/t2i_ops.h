@@ -2,7 +2,10 @@
  * t2i_ops.h -- kernel-level entry points of the denoising step.
  *
  * The same kernels t2i_dit_step launches, exposed one by one so that each can
- * be checked against its definition in isolation.  Conventions are those of
+ * be checked against its definition in isolation, and operators of transformer
+ * blocks that the models above do not have: an 8-bit linear layer, a gated
+ * feed-forward with its gradients, query / key norm with rotation and its
+ * gradients.  Conventions are those of
  * t2i_dit.h: device pointers are caller-owned HIP memory, `stream` is a
  * hipStream_t as void*, launches are asynchronous, arguments are validated
  * before any launch, errors come back as t2i_status (text in
@@ -158,6 +161,138 @@ t2i_status t2i_op_lora_merge(int32_t dtype, int32_t n_out, int32_t n_in, int32_t
 t2i_status t2i_op_lora_merge_batch(int32_t dtype, int32_t n, int32_t n_out, int32_t n_in,
                                    int32_t rank, float alpha, void* const* W, int32_t ldw,
                                    const void* const* A, const void* const* B, void* stream);
+
+/*
+ * Rows quantised to 8 bits with one scale each, the input of the 8-bit linear
+ * layer (activations per token, weights per output channel):
+ *   scale[r] = max(max_k |x[r, k]| / 127, 2^-126), rounded once to fp32;
+ *   q[r, k]  = x[r, k] / scale[r] to the nearest whole number, ties to even
+ *              (of the exact quotient; -127 .. 127).
+ * A row that holds a NaN or an infinity gets scale NaN and q = 0.
+ *   x [rows, K] of dtype (bf16 or fp32), row stride ldx >= K, any alignment of
+ *   its type (16-byte aligned rows are read in whole pieces: same results,
+ *   less time); q [rows, ldq] with ldq % 16 == 0, ldq >= K rounded up to a
+ *   multiple of 128, 16-byte aligned: columns K .. that multiple are written
+ *   as zeros, columns behind it are left alone; scale [rows] fp32.
+ */
+t2i_status t2i_op_quant_rows(int32_t dtype, int32_t rows, int32_t K, const void* x, int32_t ldx,
+                             int8_t* q, int32_t ldq, float* scale, void* stream);
+
+/*
+ * Linear layer in 8-bit integers with a scale for every row of A (token) and
+ * every row of W (output channel), with the epilogues of t2i_op_linear:
+ *   y[m, n] = a_scale[m] * w_scale[n] * sum_k A[m, k] W[n, k] + bias[n].
+ * The sum is exact (32-bit integers, K <= 131071); it is rounded once to fp32,
+ * the rest is fp32.
+ *   A [M, K], W [N, K] int8, 16-byte aligned, row strides lda, ldw multiples of
+ *   16 and at least K rounded up to a multiple of 128: both are read up to
+ *   there, and one of the two must hold zeros behind K (t2i_op_quant_rows
+ *   writes them).  dtype is the type of bias [N] (or NULL: none) and out; the
+ *   remaining arguments are those of t2i_op_linear.
+ */
+t2i_status t2i_op_linear_i8(int32_t dtype, int32_t epilogue, int32_t M, int32_t N, int32_t K,
+                            const int8_t* A, int32_t lda, const float* a_scale, const int8_t* W,
+                            int32_t ldw, const float* w_scale, const void* bias, void* out,
+                            int32_t ldo, float* resid, int32_t ldr, void* resid_copy,
+                            const float* gate, void* stream);
+
+/*
+ * Gated feed-forward, first half (both projections, the activation and the
+ * product in one kernel; t2i_op_linear is the second half):
+ *   g = A Wg^T + bg,  u = A Wu^T + bu,  out = act(g) (.) u,
+ * act T2I_EPI_GELU (tanh form) or T2I_EPI_SILU.
+ *   A [M, K] (stride lda), Wg and Wu [F, K] (common stride ldw; the halves of
+ *   one [2F, K] matrix: Wu = Wg + F ldw), bg and bu [F] (both or neither),
+ *   out [M, F] (stride ldo), all of dtype; sums, activation and product in
+ *   fp32, one rounding.
+ *   pre [M, 2F] (stride ldp) or NULL: receives g | u rounded to dtype, which
+ *   t2i_op_gated_linear_backward reads.
+ *   bf16: F, K and the strides % 8 == 0, every pointer 16-byte aligned.
+ *   fp32: any sizes.
+ * No output may overlap an input.
+ */
+t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,
+                               const void* A, int32_t lda, const void* Wg, const void* Wu,
+                               int32_t ldw, const void* bg, const void* bu, void* out,
+                               int32_t ldo, void* pre, int32_t ldp, void* stream);
+
+/*
+ * Gradients of t2i_op_gated_linear: with dout [M, F] (stride ldd) the gradient
+ * of out and pre the forward pass's,
+ *   dg = dout (.) u (.) act'(g),  du = dout (.) act(g),
+ *   dA = dg Wg + du Wu [M, K],  dWg = dg^T A,  dWu = du^T A [F, K],
+ *   dbg, dbu = column sums of dg, du [F],
+ * all of dtype.  dg and du are rounded to dtype once, for the products (the
+ * bias sums take them unrounded); products and sums are fp32.  dA (stride
+ * ldda), dWg, dWu (common stride lddw) may each be NULL: not computed; dbg and
+ * dbu both or neither.  Sizes, strides and alignment as in the forward pass.
+ * ws: device workspace of ws_bytes >= t2i_op_gated_linear_backward_ws_bytes,
+ * 256-byte aligned, used by this call until it has finished on the stream;
+ * the result does not depend on what it holds.  No output may overlap an
+ * input.  Every sum has a fixed order.
+ */
+size_t t2i_op_gated_linear_backward_ws_bytes(int32_t dtype, int32_t M, int32_t F);
+t2i_status t2i_op_gated_linear_backward(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,
+                                        const void* A, int32_t lda, const void* Wg, const void* Wu,
+                                        int32_t ldw, const void* pre, int32_t ldp, const void* dout,
+                                        int32_t ldd, void* dA, int32_t ldda, void* dWg, void* dWu,
+                                        int32_t lddw, void* dbg, void* dbu, void* ws,
+                                        size_t ws_bytes, void* stream);
+
+/* Which elements of a head make up the rotated pairs. */
+typedef enum {
+  T2I_ROPE_PAIRS = 0,   /* (2j, 2j + 1), as the joint-attention model's */
+  T2I_ROPE_HALVES = 1   /* (j, j + head_dim / 2); head_dim % 16 == 0 */
+} t2i_rope_pairing;
+
+/*
+ * RMS norm of every head of the queries and keys, then the position rotation,
+ * in one pass (before t2i_op_attention):
+ *   n = x / sqrt(mean(x^2) + eps) * w,
+ *   pair j of the head turned by (cos, sin) = table[p][j]:
+ *   (a, b) -> (a cos - b sin, a sin + b cos).
+ *   q [rows, heads_q * head_dim] (stride ldq), k [rows, heads_k * head_dim]
+ *   (stride ldk; the columns of one fused projection, or buffers of their
+ *   own), wq, wk [head_dim] or NULL (ones), outputs q_out, k_out alike, all of
+ *   dtype; the arithmetic is fp32, one rounding.  heads_q or heads_k may be 0
+ *   (its pointers are then unused); rows * (heads_q + heads_k) < 2^31.
+ *   table fp32 [n_pos][head_dim / 2][2] of (cos, sin), or NULL: no rotation
+ *   (one, two or more position axes: the table's rows say which pair turns by
+ *   which angle).  Row r turns by table row pos[r] (device, [rows]), or r when
+ *   pos is NULL (then n_pos >= rows).  pos[r] < 0: row r is not turned (text
+ *   rows of joint attention); pos[r] >= n_pos: row r's outputs are NaN.
+ *   head_dim % 8 == 0, 8 .. 256, strides % 8 == 0, every pointer 16-byte
+ *   aligned (pos: 4).
+ * In place (q_out == q, ldqo == ldq; the same for k) is allowed, any other
+ * overlap of an output with an input is not.  Keep the inputs if the backward
+ * pass is to follow.
+ */
+t2i_status t2i_op_qk_norm_rope(int32_t dtype, int32_t rows, int32_t heads_q, int32_t heads_k,
+                               int32_t head_dim, const void* q, int32_t ldq, const void* k,
+                               int32_t ldk, const void* wq, const void* wk, float eps,
+                               int32_t pairing, const float* table, int32_t n_pos,
+                               const int32_t* pos, void* q_out, int32_t ldqo, void* k_out,
+                               int32_t ldko, void* stream);
+
+/*
+ * Gradients of t2i_op_qk_norm_rope: dq, dk the gradients of q_out, k_out; q, k
+ * and the other arguments the forward pass's inputs; dq_in, dk_in receive the
+ * gradients of q, k, dwq, dwk [head_dim] (or NULL) those of the weights, summed
+ * over rows and heads in a fixed order, all of dtype.  dq_in may be dq itself
+ * (same stride), dk_in dk.  ws as in t2i_op_gated_linear_backward (may be NULL
+ * when dwq and dwk are).
+ */
+size_t t2i_op_qk_norm_rope_backward_ws_bytes(int32_t rows, int32_t heads_q, int32_t heads_k,
+                                             int32_t head_dim);
+t2i_status t2i_op_qk_norm_rope_backward(int32_t dtype, int32_t rows, int32_t heads_q,
+                                        int32_t heads_k, int32_t head_dim, const void* dq,
+                                        int32_t lddq, const void* dk, int32_t lddk, const void* q,
+                                        int32_t ldq, const void* k, int32_t ldk, const void* wq,
+                                        const void* wk, float eps, int32_t pairing,
+                                        const float* table, int32_t n_pos, const int32_t* pos,
+                                        void* dq_in, int32_t lddqi, void* dk_in, int32_t lddki,
+                                        void* dwq, void* dwk, void* ws, size_t ws_bytes,
+                                        void* stream);
 
 /*
  * Memory-counter calibration (not part of the denoising step): reads `bytes`

@@ -8,6 +8,8 @@ kernels.  The functions below carry the C ABI's names:
 * :func:`t2i_dit_step`   one model evaluation (+ guidance, + Euler update)
 * :func:`t2i_dit_sample` the whole denoising loop with the optional cache skip
 * :func:`t2i_cache_check` the cache-skip decision of one step
+* :func:`quant_rows`, :func:`linear_i8`, :func:`gated_linear`, :func:`qk_norm_rope` and
+  the gradients of the last two: operators of transformer blocks (``ops.py``)
 * :func:`t2i_dit_host_tier`, :func:`t2i_dit_evict`, :func:`t2i_dit_load_async`,
   :func:`t2i_dit_block_state`: first-layers caching with progressive loading
 """
@@ -22,11 +24,15 @@ import torch
 from . import _lib
 from ._lib import (T2I_F32, T2I_BF16, T2I_ARCH_CROSS_DIT, T2I_ARCH_MMDIT,
                    T2I_CACHE_ACCUMULATE, T2I_CACHE_PER_STEP, T2IError, check, load)
+from .ops import (gated_linear, gated_linear_backward, linear_i8, qk_norm_rope,
+                  qk_norm_rope_backward, quant_rows)
 
 __all__ = ["Config", "DiT", "t2i_dit_init", "t2i_dit_init_static", "t2i_dit_step", "t2i_dit_sample",
            "t2i_cache_check", "weight_table", "upload", "T2IError", "load",
            "t2i_dit_block_layout", "pack_blocks", "t2i_dit_host_tier", "t2i_dit_evict",
-           "t2i_dit_load_async", "t2i_dit_block_state", "t2i_first_layers"]
+           "t2i_dit_load_async", "t2i_dit_block_state", "t2i_first_layers",
+           "quant_rows", "linear_i8", "gated_linear", "gated_linear_backward", "qk_norm_rope",
+           "qk_norm_rope_backward"]
 
 
 def _stream(stream=None) -> int:

@@ -16,6 +16,7 @@ T2I_F32, T2I_BF16 = 0, 1
 T2I_ARCH_CROSS_DIT, T2I_ARCH_MMDIT = 0, 1
 T2I_CACHE_ACCUMULATE, T2I_CACHE_PER_STEP = 0, 1
 T2I_EPI_STORE, T2I_EPI_GELU, T2I_EPI_SILU, T2I_EPI_RESID, T2I_EPI_RESID_GATED = range(5)
+T2I_ROPE_PAIRS, T2I_ROPE_HALVES = 0, 1
 T2I_MAX_SEQ, T2I_MAX_REQ = 64, 32
 
 KERNEL_CLASSES = ["gemm_qkv", "attn_self", "gemm_o", "gemm_xq", "attn_cross", "gemm_xo",
@@ -109,6 +110,20 @@ SIGNATURES = {
     "t2i_op_lora_merge_batch": (i32, [i32, i32, i32, i32, i32, f32, C.POINTER(vp), i32,
                                       C.POINTER(vp), C.POINTER(vp), vp]),
     "t2i_op_lora_merge": (i32, [i32, i32, i32, i32, f32, vp, i32, vp, vp, vp]),
+    "t2i_op_quant_rows": (i32, [i32, i32, i32, vp, i32, vp, i32, vp, vp]),
+    "t2i_op_linear_i8": (i32, [i32, i32, i32, i32, i32, vp, i32, vp, vp, i32, vp, vp, vp, i32, vp,
+                               i32, vp, vp, vp]),
+    "t2i_op_gated_linear": (i32, [i32, i32, i32, i32, i32, vp, i32, vp, vp, i32, vp, vp, vp, i32,
+                                  vp, i32, vp]),
+    "t2i_op_gated_linear_backward_ws_bytes": (sz, [i32, i32, i32]),
+    "t2i_op_gated_linear_backward": (i32, [i32, i32, i32, i32, i32, vp, i32, vp, vp, i32, vp, i32,
+                                           vp, i32, vp, i32, vp, vp, i32, vp, vp, vp, sz, vp]),
+    "t2i_op_qk_norm_rope": (i32, [i32, i32, i32, i32, i32, vp, i32, vp, i32, vp, vp, f32, i32, vp,
+                                  i32, vp, vp, i32, vp, i32, vp]),
+    "t2i_op_qk_norm_rope_backward_ws_bytes": (sz, [i32, i32, i32, i32]),
+    "t2i_op_qk_norm_rope_backward": (i32, [i32, i32, i32, i32, i32, vp, i32, vp, i32, vp, i32, vp,
+                                           i32, vp, vp, f32, i32, vp, i32, vp, vp, i32, vp, i32,
+                                           vp, vp, vp, sz, vp]),
     "t2i_sched_create": (i32, [f64, C.POINTER(vp)]),
     "t2i_sched_destroy": (None, [vp]),
     "t2i_sched_submit": (i32, [vp, i32, C.c_int64, f64, f64, f64]),

@@ -16,6 +16,7 @@
 
 #include "../../include/t2i_dit.h"
 #include "../../include/t2i_ops.h"
+#include "block_ops.h"
 #include "t2i_internal.h"
 
 using namespace t2i;
@@ -271,6 +272,19 @@ t2i_status fail(t2i_dit* h, t2i_status s, const std::string& msg) {
   if (h) h->err = msg;
   return s;
 }
+
+}  // namespace
+
+t2i_status t2i::ops_fail(t2i_status s, const char* msg) noexcept {
+  try {
+    g_ops_err = msg;
+  } catch (...) {
+    g_ops_err.clear();
+  }
+  return s;
+}
+
+namespace {
 
 #define HIP_TRY(h, expr)                                                              \
   do {                                                                                \
@@ -1446,10 +1460,6 @@ t2i_status t2i_dit_sample(t2i_dit* h, const t2i_sample_args* a, void* stream) {
 
 const char* t2i_ops_last_error(void) { return g_ops_err.c_str(); }
 
-static t2i_status ops_fail(t2i_status s, const std::string& m) {
-  g_ops_err = m;
-  return s;
-}
 
 t2i_status t2i_op_linear(int32_t dtype, int32_t epilogue, int32_t M, int32_t N, int32_t K,
                          const void* A, int32_t lda, const void* W, int32_t ldw, const void* bias,

@@ -1,0 +1,587 @@
+// Row-wise block operators (gfx950): quantising rows to 8 bits, the gated
+// feed-forward's elementwise gradients, RMS norm of query and key heads with
+// the position rotation, and its gradients.  All of them are bound by HBM:
+// each input is read once, 16 bytes per lane, held in registers, and each
+// output written once.
+#include <algorithm>
+
+#include "block_ops.h"
+
+namespace t2i {
+
+// eight consecutive elements as fp32 (16 bytes of bf16, 32 of fp32)
+template <typename T>
+__device__ __forceinline__ void load8(const T* p, float (&v)[8]);
+template <>
+__device__ __forceinline__ void load8<bf16>(const bf16* p, float (&v)[8]) {
+  const bf16x8 w = *(const bf16x8*)p;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = (float)w[i];
+}
+template <>
+__device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
+  const f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+}
+template <typename T>
+__device__ __forceinline__ void store8(T* p, const float (&v)[8]);
+template <>
+__device__ __forceinline__ void store8<bf16>(bf16* p, const float (&v)[8]) {
+  bf16x8 w;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) w[i] = (bf16)v[i];
+  *(bf16x8*)p = w;
+}
+template <>
+__device__ __forceinline__ void store8<float>(float* p, const float (&v)[8]) {
+  *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+  *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+}
+
+template <int G>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = G / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
+  return v;
+}
+
+// ---------------------------------------------------------------------------
+// Quantising rows: s = max(max |x| / 127, 2^-126) in fp32, q = x / s to the
+// nearest whole number, ties to even, of the exact quotient.
+//
+// The rounding costs no division: n = rint(x (1/s)) is off by one at most, and
+// only where x / s lies within its error of a half.  r = fma(-n, s, x) is
+// then exact (|r| is at most about s / 2 and a multiple of s's last place over
+// four), so comparing 2 r with s settles the tie exactly.
+// A row with a NaN or an infinity gets s = NaN and q = 0: its outputs are NaN.
+
+__device__ __forceinline__ int quant1(float x, float s, float inv) {
+  float n = rintf(x * inv);
+  const float r2 = 2.f * fmaf(-n, s, x);
+  const bool odd = ((int)n & 1) != 0;
+  if (r2 > s || (r2 == s && odd)) n += 1.f;
+  else if (r2 < -s || (r2 == -s && odd)) n -= 1.f;
+  return (int)n;
+}
+
+__device__ __forceinline__ uint32_t abs_bits(float v) {
+  return __float_as_uint(v) & 0x7fffffffu;   // orders as |v|, infinity and NaN above
+}
+
+// TPR threads per row, NV pieces of 8 elements per thread in registers; longer
+// rows read their pieces again.  VEC: rows start at multiples of 16 bytes and
+// K % 8 == 0 is not needed (the last piece is read element by element).
+template <typename T, int TPR, int NV, bool VEC>
+__global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x, int ldx, int rows,
+                                                         int K, int8_t* __restrict__ q, int ldq,
+                                                         float* __restrict__ scale) {
+  constexpr int RPB = 256 / TPR;
+  __shared__ uint32_t red[RPB][TPR / 64];
+  const int t = threadIdx.x % TPR, rl = threadIdx.x / TPR;
+  const int row = blockIdx.x * RPB + rl;
+  const bool live = row < rows;
+  const T* xr = x + (size_t)(live ? row : 0) * ldx;
+  auto load = [&](int c, float (&v)[8]) {
+    const int k = c * 8;
+    if (VEC && k + 8 <= K) {
+      load8(xr + k, v);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = k + i < K ? to_f32(xr[k + i]) : 0.f;
+    }
+  };
+  const int chunks = (K + 127) / 128 * 16;   // the zeros behind K too
+  float v[NV][8];
+  uint32_t m = 0;
+  const int rounds = (chunks + TPR * NV - 1) / (TPR * NV);
+  for (int r = 0; r < rounds; ++r) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (r * NV + i) * TPR + t;
+      if (c * 8 < K && live) load(c, v[i]);
+      else
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[i][j]));
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, kWave));
+  if constexpr (TPR > 64) {
+    if ((t & 63) == 0) red[rl][t >> 6] = m;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < TPR / 64; ++i) m = max(m, red[rl][i]);
+  }
+  const bool finite = m < 0x7f800000u;
+  const float s = fmaxf(__uint_as_float(finite ? m : 0u) / 127.f, 1.17549435e-38f);
+  const float inv = 1.f / s;
+  if (live && t == 0) scale[row] = finite ? s : __uint_as_float(0x7fc00000u);
+  for (int r = 0; r < rounds; ++r) {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int c = (r * NV + i) * TPR + t;
+      if (c >= chunks || !live) continue;
+      if (rounds > 1) {
+        if (c * 8 < K) load(c, v[i]);
+        else
+#pragma unroll
+          for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+      }
+      uint32_t w[2] = {0, 0};
+      if (finite)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[j >> 2] |= (uint32_t)(quant1(v[i][j], s, inv) & 255) << (8 * (j & 3));
+      *(uint2*)(q + (size_t)row * ldq + c * 8) = uint2{w[0], w[1]};
+    }
+  }
+}
+
+hipError_t launch_quant_rows(bool bf16_in, int rows, int K, const void* x, int ldx, int8_t* q,
+                             int ldq, float* scale, hipStream_t st) {
+  // one wave per row up to 2048 elements, a workgroup for longer rows
+  const bool wave = K <= 2048;
+  const int rpb = wave ? 4 : 1;
+  const dim3 grid((unsigned)((rows + (long)rpb - 1) / rpb));
+  const size_t e = bf16_in ? 2 : 4;
+  const bool vec = (uintptr_t)x % 16 == 0 && ldx * e % 16 == 0;
+#define T2I_Q(T, TPR, NV, VEC)                                                                      \
+  hipLaunchKernelGGL((quant_rows_kernel<T, TPR, NV, VEC>), grid, dim3(256), 0, st, (const T*)x, ldx, \
+                     rows, K, q, ldq, scale)
+  if (bf16_in) {
+    if (wave) { if (vec) T2I_Q(bf16, 64, 4, true); else T2I_Q(bf16, 64, 4, false); }
+    else { if (vec) T2I_Q(bf16, 256, 4, true); else T2I_Q(bf16, 256, 4, false); }
+  } else {
+    if (wave) { if (vec) T2I_Q(float, 64, 4, true); else T2I_Q(float, 64, 4, false); }
+    else { if (vec) T2I_Q(float, 256, 4, true); else T2I_Q(float, 256, 4, false); }
+  }
+#undef T2I_Q
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// Query / key norm with rotation.  G lanes hold one head, 8 elements each
+// (G = the power of two at or above head_dim / 8); a group keeps one row's
+// rotation and takes HPG of its heads.
+
+// The rotation of a lane's elements.  Pairs (2j, 2j + 1): four pairs in the lane.
+// Halves (j, j + d/2): eight elements whose partners sit in another lane.
+template <bool HALVES>
+struct Rotor {
+  static constexpr int N = HALVES ? 8 : 4;
+  float c[N], s[N];
+  bool turn;
+  int partner;   // lane of the wave that holds the other half
+
+  // lg: lane within the head, nl: lanes in use; inverse: the transposed rotation
+  __device__ __forceinline__ void load(const QkNorm& a, int row, int lg, int nl, bool inverse) {
+    turn = false;
+    partner = threadIdx.x & 63;
+    if (!a.table) return;
+    const int pos = a.pos ? a.pos[row] : row;
+    if (pos < 0) return;
+    turn = true;
+    float sg = inverse ? -1.f : 1.f;
+    if (HALVES) {
+      const int hl = nl / 2;
+      partner += lg < hl ? hl : lg < nl ? -hl : 0;
+      if (lg < hl) sg = -sg;
+      lg -= lg < hl ? 0 : hl;
+    }
+    if (pos >= a.n_pos || lg * N >= a.head_dim / 2) {   // behind the table (or a spare lane)
+#pragma unroll
+      for (int i = 0; i < N; ++i) c[i] = s[i] = __uint_as_float(0x7fc00000u);
+      return;
+    }
+    const float4* t = (const float4*)(a.table + (size_t)pos * (a.head_dim / 2) + lg * N);
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) {
+      const float4 p = t[i];
+      c[2 * i] = p.x, s[2 * i] = sg * p.y, c[2 * i + 1] = p.z, s[2 * i + 1] = sg * p.w;
+    }
+  }
+  __device__ __forceinline__ void apply(float (&v)[8]) const {
+    if (HALVES) {
+      float o[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = __shfl(v[i], partner, kWave);
+      if (turn)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = fmaf(o[i], s[i], v[i] * c[i]);
+    } else if (turn) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float x = v[2 * i], y = v[2 * i + 1];
+        v[2 * i] = fmaf(-y, s[i], x * c[i]);
+        v[2 * i + 1] = fmaf(x, s[i], y * c[i]);
+      }
+    }
+  }
+};
+
+template <typename T>
+__device__ __forceinline__ void load_weight(const void* w, int lg, int nl, float (&v)[8]) {
+  if (w && lg < nl) load8((const T*)w + lg * 8, v);
+  else
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 1.f;
+}
+
+template <typename T, int G, bool HALVES, int HPG>
+__global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNorm a, int upr) {
+  const int lg = threadIdx.x % G, nl = a.head_dim / 8, H = a.heads_q + a.heads_k;
+  const unsigned unit = blockIdx.x * (256 / G) + threadIdx.x / G;
+  const unsigned r = unit / (unsigned)upr;
+  const int h0 = (int)(unit - r * (unsigned)upr);
+  const bool live = r < (unsigned)a.rows && lg < nl;
+  const int row = r < (unsigned)a.rows ? (int)r : 0;
+  float v[HPG][8];
+#pragma unroll
+  for (int i = 0; i < HPG; ++i) {
+    const int h = h0 + i * upr;
+    if (live && h < H) {
+      const T* p = h < a.heads_q ? (const T*)a.q + (size_t)row * a.ldq + h * a.head_dim
+                                 : (const T*)a.k + (size_t)row * a.ldk + (h - a.heads_q) * a.head_dim;
+      load8(p + lg * 8, v[i]);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+    }
+  }
+  Rotor<HALVES> rot;
+  rot.load(a, row, lg, nl, false);
+  float wq[8], wk[8];
+  load_weight<T>(a.wq, lg, nl, wq);
+  load_weight<T>(a.wk, lg, nl, wk);
+  const float rd = 1.f / (float)a.head_dim;
+#pragma unroll
+  for (int i = 0; i < HPG; ++i) {
+    const int h = h0 + i * upr;
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
+    const float rs = rsqrtf(fmaf(group_sum<G>(ss), rd, a.eps));
+    const bool isq = h < a.heads_q;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * rs * (isq ? wq[j] : wk[j]);
+    rot.apply(v[i]);
+    if (live && h < H) {
+      T* p = isq ? (T*)a.oq + (size_t)row * a.ldoq + h * a.head_dim
+                 : (T*)a.ok + (size_t)row * a.ldok + (h - a.heads_q) * a.head_dim;
+      store8(p + lg * 8, v[i]);
+    }
+  }
+}
+
+// lanes that hold one head
+static int head_lanes(int head_dim) {
+  int g = 1;
+  while (g * 8 < head_dim) g *= 2;
+  return g;
+}
+
+template <typename T, int G, bool HALVES>
+static void qk_launch(const QkNorm& a, hipStream_t st) {
+  const int H = a.heads_q + a.heads_k;
+  const int gr = 256 / G;
+  // several heads of a row per group where that still leaves workgroups enough
+  const int hpg = (long)a.rows * ((H + 3) / 4) / gr >= 1024 ? 4 : 1;
+  const int upr = (H + hpg - 1) / hpg;
+  const dim3 grid((unsigned)(((long)a.rows * upr + gr - 1) / gr));
+  if (hpg == 4)
+    hipLaunchKernelGGL((qk_norm_rope_kernel<T, G, HALVES, 4>), grid, dim3(256), 0, st, a, upr);
+  else
+    hipLaunchKernelGGL((qk_norm_rope_kernel<T, G, HALVES, 1>), grid, dim3(256), 0, st, a, upr);
+}
+
+// Backward.  With n = x r, r = (mean x^2 + eps)^-1/2, y = R (n w):
+//   dn = (R^T dy) w,  dx = r (dn - n mean(dn n)),  dw = sum over rows and heads
+//   of (R^T dy) n.
+// A fixed number of workgroups walks the (row, heads) units; dw adds up in
+// registers, then over the workgroup in LDS, then (qk_weight_grad_kernel) over
+// the workgroups: a fixed order.
+template <typename T, int G, bool HALVES>
+__global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, float* __restrict__ partial) {
+  constexpr int GR = 256 / G;
+  __shared__ float red[2][GR][G * 8];
+  const int lg = threadIdx.x % G, gi = threadIdx.x / G, nl = a.head_dim / 8;
+  const int H = a.heads_q + a.heads_k;
+  const unsigned units = (unsigned)a.rows * (unsigned)H, stride = gridDim.x * GR;
+  float wq[8], wk[8], aq[8], ak[8];
+  load_weight<T>(a.wq, lg, nl, wq);
+  load_weight<T>(a.wk, lg, nl, wk);
+#pragma unroll
+  for (int j = 0; j < 8; ++j) aq[j] = ak[j] = 0.f;
+  const float rd = 1.f / (float)a.head_dim;
+  for (unsigned u0 = blockIdx.x * GR; u0 < units; u0 += stride) {
+    const unsigned u = u0 + gi;
+    const bool in = u < units, live = in && lg < nl;
+    const int row = in ? (int)(u / (unsigned)H) : 0;
+    const int h = in ? (int)(u - (unsigned)row * (unsigned)H) : 0;
+    const bool isq = h < a.heads_q;
+    const int hh = isq ? h : h - a.heads_q;
+    float x[8], dy[8];
+    if (live) {
+      load8((isq ? (const T*)a.q + (size_t)row * a.ldq : (const T*)a.k + (size_t)row * a.ldk) +
+                hh * a.head_dim + lg * 8, x);
+      load8((isq ? (const T*)a.dq + (size_t)row * a.lddq : (const T*)a.dk + (size_t)row * a.lddk) +
+                hh * a.head_dim + lg * 8, dy);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) x[j] = dy[j] = 0.f;
+    }
+    Rotor<HALVES> rot;
+    rot.load(a, row, lg, nl, true);
+    rot.apply(dy);
+    if (!live)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) dy[j] = 0.f;   // (a spare lane's rotation is NaN)
+    float ss = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) ss = fmaf(x[j], x[j], ss);
+    const float r = rsqrtf(fmaf(group_sum<G>(ss), rd, a.eps));
+    float dot = 0.f;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      x[j] = live ? x[j] * r : 0.f;   // n
+      const float p = dy[j] * x[j];
+      if (isq) aq[j] += p;
+      else ak[j] += p;
+      dy[j] *= isq ? wq[j] : wk[j];
+      dot = fmaf(dy[j], x[j], dot);
+    }
+    dot = group_sum<G>(dot) * rd;
+#pragma unroll
+    for (int j = 0; j < 8; ++j) dy[j] = r * fmaf(-x[j], dot, dy[j]);
+    if (live)
+      store8((isq ? (T*)a.oq + (size_t)row * a.ldoq : (T*)a.ok + (size_t)row * a.ldok) +
+                 hh * a.head_dim + lg * 8, dy);
+  }
+  if (!partial) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    red[0][gi][lg * 8 + j] = aq[j];
+    red[1][gi][lg * 8 + j] = ak[j];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * a.head_dim; i += 256) {
+    const int w = i / a.head_dim, c = i - w * a.head_dim;
+    float s = 0.f;
+#pragma unroll 4
+    for (int g = 0; g < GR; ++g) s += red[w][g][c];
+    partial[(size_t)blockIdx.x * 2 * a.head_dim + i] = s;
+  }
+}
+
+int qk_bwd_blocks(int rows, int heads, int head_dim) {
+  const int gr = 256 / head_lanes(head_dim);
+  return (int)std::min<long>(1024, ((long)rows * heads + gr - 1) / gr);
+}
+
+template <typename T, int G, bool HALVES>
+static void qk_bwd_launch(const QkNorm& a, float* partial, hipStream_t st) {
+  const dim3 grid((unsigned)qk_bwd_blocks(a.rows, a.heads_q + a.heads_k, a.head_dim));
+  hipLaunchKernelGGL((qk_norm_rope_bwd_kernel<T, G, HALVES>), grid, dim3(256), 0, st, a, partial);
+}
+
+#define T2I_QK(FN, ...)                                                             \
+  switch (head_lanes(a.head_dim)) {                                                 \
+    case 1: FN<T, 1, HALVES>(__VA_ARGS__); break;                                   \
+    case 2: FN<T, 2, HALVES>(__VA_ARGS__); break;                                   \
+    case 4: FN<T, 4, HALVES>(__VA_ARGS__); break;                                   \
+    case 8: FN<T, 8, HALVES>(__VA_ARGS__); break;                                   \
+    case 16: FN<T, 16, HALVES>(__VA_ARGS__); break;                                 \
+    default: FN<T, 32, HALVES>(__VA_ARGS__); break;                                 \
+  }
+template <typename T, bool HALVES>
+static void qk_any(const QkNorm& a, hipStream_t st) { T2I_QK(qk_launch, a, st) }
+template <typename T, bool HALVES>
+static void qk_bwd_any(const QkNorm& a, float* partial, hipStream_t st) {
+  T2I_QK(qk_bwd_launch, a, partial, st)
+}
+#undef T2I_QK
+
+hipError_t launch_qk_norm_rope(bool is_bf16, const QkNorm& a, hipStream_t st) {
+  if (is_bf16) a.halves ? qk_any<bf16, true>(a, st) : qk_any<bf16, false>(a, st);
+  else a.halves ? qk_any<float, true>(a, st) : qk_any<float, false>(a, st);
+  return hipGetLastError();
+}
+
+hipError_t launch_qk_norm_rope_bwd(bool is_bf16, const QkNorm& a, float* partial, hipStream_t st) {
+  if (is_bf16) a.halves ? qk_bwd_any<bf16, true>(a, partial, st) : qk_bwd_any<bf16, false>(a, partial, st);
+  else a.halves ? qk_bwd_any<float, true>(a, partial, st) : qk_bwd_any<float, false>(a, partial, st);
+  return hipGetLastError();
+}
+
+// Column sums of n rows of fp32 partials (row stride ld) in fp64: 16 columns
+// per workgroup, each by 16 threads that take every 16th row, joined in a
+// fixed order.
+__device__ __forceinline__ double column_sum(const float* p, int n, size_t ld, int c, bool in) {
+  __shared__ double red[16][16];
+  const int s = threadIdx.x / 16, l = threadIdx.x % 16;
+  double v = 0.;
+  if (in)
+    for (int i = s; i < n; i += 16) v += (double)p[(size_t)i * ld + c];
+  red[s][l] = v;
+  __syncthreads();
+  v = 0.;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v += red[i][l];
+  return v;
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void qk_weight_grad_kernel(const float* __restrict__ partial,
+                                                             int blocks, int d, T* __restrict__ dwq,
+                                                             T* __restrict__ dwk) {
+  const int c = blockIdx.x * 16 + threadIdx.x % 16;
+  const double v = column_sum(partial, blocks, (size_t)2 * d, c, c < 2 * d);
+  if (threadIdx.x < 16 && c < 2 * d) {
+    T* o = c < d ? dwq : dwk;
+    if (o) o[c < d ? c : c - d] = from_f32<T>((float)v);
+  }
+}
+
+hipError_t launch_qk_weight_grad(bool is_bf16, int blocks, int head_dim, const float* partial,
+                                 void* dwq, void* dwk, hipStream_t st) {
+  const dim3 grid((unsigned)((2 * head_dim + 15) / 16));
+  if (is_bf16)
+    hipLaunchKernelGGL((qk_weight_grad_kernel<bf16>), grid, dim3(256), 0, st, partial, blocks, head_dim,
+                       (bf16*)dwq, (bf16*)dwk);
+  else
+    hipLaunchKernelGGL((qk_weight_grad_kernel<float>), grid, dim3(256), 0, st, partial, blocks,
+                       head_dim, (float*)dwq, (float*)dwk);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// Gated feed-forward, elementwise gradients: with a = act(g),
+//   dg = dh u act'(g),  du = dh a,
+// rounded once to the operands' type for the products that follow; the bias
+// gradients' column sums take the unrounded values.
+
+struct ActGrad { float a, d; };   // act(g), act'(g)
+__device__ __forceinline__ ActGrad act_grad(int act, float g) {
+  if (act == EPI_GELU) {
+    // g sigmoid(2 z), z = sqrt(2/pi) (g + 0.044715 g^3)
+    constexpr float c0 = 2.0f * 0.7978845608028654f, c1 = -c0 * 1.4426950408889634f;
+    const float g2 = g * g;
+    const float s = __builtin_amdgcn_rcpf(
+        1.f + __builtin_amdgcn_exp2f(g * fmaf(c1 * 0.044715f, g2, c1)));
+    const float p = s * (1.f - s);
+    // (p is 0 before g2 overflows)
+    const float d = p == 0.f ? 0.f : p * g * c0 * fmaf(3.f * 0.044715f, g2, 1.f);
+    return {g * s, s + d};
+  }
+  const float s = __builtin_amdgcn_rcpf(1.f + __expf(-g)), a = g * s;
+  return {a, fmaf(a, 1.f - s, s)};
+}
+
+constexpr int kGateRows = 64;   // rows per workgroup
+int gate_row_blocks(int M) { return (M + kGateRows - 1) / kGateRows; }
+
+// V columns per thread (8 where rows are whole 16-byte pieces, else 1): 32
+// threads side by side, 8 rows at a time
+template <typename T, int V>
+__global__ __launch_bounds__(256) void gate_grad_kernel(int act, int M, int F, int Fp,
+                                                        const T* __restrict__ pre, int ldp,
+                                                        const T* __restrict__ dout, int ldd,
+                                                        T* __restrict__ dgu, float* __restrict__ partial) {
+  __shared__ float red[2][8][32 * V];
+  const int tx = threadIdx.x % 32, ty = threadIdx.x / 32;
+  const int f = (blockIdx.y * 32 + tx) * V;
+  const int r0 = blockIdx.x * kGateRows;
+  float sg[V], su[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) sg[j] = su[j] = 0.f;
+  if (f < Fp)
+    for (int r = r0 + ty; r < min(r0 + kGateRows, M); r += 8) {
+      float g[V], u[V], dh[V];
+      if (f < F) {
+        const T* p = pre + (size_t)r * ldp + f;
+        if constexpr (V == 8) {
+          load8(p, g);
+          load8(p + F, u);
+          load8(dout + (size_t)r * ldd + f, dh);
+        } else {
+          g[0] = to_f32(p[0]);
+          u[0] = to_f32(p[F]);
+          dh[0] = to_f32(dout[(size_t)r * ldd + f]);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          const ActGrad ag = act_grad(act, g[j]);
+          g[j] = dh[j] * u[j] * ag.d;
+          u[j] = dh[j] * ag.a;
+          sg[j] += g[j];
+          su[j] += u[j];
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < V; ++j) g[j] = u[j] = 0.f;
+      }
+      T* o = dgu + (size_t)r * 2 * Fp + f;
+      if constexpr (V == 8) {
+        store8(o, g);
+        store8(o + Fp, u);
+      } else {
+        o[0] = from_f32<T>(g[0]);
+        o[Fp] = from_f32<T>(u[0]);
+      }
+    }
+  if (!partial) return;
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    red[0][ty][tx * V + j] = sg[j];
+    red[1][ty][tx * V + j] = su[j];
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < 2 * 32 * V; i += 256) {
+    const int w = i / (32 * V), c = i - w * 32 * V, col = blockIdx.y * 32 * V + c;
+    if (col >= Fp) continue;
+    float s = 0.f;
+#pragma unroll
+    for (int y = 0; y < 8; ++y) s += red[w][y][c];
+    partial[(size_t)blockIdx.x * 2 * Fp + w * Fp + col] = s;
+  }
+}
+
+hipError_t launch_gate_grad(bool is_bf16, int act, int M, int F, const void* pre, int ldp,
+                            const void* dout, int ldd, void* dgu, float* partial, hipStream_t st) {
+  const int Fp = gated_cols(F), per = is_bf16 ? 256 : 32;
+  const dim3 grid((unsigned)gate_row_blocks(M), (unsigned)((Fp + per - 1) / per));
+  if (is_bf16)
+    hipLaunchKernelGGL((gate_grad_kernel<bf16, 8>), grid, dim3(256), 0, st, act, M, F, Fp,
+                       (const bf16*)pre, ldp, (const bf16*)dout, ldd, (bf16*)dgu, partial);
+  else
+    hipLaunchKernelGGL((gate_grad_kernel<float, 1>), grid, dim3(256), 0, st, act, M, F, Fp,
+                       (const float*)pre, ldp, (const float*)dout, ldd, (float*)dgu, partial);
+  return hipGetLastError();
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void gate_bias_grad_kernel(const float* __restrict__ partial, int blocks,
+                                                             int F, int Fp, T* __restrict__ dbg,
+                                                             T* __restrict__ dbu) {
+  const int c = blockIdx.x * 16 + threadIdx.x % 16, w = blockIdx.y;
+  const double v = column_sum(partial + (size_t)w * Fp, blocks, (size_t)2 * Fp, c, c < F);
+  if (threadIdx.x < 16 && c < F) (w ? dbu : dbg)[c] = from_f32<T>((float)v);
+}
+
+hipError_t launch_gate_bias_grad(bool is_bf16, int M, int F, const float* partial, void* dbg,
+                                 void* dbu, hipStream_t st) {
+  const dim3 grid((unsigned)((F + 15) / 16), 2);
+  if (is_bf16)
+    hipLaunchKernelGGL((gate_bias_grad_kernel<bf16>), grid, dim3(256), 0, st, partial,
+                       gate_row_blocks(M), F, gated_cols(F), (bf16*)dbg, (bf16*)dbu);
+  else
+    hipLaunchKernelGGL((gate_bias_grad_kernel<float>), grid, dim3(256), 0, st, partial,
+                       gate_row_blocks(M), F, gated_cols(F), (float*)dbg, (float*)dbu);
+  return hipGetLastError();
+}
+
+}  // namespace t2i

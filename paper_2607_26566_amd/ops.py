@@ -1,0 +1,293 @@
+"""Block operators (``include/t2i_ops.h``): 8-bit linear layer, gated
+feed-forward, query / key norm with rotation, and their gradients.
+
+Argument marshalling only, as in the package's other calls.  Tensors are device
+tensors of one device whose last dimension is contiguous (rows may be strided);
+results are new tensors of that device.  The work runs on ``stream``, by default
+the device's current stream, and results and workspaces are allocated for that
+stream: a caller that uses another stream on either side orders the two itself.
+Wrong arguments raise :class:`T2IError` before anything is launched.
+"""
+from __future__ import annotations
+
+import contextlib
+import ctypes as C
+from typing import Optional, Tuple
+
+import torch
+
+from . import _lib
+from ._lib import T2I_BF16, T2I_F32, T2IError, load
+
+EPILOGUES = {"store": _lib.T2I_EPI_STORE, "gelu": _lib.T2I_EPI_GELU, "silu": _lib.T2I_EPI_SILU,
+             "resid": _lib.T2I_EPI_RESID, "resid_gated": _lib.T2I_EPI_RESID_GATED}
+ACTS = {"gelu": _lib.T2I_EPI_GELU, "silu": _lib.T2I_EPI_SILU}
+PAIRINGS = {"pairs": _lib.T2I_ROPE_PAIRS, "halves": _lib.T2I_ROPE_HALVES}
+_DTYPES = {torch.bfloat16: T2I_BF16, torch.float32: T2I_F32}
+
+
+def _check(status: int):
+    if status != 0:
+        raise T2IError(status, load().t2i_ops_last_error().decode())
+
+
+def _need(ok: bool, what: str, status: int = 2):
+    if not ok:
+        raise T2IError(status, what)
+
+
+def _of(table: dict, key, what: str):
+    if key not in table:
+        raise T2IError(1, f"{what} must be one of {', '.join(map(str, table))}")
+    return table[key]
+
+
+def _device(*tensors) -> torch.device:
+    """The one device of all given tensors (None entries left out)."""
+    dev = None
+    for t in tensors:
+        if t is None:
+            continue
+        if not t.is_cuda:
+            raise T2IError(1, "operands must be device tensors")
+        if dev is None:
+            dev = t.device
+        elif t.device != dev:
+            raise T2IError(1, "operands must be on one device")
+    return dev
+
+
+def _rows(t: torch.Tensor, shape, dtype, what: str) -> int:
+    """Row stride of a 2-D tensor of this shape and type (its columns contiguous)."""
+    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
+        raise T2IError(2, f"{what}: expected {tuple(shape)} {dtype}, got {tuple(t.shape)} {t.dtype}")
+    _need(shape[1] == 1 or t.stride(1) == 1, f"{what}: columns must be contiguous")
+    ld = t.stride(0) if shape[0] > 1 else shape[1]   # (a single row may come with any stride)
+    _need(shape[1] <= ld < 2 ** 31, f"{what}: rows must not overlap")
+    return ld
+
+
+def _vec(t: Optional[torch.Tensor], n: int, dtype, what: str):
+    if t is not None and (t.dtype != dtype or tuple(t.shape) != (n,) or (n > 1 and t.stride(0) != 1)):
+        raise T2IError(2, f"{what}: expected ({n},) {dtype}, contiguous")
+
+
+def _p(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+@contextlib.contextmanager
+def _on_other(dev, stream):
+    with torch.cuda.device(dev), torch.cuda.stream(stream):
+        yield C.c_void_p(stream.cuda_stream)
+
+
+class _Here:
+    """The current stream of the current device: nothing to switch."""
+
+    def __init__(self, handle):
+        self.handle = handle
+
+    def __enter__(self):
+        return self.handle
+
+    def __exit__(self, *exc):
+        return False
+
+
+def _on(dev: torch.device, stream):
+    if stream is None:
+        if dev.index == torch.cuda.current_device():
+            return _Here(C.c_void_p(torch.cuda.current_stream().cuda_stream))
+        stream = torch.cuda.current_stream(dev)
+    elif stream.device != dev:
+        raise T2IError(1, "stream belongs to another device than the operands")
+    return _on_other(dev, stream)
+
+
+def quant_rows(x: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """Rows of ``x [rows, K]`` (bf16 or fp32) in 8 bits with a scale each
+    (``t2i_op_quant_rows``): ``(q int8 [rows, K rounded up to 128], scale fp32
+    [rows])``, zeros behind column K."""
+    dev = _device(x)
+    dt = _of(_DTYPES, x.dtype, "dtype")
+    _need(x.dim() == 2, "x must be [rows, K]")
+    rows, K = x.shape
+    ld = _rows(x, (rows, K), x.dtype, "x")
+    with _on(dev, stream) as st:
+        q = torch.empty((rows, (K + 127) // 128 * 128), dtype=torch.int8, device=dev)
+        scale = torch.empty(rows, dtype=torch.float32, device=dev)
+        _check(load().t2i_op_quant_rows(dt, rows, K, x.data_ptr(), ld, q.data_ptr(), q.shape[1],
+                                        scale.data_ptr(), st))
+    return q, scale
+
+
+def linear_i8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: torch.Tensor,
+              bias: Optional[torch.Tensor] = None, *, K: int, epilogue: str = "store",
+              dtype: torch.dtype = torch.bfloat16, resid: Optional[torch.Tensor] = None,
+              resid_copy: Optional[torch.Tensor] = None, gate: Optional[torch.Tensor] = None,
+              stream=None) -> torch.Tensor:
+    """8-bit linear layer (``t2i_op_linear_i8``) of ``a [M, >= K]`` and ``w [N, >= K]``
+    as :func:`quant_rows` makes them, with the epilogues of the bf16 layer:
+    ``store``, ``gelu``, ``silu`` return ``[M, N]`` of ``dtype``; ``resid`` and
+    ``resid_gated`` add to the fp32 ``resid [M, N]`` in place (and write the bf16
+    ``resid_copy``, if given) and return it."""
+    dev = _device(a, a_scale, w, w_scale, bias, resid, resid_copy, gate)
+    dt, epi = _of(_DTYPES, dtype, "dtype"), _of(EPILOGUES, epilogue, "epilogue")
+    _need(a.dim() == 2 and w.dim() == 2, "a and w must be matrices")
+    (M, ka), (N, kw) = a.shape, w.shape
+    need = (K + 127) // 128 * 128
+    _need(K >= 1 and ka >= need and kw >= need, "a and w must reach K rounded up to 128")
+    lda, ldw = _rows(a, (M, ka), torch.int8, "a"), _rows(w, (N, kw), torch.int8, "w")
+    lda, ldw = (need if M == 1 else lda), (need if N == 1 else ldw)
+    _vec(a_scale, M, torch.float32, "a_scale")
+    _vec(w_scale, N, torch.float32, "w_scale")
+    _vec(bias, N, dtype, "bias")
+    _vec(gate, N, torch.float32, "gate")
+    ldr = N
+    if epi >= _lib.T2I_EPI_RESID:
+        _need(resid is not None, f"{epilogue} needs resid", 1)
+        ldr = _rows(resid, (M, N), torch.float32, "resid")
+        if resid_copy is not None:
+            ldc = _rows(resid_copy, (M, N), torch.bfloat16, "resid_copy")
+            _need(M == 1 or ldc == ldr, "resid_copy must have resid's row stride")
+    else:
+        _need(resid is None and resid_copy is None, "resid goes with the resid epilogues", 1)
+    _need((gate is not None) == (epilogue == "resid_gated"), "gate goes with resid_gated", 1)
+    with _on(dev, stream) as st:
+        out = None
+        if epi < _lib.T2I_EPI_RESID:
+            out = torch.empty((M, N), dtype=dtype, device=dev)
+        _check(load().t2i_op_linear_i8(dt, epi, M, N, K, a.data_ptr(), lda, a_scale.data_ptr(),
+                                       w.data_ptr(), ldw, w_scale.data_ptr(), _p(bias), _p(out), N,
+                                       _p(resid), ldr, _p(resid_copy), _p(gate), st))
+    return resid if out is None else out
+
+
+def _gated_args(x, wg, wu):
+    dt = _of(_DTYPES, x.dtype, "dtype")
+    _need(x.dim() == 2 and wg.dim() == 2, "x and the weights must be matrices")
+    (M, K), F = x.shape, wg.shape[0]
+    lda = _rows(x, (M, K), x.dtype, "x")
+    ldw = _rows(wg, (F, K), x.dtype, "wg")
+    _need(_rows(wu, (F, K), x.dtype, "wu") == ldw, "wg and wu must have one row stride")
+    return dt, M, F, K, lda, ldw
+
+
+def gated_linear(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor,
+                 bg: Optional[torch.Tensor] = None, bu: Optional[torch.Tensor] = None, *,
+                 act: str = "silu", save_pre: bool = False, stream=None):
+    """``act(x wg^T + bg) * (x wu^T + bu)`` (``t2i_op_gated_linear``): ``x [M, K]``,
+    ``wg``, ``wu`` ``[F, K]``, one dtype (bf16 or fp32); ``[M, F]``.  With ``save_pre``
+    also the pre-activations ``[M, 2F]`` that :func:`gated_linear_backward` takes."""
+    dev = _device(x, wg, wu, bg, bu)
+    dt, M, F, K, lda, ldw = _gated_args(x, wg, wu)
+    a = _of(ACTS, act, "act")
+    _vec(bg, F, x.dtype, "bg")
+    _vec(bu, F, x.dtype, "bu")
+    with _on(dev, stream) as st:
+        out = torch.empty((M, F), dtype=x.dtype, device=dev)
+        pre = torch.empty((M, 2 * F), dtype=x.dtype, device=dev) if save_pre else None
+        _check(load().t2i_op_gated_linear(dt, a, M, F, K, x.data_ptr(), lda, wg.data_ptr(),
+                                          wu.data_ptr(), ldw, _p(bg), _p(bu), out.data_ptr(), F,
+                                          _p(pre), 2 * F, st))
+    return (out, pre) if save_pre else out
+
+
+def gated_linear_backward(dout: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor,
+                          pre: torch.Tensor, *, act: str = "silu", bias: bool = False,
+                          need_dx: bool = True, need_dw: bool = True, stream=None):
+    """Gradients of :func:`gated_linear` (``t2i_op_gated_linear_backward``):
+    ``(dx, dwg, dwu, dbg, dbu)``, None for those not asked for."""
+    dev = _device(dout, x, wg, wu, pre)
+    dt, M, F, K, lda, ldw = _gated_args(x, wg, wu)
+    a = _of(ACTS, act, "act")
+    ldd = _rows(dout, (M, F), x.dtype, "dout")
+    ldp = _rows(pre, (M, 2 * F), x.dtype, "pre")
+    lib = load()
+    with _on(dev, stream) as st:
+        new = lambda on, *shape: torch.empty(shape, dtype=x.dtype, device=dev) if on else None  # noqa: E731
+        dx, dwg, dwu = new(need_dx, M, K), new(need_dw, F, K), new(need_dw, F, K)
+        dbg, dbu = new(bias, F), new(bias, F)
+        n = lib.t2i_op_gated_linear_backward_ws_bytes(dt, M, F)
+        ws = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)
+        _check(lib.t2i_op_gated_linear_backward(
+            dt, a, M, F, K, x.data_ptr(), lda, wg.data_ptr(), wu.data_ptr(), ldw, pre.data_ptr(), ldp,
+            dout.data_ptr(), ldd, _p(dx), K, _p(dwg), _p(dwu), K, _p(dbg), _p(dbu), ws.data_ptr(), n, st))
+    return dx, dwg, dwu, dbg, dbu
+
+
+def _heads(t: torch.Tensor, rows: int, d: int, dtype, what: str):
+    """(heads, row stride) of a [rows, heads, d] tensor whose heads lie side by side."""
+    if t.dtype != dtype or t.dim() != 3 or t.shape[0] != rows or t.shape[2] != d:
+        raise T2IError(2, f"{what}: expected ({rows}, heads, {d}) {dtype}, got {tuple(t.shape)} {t.dtype}")
+    h = t.shape[1]
+    _need(t.stride(2) == 1 and (h == 1 or t.stride(1) == d), f"{what}: heads must be side by side")
+    ld = t.stride(0) if rows > 1 else h * d
+    _need(h * d <= ld < 2 ** 31, f"{what}: rows must not overlap")
+    return h, ld
+
+
+def _qk_args(q, k, wq, wk, table, pos, pairing, extra=()):
+    dev = _device(q, k, wq, wk, table, pos, *extra)
+    dt = _of(_DTYPES, q.dtype, "dtype")
+    pr = _of(PAIRINGS, pairing, "pairing")
+    _need(q.dim() == 3, "q must be [rows, heads, head_dim]")
+    rows, _, d = q.shape
+    hq, ldq = _heads(q, rows, d, q.dtype, "q")
+    hk, ldk = _heads(k, rows, d, q.dtype, "k")
+    _vec(wq, d, q.dtype, "wq")
+    _vec(wk, d, q.dtype, "wk")
+    n_pos = 0
+    if table is not None:
+        n_pos = table.shape[0]
+        _need(table.dtype == torch.float32 and tuple(table.shape) == (n_pos, d // 2, 2)
+              and table.is_contiguous(), f"table must be fp32 [n_pos, {d // 2}, 2], contiguous")
+    _need(pos is None or table is not None, "pos goes with a table", 1)
+    _vec(pos, rows, torch.int32, "pos")
+    return dev, dt, pr, rows, hq, hk, d, ldq, ldk, n_pos
+
+
+def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, wq: Optional[torch.Tensor] = None,
+                 wk: Optional[torch.Tensor] = None, *, table: Optional[torch.Tensor] = None,
+                 pos: Optional[torch.Tensor] = None, eps: float = 1e-6, pairing: str = "pairs",
+                 inplace: bool = False, stream=None):
+    """RMS norm of every head of ``q [rows, heads_q, d]`` and ``k [rows, heads_k, d]``
+    with weights ``wq``, ``wk`` ``[d]`` (or None), then the rotation by
+    ``table[pos[row]]`` (``t2i_op_qk_norm_rope``): ``table`` fp32 ``[n_pos, d/2, 2]`` of
+    (cos, sin) or None, ``pos`` int32 ``[rows]`` (negative: not turned) or None (row r
+    at position r).  Returns new ``(q, k)``, or with ``inplace`` the given ones."""
+    dev, dt, pr, rows, hq, hk, d, ldq, ldk, n_pos = _qk_args(q, k, wq, wk, table, pos, pairing)
+    with _on(dev, stream) as st:
+        oq = q if inplace else torch.empty((rows, hq, d), dtype=q.dtype, device=dev)
+        ok = k if inplace else torch.empty((rows, hk, d), dtype=q.dtype, device=dev)
+        _check(load().t2i_op_qk_norm_rope(
+            dt, rows, hq, hk, d, q.data_ptr(), ldq, k.data_ptr(), ldk, _p(wq), _p(wk), eps, pr,
+            _p(table), n_pos, _p(pos), oq.data_ptr(), ldq if inplace else hq * d, ok.data_ptr(),
+            ldk if inplace else hk * d, st))
+    return oq, ok
+
+
+def qk_norm_rope_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k: torch.Tensor,
+                          wq: Optional[torch.Tensor] = None, wk: Optional[torch.Tensor] = None, *,
+                          table: Optional[torch.Tensor] = None, pos: Optional[torch.Tensor] = None,
+                          eps: float = 1e-6, pairing: str = "pairs", stream=None):
+    """Gradients of :func:`qk_norm_rope` (``t2i_op_qk_norm_rope_backward``) from those of
+    its outputs and its inputs: ``(dq, dk, dwq, dwk)``, None for a weight that is None."""
+    dev, dt, pr, rows, hq, hk, d, ldq, ldk, n_pos = _qk_args(q, k, wq, wk, table, pos, pairing, (dq, dk))
+    h1, lddq = _heads(dq, rows, d, q.dtype, "dq")
+    h2, lddk = _heads(dk, rows, d, q.dtype, "dk")
+    _need((h1, h2) == (hq, hk), "gradients must have the heads of q and k")
+    lib = load()
+    with _on(dev, stream) as st:
+        oq = torch.empty((rows, hq, d), dtype=q.dtype, device=dev)
+        ok = torch.empty((rows, hk, d), dtype=q.dtype, device=dev)
+        dwq = torch.empty(d, dtype=q.dtype, device=dev) if wq is not None else None
+        dwk = torch.empty(d, dtype=q.dtype, device=dev) if wk is not None else None
+        n = lib.t2i_op_qk_norm_rope_backward_ws_bytes(rows, hq, hk, d)
+        ws = torch.empty(n, dtype=torch.uint8, device=dev) if wq is not None or wk is not None else None
+        _check(lib.t2i_op_qk_norm_rope_backward(
+            dt, rows, hq, hk, d, dq.data_ptr(), lddq, dk.data_ptr(), lddk, q.data_ptr(), ldq,
+            k.data_ptr(), ldk, _p(wq), _p(wk), eps, pr, _p(table), n_pos, _p(pos), oq.data_ptr(), hq * d,
+            ok.data_ptr(), hk * d, _p(dwq), _p(dwk), _p(ws), n, st))
+    return oq, ok, dwq, dwk

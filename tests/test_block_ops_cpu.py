@@ -1,0 +1,227 @@
+"""The block operators on the host: the oracle's formulas against differences,
+and every refusal of the entry points (nothing here reaches a GPU: each call
+fails its argument checks)."""
+import ctypes as C
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2607_26566_amd as t2i
+from paper_2607_26566_amd import _lib
+from oracle import blocks
+
+F32, BF16 = _lib.T2I_F32, _lib.T2I_BF16
+INVALID, SHAPE, WORKSPACE = 1, 2, 4
+P = 1 << 20   # an aligned address that no call here reads
+
+
+def rng(seed):
+    return np.random.default_rng(seed)
+
+
+# ------------------------------------------------------------------ oracle
+
+@pytest.mark.parametrize("act", ["gelu", "silu"])
+def test_gated_gradients_against_differences(act):
+    r = rng(1)
+    M, F, K = 3, 4, 5
+    p = dict(x=r.normal(size=(M, K)), wg=r.normal(size=(F, K)), wu=r.normal(size=(F, K)),
+             bg=r.normal(size=F), bu=r.normal(size=F))
+    dout = r.normal(size=(M, F))
+    loss = lambda q: (blocks.gated(act, *blocks.gated_pre(**q)) * dout).sum()  # noqa: E731
+    g, u = blocks.gated_pre(**p)
+    got = blocks.gated_grads(act, dout, p["x"], p["wg"], p["wu"], g, u)
+    for name in p:
+        num = np.zeros_like(p[name])
+        for i in np.ndindex(*p[name].shape):
+            hi, lo = ({**p, name: p[name].copy()} for _ in range(2))
+            hi[name][i] += 1e-6
+            lo[name][i] -= 1e-6
+            num[i] = (loss(hi) - loss(lo)) / 2e-6
+        # central differences: h^2 f''' / 6 + 2^-53 |f| / h, both below 1e-8 here
+        assert np.allclose(got["d" + name], num, rtol=1e-6, atol=1e-7), name
+
+
+@pytest.mark.parametrize("pairing", ["pairs", "halves"])
+def test_qk_gradients_against_differences(pairing):
+    r = rng(2)
+    rows, H, d, eps = 3, 2, 16, 1e-5
+    x, w, dy = r.normal(size=(rows, H, d)), r.normal(size=d), r.normal(size=(rows, H, d))
+    ang = r.uniform(-3, 3, size=(4, d // 2))
+    rot = dict(table=np.stack([np.cos(ang), np.sin(ang)], -1), pos=np.array([2, -1, 0]), pairing=pairing)
+    loss = lambda a, b: (blocks.qk_norm_rope(a, b, eps, **rot) * dy).sum()  # noqa: E731
+    dx, dw = blocks.qk_norm_rope_grads(dy, x, w, eps, **rot)
+    for v, got, f in ((x, dx, lambda t: loss(t, w)), (w, dw, lambda t: loss(x, t))):
+        num = np.zeros_like(v)
+        for i in np.ndindex(*v.shape):
+            hi, lo = v.copy(), v.copy()
+            hi[i] += 1e-6
+            lo[i] -= 1e-6
+            num[i] = (f(hi) - f(lo)) / 2e-6
+        assert np.allclose(got, num, rtol=1e-6, atol=1e-7)
+
+
+def test_rotation_by_complex_numbers():
+    r = rng(3)
+    x, ang = r.normal(size=(5, 3, 8)), r.uniform(-9, 9, size=(5, 4))
+    t = np.stack([np.cos(ang), np.sin(ang)], -1)
+    z = np.exp(1j * ang)[:, None]
+    pairs = blocks.rotate(x, t, np.arange(5), "pairs")
+    halves = blocks.rotate(x, t, np.arange(5), "halves")
+    assert np.allclose(pairs[..., 0::2] + 1j * pairs[..., 1::2], (x[..., 0::2] + 1j * x[..., 1::2]) * z)
+    assert np.allclose(halves[..., :4] + 1j * halves[..., 4:], (x[..., :4] + 1j * x[..., 4:]) * z)
+    assert np.allclose(blocks.rotate(pairs, t, np.arange(5), "pairs", inverse=True), x)
+
+
+def test_quantising_by_whole_number_arithmetic():
+    """Against fractions: every q is the nearest, and even where two are equally near."""
+    from fractions import Fraction
+    x = np.array([[127.0, 0.5, 1.5, 2.5, -0.5, -1.5, -126.5, 126.5], [3.0, 1.0, -2.0, 0.1, 0, 0, 0, 1e-30]])
+    q, s = blocks.quant_rows(x)
+    assert s[0] == 1 and list(q[0]) == [127, 0, 2, 2, 0, -2, -126, 126]
+    for row, qs, sc in zip(x, q, s):
+        for v, n in zip(row, qs):
+            f = Fraction(float(v)) / Fraction(float(sc))
+            assert abs(f - int(n)) < Fraction(1, 2) or (abs(f - int(n)) == Fraction(1, 2) and n % 2 == 0)
+    q, s = blocks.quant_rows(np.array([[0.0, 0.0], [np.nan, 1.0], [np.inf, 1.0]]))
+    assert s[0] == np.float32(2.0 ** -126) and np.isnan(s[1:]).all() and not q.any()
+
+
+# ------------------------------------------------------------------ refusals of the C entry points
+
+def call(name, spec, **change):
+    """Status of the call with the spec's arguments, some changed."""
+    args = dict(spec)
+    assert set(change) <= set(args), change
+    args.update(change)
+    return getattr(t2i.load(), name)(*args.values())
+
+
+def check_refusals(name, spec, cases):
+    for change, status in cases:
+        assert call(name, spec, **change) == status, (name, change)
+        assert t2i.load().t2i_ops_last_error(), (name, change)
+
+
+QUANT = dict(dtype=BF16, rows=3, K=130, x=P, ldx=130, q=P, ldq=256, scale=P, stream=None)
+
+
+def test_quant_rows_refuses():
+    check_refusals("t2i_op_quant_rows", QUANT, [
+        (dict(dtype=2), INVALID), (dict(rows=0), SHAPE), (dict(rows=-1), SHAPE), (dict(K=0), SHAPE),
+        (dict(x=None), INVALID), (dict(q=None), INVALID), (dict(scale=None), INVALID),
+        (dict(ldx=129), SHAPE), (dict(ldq=240), SHAPE), (dict(ldq=264), SHAPE),
+        (dict(x=P + 1), INVALID), (dict(dtype=F32, x=P + 2), INVALID), (dict(q=P + 8), INVALID),
+        (dict(scale=P + 2), INVALID)])
+
+
+I8 = dict(dtype=BF16, epilogue=0, M=3, N=5, K=130, A=P, lda=256, a_scale=P, W=P, ldw=256, w_scale=P,
+          bias=None, out=P, ldo=5, resid=None, ldr=5, resid_copy=None, gate=None, stream=None)
+
+
+def test_linear_i8_refuses():
+    res = dict(epilogue=_lib.T2I_EPI_RESID, out=None, resid=P)
+    gated = dict(res, epilogue=_lib.T2I_EPI_RESID_GATED, gate=P)
+    check_refusals("t2i_op_linear_i8", I8, [
+        (dict(dtype=3), INVALID), (dict(epilogue=5), INVALID), (dict(epilogue=-1), INVALID),
+        (dict(M=0), SHAPE), (dict(N=0), SHAPE), (dict(K=0), SHAPE), (dict(K=131072), SHAPE),
+        (dict(M=2 ** 30, N=2 ** 30), SHAPE), (dict(A=None), INVALID), (dict(W=None), INVALID),
+        (dict(a_scale=None), INVALID), (dict(w_scale=None), INVALID), (dict(out=None), INVALID),
+        (dict(lda=240), SHAPE), (dict(lda=264), SHAPE), (dict(ldw=130), SHAPE), (dict(ldo=4), INVALID),
+        (dict(A=P + 8), INVALID), (dict(W=P + 1), INVALID), (dict(a_scale=P + 1), INVALID),
+        (dict(w_scale=P + 2), INVALID), (dict(bias=P + 1), INVALID), (dict(out=P + 1), INVALID),
+        (dict(res, resid=None), INVALID), (dict(res, ldr=4), INVALID), (dict(res, resid=P + 2), INVALID),
+        (dict(res, resid_copy=P + 1), INVALID), (dict(gated, gate=None), INVALID),
+        (dict(gated, gate=P + 2), INVALID)])
+
+
+GATED = dict(dtype=BF16, act=_lib.T2I_EPI_SILU, M=3, F=8, K=16, A=P, lda=16, Wg=P, Wu=P, ldw=16, bg=None,
+             bu=None, out=P, ldo=8, pre=None, ldp=16, stream=None)
+
+
+def test_gated_linear_refuses():
+    check_refusals("t2i_op_gated_linear", GATED, [
+        (dict(dtype=2), INVALID), (dict(act=0), INVALID), (dict(act=3), INVALID), (dict(M=0), SHAPE),
+        (dict(F=0), SHAPE), (dict(K=0), SHAPE), (dict(F=2 ** 29), SHAPE), (dict(A=None), INVALID),
+        (dict(Wg=None), INVALID), (dict(Wu=None), INVALID), (dict(out=None), INVALID),
+        (dict(bg=P), INVALID), (dict(bu=P), INVALID), (dict(lda=8), SHAPE), (dict(ldw=8), SHAPE),
+        (dict(ldo=0), SHAPE), (dict(pre=P, ldp=8), SHAPE), (dict(F=12, ldo=16), SHAPE),
+        (dict(K=12), SHAPE), (dict(lda=20), SHAPE), (dict(ldw=20), SHAPE), (dict(ldo=12), SHAPE),
+        (dict(pre=P, ldp=20), SHAPE), (dict(A=P + 8), INVALID), (dict(Wg=P + 8), INVALID),
+        (dict(Wu=P + 8), INVALID), (dict(out=P + 8), INVALID), (dict(pre=P + 8), INVALID),
+        (dict(bg=P + 8, bu=P), INVALID), (dict(dtype=F32, A=P + 2), INVALID)])
+
+
+GBWD = dict(dtype=BF16, act=_lib.T2I_EPI_SILU, M=3, F=8, K=16, A=P, lda=16, Wg=P, Wu=P, ldw=16, pre=P,
+            ldp=16, dout=P, ldd=8, dA=P, ldda=16, dWg=P, dWu=P, lddw=16, dbg=P, dbu=P, ws=P,
+            ws_bytes=1 << 20, stream=None)
+
+
+def test_gated_linear_backward_refuses():
+    need = t2i.load().t2i_op_gated_linear_backward_ws_bytes(BF16, 3, 8)
+    assert 0 < need <= 1 << 20
+    check_refusals("t2i_op_gated_linear_backward", GBWD, [
+        (dict(dtype=2), INVALID), (dict(act=4), INVALID), (dict(M=0), SHAPE), (dict(F=0), SHAPE),
+        (dict(K=0), SHAPE), (dict(A=None), INVALID), (dict(Wg=None), INVALID), (dict(Wu=None), INVALID),
+        (dict(pre=None), INVALID), (dict(dout=None), INVALID), (dict(ws=None), INVALID),
+        (dict(dbg=None), INVALID), (dict(dbu=None), INVALID),
+        (dict(dA=None, dWg=None, dWu=None, dbg=None, dbu=None), INVALID),
+        (dict(lda=8), SHAPE), (dict(ldw=8), SHAPE), (dict(ldp=8), SHAPE), (dict(ldd=0), SHAPE),
+        (dict(ldda=8), SHAPE), (dict(lddw=8), SHAPE), (dict(K=12), SHAPE), (dict(F=4), SHAPE),
+        (dict(ldda=20), SHAPE), (dict(lddw=20), SHAPE), (dict(ldd=12), SHAPE), (dict(dA=P + 8), INVALID),
+        (dict(dWg=P + 8), INVALID), (dict(dWu=P + 8), INVALID), (dict(dbg=P + 8), INVALID),
+        (dict(ws=P + 128), INVALID), (dict(ws_bytes=need - 1), WORKSPACE)])
+    ws = t2i.load().t2i_op_gated_linear_backward_ws_bytes
+    assert ws(2, 3, 8) == 0 and ws(BF16, 0, 8) == 0 and ws(BF16, 3, 0) == 0
+
+
+QK = dict(dtype=BF16, rows=3, heads_q=2, heads_k=1, head_dim=16, q=P, ldq=32, k=P, ldk=16, wq=None, wk=None,
+          eps=1e-6, pairing=0, table=P, n_pos=3, pos=None, q_out=P, ldqo=32, k_out=P, ldko=16, stream=None)
+QK_BAD = [
+    (dict(dtype=2), INVALID), (dict(pairing=2), INVALID), (dict(rows=0), SHAPE),
+    (dict(heads_q=0, heads_k=0), SHAPE), (dict(heads_q=-1), SHAPE), (dict(head_dim=12), SHAPE),
+    (dict(head_dim=264, ldq=528, ldk=264), SHAPE), (dict(head_dim=8, pairing=1), SHAPE),
+    (dict(rows=2 ** 30, pos=P), SHAPE), (dict(q=None), INVALID), (dict(k=None), INVALID),
+    (dict(ldq=24), SHAPE), (dict(ldk=8), SHAPE), (dict(ldq=36), SHAPE), (dict(q=P + 8), INVALID),
+    (dict(k=P + 8), INVALID), (dict(wq=P + 8), INVALID), (dict(wk=P + 2), INVALID),
+    (dict(table=P + 8), INVALID), (dict(pos=P + 2), INVALID), (dict(eps=-1e-6), INVALID),
+    (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID), (dict(n_pos=2), SHAPE),
+    (dict(n_pos=0, pos=P), SHAPE)]
+
+
+def test_qk_norm_rope_refuses():
+    check_refusals("t2i_op_qk_norm_rope", QK, QK_BAD + [
+        (dict(q_out=None), INVALID), (dict(k_out=None), INVALID), (dict(ldqo=24), SHAPE),
+        (dict(ldko=20), SHAPE), (dict(q_out=P + 8), INVALID), (dict(k_out=P + 8), INVALID)])
+
+
+QKB = dict(dtype=BF16, rows=3, heads_q=2, heads_k=1, head_dim=16, dq=P, lddq=32, dk=P, lddk=16, q=P, ldq=32,
+           k=P, ldk=16, wq=None, wk=None, eps=1e-6, pairing=0, table=P, n_pos=3, pos=None, dq_in=P,
+           lddqi=32, dk_in=P, lddki=16, dwq=P, dwk=P, ws=P, ws_bytes=1 << 20, stream=None)
+
+
+def test_qk_norm_rope_backward_refuses():
+    need = t2i.load().t2i_op_qk_norm_rope_backward_ws_bytes(3, 2, 1, 16)
+    assert 0 < need <= 1 << 20
+    check_refusals("t2i_op_qk_norm_rope_backward", QKB, QK_BAD + [
+        (dict(dq=None), INVALID), (dict(dk=None), INVALID), (dict(lddq=24), SHAPE), (dict(lddk=20), SHAPE),
+        (dict(dq=P + 8), INVALID), (dict(dk=P + 8), INVALID), (dict(dq_in=None), INVALID),
+        (dict(lddki=8), SHAPE), (dict(dwq=P + 1), INVALID), (dict(ws=P + 64), INVALID),
+        (dict(ws=None), WORKSPACE), (dict(ws_bytes=need - 1), WORKSPACE)])
+    ws = t2i.load().t2i_op_qk_norm_rope_backward_ws_bytes
+    assert ws(0, 1, 1, 16) == 0 and ws(3, 0, 0, 16) == 0 and ws(3, 1, 1, 12) == 0 and ws(3, 1, 1, 264) == 0
+
+
+# ------------------------------------------------------------------ refusals of the Python calls
+
+def test_python_calls_refuse_host_tensors():
+    x, w = torch.zeros(4, 128), torch.zeros(8, 128)
+    q = torch.zeros(4, 128, dtype=torch.int8)
+    h = torch.zeros(4, 2, 64)
+    for f in (lambda: t2i.quant_rows(x), lambda: t2i.linear_i8(q, x[:, 0], q, x[:, 0], K=128),
+              lambda: t2i.gated_linear(x, w, w), lambda: t2i.gated_linear_backward(x, x, w, w, x),
+              lambda: t2i.qk_norm_rope(h, h), lambda: t2i.qk_norm_rope_backward(h, h, h, h)):
+        with pytest.raises(t2i.T2IError) as e:
+            f()
+        assert e.value.status == INVALID
