@@ -185,8 +185,8 @@ t2i_status t2i_op_quant_rows(int32_t dtype, int32_t rows, int32_t K, const void*
  * The sum is exact (32-bit integers, K <= 131071); it is rounded once to fp32,
  * the rest is fp32.
  *   A [M, K], W [N, K] int8, 16-byte aligned, row strides lda, ldw multiples of
- *   16 and at least K rounded up to a multiple of 128: both are read up to
- *   there, and one of the two must hold zeros behind K (t2i_op_quant_rows
+ *   16, at least K rounded up to a multiple of 128 and at most 8 MiB: both are
+ *   read up to that multiple, and one of the two must hold zeros behind K (t2i_op_quant_rows
  *   writes them).  dtype is the type of bias [N] (or NULL: none) and out; the
  *   remaining arguments are those of t2i_op_linear.
  */
@@ -205,16 +205,17 @@ t2i_status t2i_op_linear_i8(int32_t dtype, int32_t epilogue, int32_t M, int32_t 
  *   one [2F, K] matrix: Wu = Wg + F ldw), bg and bu [F] (both or neither),
  *   out [M, F] (stride ldo), all of dtype; sums, activation and product in
  *   fp32, one rounding.
- *   pre [M, 2F] (stride ldp) or NULL: receives g | u rounded to dtype, which
- *   t2i_op_gated_linear_backward reads.
- *   bf16: F, K and the strides % 8 == 0, every pointer 16-byte aligned.
- *   fp32: any sizes.
+ *   pre [M, 2F] fp32 (stride ldp) or NULL: receives g | u, which
+ *   t2i_op_gated_linear_backward reads (fp32 for bf16 operands too: rounded to
+ *   bf16 they would add a quarter to the gradients' error).
+ *   bf16: F, K and the strides % 8 == 0 (ldp % 4), every pointer 16-byte
+ *   aligned, rows of A, Wg and Wu at most 8 MiB apart.  fp32: any sizes.
  * No output may overlap an input.
  */
 t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,
                                const void* A, int32_t lda, const void* Wg, const void* Wu,
                                int32_t ldw, const void* bg, const void* bu, void* out,
-                               int32_t ldo, void* pre, int32_t ldp, void* stream);
+                               int32_t ldo, float* pre, int32_t ldp, void* stream);
 
 /*
  * Gradients of t2i_op_gated_linear: with dout [M, F] (stride ldd) the gradient
@@ -225,7 +226,8 @@ t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F,
  * all of dtype.  dg and du are rounded to dtype once, for the products (the
  * bias sums take them unrounded); products and sums are fp32.  dA (stride
  * ldda), dWg, dWu (common stride lddw) may each be NULL: not computed; dbg and
- * dbu both or neither.  Sizes, strides and alignment as in the forward pass.
+ * dbu both or neither.  Sizes, strides and alignment as in the forward pass
+ * (bf16: F up to 2^20).
  * ws: device workspace of ws_bytes >= t2i_op_gated_linear_backward_ws_bytes,
  * 256-byte aligned, used by this call until it has finished on the stream;
  * the result does not depend on what it holds.  No output may overlap an
@@ -234,7 +236,7 @@ t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F,
 size_t t2i_op_gated_linear_backward_ws_bytes(int32_t dtype, int32_t M, int32_t F);
 t2i_status t2i_op_gated_linear_backward(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,
                                         const void* A, int32_t lda, const void* Wg, const void* Wu,
-                                        int32_t ldw, const void* pre, int32_t ldp, const void* dout,
+                                        int32_t ldw, const float* pre, int32_t ldp, const void* dout,
                                         int32_t ldd, void* dA, int32_t ldda, void* dWg, void* dWu,
                                         int32_t lddw, void* dbg, void* dbu, void* ws,
                                         size_t ws_bytes, void* stream);

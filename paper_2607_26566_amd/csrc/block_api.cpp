@@ -14,6 +14,8 @@ bool off(const void* p, size_t n) { return (uintptr_t)p % n != 0; }
 bool too_large(int32_t M, int32_t N) {
   return ((int64_t)M / 16 + 1) * ((int64_t)N / 16 + 1) > 0x7fffffff || M > (1 << 30) || N > (1 << 30);
 }
+// the kernels address up to 256 rows of an operand with 32-bit byte offsets
+bool far_rows(int32_t ld, size_t elem) { return (int64_t)ld * (int64_t)elem * 256 > 0x7fffffff; }
 t2i_status done(hipError_t e) {
   return e == hipSuccess ? T2I_OK : ops_fail(T2I_ERR_DEVICE, hipGetErrorString(e));
 }
@@ -105,6 +107,7 @@ t2i_status t2i_op_linear_i8(int32_t dtype, int32_t epilogue, int32_t M, int32_t 
   if (!A || !W || !a_scale || !w_scale) return ops_fail(T2I_ERR_INVALID_ARG, "NULL operand");
   if (lda < i8_row(K) || ldw < i8_row(K) || lda % 16 || ldw % 16)
     return ops_fail(T2I_ERR_SHAPE, "lda, ldw must be multiples of 16, at least K rounded up to 128");
+  if (far_rows(lda, 1) || far_rows(ldw, 1)) return ops_fail(T2I_ERR_SHAPE, "rows more than 8 MiB apart");
   const bool res = epilogue >= T2I_EPI_RESID;
   if (res && (!resid || ldr < N)) return ops_fail(T2I_ERR_INVALID_ARG, "bad residual");
   if (!res && (!out || ldo < N)) return ops_fail(T2I_ERR_INVALID_ARG, "bad out");
@@ -133,7 +136,7 @@ t2i_status t2i_op_linear_i8(int32_t dtype, int32_t epilogue, int32_t M, int32_t 
 t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,
                                const void* A, int32_t lda, const void* Wg, const void* Wu,
                                int32_t ldw, const void* bg, const void* bu, void* out, int32_t ldo,
-                               void* pre, int32_t ldp, void* stream) {
+                               float* pre, int32_t ldp, void* stream) {
   if (bad_dtype(dtype)) return ops_fail(T2I_ERR_INVALID_ARG, "bad dtype");
   if (act != T2I_EPI_GELU && act != T2I_EPI_SILU)
     return ops_fail(T2I_ERR_INVALID_ARG, "act must be T2I_EPI_GELU or T2I_EPI_SILU");
@@ -144,8 +147,9 @@ t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F,
   if (lda < K || ldw < K || ldo < F || (pre && ldp < 2 * F))
     return ops_fail(T2I_ERR_SHAPE, "bad leading dimension");
   const bool bf = dtype == T2I_BF16;
-  if (bf && (F % 8 || K % 8 || lda % 8 || ldw % 8 || ldo % 8 || (pre && ldp % 8)))
-    return ops_fail(T2I_ERR_SHAPE, "bf16 needs F, K and strides % 8 == 0");
+  if (bf && (F % 8 || K % 8 || lda % 8 || ldw % 8 || ldo % 8 || (pre && ldp % 4)))
+    return ops_fail(T2I_ERR_SHAPE, "bf16 needs F, K and strides % 8 == 0 (pre: 4)");
+  if (bf && (far_rows(lda, 2) || far_rows(ldw, 2))) return ops_fail(T2I_ERR_SHAPE, "rows more than 8 MiB apart");
   const size_t al = bf ? 16 : 4;
   if (off(A, al) || off(Wg, al) || off(Wu, al) || off(bg, al) || off(bu, al) || off(out, al) || off(pre, al))
     return ops_fail(T2I_ERR_INVALID_ARG, "pointers need 16-byte (bf16) or 4-byte (fp32) alignment");
@@ -173,7 +177,7 @@ size_t t2i_op_gated_linear_backward_ws_bytes(int32_t dtype, int32_t M, int32_t F
 
 t2i_status t2i_op_gated_linear_backward(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,
                                         const void* A, int32_t lda, const void* Wg, const void* Wu,
-                                        int32_t ldw, const void* pre, int32_t ldp, const void* dout,
+                                        int32_t ldw, const float* pre, int32_t ldp, const void* dout,
                                         int32_t ldd, void* dA, int32_t ldda, void* dWg, void* dWu,
                                         int32_t lddw, void* dbg, void* dbu, void* ws, size_t ws_bytes,
                                         void* stream) {
@@ -190,9 +194,11 @@ t2i_status t2i_op_gated_linear_backward(int32_t dtype, int32_t act, int32_t M, i
   if (lda < K || ldw < K || ldp < 2 * F || ldd < F || (dA && ldda < K) || (dw && lddw < K))
     return ops_fail(T2I_ERR_SHAPE, "bad leading dimension");
   const bool bf = dtype == T2I_BF16;
-  if (bf && (F % 8 || K % 8 || lda % 8 || ldw % 8 || ldp % 8 || ldd % 8 || (dA && ldda % 8) ||
+  if (bf && (F % 8 || K % 8 || lda % 8 || ldw % 8 || ldp % 4 || ldd % 8 || (dA && ldda % 8) ||
              (dw && lddw % 8)))
-    return ops_fail(T2I_ERR_SHAPE, "bf16 needs F, K and strides % 8 == 0");
+    return ops_fail(T2I_ERR_SHAPE, "bf16 needs F, K and strides % 8 == 0 (pre: 4)");
+  if (bf && (far_rows(lda, 2) || far_rows(ldw, 2) || far_rows(gated_cols(F), 4)))
+    return ops_fail(T2I_ERR_SHAPE, "rows more than 8 MiB apart");
   const size_t al = bf ? 16 : 4;
   if (off(A, al) || off(Wg, al) || off(Wu, al) || off(pre, al) || off(dout, al) || off(dA, al) ||
       off(dWg, al) || off(dWu, al) || off(dbg, al) || off(dbu, al) || off(ws, 256))

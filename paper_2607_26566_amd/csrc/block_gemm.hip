@@ -1,56 +1,55 @@
 // Matrix products of the block operators: the 8-bit linear layer, the gated
-// feed-forward and its gradients.
+// feed-forward and its gradients.  bf16 and 8-bit operands go through the tiles
+// of gemm_tile.h, fp32 ones through gemm_f32_tile_kernel:
 //
-// gemm_tile_kernel: one product C[m][n] = sum_k a(m, k) b(n, k) on 64 x 64
+// One product C[m][n] = sum_k a(m, k) b(n, k) on 64 x 64
 // tiles by 4 waves of 32 x 32 (v_mfma_f32_16x16x4_f32), 32 values of k at a
 // time through LDS, the next step's operands fetched into registers under
 // this step's MFMAs.  The operands are read by element through two functors,
 // so any stride and size goes.
-#include "block_ops.h"
+#include "gemm_tile.h"
 
 namespace t2i {
 
 // Elements of a row-major matrix, 0 outside [0, rows) x [0, cols).
 // ALONG: the k axis runs along the rows (contiguous in memory).
-template <typename T, bool ALONG>
+template <bool ALONG>
 struct Mat {
   static constexpr bool along = ALONG;
-  const T* p;
+  const float* p;
   int ld, rows, cols;
   __device__ __forceinline__ float at(int r, int k) const {
     const int y = ALONG ? r : k, x = ALONG ? k : r;
-    return y < rows && x < cols ? (float)p[(size_t)y * ld + x] : 0.f;
+    return y < rows && x < cols ? p[(size_t)y * ld + x] : 0.f;
   }
 };
 
 // Gate and up weights side by side: of every 32 rows, 16 of the gate and the
 // same 16 of the up projection, so that one lane ends up with both
-template <typename T>
 struct GateUp {
   static constexpr bool along = true;
-  const T *g, *u;
+  const float *g, *u;
   int ld, rows, cols;
   __device__ __forceinline__ float at(int r, int k) const {
     const int f = r / 32 * 16 + r % 16;
-    return f < rows && k < cols ? (float)((r & 16) ? u : g)[(size_t)f * ld + k] : 0.f;
+    return f < rows && k < cols ? ((r & 16) ? u : g)[(size_t)f * ld + k] : 0.f;
   }
 };
 
 // The gradients' operand [dg | du]^T... as rows of the contraction over both
 // halves: k < Fp the gate's row k, else the up projection's row k - Fp
-template <typename T>
 struct TwoRows {
   static constexpr bool along = false;
-  const T *g, *u;
+  const float *g, *u;
   int ld, rows, cols, half;
   __device__ __forceinline__ float at(int n, int k) const {
     const int f = k < half ? k : k - half;
-    return f < rows && n < cols ? (float)(k < half ? g : u)[(size_t)f * ld + n] : 0.f;
+    return f < rows && n < cols ? (k < half ? g : u)[(size_t)f * ld + n] : 0.f;
   }
 };
 
-template <bool INT, class LA, class LB, class EP>
-__global__ __launch_bounds__(256) void gemm_tile_kernel(LA la, LB lb, EP ep, int tiles_n, int K) {
+template <class LA, class LB, class EP>
+__global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep, int tiles_n, int K) {
   constexpr int BK = 32, LD = 65;
   __shared__ float sA[BK][LD], sB[BK][LD];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
@@ -66,15 +65,10 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(LA la, LB lb, EP ep, int
     }
   };
   f32x4 acc[2][2];
-  int iacc[2][2][4];
 #pragma unroll
   for (int i = 0; i < 2; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-      acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int r = 0; r < 4; ++r) iacc[i][j][r] = 0;
-    }
+    for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   fetch(0);
   for (int k0 = 0; k0 < K; k0 += BK) {
     __syncthreads();
@@ -100,18 +94,6 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(LA la, LB lb, EP ep, int
         for (int j = 0; j < 2; ++j)
           acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j], a[i], acc[i][j], 0, 0, 0);
     }
-    if (INT) {
-      // 32 products of 8-bit values: below 2^24, exact in fp32
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int j = 0; j < 2; ++j)
-#pragma unroll
-          for (int r = 0; r < 4; ++r) {
-            iacc[i][j][r] += (int)acc[i][j][r];
-            acc[i][j][r] = 0.f;
-          }
-    }
   }
   // operands swapped: a lane holds row m0 + fr, four columns from g * 4
 #pragma unroll
@@ -120,49 +102,22 @@ __global__ __launch_bounds__(256) void gemm_tile_kernel(LA la, LB lb, EP ep, int
     for (int r = 0; r < 4; ++r) {
       float v[2];
 #pragma unroll
-      for (int j = 0; j < 2; ++j) v[j] = INT ? (float)iacc[i][j][r] : acc[i][j][r];
+      for (int j = 0; j < 2; ++j) v[j] = acc[i][j][r];
       ep(m0 + wm * 32 + i * 16 + fr, n0 + wn * 32 + g * 4 + r, v);
     }
 }
 
-template <bool INT, class LA, class LB, class EP>
-static hipError_t gemm_tile(const LA& la, const LB& lb, const EP& ep, int M, int N, int K, hipStream_t st) {
+template <class LA, class LB, class EP>
+static hipError_t gemm_f32_tile(const LA& la, const LB& lb, const EP& ep, int M, int N, int K, hipStream_t st) {
   const int tn = (N + 63) / 64;
   const long tiles = (long)((M + 63) / 64) * tn;
-  hipLaunchKernelGGL((gemm_tile_kernel<INT, LA, LB, EP>), dim3((unsigned)tiles), dim3(256), 0, st, la, lb,
+  hipLaunchKernelGGL((gemm_f32_tile_kernel<LA, LB, EP>), dim3((unsigned)tiles), dim3(256), 0, st, la, lb,
                      ep, tn, K);
   return hipGetLastError();
 }
 
 // ---- epilogues: v[0] column n, v[1] column n + 16
 
-struct I8Store {
-  I8Epi e;
-  int M, N;
-  __device__ __forceinline__ void one(int m, int n, float acc) const {
-    if (m >= M || n >= N) return;
-    float y = acc * e.sa[m] * e.sw[n];
-    if (e.bias) y += e.bf16_out ? (float)((const bf16*)e.bias)[n] : ((const float*)e.bias)[n];
-    if (e.kind == EPI_GELU) y = gelu_tanh(y);
-    if (e.kind == EPI_SILU) y = silu(y);
-    if (e.kind >= EPI_RESID) {
-      const size_t i = (size_t)m * e.ldx + n;
-      const float x = e.x[i] + (e.kind == EPI_RESID_GATED ? e.gate[n] : 1.f) * y;
-      e.x[i] = x;
-      if (e.xb) e.xb[i] = (bf16)x;
-    } else if (e.bf16_out) {
-      ((bf16*)e.out)[(size_t)m * e.ldo + n] = (bf16)y;
-    } else {
-      ((float*)e.out)[(size_t)m * e.ldo + n] = y;
-    }
-  }
-  __device__ __forceinline__ void operator()(int m, int n, const float (&v)[2]) const {
-    one(m, n, v[0]);
-    one(m, n + 16, v[1]);
-  }
-};
-
-template <typename T>
 struct GatedStore {
   GatedFwd a;
   int M, F;
@@ -170,78 +125,371 @@ struct GatedStore {
     const int f = n / 32 * 16 + n % 16;
     if (m >= M || f >= F) return;
     float g = v[0], u = v[1];
-    if (a.bg) g += to_f32(((const T*)a.bg)[f]), u += to_f32(((const T*)a.bu)[f]);
+    if (a.bg) g += ((const float*)a.bg)[f], u += ((const float*)a.bu)[f];
     if (a.pre) {
-      T* p = (T*)a.pre + (size_t)m * a.ldp + f;
-      p[0] = from_f32<T>(g);
-      p[F] = from_f32<T>(u);
+      float* p = a.pre + (size_t)m * a.ldp + f;
+      p[0] = g;
+      p[F] = u;
     }
-    ((T*)a.out)[(size_t)m * a.ldo + f] = from_f32<T>((a.act == EPI_GELU ? gelu_tanh(g) : silu(g)) * u);
+    ((float*)a.out)[(size_t)m * a.ldo + f] = (a.act == EPI_GELU ? gelu_tanh(g) : silu(g)) * u;
   }
 };
 
-template <typename T>
 struct PlainStore {
-  T* p;
+  float* p;
   int ld, rows, cols;
   __device__ __forceinline__ void operator()(int m, int n, const float (&v)[2]) const {
     if (m >= rows) return;
-    if (n < cols) p[(size_t)m * ld + n] = from_f32<T>(v[0]);
-    if (n + 16 < cols) p[(size_t)m * ld + n + 16] = from_f32<T>(v[1]);
+    if (n < cols) p[(size_t)m * ld + n] = v[0];
+    if (n + 16 < cols) p[(size_t)m * ld + n + 16] = v[1];
   }
 };
 
-hipError_t launch_linear_i8(const int8_t* A, int lda, const int8_t* W, int ldw, int M, int N, int K,
-                            const I8Epi& e, hipStream_t st) {
-  return gemm_tile<true>(Mat<int8_t, true>{A, lda, M, K}, Mat<int8_t, true>{W, ldw, N, K}, I8Store{e, M, N},
-                         M, N, K, st);
+// ---------------------------------------------------------------------------
+// bf16 and 8-bit products on the tiles of gemm_tile.h.
+
+// rows of fp32 values that the epilogue needs, fetched into registers before the
+// main loop (older than its loads, whose waits count younger ones) and put into
+// LDS behind the ring after it: the epilogue's stores then wait for no load
+template <int N, int THREADS, class F>
+struct Staged {
+  static constexpr int PER = (N + THREADS - 1) / THREADS;
+  float v[PER];
+  __device__ __forceinline__ void fetch(const F& f) {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int x = (int)threadIdx.x + i * THREADS;
+      v[i] = x < N ? f(x) : 0.f;
+    }
+  }
+  __device__ __forceinline__ void put(float* lds) const {
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int x = (int)threadIdx.x + i * THREADS;
+      if (x < N) lds[x] = v[i];
+    }
+  }
+};
+
+// four consecutive values of a row, to memory as T
+template <typename T>
+__device__ __forceinline__ void store4(T* p, int left, bool vec, const float (&v)[4]) {
+  if (vec && left >= 4) {
+    if constexpr (sizeof(T) == 2) *(bf16x4*)p = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
+    else *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+      if (r < left) p[r] = from_f32<T>(v[r]);
+  }
 }
 
-template <typename T>
-static hipError_t gated_fwd(const GatedFwd& a, int M, int F, int K, hipStream_t st) {
-  return gemm_tile<false>(Mat<T, true>{(const T*)a.A, a.lda, M, K},
-                          GateUp<T>{(const T*)a.Wg, (const T*)a.Wu, a.ldw, F, K}, GatedStore<T>{a, M, F}, M,
+template <class D, typename T, int KIND>
+__global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a, TileOperand b, TileShape s,
+                                                                  I8Epi e, int M, int N, int vec) {
+  using P = TileProduct<D, true, false, false, false, false>;
+  constexpr int THREADS = D::NW * 64, NE = D::BM + (KIND == EPI_RESID_GATED ? 3 : 2) * D::BN;
+  __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + NE * 4];
+  int tm, tn;
+  P::place(s, blockIdx.x, gridDim.x, tm, tn);
+  const int m0 = tm * D::BM, n0 = tn * D::BN;
+  auto value = [&](int x) -> float {
+    if (x < D::BM) return e.sa[min(m0 + x, M - 1)];
+    const int n = min(n0 + (x - D::BM) % D::BN, N - 1), which = (x - D::BM) / D::BN;
+    if (which == 0) return e.sw[n];
+    if (which == 1) return e.bias ? to_f32(((const T*)e.bias)[n]) : 0.f;
+    return e.gate[n];
+  };
+  Staged<NE, THREADS, decltype(value)> st;
+  st.fetch(value);
+  typename P::Acc acc[D::TM][D::TN];
+  P::run(smem, a, b, s, m0, n0, acc);
+  float* const ev = (float*)(smem + D::ST * D::STAGE);
+  st.put(ev);
+  tile_barrier();
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
+  const int mw = (wave / D::WGN) * D::WM, nw = (wave % D::WGN) * D::WN;
+#pragma unroll
+  for (int i = 0; i < D::TM; ++i) {
+    const int ml = mw + i * 16 + fr, m = m0 + ml;
+    if (m >= M) continue;
+    const float sa = ev[ml];
+#pragma unroll
+    for (int j = 0; j < D::TN; ++j) {
+      const int nl = nw + j * 16 + g * 4, n = n0 + nl, left = N - n;
+      if (left <= 0) continue;
+      const f32x4 sw = *(const f32x4*)(ev + D::BM + nl), bb = *(const f32x4*)(ev + D::BM + D::BN + nl);
+      float y[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        y[r] = fmaf((float)acc[i][j][r] * sa, sw[r], bb[r]);
+        if (KIND == EPI_GELU) y[r] = gelu_tanh(y[r]);
+        if (KIND == EPI_SILU) y[r] = silu(y[r]);
+      }
+      if constexpr (KIND >= EPI_RESID) {
+        float* x = e.x + (size_t)m * e.ldx + n;
+        f32x4 gt{1.f, 1.f, 1.f, 1.f};
+        if (KIND == EPI_RESID_GATED) gt = *(const f32x4*)(ev + D::BM + 2 * D::BN + nl);
+        float xv[4];
+        if (vec && left >= 4) {
+          const f32x4 x4 = *(const f32x4*)x;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) xv[r] = x4[r] + gt[r] * y[r];
+        } else {
+#pragma unroll
+          for (int r = 0; r < 4; ++r) xv[r] = r < left ? x[r] + gt[r] * y[r] : 0.f;
+        }
+        store4(x, left, vec, xv);
+        if (e.xb) store4(e.xb + (size_t)m * e.ldx + n, left, vec, xv);
+      } else {
+        store4((T*)e.out + (size_t)m * e.ldo + n, left, vec, y);
+      }
+    }
+  }
+}
+
+template <class D>
+__global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand a, TileOperand b, TileShape s,
+                                                                     GatedFwd p, int M, int F) {
+  using P = TileProduct<D, false, false, false, true, false>;
+  constexpr int THREADS = D::NW * 64, H = D::BN / 2, TH = D::TN / 2;
+  __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + D::BN * 4];
+  int tm, tn;
+  P::place(s, blockIdx.x, gridDim.x, tm, tn);
+  const int m0 = tm * D::BM, f0 = tn * H;
+  auto value = [&](int x) -> float {
+    if (!p.bg) return 0.f;
+    return (float)((const bf16*)(x < H ? p.bg : p.bu))[min(f0 + x % H, F - 1)];
+  };
+  Staged<D::BN, THREADS, decltype(value)> st;
+  st.fetch(value);
+  typename P::Acc acc[D::TM][D::TN];
+  P::run(smem, a, b, s, m0, f0, acc);
+  float* const ev = (float*)(smem + D::ST * D::STAGE);
+  st.put(ev);
+  tile_barrier();
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
+  const int mw = (wave / D::WGN) * D::WM, nw = (wave % D::WGN) * (D::WN / 2);
+#pragma unroll
+  for (int i = 0; i < D::TM; ++i) {
+    const int m = m0 + mw + i * 16 + fr;
+    if (m >= M) continue;
+#pragma unroll
+    for (int j = 0; j < TH; ++j) {
+      const int fl = nw + j * 16 + g * 4, f = f0 + fl;
+      if (f >= F) continue;   // (F % 8 == 0: four columns or none)
+      const f32x4 bg = *(const f32x4*)(ev + fl), bu = *(const f32x4*)(ev + H + fl);
+      float gv[4], uv[4], y[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        gv[r] = acc[i][j][r] + bg[r];
+        uv[r] = acc[i][j + TH][r] + bu[r];
+        y[r] = (p.act == EPI_GELU ? gelu_tanh(gv[r]) : silu(gv[r])) * uv[r];
+      }
+      if (p.pre) {
+        float* q = p.pre + (size_t)m * p.ldp + f;
+        store4(q, 4, true, gv);
+        store4(q + F, 4, true, uv);
+      }
+      store4((bf16*)p.out + (size_t)m * p.ldo + f, 4, true, y);
+    }
+  }
+}
+
+// the gradients' products: C stored as bf16 (row stride ldc).  b is a KR operand:
+// a pair of fragments holds 8 neighbouring columns of a row (N % 8 == 0)
+template <class D, class P>
+__device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D::TN], bf16* C, int ldc, int m0,
+                                           int n0, int M, int N) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
+  const int mw = m0 + (wave / D::WGN) * D::WM, nw = n0 + (wave % D::WGN) * D::WN;
+#pragma unroll
+  for (int i = 0; i < D::TM; ++i) {
+    const int m = mw + P::row_of(i, fr);
+    if (m >= M) continue;
+#pragma unroll
+    for (int j = 0; j < D::TN; j += 2) {
+      const int n = nw + P::col_of(j, g * 4);
+      if (n >= N) continue;
+      bf16x8 v;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[2 * r] = (bf16)acc[i][j][r], v[2 * r + 1] = (bf16)acc[i][j + 1][r];
+      *(bf16x8*)(C + (size_t)m * ldc + n) = v;
+    }
+  }
+}
+
+template <class D>
+__global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, TileOperand b, TileShape s,
+                                                                 bf16* dx, int ldx, int M, int K) {
+  using P = TileProduct<D, false, false, true, false, true>;
+  __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
+  int tm, tn;
+  P::place(s, blockIdx.x, gridDim.x, tm, tn);
+  typename P::Acc acc[D::TM][D::TN];
+  P::run(smem, a, b, s, tm * D::BM, tn * D::BN, acc);
+  store_tile<D, P>(acc, dx, ldx, tm * D::BM, tn * D::BN, M, K);
+}
+
+// row blocks [0, half) are dWg's, the others dWu's (their operand lies `shift`
+// bytes further); only one of the two wanted: both pointers and no shift
+template <class D>
+__global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, TileOperand b, TileShape s, int half,
+                                                                 int shift, bf16* dg, bf16* du, int ldw, int F, int K) {
+  using P = TileProduct<D, false, true, true, false, false>;
+  __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
+  int tm, tn;
+  P::place(s, blockIdx.x, gridDim.x, tm, tn);
+  const bool up = tm >= half;
+  const int m0 = (up ? tm - half : tm) * D::BM;
+  if (up) a.p += shift;
+  typename P::Acc acc[D::TM][D::TN];
+  P::run(smem, a, b, s, m0, tn * D::BN, acc);
+  store_tile<D, P>(acc, up ? du : dg, ldw, m0, tn * D::BN, F, K);
+}
+
+// ---- tile shapes.  The shape whose rounds of 256 workgroups cost least.
+struct TileChoice { int bm, bn, cost; };
+static int choose_tile(const TileChoice* c, int n, long rows, long cols) {
+  int best = 0;
+  double least = 0;
+  for (int i = 0; i < n; ++i) {
+    const long tiles = ((rows + c[i].bm - 1) / c[i].bm) * ((cols + c[i].bn - 1) / c[i].bn);
+    const double cost = (double)((tiles + 255) / 256) * c[i].cost;
+    if (i == 0 || cost < least) least = cost, best = i;
+  }
+  return best;
+}
+using Tile256 = TileDims<256, 256, 2, 4, 2>;
+using Tile128 = TileDims<128, 128, 2, 4, 4>;
+using Tile64 = TileDims<64, 128, 2, 4, 4>;
+using Tile32 = TileDims<32, 128, 1, 4, 4>;
+constexpr TileChoice kTiles[] = {{256, 256, 100}, {128, 128, 32}, {64, 128, 20}, {32, 128, 15}};
+
+template <class D>
+static TileShape tile_shape(int rows, int cols, int steps, int kbytes, int half) {
+  TileShape s;
+  s.tiles_m = (rows + D::BM - 1) / D::BM;
+  s.tiles_n = (cols + D::BN - 1) / D::BN;
+  s.group_m = 8;
+  s.steps = steps;
+  s.kbytes = kbytes;
+  s.half = half;
+  return s;
+}
+
+template <class D>
+static void i8_launch(const TileOperand& a, const TileOperand& b, const I8Epi& e, int M, int N, int K, hipStream_t st) {
+  const TileShape s = tile_shape<D>(M, N, i8_row(K) / 128, i8_row(K), 0);
+  const dim3 grid((unsigned)(s.tiles_m * s.tiles_n));
+  const bool res = e.kind >= EPI_RESID;
+  const size_t align = res ? (size_t)e.x | (size_t)(e.ldx * 4) : (size_t)e.out | (size_t)(e.ldo * (e.bf16_out ? 2 : 4));
+  const int vec = align % (res || !e.bf16_out ? 16 : 8) == 0 && (size_t)e.xb % 8 == 0;
+#define T2I_I8(T, KIND)                                                                                       \
+  hipLaunchKernelGGL((linear_i8_kernel<D, T, KIND>), grid, dim3(D::NW * 64), 0, st, a, b, s, e, M, N, vec)
+#define T2I_I8K(T)                                     \
+  switch (e.kind) {                                    \
+    case EPI_STORE: T2I_I8(T, EPI_STORE); break;       \
+    case EPI_GELU: T2I_I8(T, EPI_GELU); break;         \
+    case EPI_SILU: T2I_I8(T, EPI_SILU); break;         \
+    case EPI_RESID: T2I_I8(T, EPI_RESID); break;       \
+    default: T2I_I8(T, EPI_RESID_GATED); break;        \
+  }
+  if (e.bf16_out) T2I_I8K(bf16) else T2I_I8K(float)
+#undef T2I_I8K
+#undef T2I_I8
+}
+
+#define T2I_TILES(rows, cols, CALL)                              \
+  switch (choose_tile(kTiles, 4, rows, cols)) {                  \
+    case 0: { using D = Tile256; CALL; break; }                  \
+    case 1: { using D = Tile128; CALL; break; }                  \
+    case 2: { using D = Tile64; CALL; break; }                   \
+    default: { using D = Tile32; CALL; break; }                  \
+  }
+
+hipError_t launch_linear_i8(const int8_t* A, int lda, const int8_t* W, int ldw, int M, int N, int K,
+                            const I8Epi& e, hipStream_t st) {
+  const TileOperand a{(const char*)A, nullptr, (uint32_t)lda, M, 0}, b{(const char*)W, nullptr, (uint32_t)ldw, N, 0};
+  T2I_TILES(M, N, i8_launch<D>(a, b, e, M, N, K, st))
+  return hipGetLastError();
+}
+
+static hipError_t gated_fwd_bf16(const GatedFwd& p, int M, int F, int K, hipStream_t st) {
+  const TileOperand a{(const char*)p.A, nullptr, 2u * p.lda, M, 0},
+      b{(const char*)p.Wg, (const char*)p.Wu, 2u * p.ldw, F, 0};
+  T2I_TILES(M, 2L * F, const TileShape s = tile_shape<D>(M, 2 * F, (K + 63) / 64, 2 * K, 0);
+            hipLaunchKernelGGL((gated_linear_kernel<D>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64),
+                               0, st, a, b, s, p, M, F))
+  return hipGetLastError();
+}
+
+static hipError_t gated_dx_bf16(int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw,
+                                void* dx, int ldx, hipStream_t st) {
+  const int Fp = gated_cols(F);
+  const TileOperand a{(const char*)dgu, nullptr, 4u * Fp, M, 0},
+      b{(const char*)Wg, (const char*)Wu, 2u * ldw, F, K};
+  T2I_TILES(M, K, const TileShape s = tile_shape<D>(M, K, 2 * Fp / 64, 4 * Fp, Fp / 64);
+            hipLaunchKernelGGL((gated_dx_kernel<D>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64), 0, st,
+                               a, b, s, (bf16*)dx, ldx, M, K))
+  return hipGetLastError();
+}
+
+static hipError_t gated_dw_bf16(int M, int F, int K, const void* dgu, const void* A, int lda, void* dWg, void* dWu,
+                                int lddw, hipStream_t st) {
+  const int Fp = gated_cols(F);
+  const int n = dWg && dWu ? 2 : 1;
+  const TileOperand a{(const char*)dgu + (dWg ? 0 : 2 * (size_t)Fp), nullptr, 4u * Fp, M, F},
+      b{(const char*)A, nullptr, 2u * lda, M, K};
+  T2I_TILES((long)n * F, K, TileShape s = tile_shape<D>(F, K, (M + 63) / 64, 0, 0); const int half = s.tiles_m;
+            s.tiles_m *= n;
+            hipLaunchKernelGGL((gated_dw_kernel<D>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64), 0, st,
+                               a, b, s, half, 2 * Fp, (bf16*)(dWg ? dWg : dWu), (bf16*)dWu, lddw, F, K))
+  return hipGetLastError();
+}
+
+static hipError_t gated_fwd_f32(const GatedFwd& a, int M, int F, int K, hipStream_t st) {
+  return gemm_f32_tile(Mat<true>{(const float*)a.A, a.lda, M, K},
+                          GateUp{(const float*)a.Wg, (const float*)a.Wu, a.ldw, F, K}, GatedStore{a, M, F}, M,
                           (F + 15) / 16 * 32, K, st);
 }
 
-template <typename T>
-static hipError_t gated_dx(int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw,
+static hipError_t gated_dx_f32(int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw,
                            void* dx, int ldx, hipStream_t st) {
   const int Fp = gated_cols(F);
-  return gemm_tile<false>(Mat<T, true>{(const T*)dgu, 2 * Fp, M, 2 * Fp},
-                          TwoRows<T>{(const T*)Wg, (const T*)Wu, ldw, F, K, Fp},
-                          PlainStore<T>{(T*)dx, ldx, M, K}, M, K, 2 * Fp, st);
+  return gemm_f32_tile(Mat<true>{(const float*)dgu, 2 * Fp, M, 2 * Fp},
+                          TwoRows{(const float*)Wg, (const float*)Wu, ldw, F, K, Fp},
+                          PlainStore{(float*)dx, ldx, M, K}, M, K, 2 * Fp, st);
 }
 
-template <typename T>
-static hipError_t gated_dw(int M, int F, int K, const void* dgu, const void* A, int lda, void* dWg,
+static hipError_t gated_dw_f32(int M, int F, int K, const void* dgu, const void* A, int lda, void* dWg,
                            void* dWu, int lddw, hipStream_t st) {
   const int Fp = gated_cols(F);
   for (int i = 0; i < 2; ++i) {
-    T* o = (T*)(i ? dWu : dWg);
+    float* o = (float*)(i ? dWu : dWg);
     if (!o) continue;
-    const hipError_t e = gemm_tile<false>(Mat<T, false>{(const T*)dgu + i * Fp, 2 * Fp, M, F},
-                                          Mat<T, false>{(const T*)A, lda, M, K},
-                                          PlainStore<T>{o, lddw, F, K}, F, K, M, st);
+    const hipError_t e = gemm_f32_tile(Mat<false>{(const float*)dgu + i * Fp, 2 * Fp, M, F},
+                                          Mat<false>{(const float*)A, lda, M, K},
+                                          PlainStore{o, lddw, F, K}, F, K, M, st);
     if (e != hipSuccess) return e;
   }
   return hipSuccess;
 }
 
 hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& a, int M, int F, int K, hipStream_t st) {
-  return is_bf16 ? gated_fwd<bf16>(a, M, F, K, st) : gated_fwd<float>(a, M, F, K, st);
+  return is_bf16 ? gated_fwd_bf16(a, M, F, K, st) : gated_fwd_f32(a, M, F, K, st);
 }
 
 hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, const void* Wg,
                            const void* Wu, int ldw, void* dx, int ldx, hipStream_t st) {
-  return is_bf16 ? gated_dx<bf16>(M, F, K, dgu, Wg, Wu, ldw, dx, ldx, st)
-                 : gated_dx<float>(M, F, K, dgu, Wg, Wu, ldw, dx, ldx, st);
+  return is_bf16 ? gated_dx_bf16(M, F, K, dgu, Wg, Wu, ldw, dx, ldx, st)
+                 : gated_dx_f32(M, F, K, dgu, Wg, Wu, ldw, dx, ldx, st);
 }
 
 hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, const void* A, int lda,
                            void* dWg, void* dWu, int lddw, hipStream_t st) {
-  return is_bf16 ? gated_dw<bf16>(M, F, K, dgu, A, lda, dWg, dWu, lddw, st)
-                 : gated_dw<float>(M, F, K, dgu, A, lda, dWg, dWu, lddw, st);
+  return is_bf16 ? gated_dw_bf16(M, F, K, dgu, A, lda, dWg, dWu, lddw, st)
+                 : gated_dw_f32(M, F, K, dgu, A, lda, dWg, dWu, lddw, st);
 }
 
 }  // namespace t2i

@@ -49,7 +49,7 @@ struct GatedFwd {
   int lda, ldw;
   void* out;
   int ldo;
-  void* pre;             // or NULL: [M, 2F] pre-activations g | u
+  float* pre;            // or NULL: [M, 2F] pre-activations g | u
   int ldp;
 };
 hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& a, int M, int F, int K, hipStream_t st);
@@ -57,7 +57,7 @@ hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& a, int M, int F, in
 // dgu [M][2 gated_cols(F)] and, when partial != NULL, the column sums of every
 // row block: partial [gate_row_blocks(M)][2 gated_cols(F)]
 int gate_row_blocks(int M);
-hipError_t launch_gate_grad(bool is_bf16, int act, int M, int F, const void* pre, int ldp,
+hipError_t launch_gate_grad(bool is_bf16, int act, int M, int F, const float* pre, int ldp,
                             const void* dout, int ldd, void* dgu, float* partial, hipStream_t st);
 // dbg[f] / dbu[f] = sum of the partials, in ascending block order
 hipError_t launch_gate_bias_grad(bool is_bf16, int M, int F, const float* partial, void* dbg,

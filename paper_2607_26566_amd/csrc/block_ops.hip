@@ -488,7 +488,7 @@ int gate_row_blocks(int M) { return (M + kGateRows - 1) / kGateRows; }
 // threads side by side, 8 rows at a time
 template <typename T, int V>
 __global__ __launch_bounds__(256) void gate_grad_kernel(int act, int M, int F, int Fp,
-                                                        const T* __restrict__ pre, int ldp,
+                                                        const float* __restrict__ pre, int ldp,
                                                         const T* __restrict__ dout, int ldd,
                                                         T* __restrict__ dgu, float* __restrict__ partial) {
   __shared__ float red[2][8][32 * V];
@@ -502,14 +502,14 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(int act, int M, int F, i
     for (int r = r0 + ty; r < min(r0 + kGateRows, M); r += 8) {
       float g[V], u[V], dh[V];
       if (f < F) {
-        const T* p = pre + (size_t)r * ldp + f;
+        const float* p = pre + (size_t)r * ldp + f;
         if constexpr (V == 8) {
           load8(p, g);
           load8(p + F, u);
           load8(dout + (size_t)r * ldd + f, dh);
         } else {
-          g[0] = to_f32(p[0]);
-          u[0] = to_f32(p[F]);
+          g[0] = p[0];
+          u[0] = p[F];
           dh[0] = to_f32(dout[(size_t)r * ldd + f]);
         }
 #pragma unroll
@@ -550,16 +550,16 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(int act, int M, int F, i
   }
 }
 
-hipError_t launch_gate_grad(bool is_bf16, int act, int M, int F, const void* pre, int ldp,
+hipError_t launch_gate_grad(bool is_bf16, int act, int M, int F, const float* pre, int ldp,
                             const void* dout, int ldd, void* dgu, float* partial, hipStream_t st) {
   const int Fp = gated_cols(F), per = is_bf16 ? 256 : 32;
   const dim3 grid((unsigned)gate_row_blocks(M), (unsigned)((Fp + per - 1) / per));
   if (is_bf16)
     hipLaunchKernelGGL((gate_grad_kernel<bf16, 8>), grid, dim3(256), 0, st, act, M, F, Fp,
-                       (const bf16*)pre, ldp, (const bf16*)dout, ldd, (bf16*)dgu, partial);
+                       pre, ldp, (const bf16*)dout, ldd, (bf16*)dgu, partial);
   else
     hipLaunchKernelGGL((gate_grad_kernel<float, 1>), grid, dim3(256), 0, st, act, M, F, Fp,
-                       (const float*)pre, ldp, (const float*)dout, ldd, (float*)dgu, partial);
+                       pre, ldp, (const float*)dout, ldd, (float*)dgu, partial);
   return hipGetLastError();
 }
 

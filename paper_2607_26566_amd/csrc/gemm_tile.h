@@ -1,0 +1,335 @@
+// Tile products of the block operators on the gfx950 matrix cores (bf16 and
+// 8-bit integers), fed by direct HBM -> LDS loads.
+//
+// A workgroup of WGM x WGN waves owns a BM x BN tile of C[m][n] = sum_k a(m, k)
+// b(n, k); a wave owns (BM / WGM) x (BN / WGN) of it in 16 x 16 MFMA tiles
+// (v_mfma_f32_16x16x32_bf16, v_mfma_i32_16x16x64_i8: both take 16 bytes per lane
+// and operand).  k advances by a step of 128 bytes of k per row (64 bf16, 128
+// 8-bit values) through a ring of ST LDS stages; 16 bytes per lane go straight
+// from global memory into LDS (no registers).
+//
+// Each operand lies in memory in one of two ways:
+//   k along the rows ("KC": weights [out, in], activations [rows, in]).  A stage
+//     holds 128 bytes of every tile row; the 16-byte piece c of row r sits in
+//     slot c ^ ((r >> 1) & 7), so the 16 rows of a fragment spread over all LDS
+//     banks.
+//   k across the rows ("KR": the operands of the gradients, contracted over
+//     tokens or over output features).  A stage holds 64 rows of the tile's
+//     columns.  A lane reads the same N neighbouring columns of its 8 rows k and
+//     joins the halves of the dwords by v_perm, which gives it 8 k of N columns,
+//     the operands of N MFMAs: fragment j of such a group has columns j, N + j,
+//     2 N + j ...  The 64-byte piece p of row k sits in piece p ^ f(k), f the bits
+//     of (k >> 3) & 3 swapped, so that the four rows of a read lie in different
+//     banks.  (ds_read_b64_tr_b16 would turn the block by itself, but the compiler
+//     lets such a read wait for every load into LDS that is on its way.)
+//
+// Loop over the steps (a step is two half-steps of one MFMA depth): the MFMAs of
+// half-step h run while the fragments of h + 1 are read -- the a fragments into
+// the other register set, each b fragment in place once its column is done --
+// and the workgroup meets once per step, a third of the way into half-step 1,
+// when every fragment of the stage is in registers; then the stage is refilled
+// and the next stage's fragments are read under the remaining columns.
+//
+// Sizes: rows behind the operand are read as its last row (KC) or as zeros (KR,
+// by the buffer resource's bound), k behind the end as zeros (by an offset
+// behind the resource); what they add up to is not stored.
+#pragma once
+
+#include <type_traits>
+
+#include "block_ops.h"
+
+namespace t2i {
+
+typedef int i32x4 __attribute__((ext_vector_type(4)));
+
+// s_waitcnt with only vmcnt constrained (low bits [3:0], high bits [15:14])
+template <int N>
+__device__ __forceinline__ void tile_vmcnt() {
+  static_assert(N >= 0 && N < 64, "vmcnt range");
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+}
+// at most `younger` load rounds of B instructions outstanding
+template <int B>
+__device__ __forceinline__ void tile_wait(int younger) {
+  switch (younger) {
+    case 0: tile_vmcnt<0>(); break;
+    case 1: tile_vmcnt<(B < 64 ? B : 0)>(); break;
+    case 2: tile_vmcnt<(2 * B < 64 ? 2 * B : 0)>(); break;
+    default: tile_vmcnt<(3 * B < 64 ? 3 * B : 0)>(); break;
+  }
+}
+// this wave's LDS accesses done, then the barrier; outstanding loads go on
+__device__ __forceinline__ void tile_barrier() {
+  __builtin_amdgcn_s_waitcnt(0xC07F);
+  asm volatile("s_barrier" ::: "memory");
+}
+
+// consecutive workgroups of one XCD (they are dealt out in turn over 8) get
+// consecutive tiles
+__device__ __forceinline__ int tile_of_block(int b, int nb) {
+  const int q = nb >> 3, r = nb & 7, x = b & 7, j = b >> 3;
+  return (x < r ? x * (q + 1) : r * (q + 1) + (x - r) * q) + j;
+}
+
+// One operand of a product.  `p` (and `p2`) in bytes.
+struct TileOperand {
+  const char* p;
+  const char* p2;    // second matrix (two: see TileProduct), else unused
+  uint32_t ld;       // bytes from row to row
+  int rows;          // KC: rows of the matrix; KR: rows of the contraction
+  int cols;          // KR: columns that may be read (a multiple of 8)
+};
+
+struct TileShape {
+  int tiles_m, tiles_n, group_m;
+  int steps;         // k steps in all
+  int kbytes;        // KC: bytes of a row that hold k
+  int half;          // steps in the first matrix of a two-matrix contraction
+};
+
+constexpr uint32_t kTileOff = 0x80000000u;   // behind every resource: reads as zero
+
+template <int BM_, int BN_, int WGM_, int WGN_, int ST_>
+struct TileDims {
+  static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, ST = ST_;
+  static constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16;
+  static constexpr int STAGE = (BM + BN) * 128;
+  static constexpr int LOADS = (BM + BN) / 8 / NW;   // load instructions per wave and step
+  static_assert((BM + BN) / 8 % NW == 0 && BM / 8 % NW == 0, "whole load rounds per operand");
+  static_assert(WM % 16 == 0 && WN % 16 == 0 && ST >= 2 && ST <= 5 && (ST - 1) * LOADS < 64, "tile shape");
+};
+
+// I8: 8-bit integers, else bf16.  AKR, BKR: operand layouts.  DUAL: b is two
+// matrices side by side, p for the first half of the tile's columns and p2 for the
+// second, so that a wave holds both of an output.  SEGS (BKR): the contraction
+// runs over p's rows, then p2's.
+template <class D, bool I8, bool AKR, bool BKR, bool DUAL, bool SEGS>
+struct TileProduct {
+  using Acc = typename std::conditional<I8, i32x4, f32x4>::type;
+  static constexpr int BM = D::BM, BN = D::BN, TM = D::TM, TN = D::TN, ST = D::ST;
+
+  // columns per group of a KR operand (see above): a's whole set, two of b's
+  static constexpr int NA = AKR ? TM : 1, NB = BKR ? 2 : 1;
+  static_assert(!AKR || TM == 2 || TM == 4 || TM == 8, "fragments per wave");
+  static_assert(!BKR || TN % 2 == 0, "fragments per wave");
+
+  // the (row, column) of a KR tile of W columns that lane `lane` of load block b fills
+  template <int W>
+  static __device__ __forceinline__ void kr_source(int b, int lane, int& row, int& col) {
+    constexpr int RB = W * 2, MASK = W >= 128 ? 3 : W / 32 - 1;
+    const int at = b * 1024 + lane * 16;
+    row = at / RB;
+    const int o = at % RB, f = (((row >> 2) & 2) | ((row >> 4) & 1)) & MASK;
+    col = ((o >> 6) ^ f) * 32 + (o & 63) / 2;
+  }
+
+  // tile row (column) that index x = 0 .. 15 of fragment i (j) of a wave stands for
+  static __device__ __forceinline__ int row_of(int i, int x) { return i / NA * NA * 16 + x * NA + i % NA; }
+  static __device__ __forceinline__ int col_of(int j, int x) { return j / NB * NB * 16 + x * NB + j % NB; }
+
+  // the tile product: acc[i][j][r] belongs to the wave's row row_of(i, lane & 15)
+  // and column col_of(j, 4 (lane >> 4) + r)
+  static __device__ __forceinline__ void run(char* smem, const TileOperand& a, const TileOperand& b,
+                                             const TileShape& s, int m0, int n0, Acc (&acc)[TM][TN]) {
+    const int tid = threadIdx.x, lane = tid & 63;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wm = wave / D::WGN, wn = wave % D::WGN, fr = lane & 15, g = lane >> 4;
+    constexpr int LA = BM / 8 / D::NW, LB = D::LOADS - LA;
+    const int KT = s.steps;
+
+    // ---- sources: this lane's offset of each load, the resource by operand
+    uint32_t src[D::LOADS];
+#pragma unroll
+    for (int i = 0; i < D::LOADS; ++i) {
+      const bool is_a = i < LA;
+      const int blk = wave + (is_a ? i : i - LA) * D::NW;
+      if (is_a ? AKR : BKR) {
+        int row, col;
+        if (is_a) kr_source<BM>(blk, lane, row, col);
+        else kr_source<BN>(blk, lane, row, col);
+        const TileOperand& o = is_a ? a : b;
+        src[i] = (uint32_t)row * o.ld + 2u * (uint32_t)min((is_a ? m0 : n0) + col, o.cols - 8);
+      } else {
+        const int lr = blk * 8 + (lane >> 3), c = (lane & 7) ^ ((lr >> 1) & 7);
+        const TileOperand& o = is_a ? a : b;
+        // rows from the tile's first, not behind the last (DUAL: within the half)
+        const int r0 = is_a ? m0 : n0;
+        const int rr = !is_a && DUAL && lr >= BN / 2 ? lr - BN / 2 : lr;
+        src[i] = (uint32_t)min(rr, o.rows - 1 - r0) * o.ld + c * 16;
+      }
+    }
+    const bool ragged_k = !I8 && s.kbytes % 128 != 0;   // KC: pieces of the last step lie behind k
+    // KC: rows at fixed offsets from the tile's first, k as the scalar offset.
+    // KR: the step's first row as the base, the resource ends with its last row.
+    auto kc_res = [](const char* p, size_t off) {
+      return __builtin_amdgcn_make_buffer_rsrc((void*)(p + off), 0, 0x7fffffff, 0x00020000);
+    };
+    auto kr_res = [&](const TileOperand& o, int t, bool segs) {
+      const bool second = segs && t >= s.half;
+      const int row0 = (second ? t - s.half : t) * 64;
+      return __builtin_amdgcn_make_buffer_rsrc((void*)((second ? o.p2 : o.p) + (size_t)row0 * o.ld), 0,
+                                               (min(o.rows - row0, 64) - 1) * (int)o.ld + 2 * o.cols, 0x00020000);
+    };
+    const __amdgpu_buffer_rsrc_t ra_kc = kc_res(a.p, AKR ? 0 : (size_t)m0 * a.ld);
+    const __amdgpu_buffer_rsrc_t rb_kc = kc_res(b.p, BKR ? 0 : (size_t)n0 * b.ld);
+    const __amdgpu_buffer_rsrc_t rb2_kc = kc_res(DUAL ? b.p2 : b.p, BKR ? 0 : (size_t)n0 * b.ld);
+    auto res_a = [&](int t) { return AKR ? kr_res(a, t, false) : ra_kc; };
+    auto res_b = [&](int t) { return BKR ? kr_res(b, t, SEGS) : rb_kc; };
+    auto issue = [&](int i, int t, uint32_t slot, const __amdgpu_buffer_rsrc_t& ra,
+                     const __amdgpu_buffer_rsrc_t& rb) {
+      const bool is_a = i < LA;
+      const int blk = wave + (is_a ? i : i - LA) * D::NW;
+      auto* dst = (__attribute__((address_space(3))) void*)(smem + slot + (is_a ? 0 : BM * 128) + blk * 1024);
+      if (is_a ? AKR : BKR) {
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? ra : rb, dst, 16, src[i], 0, 0, 0);
+      } else {
+        uint32_t v = src[i];
+        if (ragged_k && t == KT - 1) {
+          const int lr = blk * 8 + (lane >> 3), c = (lane & 7) ^ ((lr >> 1) & 7);
+          if (t * 128 + c * 16 >= s.kbytes) v = kTileOff;
+        }
+        const bool up = DUAL && !is_a && blk * 8 >= BN / 2;
+        __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? ra : up ? rb2_kc : rb, dst, 16, v, t * 128, 0, 0);
+      }
+    };
+
+    // ---- fragments
+    const uint32_t kc = fr * 128 + ((g ^ ((fr >> 1) & 7)) << 4);   // half-step 1: ^ 64
+    const int krf = ((g & 1) << 1) | (g >> 1);
+    auto read_kc = [&](bool is_a, uint32_t slot, int kk, int i) -> i32x4 {
+      int row = is_a ? wm * D::WM + i * 16 : wn * D::WN + i * 16;
+      if (!is_a && DUAL)
+        row = i < TN / 2 ? wn * (D::WN / 2) + i * 16 : BN / 2 + wn * (D::WN / 2) + (i - TN / 2) * 16;
+      return *(const i32x4*)(smem + slot + (is_a ? 0 : BM * 128) + row * 128 + (kc ^ (kk ? 64u : 0u)));
+    };
+    // N fragments of a KR tile of W columns from column c0 on, its rows from `base`
+    auto read_kr = [&](auto n, auto w, uint32_t base, int kk, int c0, i32x4* f) {
+      constexpr int N = decltype(n)::value, W = decltype(w)::value, MASK = W >= 128 ? 3 : W / 32 - 1;
+      typedef int raw_t __attribute__((ext_vector_type(N / 2 > 1 ? N / 2 : 2)));
+      const int o = (c0 + N * fr) * 2;
+      const char* at = smem + base + (kk * 32 + g * 8) * W * 2 + (((o >> 6) ^ (krf & MASK)) << 6) + (o & 63);
+      int raw[8][N / 2];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        if constexpr (N == 2) {
+          raw[k][0] = *(const int*)(at + k * W * 2);
+        } else {
+          const raw_t v = *(const raw_t*)(at + k * W * 2);
+#pragma unroll
+          for (int p = 0; p < N / 2; ++p) raw[k][p] = v[p];
+        }
+      }
+#pragma unroll
+      for (int p = 0; p < N / 2; ++p)
+#pragma unroll
+        for (int d = 0; d < 4; ++d) {
+          f[2 * p][d] = __builtin_amdgcn_perm(raw[2 * d + 1][p], raw[2 * d][p], 0x05040100);
+          f[2 * p + 1][d] = __builtin_amdgcn_perm(raw[2 * d + 1][p], raw[2 * d][p], 0x07060302);
+        }
+    };
+    auto read_a = [&](uint32_t slot, int kk, i32x4 (&av)[TM]) {
+      if constexpr (AKR) {
+        read_kr(std::integral_constant<int, TM>(), std::integral_constant<int, BM>(), slot, kk, wm * D::WM, av);
+      } else {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) av[i] = read_kc(true, slot, kk, i);
+      }
+    };
+    i32x4 a0[TM], a1[TM], bf[TN];
+    // the b fragments that column j completes: j's own, or its pair's
+    auto read_b = [&](uint32_t slot, int kk, int j) {
+      if constexpr (BKR) {
+        if (j % 2 == 1)
+          read_kr(std::integral_constant<int, 2>(), std::integral_constant<int, BN>(), slot + BM * 128, kk,
+                  wn * D::WN + (j - 1) * 16, bf + (j - 1));
+      } else {
+        bf[j] = read_kc(false, slot, kk, j);
+      }
+    };
+    auto column = [&](int j, const i32x4 (&av)[TM]) {
+#pragma unroll
+      for (int i = 0; i < TM; ++i) {
+        if constexpr (I8)
+          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bf[j], av[i], acc[i][j], 0, 0, 0);
+        else
+          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bf[j]),
+                                                             __builtin_bit_cast(bf16x8, av[i]), acc[i][j], 0, 0, 0);
+      }
+    };
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+#pragma unroll
+      for (int j = 0; j < TN; ++j) acc[i][j] = Acc{0, 0, 0, 0};
+
+    // ---- loop
+    constexpr int S = TN / 3;                                   // columns before the barrier
+    constexpr int LPC = (D::LOADS + TN - S - 1) / (TN - S);     // loads per column after it
+#pragma unroll
+    for (int t = 0; t < ST; ++t)
+      if (t < KT) {
+        const __amdgpu_buffer_rsrc_t ra = res_a(t), rb = res_b(t);
+#pragma unroll
+        for (int i = 0; i < D::LOADS; ++i) issue(i, t, t * D::STAGE, ra, rb);
+      }
+    tile_wait<D::LOADS>(min(ST, KT) - 1);
+    tile_barrier();
+    read_a(0, 0, a0);
+#pragma unroll
+    for (int j = 0; j < TN; ++j) read_b(0, 0, j);
+    auto half0 = [&](uint32_t slot) {
+      read_a(slot, 1, a1);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        column(j, a0);
+        read_b(slot, 1, j);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+#pragma unroll
+      for (int j = 0; j < S; ++j) column(j, a1);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    uint32_t slot = 0;
+#pragma unroll 1
+    for (int t = 0; t < KT - 1; ++t) {
+      half0(slot);
+      if constexpr (ST == 2) tile_vmcnt<0>();
+      else tile_wait<D::LOADS>(min(ST - 2, KT - 2 - t));   // stage t + 1 landed
+      tile_barrier();
+      const uint32_t next = slot == (ST - 1) * D::STAGE ? 0 : slot + D::STAGE;
+      const bool more = t + ST < KT;
+      const __amdgpu_buffer_rsrc_t ra = res_a(more ? t + ST : 0), rb = res_b(more ? t + ST : 0);
+      read_a(next, 0, a0);
+#pragma unroll
+      for (int j = 0; j < S; ++j) read_b(next, 0, j);
+#pragma unroll
+      for (int j = S; j < TN; ++j) {
+        column(j, a1);
+        read_b(next, 0, j);
+        if (more) {
+#pragma unroll
+          for (int q = 0; q < LPC; ++q)
+            if ((j - S) * LPC + q < D::LOADS) issue((j - S) * LPC + q, t + ST, slot, ra, rb);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      slot = next;
+    }
+    half0(slot);
+#pragma unroll
+    for (int j = S; j < TN; ++j) column(j, a1);
+  }
+
+  // first row and column (KC b with two matrices: of either) of this workgroup's
+  // tile: tiles of one XCD are consecutive and walk group_m row blocks down
+  // before moving one column block right, sharing both operands in its L2
+  static __device__ __forceinline__ void place(const TileShape& s, int block, int blocks, int& tm, int& tn) {
+    const int tile = tile_of_block(block, blocks);
+    const int per_group = s.group_m * s.tiles_n, grp = tile / per_group, first = grp * s.group_m;
+    const int rows_in = min(s.tiles_m - first, s.group_m), in_grp = tile - grp * per_group;
+    tm = first + in_grp % rows_in;
+    tn = in_grp / rows_in;
+  }
+};
+
+}  // namespace t2i

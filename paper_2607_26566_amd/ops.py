@@ -179,7 +179,7 @@ def gated_linear(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor,
                  act: str = "silu", save_pre: bool = False, stream=None):
     """``act(x wg^T + bg) * (x wu^T + bu)`` (``t2i_op_gated_linear``): ``x [M, K]``,
     ``wg``, ``wu`` ``[F, K]``, one dtype (bf16 or fp32); ``[M, F]``.  With ``save_pre``
-    also the pre-activations ``[M, 2F]`` that :func:`gated_linear_backward` takes."""
+    also the fp32 pre-activations ``[M, 2F]`` that :func:`gated_linear_backward` takes."""
     dev = _device(x, wg, wu, bg, bu)
     dt, M, F, K, lda, ldw = _gated_args(x, wg, wu)
     a = _of(ACTS, act, "act")
@@ -187,7 +187,7 @@ def gated_linear(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor,
     _vec(bu, F, x.dtype, "bu")
     with _on(dev, stream) as st:
         out = torch.empty((M, F), dtype=x.dtype, device=dev)
-        pre = torch.empty((M, 2 * F), dtype=x.dtype, device=dev) if save_pre else None
+        pre = torch.empty((M, 2 * F), dtype=torch.float32, device=dev) if save_pre else None
         _check(load().t2i_op_gated_linear(dt, a, M, F, K, x.data_ptr(), lda, wg.data_ptr(),
                                           wu.data_ptr(), ldw, _p(bg), _p(bu), out.data_ptr(), F,
                                           _p(pre), 2 * F, st))
@@ -203,7 +203,7 @@ def gated_linear_backward(dout: torch.Tensor, x: torch.Tensor, wg: torch.Tensor,
     dt, M, F, K, lda, ldw = _gated_args(x, wg, wu)
     a = _of(ACTS, act, "act")
     ldd = _rows(dout, (M, F), x.dtype, "dout")
-    ldp = _rows(pre, (M, 2 * F), x.dtype, "pre")
+    ldp = _rows(pre, (M, 2 * F), torch.float32, "pre")
     lib = load()
     with _on(dev, stream) as st:
         new = lambda on, *shape: torch.empty(shape, dtype=x.dtype, device=dev) if on else None  # noqa: E731

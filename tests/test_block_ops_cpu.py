@@ -128,7 +128,8 @@ def test_linear_i8_refuses():
         (dict(M=0), SHAPE), (dict(N=0), SHAPE), (dict(K=0), SHAPE), (dict(K=131072), SHAPE),
         (dict(M=2 ** 30, N=2 ** 30), SHAPE), (dict(A=None), INVALID), (dict(W=None), INVALID),
         (dict(a_scale=None), INVALID), (dict(w_scale=None), INVALID), (dict(out=None), INVALID),
-        (dict(lda=240), SHAPE), (dict(lda=264), SHAPE), (dict(ldw=130), SHAPE), (dict(ldo=4), INVALID),
+        (dict(lda=240), SHAPE), (dict(lda=264), SHAPE), (dict(ldw=130), SHAPE), (dict(lda=2 ** 24), SHAPE),
+        (dict(ldw=2 ** 24), SHAPE), (dict(ldo=4), INVALID),
         (dict(A=P + 8), INVALID), (dict(W=P + 1), INVALID), (dict(a_scale=P + 1), INVALID),
         (dict(w_scale=P + 2), INVALID), (dict(bias=P + 1), INVALID), (dict(out=P + 1), INVALID),
         (dict(res, resid=None), INVALID), (dict(res, ldr=4), INVALID), (dict(res, resid=P + 2), INVALID),
@@ -148,7 +149,8 @@ def test_gated_linear_refuses():
         (dict(bg=P), INVALID), (dict(bu=P), INVALID), (dict(lda=8), SHAPE), (dict(ldw=8), SHAPE),
         (dict(ldo=0), SHAPE), (dict(pre=P, ldp=8), SHAPE), (dict(F=12, ldo=16), SHAPE),
         (dict(K=12), SHAPE), (dict(lda=20), SHAPE), (dict(ldw=20), SHAPE), (dict(ldo=12), SHAPE),
-        (dict(pre=P, ldp=20), SHAPE), (dict(A=P + 8), INVALID), (dict(Wg=P + 8), INVALID),
+        (dict(lda=2 ** 23), SHAPE), (dict(ldw=2 ** 23), SHAPE),
+        (dict(pre=P, ldp=18), SHAPE), (dict(A=P + 8), INVALID), (dict(Wg=P + 8), INVALID),
         (dict(Wu=P + 8), INVALID), (dict(out=P + 8), INVALID), (dict(pre=P + 8), INVALID),
         (dict(bg=P + 8, bu=P), INVALID), (dict(dtype=F32, A=P + 2), INVALID)])
 
@@ -169,7 +171,8 @@ def test_gated_linear_backward_refuses():
         (dict(dA=None, dWg=None, dWu=None, dbg=None, dbu=None), INVALID),
         (dict(lda=8), SHAPE), (dict(ldw=8), SHAPE), (dict(ldp=8), SHAPE), (dict(ldd=0), SHAPE),
         (dict(ldda=8), SHAPE), (dict(lddw=8), SHAPE), (dict(K=12), SHAPE), (dict(F=4), SHAPE),
-        (dict(ldda=20), SHAPE), (dict(lddw=20), SHAPE), (dict(ldd=12), SHAPE), (dict(dA=P + 8), INVALID),
+        (dict(ldda=20), SHAPE), (dict(lddw=20), SHAPE), (dict(ldd=12), SHAPE), (dict(ldp=18), SHAPE), (dict(lda=2 ** 23), SHAPE),
+        (dict(ldw=2 ** 23), SHAPE), (dict(dA=P + 8), INVALID),
         (dict(dWg=P + 8), INVALID), (dict(dWu=P + 8), INVALID), (dict(dbg=P + 8), INVALID),
         (dict(ws=P + 128), INVALID), (dict(ws_bytes=need - 1), WORKSPACE)])
     ws = t2i.load().t2i_op_gated_linear_backward_ws_bytes
