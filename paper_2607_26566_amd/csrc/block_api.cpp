@@ -172,7 +172,7 @@ t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F,
 
 size_t t2i_op_gated_linear_backward_ws_bytes(int32_t dtype, int32_t M, int32_t F) {
   if (bad_dtype(dtype) || M < 1 || F < 1 || F > (1 << 28) || too_large(M, 2 * F)) return 0;
-  return gated_dgu_bytes(dtype, M, F) + (size_t)gate_row_blocks(M) * 2 * gated_cols(F) * 4;
+  return gated_dgu_bytes(dtype, M, F) + (size_t)gate_row_blocks(M, F) * 2 * gated_cols(F) * 4;
 }
 
 t2i_status t2i_op_gated_linear_backward(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,

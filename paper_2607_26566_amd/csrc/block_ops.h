@@ -55,8 +55,8 @@ struct GatedFwd {
 hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& a, int M, int F, int K, hipStream_t st);
 
 // dgu [M][2 gated_cols(F)] and, when partial != NULL, the column sums of every
-// row block: partial [gate_row_blocks(M)][2 gated_cols(F)]
-int gate_row_blocks(int M);
+// row block: partial [gate_row_blocks(M, F)][2 gated_cols(F)]
+int gate_row_blocks(int M, int F);
 hipError_t launch_gate_grad(bool is_bf16, int act, int M, int F, const float* pre, int ldp,
                             const void* dout, int ldd, void* dgu, float* partial, hipStream_t st);
 // dbg[f] / dbu[f] = sum of the partials, in ascending block order

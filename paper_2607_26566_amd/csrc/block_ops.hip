@@ -50,10 +50,12 @@ __device__ __forceinline__ float group_sum(float v) {
 // Quantising rows: s = max(max |x| / 127, 2^-126) in fp32, q = x / s to the
 // nearest whole number, ties to even, of the exact quotient.
 //
-// The rounding costs no division: n = rint(x (1/s)) is off by one at most, and
-// only where x / s lies within its error of a half.  r = fma(-n, s, x) is
-// then exact (|r| is at most about s / 2 and a multiple of s's last place over
-// four), so comparing 2 r with s settles the tie exactly.
+// The rounding costs no division: m = fma(x, 1/s, 1.5 2^23) leaves the nearest
+// whole number n in its low bits, wrong by one at most and only where x / s lies
+// within the error of 1/s of a half.  r = fma(-n, s, x) is exact (|r| is at most
+// about s / 2 and a multiple of s's last place over four), so |r| against s / 2
+// says which pieces hold such a value; those (about one value in 10^5) are
+// settled by comparing 2 r with s.
 // A row with a NaN or an infinity gets s = NaN and q = 0: its outputs are NaN.
 
 __device__ __forceinline__ int quant1(float x, float s, float inv) {
@@ -65,13 +67,56 @@ __device__ __forceinline__ int quant1(float x, float s, float inv) {
   return (int)n;
 }
 
-__device__ __forceinline__ uint32_t abs_bits(float v) {
-  return __float_as_uint(v) & 0x7fffffffu;   // orders as |v|, infinity and NaN above
-}
+// eight elements of a row as they lie in memory, and the largest of their
+// magnitudes' bits (which order as the magnitudes do, infinity and NaN above)
+template <typename T>
+struct Piece;
+template <>
+struct Piece<bf16> {
+  uint32_t w[4];
+  __device__ __forceinline__ void load(const bf16* p) {
+    const uint4 v = *(const uint4*)p;
+    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+  }
+  __device__ __forceinline__ void set(int i, bf16 v) {
+    const uint32_t b = __builtin_bit_cast(uint16_t, v);
+    w[i >> 1] |= b << (16 * (i & 1));
+  }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = 0;
+  }
+  __device__ __forceinline__ float get(int i) const {
+    return __uint_as_float(i & 1 ? w[i >> 1] & 0xffff0000u : w[i >> 1] << 16);
+  }
+  __device__ __forceinline__ uint32_t largest() const {
+    typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+    u16x2 m = __builtin_bit_cast(u16x2, w[0] & 0x7fff7fffu);
+#pragma unroll
+    for (int i = 1; i < 4; ++i) m = __builtin_elementwise_max(m, __builtin_bit_cast(u16x2, w[i] & 0x7fff7fffu));
+    return (uint32_t)max((uint32_t)m[0], (uint32_t)m[1]) << 16;
+  }
+};
+template <>
+struct Piece<float> {
+  float v[8];
+  __device__ __forceinline__ void load(const float* p) { load8(p, v); }
+  __device__ __forceinline__ void set(int i, float x) { v[i] = x; }
+  __device__ __forceinline__ void clear() {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = 0.f;
+  }
+  __device__ __forceinline__ float get(int i) const { return v[i]; }
+  __device__ __forceinline__ uint32_t largest() const {
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7fffffffu);
+    return m;
+  }
+};
 
-// TPR threads per row, NV pieces of 8 elements per thread in registers; longer
-// rows read their pieces again.  VEC: rows start at multiples of 16 bytes and
-// K % 8 == 0 is not needed (the last piece is read element by element).
+// TPR threads per row, NV pieces per thread in registers; longer rows read their
+// pieces again.  VEC: rows start at multiples of 16 bytes.
 template <typename T, int TPR, int NV, bool VEC>
 __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x, int ldx, int rows,
                                                          int K, int8_t* __restrict__ q, int ldq,
@@ -82,32 +127,30 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x
   const int row = blockIdx.x * RPB + rl;
   const bool live = row < rows;
   const T* xr = x + (size_t)(live ? row : 0) * ldx;
-  auto load = [&](int c, float (&v)[8]) {
+  Piece<T> v[NV];
+  auto load = [&](int c, Piece<T>& p) {
     const int k = c * 8;
     if (VEC && k + 8 <= K) {
-      load8(xr + k, v);
+      p.load(xr + k);
     } else {
+      p.clear();
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = k + i < K ? to_f32(xr[k + i]) : 0.f;
+      for (int i = 0; i < 8; ++i)
+        if (k + i < K) p.set(i, xr[k + i]);
     }
   };
   const int chunks = (K + 127) / 128 * 16;   // the zeros behind K too
-  float v[NV][8];
   uint32_t m = 0;
   const int rounds = (chunks + TPR * NV - 1) / (TPR * NV);
   for (int r = 0; r < rounds; ++r) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (r * NV + i) * TPR + t;
-      if (c * 8 < K && live) load(c, v[i]);
-      else
-#pragma unroll
-        for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
+      if (c < chunks) load(c, v[i]);
+      else v[i].clear();
     }
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int j = 0; j < 8; ++j) m = max(m, abs_bits(v[i][j]));
+    for (int i = 0; i < NV; ++i) m = max(m, v[i].largest());
   }
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) m = max(m, (uint32_t)__shfl_xor((int)m, o, kWave));
@@ -120,46 +163,69 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x
   const bool finite = m < 0x7f800000u;
   const float s = fmaxf(__uint_as_float(finite ? m : 0u) / 127.f, 1.17549435e-38f);
   const float inv = 1.f / s;
+  // (below s / 2 by its last place: 0.5 s may be off by that where s is near 2^-126)
+  const float near_half = 0.5f * s * (1.f - 2.4e-7f);
   if (live && t == 0) scale[row] = finite ? s : __uint_as_float(0x7fc00000u);
+  if (!live) return;
   for (int r = 0; r < rounds; ++r) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int c = (r * NV + i) * TPR + t;
-      if (c >= chunks || !live) continue;
-      if (rounds > 1) {
-        if (c * 8 < K) load(c, v[i]);
-        else
-#pragma unroll
-          for (int j = 0; j < 8; ++j) v[i][j] = 0.f;
-      }
+      if (c >= chunks) break;
+      if (rounds > 1) load(c, v[i]);
       uint32_t w[2] = {0, 0};
-      if (finite)
+      if (finite) {
+        constexpr float MAGIC = 12582912.f;   // 1.5 2^23
+        uint32_t b[8];
+        float far = 0.f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) w[j >> 2] |= (uint32_t)(quant1(v[i][j], s, inv) & 255) << (8 * (j & 3));
+        for (int j = 0; j < 8; ++j) {
+          const float xv = v[i].get(j), mg = fmaf(xv, inv, MAGIC);
+          far = fmaxf(far, fabsf(fmaf(MAGIC - mg, s, xv)));
+          b[j] = __float_as_uint(mg);
+        }
+        if (far >= near_half)
+#pragma unroll
+          for (int j = 0; j < 8; ++j) b[j] = (uint32_t)quant1(v[i].get(j), s, inv);
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+          w[h] = __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[4 * h + 3], b[4 * h + 2], 0x0c0c0400),
+                                       __builtin_amdgcn_perm(b[4 * h + 1], b[4 * h], 0x0c0c0400), 0x05040100);
+      }
       *(uint2*)(q + (size_t)row * ldq + c * 8) = uint2{w[0], w[1]};
     }
   }
 }
 
+template <typename T>
+static void quant_rows_any(int rows, int K, const T* x, int ldx, int8_t* q, int ldq, float* scale, hipStream_t st) {
+  const bool vec = (uintptr_t)x % 16 == 0 && ldx * sizeof(T) % 16 == 0;
+#define T2I_Q(TPR, NV)                                                                                          \
+  {                                                                                                            \
+    const dim3 grid((unsigned)((rows + 256L / TPR - 1) / (256 / TPR)));                                         \
+    if (vec)                                                                                                   \
+      hipLaunchKernelGGL((quant_rows_kernel<T, TPR, NV, true>), grid, dim3(256), 0, st, x, ldx, rows, K, q,     \
+                         ldq, scale);                                                                          \
+    else                                                                                                       \
+      hipLaunchKernelGGL((quant_rows_kernel<T, TPR, NV, false>), grid, dim3(256), 0, st, x, ldx, rows, K, q,    \
+                         ldq, scale);                                                                          \
+  }
+  // one wave per row up to 2048 elements, a workgroup for longer rows; just the
+  // pieces that the row has, up to what registers hold
+  if (K <= 512) T2I_Q(64, 1)
+  else if (K <= 1024) T2I_Q(64, 2)
+  else if (K <= 1536) T2I_Q(64, 3)
+  else if (K <= 2048) T2I_Q(64, 4)
+  else if (K <= 4096) T2I_Q(256, 2)
+  else if (K <= 8192) T2I_Q(256, 4)
+  else T2I_Q(256, 8)
+#undef T2I_Q
+}
+
 hipError_t launch_quant_rows(bool bf16_in, int rows, int K, const void* x, int ldx, int8_t* q,
                              int ldq, float* scale, hipStream_t st) {
-  // one wave per row up to 2048 elements, a workgroup for longer rows
-  const bool wave = K <= 2048;
-  const int rpb = wave ? 4 : 1;
-  const dim3 grid((unsigned)((rows + (long)rpb - 1) / rpb));
-  const size_t e = bf16_in ? 2 : 4;
-  const bool vec = (uintptr_t)x % 16 == 0 && ldx * e % 16 == 0;
-#define T2I_Q(T, TPR, NV, VEC)                                                                      \
-  hipLaunchKernelGGL((quant_rows_kernel<T, TPR, NV, VEC>), grid, dim3(256), 0, st, (const T*)x, ldx, \
-                     rows, K, q, ldq, scale)
-  if (bf16_in) {
-    if (wave) { if (vec) T2I_Q(bf16, 64, 4, true); else T2I_Q(bf16, 64, 4, false); }
-    else { if (vec) T2I_Q(bf16, 256, 4, true); else T2I_Q(bf16, 256, 4, false); }
-  } else {
-    if (wave) { if (vec) T2I_Q(float, 64, 4, true); else T2I_Q(float, 64, 4, false); }
-    else { if (vec) T2I_Q(float, 256, 4, true); else T2I_Q(float, 256, 4, false); }
-  }
-#undef T2I_Q
+  if (bf16_in) quant_rows_any(rows, K, (const bf16*)x, ldx, q, ldq, scale, st);
+  else quant_rows_any(rows, K, (const float*)x, ldx, q, ldq, scale, st);
   return hipGetLastError();
 }
 
@@ -418,24 +484,30 @@ hipError_t launch_qk_norm_rope_bwd(bool is_bf16, const QkNorm& a, float* partial
 }
 
 // Column sums of n rows of fp32 partials (row stride ld) in fp64: 16 columns
-// per workgroup, each by 16 threads that take every 16th row, joined in a
-// fixed order.
+// per workgroup of 1024, each by 64 threads that take every 64th row (so that a
+// sum's reads are all under way at once), joined in a fixed order.
 __device__ __forceinline__ double column_sum(const float* p, int n, size_t ld, int c, bool in) {
-  __shared__ double red[16][16];
+  __shared__ double red[64][16];
   const int s = threadIdx.x / 16, l = threadIdx.x % 16;
   double v = 0.;
-  if (in)
-    for (int i = s; i < n; i += 16) v += (double)p[(size_t)i * ld + c];
+  if (in) {
+#pragma unroll 4
+    for (int i = s; i < n; i += 64) v += (double)p[(size_t)i * ld + c];
+  }
   red[s][l] = v;
   __syncthreads();
-  v = 0.;
+  if (s < 4) {
 #pragma unroll
-  for (int i = 0; i < 16; ++i) v += red[i][l];
-  return v;
+    for (int i = 1; i < 16; ++i) v += red[s + 4 * i][l];
+  }
+  __syncthreads();
+  if (s < 4) red[s][l] = v;
+  __syncthreads();
+  return (red[0][l] + red[1][l]) + (red[2][l] + red[3][l]);
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void qk_weight_grad_kernel(const float* __restrict__ partial,
+__global__ __launch_bounds__(1024) void qk_weight_grad_kernel(const float* __restrict__ partial,
                                                              int blocks, int d, T* __restrict__ dwq,
                                                              T* __restrict__ dwk) {
   const int c = blockIdx.x * 16 + threadIdx.x % 16;
@@ -450,10 +522,10 @@ hipError_t launch_qk_weight_grad(bool is_bf16, int blocks, int head_dim, const f
                                  void* dwq, void* dwk, hipStream_t st) {
   const dim3 grid((unsigned)((2 * head_dim + 15) / 16));
   if (is_bf16)
-    hipLaunchKernelGGL((qk_weight_grad_kernel<bf16>), grid, dim3(256), 0, st, partial, blocks, head_dim,
+    hipLaunchKernelGGL((qk_weight_grad_kernel<bf16>), grid, dim3(1024), 0, st, partial, blocks, head_dim,
                        (bf16*)dwq, (bf16*)dwk);
   else
-    hipLaunchKernelGGL((qk_weight_grad_kernel<float>), grid, dim3(256), 0, st, partial, blocks,
+    hipLaunchKernelGGL((qk_weight_grad_kernel<float>), grid, dim3(1024), 0, st, partial, blocks,
                        head_dim, (float*)dwq, (float*)dwk);
   return hipGetLastError();
 }
@@ -481,25 +553,34 @@ __device__ __forceinline__ ActGrad act_grad(int act, float g) {
   return {a, fmaf(a, 1.f - s, s)};
 }
 
-constexpr int kGateRows = 64;   // rows per workgroup
-int gate_row_blocks(int M) { return (M + kGateRows - 1) / kGateRows; }
+// rows per workgroup: 64, or down to the 8 that its threads take at a time while
+// there are fewer than two workgroups per CU (333 rows of 1544: 13.9 -> 4.4 us)
+static int gate_rows(int M, int F) {
+  int rows = 64;
+  while (rows > 8 && (long)((M + rows - 1) / rows) * ((gated_cols(F) + 255) / 256) < 512) rows /= 2;
+  return rows;
+}
+int gate_row_blocks(int M, int F) {
+  const int rows = gate_rows(M, F);
+  return (M + rows - 1) / rows;
+}
 
 // V columns per thread (8 where rows are whole 16-byte pieces, else 1): 32
 // threads side by side, 8 rows at a time
 template <typename T, int V>
-__global__ __launch_bounds__(256) void gate_grad_kernel(int act, int M, int F, int Fp,
+__global__ __launch_bounds__(256) void gate_grad_kernel(int act, int M, int F, int Fp, int rows,
                                                         const float* __restrict__ pre, int ldp,
                                                         const T* __restrict__ dout, int ldd,
                                                         T* __restrict__ dgu, float* __restrict__ partial) {
   __shared__ float red[2][8][32 * V];
   const int tx = threadIdx.x % 32, ty = threadIdx.x / 32;
   const int f = (blockIdx.y * 32 + tx) * V;
-  const int r0 = blockIdx.x * kGateRows;
+  const int r0 = blockIdx.x * rows;
   float sg[V], su[V];
 #pragma unroll
   for (int j = 0; j < V; ++j) sg[j] = su[j] = 0.f;
   if (f < Fp)
-    for (int r = r0 + ty; r < min(r0 + kGateRows, M); r += 8) {
+    for (int r = r0 + ty; r < min(r0 + rows, M); r += 8) {
       float g[V], u[V], dh[V];
       if (f < F) {
         const float* p = pre + (size_t)r * ldp + f;
@@ -552,19 +633,19 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(int act, int M, int F, i
 
 hipError_t launch_gate_grad(bool is_bf16, int act, int M, int F, const float* pre, int ldp,
                             const void* dout, int ldd, void* dgu, float* partial, hipStream_t st) {
-  const int Fp = gated_cols(F), per = is_bf16 ? 256 : 32;
-  const dim3 grid((unsigned)gate_row_blocks(M), (unsigned)((Fp + per - 1) / per));
+  const int Fp = gated_cols(F), per = is_bf16 ? 256 : 32, rows = gate_rows(M, F);
+  const dim3 grid((unsigned)gate_row_blocks(M, F), (unsigned)((Fp + per - 1) / per));
   if (is_bf16)
-    hipLaunchKernelGGL((gate_grad_kernel<bf16, 8>), grid, dim3(256), 0, st, act, M, F, Fp,
+    hipLaunchKernelGGL((gate_grad_kernel<bf16, 8>), grid, dim3(256), 0, st, act, M, F, Fp, rows,
                        pre, ldp, (const bf16*)dout, ldd, (bf16*)dgu, partial);
   else
-    hipLaunchKernelGGL((gate_grad_kernel<float, 1>), grid, dim3(256), 0, st, act, M, F, Fp,
+    hipLaunchKernelGGL((gate_grad_kernel<float, 1>), grid, dim3(256), 0, st, act, M, F, Fp, rows,
                        pre, ldp, (const float*)dout, ldd, (float*)dgu, partial);
   return hipGetLastError();
 }
 
 template <typename T>
-__global__ __launch_bounds__(256) void gate_bias_grad_kernel(const float* __restrict__ partial, int blocks,
+__global__ __launch_bounds__(1024) void gate_bias_grad_kernel(const float* __restrict__ partial, int blocks,
                                                              int F, int Fp, T* __restrict__ dbg,
                                                              T* __restrict__ dbu) {
   const int c = blockIdx.x * 16 + threadIdx.x % 16, w = blockIdx.y;
@@ -576,11 +657,11 @@ hipError_t launch_gate_bias_grad(bool is_bf16, int M, int F, const float* partia
                                  void* dbu, hipStream_t st) {
   const dim3 grid((unsigned)((F + 15) / 16), 2);
   if (is_bf16)
-    hipLaunchKernelGGL((gate_bias_grad_kernel<bf16>), grid, dim3(256), 0, st, partial,
-                       gate_row_blocks(M), F, gated_cols(F), (bf16*)dbg, (bf16*)dbu);
+    hipLaunchKernelGGL((gate_bias_grad_kernel<bf16>), grid, dim3(1024), 0, st, partial,
+                       gate_row_blocks(M, F), F, gated_cols(F), (bf16*)dbg, (bf16*)dbu);
   else
-    hipLaunchKernelGGL((gate_bias_grad_kernel<float>), grid, dim3(256), 0, st, partial,
-                       gate_row_blocks(M), F, gated_cols(F), (float*)dbg, (float*)dbu);
+    hipLaunchKernelGGL((gate_bias_grad_kernel<float>), grid, dim3(1024), 0, st, partial,
+                       gate_row_blocks(M, F), F, gated_cols(F), (float*)dbg, (float*)dbu);
   return hipGetLastError();
 }
 
