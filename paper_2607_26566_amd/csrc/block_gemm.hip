@@ -2,26 +2,27 @@
 // feed-forward and its gradients.  bf16 and 8-bit operands go through the tiles
 // of gemm_tile.h, fp32 ones through gemm_f32_tile_kernel:
 //
-// One product C[m][n] = sum_k a(m, k) b(n, k) on 64 x 64
-// tiles by 4 waves of 32 x 32 (v_mfma_f32_16x16x4_f32), 32 values of k at a
-// time through LDS, the next step's operands fetched into registers under
-// this step's MFMAs.  The operands are read by element through two functors,
-// so any stride and size goes.
+// One product C[m][n] = sum_k a(m, k) b(n, k) on BM x 64 tiles by 4 waves of
+// BM / 2 x 32 (v_mfma_f32_16x16x4_f32), 32 values of k at a time through two LDS
+// stages, the next step's operands on their way into registers meanwhile.  A
+// stage holds [row][k] in rows of 144 bytes; a lane's 16 bytes are k = 4 g .. 4 g + 3
+// of its row and feed four MFMAs, which between them take 16 of k in an order of
+// their own, the same for both operands.  Reads come from different banks (36
+// dwords a row: 16 rows, 16 places).  VEC: operands are read 16 bytes at a time
+// (rows of whole, aligned 16-byte pieces), else by element; addresses stay inside
+// the operand and what lies outside is taken as 0, without branches.
 #include "gemm_tile.h"
 
 namespace t2i {
 
-// Elements of a row-major matrix, 0 outside [0, rows) x [0, cols).
-// ALONG: the k axis runs along the rows (contiguous in memory).
+// Rows [0, rows) x columns [0, cols) of a row-major matrix.  along: the k axis
+// runs along the rows (contiguous in memory), else across them.
 template <bool ALONG>
 struct Mat {
   static constexpr bool along = ALONG;
   const float* p;
   int ld, rows, cols;
-  __device__ __forceinline__ float at(int r, int k) const {
-    const int y = ALONG ? r : k, x = ALONG ? k : r;
-    return y < rows && x < cols ? p[(size_t)y * ld + x] : 0.f;
-  }
+  __device__ __forceinline__ const float* at(int y, int x) const { return p + (size_t)y * ld + x; }
 };
 
 // Gate and up weights side by side: of every 32 rows, 16 of the gate and the
@@ -30,89 +31,145 @@ struct GateUp {
   static constexpr bool along = true;
   const float *g, *u;
   int ld, rows, cols;
-  __device__ __forceinline__ float at(int r, int k) const {
-    const int f = r / 32 * 16 + r % 16;
-    return f < rows && k < cols ? ((r & 16) ? u : g)[(size_t)f * ld + k] : 0.f;
+  __device__ __forceinline__ const float* at(int y, int x) const {
+    const int f = min(y / 32 * 16 + y % 16, rows - 1);
+    return ((y & 16) ? u : g) + (size_t)f * ld + x;
   }
 };
 
-// The gradients' operand [dg | du]^T... as rows of the contraction over both
-// halves: k < Fp the gate's row k, else the up projection's row k - Fp
+// The rows of the gate weights, then those of the up weights, from row `half` on
 struct TwoRows {
   static constexpr bool along = false;
   const float *g, *u;
   int ld, rows, cols, half;
-  __device__ __forceinline__ float at(int n, int k) const {
-    const int f = k < half ? k : k - half;
-    return f < rows && n < cols ? (k < half ? g : u)[(size_t)f * ld + n] : 0.f;
+  __device__ __forceinline__ const float* at(int y, int x) const {
+    const int f = min(y < half ? y : y - half, rows - 1);
+    return (y < half ? g : u) + (size_t)f * ld + x;
   }
 };
 
-template <class LA, class LB, class EP>
+// whether element (y, x) lies in the operand, and the nearest (y, x) that does
+template <bool ALONG>
+__device__ __forceinline__ bool inside(const Mat<ALONG>& m, int& y, int& x) {
+  const bool in = y < m.rows && x < m.cols;
+  y = min(y, m.rows - 1);
+  return in;
+}
+__device__ __forceinline__ bool inside(const GateUp& m, int& y, int& x) {
+  return y / 32 * 16 + y % 16 < m.rows && x < m.cols;
+}
+__device__ __forceinline__ bool inside(const TwoRows& m, int& y, int& x) {
+  return (y < m.half ? y : y - m.half) < m.rows && x < m.cols;
+}
+
+template <int BM, bool VEC, class LA, class LB, class EP>
 __global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep, int tiles_n, int K) {
-  constexpr int BK = 32, LD = 65;
-  __shared__ float sA[BK][LD], sB[BK][LD];
+  constexpr int BK = 32, LD = 36, TM = BM / 32;
+  __shared__ __attribute__((aligned(16))) float smem[2][(BM + 64) * LD];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave >> 1, wn = wave & 1, fr = lane & 15, g = lane >> 4;
-  const int m0 = (int)(blockIdx.x / (unsigned)tiles_n) * 64, n0 = (int)(blockIdx.x % (unsigned)tiles_n) * 64;
-  float ra[8], rb[8];
+  const int m0 = (int)(blockIdx.x / (unsigned)tiles_n) * BM, n0 = (int)(blockIdx.x % (unsigned)tiles_n) * 64;
+  // a thread's pieces of four: along k of one row, or four rows' of one k
+  f32x4 ra[BM / 32], rb[2];
+  auto load = [&](const auto& op, int r0, int k0, int c, int R) -> f32x4 {
+    using O = typename std::decay<decltype(op)>::type;
+    f32x4 v;
+    int y, x;
+    if constexpr (O::along) y = r0 + c / 8, x = k0 + c % 8 * 4;
+    else y = k0 + c / (R / 4), x = r0 + c % (R / 4) * 4;
+    if constexpr (VEC) {
+      const bool in = inside(op, y, x);
+      const f32x4 w = *(const f32x4*)op.at(y, min(x, op.cols - 4));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = in ? w[e] : 0.f;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        int ye = y, xe = x + e;
+        const bool in = inside(op, ye, xe);
+        const float w = *op.at(ye, min(xe, op.cols - 1));
+        v[e] = in ? w : 0.f;
+      }
+    }
+    return v;
+  };
   auto fetch = [&](int k0) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int x = tid + i * 256;
-      ra[i] = LA::along ? la.at(m0 + x / BK, k0 + x % BK) : la.at(m0 + x % 64, k0 + x / 64);
-      rb[i] = LB::along ? lb.at(n0 + x / BK, k0 + x % BK) : lb.at(n0 + x % 64, k0 + x / 64);
+    for (int i = 0; i < BM / 32; ++i) ra[i] = load(la, m0, k0, tid + i * 256, BM);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) rb[i] = load(lb, n0, k0, tid + i * 256, 64);
+  };
+  auto put = [&](bool along, float* s, int c, int R, f32x4 v) {
+    if (along) {
+      *(f32x4*)(s + c / 8 * LD + c % 8 * 4) = v;
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[(c % (R / 4) * 4 + e) * LD + c / (R / 4)] = v[e];
     }
   };
-  f32x4 acc[2][2];
+  f32x4 acc[TM][2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   fetch(0);
-  for (int k0 = 0; k0 < K; k0 += BK) {
-    __syncthreads();
+  int stage = 0;
+  for (int k0 = 0; k0 < K; k0 += BK, stage ^= 1) {
+    float *sA = smem[stage], *sB = sA + BM * LD;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      const int x = tid + i * 256;
-      if (LA::along) sA[x % BK][x / BK] = ra[i]; else sA[x / 64][x % 64] = ra[i];
-      if (LB::along) sB[x % BK][x / BK] = rb[i]; else sB[x / 64][x % 64] = rb[i];
-    }
-    __syncthreads();
+    for (int i = 0; i < BM / 32; ++i) put(LA::along, sA, tid + i * 256, BM, ra[i]);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) put(LB::along, sB, tid + i * 256, 64, rb[i]);
+    __syncthreads();   // (the other stage was read before this step's writes: one barrier a step)
     if (k0 + BK < K) fetch(k0 + BK);
 #pragma unroll
-    for (int kk = 0; kk < BK; kk += 4) {
-      float a[2], b[2];
+    for (int h = 0; h < 2; ++h) {
+      f32x4 a[TM], b[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        a[i] = sA[kk + g][wm * 32 + i * 16 + fr];
-        b[i] = sB[kk + g][wn * 32 + i * 16 + fr];
-      }
+      for (int i = 0; i < TM; ++i) a[i] = *(const f32x4*)(sA + (wm * (BM / 2) + i * 16 + fr) * LD + h * 16 + g * 4);
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+      for (int j = 0; j < 2; ++j) b[j] = *(const f32x4*)(sB + (wn * 32 + j * 16 + fr) * LD + h * 16 + g * 4);
 #pragma unroll
-        for (int j = 0; j < 2; ++j)
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j], a[i], acc[i][j], 0, 0, 0);
+      for (int e = 0; e < 4; ++e)
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j][e], a[i][e], acc[i][j], 0, 0, 0);
     }
   }
-  // operands swapped: a lane holds row m0 + fr, four columns from g * 4
+  // operands swapped: a lane holds row fr, four columns from g * 4
 #pragma unroll
-  for (int i = 0; i < 2; ++i)
+  for (int i = 0; i < TM; ++i)
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
       float v[2];
 #pragma unroll
       for (int j = 0; j < 2; ++j) v[j] = acc[i][j][r];
-      ep(m0 + wm * 32 + i * 16 + fr, n0 + wn * 32 + g * 4 + r, v);
+      ep(m0 + wm * (BM / 2) + i * 16 + fr, n0 + wn * 32 + g * 4 + r, v);
     }
 }
 
-template <class LA, class LB, class EP>
-static hipError_t gemm_f32_tile(const LA& la, const LB& lb, const EP& ep, int M, int N, int K, hipStream_t st) {
+template <int BM, class LA, class LB, class EP>
+static void gemm_f32_launch(bool vec, const LA& la, const LB& lb, const EP& ep, int M, int N, int K, hipStream_t st) {
   const int tn = (N + 63) / 64;
-  const long tiles = (long)((M + 63) / 64) * tn;
-  hipLaunchKernelGGL((gemm_f32_tile_kernel<LA, LB, EP>), dim3((unsigned)tiles), dim3(256), 0, st, la, lb,
-                     ep, tn, K);
+  const dim3 grid((unsigned)((long)((M + BM - 1) / BM) * tn));
+  if (vec)
+    hipLaunchKernelGGL((gemm_f32_tile_kernel<BM, true, LA, LB, EP>), grid, dim3(256), 0, st, la, lb, ep, tn, K);
+  else
+    hipLaunchKernelGGL((gemm_f32_tile_kernel<BM, false, LA, LB, EP>), grid, dim3(256), 0, st, la, lb, ep, tn, K);
+}
+
+template <class LA, class LB, class EP>
+static hipError_t gemm_f32_tile(size_t bits, const LA& la, const LB& lb, const EP& ep, int M,
+                                int N, int K, hipStream_t st) {
+  const bool vec = bits % 16 == 0 && la.ld % 4 == 0 && lb.ld % 4 == 0 &&
+                   la.cols % 4 == 0 && lb.cols % 4 == 0;
+  // 32-row tiles where they spread over the CUs better: a tile of half the size
+  // takes a little more than half the time
+  const long t64 = (long)((M + 63) / 64) * ((N + 63) / 64), t32 = (long)((M + 31) / 32) * ((N + 63) / 64);
+  if ((t32 + 255) / 256 * 11 < (t64 + 255) / 256 * 20) gemm_f32_launch<32>(vec, la, lb, ep, M, N, K, st);
+  else gemm_f32_launch<64>(vec, la, lb, ep, M, N, K, st);
   return hipGetLastError();
 }
 
@@ -449,7 +506,7 @@ static hipError_t gated_dw_bf16(int M, int F, int K, const void* dgu, const void
 }
 
 static hipError_t gated_fwd_f32(const GatedFwd& a, int M, int F, int K, hipStream_t st) {
-  return gemm_f32_tile(Mat<true>{(const float*)a.A, a.lda, M, K},
+  return gemm_f32_tile((size_t)a.A | (size_t)a.Wg | (size_t)a.Wu, Mat<true>{(const float*)a.A, a.lda, M, K},
                           GateUp{(const float*)a.Wg, (const float*)a.Wu, a.ldw, F, K}, GatedStore{a, M, F}, M,
                           (F + 15) / 16 * 32, K, st);
 }
@@ -457,7 +514,7 @@ static hipError_t gated_fwd_f32(const GatedFwd& a, int M, int F, int K, hipStrea
 static hipError_t gated_dx_f32(int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw,
                            void* dx, int ldx, hipStream_t st) {
   const int Fp = gated_cols(F);
-  return gemm_f32_tile(Mat<true>{(const float*)dgu, 2 * Fp, M, 2 * Fp},
+  return gemm_f32_tile((size_t)dgu | (size_t)Wg | (size_t)Wu, Mat<true>{(const float*)dgu, 2 * Fp, M, 2 * Fp},
                           TwoRows{(const float*)Wg, (const float*)Wu, ldw, F, K, Fp},
                           PlainStore{(float*)dx, ldx, M, K}, M, K, 2 * Fp, st);
 }
@@ -468,7 +525,7 @@ static hipError_t gated_dw_f32(int M, int F, int K, const void* dgu, const void*
   for (int i = 0; i < 2; ++i) {
     float* o = (float*)(i ? dWu : dWg);
     if (!o) continue;
-    const hipError_t e = gemm_f32_tile(Mat<false>{(const float*)dgu + i * Fp, 2 * Fp, M, F},
+    const hipError_t e = gemm_f32_tile((size_t)dgu | (size_t)A, Mat<false>{(const float*)dgu + i * Fp, 2 * Fp, M, Fp},   // (zeros behind F)
                                           Mat<false>{(const float*)A, lda, M, K},
                                           PlainStore{o, lddw, F, K}, F, K, M, st);
     if (e != hipSuccess) return e;

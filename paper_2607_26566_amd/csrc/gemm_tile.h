@@ -18,8 +18,8 @@
 //     columns.  A lane reads the same N neighbouring columns of its 8 rows k and
 //     joins the halves of the dwords by v_perm, which gives it 8 k of N columns,
 //     the operands of N MFMAs: fragment j of such a group has columns j, N + j,
-//     2 N + j ...  The 64-byte piece p of row k sits in piece p ^ f(k), f the bits
-//     of (k >> 3) & 3 swapped, so that the four rows of a read lie in different
+//     2 N + j ...  For N = 2 (4-byte reads) the 64-byte piece p of row k sits in
+//     piece p ^ f, f = (k >> 3) & 3, so that the four rows of a read lie in different
 //     banks.  (ds_read_b64_tr_b16 would turn the block by itself, but the compiler
 //     lets such a read wait for every load into LDS that is on its way.)
 //
@@ -114,13 +114,17 @@ struct TileProduct {
   static_assert(!AKR || TM == 2 || TM == 4 || TM == 8, "fragments per wave");
   static_assert(!BKR || TN % 2 == 0, "fragments per wave");
 
+  // f of the rows k with (k >> 3) & 3 = g (see above; counted by SQ_LDS_BANK_CONFLICT:
+  // none so, a half of the LDS cycles with the bits of g swapped for every N)
+  template <int N>
+  static __device__ __forceinline__ int kr_swap(int g) { return N == 2 ? g : 0; }
   // the (row, column) of a KR tile of W columns that lane `lane` of load block b fills
-  template <int W>
+  template <int W, int N>
   static __device__ __forceinline__ void kr_source(int b, int lane, int& row, int& col) {
     constexpr int RB = W * 2, MASK = W >= 128 ? 3 : W / 32 - 1;
     const int at = b * 1024 + lane * 16;
     row = at / RB;
-    const int o = at % RB, f = (((row >> 2) & 2) | ((row >> 4) & 1)) & MASK;
+    const int o = at % RB, f = kr_swap<N>((row >> 3) & 3) & MASK;
     col = ((o >> 6) ^ f) * 32 + (o & 63) / 2;
   }
 
@@ -146,8 +150,8 @@ struct TileProduct {
       const int blk = wave + (is_a ? i : i - LA) * D::NW;
       if (is_a ? AKR : BKR) {
         int row, col;
-        if (is_a) kr_source<BM>(blk, lane, row, col);
-        else kr_source<BN>(blk, lane, row, col);
+        if (is_a) kr_source<BM, NA>(blk, lane, row, col);
+        else kr_source<BN, NB>(blk, lane, row, col);
         const TileOperand& o = is_a ? a : b;
         src[i] = (uint32_t)row * o.ld + 2u * (uint32_t)min((is_a ? m0 : n0) + col, o.cols - 8);
       } else {
@@ -196,7 +200,6 @@ struct TileProduct {
 
     // ---- fragments
     const uint32_t kc = fr * 128 + ((g ^ ((fr >> 1) & 7)) << 4);   // half-step 1: ^ 64
-    const int krf = ((g & 1) << 1) | (g >> 1);
     auto read_kc = [&](bool is_a, uint32_t slot, int kk, int i) -> i32x4 {
       int row = is_a ? wm * D::WM + i * 16 : wn * D::WN + i * 16;
       if (!is_a && DUAL)
@@ -208,7 +211,7 @@ struct TileProduct {
       constexpr int N = decltype(n)::value, W = decltype(w)::value, MASK = W >= 128 ? 3 : W / 32 - 1;
       typedef int raw_t __attribute__((ext_vector_type(N / 2 > 1 ? N / 2 : 2)));
       const int o = (c0 + N * fr) * 2;
-      const char* at = smem + base + (kk * 32 + g * 8) * W * 2 + (((o >> 6) ^ (krf & MASK)) << 6) + (o & 63);
+      const char* at = smem + base + (kk * 32 + g * 8) * W * 2 + (((o >> 6) ^ (kr_swap<N>(g) & MASK)) << 6) + (o & 63);
       int raw[8][N / 2];
 #pragma unroll
       for (int k = 0; k < 8; ++k) {

@@ -42,33 +42,32 @@ def _of(table: dict, key, what: str):
     return table[key]
 
 
-def _device(*tensors) -> torch.device:
+def _device(first: torch.Tensor, *others) -> torch.device:
     """The one device of all given tensors (None entries left out)."""
-    dev = None
-    for t in tensors:
-        if t is None:
-            continue
-        if not t.is_cuda:
-            raise T2IError(1, "operands must be device tensors")
-        if dev is None:
-            dev = t.device
-        elif t.device != dev:
-            raise T2IError(1, "operands must be on one device")
+    _need(first.is_cuda, "operands must be device tensors", 1)
+    dev = first.device
+    for t in others:
+        if t is not None and t.device != dev:
+            raise T2IError(1, "operands must be device tensors of one device")
     return dev
 
 
-def _rows(t: torch.Tensor, shape, dtype, what: str) -> int:
-    """Row stride of a 2-D tensor of this shape and type (its columns contiguous)."""
-    if t.dtype != dtype or tuple(t.shape) != tuple(shape):
-        raise T2IError(2, f"{what}: expected {tuple(shape)} {dtype}, got {tuple(t.shape)} {t.dtype}")
-    _need(shape[1] == 1 or t.stride(1) == 1, f"{what}: columns must be contiguous")
-    ld = t.stride(0) if shape[0] > 1 else shape[1]   # (a single row may come with any stride)
-    _need(shape[1] <= ld < 2 ** 31, f"{what}: rows must not overlap")
+def _rows(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> int:
+    """Row stride of a matrix of this shape and type (its columns contiguous)."""
+    if t.dtype != dtype or t.shape != (rows, cols):
+        raise T2IError(2, f"{what}: expected ({rows}, {cols}) {dtype}, got {tuple(t.shape)} {t.dtype}")
+    ld, step = t.stride()
+    if cols != 1 and step != 1:
+        raise T2IError(2, f"{what}: columns must be contiguous")
+    if rows == 1:       # a single row may come with any stride
+        ld = cols
+    if not cols <= ld < 2 ** 31:
+        raise T2IError(2, f"{what}: rows must not overlap")
     return ld
 
 
 def _vec(t: Optional[torch.Tensor], n: int, dtype, what: str):
-    if t is not None and (t.dtype != dtype or tuple(t.shape) != (n,) or (n > 1 and t.stride(0) != 1)):
+    if t is not None and (t.dtype != dtype or t.shape != (n,) or (n > 1 and t.stride(0) != 1)):
         raise T2IError(2, f"{what}: expected ({n},) {dtype}, contiguous")
 
 
@@ -79,11 +78,13 @@ def _p(t: Optional[torch.Tensor]):
 @contextlib.contextmanager
 def _on_other(dev, stream):
     with torch.cuda.device(dev), torch.cuda.stream(stream):
-        yield C.c_void_p(stream.cuda_stream)
+        yield stream.cuda_stream
 
 
 class _Here:
     """The current stream of the current device: nothing to switch."""
+
+    __slots__ = ("handle",)
 
     def __init__(self, handle):
         self.handle = handle
@@ -98,7 +99,8 @@ class _Here:
 def _on(dev: torch.device, stream):
     if stream is None:
         if dev.index == torch.cuda.current_device():
-            return _Here(C.c_void_p(torch.cuda.current_stream().cuda_stream))
+            # (the handle alone: torch.cuda.current_stream() makes a stream object, 2.7 us of a 10 us call)
+            return _Here(torch._C._cuda_getCurrentRawStream(dev.index))
         stream = torch.cuda.current_stream(dev)
     elif stream.device != dev:
         raise T2IError(1, "stream belongs to another device than the operands")
@@ -113,7 +115,7 @@ def quant_rows(x: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor
     dt = _of(_DTYPES, x.dtype, "dtype")
     _need(x.dim() == 2, "x must be [rows, K]")
     rows, K = x.shape
-    ld = _rows(x, (rows, K), x.dtype, "x")
+    ld = _rows(x, rows, K, x.dtype, "x")
     with _on(dev, stream) as st:
         q = torch.empty((rows, (K + 127) // 128 * 128), dtype=torch.int8, device=dev)
         scale = torch.empty(rows, dtype=torch.float32, device=dev)
@@ -138,7 +140,7 @@ def linear_i8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: 
     (M, ka), (N, kw) = a.shape, w.shape
     need = (K + 127) // 128 * 128
     _need(K >= 1 and ka >= need and kw >= need, "a and w must reach K rounded up to 128")
-    lda, ldw = _rows(a, (M, ka), torch.int8, "a"), _rows(w, (N, kw), torch.int8, "w")
+    lda, ldw = _rows(a, M, ka, torch.int8, "a"), _rows(w, N, kw, torch.int8, "w")
     lda, ldw = (need if M == 1 else lda), (need if N == 1 else ldw)
     _vec(a_scale, M, torch.float32, "a_scale")
     _vec(w_scale, N, torch.float32, "w_scale")
@@ -147,9 +149,9 @@ def linear_i8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: 
     ldr = N
     if epi >= _lib.T2I_EPI_RESID:
         _need(resid is not None, f"{epilogue} needs resid", 1)
-        ldr = _rows(resid, (M, N), torch.float32, "resid")
+        ldr = _rows(resid, M, N, torch.float32, "resid")
         if resid_copy is not None:
-            ldc = _rows(resid_copy, (M, N), torch.bfloat16, "resid_copy")
+            ldc = _rows(resid_copy, M, N, torch.bfloat16, "resid_copy")
             _need(M == 1 or ldc == ldr, "resid_copy must have resid's row stride")
     else:
         _need(resid is None and resid_copy is None, "resid goes with the resid epilogues", 1)
@@ -168,9 +170,9 @@ def _gated_args(x, wg, wu):
     dt = _of(_DTYPES, x.dtype, "dtype")
     _need(x.dim() == 2 and wg.dim() == 2, "x and the weights must be matrices")
     (M, K), F = x.shape, wg.shape[0]
-    lda = _rows(x, (M, K), x.dtype, "x")
-    ldw = _rows(wg, (F, K), x.dtype, "wg")
-    _need(_rows(wu, (F, K), x.dtype, "wu") == ldw, "wg and wu must have one row stride")
+    lda = _rows(x, M, K, x.dtype, "x")
+    ldw = _rows(wg, F, K, x.dtype, "wg")
+    _need(_rows(wu, F, K, x.dtype, "wu") == ldw, "wg and wu must have one row stride")
     return dt, M, F, K, lda, ldw
 
 
@@ -202,8 +204,8 @@ def gated_linear_backward(dout: torch.Tensor, x: torch.Tensor, wg: torch.Tensor,
     dev = _device(dout, x, wg, wu, pre)
     dt, M, F, K, lda, ldw = _gated_args(x, wg, wu)
     a = _of(ACTS, act, "act")
-    ldd = _rows(dout, (M, F), x.dtype, "dout")
-    ldp = _rows(pre, (M, 2 * F), torch.float32, "pre")
+    ldd = _rows(dout, M, F, x.dtype, "dout")
+    ldp = _rows(pre, M, 2 * F, torch.float32, "pre")
     lib = load()
     with _on(dev, stream) as st:
         new = lambda on, *shape: torch.empty(shape, dtype=x.dtype, device=dev) if on else None  # noqa: E731
@@ -219,12 +221,17 @@ def gated_linear_backward(dout: torch.Tensor, x: torch.Tensor, wg: torch.Tensor,
 
 def _heads(t: torch.Tensor, rows: int, d: int, dtype, what: str):
     """(heads, row stride) of a [rows, heads, d] tensor whose heads lie side by side."""
-    if t.dtype != dtype or t.dim() != 3 or t.shape[0] != rows or t.shape[2] != d:
-        raise T2IError(2, f"{what}: expected ({rows}, heads, {d}) {dtype}, got {tuple(t.shape)} {t.dtype}")
-    h = t.shape[1]
-    _need(t.stride(2) == 1 and (h == 1 or t.stride(1) == d), f"{what}: heads must be side by side")
-    ld = t.stride(0) if rows > 1 else h * d
-    _need(h * d <= ld < 2 ** 31, f"{what}: rows must not overlap")
+    shape = t.shape
+    if t.dtype != dtype or len(shape) != 3 or shape[0] != rows or shape[2] != d:
+        raise T2IError(2, f"{what}: expected ({rows}, heads, {d}) {dtype}, got {tuple(shape)} {t.dtype}")
+    h = shape[1]
+    ld, head, step = t.stride()
+    if step != 1 or (h > 1 and head != d):
+        raise T2IError(2, f"{what}: heads must be side by side")
+    if rows == 1:
+        ld = h * d
+    if not h * d <= ld < 2 ** 31:
+        raise T2IError(2, f"{what}: rows must not overlap")
     return h, ld
 
 
@@ -240,9 +247,9 @@ def _qk_args(q, k, wq, wk, table, pos, pairing, extra=()):
     _vec(wk, d, q.dtype, "wk")
     n_pos = 0
     if table is not None:
-        n_pos = table.shape[0]
-        _need(table.dtype == torch.float32 and tuple(table.shape) == (n_pos, d // 2, 2)
-              and table.is_contiguous(), f"table must be fp32 [n_pos, {d // 2}, 2], contiguous")
+        n_pos = table.shape[0] if table.dim() == 3 else -1
+        if table.dtype != torch.float32 or table.shape != (n_pos, d // 2, 2) or not table.is_contiguous():
+            raise T2IError(2, f"table must be fp32 [n_pos, {d // 2}, 2], contiguous")
     _need(pos is None or table is not None, "pos goes with a table", 1)
     _vec(pos, rows, torch.int32, "pos")
     return dev, dt, pr, rows, hq, hk, d, ldq, ldk, n_pos
