@@ -2,18 +2,36 @@
 // feed-forward and its gradients.  bf16 and 8-bit operands go through the tiles
 // of gemm_tile.h, fp32 ones through gemm_f32_tile_kernel:
 //
-// One product C[m][n] = sum_k a(m, k) b(n, k) on BM x 64 tiles by 4 waves of
-// BM / 2 x 32 (v_mfma_f32_16x16x4_f32), 32 values of k at a time through two LDS
-// stages, the next step's operands on their way into registers meanwhile.  A
-// stage holds [row][k] in rows of 144 bytes; a lane's 16 bytes are k = 4 g .. 4 g + 3
-// of its row and feed four MFMAs, which between them take 16 of k in an order of
-// their own, the same for both operands.  Reads come from different banks (36
-// dwords a row: 16 rows, 16 places).  VEC: operands are read 16 bytes at a time
+// One product C[m][n] = sum_k a(m, k) b(n, k) on BM x BN tiles by 2 x 2 waves
+// (v_mfma_f32_16x16x4_f32), 32 values of k at a time through two LDS stages, the
+// next step's operands on their way into registers meanwhile.  A lane's four
+// values k = 4 g .. 4 g + 3 of its row feed four MFMAs, which between them take 16
+// of k in an order of their own, the same for both operands.  An operand whose k
+// runs along its rows is staged as [row][k] in rows of 36 dwords (16-byte reads of
+// 16 rows from 16 places), one whose k runs across them as [k][row] in rows of R + 4
+// (4-byte reads of four k from four places): neither meets itself in a bank.  What
+// bounds the 64 x 64 tile is the operands' way from L2 (16 bytes per clock and CU at
+// the matrix cores' full rate), hence 128 x 128 where enough of them fill the chip.
+// VEC: operands are read 16 bytes at a time
 // (rows of whole, aligned 16-byte pieces), else by element; addresses stay inside
 // the operand and what lies outside is taken as 0, without branches.
 #include "gemm_tile.h"
 
 namespace t2i {
+
+// ---- tile shapes.  The shape whose rounds of 256 workgroups cost least.
+struct TileChoice { int bm, bn, cost; };
+static int choose_tile(const TileChoice* c, int n, long rows, long cols) {
+  int best = 0;
+  double least = 0;
+  for (int i = 0; i < n; ++i) {
+    const long tiles = ((rows + c[i].bm - 1) / c[i].bm) * ((cols + c[i].bn - 1) / c[i].bn);
+    const double cost = (double)((tiles + 255) / 256) * c[i].cost;
+    if (i == 0 || cost < least) least = cost, best = i;
+  }
+  return best;
+}
+// ---- fp32
 
 // Rows [0, rows) x columns [0, cols) of a row-major matrix.  along: the k axis
 // runs along the rows (contiguous in memory), else across them.
@@ -62,22 +80,28 @@ __device__ __forceinline__ bool inside(const TwoRows& m, int& y, int& x) {
   return (y < m.half ? y : y - m.half) < m.rows && x < m.cols;
 }
 
-template <int BM, bool VEC, class LA, class LB, class EP>
-__global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep, int tiles_n, int K) {
-  constexpr int BK = 32, LD = 36, TM = BM / 32;
-  __shared__ __attribute__((aligned(16))) float smem[2][(BM + 64) * LD];
+template <int BM, int BN, bool VEC, class LA, class LB, class EP>
+__global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep, TileShape s, int K) {
+  constexpr int BK = 32, LD = 36, TM = BM / 32, TN = BN / 32;
+  constexpr int SA = LA::along ? BM * LD : BK * (BM + 4), SB = LB::along ? BN * LD : BK * (BN + 4);
+  __shared__ __attribute__((aligned(16))) float smem[2][SA + SB];
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int wm = wave >> 1, wn = wave & 1, fr = lane & 15, g = lane >> 4;
-  const int m0 = (int)(blockIdx.x / (unsigned)tiles_n) * BM, n0 = (int)(blockIdx.x % (unsigned)tiles_n) * 64;
-  // a thread's pieces of four: along k of one row, or four rows' of one k
-  f32x4 ra[BM / 32], rb[2];
-  auto load = [&](const auto& op, int r0, int k0, int c, int R) -> f32x4 {
+  int tm, tn;
+  tile_place(s, blockIdx.x, gridDim.x, tm, tn);
+  const int m0 = tm * BM, n0 = tn * BN;
+  // a thread's pieces i of four: along k of one row, or four rows' of one k; by
+  // element, four that lie 256 elements of the stage apart, so that neighbouring
+  // lanes read neighbouring addresses either way
+  f32x4 ra[BM / 32], rb[BN / 32];
+  auto load = [&](const auto& op, int r0, int k0, int i, int R) -> f32x4 {
     using O = typename std::decay<decltype(op)>::type;
     f32x4 v;
     int y, x;
-    if constexpr (O::along) y = r0 + c / 8, x = k0 + c % 8 * 4;
-    else y = k0 + c / (R / 4), x = r0 + c % (R / 4) * 4;
     if constexpr (VEC) {
+      const int c = tid + i * 256;
+      if constexpr (O::along) y = r0 + c / 8, x = k0 + c % 8 * 4;
+      else y = k0 + c / (R / 4), x = r0 + c % (R / 4) * 4;
       const bool in = inside(op, y, x);
       const f32x4 w = *(const f32x4*)op.at(y, min(x, op.cols - 4));
 #pragma unroll
@@ -85,9 +109,11 @@ __global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep,
     } else {
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        int ye = y, xe = x + e;
-        const bool in = inside(op, ye, xe);
-        const float w = *op.at(ye, min(xe, op.cols - 1));
+        const int c = tid + (i * 4 + e) * 256;
+        if constexpr (O::along) y = r0 + c / BK, x = k0 + c % BK;
+        else y = k0 + c / R, x = r0 + c % R;
+        const bool in = inside(op, y, x);
+        const float w = *op.at(y, min(x, op.cols - 1));
         v[e] = in ? w : 0.f;
       }
     }
@@ -95,46 +121,57 @@ __global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep,
   };
   auto fetch = [&](int k0) {
 #pragma unroll
-    for (int i = 0; i < BM / 32; ++i) ra[i] = load(la, m0, k0, tid + i * 256, BM);
+    for (int i = 0; i < BM / 32; ++i) ra[i] = load(la, m0, k0, i, BM);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) rb[i] = load(lb, n0, k0, tid + i * 256, 64);
+    for (int i = 0; i < BN / 32; ++i) rb[i] = load(lb, n0, k0, i, BN);
   };
-  auto put = [&](bool along, float* s, int c, int R, f32x4 v) {
-    if (along) {
-      *(f32x4*)(s + c / 8 * LD + c % 8 * 4) = v;
+  auto put = [&](bool along, float* p, int i, int R, f32x4 v) {
+    if constexpr (VEC) {
+      const int c = tid + i * 256;
+      *(f32x4*)(along ? p + c / 8 * LD + c % 8 * 4 : p + c / (R / 4) * (R + 4) + c % (R / 4) * 4) = v;
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) s[(c % (R / 4) * 4 + e) * LD + c / (R / 4)] = v[e];
+      for (int e = 0; e < 4; ++e) {
+        const int c = tid + (i * 4 + e) * 256;
+        p[along ? c / BK * LD + c % BK : c / R * (R + 4) + c % R] = v[e];
+      }
     }
   };
-  f32x4 acc[TM][2];
+  auto frag = [&](bool along, const float* p, int row, int k, int R) -> f32x4 {
+    if (along) return *(const f32x4*)(p + row * LD + k);
+    f32x4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] = p[(k + e) * (R + 4) + row];
+    return v;
+  };
+  f32x4 acc[TM][TN];
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int j = 0; j < 2; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
   fetch(0);
   int stage = 0;
   for (int k0 = 0; k0 < K; k0 += BK, stage ^= 1) {
-    float *sA = smem[stage], *sB = sA + BM * LD;
+    float *sA = smem[stage], *sB = sA + SA;
 #pragma unroll
-    for (int i = 0; i < BM / 32; ++i) put(LA::along, sA, tid + i * 256, BM, ra[i]);
+    for (int i = 0; i < BM / 32; ++i) put(LA::along, sA, i, BM, ra[i]);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) put(LB::along, sB, tid + i * 256, 64, rb[i]);
+    for (int i = 0; i < BN / 32; ++i) put(LB::along, sB, i, BN, rb[i]);
     __syncthreads();   // (the other stage was read before this step's writes: one barrier a step)
     if (k0 + BK < K) fetch(k0 + BK);
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      f32x4 a[TM], b[2];
+      f32x4 a[TM], b[TN];
 #pragma unroll
-      for (int i = 0; i < TM; ++i) a[i] = *(const f32x4*)(sA + (wm * (BM / 2) + i * 16 + fr) * LD + h * 16 + g * 4);
+      for (int i = 0; i < TM; ++i) a[i] = frag(LA::along, sA, wm * (BM / 2) + i * 16 + fr, h * 16 + g * 4, BM);
 #pragma unroll
-      for (int j = 0; j < 2; ++j) b[j] = *(const f32x4*)(sB + (wn * 32 + j * 16 + fr) * LD + h * 16 + g * 4);
+      for (int j = 0; j < TN; ++j) b[j] = frag(LB::along, sB, wn * (BN / 2) + j * 16 + fr, h * 16 + g * 4, BN);
 #pragma unroll
       for (int e = 0; e < 4; ++e)
 #pragma unroll
         for (int i = 0; i < TM; ++i)
 #pragma unroll
-          for (int j = 0; j < 2; ++j)
+          for (int j = 0; j < TN; ++j)
             acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j][e], a[i][e], acc[i][j], 0, 0, 0);
     }
   }
@@ -142,34 +179,34 @@ __global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep,
 #pragma unroll
   for (int i = 0; i < TM; ++i)
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
-      float v[2];
+    for (int j = 0; j < TN; j += 2)
 #pragma unroll
-      for (int j = 0; j < 2; ++j) v[j] = acc[i][j][r];
-      ep(m0 + wm * (BM / 2) + i * 16 + fr, n0 + wn * 32 + g * 4 + r, v);
-    }
+      for (int r = 0; r < 4; ++r) {
+        const float v[2] = {acc[i][j][r], acc[i][j + 1][r]};
+        ep(m0 + wm * (BM / 2) + i * 16 + fr, n0 + wn * (BN / 2) + j * 16 + g * 4 + r, v);
+      }
 }
 
-template <int BM, class LA, class LB, class EP>
+template <int BM, int BN, class LA, class LB, class EP>
 static void gemm_f32_launch(bool vec, const LA& la, const LB& lb, const EP& ep, int M, int N, int K, hipStream_t st) {
-  const int tn = (N + 63) / 64;
-  const dim3 grid((unsigned)((long)((M + BM - 1) / BM) * tn));
+  TileShape s{(M + BM - 1) / BM, (N + BN - 1) / BN, 8, 0, 0, 0};
+  const dim3 grid((unsigned)(s.tiles_m * s.tiles_n));
   if (vec)
-    hipLaunchKernelGGL((gemm_f32_tile_kernel<BM, true, LA, LB, EP>), grid, dim3(256), 0, st, la, lb, ep, tn, K);
+    hipLaunchKernelGGL((gemm_f32_tile_kernel<BM, BN, true, LA, LB, EP>), grid, dim3(256), 0, st, la, lb, ep, s, K);
   else
-    hipLaunchKernelGGL((gemm_f32_tile_kernel<BM, false, LA, LB, EP>), grid, dim3(256), 0, st, la, lb, ep, tn, K);
+    hipLaunchKernelGGL((gemm_f32_tile_kernel<BM, BN, false, LA, LB, EP>), grid, dim3(256), 0, st, la, lb, ep, s, K);
 }
 
 template <class LA, class LB, class EP>
-static hipError_t gemm_f32_tile(size_t bits, const LA& la, const LB& lb, const EP& ep, int M,
-                                int N, int K, hipStream_t st) {
-  const bool vec = bits % 16 == 0 && la.ld % 4 == 0 && lb.ld % 4 == 0 &&
-                   la.cols % 4 == 0 && lb.cols % 4 == 0;
-  // 32-row tiles where they spread over the CUs better: a tile of half the size
-  // takes a little more than half the time
-  const long t64 = (long)((M + 63) / 64) * ((N + 63) / 64), t32 = (long)((M + 31) / 32) * ((N + 63) / 64);
-  if ((t32 + 255) / 256 * 11 < (t64 + 255) / 256 * 20) gemm_f32_launch<32>(vec, la, lb, ep, M, N, K, st);
-  else gemm_f32_launch<64>(vec, la, lb, ep, M, N, K, st);
+static hipError_t gemm_f32_tile(size_t bits, const LA& la, const LB& lb, const EP& ep, int M, int N, int K,
+                                hipStream_t st) {
+  const bool vec = bits % 16 == 0 && la.ld % 4 == 0 && lb.ld % 4 == 0 && la.cols % 4 == 0 && lb.cols % 4 == 0;
+  constexpr TileChoice tiles[] = {{128, 128, 80}, {64, 64, 24}, {32, 64, 13}};
+  switch (choose_tile(tiles, 3, M, N)) {
+    case 0: gemm_f32_launch<128, 128>(vec, la, lb, ep, M, N, K, st); break;
+    case 1: gemm_f32_launch<64, 64>(vec, la, lb, ep, M, N, K, st); break;
+    default: gemm_f32_launch<32, 64>(vec, la, lb, ep, M, N, K, st);
+  }
   return hipGetLastError();
 }
 
@@ -248,7 +285,7 @@ __global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a,
   constexpr int THREADS = D::NW * 64, NE = D::BM + (KIND == EPI_RESID_GATED ? 3 : 2) * D::BN;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + NE * 4];
   int tm, tn;
-  P::place(s, blockIdx.x, gridDim.x, tm, tn);
+  tile_place(s, blockIdx.x, gridDim.x, tm, tn);
   const int m0 = tm * D::BM, n0 = tn * D::BN;
   auto value = [&](int x) -> float {
     if (x < D::BM) return e.sa[min(m0 + x, M - 1)];
@@ -312,7 +349,7 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
   constexpr int THREADS = D::NW * 64, H = D::BN / 2, TH = D::TN / 2;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + D::BN * 4];
   int tm, tn;
-  P::place(s, blockIdx.x, gridDim.x, tm, tn);
+  tile_place(s, blockIdx.x, gridDim.x, tm, tn);
   const int m0 = tm * D::BM, f0 = tn * H;
   auto value = [&](int x) -> float {
     if (!p.bg) return 0.f;
@@ -382,7 +419,7 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, 
   using P = TileProduct<D, false, false, true, false, true>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
-  P::place(s, blockIdx.x, gridDim.x, tm, tn);
+  tile_place(s, blockIdx.x, gridDim.x, tm, tn);
   typename P::Acc acc[D::TM][D::TN];
   P::run(smem, a, b, s, tm * D::BM, tn * D::BN, acc);
   store_tile<D, P>(acc, dx, ldx, tm * D::BM, tn * D::BN, M, K);
@@ -396,7 +433,7 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, 
   using P = TileProduct<D, false, true, true, false, false>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
-  P::place(s, blockIdx.x, gridDim.x, tm, tn);
+  tile_place(s, blockIdx.x, gridDim.x, tm, tn);
   const bool up = tm >= half;
   const int m0 = (up ? tm - half : tm) * D::BM;
   if (up) a.p += shift;
@@ -405,18 +442,7 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, 
   store_tile<D, P>(acc, up ? du : dg, ldw, m0, tn * D::BN, F, K);
 }
 
-// ---- tile shapes.  The shape whose rounds of 256 workgroups cost least.
-struct TileChoice { int bm, bn, cost; };
-static int choose_tile(const TileChoice* c, int n, long rows, long cols) {
-  int best = 0;
-  double least = 0;
-  for (int i = 0; i < n; ++i) {
-    const long tiles = ((rows + c[i].bm - 1) / c[i].bm) * ((cols + c[i].bn - 1) / c[i].bn);
-    const double cost = (double)((tiles + 255) / 256) * c[i].cost;
-    if (i == 0 || cost < least) least = cost, best = i;
-  }
-  return best;
-}
+// ---- launches
 using Tile256 = TileDims<256, 256, 2, 4, 2>;
 using Tile128 = TileDims<128, 128, 2, 4, 4>;
 using Tile64 = TileDims<64, 128, 2, 4, 4>;

@@ -88,6 +88,16 @@ struct TileShape {
   int half;          // steps in the first matrix of a two-matrix contraction
 };
 
+// The tile of a workgroup: tiles of one XCD are consecutive and walk group_m row
+// blocks down before moving one column block right, sharing both operands in its L2
+__device__ __forceinline__ void tile_place(const TileShape& s, int block, int blocks, int& tm, int& tn) {
+  const int tile = tile_of_block(block, blocks);
+  const int per_group = s.group_m * s.tiles_n, grp = tile / per_group, first = grp * s.group_m;
+  const int rows_in = min(s.tiles_m - first, s.group_m), in_grp = tile - grp * per_group;
+  tm = first + in_grp % rows_in;
+  tn = in_grp / rows_in;
+}
+
 constexpr uint32_t kTileOff = 0x80000000u;   // behind every resource: reads as zero
 
 template <int BM_, int BN_, int WGM_, int WGN_, int ST_>
@@ -321,17 +331,6 @@ struct TileProduct {
     half0(slot);
 #pragma unroll
     for (int j = S; j < TN; ++j) column(j, a1);
-  }
-
-  // first row and column (KC b with two matrices: of either) of this workgroup's
-  // tile: tiles of one XCD are consecutive and walk group_m row blocks down
-  // before moving one column block right, sharing both operands in its L2
-  static __device__ __forceinline__ void place(const TileShape& s, int block, int blocks, int& tm, int& tn) {
-    const int tile = tile_of_block(block, blocks);
-    const int per_group = s.group_m * s.tiles_n, grp = tile / per_group, first = grp * s.group_m;
-    const int rows_in = min(s.tiles_m - first, s.group_m), in_grp = tile - grp * per_group;
-    tm = first + in_grp % rows_in;
-    tn = in_grp / rows_in;
   }
 };
 
