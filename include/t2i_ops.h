@@ -233,7 +233,7 @@ t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F,
  * the result does not depend on what it holds.  No output may overlap an
  * input.  Every sum has a fixed order.
  */
-size_t t2i_op_gated_linear_backward_ws_bytes(int32_t dtype, int32_t M, int32_t F);
+size_t t2i_op_gated_linear_backward_ws_bytes(int32_t dtype, int32_t M, int32_t F, int32_t K);
 t2i_status t2i_op_gated_linear_backward(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,
                                         const void* A, int32_t lda, const void* Wg, const void* Wu,
                                         int32_t ldw, const float* pre, int32_t ldp, const void* dout,

@@ -115,7 +115,7 @@ SIGNATURES = {
                                i32, vp, vp, vp]),
     "t2i_op_gated_linear": (i32, [i32, i32, i32, i32, i32, vp, i32, vp, vp, i32, vp, vp, vp, i32,
                                   vp, i32, vp]),
-    "t2i_op_gated_linear_backward_ws_bytes": (sz, [i32, i32, i32]),
+    "t2i_op_gated_linear_backward_ws_bytes": (sz, [i32, i32, i32, i32]),
     "t2i_op_gated_linear_backward": (i32, [i32, i32, i32, i32, i32, vp, i32, vp, vp, i32, vp, i32,
                                            vp, i32, vp, i32, vp, vp, i32, vp, vp, vp, sz, vp]),
     "t2i_op_qk_norm_rope": (i32, [i32, i32, i32, i32, i32, vp, i32, vp, i32, vp, vp, f32, i32, vp,

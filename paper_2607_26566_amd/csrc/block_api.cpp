@@ -170,9 +170,13 @@ t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F,
   return done(launch_gated_linear(bf, g, M, F, K, (hipStream_t)stream));
 }
 
-size_t t2i_op_gated_linear_backward_ws_bytes(int32_t dtype, int32_t M, int32_t F) {
-  if (bad_dtype(dtype) || M < 1 || F < 1 || F > (1 << 28) || too_large(M, 2 * F)) return 0;
-  return gated_dgu_bytes(dtype, M, F) + (size_t)gate_row_blocks(M, F) * 2 * gated_cols(F) * 4;
+size_t t2i_op_gated_linear_backward_ws_bytes(int32_t dtype, int32_t M, int32_t F, int32_t K) {
+  if (bad_dtype(dtype) || M < 1 || F < 1 || K < 1 || K > (1 << 30) || F > (1 << 28) || too_large(M, 2 * F) ||
+      too_large(M, K) || too_large(F, K))
+    return 0;
+  // dg | du, the bias gradients' column sums, the products' partial sums
+  const size_t partial = ((size_t)gate_row_blocks(M, F) * 2 * gated_cols(F) * 4 + 255) / 256 * 256;
+  return gated_dgu_bytes(dtype, M, F) + partial + (dtype == T2I_BF16 ? gated_split_floats(M, F, K) * 4 : 0);
 }
 
 t2i_status t2i_op_gated_linear_backward(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,
@@ -204,14 +208,15 @@ t2i_status t2i_op_gated_linear_backward(int32_t dtype, int32_t act, int32_t M, i
       off(dWg, al) || off(dWu, al) || off(dbg, al) || off(dbu, al) || off(ws, 256))
     return ops_fail(T2I_ERR_INVALID_ARG,
                     "pointers need 16-byte (bf16) or 4-byte (fp32) alignment, ws 256-byte");
-  if (ws_bytes < t2i_op_gated_linear_backward_ws_bytes(dtype, M, F))
+  if (ws_bytes < t2i_op_gated_linear_backward_ws_bytes(dtype, M, F, K))
     return ops_fail(T2I_ERR_WORKSPACE, "workspace too small");
   hipStream_t st = (hipStream_t)stream;
   float* partial = (float*)((char*)ws + gated_dgu_bytes(dtype, M, F));
+  float* slices = partial + ((size_t)gate_row_blocks(M, F) * 2 * gated_cols(F) + 63) / 64 * 64;
   hipError_t e = launch_gate_grad(bf, act, M, F, pre, ldp, dout, ldd, ws, dbg ? partial : nullptr, st);
   if (e == hipSuccess && dbg) e = launch_gate_bias_grad(bf, M, F, partial, dbg, dbu, st);
-  if (e == hipSuccess && dA) e = launch_gated_dx(bf, M, F, K, ws, Wg, Wu, ldw, dA, ldda, st);
-  if (e == hipSuccess && dw) e = launch_gated_dw(bf, M, F, K, ws, A, lda, dWg, dWu, lddw, st);
+  if (e == hipSuccess && dA) e = launch_gated_dx(bf, M, F, K, ws, Wg, Wu, ldw, dA, ldda, slices, st);
+  if (e == hipSuccess && dw) e = launch_gated_dw(bf, M, F, K, ws, A, lda, dWg, dWu, lddw, slices, st);
   return done(e);
 }
 

@@ -15,22 +15,32 @@
 // VEC: operands are read 16 bytes at a time
 // (rows of whole, aligned 16-byte pieces), else by element; addresses stay inside
 // the operand and what lies outside is taken as 0, without branches.
+#include <algorithm>
+
 #include "gemm_tile.h"
 
 namespace t2i {
 
-// ---- tile shapes.  The shape whose rounds of 256 workgroups cost least.
-struct TileChoice { int bm, bn, cost; };
-static int choose_tile(const TileChoice* c, int n, long rows, long cols) {
-  int best = 0;
-  double least = 0;
-  for (int i = 0; i < n; ++i) {
+// ---- tile shapes.  `per_cu` workgroups of a shape share a CU.  A launch of n
+// tiles takes rounds of 256 per_cu; a round takes `full` us per k step and `end` us
+// for its first loads and its epilogue, the last one `alone` per step if it has 256
+// tiles or fewer.
+struct TileChoice { int bm, bn, per_cu; float alone, full, end; };
+struct TilePick { int shape; float us; };
+template <int N>
+static TilePick choose_tile(const TileChoice (&c)[N], long rows, long cols, int steps, float end_scale) {
+  TilePick best{0, 0.f};
+  for (int i = 0; i < N; ++i) {
     const long tiles = ((rows + c[i].bm - 1) / c[i].bm) * ((cols + c[i].bn - 1) / c[i].bn);
-    const double cost = (double)((tiles + 255) / 256) * c[i].cost;
-    if (i == 0 || cost < least) least = cost, best = i;
+    const long slots = 256L * c[i].per_cu, rest = tiles % slots;
+    const float end = c[i].end * end_scale;
+    const float us = (float)(tiles / slots) * (c[i].full * steps + end) +
+                     (rest == 0 ? 0.f : (rest <= 256 ? c[i].alone : c[i].full) * steps + end);
+    if (i == 0 || us < best.us) best = {i, us};
   }
   return best;
 }
+
 // ---- fp32
 
 // Rows [0, rows) x columns [0, cols) of a row-major matrix.  along: the k axis
@@ -189,7 +199,7 @@ __global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep,
 
 template <int BM, int BN, class LA, class LB, class EP>
 static void gemm_f32_launch(bool vec, const LA& la, const LB& lb, const EP& ep, int M, int N, int K, hipStream_t st) {
-  TileShape s{(M + BM - 1) / BM, (N + BN - 1) / BN, 8, 0, 0, 0};
+  TileShape s{(M + BM - 1) / BM, (N + BN - 1) / BN, 8, 0, 0, 0, 0};
   const dim3 grid((unsigned)(s.tiles_m * s.tiles_n));
   if (vec)
     hipLaunchKernelGGL((gemm_f32_tile_kernel<BM, BN, true, LA, LB, EP>), grid, dim3(256), 0, st, la, lb, ep, s, K);
@@ -201,8 +211,8 @@ template <class LA, class LB, class EP>
 static hipError_t gemm_f32_tile(size_t bits, const LA& la, const LB& lb, const EP& ep, int M, int N, int K,
                                 hipStream_t st) {
   const bool vec = bits % 16 == 0 && la.ld % 4 == 0 && lb.ld % 4 == 0 && la.cols % 4 == 0 && lb.cols % 4 == 0;
-  constexpr TileChoice tiles[] = {{128, 128, 80}, {64, 64, 24}, {32, 64, 13}};
-  switch (choose_tile(tiles, 3, M, N)) {
+  constexpr TileChoice tiles[] = {{128, 128, 1, 80, 80, 0}, {64, 64, 1, 24, 24, 0}, {32, 64, 1, 13, 13, 0}};
+  switch (choose_tile(tiles, M, N, 1, 0.f).shape) {
     case 0: gemm_f32_launch<128, 128>(vec, la, lb, ep, M, N, K, st); break;
     case 1: gemm_f32_launch<64, 64>(vec, la, lb, ep, M, N, K, st); break;
     default: gemm_f32_launch<32, 64>(vec, la, lb, ep, M, N, K, st);
@@ -278,11 +288,17 @@ __device__ __forceinline__ void store4(T* p, int left, bool vec, const float (&v
   }
 }
 
-template <class D, typename T, int KIND>
+// one output of the 8-bit layer before the residual update
+__device__ __forceinline__ float i8_value(int acc, float sa, float sw, float b, int kind) {
+  const float y = fmaf((float)acc * sa, sw, b);
+  return kind == EPI_GELU ? gelu_tanh(y) : kind == EPI_SILU ? silu(y) : y;
+}
+
+template <class D, typename T, bool RES>
 __global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a, TileOperand b, TileShape s,
                                                                   I8Epi e, int M, int N, int vec) {
   using P = TileProduct<D, true, false, false, false, false>;
-  constexpr int THREADS = D::NW * 64, NE = D::BM + (KIND == EPI_RESID_GATED ? 3 : 2) * D::BN;
+  constexpr int THREADS = D::NW * 64, NE = D::BM + (RES ? 3 : 2) * D::BN;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + NE * 4];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
@@ -292,7 +308,7 @@ __global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a,
     const int n = min(n0 + (x - D::BM) % D::BN, N - 1), which = (x - D::BM) / D::BN;
     if (which == 0) return e.sw[n];
     if (which == 1) return e.bias ? to_f32(((const T*)e.bias)[n]) : 0.f;
-    return e.gate[n];
+    return e.kind == EPI_RESID_GATED ? e.gate[n] : 1.f;
   };
   Staged<NE, THREADS, decltype(value)> st;
   st.fetch(value);
@@ -315,15 +331,10 @@ __global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a,
       const f32x4 sw = *(const f32x4*)(ev + D::BM + nl), bb = *(const f32x4*)(ev + D::BM + D::BN + nl);
       float y[4];
 #pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        y[r] = fmaf((float)acc[i][j][r] * sa, sw[r], bb[r]);
-        if (KIND == EPI_GELU) y[r] = gelu_tanh(y[r]);
-        if (KIND == EPI_SILU) y[r] = silu(y[r]);
-      }
-      if constexpr (KIND >= EPI_RESID) {
+      for (int r = 0; r < 4; ++r) y[r] = i8_value(acc[i][j][r], sa, sw[r], bb[r], e.kind);
+      if constexpr (RES) {
         float* x = e.x + (size_t)m * e.ldx + n;
-        f32x4 gt{1.f, 1.f, 1.f, 1.f};
-        if (KIND == EPI_RESID_GATED) gt = *(const f32x4*)(ev + D::BM + 2 * D::BN + nl);
+        const f32x4 gt = *(const f32x4*)(ev + D::BM + 2 * D::BN + nl);
         float xv[4];
         if (vec && left >= 4) {
           const f32x4 x4 = *(const f32x4*)x;
@@ -390,10 +401,11 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
   }
 }
 
-// the gradients' products: C stored as bf16 (row stride ldc).  b is a KR operand:
-// a pair of fragments holds 8 neighbouring columns of a row (N % 8 == 0)
-template <class D, class P>
-__device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D::TN], bf16* C, int ldc, int m0,
+// The gradients' products.  b is a KR operand: a pair of fragments holds 8
+// neighbouring columns of a row (N % 8 == 0).  Stored as bf16 (row stride ldc), or
+// as fp32 partial sums (row stride N) where the contraction is split.
+template <class D, class P, typename T>
+__device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D::TN], T* C, int ldc, int m0,
                                            int n0, int M, int N) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
   const int mw = m0 + (wave / D::WGN) * D::WM, nw = n0 + (wave % D::WGN) * D::WN;
@@ -405,49 +417,113 @@ __device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D
     for (int j = 0; j < D::TN; j += 2) {
       const int n = nw + P::col_of(j, g * 4);
       if (n >= N) continue;
-      bf16x8 v;
+      T* p = C + (size_t)m * ldc + n;
+      if constexpr (sizeof(T) == 2) {
+        bf16x8 v;
 #pragma unroll
-      for (int r = 0; r < 4; ++r) v[2 * r] = (bf16)acc[i][j][r], v[2 * r + 1] = (bf16)acc[i][j + 1][r];
-      *(bf16x8*)(C + (size_t)m * ldc + n) = v;
+        for (int r = 0; r < 4; ++r) v[2 * r] = (bf16)acc[i][j][r], v[2 * r + 1] = (bf16)acc[i][j + 1][r];
+        *(bf16x8*)p = v;
+      } else {
+        *(f32x4*)p = f32x4{acc[i][j][0], acc[i][j + 1][0], acc[i][j][1], acc[i][j + 1][1]};
+        *(f32x4*)(p + 4) = f32x4{acc[i][j][2], acc[i][j + 1][2], acc[i][j][3], acc[i][j + 1][3]};
+      }
     }
   }
 }
 
+// A contraction split over gridDim.y slices of `per` steps: slice y writes fp32
+// partial sums [rows][cols] behind those of the slices before it, which
+// split_sum_kernel adds up in order.
+struct Split {
+  float* partial;   // NULL: not split
+  int per;
+};
+__device__ __forceinline__ void take_slice(const Split& sp, TileShape& s) {
+  s.first = (int)blockIdx.y * sp.per;
+  s.steps = min(sp.per, s.steps - s.first);
+}
+
 template <class D>
-__global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, TileOperand b, TileShape s,
+__global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
                                                                  bf16* dx, int ldx, int M, int K) {
   using P = TileProduct<D, false, false, true, false, true>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
+  if (sp.partial) take_slice(sp, s);
   typename P::Acc acc[D::TM][D::TN];
   P::run(smem, a, b, s, tm * D::BM, tn * D::BN, acc);
-  store_tile<D, P>(acc, dx, ldx, tm * D::BM, tn * D::BN, M, K);
+  if (sp.partial)
+    store_tile<D, P>(acc, sp.partial + (size_t)blockIdx.y * M * K, K, tm * D::BM, tn * D::BN, M, K);
+  else
+    store_tile<D, P>(acc, dx, ldx, tm * D::BM, tn * D::BN, M, K);
 }
 
-// row blocks [0, half) are dWg's, the others dWu's (their operand lies `shift`
-// bytes further); only one of the two wanted: both pointers and no shift
+// row blocks [0, half) are the first output's, the others the second's (their
+// operand lies `shift` bytes further)
 template <class D>
-__global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, TileOperand b, TileShape s, int half,
-                                                                 int shift, bf16* dg, bf16* du, int ldw, int F, int K) {
+__global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
+                                                                 int half, int shift, bf16* d0, bf16* d1, int ldw,
+                                                                 int F, int K) {
   using P = TileProduct<D, false, true, true, false, false>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
-  const bool up = tm >= half;
-  const int m0 = (up ? tm - half : tm) * D::BM;
-  if (up) a.p += shift;
+  if (sp.partial) take_slice(sp, s);
+  const bool second = tm >= half;
+  const int m0 = (second ? tm - half : tm) * D::BM;
+  if (second) a.p += shift;
   typename P::Acc acc[D::TM][D::TN];
   P::run(smem, a, b, s, m0, tn * D::BN, acc);
-  store_tile<D, P>(acc, up ? du : dg, ldw, m0, tn * D::BN, F, K);
+  if (sp.partial) {
+    const size_t of = (size_t)blockIdx.y * (s.tiles_m / half) * F + (second ? F : 0);
+    store_tile<D, P>(acc, sp.partial + of * K, K, m0, tn * D::BN, F, K);
+  } else {
+    store_tile<D, P>(acc, second ? d1 : d0, ldw, m0, tn * D::BN, F, K);
+  }
+}
+
+// out (rows [0, half) to o0, the others to o1) = the sum of the slices' partials
+// [rows][cols], in ascending slice order; cols % 8 == 0, one thread per 8 columns
+__global__ __launch_bounds__(256) void split_sum_kernel(const float* __restrict__ partial, int slices, long rows,
+                                                        long half, int cols, bf16* o0, bf16* o1, int ld) {
+  const long x = blockIdx.x * 256L + threadIdx.x, n8 = cols / 8;
+  if (x >= rows * n8) return;
+  const long r = x / n8;
+  const int c = (int)(x - r * n8) * 8;
+  const float* p = partial + r * cols + c;
+  f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
+  for (int i = 1; i < slices; ++i) {
+    p += rows * cols;
+    a += *(const f32x4*)p;
+    b += *(const f32x4*)(p + 4);
+  }
+  bf16x8 v;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) v[i] = (bf16)a[i], v[4 + i] = (bf16)b[i];
+  *(bf16x8*)((r < half ? o0 + r * ld : o1 + (r - half) * ld) + c) = v;
 }
 
 // ---- launches
+// Shapes of the bf16 and 8-bit products, measured on products of 4096 x 20480 x 4096
+// (full), 333 rows (alone) and K = 1152 (end; with bf16 outputs for every column of
+// the tile, half of it for the gated block).  Two stages and several workgroups per
+// CU where the tiles fill the chip -- the epilogue of one then runs beside the loop
+// of another --, four stages and one where they do not: 7531 x 4608 x 1152 in 8 bits
+// 84 us on 256 x 256, 63 on 128 x 128 with two stages, 89 with four; 600 x 1152 x
+// 4608 57, 28 and 21, 16 on 64 x 128 with four.
 using Tile256 = TileDims<256, 256, 2, 4, 2>;
-using Tile128 = TileDims<128, 128, 2, 4, 4>;
-using Tile64 = TileDims<64, 128, 2, 4, 4>;
-using Tile32 = TileDims<32, 128, 1, 4, 4>;
-constexpr TileChoice kTiles[] = {{256, 256, 100}, {128, 128, 32}, {64, 128, 20}, {32, 128, 15}};
+using Tile256n = TileDims<256, 128, 4, 2, 3>;
+using Tile128 = TileDims<128, 128, 2, 4, 2>;
+using Tile128d = TileDims<128, 128, 2, 4, 4>;
+using Tile64 = TileDims<64, 128, 2, 4, 2>;
+using Tile64d = TileDims<64, 128, 2, 4, 4>;
+using Tile32d = TileDims<32, 128, 1, 4, 4>;
+constexpr int kMaxSlices = 16;
+constexpr TileChoice kTiles[] = {{256, 256, 1, 1.60f, 1.60f, 13.f}, {256, 128, 1, 0.95f, 0.95f, 8.f},
+                                 {128, 128, 2, 0.72f, 1.02f, 6.f},  {128, 128, 1, 0.61f, 0.61f, 5.f},
+                                 {64, 128, 3, 0.60f, 1.01f, 4.5f},  {64, 128, 1, 0.48f, 0.48f, 3.f},
+                                 {32, 128, 1, 0.41f, 0.41f, 2.f}};
 
 template <class D>
 static TileShape tile_shape(int rows, int cols, int steps, int kbytes, int half) {
@@ -458,6 +534,7 @@ static TileShape tile_shape(int rows, int cols, int steps, int kbytes, int half)
   s.steps = steps;
   s.kbytes = kbytes;
   s.half = half;
+  s.first = 0;
   return s;
 }
 
@@ -468,66 +545,104 @@ static void i8_launch(const TileOperand& a, const TileOperand& b, const I8Epi& e
   const bool res = e.kind >= EPI_RESID;
   const size_t align = res ? (size_t)e.x | (size_t)(e.ldx * 4) : (size_t)e.out | (size_t)(e.ldo * (e.bf16_out ? 2 : 4));
   const int vec = align % (res || !e.bf16_out ? 16 : 8) == 0 && (size_t)e.xb % 8 == 0;
-#define T2I_I8(T, KIND)                                                                                       \
-  hipLaunchKernelGGL((linear_i8_kernel<D, T, KIND>), grid, dim3(D::NW * 64), 0, st, a, b, s, e, M, N, vec)
-#define T2I_I8K(T)                                     \
-  switch (e.kind) {                                    \
-    case EPI_STORE: T2I_I8(T, EPI_STORE); break;       \
-    case EPI_GELU: T2I_I8(T, EPI_GELU); break;         \
-    case EPI_SILU: T2I_I8(T, EPI_SILU); break;         \
-    case EPI_RESID: T2I_I8(T, EPI_RESID); break;       \
-    default: T2I_I8(T, EPI_RESID_GATED); break;        \
+#define T2I_I8(T, RES)                                                                                         \
+  hipLaunchKernelGGL((linear_i8_kernel<D, T, RES>), grid, dim3(D::NW * 64), 0, st, a, b, s, e, M, N, vec)
+  if (e.bf16_out) {
+    if (res) T2I_I8(bf16, true);
+    else T2I_I8(bf16, false);
+  } else {
+    if (res) T2I_I8(float, true);
+    else T2I_I8(float, false);
   }
-  if (e.bf16_out) T2I_I8K(bf16) else T2I_I8K(float)
-#undef T2I_I8K
 #undef T2I_I8
 }
 
-#define T2I_TILES(rows, cols, CALL)                              \
-  switch (choose_tile(kTiles, 4, rows, cols)) {                  \
-    case 0: { using D = Tile256; CALL; break; }                  \
-    case 1: { using D = Tile128; CALL; break; }                  \
-    case 2: { using D = Tile64; CALL; break; }                   \
-    default: { using D = Tile32; CALL; break; }                  \
+#define T2I_TILES(SHAPE, CALL)                  \
+  switch (SHAPE) {                               \
+    case 0: { using D = Tile256; CALL; break; }  \
+    case 1: { using D = Tile256n; CALL; break; } \
+    case 2: { using D = Tile128; CALL; break; }  \
+    case 3: { using D = Tile128d; CALL; break; } \
+    case 4: { using D = Tile64; CALL; break; }   \
+    case 5: { using D = Tile64d; CALL; break; }  \
+    default: { using D = Tile32d; CALL; break; } \
   }
 
 hipError_t launch_linear_i8(const int8_t* A, int lda, const int8_t* W, int ldw, int M, int N, int K,
                             const I8Epi& e, hipStream_t st) {
   const TileOperand a{(const char*)A, nullptr, (uint32_t)lda, M, 0}, b{(const char*)W, nullptr, (uint32_t)ldw, N, 0};
-  T2I_TILES(M, N, i8_launch<D>(a, b, e, M, N, K, st))
+  T2I_TILES(choose_tile(kTiles, M, N, i8_row(K) / 128, 1.f).shape, i8_launch<D>(a, b, e, M, N, K, st))
   return hipGetLastError();
 }
 
 static hipError_t gated_fwd_bf16(const GatedFwd& p, int M, int F, int K, hipStream_t st) {
   const TileOperand a{(const char*)p.A, nullptr, 2u * p.lda, M, 0},
       b{(const char*)p.Wg, (const char*)p.Wu, 2u * p.ldw, F, 0};
-  T2I_TILES(M, 2L * F, const TileShape s = tile_shape<D>(M, 2 * F, (K + 63) / 64, 2 * K, 0);
+  T2I_TILES(choose_tile(kTiles, M, 2L * F, (K + 63) / 64, 0.5f).shape, const TileShape s = tile_shape<D>(M, 2 * F, (K + 63) / 64, 2 * K, 0);
             hipLaunchKernelGGL((gated_linear_kernel<D>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64),
                                0, st, a, b, s, p, M, F))
   return hipGetLastError();
 }
 
+// Tile shape and slices of a gradient's product: as few slices as keep the time
+// least, counting 4 us for the second launch and the partial sums' way out and back
+// at 4 TB/s (1024 x 9216 x 1152: 63 us on 144 64 x 128 tiles, 41 in slices).
+struct SplitPick { int shape, slices, per; };
+static SplitPick choose_split(long rows, long cols, int steps) {
+  SplitPick best{0, 1, steps};
+  float least = 0.f;
+  for (int n = 1; n <= kMaxSlices; ++n) {
+    const int per = (steps + n - 1) / n, slices = (steps + per - 1) / per;
+    if (slices != n || (n > 1 && per < 4)) continue;
+    const TilePick p = choose_tile(kTiles, rows * n, cols, per, n > 1 ? 2.f : 1.f);
+    const float us = p.us + (n > 1 ? 4.f + (float)n * rows * cols * 8 / 4e6f : 0.f);
+    if (n == 1 || us < least) least = us, best = {p.shape, n, per};
+  }
+  return best;
+}
+
+size_t gated_split_floats(int M, int F, int K) {
+  const SplitPick x = choose_split(M, K, 2 * gated_cols(F) / 64), w = choose_split(2L * F, K, (M + 63) / 64),
+                  w1 = choose_split(F, K, (M + 63) / 64);
+  auto floats = [](const SplitPick& p, size_t n) { return p.slices > 1 ? n * p.slices : 0; };
+  return std::max({floats(x, (size_t)M * K), floats(w, (size_t)2 * F * K), floats(w1, (size_t)F * K)});
+}
+
+static void split_sum(const SplitPick& pick, const float* partial, long rows, long half, int cols, void* o0, void* o1,
+                      int ld, hipStream_t st) {
+  hipLaunchKernelGGL(split_sum_kernel, dim3((unsigned)((rows * (cols / 8) + 255) / 256)), dim3(256), 0, st, partial,
+                     pick.slices, rows, half, cols, (bf16*)o0, (bf16*)o1, ld);
+}
+
 static hipError_t gated_dx_bf16(int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw,
-                                void* dx, int ldx, hipStream_t st) {
+                                void* dx, int ldx, float* partial, hipStream_t st) {
   const int Fp = gated_cols(F);
   const TileOperand a{(const char*)dgu, nullptr, 4u * Fp, M, 0},
       b{(const char*)Wg, (const char*)Wu, 2u * ldw, F, K};
-  T2I_TILES(M, K, const TileShape s = tile_shape<D>(M, K, 2 * Fp / 64, 4 * Fp, Fp / 64);
-            hipLaunchKernelGGL((gated_dx_kernel<D>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64), 0, st,
-                               a, b, s, (bf16*)dx, ldx, M, K))
+  const SplitPick pick = choose_split(M, K, 2 * Fp / 64);
+  const Split sp{pick.slices > 1 ? partial : nullptr, pick.per};
+  T2I_TILES(pick.shape, const TileShape s = tile_shape<D>(M, K, 2 * Fp / 64, 4 * Fp, Fp / 64);
+            hipLaunchKernelGGL((gated_dx_kernel<D>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices),
+                               dim3(D::NW * 64), 0, st, a, b, s, sp, (bf16*)dx, ldx, M, K))
+  if (sp.partial) split_sum(pick, partial, M, M, K, dx, dx, ldx, st);
   return hipGetLastError();
 }
 
 static hipError_t gated_dw_bf16(int M, int F, int K, const void* dgu, const void* A, int lda, void* dWg, void* dWu,
-                                int lddw, hipStream_t st) {
+                                int lddw, float* partial, hipStream_t st) {
   const int Fp = gated_cols(F);
   const int n = dWg && dWu ? 2 : 1;
+  void* const first = dWg ? dWg : dWu;
   const TileOperand a{(const char*)dgu + (dWg ? 0 : 2 * (size_t)Fp), nullptr, 4u * Fp, M, F},
       b{(const char*)A, nullptr, 2u * lda, M, K};
-  T2I_TILES((long)n * F, K, TileShape s = tile_shape<D>(F, K, (M + 63) / 64, 0, 0); const int half = s.tiles_m;
+  const SplitPick pick = choose_split((long)n * F, K, (M + 63) / 64);
+  const Split sp{pick.slices > 1 ? partial : nullptr, pick.per};
+  T2I_TILES(pick.shape, TileShape s = tile_shape<D>(F, K, (M + 63) / 64, 0, 0); const int half = s.tiles_m;
             s.tiles_m *= n;
-            hipLaunchKernelGGL((gated_dw_kernel<D>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64), 0, st,
-                               a, b, s, half, 2 * Fp, (bf16*)(dWg ? dWg : dWu), (bf16*)dWu, lddw, F, K))
+            hipLaunchKernelGGL((gated_dw_kernel<D>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices),
+                               dim3(D::NW * 64), 0, st, a, b, s, sp, half, 2 * Fp, (bf16*)first, (bf16*)dWu, lddw,
+                               F, K))
+  if (sp.partial) split_sum(pick, partial, (long)n * F, F, K, first, dWu, lddw, st);
   return hipGetLastError();
 }
 
@@ -564,14 +679,14 @@ hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& a, int M, int F, in
 }
 
 hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, const void* Wg,
-                           const void* Wu, int ldw, void* dx, int ldx, hipStream_t st) {
-  return is_bf16 ? gated_dx_bf16(M, F, K, dgu, Wg, Wu, ldw, dx, ldx, st)
+                           const void* Wu, int ldw, void* dx, int ldx, float* partial, hipStream_t st) {
+  return is_bf16 ? gated_dx_bf16(M, F, K, dgu, Wg, Wu, ldw, dx, ldx, partial, st)
                  : gated_dx_f32(M, F, K, dgu, Wg, Wu, ldw, dx, ldx, st);
 }
 
 hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, const void* A, int lda,
-                           void* dWg, void* dWu, int lddw, hipStream_t st) {
-  return is_bf16 ? gated_dw_bf16(M, F, K, dgu, A, lda, dWg, dWu, lddw, st)
+                           void* dWg, void* dWu, int lddw, float* partial, hipStream_t st) {
+  return is_bf16 ? gated_dw_bf16(M, F, K, dgu, A, lda, dWg, dWu, lddw, partial, st)
                  : gated_dw_f32(M, F, K, dgu, A, lda, dWg, dWu, lddw, st);
 }
 

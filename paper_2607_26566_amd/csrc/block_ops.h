@@ -62,12 +62,14 @@ hipError_t launch_gate_grad(bool is_bf16, int act, int M, int F, const float* pr
 // dbg[f] / dbu[f] = sum of the partials, in ascending block order
 hipError_t launch_gate_bias_grad(bool is_bf16, int M, int F, const float* partial, void* dbg,
                                  void* dbu, hipStream_t st);
+// fp32 room that the two products below need at `partial` for bf16 operands
+size_t gated_split_floats(int M, int F, int K);
 // dx [M, K] = dg Wg + du Wu
 hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, const void* Wg,
-                           const void* Wu, int ldw, void* dx, int ldx, hipStream_t st);
+                           const void* Wu, int ldw, void* dx, int ldx, float* partial, hipStream_t st);
 // dWg, dWu [F, K] = dg^T A, du^T A (either may be NULL)
 hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, const void* A, int lda,
-                           void* dWg, void* dWu, int lddw, hipStream_t st);
+                           void* dWg, void* dWu, int lddw, float* partial, hipStream_t st);
 
 // ---- query / key norm with rotation
 

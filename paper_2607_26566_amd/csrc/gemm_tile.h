@@ -86,6 +86,7 @@ struct TileShape {
   int steps;         // k steps in all
   int kbytes;        // KC: bytes of a row that hold k
   int half;          // steps in the first matrix of a two-matrix contraction
+  int first;         // the first step (a KC operand's resource starts there, too)
 };
 
 // The tile of a workgroup: tiles of one XCD are consecutive and walk group_m row
@@ -180,14 +181,15 @@ struct TileProduct {
       return __builtin_amdgcn_make_buffer_rsrc((void*)(p + off), 0, 0x7fffffff, 0x00020000);
     };
     auto kr_res = [&](const TileOperand& o, int t, bool segs) {
+      t += s.first;
       const bool second = segs && t >= s.half;
       const int row0 = (second ? t - s.half : t) * 64;
       return __builtin_amdgcn_make_buffer_rsrc((void*)((second ? o.p2 : o.p) + (size_t)row0 * o.ld), 0,
                                                (min(o.rows - row0, 64) - 1) * (int)o.ld + 2 * o.cols, 0x00020000);
     };
-    const __amdgpu_buffer_rsrc_t ra_kc = kc_res(a.p, AKR ? 0 : (size_t)m0 * a.ld);
-    const __amdgpu_buffer_rsrc_t rb_kc = kc_res(b.p, BKR ? 0 : (size_t)n0 * b.ld);
-    const __amdgpu_buffer_rsrc_t rb2_kc = kc_res(DUAL ? b.p2 : b.p, BKR ? 0 : (size_t)n0 * b.ld);
+    const __amdgpu_buffer_rsrc_t ra_kc = kc_res(a.p, AKR ? 0 : (size_t)m0 * a.ld + (size_t)s.first * 128);
+    const __amdgpu_buffer_rsrc_t rb_kc = kc_res(b.p, BKR ? 0 : (size_t)n0 * b.ld + (size_t)s.first * 128);
+    const __amdgpu_buffer_rsrc_t rb2_kc = kc_res(DUAL ? b.p2 : b.p, BKR ? 0 : (size_t)n0 * b.ld + (size_t)s.first * 128);
     auto res_a = [&](int t) { return AKR ? kr_res(a, t, false) : ra_kc; };
     auto res_b = [&](int t) { return BKR ? kr_res(b, t, SEGS) : rb_kc; };
     auto issue = [&](int i, int t, uint32_t slot, const __amdgpu_buffer_rsrc_t& ra,
@@ -201,7 +203,7 @@ struct TileProduct {
         uint32_t v = src[i];
         if (ragged_k && t == KT - 1) {
           const int lr = blk * 8 + (lane >> 3), c = (lane & 7) ^ ((lr >> 1) & 7);
-          if (t * 128 + c * 16 >= s.kbytes) v = kTileOff;
+          if ((s.first + t) * 128 + c * 16 >= s.kbytes) v = kTileOff;
         }
         const bool up = DUAL && !is_a && blk * 8 >= BN / 2;
         __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? ra : up ? rb2_kc : rb, dst, 16, v, t * 128, 0, 0);

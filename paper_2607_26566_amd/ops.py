@@ -211,7 +211,7 @@ def gated_linear_backward(dout: torch.Tensor, x: torch.Tensor, wg: torch.Tensor,
         new = lambda on, *shape: torch.empty(shape, dtype=x.dtype, device=dev) if on else None  # noqa: E731
         dx, dwg, dwu = new(need_dx, M, K), new(need_dw, F, K), new(need_dw, F, K)
         dbg, dbu = new(bias, F), new(bias, F)
-        n = lib.t2i_op_gated_linear_backward_ws_bytes(dt, M, F)
+        n = lib.t2i_op_gated_linear_backward_ws_bytes(dt, M, F, K)
         ws = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)
         _check(lib.t2i_op_gated_linear_backward(
             dt, a, M, F, K, x.data_ptr(), lda, wg.data_ptr(), wu.data_ptr(), ldw, pre.data_ptr(), ldp,

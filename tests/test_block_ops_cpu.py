@@ -161,7 +161,7 @@ GBWD = dict(dtype=BF16, act=_lib.T2I_EPI_SILU, M=3, F=8, K=16, A=P, lda=16, Wg=P
 
 
 def test_gated_linear_backward_refuses():
-    need = t2i.load().t2i_op_gated_linear_backward_ws_bytes(BF16, 3, 8)
+    need = t2i.load().t2i_op_gated_linear_backward_ws_bytes(BF16, 3, 8, 16)
     assert 0 < need <= 1 << 20
     check_refusals("t2i_op_gated_linear_backward", GBWD, [
         (dict(dtype=2), INVALID), (dict(act=4), INVALID), (dict(M=0), SHAPE), (dict(F=0), SHAPE),
@@ -176,7 +176,7 @@ def test_gated_linear_backward_refuses():
         (dict(dWg=P + 8), INVALID), (dict(dWu=P + 8), INVALID), (dict(dbg=P + 8), INVALID),
         (dict(ws=P + 128), INVALID), (dict(ws_bytes=need - 1), WORKSPACE)])
     ws = t2i.load().t2i_op_gated_linear_backward_ws_bytes
-    assert ws(2, 3, 8) == 0 and ws(BF16, 0, 8) == 0 and ws(BF16, 3, 0) == 0
+    assert ws(2, 3, 8, 8) == 0 and ws(BF16, 0, 8, 8) == 0 and ws(BF16, 3, 0, 8) == 0 and ws(F32, 3, 8, 0) == 0
 
 
 QK = dict(dtype=BF16, rows=3, heads_q=2, heads_k=1, head_dim=16, q=P, ldq=32, k=P, ldk=16, wq=None, wk=None,

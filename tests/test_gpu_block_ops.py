@@ -384,7 +384,7 @@ def test_gated_strides_and_surroundings(dtype):
     do, _ = padded(dout, 16)
     dx = torch.full((M + 1, K + 8), 7.0, dtype=dtype, device=DEV)
     dw = torch.full((2 * F + 1, K + 16), 7.0, dtype=dtype, device=DEV)
-    n = t2i.load().t2i_op_gated_linear_backward_ws_bytes(dt, M, F)
+    n = t2i.load().t2i_op_gated_linear_backward_ws_bytes(dt, M, F, K)
     for fill in (0, 255):   # whatever the workspace held
         ws = torch.full((n,), fill, dtype=torch.uint8, device=DEV)
         _lib.check(t2i.load().t2i_op_gated_linear_backward(
