@@ -28,10 +28,10 @@ namespace t2i {
 struct TileChoice { int bm, bn, per_cu; float alone, full, end; };
 struct TilePick { int shape; float us; };
 template <int N>
-static TilePick choose_tile(const TileChoice (&c)[N], long rows, long cols, int steps, float end_scale) {
+static TilePick choose_tile(const TileChoice (&c)[N], long rows, long cols, int steps, float end_scale, int slices = 1) {
   TilePick best{0, 0.f};
   for (int i = 0; i < N; ++i) {
-    const long tiles = ((rows + c[i].bm - 1) / c[i].bm) * ((cols + c[i].bn - 1) / c[i].bn);
+    const long tiles = ((rows + c[i].bm - 1) / c[i].bm) * ((cols + c[i].bn - 1) / c[i].bn) * slices;
     const long slots = 256L * c[i].per_cu, rest = tiles % slots;
     const float end = c[i].end * end_scale;
     const float us = (float)(tiles / slots) * (c[i].full * steps + end) +
@@ -594,7 +594,7 @@ static SplitPick choose_split(long rows, long cols, int steps) {
   for (int n = 1; n <= kMaxSlices; ++n) {
     const int per = (steps + n - 1) / n, slices = (steps + per - 1) / per;
     if (slices != n || (n > 1 && per < 4)) continue;
-    const TilePick p = choose_tile(kTiles, rows * n, cols, per, n > 1 ? 2.f : 1.f);
+    const TilePick p = choose_tile(kTiles, rows, cols, per, n > 1 ? 2.f : 1.f, n);
     const float us = p.us + (n > 1 ? 4.f + (float)n * rows * cols * 8 / 4e6f : 0.f);
     if (n == 1 || us < least) least = us, best = {p.shape, n, per};
   }

@@ -25,18 +25,16 @@ __device__ __forceinline__ void load8<float>(const float* p, float (&v)[8]) {
   for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
 }
 template <typename T>
-__device__ __forceinline__ void store8(T* p, const float (&v)[8]);
-template <>
-__device__ __forceinline__ void store8<bf16>(bf16* p, const float (&v)[8]) {
-  bf16x8 w;
+__device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
+  if constexpr (sizeof(T) == 2) {
+    bf16x8 w;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) w[i] = (bf16)v[i];
-  *(bf16x8*)p = w;
-}
-template <>
-__device__ __forceinline__ void store8<float>(float* p, const float (&v)[8]) {
-  *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
-  *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    for (int i = 0; i < 8; ++i) w[i] = (bf16)v[i];
+    *(bf16x8*)p = w;
+  } else {
+    *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+    *(f32x4*)(p + 4) = f32x4{v[4], v[5], v[6], v[7]};
+  }
 }
 
 template <int G>
@@ -350,16 +348,19 @@ static int head_lanes(int head_dim) {
   return g;
 }
 
+// heads per group of the forward kernel (two: 9216 rows of 48 heads of 128 54.3 us,
+// four 51.9, six 51.4 but 22.0 instead of 20.5 for 16384 of 20 heads of 64)
+constexpr int kFwdHeads = 4;
 template <typename T, int G, bool HALVES>
 static void qk_launch(const QkNorm& a, hipStream_t st) {
   const int H = a.heads_q + a.heads_k;
   const int gr = 256 / G;
   // several heads of a row per group where that still leaves workgroups enough
-  const int hpg = (long)a.rows * ((H + 3) / 4) / gr >= 1024 ? 4 : 1;
+  const int hpg = (long)a.rows * ((H + kFwdHeads - 1) / kFwdHeads) / gr >= 1024 ? kFwdHeads : 1;
   const int upr = (H + hpg - 1) / hpg;
   const dim3 grid((unsigned)(((long)a.rows * upr + gr - 1) / gr));
-  if (hpg == 4)
-    hipLaunchKernelGGL((qk_norm_rope_kernel<T, G, HALVES, 4>), grid, dim3(256), 0, st, a, upr);
+  if (hpg > 1)
+    hipLaunchKernelGGL((qk_norm_rope_kernel<T, G, HALVES, kFwdHeads>), grid, dim3(256), 0, st, a, upr);
   else
     hipLaunchKernelGGL((qk_norm_rope_kernel<T, G, HALVES, 1>), grid, dim3(256), 0, st, a, upr);
 }
@@ -370,13 +371,13 @@ static void qk_launch(const QkNorm& a, hipStream_t st) {
 // A fixed number of workgroups walks the (row, heads) units; dw adds up in
 // registers, then over the workgroup in LDS, then (qk_weight_grad_kernel) over
 // the workgroups: a fixed order.
-template <typename T, int G, bool HALVES>
-__global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, float* __restrict__ partial) {
+template <typename T, int G, bool HALVES, int HPG>
+__global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, int upr, float* __restrict__ partial) {
   constexpr int GR = 256 / G;
   __shared__ float red[2][GR][G * 8];
   const int lg = threadIdx.x % G, gi = threadIdx.x / G, nl = a.head_dim / 8;
   const int H = a.heads_q + a.heads_k;
-  const unsigned units = (unsigned)a.rows * (unsigned)H, stride = gridDim.x * GR;
+  const unsigned units = (unsigned)a.rows * (unsigned)upr, stride = gridDim.x * GR;
   float wq[8], wk[8], aq[8], ak[8];
   load_weight<T>(a.wq, lg, nl, wq);
   load_weight<T>(a.wk, lg, nl, wk);
@@ -385,47 +386,55 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, float* 
   const float rd = 1.f / (float)a.head_dim;
   for (unsigned u0 = blockIdx.x * GR; u0 < units; u0 += stride) {
     const unsigned u = u0 + gi;
-    const bool in = u < units, live = in && lg < nl;
-    const int row = in ? (int)(u / (unsigned)H) : 0;
-    const int h = in ? (int)(u - (unsigned)row * (unsigned)H) : 0;
-    const bool isq = h < a.heads_q;
-    const int hh = isq ? h : h - a.heads_q;
-    float x[8], dy[8];
-    if (live) {
-      load8((isq ? (const T*)a.q + (size_t)row * a.ldq : (const T*)a.k + (size_t)row * a.ldk) +
-                hh * a.head_dim + lg * 8, x);
-      load8((isq ? (const T*)a.dq + (size_t)row * a.lddq : (const T*)a.dk + (size_t)row * a.lddk) +
-                hh * a.head_dim + lg * 8, dy);
-    } else {
+    const bool in = u < units && lg < nl;
+    const int row = u < units ? (int)(u / (unsigned)upr) : 0;
+    const int h0 = u < units ? (int)(u - (unsigned)row * (unsigned)upr) : 0;
+    float x[HPG][8], dy[HPG][8];
 #pragma unroll
-      for (int j = 0; j < 8; ++j) x[j] = dy[j] = 0.f;
+    for (int i = 0; i < HPG; ++i) {
+      const int h = h0 + i * upr;
+      const bool isq = h < a.heads_q;
+      const int at = (isq ? h : h - a.heads_q) * a.head_dim + lg * 8;
+      if (in && h < H) {
+        load8((isq ? (const T*)a.q + (size_t)row * a.ldq : (const T*)a.k + (size_t)row * a.ldk) + at, x[i]);
+        load8((isq ? (const T*)a.dq + (size_t)row * a.lddq : (const T*)a.dk + (size_t)row * a.lddk) + at, dy[i]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) x[i][j] = dy[i][j] = 0.f;
+      }
     }
     Rotor<HALVES> rot;
     rot.load(a, row, lg, nl, true);
-    rot.apply(dy);
-    if (!live)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) dy[j] = 0.f;   // (a spare lane's rotation is NaN)
-    float ss = 0.f;
+    for (int i = 0; i < HPG; ++i) {
+      const int h = h0 + i * upr;
+      const bool isq = h < a.heads_q, live = in && h < H;
+      float (&n)[8] = x[i], (&d)[8] = dy[i];
+      rot.apply(d);
+      if (!live)
 #pragma unroll
-    for (int j = 0; j < 8; ++j) ss = fmaf(x[j], x[j], ss);
-    const float r = rsqrtf(fmaf(group_sum<G>(ss), rd, a.eps));
-    float dot = 0.f;
+        for (int j = 0; j < 8; ++j) d[j] = 0.f;   // (a spare lane's rotation is NaN)
+      float ss = 0.f;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) {
-      x[j] = live ? x[j] * r : 0.f;   // n
-      const float p = dy[j] * x[j];
-      if (isq) aq[j] += p;
-      else ak[j] += p;
-      dy[j] *= isq ? wq[j] : wk[j];
-      dot = fmaf(dy[j], x[j], dot);
+      for (int j = 0; j < 8; ++j) ss = fmaf(n[j], n[j], ss);
+      const float r = rsqrtf(fmaf(group_sum<G>(ss), rd, a.eps));
+      float dot = 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        n[j] = live ? n[j] * r : 0.f;
+        const float p = d[j] * n[j];
+        if (isq) aq[j] += p;
+        else ak[j] += p;
+        d[j] *= isq ? wq[j] : wk[j];
+        dot = fmaf(d[j], n[j], dot);
+      }
+      dot = group_sum<G>(dot) * rd;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) d[j] = r * fmaf(-n[j], dot, d[j]);
+      if (live)
+        store8((isq ? (T*)a.oq + (size_t)row * a.ldoq : (T*)a.ok + (size_t)row * a.ldok) +
+                   (isq ? h : h - a.heads_q) * a.head_dim + lg * 8, d);
     }
-    dot = group_sum<G>(dot) * rd;
-#pragma unroll
-    for (int j = 0; j < 8; ++j) dy[j] = r * fmaf(-x[j], dot, dy[j]);
-    if (live)
-      store8((isq ? (T*)a.oq + (size_t)row * a.ldoq : (T*)a.ok + (size_t)row * a.ldok) +
-                 hh * a.head_dim + lg * 8, dy);
   }
   if (!partial) return;
 #pragma unroll
@@ -443,15 +452,27 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, float* 
   }
 }
 
-int qk_bwd_blocks(int rows, int heads, int head_dim) {
+// heads per group and step: two where that leaves every workgroup a step (9216 rows
+// of 48 heads of 128: 93 us with one, 86 with two, 126 with four, whose registers
+// halve the waves), 1024 workgroups (four per CU; 2048: 89 us, 768: 99)
+constexpr int kBwdHeads = 2, kBwdBlocks = 1024;
+static int qk_bwd_hpg(int rows, int heads, int head_dim) {
   const int gr = 256 / head_lanes(head_dim);
-  return (int)std::min<long>(1024, ((long)rows * heads + gr - 1) / gr);
+  return (long)rows * ((heads + kBwdHeads - 1) / kBwdHeads) / gr >= kBwdBlocks ? kBwdHeads : 1;
+}
+int qk_bwd_blocks(int rows, int heads, int head_dim) {
+  const int gr = 256 / head_lanes(head_dim), hpg = qk_bwd_hpg(rows, heads, head_dim);
+  return (int)std::min<long>(kBwdBlocks, ((long)rows * ((heads + hpg - 1) / hpg) + gr - 1) / gr);
 }
 
 template <typename T, int G, bool HALVES>
 static void qk_bwd_launch(const QkNorm& a, float* partial, hipStream_t st) {
-  const dim3 grid((unsigned)qk_bwd_blocks(a.rows, a.heads_q + a.heads_k, a.head_dim));
-  hipLaunchKernelGGL((qk_norm_rope_bwd_kernel<T, G, HALVES>), grid, dim3(256), 0, st, a, partial);
+  const int H = a.heads_q + a.heads_k, hpg = qk_bwd_hpg(a.rows, H, a.head_dim), upr = (H + hpg - 1) / hpg;
+  const dim3 grid((unsigned)qk_bwd_blocks(a.rows, H, a.head_dim));
+  if (hpg > 1)
+    hipLaunchKernelGGL((qk_norm_rope_bwd_kernel<T, G, HALVES, kBwdHeads>), grid, dim3(256), 0, st, a, upr, partial);
+  else
+    hipLaunchKernelGGL((qk_norm_rope_bwd_kernel<T, G, HALVES, 1>), grid, dim3(256), 0, st, a, upr, partial);
 }
 
 #define T2I_QK(FN, ...)                                                             \
@@ -554,7 +575,7 @@ __device__ __forceinline__ ActGrad act_grad(int act, float g) {
 }
 
 // rows per workgroup: 64, or down to the 8 that its threads take at a time while
-// there are fewer than two workgroups per CU (333 rows of 1544: 13.9 -> 4.4 us)
+// there are fewer than two workgroups per CU (333 rows of 1544: 13.9 -> 5.5 us)
 static int gate_rows(int M, int F) {
   int rows = 64;
   while (rows > 8 && (long)((M + rows - 1) / rows) * ((gated_cols(F) + 255) / 256) < 512) rows /= 2;
