@@ -11,7 +11,6 @@ Wrong arguments raise :class:`T2IError` before anything is launched.
 from __future__ import annotations
 
 import contextlib
-import ctypes as C
 from typing import Optional, Tuple
 
 import torch
@@ -37,15 +36,17 @@ def _need(ok: bool, what: str, status: int = 2):
 
 
 def _of(table: dict, key, what: str):
-    if key not in table:
+    v = table.get(key)
+    if v is None:
         raise T2IError(1, f"{what} must be one of {', '.join(map(str, table))}")
-    return table[key]
+    return v
 
 
 def _device(first: torch.Tensor, *others) -> torch.device:
     """The one device of all given tensors (None entries left out)."""
-    _need(first.is_cuda, "operands must be device tensors", 1)
     dev = first.device
+    if dev.type != "cuda":
+        raise T2IError(1, "operands must be device tensors")
     for t in others:
         if t is not None and t.device != dev:
             raise T2IError(1, "operands must be device tensors of one device")
@@ -75,36 +76,26 @@ def _p(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+# A call's own work is a few microseconds, so the common case -- no stream given,
+# operands on the current device -- goes without stream objects and contexts.
+
+def _elsewhere(dev: torch.device, stream) -> bool:
+    return stream is not None or dev.index != torch.cuda.current_device()
+
+
 @contextlib.contextmanager
-def _on_other(dev, stream):
-    with torch.cuda.device(dev), torch.cuda.stream(stream):
-        yield stream.cuda_stream
-
-
-class _Here:
-    """The current stream of the current device: nothing to switch."""
-
-    __slots__ = ("handle",)
-
-    def __init__(self, handle):
-        self.handle = handle
-
-    def __enter__(self):
-        return self.handle
-
-    def __exit__(self, *exc):
-        return False
-
-
-def _on(dev: torch.device, stream):
+def _switch(dev: torch.device, stream):
+    """The operands' device and the stream asked for (or that device's own) made current."""
     if stream is None:
-        if dev.index == torch.cuda.current_device():
-            # (the handle alone: torch.cuda.current_stream() makes a stream object, 2.7 us of a 10 us call)
-            return _Here(torch._C._cuda_getCurrentRawStream(dev.index))
         stream = torch.cuda.current_stream(dev)
     elif stream.device != dev:
         raise T2IError(1, "stream belongs to another device than the operands")
-    return _on_other(dev, stream)
+    with torch.cuda.device(dev), torch.cuda.stream(stream):
+        yield
+
+
+def _stream(dev: torch.device) -> int:
+    return torch._C._cuda_getCurrentRawStream(dev.index)
 
 
 def quant_rows(x: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -112,15 +103,18 @@ def quant_rows(x: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor
     (``t2i_op_quant_rows``): ``(q int8 [rows, K rounded up to 128], scale fp32
     [rows])``, zeros behind column K."""
     dev = _device(x)
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return quant_rows(x)
     dt = _of(_DTYPES, x.dtype, "dtype")
     _need(x.dim() == 2, "x must be [rows, K]")
     rows, K = x.shape
     ld = _rows(x, rows, K, x.dtype, "x")
-    with _on(dev, stream) as st:
-        q = torch.empty((rows, (K + 127) // 128 * 128), dtype=torch.int8, device=dev)
-        scale = torch.empty(rows, dtype=torch.float32, device=dev)
-        _check(load().t2i_op_quant_rows(dt, rows, K, x.data_ptr(), ld, q.data_ptr(), q.shape[1],
-                                        scale.data_ptr(), st))
+    ldq = (K + 127) // 128 * 128
+    q = x.new_empty((rows, ldq), dtype=torch.int8)
+    scale = x.new_empty(rows, dtype=torch.float32)
+    _check(load().t2i_op_quant_rows(dt, rows, K, x.data_ptr(), ld, q.data_ptr(), ldq, scale.data_ptr(),
+                                    _stream(dev)))
     return q, scale
 
 
@@ -135,6 +129,10 @@ def linear_i8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: 
     ``resid_gated`` add to the fp32 ``resid [M, N]`` in place (and write the bf16
     ``resid_copy``, if given) and return it."""
     dev = _device(a, a_scale, w, w_scale, bias, resid, resid_copy, gate)
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return linear_i8(a, a_scale, w, w_scale, bias, K=K, epilogue=epilogue, dtype=dtype, resid=resid,
+                             resid_copy=resid_copy, gate=gate)
     dt, epi = _of(_DTYPES, dtype, "dtype"), _of(EPILOGUES, epilogue, "epilogue")
     _need(a.dim() == 2 and w.dim() == 2, "a and w must be matrices")
     (M, ka), (N, kw) = a.shape, w.shape
@@ -148,7 +146,7 @@ def linear_i8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: 
     _vec(gate, N, torch.float32, "gate")
     ldr = N
     if epi >= _lib.T2I_EPI_RESID:
-        _need(resid is not None, f"{epilogue} needs resid", 1)
+        _need(resid is not None, "the resid epilogues need resid", 1)
         ldr = _rows(resid, M, N, torch.float32, "resid")
         if resid_copy is not None:
             ldc = _rows(resid_copy, M, N, torch.bfloat16, "resid_copy")
@@ -156,13 +154,12 @@ def linear_i8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: 
     else:
         _need(resid is None and resid_copy is None, "resid goes with the resid epilogues", 1)
     _need((gate is not None) == (epilogue == "resid_gated"), "gate goes with resid_gated", 1)
-    with _on(dev, stream) as st:
-        out = None
-        if epi < _lib.T2I_EPI_RESID:
-            out = torch.empty((M, N), dtype=dtype, device=dev)
-        _check(load().t2i_op_linear_i8(dt, epi, M, N, K, a.data_ptr(), lda, a_scale.data_ptr(),
-                                       w.data_ptr(), ldw, w_scale.data_ptr(), _p(bias), _p(out), N,
-                                       _p(resid), ldr, _p(resid_copy), _p(gate), st))
+    out = None
+    if epi < _lib.T2I_EPI_RESID:
+        out = a.new_empty((M, N), dtype=dtype)
+    _check(load().t2i_op_linear_i8(dt, epi, M, N, K, a.data_ptr(), lda, a_scale.data_ptr(), w.data_ptr(),
+                                   ldw, w_scale.data_ptr(), _p(bias), _p(out), N, _p(resid), ldr,
+                                   _p(resid_copy), _p(gate), _stream(dev)))
     return resid if out is None else out
 
 
@@ -183,16 +180,17 @@ def gated_linear(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor,
     ``wg``, ``wu`` ``[F, K]``, one dtype (bf16 or fp32); ``[M, F]``.  With ``save_pre``
     also the fp32 pre-activations ``[M, 2F]`` that :func:`gated_linear_backward` takes."""
     dev = _device(x, wg, wu, bg, bu)
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return gated_linear(x, wg, wu, bg, bu, act=act, save_pre=save_pre)
     dt, M, F, K, lda, ldw = _gated_args(x, wg, wu)
     a = _of(ACTS, act, "act")
     _vec(bg, F, x.dtype, "bg")
     _vec(bu, F, x.dtype, "bu")
-    with _on(dev, stream) as st:
-        out = torch.empty((M, F), dtype=x.dtype, device=dev)
-        pre = torch.empty((M, 2 * F), dtype=torch.float32, device=dev) if save_pre else None
-        _check(load().t2i_op_gated_linear(dt, a, M, F, K, x.data_ptr(), lda, wg.data_ptr(),
-                                          wu.data_ptr(), ldw, _p(bg), _p(bu), out.data_ptr(), F,
-                                          _p(pre), 2 * F, st))
+    out = x.new_empty((M, F))
+    pre = x.new_empty((M, 2 * F), dtype=torch.float32) if save_pre else None
+    _check(load().t2i_op_gated_linear(dt, a, M, F, K, x.data_ptr(), lda, wg.data_ptr(), wu.data_ptr(), ldw,
+                                      _p(bg), _p(bu), out.data_ptr(), F, _p(pre), 2 * F, _stream(dev)))
     return (out, pre) if save_pre else out
 
 
@@ -202,20 +200,24 @@ def gated_linear_backward(dout: torch.Tensor, x: torch.Tensor, wg: torch.Tensor,
     """Gradients of :func:`gated_linear` (``t2i_op_gated_linear_backward``):
     ``(dx, dwg, dwu, dbg, dbu)``, None for those not asked for."""
     dev = _device(dout, x, wg, wu, pre)
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return gated_linear_backward(dout, x, wg, wu, pre, act=act, bias=bias, need_dx=need_dx,
+                                         need_dw=need_dw)
     dt, M, F, K, lda, ldw = _gated_args(x, wg, wu)
     a = _of(ACTS, act, "act")
     ldd = _rows(dout, M, F, x.dtype, "dout")
     ldp = _rows(pre, M, 2 * F, torch.float32, "pre")
     lib = load()
-    with _on(dev, stream) as st:
-        new = lambda on, *shape: torch.empty(shape, dtype=x.dtype, device=dev) if on else None  # noqa: E731
-        dx, dwg, dwu = new(need_dx, M, K), new(need_dw, F, K), new(need_dw, F, K)
-        dbg, dbu = new(bias, F), new(bias, F)
-        n = lib.t2i_op_gated_linear_backward_ws_bytes(dt, M, F, K)
-        ws = torch.empty(max(n, 1), dtype=torch.uint8, device=dev)
-        _check(lib.t2i_op_gated_linear_backward(
-            dt, a, M, F, K, x.data_ptr(), lda, wg.data_ptr(), wu.data_ptr(), ldw, pre.data_ptr(), ldp,
-            dout.data_ptr(), ldd, _p(dx), K, _p(dwg), _p(dwu), K, _p(dbg), _p(dbu), ws.data_ptr(), n, st))
+    dx = x.new_empty((M, K)) if need_dx else None
+    dwg, dwu = (x.new_empty((F, K)), x.new_empty((F, K))) if need_dw else (None, None)
+    dbg, dbu = (x.new_empty(F), x.new_empty(F)) if bias else (None, None)
+    n = lib.t2i_op_gated_linear_backward_ws_bytes(dt, M, F, K)
+    ws = x.new_empty(n, dtype=torch.uint8)
+    _check(lib.t2i_op_gated_linear_backward(
+        dt, a, M, F, K, x.data_ptr(), lda, wg.data_ptr(), wu.data_ptr(), ldw, pre.data_ptr(), ldp,
+        dout.data_ptr(), ldd, _p(dx), K, _p(dwg), _p(dwu), K, _p(dbg), _p(dbu), ws.data_ptr(), n,
+        _stream(dev)))
     return dx, dwg, dwu, dbg, dbu
 
 
@@ -235,8 +237,7 @@ def _heads(t: torch.Tensor, rows: int, d: int, dtype, what: str):
     return h, ld
 
 
-def _qk_args(q, k, wq, wk, table, pos, pairing, extra=()):
-    dev = _device(q, k, wq, wk, table, pos, *extra)
+def _qk_args(q, k, wq, wk, table, pos, pairing):
     dt = _of(_DTYPES, q.dtype, "dtype")
     pr = _of(PAIRINGS, pairing, "pairing")
     _need(q.dim() == 3, "q must be [rows, heads, head_dim]")
@@ -252,7 +253,7 @@ def _qk_args(q, k, wq, wk, table, pos, pairing, extra=()):
             raise T2IError(2, f"table must be fp32 [n_pos, {d // 2}, 2], contiguous")
     _need(pos is None or table is not None, "pos goes with a table", 1)
     _vec(pos, rows, torch.int32, "pos")
-    return dev, dt, pr, rows, hq, hk, d, ldq, ldk, n_pos
+    return dt, pr, rows, hq, hk, d, ldq, ldk, n_pos
 
 
 def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, wq: Optional[torch.Tensor] = None,
@@ -264,14 +265,18 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, wq: Optional[torch.Tensor] = 
     ``table[pos[row]]`` (``t2i_op_qk_norm_rope``): ``table`` fp32 ``[n_pos, d/2, 2]`` of
     (cos, sin) or None, ``pos`` int32 ``[rows]`` (negative: not turned) or None (row r
     at position r).  Returns new ``(q, k)``, or with ``inplace`` the given ones."""
-    dev, dt, pr, rows, hq, hk, d, ldq, ldk, n_pos = _qk_args(q, k, wq, wk, table, pos, pairing)
-    with _on(dev, stream) as st:
-        oq = q if inplace else torch.empty((rows, hq, d), dtype=q.dtype, device=dev)
-        ok = k if inplace else torch.empty((rows, hk, d), dtype=q.dtype, device=dev)
-        _check(load().t2i_op_qk_norm_rope(
-            dt, rows, hq, hk, d, q.data_ptr(), ldq, k.data_ptr(), ldk, _p(wq), _p(wk), eps, pr,
-            _p(table), n_pos, _p(pos), oq.data_ptr(), ldq if inplace else hq * d, ok.data_ptr(),
-            ldk if inplace else hk * d, st))
+    dev = _device(q, k, wq, wk, table, pos)
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return qk_norm_rope(q, k, wq, wk, table=table, pos=pos, eps=eps, pairing=pairing, inplace=inplace)
+    dt, pr, rows, hq, hk, d, ldq, ldk, n_pos = _qk_args(q, k, wq, wk, table, pos, pairing)
+    if inplace:
+        oq, ok, ldoq, ldok = q, k, ldq, ldk
+    else:
+        oq, ok, ldoq, ldok = q.new_empty((rows, hq, d)), q.new_empty((rows, hk, d)), hq * d, hk * d
+    _check(load().t2i_op_qk_norm_rope(
+        dt, rows, hq, hk, d, q.data_ptr(), ldq, k.data_ptr(), ldk, _p(wq), _p(wk), eps, pr, _p(table), n_pos,
+        _p(pos), oq.data_ptr(), ldoq, ok.data_ptr(), ldok, _stream(dev)))
     return oq, ok
 
 
@@ -281,20 +286,24 @@ def qk_norm_rope_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k
                           eps: float = 1e-6, pairing: str = "pairs", stream=None):
     """Gradients of :func:`qk_norm_rope` (``t2i_op_qk_norm_rope_backward``) from those of
     its outputs and its inputs: ``(dq, dk, dwq, dwk)``, None for a weight that is None."""
-    dev, dt, pr, rows, hq, hk, d, ldq, ldk, n_pos = _qk_args(q, k, wq, wk, table, pos, pairing, (dq, dk))
+    dev = _device(q, k, wq, wk, table, pos, dq, dk)
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return qk_norm_rope_backward(dq, dk, q, k, wq, wk, table=table, pos=pos, eps=eps, pairing=pairing)
+    dt, pr, rows, hq, hk, d, ldq, ldk, n_pos = _qk_args(q, k, wq, wk, table, pos, pairing)
     h1, lddq = _heads(dq, rows, d, q.dtype, "dq")
     h2, lddk = _heads(dk, rows, d, q.dtype, "dk")
-    _need((h1, h2) == (hq, hk), "gradients must have the heads of q and k")
+    _need(h1 == hq and h2 == hk, "gradients must have the heads of q and k")
     lib = load()
-    with _on(dev, stream) as st:
-        oq = torch.empty((rows, hq, d), dtype=q.dtype, device=dev)
-        ok = torch.empty((rows, hk, d), dtype=q.dtype, device=dev)
-        dwq = torch.empty(d, dtype=q.dtype, device=dev) if wq is not None else None
-        dwk = torch.empty(d, dtype=q.dtype, device=dev) if wk is not None else None
+    oq, ok = q.new_empty((rows, hq, d)), q.new_empty((rows, hk, d))
+    dwq = q.new_empty(d) if wq is not None else None
+    dwk = q.new_empty(d) if wk is not None else None
+    n, ws = 0, None
+    if wq is not None or wk is not None:
         n = lib.t2i_op_qk_norm_rope_backward_ws_bytes(rows, hq, hk, d)
-        ws = torch.empty(n, dtype=torch.uint8, device=dev) if wq is not None or wk is not None else None
-        _check(lib.t2i_op_qk_norm_rope_backward(
-            dt, rows, hq, hk, d, dq.data_ptr(), lddq, dk.data_ptr(), lddk, q.data_ptr(), ldq,
-            k.data_ptr(), ldk, _p(wq), _p(wk), eps, pr, _p(table), n_pos, _p(pos), oq.data_ptr(), hq * d,
-            ok.data_ptr(), hk * d, _p(dwq), _p(dwk), _p(ws), n, st))
+        ws = q.new_empty(n, dtype=torch.uint8)
+    _check(lib.t2i_op_qk_norm_rope_backward(
+        dt, rows, hq, hk, d, dq.data_ptr(), lddq, dk.data_ptr(), lddk, q.data_ptr(), ldq, k.data_ptr(), ldk,
+        _p(wq), _p(wk), eps, pr, _p(table), n_pos, _p(pos), oq.data_ptr(), hq * d, ok.data_ptr(), hk * d,
+        _p(dwq), _p(dwk), _p(ws), n, _stream(dev)))
     return oq, ok, dwq, dwk
