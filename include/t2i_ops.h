@@ -209,7 +209,8 @@ t2i_status t2i_op_linear_i8(int32_t dtype, int32_t epilogue, int32_t M, int32_t 
  *   t2i_op_gated_linear_backward reads (fp32 for bf16 operands too: rounded to
  *   bf16 they would add a quarter to the gradients' error).
  *   bf16: F, K and the strides % 8 == 0 (ldp % 4), every pointer 16-byte
- *   aligned, rows of A, Wg and Wu at most 8 MiB apart.  fp32: any sizes.
+ *   aligned.  fp32: any sizes (F, K, strides % 4 == 0 and 16-byte aligned
+ *   pointers are faster).  Rows of A, Wg and Wu at most 8 MiB apart.
  * No output may overlap an input.
  */
 t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,
@@ -227,7 +228,7 @@ t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F,
  * bias sums take them unrounded); products and sums are fp32.  dA (stride
  * ldda), dWg, dWu (common stride lddw) may each be NULL: not computed; dbg and
  * dbu both or neither.  Sizes, strides and alignment as in the forward pass
- * (bf16: F up to 2^20).
+ * (F up to 2^20).
  * ws: device workspace of ws_bytes >= t2i_op_gated_linear_backward_ws_bytes,
  * 256-byte aligned, used by this call until it has finished on the stream;
  * the result does not depend on what it holds.  No output may overlap an

@@ -149,7 +149,7 @@ t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F,
   const bool bf = dtype == T2I_BF16;
   if (bf && (F % 8 || K % 8 || lda % 8 || ldw % 8 || ldo % 8 || (pre && ldp % 4)))
     return ops_fail(T2I_ERR_SHAPE, "bf16 needs F, K and strides % 8 == 0 (pre: 4)");
-  if (bf && (far_rows(lda, 2) || far_rows(ldw, 2))) return ops_fail(T2I_ERR_SHAPE, "rows more than 8 MiB apart");
+  if (far_rows(lda, bf ? 2 : 4) || far_rows(ldw, bf ? 2 : 4)) return ops_fail(T2I_ERR_SHAPE, "rows more than 8 MiB apart");
   const size_t al = bf ? 16 : 4;
   if (off(A, al) || off(Wg, al) || off(Wu, al) || off(bg, al) || off(bu, al) || off(out, al) || off(pre, al))
     return ops_fail(T2I_ERR_INVALID_ARG, "pointers need 16-byte (bf16) or 4-byte (fp32) alignment");
@@ -176,7 +176,7 @@ size_t t2i_op_gated_linear_backward_ws_bytes(int32_t dtype, int32_t M, int32_t F
     return 0;
   // dg | du, the bias gradients' column sums, the products' partial sums
   const size_t partial = ((size_t)gate_row_blocks(M, F) * 2 * gated_cols(F) * 4 + 255) / 256 * 256;
-  return gated_dgu_bytes(dtype, M, F) + partial + (dtype == T2I_BF16 ? gated_split_floats(M, F, K) * 4 : 0);
+  return gated_dgu_bytes(dtype, M, F) + partial + gated_split_floats(dtype == T2I_BF16, M, F, K) * 4;
 }
 
 t2i_status t2i_op_gated_linear_backward(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,
@@ -201,7 +201,7 @@ t2i_status t2i_op_gated_linear_backward(int32_t dtype, int32_t act, int32_t M, i
   if (bf && (F % 8 || K % 8 || lda % 8 || ldw % 8 || ldp % 4 || ldd % 8 || (dA && ldda % 8) ||
              (dw && lddw % 8)))
     return ops_fail(T2I_ERR_SHAPE, "bf16 needs F, K and strides % 8 == 0 (pre: 4)");
-  if (bf && (far_rows(lda, 2) || far_rows(ldw, 2) || far_rows(gated_cols(F), 4)))
+  if (far_rows(lda, bf ? 2 : 4) || far_rows(ldw, bf ? 2 : 4) || far_rows(gated_cols(F), bf ? 4 : 8))
     return ops_fail(T2I_ERR_SHAPE, "rows more than 8 MiB apart");
   const size_t al = bf ? 16 : 4;
   if (off(A, al) || off(Wg, al) || off(Wu, al) || off(pre, al) || off(dout, al) || off(dA, al) ||

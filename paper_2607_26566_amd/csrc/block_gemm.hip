@@ -1,6 +1,7 @@
 // Matrix products of the block operators: the 8-bit linear layer, the gated
-// feed-forward and its gradients.  bf16 and 8-bit operands go through the tiles
-// of gemm_tile.h, fp32 ones through gemm_f32_tile_kernel:
+// feed-forward and its gradients.  They go through the tiles of gemm_tile.h, but
+// for fp32 operands that do not lie in whole, aligned 16-byte pieces, which take
+// gemm_f32_tile_kernel:
 //
 // One product C[m][n] = sum_k a(m, k) b(n, k) on BM x BN tiles by 2 x 2 waves
 // (v_mfma_f32_16x16x4_f32), 32 values of k at a time through two LDS stages, the
@@ -12,10 +13,11 @@
 // (4-byte reads of four k from four places): neither meets itself in a bank.  What
 // bounds the 64 x 64 tile is the operands' way from L2 (16 bytes per clock and CU at
 // the matrix cores' full rate), hence 128 x 128 where enough of them fill the chip.
-// VEC: operands are read 16 bytes at a time
-// (rows of whole, aligned 16-byte pieces), else by element; addresses stay inside
-// the operand and what lies outside is taken as 0, without branches.
+// Operands are
+// read by element; addresses stay inside the operand and what lies outside is taken
+// as 0, without branches.
 #include <algorithm>
+#include <initializer_list>
 
 #include "gemm_tile.h"
 
@@ -90,7 +92,7 @@ __device__ __forceinline__ bool inside(const TwoRows& m, int& y, int& x) {
   return (y < m.half ? y : y - m.half) < m.rows && x < m.cols;
 }
 
-template <int BM, int BN, bool VEC, class LA, class LB, class EP>
+template <int BM, int BN, class LA, class LB, class EP>
 __global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep, TileShape s, int K) {
   constexpr int BK = 32, LD = 36, TM = BM / 32, TN = BN / 32;
   constexpr int SA = LA::along ? BM * LD : BK * (BM + 4), SB = LB::along ? BN * LD : BK * (BN + 4);
@@ -100,32 +102,21 @@ __global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep,
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
   const int m0 = tm * BM, n0 = tn * BN;
-  // a thread's pieces i of four: along k of one row, or four rows' of one k; by
-  // element, four that lie 256 elements of the stage apart, so that neighbouring
-  // lanes read neighbouring addresses either way
+  // a thread's elements lie 256 of the stage apart: neighbouring lanes read
+  // neighbouring addresses
   f32x4 ra[BM / 32], rb[BN / 32];
   auto load = [&](const auto& op, int r0, int k0, int i, int R) -> f32x4 {
     using O = typename std::decay<decltype(op)>::type;
     f32x4 v;
     int y, x;
-    if constexpr (VEC) {
-      const int c = tid + i * 256;
-      if constexpr (O::along) y = r0 + c / 8, x = k0 + c % 8 * 4;
-      else y = k0 + c / (R / 4), x = r0 + c % (R / 4) * 4;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int c = tid + (i * 4 + e) * 256;
+      if constexpr (O::along) y = r0 + c / BK, x = k0 + c % BK;
+      else y = k0 + c / R, x = r0 + c % R;
       const bool in = inside(op, y, x);
-      const f32x4 w = *(const f32x4*)op.at(y, min(x, op.cols - 4));
-#pragma unroll
-      for (int e = 0; e < 4; ++e) v[e] = in ? w[e] : 0.f;
-    } else {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int c = tid + (i * 4 + e) * 256;
-        if constexpr (O::along) y = r0 + c / BK, x = k0 + c % BK;
-        else y = k0 + c / R, x = r0 + c % R;
-        const bool in = inside(op, y, x);
-        const float w = *op.at(y, min(x, op.cols - 1));
-        v[e] = in ? w : 0.f;
-      }
+      const float w = *op.at(y, min(x, op.cols - 1));
+      v[e] = in ? w : 0.f;
     }
     return v;
   };
@@ -136,15 +127,10 @@ __global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep,
     for (int i = 0; i < BN / 32; ++i) rb[i] = load(lb, n0, k0, i, BN);
   };
   auto put = [&](bool along, float* p, int i, int R, f32x4 v) {
-    if constexpr (VEC) {
-      const int c = tid + i * 256;
-      *(f32x4*)(along ? p + c / 8 * LD + c % 8 * 4 : p + c / (R / 4) * (R + 4) + c % (R / 4) * 4) = v;
-    } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const int c = tid + (i * 4 + e) * 256;
-        p[along ? c / BK * LD + c % BK : c / R * (R + 4) + c % R] = v[e];
-      }
+    for (int e = 0; e < 4; ++e) {
+      const int c = tid + (i * 4 + e) * 256;
+      p[along ? c / BK * LD + c % BK : c / R * (R + 4) + c % R] = v[e];
     }
   };
   auto frag = [&](bool along, const float* p, int row, int k, int R) -> f32x4 {
@@ -198,24 +184,19 @@ __global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep,
 }
 
 template <int BM, int BN, class LA, class LB, class EP>
-static void gemm_f32_launch(bool vec, const LA& la, const LB& lb, const EP& ep, int M, int N, int K, hipStream_t st) {
-  TileShape s{(M + BM - 1) / BM, (N + BN - 1) / BN, 8, 0, 0, 0, 0};
-  const dim3 grid((unsigned)(s.tiles_m * s.tiles_n));
-  if (vec)
-    hipLaunchKernelGGL((gemm_f32_tile_kernel<BM, BN, true, LA, LB, EP>), grid, dim3(256), 0, st, la, lb, ep, s, K);
-  else
-    hipLaunchKernelGGL((gemm_f32_tile_kernel<BM, BN, false, LA, LB, EP>), grid, dim3(256), 0, st, la, lb, ep, s, K);
+static void gemm_f32_launch(const LA& la, const LB& lb, const EP& ep, int M, int N, int K, hipStream_t st) {
+  const TileShape s{(M + BM - 1) / BM, (N + BN - 1) / BN, 8, 0, 0, 0, 0};
+  hipLaunchKernelGGL((gemm_f32_tile_kernel<BM, BN, LA, LB, EP>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(256), 0,
+                     st, la, lb, ep, s, K);
 }
 
 template <class LA, class LB, class EP>
-static hipError_t gemm_f32_tile(size_t bits, const LA& la, const LB& lb, const EP& ep, int M, int N, int K,
-                                hipStream_t st) {
-  const bool vec = bits % 16 == 0 && la.ld % 4 == 0 && lb.ld % 4 == 0 && la.cols % 4 == 0 && lb.cols % 4 == 0;
+static hipError_t gemm_f32_tile(const LA& la, const LB& lb, const EP& ep, int M, int N, int K, hipStream_t st) {
   constexpr TileChoice tiles[] = {{128, 128, 1, 80, 80, 0}, {64, 64, 1, 24, 24, 0}, {32, 64, 1, 13, 13, 0}};
   switch (choose_tile(tiles, M, N, 1, 0.f).shape) {
-    case 0: gemm_f32_launch<128, 128>(vec, la, lb, ep, M, N, K, st); break;
-    case 1: gemm_f32_launch<64, 64>(vec, la, lb, ep, M, N, K, st); break;
-    default: gemm_f32_launch<32, 64>(vec, la, lb, ep, M, N, K, st);
+    case 0: gemm_f32_launch<128, 128>(la, lb, ep, M, N, K, st); break;
+    case 1: gemm_f32_launch<64, 64>(la, lb, ep, M, N, K, st); break;
+    default: gemm_f32_launch<32, 64>(la, lb, ep, M, N, K, st);
   }
   return hipGetLastError();
 }
@@ -297,7 +278,7 @@ __device__ __forceinline__ float i8_value(int acc, float sa, float sw, float b, 
 template <class D, typename T, bool RES>
 __global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a, TileOperand b, TileShape s,
                                                                   I8Epi e, int M, int N, int vec) {
-  using P = TileProduct<D, true, false, false, false, false>;
+  using P = TileProduct<D, ELEM_I8, false, false, false, false>;
   constexpr int THREADS = D::NW * 64, NE = D::BM + (RES ? 3 : 2) * D::BN;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + NE * 4];
   int tm, tn;
@@ -353,10 +334,13 @@ __global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a,
   }
 }
 
-template <class D>
+template <typename T>
+constexpr TileElem elem_of() { return sizeof(T) == 4 ? ELEM_F32 : ELEM_BF16; }
+
+template <class D, typename T>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand a, TileOperand b, TileShape s,
                                                                      GatedFwd p, int M, int F) {
-  using P = TileProduct<D, false, false, false, true, false>;
+  using P = TileProduct<D, elem_of<T>(), false, false, true, false>;
   constexpr int THREADS = D::NW * 64, H = D::BN / 2, TH = D::TN / 2;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + D::BN * 4];
   int tm, tn;
@@ -364,7 +348,7 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
   const int m0 = tm * D::BM, f0 = tn * H;
   auto value = [&](int x) -> float {
     if (!p.bg) return 0.f;
-    return (float)((const bf16*)(x < H ? p.bg : p.bu))[min(f0 + x % H, F - 1)];
+    return to_f32(((const T*)(x < H ? p.bg : p.bu))[min(f0 + x % H, F - 1)]);
   };
   Staged<D::BN, THREADS, decltype(value)> st;
   st.fetch(value);
@@ -382,7 +366,7 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
 #pragma unroll
     for (int j = 0; j < TH; ++j) {
       const int fl = nw + j * 16 + g * 4, f = f0 + fl;
-      if (f >= F) continue;   // (F % 8 == 0: four columns or none)
+      if (f >= F) continue;   // (F % 4 == 0: four columns or none)
       const f32x4 bg = *(const f32x4*)(ev + fl), bu = *(const f32x4*)(ev + H + fl);
       float gv[4], uv[4], y[4];
 #pragma unroll
@@ -396,14 +380,15 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
         store4(q, 4, true, gv);
         store4(q + F, 4, true, uv);
       }
-      store4((bf16*)p.out + (size_t)m * p.ldo + f, 4, true, y);
+      store4((T*)p.out + (size_t)m * p.ldo + f, 4, true, y);
     }
   }
 }
 
 // The gradients' products.  b is a KR operand: a pair of fragments holds 8
-// neighbouring columns of a row (N % 8 == 0).  Stored as bf16 (row stride ldc), or
-// as fp32 partial sums (row stride N) where the contraction is split.
+// neighbouring columns of a row, of which all or the first four exist (N % 4 == 0).
+// Stored in the operands' type (row stride ldc), or as fp32 partial sums (row stride
+// N) where the contraction is split.
 template <class D, class P, typename T>
 __device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D::TN], T* C, int ldc, int m0,
                                            int n0, int M, int N) {
@@ -425,7 +410,7 @@ __device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D
         *(bf16x8*)p = v;
       } else {
         *(f32x4*)p = f32x4{acc[i][j][0], acc[i][j + 1][0], acc[i][j][1], acc[i][j + 1][1]};
-        *(f32x4*)(p + 4) = f32x4{acc[i][j][2], acc[i][j + 1][2], acc[i][j][3], acc[i][j + 1][3]};
+        if (n + 4 < N) *(f32x4*)(p + 4) = f32x4{acc[i][j][2], acc[i][j + 1][2], acc[i][j][3], acc[i][j + 1][3]};
       }
     }
   }
@@ -443,10 +428,10 @@ __device__ __forceinline__ void take_slice(const Split& sp, TileShape& s) {
   s.steps = min(sp.per, s.steps - s.first);
 }
 
-template <class D>
+template <class D, typename T>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
-                                                                 bf16* dx, int ldx, int M, int K) {
-  using P = TileProduct<D, false, false, true, false, true>;
+                                                                 T* dx, int ldx, int M, int K) {
+  using P = TileProduct<D, elem_of<T>(), false, true, false, true>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
@@ -461,11 +446,11 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, 
 
 // row blocks [0, half) are the first output's, the others the second's (their
 // operand lies `shift` bytes further)
-template <class D>
+template <class D, typename T>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
-                                                                 int half, int shift, bf16* d0, bf16* d1, int ldw,
+                                                                 int half, int shift, T* d0, T* d1, int ldw,
                                                                  int F, int K) {
-  using P = TileProduct<D, false, true, true, false, false>;
+  using P = TileProduct<D, elem_of<T>(), true, true, false, false>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
@@ -484,24 +469,20 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, 
 }
 
 // out (rows [0, half) to o0, the others to o1) = the sum of the slices' partials
-// [rows][cols], in ascending slice order; cols % 8 == 0, one thread per 8 columns
+// [rows][cols], in ascending slice order; cols % 4 == 0, one thread per 4 columns
+template <typename T>
 __global__ __launch_bounds__(256) void split_sum_kernel(const float* __restrict__ partial, int slices, long rows,
-                                                        long half, int cols, bf16* o0, bf16* o1, int ld) {
-  const long x = blockIdx.x * 256L + threadIdx.x, n8 = cols / 8;
-  if (x >= rows * n8) return;
-  const long r = x / n8;
-  const int c = (int)(x - r * n8) * 8;
+                                                        long half, int cols, T* o0, T* o1, int ld) {
+  const long x = blockIdx.x * 256L + threadIdx.x, n4 = cols / 4;
+  if (x >= rows * n4) return;
+  const long r = x / n4;
+  const int c = (int)(x - r * n4) * 4;
   const float* p = partial + r * cols + c;
-  f32x4 a = *(const f32x4*)p, b = *(const f32x4*)(p + 4);
-  for (int i = 1; i < slices; ++i) {
-    p += rows * cols;
-    a += *(const f32x4*)p;
-    b += *(const f32x4*)(p + 4);
-  }
-  bf16x8 v;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = (bf16)a[i], v[4 + i] = (bf16)b[i];
-  *(bf16x8*)((r < half ? o0 + r * ld : o1 + (r - half) * ld) + c) = v;
+  f32x4 a = *(const f32x4*)p;
+#pragma unroll 4
+  for (int i = 1; i < slices; ++i) a += *(const f32x4*)(p + i * rows * cols);
+  const float v[4] = {a[0], a[1], a[2], a[3]};
+  store4((r < half ? o0 + r * ld : o1 + (r - half) * ld) + c, 4, true, v);
 }
 
 // ---- launches
@@ -519,6 +500,10 @@ using Tile128d = TileDims<128, 128, 2, 4, 4>;
 using Tile64 = TileDims<64, 128, 2, 4, 2>;
 using Tile64d = TileDims<64, 128, 2, 4, 4>;
 using Tile32d = TileDims<32, 128, 1, 4, 4>;
+// fp32: bound by the matrix cores (154 TFLOP/s: 1.7 us per step of 128 x 128); no
+// larger tiles, which would only spread worse
+constexpr TileChoice kTilesF32[] = {{128, 128, 1, 1.90f, 1.90f, 5.f}, {64, 128, 1, 0.98f, 0.98f, 3.f},
+                                    {32, 128, 1, 0.55f, 0.55f, 2.f}};
 constexpr int kMaxSlices = 16;
 constexpr TileChoice kTiles[] = {{256, 256, 1, 1.60f, 1.60f, 13.f}, {256, 128, 1, 0.95f, 0.95f, 8.f},
                                  {128, 128, 2, 0.72f, 1.02f, 6.f},  {128, 128, 1, 0.61f, 0.61f, 5.f},
@@ -575,79 +560,100 @@ hipError_t launch_linear_i8(const int8_t* A, int lda, const int8_t* W, int ldw, 
   return hipGetLastError();
 }
 
-static hipError_t gated_fwd_bf16(const GatedFwd& p, int M, int F, int K, hipStream_t st) {
-  const TileOperand a{(const char*)p.A, nullptr, 2u * p.lda, M, 0},
-      b{(const char*)p.Wg, (const char*)p.Wu, 2u * p.ldw, F, 0};
-  T2I_TILES(choose_tile(kTiles, M, 2L * F, (K + 63) / 64, 0.5f).shape, const TileShape s = tile_shape<D>(M, 2 * F, (K + 63) / 64, 2 * K, 0);
-            hipLaunchKernelGGL((gated_linear_kernel<D>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64),
-                               0, st, a, b, s, p, M, F))
-  return hipGetLastError();
+#define T2I_TILES_F32(SHAPE, CALL)               \
+  switch (SHAPE) {                               \
+    case 0: { using D = Tile128d; CALL; break; } \
+    case 1: { using D = Tile64d; CALL; break; }  \
+    default: { using D = Tile32d; CALL; break; } \
+  }
+
+template <class D, typename T>
+static void gated_fwd_launch(const GatedFwd& p, int M, int F, int K, hipStream_t st) {
+  constexpr int e = sizeof(T), per = 128 / e;
+  const TileOperand a{(const char*)p.A, nullptr, (uint32_t)e * p.lda, M, 0},
+      b{(const char*)p.Wg, (const char*)p.Wu, (uint32_t)e * p.ldw, F, 0};
+  const TileShape s = tile_shape<D>(M, 2 * F, (K + per - 1) / per, e * K, 0);
+  hipLaunchKernelGGL((gated_linear_kernel<D, T>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64), 0, st, a,
+                     b, s, p, M, F);
+}
+
+// whether fp32 operands lie in whole, aligned 16-byte pieces (sizes and strides, and
+// the bits of all pointers): then they go through the same tiles
+static bool f32_pieces(std::initializer_list<int> sizes, std::initializer_list<const void*> ptrs) {
+  uintptr_t bits = 0;
+  for (int n : sizes) bits |= (uintptr_t)n * 4;
+  for (const void* p : ptrs) bits |= (uintptr_t)p;
+  return bits % 16 == 0;
 }
 
 // Tile shape and slices of a gradient's product: as few slices as keep the time
 // least, counting 4 us for the second launch and the partial sums' way out and back
 // at 4 TB/s (1024 x 9216 x 1152: 63 us on 144 64 x 128 tiles, 41 in slices).
 struct SplitPick { int shape, slices, per; };
-static SplitPick choose_split(long rows, long cols, int steps) {
+template <int N>
+static SplitPick choose_split(const TileChoice (&tiles)[N], long rows, long cols, int steps) {
   SplitPick best{0, 1, steps};
   float least = 0.f;
   for (int n = 1; n <= kMaxSlices; ++n) {
     const int per = (steps + n - 1) / n, slices = (steps + per - 1) / per;
     if (slices != n || (n > 1 && per < 4)) continue;
-    const TilePick p = choose_tile(kTiles, rows, cols, per, n > 1 ? 2.f : 1.f, n);
+    const TilePick p = choose_tile(tiles, rows, cols, per, n > 1 ? 2.f : 1.f, n);
     const float us = p.us + (n > 1 ? 4.f + (float)n * rows * cols * 8 / 4e6f : 0.f);
     if (n == 1 || us < least) least = us, best = {p.shape, n, per};
   }
   return best;
 }
 
-size_t gated_split_floats(int M, int F, int K) {
-  const SplitPick x = choose_split(M, K, 2 * gated_cols(F) / 64), w = choose_split(2L * F, K, (M + 63) / 64),
-                  w1 = choose_split(F, K, (M + 63) / 64);
-  auto floats = [](const SplitPick& p, size_t n) { return p.slices > 1 ? n * p.slices : 0; };
-  return std::max({floats(x, (size_t)M * K), floats(w, (size_t)2 * F * K), floats(w1, (size_t)F * K)});
+static SplitPick split_of(bool is_bf16, long rows, long cols, int k) {
+  return is_bf16 ? choose_split(kTiles, rows, cols, (k + 63) / 64) : choose_split(kTilesF32, rows, cols, (k + 31) / 32);
 }
 
-static void split_sum(const SplitPick& pick, const float* partial, long rows, long half, int cols, void* o0, void* o1,
+size_t gated_split_floats(bool is_bf16, int M, int F, int K) {
+  auto floats = [&](long rows, long cols, int k) -> size_t {
+    const int n = split_of(is_bf16, rows, cols, k).slices;
+    return n > 1 ? (size_t)n * rows * cols : 0;
+  };
+  return std::max({floats(M, K, 2 * gated_cols(F)), floats(2L * F, K, M), floats(F, K, M)});
+}
+
+template <typename T>
+static void split_sum(const SplitPick& pick, const float* partial, long rows, long half, int cols, T* o0, T* o1,
                       int ld, hipStream_t st) {
-  hipLaunchKernelGGL(split_sum_kernel, dim3((unsigned)((rows * (cols / 8) + 255) / 256)), dim3(256), 0, st, partial,
-                     pick.slices, rows, half, cols, (bf16*)o0, (bf16*)o1, ld);
+  hipLaunchKernelGGL((split_sum_kernel<T>), dim3((unsigned)((rows * (cols / 4) + 255) / 256)), dim3(256), 0, st,
+                     partial, pick.slices, rows, half, cols, o0, o1, ld);
 }
 
-static hipError_t gated_dx_bf16(int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw,
-                                void* dx, int ldx, float* partial, hipStream_t st) {
+template <class D, typename T>
+static void gated_dx_launch(int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw, T* dx,
+                            int ldx, const SplitPick& pick, const Split& sp, hipStream_t st) {
+  constexpr int e = sizeof(T), per = 128 / e;
   const int Fp = gated_cols(F);
-  const TileOperand a{(const char*)dgu, nullptr, 4u * Fp, M, 0},
-      b{(const char*)Wg, (const char*)Wu, 2u * ldw, F, K};
-  const SplitPick pick = choose_split(M, K, 2 * Fp / 64);
-  const Split sp{pick.slices > 1 ? partial : nullptr, pick.per};
-  T2I_TILES(pick.shape, const TileShape s = tile_shape<D>(M, K, 2 * Fp / 64, 4 * Fp, Fp / 64);
-            hipLaunchKernelGGL((gated_dx_kernel<D>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices),
-                               dim3(D::NW * 64), 0, st, a, b, s, sp, (bf16*)dx, ldx, M, K))
-  if (sp.partial) split_sum(pick, partial, M, M, K, dx, dx, ldx, st);
-  return hipGetLastError();
+  const TileOperand a{(const char*)dgu, nullptr, 2u * e * Fp, M, 0},
+      b{(const char*)Wg, (const char*)Wu, (uint32_t)e * ldw, F, K};
+  const TileShape s = tile_shape<D>(M, K, 2 * Fp / per, 2 * e * Fp, Fp / per);
+  hipLaunchKernelGGL((gated_dx_kernel<D, T>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
+                     st, a, b, s, sp, dx, ldx, M, K);
+  if (sp.partial) split_sum(pick, sp.partial, M, M, K, dx, dx, ldx, st);
 }
 
-static hipError_t gated_dw_bf16(int M, int F, int K, const void* dgu, const void* A, int lda, void* dWg, void* dWu,
-                                int lddw, float* partial, hipStream_t st) {
-  const int Fp = gated_cols(F);
-  const int n = dWg && dWu ? 2 : 1;
-  void* const first = dWg ? dWg : dWu;
-  const TileOperand a{(const char*)dgu + (dWg ? 0 : 2 * (size_t)Fp), nullptr, 4u * Fp, M, F},
-      b{(const char*)A, nullptr, 2u * lda, M, K};
-  const SplitPick pick = choose_split((long)n * F, K, (M + 63) / 64);
-  const Split sp{pick.slices > 1 ? partial : nullptr, pick.per};
-  T2I_TILES(pick.shape, TileShape s = tile_shape<D>(F, K, (M + 63) / 64, 0, 0); const int half = s.tiles_m;
-            s.tiles_m *= n;
-            hipLaunchKernelGGL((gated_dw_kernel<D>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices),
-                               dim3(D::NW * 64), 0, st, a, b, s, sp, half, 2 * Fp, (bf16*)first, (bf16*)dWu, lddw,
-                               F, K))
-  if (sp.partial) split_sum(pick, partial, (long)n * F, F, K, first, dWu, lddw, st);
-  return hipGetLastError();
+template <class D, typename T>
+static void gated_dw_launch(int M, int F, int K, const void* dgu, const void* A, int lda, T* dWg, T* dWu, int lddw,
+                            const SplitPick& pick, const Split& sp, hipStream_t st) {
+  constexpr int e = sizeof(T), per = 128 / e;
+  const int Fp = gated_cols(F), n = dWg && dWu ? 2 : 1;
+  T* const first = dWg ? dWg : dWu;
+  const TileOperand a{(const char*)dgu + (dWg ? 0 : (size_t)e * Fp), nullptr, 2u * e * Fp, M, F},
+      b{(const char*)A, nullptr, (uint32_t)e * lda, M, K};
+  TileShape s = tile_shape<D>(F, K, (M + per - 1) / per, 0, 0);
+  const int half = s.tiles_m;
+  s.tiles_m *= n;
+  hipLaunchKernelGGL((gated_dw_kernel<D, T>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
+                     st, a, b, s, sp, half, e * Fp, first, dWu, lddw, F, K);
+  if (sp.partial) split_sum(pick, sp.partial, (long)n * F, F, K, first, dWu, lddw, st);
 }
 
 static hipError_t gated_fwd_f32(const GatedFwd& a, int M, int F, int K, hipStream_t st) {
-  return gemm_f32_tile((size_t)a.A | (size_t)a.Wg | (size_t)a.Wu, Mat<true>{(const float*)a.A, a.lda, M, K},
+  return gemm_f32_tile(Mat<true>{(const float*)a.A, a.lda, M, K},
                           GateUp{(const float*)a.Wg, (const float*)a.Wu, a.ldw, F, K}, GatedStore{a, M, F}, M,
                           (F + 15) / 16 * 32, K, st);
 }
@@ -655,7 +661,7 @@ static hipError_t gated_fwd_f32(const GatedFwd& a, int M, int F, int K, hipStrea
 static hipError_t gated_dx_f32(int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw,
                            void* dx, int ldx, hipStream_t st) {
   const int Fp = gated_cols(F);
-  return gemm_f32_tile((size_t)dgu | (size_t)Wg | (size_t)Wu, Mat<true>{(const float*)dgu, 2 * Fp, M, 2 * Fp},
+  return gemm_f32_tile(Mat<true>{(const float*)dgu, 2 * Fp, M, 2 * Fp},
                           TwoRows{(const float*)Wg, (const float*)Wu, ldw, F, K, Fp},
                           PlainStore{(float*)dx, ldx, M, K}, M, K, 2 * Fp, st);
 }
@@ -666,7 +672,7 @@ static hipError_t gated_dw_f32(int M, int F, int K, const void* dgu, const void*
   for (int i = 0; i < 2; ++i) {
     float* o = (float*)(i ? dWu : dWg);
     if (!o) continue;
-    const hipError_t e = gemm_f32_tile((size_t)dgu | (size_t)A, Mat<false>{(const float*)dgu + i * Fp, 2 * Fp, M, Fp},   // (zeros behind F)
+    const hipError_t e = gemm_f32_tile(Mat<false>{(const float*)dgu + i * Fp, 2 * Fp, M, Fp},   // (zeros behind F)
                                           Mat<false>{(const float*)A, lda, M, K},
                                           PlainStore{o, lddw, F, K}, F, K, M, st);
     if (e != hipSuccess) return e;
@@ -674,20 +680,42 @@ static hipError_t gated_dw_f32(int M, int F, int K, const void* dgu, const void*
   return hipSuccess;
 }
 
-hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& a, int M, int F, int K, hipStream_t st) {
-  return is_bf16 ? gated_fwd_bf16(a, M, F, K, st) : gated_fwd_f32(a, M, F, K, st);
+hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& p, int M, int F, int K, hipStream_t st) {
+  if (is_bf16)
+    T2I_TILES(choose_tile(kTiles, M, 2L * F, (K + 63) / 64, 0.5f).shape, (gated_fwd_launch<D, bf16>(p, M, F, K, st)))
+  else if (f32_pieces({F, K, p.lda, p.ldw, p.ldo, p.pre ? p.ldp : 0}, {p.A, p.Wg, p.Wu, p.out, p.pre}))
+    T2I_TILES_F32(choose_tile(kTilesF32, M, 2L * F, (K + 31) / 32, 0.5f).shape,
+                  (gated_fwd_launch<D, float>(p, M, F, K, st)))
+  else
+    return gated_fwd_f32(p, M, F, K, st);
+  return hipGetLastError();
 }
 
-hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, const void* Wg,
-                           const void* Wu, int ldw, void* dx, int ldx, float* partial, hipStream_t st) {
-  return is_bf16 ? gated_dx_bf16(M, F, K, dgu, Wg, Wu, ldw, dx, ldx, partial, st)
-                 : gated_dx_f32(M, F, K, dgu, Wg, Wu, ldw, dx, ldx, st);
+hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw,
+                           void* dx, int ldx, float* partial, hipStream_t st) {
+  if (!is_bf16 && !f32_pieces({K, ldw, ldx}, {Wg, Wu, dx})) return gated_dx_f32(M, F, K, dgu, Wg, Wu, ldw, dx, ldx, st);
+  const SplitPick pick = split_of(is_bf16, M, K, 2 * gated_cols(F));
+  const Split sp{pick.slices > 1 ? partial : nullptr, pick.per};
+  if (is_bf16)
+    T2I_TILES(pick.shape, (gated_dx_launch<D, bf16>(M, F, K, dgu, Wg, Wu, ldw, (bf16*)dx, ldx, pick, sp, st)))
+  else
+    T2I_TILES_F32(pick.shape, (gated_dx_launch<D, float>(M, F, K, dgu, Wg, Wu, ldw, (float*)dx, ldx, pick, sp, st)))
+  return hipGetLastError();
 }
 
-hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, const void* A, int lda,
-                           void* dWg, void* dWu, int lddw, float* partial, hipStream_t st) {
-  return is_bf16 ? gated_dw_bf16(M, F, K, dgu, A, lda, dWg, dWu, lddw, partial, st)
-                 : gated_dw_f32(M, F, K, dgu, A, lda, dWg, dWu, lddw, st);
+hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, const void* A, int lda, void* dWg,
+                           void* dWu, int lddw, float* partial, hipStream_t st) {
+  if (!is_bf16 && !f32_pieces({F, K, lda, lddw}, {A, dWg, dWu}))
+    return gated_dw_f32(M, F, K, dgu, A, lda, dWg, dWu, lddw, st);
+  const SplitPick pick = split_of(is_bf16, (dWg && dWu ? 2L : 1L) * F, K, M);
+  const Split sp{pick.slices > 1 ? partial : nullptr, pick.per};
+  if (is_bf16)
+    T2I_TILES(pick.shape,
+              (gated_dw_launch<D, bf16>(M, F, K, dgu, A, lda, (bf16*)dWg, (bf16*)dWu, lddw, pick, sp, st)))
+  else
+    T2I_TILES_F32(pick.shape,
+                  (gated_dw_launch<D, float>(M, F, K, dgu, A, lda, (float*)dWg, (float*)dWu, lddw, pick, sp, st)))
+  return hipGetLastError();
 }
 
 }  // namespace t2i

@@ -62,8 +62,8 @@ hipError_t launch_gate_grad(bool is_bf16, int act, int M, int F, const float* pr
 // dbg[f] / dbu[f] = sum of the partials, in ascending block order
 hipError_t launch_gate_bias_grad(bool is_bf16, int M, int F, const float* partial, void* dbg,
                                  void* dbu, hipStream_t st);
-// fp32 room that the two products below need at `partial` for bf16 operands
-size_t gated_split_floats(int M, int F, int K);
+// fp32 room that the two products below need at `partial`
+size_t gated_split_floats(bool is_bf16, int M, int F, int K);
 // dx [M, K] = dg Wg + du Wu
 hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, const void* Wg,
                            const void* Wu, int ldw, void* dx, int ldx, float* partial, hipStream_t st);

@@ -1,10 +1,12 @@
-// Tile products of the block operators on the gfx950 matrix cores (bf16 and
+// Tile products of the block operators on the gfx950 matrix cores (bf16, fp32 and
 // 8-bit integers), fed by direct HBM -> LDS loads.
 //
 // A workgroup of WGM x WGN waves owns a BM x BN tile of C[m][n] = sum_k a(m, k)
 // b(n, k); a wave owns (BM / WGM) x (BN / WGN) of it in 16 x 16 MFMA tiles
 // (v_mfma_f32_16x16x32_bf16, v_mfma_i32_16x16x64_i8: both take 16 bytes per lane
-// and operand).  k advances by a step of 128 bytes of k per row (64 bf16, 128
+// and operand; fp32: the 16 bytes are the operands of four v_mfma_f32_16x16x4_f32,
+// which between them take 16 of k in an order of their own, the same for both
+// operands).  k advances by a step of 128 bytes of k per row (64 bf16, 32 fp32, 128
 // 8-bit values) through a ring of ST LDS stages; 16 bytes per lane go straight
 // from global memory into LDS (no registers).
 //
@@ -14,9 +16,9 @@
 //     slot c ^ ((r >> 1) & 7), so the 16 rows of a fragment spread over all LDS
 //     banks.
 //   k across the rows ("KR": the operands of the gradients, contracted over
-//     tokens or over output features).  A stage holds 64 rows of the tile's
-//     columns.  A lane reads the same N neighbouring columns of its 8 rows k and
-//     joins the halves of the dwords by v_perm, which gives it 8 k of N columns,
+//     tokens or over output features).  A stage holds 64 (fp32: 32) rows of the tile's
+//     columns.  A lane reads the same N neighbouring columns of its 8 (4) rows k and
+//     joins the halves of bf16 dwords by v_perm, which gives it 8 k of N columns,
 //     the operands of N MFMAs: fragment j of such a group has columns j, N + j,
 //     2 N + j ...  For N = 2 (4-byte reads) the 64-byte piece p of row k sits in
 //     piece p ^ f, f = (k >> 3) & 3, so that the four rows of a read lie in different
@@ -78,7 +80,7 @@ struct TileOperand {
   const char* p2;    // second matrix (two: see TileProduct), else unused
   uint32_t ld;       // bytes from row to row
   int rows;          // KC: rows of the matrix; KR: rows of the contraction
-  int cols;          // KR: columns that may be read (a multiple of 8)
+  int cols;          // KR: columns that may be read (whole 16-byte pieces)
 };
 
 struct TileShape {
@@ -111,32 +113,37 @@ struct TileDims {
   static_assert(WM % 16 == 0 && WN % 16 == 0 && ST >= 2 && ST <= 5 && (ST - 1) * LOADS < 64, "tile shape");
 };
 
-// I8: 8-bit integers, else bf16.  AKR, BKR: operand layouts.  DUAL: b is two
+enum TileElem { ELEM_BF16, ELEM_I8, ELEM_F32 };
+
+// E: element type.  AKR, BKR: operand layouts.  DUAL: b is two
 // matrices side by side, p for the first half of the tile's columns and p2 for the
 // second, so that a wave holds both of an output.  SEGS (BKR): the contraction
 // runs over p's rows, then p2's.
-template <class D, bool I8, bool AKR, bool BKR, bool DUAL, bool SEGS>
+template <class D, TileElem E, bool AKR, bool BKR, bool DUAL, bool SEGS>
 struct TileProduct {
+  static constexpr bool I8 = E == ELEM_I8;
+  static constexpr int EB = E == ELEM_F32 ? 4 : I8 ? 1 : 2;   // bytes of an element
+  static constexpr int KROWS = 128 / EB;                      // k of a step
   using Acc = typename std::conditional<I8, i32x4, f32x4>::type;
   static constexpr int BM = D::BM, BN = D::BN, TM = D::TM, TN = D::TN, ST = D::ST;
 
   // columns per group of a KR operand (see above): a's whole set, two of b's
   static constexpr int NA = AKR ? TM : 1, NB = BKR ? 2 : 1;
-  static_assert(!AKR || TM == 2 || TM == 4 || TM == 8, "fragments per wave");
+  static_assert(!AKR || TM == 2 || TM == 4 || (TM == 8 && EB == 2), "fragments per wave");
   static_assert(!BKR || TN % 2 == 0, "fragments per wave");
 
   // f of the rows k with (k >> 3) & 3 = g (see above; counted by SQ_LDS_BANK_CONFLICT:
   // none so, a half of the LDS cycles with the bits of g swapped for every N)
   template <int N>
-  static __device__ __forceinline__ int kr_swap(int g) { return N == 2 ? g : 0; }
+  static __device__ __forceinline__ int kr_swap(int g) { return EB == 2 && N == 2 ? g : 0; }
   // the (row, column) of a KR tile of W columns that lane `lane` of load block b fills
   template <int W, int N>
   static __device__ __forceinline__ void kr_source(int b, int lane, int& row, int& col) {
-    constexpr int RB = W * 2, MASK = W >= 128 ? 3 : W / 32 - 1;
+    constexpr int RB = W * EB, MASK = W >= 128 ? 3 : W / 32 - 1;
     const int at = b * 1024 + lane * 16;
     row = at / RB;
     const int o = at % RB, f = kr_swap<N>((row >> 3) & 3) & MASK;
-    col = ((o >> 6) ^ f) * 32 + (o & 63) / 2;
+    col = ((o >> 6) ^ f) * (64 / EB) + (o & 63) / EB;
   }
 
   // tile row (column) that index x = 0 .. 15 of fragment i (j) of a wave stands for
@@ -164,7 +171,7 @@ struct TileProduct {
         if (is_a) kr_source<BM, NA>(blk, lane, row, col);
         else kr_source<BN, NB>(blk, lane, row, col);
         const TileOperand& o = is_a ? a : b;
-        src[i] = (uint32_t)row * o.ld + 2u * (uint32_t)min((is_a ? m0 : n0) + col, o.cols - 8);
+        src[i] = (uint32_t)row * o.ld + EB * (uint32_t)min((is_a ? m0 : n0) + col, o.cols - 16 / EB);
       } else {
         const int lr = blk * 8 + (lane >> 3), c = (lane & 7) ^ ((lr >> 1) & 7);
         const TileOperand& o = is_a ? a : b;
@@ -183,9 +190,9 @@ struct TileProduct {
     auto kr_res = [&](const TileOperand& o, int t, bool segs) {
       t += s.first;
       const bool second = segs && t >= s.half;
-      const int row0 = (second ? t - s.half : t) * 64;
+      const int row0 = (second ? t - s.half : t) * KROWS;
       return __builtin_amdgcn_make_buffer_rsrc((void*)((second ? o.p2 : o.p) + (size_t)row0 * o.ld), 0,
-                                               (min(o.rows - row0, 64) - 1) * (int)o.ld + 2 * o.cols, 0x00020000);
+                                               (min(o.rows - row0, KROWS) - 1) * (int)o.ld + EB * o.cols, 0x00020000);
     };
     const __amdgpu_buffer_rsrc_t ra_kc = kc_res(a.p, AKR ? 0 : (size_t)m0 * a.ld + (size_t)s.first * 128);
     const __amdgpu_buffer_rsrc_t rb_kc = kc_res(b.p, BKR ? 0 : (size_t)n0 * b.ld + (size_t)s.first * 128);
@@ -221,27 +228,35 @@ struct TileProduct {
     // N fragments of a KR tile of W columns from column c0 on, its rows from `base`
     auto read_kr = [&](auto n, auto w, uint32_t base, int kk, int c0, i32x4* f) {
       constexpr int N = decltype(n)::value, W = decltype(w)::value, MASK = W >= 128 ? 3 : W / 32 - 1;
-      typedef int raw_t __attribute__((ext_vector_type(N / 2 > 1 ? N / 2 : 2)));
-      const int o = (c0 + N * fr) * 2;
-      const char* at = smem + base + (kk * 32 + g * 8) * W * 2 + (((o >> 6) ^ (kr_swap<N>(g) & MASK)) << 6) + (o & 63);
-      int raw[8][N / 2];
+      constexpr int LK = 16 / EB, DW = N * EB / 4;   // k of a lane, dwords of its read
+      typedef int raw_t __attribute__((ext_vector_type(DW > 1 ? DW : 2)));
+      const int o = (c0 + N * fr) * EB;
+      const char* at = smem + base + (kk * (KROWS / 2) + g * LK) * W * EB + (((o >> 6) ^ (kr_swap<N>(g) & MASK)) << 6) + (o & 63);
+      int raw[LK][DW];
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        if constexpr (N == 2) {
-          raw[k][0] = *(const int*)(at + k * W * 2);
+      for (int k = 0; k < LK; ++k) {
+        if constexpr (DW == 1) {
+          raw[k][0] = *(const int*)(at + k * W * EB);
         } else {
-          const raw_t v = *(const raw_t*)(at + k * W * 2);
+          const raw_t v = *(const raw_t*)(at + k * W * EB);
 #pragma unroll
-          for (int p = 0; p < N / 2; ++p) raw[k][p] = v[p];
+          for (int p = 0; p < DW; ++p) raw[k][p] = v[p];
         }
       }
+      if constexpr (EB == 4) {
 #pragma unroll
-      for (int p = 0; p < N / 2; ++p)
+        for (int p = 0; p < N; ++p)
 #pragma unroll
-        for (int d = 0; d < 4; ++d) {
-          f[2 * p][d] = __builtin_amdgcn_perm(raw[2 * d + 1][p], raw[2 * d][p], 0x05040100);
-          f[2 * p + 1][d] = __builtin_amdgcn_perm(raw[2 * d + 1][p], raw[2 * d][p], 0x07060302);
-        }
+          for (int k = 0; k < 4; ++k) f[p][k] = raw[k][p];
+      } else {
+#pragma unroll
+        for (int p = 0; p < DW; ++p)
+#pragma unroll
+          for (int d = 0; d < 4; ++d) {
+            f[2 * p][d] = __builtin_amdgcn_perm(raw[2 * d + 1][p], raw[2 * d][p], 0x05040100);
+            f[2 * p + 1][d] = __builtin_amdgcn_perm(raw[2 * d + 1][p], raw[2 * d][p], 0x07060302);
+          }
+      }
     };
     auto read_a = [&](uint32_t slot, int kk, i32x4 (&av)[TM]) {
       if constexpr (AKR) {
@@ -263,13 +278,22 @@ struct TileProduct {
       }
     };
     auto column = [&](int j, const i32x4 (&av)[TM]) {
+      if constexpr (E == ELEM_F32) {
 #pragma unroll
-      for (int i = 0; i < TM; ++i) {
-        if constexpr (I8)
-          acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bf[j], av[i], acc[i][j], 0, 0, 0);
-        else
-          acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bf[j]),
-                                                             __builtin_bit_cast(bf16x8, av[i]), acc[i][j], 0, 0, 0);
+        for (int k = 0; k < 4; ++k)
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(bf[j][k]), __int_as_float(av[i][k]),
+                                                             acc[i][j], 0, 0, 0);
+      } else {
+#pragma unroll
+        for (int i = 0; i < TM; ++i) {
+          if constexpr (I8)
+            acc[i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(bf[j], av[i], acc[i][j], 0, 0, 0);
+          else
+            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, bf[j]),
+                                                               __builtin_bit_cast(bf16x8, av[i]), acc[i][j], 0, 0, 0);
+        }
       }
     };
 #pragma unroll

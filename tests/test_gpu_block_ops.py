@@ -263,9 +263,13 @@ def test_gated_linear(M, F, K, act, dtype):
         assert torch.equal(t2i.gated_linear(*d.values(), act=act), out)
 
 
-@pytest.mark.parametrize("M,F,K", [(5, 1, 1), (3, 7, 5), (70, 33, 65), (130, 131, 257)])
-def test_gated_linear_f32_any_width(M, F, K):
+@pytest.mark.parametrize("M,F,K,extra", [(5, 1, 1, 0), (3, 7, 5, 0), (70, 33, 65, 0), (130, 131, 257, 0),
+                                         (130, 132, 260, 0), (70, 36, 68, 4), (70, 36, 68, 1), (300, 700, 333, 2),
+                                         (2100, 12, 20, 0)])
+def test_gated_linear_f32_any_width(M, F, K, extra):
+    """Widths and strides that are no multiples of 16 bytes, and of 16 but not of 32."""
     d, h = gated_case(M, F, K, F32, True, 30)
+    d["x"] = padded(d["x"], extra)[0]
     g, u = blocks.gated_pre(**h)
     eg, eu = pre_bound(h, K)
     ref = blocks.gated("silu", g, u)
