@@ -500,10 +500,12 @@ using Tile128d = TileDims<128, 128, 2, 4, 4>;
 using Tile64 = TileDims<64, 128, 2, 4, 2>;
 using Tile64d = TileDims<64, 128, 2, 4, 4>;
 using Tile32d = TileDims<32, 128, 1, 4, 4>;
-// fp32: bound by the matrix cores (154 TFLOP/s: 1.7 us per step of 128 x 128); no
-// larger tiles, which would only spread worse
-constexpr TileChoice kTilesF32[] = {{128, 128, 1, 1.90f, 1.90f, 5.f}, {64, 128, 1, 0.98f, 0.98f, 3.f},
-                                    {32, 128, 1, 0.55f, 0.55f, 2.f}};
+// fp32: bound by the matrix cores (154 TFLOP/s: 1.7 us per step of 128 x 128), so that
+// two stages are enough and several workgroups share a CU (4096 x 9216 x 1152: 143
+// TFLOP/s on 128 x 128, 139 on 64 x 64, 134 and 128 with four stages; 517 x 2832 x 1152
+// 71 and 39 us)
+using Tile64s = TileDims<64, 64, 2, 2, 2>;
+constexpr TileChoice kTilesF32[] = {{128, 128, 1, 1.95f, 1.85f, 3.f}, {64, 64, 1, 0.65f, 0.50f, 1.5f}};
 constexpr int kMaxSlices = 16;
 constexpr TileChoice kTiles[] = {{256, 256, 1, 1.60f, 1.60f, 13.f}, {256, 128, 1, 0.95f, 0.95f, 8.f},
                                  {128, 128, 2, 0.72f, 1.02f, 6.f},  {128, 128, 1, 0.61f, 0.61f, 5.f},
@@ -560,11 +562,10 @@ hipError_t launch_linear_i8(const int8_t* A, int lda, const int8_t* W, int ldw, 
   return hipGetLastError();
 }
 
-#define T2I_TILES_F32(SHAPE, CALL)               \
-  switch (SHAPE) {                               \
-    case 0: { using D = Tile128d; CALL; break; } \
-    case 1: { using D = Tile64d; CALL; break; }  \
-    default: { using D = Tile32d; CALL; break; } \
+#define T2I_TILES_F32(SHAPE, CALL)              \
+  switch (SHAPE) {                              \
+    case 0: { using D = Tile128; CALL; break; } \
+    default: { using D = Tile64s; CALL; break; } \
   }
 
 template <class D, typename T>
