@@ -1,21 +1,5 @@
-// Matrix products of the block operators: the 8-bit linear layer, the gated
-// feed-forward and its gradients.  They go through the tiles of gemm_tile.h, but
-// for fp32 operands that do not lie in whole, aligned 16-byte pieces, which take
-// gemm_f32_tile_kernel:
-//
-// One product C[m][n] = sum_k a(m, k) b(n, k) on BM x BN tiles by 2 x 2 waves
-// (v_mfma_f32_16x16x4_f32), 32 values of k at a time through two LDS stages, the
-// next step's operands on their way into registers meanwhile.  A lane's four
-// values k = 4 g .. 4 g + 3 of its row feed four MFMAs, which between them take 16
-// of k in an order of their own, the same for both operands.  An operand whose k
-// runs along its rows is staged as [row][k] in rows of 36 dwords (16-byte reads of
-// 16 rows from 16 places), one whose k runs across them as [k][row] in rows of R + 4
-// (4-byte reads of four k from four places): neither meets itself in a bank.  What
-// bounds the 64 x 64 tile is the operands' way from L2 (16 bytes per clock and CU at
-// the matrix cores' full rate), hence 128 x 128 where enough of them fill the chip.
-// Operands are
-// read by element; addresses stay inside the operand and what lies outside is taken
-// as 0, without branches.
+// Matrix products of the block operators on the tiles of gemm_tile.h: the 8-bit
+// linear layer, the gated feed-forward and its gradients.
 #include <algorithm>
 #include <initializer_list>
 
@@ -43,195 +27,7 @@ static TilePick choose_tile(const TileChoice (&c)[N], long rows, long cols, int 
   return best;
 }
 
-// ---- fp32
-
-// Rows [0, rows) x columns [0, cols) of a row-major matrix.  along: the k axis
-// runs along the rows (contiguous in memory), else across them.
-template <bool ALONG>
-struct Mat {
-  static constexpr bool along = ALONG;
-  const float* p;
-  int ld, rows, cols;
-  __device__ __forceinline__ const float* at(int y, int x) const { return p + (size_t)y * ld + x; }
-};
-
-// Gate and up weights side by side: of every 32 rows, 16 of the gate and the
-// same 16 of the up projection, so that one lane ends up with both
-struct GateUp {
-  static constexpr bool along = true;
-  const float *g, *u;
-  int ld, rows, cols;
-  __device__ __forceinline__ const float* at(int y, int x) const {
-    const int f = min(y / 32 * 16 + y % 16, rows - 1);
-    return ((y & 16) ? u : g) + (size_t)f * ld + x;
-  }
-};
-
-// The rows of the gate weights, then those of the up weights, from row `half` on
-struct TwoRows {
-  static constexpr bool along = false;
-  const float *g, *u;
-  int ld, rows, cols, half;
-  __device__ __forceinline__ const float* at(int y, int x) const {
-    const int f = min(y < half ? y : y - half, rows - 1);
-    return (y < half ? g : u) + (size_t)f * ld + x;
-  }
-};
-
-// whether element (y, x) lies in the operand, and the nearest (y, x) that does
-template <bool ALONG>
-__device__ __forceinline__ bool inside(const Mat<ALONG>& m, int& y, int& x) {
-  const bool in = y < m.rows && x < m.cols;
-  y = min(y, m.rows - 1);
-  return in;
-}
-__device__ __forceinline__ bool inside(const GateUp& m, int& y, int& x) {
-  return y / 32 * 16 + y % 16 < m.rows && x < m.cols;
-}
-__device__ __forceinline__ bool inside(const TwoRows& m, int& y, int& x) {
-  return (y < m.half ? y : y - m.half) < m.rows && x < m.cols;
-}
-
-template <int BM, int BN, class LA, class LB, class EP>
-__global__ __launch_bounds__(256) void gemm_f32_tile_kernel(LA la, LB lb, EP ep, TileShape s, int K) {
-  constexpr int BK = 32, LD = 36, TM = BM / 32, TN = BN / 32;
-  constexpr int SA = LA::along ? BM * LD : BK * (BM + 4), SB = LB::along ? BN * LD : BK * (BN + 4);
-  __shared__ __attribute__((aligned(16))) float smem[2][SA + SB];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-  const int wm = wave >> 1, wn = wave & 1, fr = lane & 15, g = lane >> 4;
-  int tm, tn;
-  tile_place(s, blockIdx.x, gridDim.x, tm, tn);
-  const int m0 = tm * BM, n0 = tn * BN;
-  // a thread's elements lie 256 of the stage apart: neighbouring lanes read
-  // neighbouring addresses
-  f32x4 ra[BM / 32], rb[BN / 32];
-  auto load = [&](const auto& op, int r0, int k0, int i, int R) -> f32x4 {
-    using O = typename std::decay<decltype(op)>::type;
-    f32x4 v;
-    int y, x;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = tid + (i * 4 + e) * 256;
-      if constexpr (O::along) y = r0 + c / BK, x = k0 + c % BK;
-      else y = k0 + c / R, x = r0 + c % R;
-      const bool in = inside(op, y, x);
-      const float w = *op.at(y, min(x, op.cols - 1));
-      v[e] = in ? w : 0.f;
-    }
-    return v;
-  };
-  auto fetch = [&](int k0) {
-#pragma unroll
-    for (int i = 0; i < BM / 32; ++i) ra[i] = load(la, m0, k0, i, BM);
-#pragma unroll
-    for (int i = 0; i < BN / 32; ++i) rb[i] = load(lb, n0, k0, i, BN);
-  };
-  auto put = [&](bool along, float* p, int i, int R, f32x4 v) {
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int c = tid + (i * 4 + e) * 256;
-      p[along ? c / BK * LD + c % BK : c / R * (R + 4) + c % R] = v[e];
-    }
-  };
-  auto frag = [&](bool along, const float* p, int row, int k, int R) -> f32x4 {
-    if (along) return *(const f32x4*)(p + row * LD + k);
-    f32x4 v;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) v[e] = p[(k + e) * (R + 4) + row];
-    return v;
-  };
-  f32x4 acc[TM][TN];
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-  fetch(0);
-  int stage = 0;
-  for (int k0 = 0; k0 < K; k0 += BK, stage ^= 1) {
-    float *sA = smem[stage], *sB = sA + SA;
-#pragma unroll
-    for (int i = 0; i < BM / 32; ++i) put(LA::along, sA, i, BM, ra[i]);
-#pragma unroll
-    for (int i = 0; i < BN / 32; ++i) put(LB::along, sB, i, BN, rb[i]);
-    __syncthreads();   // (the other stage was read before this step's writes: one barrier a step)
-    if (k0 + BK < K) fetch(k0 + BK);
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      f32x4 a[TM], b[TN];
-#pragma unroll
-      for (int i = 0; i < TM; ++i) a[i] = frag(LA::along, sA, wm * (BM / 2) + i * 16 + fr, h * 16 + g * 4, BM);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) b[j] = frag(LB::along, sB, wn * (BN / 2) + j * 16 + fr, h * 16 + g * 4, BN);
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-#pragma unroll
-        for (int i = 0; i < TM; ++i)
-#pragma unroll
-          for (int j = 0; j < TN; ++j)
-            acc[i][j] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[j][e], a[i][e], acc[i][j], 0, 0, 0);
-    }
-  }
-  // operands swapped: a lane holds row fr, four columns from g * 4
-#pragma unroll
-  for (int i = 0; i < TM; ++i)
-#pragma unroll
-    for (int j = 0; j < TN; j += 2)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const float v[2] = {acc[i][j][r], acc[i][j + 1][r]};
-        ep(m0 + wm * (BM / 2) + i * 16 + fr, n0 + wn * (BN / 2) + j * 16 + g * 4 + r, v);
-      }
-}
-
-template <int BM, int BN, class LA, class LB, class EP>
-static void gemm_f32_launch(const LA& la, const LB& lb, const EP& ep, int M, int N, int K, hipStream_t st) {
-  const TileShape s{(M + BM - 1) / BM, (N + BN - 1) / BN, 8, 0, 0, 0, 0};
-  hipLaunchKernelGGL((gemm_f32_tile_kernel<BM, BN, LA, LB, EP>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(256), 0,
-                     st, la, lb, ep, s, K);
-}
-
-template <class LA, class LB, class EP>
-static hipError_t gemm_f32_tile(const LA& la, const LB& lb, const EP& ep, int M, int N, int K, hipStream_t st) {
-  constexpr TileChoice tiles[] = {{128, 128, 1, 80, 80, 0}, {64, 64, 1, 24, 24, 0}, {32, 64, 1, 13, 13, 0}};
-  switch (choose_tile(tiles, M, N, 1, 0.f).shape) {
-    case 0: gemm_f32_launch<128, 128>(la, lb, ep, M, N, K, st); break;
-    case 1: gemm_f32_launch<64, 64>(la, lb, ep, M, N, K, st); break;
-    default: gemm_f32_launch<32, 64>(la, lb, ep, M, N, K, st);
-  }
-  return hipGetLastError();
-}
-
-// ---- epilogues: v[0] column n, v[1] column n + 16
-
-struct GatedStore {
-  GatedFwd a;
-  int M, F;
-  __device__ __forceinline__ void operator()(int m, int n, const float (&v)[2]) const {
-    const int f = n / 32 * 16 + n % 16;
-    if (m >= M || f >= F) return;
-    float g = v[0], u = v[1];
-    if (a.bg) g += ((const float*)a.bg)[f], u += ((const float*)a.bu)[f];
-    if (a.pre) {
-      float* p = a.pre + (size_t)m * a.ldp + f;
-      p[0] = g;
-      p[F] = u;
-    }
-    ((float*)a.out)[(size_t)m * a.ldo + f] = (a.act == EPI_GELU ? gelu_tanh(g) : silu(g)) * u;
-  }
-};
-
-struct PlainStore {
-  float* p;
-  int ld, rows, cols;
-  __device__ __forceinline__ void operator()(int m, int n, const float (&v)[2]) const {
-    if (m >= rows) return;
-    if (n < cols) p[(size_t)m * ld + n] = v[0];
-    if (n + 16 < cols) p[(size_t)m * ld + n + 16] = v[1];
-  }
-};
-
-// ---------------------------------------------------------------------------
-// bf16 and 8-bit products on the tiles of gemm_tile.h.
+// ---- kernels
 
 // rows of fp32 values that the epilogue needs, fetched into registers before the
 // main loop (older than its loads, whose waits count younger ones) and put into
@@ -337,10 +133,10 @@ __global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a,
 template <typename T>
 constexpr TileElem elem_of() { return sizeof(T) == 4 ? ELEM_F32 : ELEM_BF16; }
 
-template <class D, typename T>
+template <class D, typename T, bool P4>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand a, TileOperand b, TileShape s,
                                                                      GatedFwd p, int M, int F) {
-  using P = TileProduct<D, elem_of<T>(), false, false, true, false>;
+  using P = TileProduct<D, elem_of<T>(), false, false, true, false, P4>;
   constexpr int THREADS = D::NW * 64, H = D::BN / 2, TH = D::TN / 2;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + D::BN * 4];
   int tm, tn;
@@ -366,7 +162,8 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
 #pragma unroll
     for (int j = 0; j < TH; ++j) {
       const int fl = nw + j * 16 + g * 4, f = f0 + fl;
-      if (f >= F) continue;   // (F % 4 == 0: four columns or none)
+      const int left = P4 ? F - f : 4;   // (else F % 4 == 0: four columns or none)
+      if (f >= F) continue;
       const f32x4 bg = *(const f32x4*)(ev + fl), bu = *(const f32x4*)(ev + H + fl);
       float gv[4], uv[4], y[4];
 #pragma unroll
@@ -377,19 +174,20 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
       }
       if (p.pre) {
         float* q = p.pre + (size_t)m * p.ldp + f;
-        store4(q, 4, true, gv);
-        store4(q + F, 4, true, uv);
+        store4(q, left, !P4, gv);
+        store4(q + F, left, !P4, uv);
       }
-      store4((T*)p.out + (size_t)m * p.ldo + f, 4, true, y);
+      store4((T*)p.out + (size_t)m * p.ldo + f, left, !P4, y);
     }
   }
 }
 
 // The gradients' products.  b is a KR operand: a pair of fragments holds 8
-// neighbouring columns of a row, of which all or the first four exist (N % 4 == 0).
+// neighbouring columns of a row, of which all or the first four exist (N % 4 == 0)
+// except with 4-byte loads.
 // Stored in the operands' type (row stride ldc), or as fp32 partial sums (row stride
 // N) where the contraction is split.
-template <class D, class P, typename T>
+template <class D, class P, bool P4, typename T>
 __device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D::TN], T* C, int ldc, int m0,
                                            int n0, int M, int N) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
@@ -409,8 +207,10 @@ __device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D
         for (int r = 0; r < 4; ++r) v[2 * r] = (bf16)acc[i][j][r], v[2 * r + 1] = (bf16)acc[i][j + 1][r];
         *(bf16x8*)p = v;
       } else {
-        *(f32x4*)p = f32x4{acc[i][j][0], acc[i][j + 1][0], acc[i][j][1], acc[i][j + 1][1]};
-        if (n + 4 < N) *(f32x4*)(p + 4) = f32x4{acc[i][j][2], acc[i][j + 1][2], acc[i][j][3], acc[i][j + 1][3]};
+        const float lo[4] = {acc[i][j][0], acc[i][j + 1][0], acc[i][j][1], acc[i][j + 1][1]};
+        const float hi[4] = {acc[i][j][2], acc[i][j + 1][2], acc[i][j][3], acc[i][j + 1][3]};
+        store4(p, N - n, !P4, lo);
+        store4(p + 4, N - n - 4, !P4, hi);
       }
     }
   }
@@ -428,10 +228,10 @@ __device__ __forceinline__ void take_slice(const Split& sp, TileShape& s) {
   s.steps = min(sp.per, s.steps - s.first);
 }
 
-template <class D, typename T>
+template <class D, typename T, bool P4>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
                                                                  T* dx, int ldx, int M, int K) {
-  using P = TileProduct<D, elem_of<T>(), false, true, false, true>;
+  using P = TileProduct<D, elem_of<T>(), false, true, false, true, P4>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
@@ -439,18 +239,18 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, 
   typename P::Acc acc[D::TM][D::TN];
   P::run(smem, a, b, s, tm * D::BM, tn * D::BN, acc);
   if (sp.partial)
-    store_tile<D, P>(acc, sp.partial + (size_t)blockIdx.y * M * K, K, tm * D::BM, tn * D::BN, M, K);
+    store_tile<D, P, P4>(acc, sp.partial + (size_t)blockIdx.y * M * K, K, tm * D::BM, tn * D::BN, M, K);
   else
-    store_tile<D, P>(acc, dx, ldx, tm * D::BM, tn * D::BN, M, K);
+    store_tile<D, P, P4>(acc, dx, ldx, tm * D::BM, tn * D::BN, M, K);
 }
 
 // row blocks [0, half) are the first output's, the others the second's (their
 // operand lies `shift` bytes further)
-template <class D, typename T>
+template <class D, typename T, bool P4>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
                                                                  int half, int shift, T* d0, T* d1, int ldw,
                                                                  int F, int K) {
-  using P = TileProduct<D, elem_of<T>(), true, true, false, false>;
+  using P = TileProduct<D, elem_of<T>(), true, true, false, false, P4>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
@@ -462,9 +262,9 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, 
   P::run(smem, a, b, s, m0, tn * D::BN, acc);
   if (sp.partial) {
     const size_t of = (size_t)blockIdx.y * (s.tiles_m / half) * F + (second ? F : 0);
-    store_tile<D, P>(acc, sp.partial + of * K, K, m0, tn * D::BN, F, K);
+    store_tile<D, P, P4>(acc, sp.partial + of * K, K, m0, tn * D::BN, F, K);
   } else {
-    store_tile<D, P>(acc, second ? d1 : d0, ldw, m0, tn * D::BN, F, K);
+    store_tile<D, P, P4>(acc, second ? d1 : d0, ldw, m0, tn * D::BN, F, K);
   }
 }
 
@@ -568,13 +368,13 @@ hipError_t launch_linear_i8(const int8_t* A, int lda, const int8_t* W, int ldw, 
     default: { using D = Tile64s; CALL; break; } \
   }
 
-template <class D, typename T>
+template <class D, typename T, bool P4 = false>
 static void gated_fwd_launch(const GatedFwd& p, int M, int F, int K, hipStream_t st) {
   constexpr int e = sizeof(T), per = 128 / e;
   const TileOperand a{(const char*)p.A, nullptr, (uint32_t)e * p.lda, M, 0},
       b{(const char*)p.Wg, (const char*)p.Wu, (uint32_t)e * p.ldw, F, 0};
   const TileShape s = tile_shape<D>(M, 2 * F, (K + per - 1) / per, e * K, 0);
-  hipLaunchKernelGGL((gated_linear_kernel<D, T>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64), 0, st, a,
+  hipLaunchKernelGGL((gated_linear_kernel<D, T, P4>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64), 0, st, a,
                      b, s, p, M, F);
 }
 
@@ -624,7 +424,7 @@ static void split_sum(const SplitPick& pick, const float* partial, long rows, lo
                      partial, pick.slices, rows, half, cols, o0, o1, ld);
 }
 
-template <class D, typename T>
+template <class D, typename T, bool P4 = false>
 static void gated_dx_launch(int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw, T* dx,
                             int ldx, const SplitPick& pick, const Split& sp, hipStream_t st) {
   constexpr int e = sizeof(T), per = 128 / e;
@@ -632,12 +432,12 @@ static void gated_dx_launch(int M, int F, int K, const void* dgu, const void* Wg
   const TileOperand a{(const char*)dgu, nullptr, 2u * e * Fp, M, 0},
       b{(const char*)Wg, (const char*)Wu, (uint32_t)e * ldw, F, K};
   const TileShape s = tile_shape<D>(M, K, 2 * Fp / per, 2 * e * Fp, Fp / per);
-  hipLaunchKernelGGL((gated_dx_kernel<D, T>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
+  hipLaunchKernelGGL((gated_dx_kernel<D, T, P4>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
                      st, a, b, s, sp, dx, ldx, M, K);
   if (sp.partial) split_sum(pick, sp.partial, M, M, K, dx, dx, ldx, st);
 }
 
-template <class D, typename T>
+template <class D, typename T, bool P4 = false>
 static void gated_dw_launch(int M, int F, int K, const void* dgu, const void* A, int lda, T* dWg, T* dWu, int lddw,
                             const SplitPick& pick, const Split& sp, hipStream_t st) {
   constexpr int e = sizeof(T), per = 128 / e;
@@ -648,74 +448,56 @@ static void gated_dw_launch(int M, int F, int K, const void* dgu, const void* A,
   TileShape s = tile_shape<D>(F, K, (M + per - 1) / per, 0, 0);
   const int half = s.tiles_m;
   s.tiles_m *= n;
-  hipLaunchKernelGGL((gated_dw_kernel<D, T>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
+  hipLaunchKernelGGL((gated_dw_kernel<D, T, P4>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
                      st, a, b, s, sp, half, e * Fp, first, dWu, lddw, F, K);
   if (sp.partial) split_sum(pick, sp.partial, (long)n * F, F, K, first, dWu, lddw, st);
 }
 
-static hipError_t gated_fwd_f32(const GatedFwd& a, int M, int F, int K, hipStream_t st) {
-  return gemm_f32_tile(Mat<true>{(const float*)a.A, a.lda, M, K},
-                          GateUp{(const float*)a.Wg, (const float*)a.Wu, a.ldw, F, K}, GatedStore{a, M, F}, M,
-                          (F + 15) / 16 * 32, K, st);
-}
-
-static hipError_t gated_dx_f32(int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw,
-                           void* dx, int ldx, hipStream_t st) {
-  const int Fp = gated_cols(F);
-  return gemm_f32_tile(Mat<true>{(const float*)dgu, 2 * Fp, M, 2 * Fp},
-                          TwoRows{(const float*)Wg, (const float*)Wu, ldw, F, K, Fp},
-                          PlainStore{(float*)dx, ldx, M, K}, M, K, 2 * Fp, st);
-}
-
-static hipError_t gated_dw_f32(int M, int F, int K, const void* dgu, const void* A, int lda, void* dWg,
-                           void* dWu, int lddw, hipStream_t st) {
-  const int Fp = gated_cols(F);
-  for (int i = 0; i < 2; ++i) {
-    float* o = (float*)(i ? dWu : dWg);
-    if (!o) continue;
-    const hipError_t e = gemm_f32_tile(Mat<false>{(const float*)dgu + i * Fp, 2 * Fp, M, Fp},   // (zeros behind F)
-                                          Mat<false>{(const float*)A, lda, M, K},
-                                          PlainStore{o, lddw, F, K}, F, K, M, st);
-    if (e != hipSuccess) return e;
-  }
-  return hipSuccess;
-}
-
 hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& p, int M, int F, int K, hipStream_t st) {
+  const TilePick f32 = choose_tile(kTilesF32, M, 2L * F, (K + 31) / 32, 0.5f);
   if (is_bf16)
     T2I_TILES(choose_tile(kTiles, M, 2L * F, (K + 63) / 64, 0.5f).shape, (gated_fwd_launch<D, bf16>(p, M, F, K, st)))
   else if (f32_pieces({F, K, p.lda, p.ldw, p.ldo, p.pre ? p.ldp : 0}, {p.A, p.Wg, p.Wu, p.out, p.pre}))
-    T2I_TILES_F32(choose_tile(kTilesF32, M, 2L * F, (K + 31) / 32, 0.5f).shape,
-                  (gated_fwd_launch<D, float>(p, M, F, K, st)))
+    T2I_TILES_F32(f32.shape, (gated_fwd_launch<D, float>(p, M, F, K, st)))
   else
-    return gated_fwd_f32(p, M, F, K, st);
+    T2I_TILES_F32(f32.shape, (gated_fwd_launch<D, float, true>(p, M, F, K, st)))
   return hipGetLastError();
 }
 
 hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw,
                            void* dx, int ldx, float* partial, hipStream_t st) {
-  if (!is_bf16 && !f32_pieces({K, ldw, ldx}, {Wg, Wu, dx})) return gated_dx_f32(M, F, K, dgu, Wg, Wu, ldw, dx, ldx, st);
   const SplitPick pick = split_of(is_bf16, M, K, 2 * gated_cols(F));
   const Split sp{pick.slices > 1 ? partial : nullptr, pick.per};
-  if (is_bf16)
+  if (is_bf16) {
     T2I_TILES(pick.shape, (gated_dx_launch<D, bf16>(M, F, K, dgu, Wg, Wu, ldw, (bf16*)dx, ldx, pick, sp, st)))
-  else
+  } else if (f32_pieces({K, ldw, ldx}, {Wg, Wu, dx})) {
     T2I_TILES_F32(pick.shape, (gated_dx_launch<D, float>(M, F, K, dgu, Wg, Wu, ldw, (float*)dx, ldx, pick, sp, st)))
+  } else {
+    const int steps = 2 * gated_cols(F) / 32;   // (the slices' sum takes whole pieces: one slice)
+    T2I_TILES_F32(choose_tile(kTilesF32, M, K, steps, 1.f).shape,
+                  (gated_dx_launch<D, float, true>(M, F, K, dgu, Wg, Wu, ldw, (float*)dx, ldx, SplitPick{0, 1, steps},
+                                                   Split{nullptr, steps}, st)))
+  }
   return hipGetLastError();
 }
 
 hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, const void* A, int lda, void* dWg,
                            void* dWu, int lddw, float* partial, hipStream_t st) {
-  if (!is_bf16 && !f32_pieces({F, K, lda, lddw}, {A, dWg, dWu}))
-    return gated_dw_f32(M, F, K, dgu, A, lda, dWg, dWu, lddw, st);
-  const SplitPick pick = split_of(is_bf16, (dWg && dWu ? 2L : 1L) * F, K, M);
+  const long rows = (dWg && dWu ? 2L : 1L) * F;
+  const SplitPick pick = split_of(is_bf16, rows, K, M);
   const Split sp{pick.slices > 1 ? partial : nullptr, pick.per};
-  if (is_bf16)
+  if (is_bf16) {
     T2I_TILES(pick.shape,
               (gated_dw_launch<D, bf16>(M, F, K, dgu, A, lda, (bf16*)dWg, (bf16*)dWu, lddw, pick, sp, st)))
-  else
+  } else if (f32_pieces({F, K, lda, lddw}, {A, dWg, dWu})) {
     T2I_TILES_F32(pick.shape,
                   (gated_dw_launch<D, float>(M, F, K, dgu, A, lda, (float*)dWg, (float*)dWu, lddw, pick, sp, st)))
+  } else {
+    const int steps = (M + 31) / 32;
+    T2I_TILES_F32(choose_tile(kTilesF32, rows, K, steps, 1.f).shape,
+                  (gated_dw_launch<D, float, true>(M, F, K, dgu, A, lda, (float*)dWg, (float*)dWu, lddw,
+                                                   SplitPick{0, 1, steps}, Split{nullptr, steps}, st)))
+  }
   return hipGetLastError();
 }
 

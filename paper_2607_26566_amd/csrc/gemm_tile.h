@@ -32,6 +32,9 @@
 // when every fragment of the stage is in registers; then the stage is refilled
 // and the next stage's fragments are read under the remaining columns.
 //
+// fp32 operands that do not lie in whole, aligned 16-byte pieces are loaded 4 bytes
+// per lane instead (P4), four times the load instructions into the same layout.
+//
 // Sizes: rows behind the operand are read as its last row (KC) or as zeros (KR,
 // by the buffer resource's bound), k behind the end as zeros (by an offset
 // behind the resource); what they add up to is not stored.
@@ -67,6 +70,14 @@ __device__ __forceinline__ void tile_barrier() {
   asm volatile("s_barrier" ::: "memory");
 }
 
+// BYTES per lane from global memory into LDS at the wave-uniform address lds
+template <int BYTES>
+__device__ __forceinline__ void tile_load(__amdgpu_buffer_rsrc_t r, char* lds, uint32_t voff, int soff) {
+  auto* d = (__attribute__((address_space(3))) void*)lds;
+  if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, d, 16, voff, soff, 0, 0);
+  else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, d, 4, voff, soff, 0, 0);
+}
+
 // consecutive workgroups of one XCD (they are dealt out in turn over 8) get
 // consecutive tiles
 __device__ __forceinline__ int tile_of_block(int b, int nb) {
@@ -80,7 +91,7 @@ struct TileOperand {
   const char* p2;    // second matrix (two: see TileProduct), else unused
   uint32_t ld;       // bytes from row to row
   int rows;          // KC: rows of the matrix; KR: rows of the contraction
-  int cols;          // KR: columns that may be read (whole 16-byte pieces)
+  int cols;          // KR: columns that may be read (whole pieces of a load)
 };
 
 struct TileShape {
@@ -118,9 +129,14 @@ enum TileElem { ELEM_BF16, ELEM_I8, ELEM_F32 };
 // E: element type.  AKR, BKR: operand layouts.  DUAL: b is two
 // matrices side by side, p for the first half of the tile's columns and p2 for the
 // second, so that a wave holds both of an output.  SEGS (BKR): the contraction
-// runs over p's rows, then p2's.
-template <class D, TileElem E, bool AKR, bool BKR, bool DUAL, bool SEGS>
+// runs over p's rows, then p2's.  P4: loads of 4 bytes (fp32).
+template <class D, TileElem E, bool AKR, bool BKR, bool DUAL, bool SEGS, bool P4 = false>
 struct TileProduct {
+  static_assert(!P4 || E == ELEM_F32, "4-byte loads");
+  static constexpr int Q = P4 ? 4 : 1;   // load instructions per KB
+  static constexpr int PB = 16 / Q;      // bytes per lane of one
+  static constexpr int LOADS = D::LOADS * Q;
+  static_assert((D::ST - 1) * LOADS < 64, "outstanding loads");
   static constexpr bool I8 = E == ELEM_I8;
   static constexpr int EB = E == ELEM_F32 ? 4 : I8 ? 1 : 2;   // bytes of an element
   static constexpr int KROWS = 128 / EB;                      // k of a step
@@ -136,11 +152,10 @@ struct TileProduct {
   // none so, a half of the LDS cycles with the bits of g swapped for every N)
   template <int N>
   static __device__ __forceinline__ int kr_swap(int g) { return EB == 2 && N == 2 ? g : 0; }
-  // the (row, column) of a KR tile of W columns that lane `lane` of load block b fills
+  // the (row, column) of a KR tile of W columns that byte `at` of its stage holds
   template <int W, int N>
-  static __device__ __forceinline__ void kr_source(int b, int lane, int& row, int& col) {
+  static __device__ __forceinline__ void kr_source(int at, int& row, int& col) {
     constexpr int RB = W * EB, MASK = W >= 128 ? 3 : W / 32 - 1;
-    const int at = b * 1024 + lane * 16;
     row = at / RB;
     const int o = at % RB, f = kr_swap<N>((row >> 3) & 3) & MASK;
     col = ((o >> 6) ^ f) * (64 / EB) + (o & 63) / EB;
@@ -157,31 +172,35 @@ struct TileProduct {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / D::WGN, wn = wave % D::WGN, fr = lane & 15, g = lane >> 4;
-    constexpr int LA = BM / 8 / D::NW, LB = D::LOADS - LA;
+    constexpr int LA = BM / 8 / D::NW;
     const int KT = s.steps;
 
-    // ---- sources: this lane's offset of each load, the resource by operand
-    uint32_t src[D::LOADS];
+    // ---- sources: this lane's offset of each load.  Load i takes part i % Q of KB
+    // block wave + i / Q waves, a's blocks first; byte `at` of that operand's stage.
+    auto block_of = [&](int i) { return wave + (i / Q < LA ? i / Q : i / Q - LA) * D::NW; };
+    auto at_of = [&](int i) { return block_of(i) * 1024 + i % Q * 256 + lane * PB; };
+    // KC: row and byte of k (within the step) of a place in the stage
+    auto kc_row = [](int at) { return at >> 7; };
+    auto kc_byte = [](int at) { return ((((at >> 4) & 7) ^ ((at >> 8) & 7)) << 4) | (at & 15); };
+    uint32_t src[LOADS];
 #pragma unroll
-    for (int i = 0; i < D::LOADS; ++i) {
-      const bool is_a = i < LA;
-      const int blk = wave + (is_a ? i : i - LA) * D::NW;
+    for (int i = 0; i < LOADS; ++i) {
+      const bool is_a = i / Q < LA;
+      const TileOperand& o = is_a ? a : b;
+      const int at = at_of(i);
       if (is_a ? AKR : BKR) {
         int row, col;
-        if (is_a) kr_source<BM, NA>(blk, lane, row, col);
-        else kr_source<BN, NB>(blk, lane, row, col);
-        const TileOperand& o = is_a ? a : b;
-        src[i] = (uint32_t)row * o.ld + EB * (uint32_t)min((is_a ? m0 : n0) + col, o.cols - 16 / EB);
+        if (is_a) kr_source<BM, NA>(at, row, col);
+        else kr_source<BN, NB>(at, row, col);
+        src[i] = (uint32_t)row * o.ld + EB * (uint32_t)min((is_a ? m0 : n0) + col, o.cols - PB / EB);
       } else {
-        const int lr = blk * 8 + (lane >> 3), c = (lane & 7) ^ ((lr >> 1) & 7);
-        const TileOperand& o = is_a ? a : b;
         // rows from the tile's first, not behind the last (DUAL: within the half)
-        const int r0 = is_a ? m0 : n0;
+        const int r0 = is_a ? m0 : n0, lr = kc_row(at);
         const int rr = !is_a && DUAL && lr >= BN / 2 ? lr - BN / 2 : lr;
-        src[i] = (uint32_t)min(rr, o.rows - 1 - r0) * o.ld + c * 16;
+        src[i] = (uint32_t)min(rr, o.rows - 1 - r0) * o.ld + kc_byte(at);
       }
     }
-    const bool ragged_k = !I8 && s.kbytes % 128 != 0;   // KC: pieces of the last step lie behind k
+    const bool ragged_k = !I8 && s.kbytes % 128 != 0;   // KC: places of the last step lie behind k
     // KC: rows at fixed offsets from the tile's first, k as the scalar offset.
     // KR: the step's first row as the base, the resource ends with its last row.
     auto kc_res = [](const char* p, size_t off) {
@@ -201,19 +220,16 @@ struct TileProduct {
     auto res_b = [&](int t) { return BKR ? kr_res(b, t, SEGS) : rb_kc; };
     auto issue = [&](int i, int t, uint32_t slot, const __amdgpu_buffer_rsrc_t& ra,
                      const __amdgpu_buffer_rsrc_t& rb) {
-      const bool is_a = i < LA;
-      const int blk = wave + (is_a ? i : i - LA) * D::NW;
-      auto* dst = (__attribute__((address_space(3))) void*)(smem + slot + (is_a ? 0 : BM * 128) + blk * 1024);
+      const bool is_a = i / Q < LA;
+      const int blk = block_of(i);
+      char* const dst = smem + slot + (is_a ? 0 : BM * 128) + blk * 1024 + i % Q * 256;
       if (is_a ? AKR : BKR) {
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? ra : rb, dst, 16, src[i], 0, 0, 0);
+        tile_load<PB>(is_a ? ra : rb, dst, src[i], 0);
       } else {
         uint32_t v = src[i];
-        if (ragged_k && t == KT - 1) {
-          const int lr = blk * 8 + (lane >> 3), c = (lane & 7) ^ ((lr >> 1) & 7);
-          if ((s.first + t) * 128 + c * 16 >= s.kbytes) v = kTileOff;
-        }
+        if (ragged_k && t == KT - 1 && (s.first + t) * 128 + kc_byte(at_of(i)) >= s.kbytes) v = kTileOff;
         const bool up = DUAL && !is_a && blk * 8 >= BN / 2;
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(is_a ? ra : up ? rb2_kc : rb, dst, 16, v, t * 128, 0, 0);
+        tile_load<PB>(is_a ? ra : up ? rb2_kc : rb, dst, v, t * 128);
       }
     };
 
@@ -303,15 +319,15 @@ struct TileProduct {
 
     // ---- loop
     constexpr int S = TN / 3;                                   // columns before the barrier
-    constexpr int LPC = (D::LOADS + TN - S - 1) / (TN - S);     // loads per column after it
+    constexpr int LPC = (LOADS + TN - S - 1) / (TN - S);     // loads per column after it
 #pragma unroll
     for (int t = 0; t < ST; ++t)
       if (t < KT) {
         const __amdgpu_buffer_rsrc_t ra = res_a(t), rb = res_b(t);
 #pragma unroll
-        for (int i = 0; i < D::LOADS; ++i) issue(i, t, t * D::STAGE, ra, rb);
+        for (int i = 0; i < LOADS; ++i) issue(i, t, t * D::STAGE, ra, rb);
       }
-    tile_wait<D::LOADS>(min(ST, KT) - 1);
+    tile_wait<LOADS>(min(ST, KT) - 1);
     tile_barrier();
     read_a(0, 0, a0);
 #pragma unroll
@@ -333,7 +349,7 @@ struct TileProduct {
     for (int t = 0; t < KT - 1; ++t) {
       half0(slot);
       if constexpr (ST == 2) tile_vmcnt<0>();
-      else tile_wait<D::LOADS>(min(ST - 2, KT - 2 - t));   // stage t + 1 landed
+      else tile_wait<LOADS>(min(ST - 2, KT - 2 - t));   // stage t + 1 landed
       tile_barrier();
       const uint32_t next = slot == (ST - 1) * D::STAGE ? 0 : slot + D::STAGE;
       const bool more = t + ST < KT;
@@ -348,7 +364,7 @@ struct TileProduct {
         if (more) {
 #pragma unroll
           for (int q = 0; q < LPC; ++q)
-            if ((j - S) * LPC + q < D::LOADS) issue((j - S) * LPC + q, t + ST, slot, ra, rb);
+            if ((j - S) * LPC + q < LOADS) issue((j - S) * LPC + q, t + ST, slot, ra, rb);
         }
         __builtin_amdgcn_sched_barrier(0);
       }
