@@ -210,8 +210,10 @@ struct TileProduct {
       t += s.first;
       const bool second = segs && t >= s.half;
       const int row0 = (second ? t - s.half : t) * KROWS;
+      // (a step may lie wholly behind the rows: nothing to read)
+      const int left = min(o.rows - row0, KROWS);
       return __builtin_amdgcn_make_buffer_rsrc((void*)((second ? o.p2 : o.p) + (size_t)row0 * o.ld), 0,
-                                               (min(o.rows - row0, KROWS) - 1) * (int)o.ld + EB * o.cols, 0x00020000);
+                                               left > 0 ? (left - 1) * (int)o.ld + EB * o.cols : 0, 0x00020000);
     };
     const __amdgpu_buffer_rsrc_t ra_kc = kc_res(a.p, AKR ? 0 : (size_t)m0 * a.ld + (size_t)s.first * 128);
     const __amdgpu_buffer_rsrc_t rb_kc = kc_res(b.p, BKR ? 0 : (size_t)n0 * b.ld + (size_t)s.first * 128);

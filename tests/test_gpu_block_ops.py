@@ -400,6 +400,25 @@ def test_gated_strides_and_surroundings(dtype):
         assert (dw[:, K:] == 7).all() and (dw[2 * F] == 7).all()
 
 
+def inside_nan(t, rows=70):
+    """t as the first rows and columns of a buffer of NaN, `rows` rows of it behind t."""
+    buf = torch.full((t.shape[0] + rows, t.shape[1] + 8), float("nan"), dtype=t.dtype, device=DEV)
+    buf[:t.shape[0], :t.shape[1]] = t
+    return buf[:t.shape[0], :t.shape[1]]
+
+
+@pytest.mark.parametrize("M,F,K", [(2, 8, 1256), (3, 72, 40), (33, 40, 72), (65, 104, 200), (130, 264, 136)])
+@DTYPES
+def test_gated_reads_nothing_behind_its_operands(M, F, K, dtype):
+    d, h = gated_case(M, F, K, dtype, True, 110)
+    for name in ("x", "wg", "wu"):
+        d[name] = inside_nan(d[name])
+    out, pre = t2i.gated_linear(*d.values(), save_pre=True)
+    assert torch.isfinite(out).all() and torch.isfinite(pre).all()
+    dout, hd = rnd(111, (M, F), 1.0, dtype)
+    check_backward(dtype, "silu", d, h, inside_nan(pre), inside_nan(dout), hd)
+
+
 def test_gated_not_finite_values_stay_where_they_belong():
     M, F, K = 70, 72, 136
     d, _ = gated_case(M, F, K, BF16, False, 100)
