@@ -501,4 +501,22 @@ hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, c
   return hipGetLastError();
 }
 
+// The tile and the slices that a product takes (op 0: 8-bit layer with F columns, 1:
+// gated forward, 2: dx, 3: dWg and dWu)
+extern "C" int t2i_test_block_tile(int op, int is_bf16, int M, int F, int K, int* rows, int* columns, int* per_cu,
+                                   int* slices) {
+  if (M < 1 || F < 1 || K < 1 || op < 0 || op > 3) return 0;
+  SplitPick p{0, 1, 0};
+  if (op == 0) p.shape = choose_tile(kTiles, M, F, i8_row(K) / 128, 1.f).shape;
+  else if (op == 1) p.shape = is_bf16 ? choose_tile(kTiles, M, 2L * F, (K + 63) / 64, 0.5f).shape
+                                      : choose_tile(kTilesF32, M, 2L * F, (K + 31) / 32, 0.5f).shape;
+  else p = op == 2 ? split_of(is_bf16, M, K, 2 * gated_cols(F)) : split_of(is_bf16, 2L * F, K, M);
+  const TileChoice& c = op == 0 || is_bf16 ? kTiles[p.shape] : kTilesF32[p.shape];
+  *rows = c.bm;
+  *columns = c.bn;
+  *per_cu = c.per_cu;
+  *slices = p.slices;
+  return 1;
+}
+
 }  // namespace t2i

@@ -71,6 +71,11 @@ hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, c
 hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, const void* A, int lda,
                            void* dWg, void* dWu, int lddw, float* partial, hipStream_t st);
 
+// For the tests, which assert that a shape reaches the tile it is there for (host
+// arithmetic only): the tile of a product, its workgroups per CU and slices.
+extern "C" int t2i_test_block_tile(int op, int is_bf16, int M, int F, int K, int* rows, int* columns, int* per_cu,
+                                   int* slices);
+
 // ---- query / key norm with rotation
 
 struct QkNorm {

@@ -442,6 +442,146 @@ def test_gated_not_finite_values_stay_where_they_belong():
         assert torch.isnan(b[:, col]).all() and torch.equal(a[:, keep], b[:, keep])
 
 
+# ------------------------------------------------------------------ every tile, long rows
+
+def tile_of(op, dtype, M, F, K):
+    """(rows, columns, workgroups per CU, slices) that a product takes"""
+    v = [C.c_int() for _ in range(4)]
+    assert t2i.load().t2i_test_block_tile(op, int(dtype == BF16), M, F, K, *map(C.byref, v))
+    return tuple(x.value for x in v)
+
+
+def some(n, seed):
+    """A few indices below n, the first and the last among them."""
+    r = np.random.default_rng(seed)
+    return np.unique(np.concatenate([[0, n - 1], r.integers(0, n, min(n, 40))]))
+
+
+@pytest.mark.parametrize("M,N,K,tile", [
+    (33, 72, 72, (32, 128, 1)), (4100, 136, 72, (64, 128, 1)), (8200, 136, 72, (64, 128, 3)),
+    (8200, 136, 200, (128, 128, 1)), (8200, 4104, 520, (128, 128, 2)), (2050, 2056, 12300, (256, 128, 1)),
+    (2050, 4104, 2056, (256, 256, 1))])
+def test_linear_i8_on_every_tile(M, N, K, tile):
+    assert tile_of(0, BF16, M, N, K) == (*tile, 1)
+    a, sa, w, sw = i8_operands(M, N, K, 120)
+    d = [dev(v, torch.int8) if v.dtype == np.int8 else dev(v) for v in (a, sa, w, sw)]
+    b, rb = rnd(121, (N,), 0.3, BF16)
+    i = some(M, 1)
+    # (an exact product in float64: whole numbers below 2^53)
+    acc = (a[i, :K].astype(np.float64) @ w[:, :K].astype(np.float64).T) * sa[i, None].astype(np.float64) * sw
+    for dtype in (BF16, F32):
+        bias = b.to(dtype)
+        for epi in ("store", "gelu"):
+            ref = acc + rb if epi == "store" else blocks.act(epi, acc + rb)
+            out = t2i.linear_i8(*d, bias, K=K, epilogue=epi, dtype=dtype)
+            within(out[torch.from_numpy(i).to(DEV)], ref, i8_bound(acc, rb, ref, dtype, epi), (epi, dtype))
+    x0, _ = rnd(122, (M, N), 2.0)
+    gate, rg = rnd(123, (N,), 0.5)
+    x = t2i.linear_i8(*d, b, K=K, epilogue="resid_gated", resid=x0.clone(), gate=gate)
+    y = acc + rb
+    ref = to_host(x0[torch.from_numpy(i).to(DEV)]) + rg * y
+    within(x[torch.from_numpy(i).to(DEV)], ref,
+           np.abs(rg) * i8_bound(acc, rb, y, F32, "store") + 2 * E * (np.abs(rg * y) + np.abs(ref)), "resid")
+
+
+@pytest.mark.parametrize("M,F,K,dtype,tile", [
+    (33, 72, 72, BF16, (32, 128, 1)), (4100, 72, 72, BF16, (64, 128, 1)), (2050, 1032, 72, BF16, (64, 128, 3)),
+    (8200, 72, 72, BF16, (128, 128, 1)), (4100, 4104, 72, BF16, (128, 128, 2)),
+    (2050, 1032, 2056, BF16, (256, 128, 1)), (2050, 2056, 520, BF16, (256, 256, 1)),
+    (300, 200, 72, F32, (64, 64, 1)), (4100, 4104, 72, F32, (128, 128, 1)), (4100, 4101, 71, F32, (128, 128, 1))])
+def test_gated_linear_on_every_tile(M, F, K, dtype, tile):
+    assert tile_of(1, dtype, M, F, K) == (*tile, 1)
+    d, h = gated_case(M, F, K, dtype, True, 130)
+    out, pre = t2i.gated_linear(*d.values(), act="silu", save_pre=True)
+    i = some(M, 2)
+    it = torch.from_numpy(i).to(DEV)
+    h["x"] = h["x"][i]
+    g, u = blocks.gated_pre(**h)
+    eg, eu = pre_bound(h, K)
+    ref = blocks.gated("silu", g, u)
+    tol = 1.13 * eg * (np.abs(u) + eu) + np.abs(blocks.act("silu", g)) * eu + 2.0 ** -20 * np.abs(g * u) + 2 * E * np.abs(ref)
+    within(out[it], ref, tol + U[dtype] * (np.abs(ref) + tol))
+    within(pre[it], np.concatenate([g, u], 1), np.concatenate([eg, eu], 1) + E * np.abs(np.concatenate([g, u], 1)))
+
+
+@pytest.mark.parametrize("op,M,F,K,dtype,tile", [
+    ("dx", 33, 72, 72, BF16, (32, 128, 1, 1)), ("dx", 8200, 72, 72, BF16, (64, 128, 1, 1)),
+    ("dx", 2050, 72, 2056, BF16, (64, 128, 3, 1)), ("dx", 8200, 72, 200, BF16, (128, 128, 1, 1)),
+    ("dx", 8200, 72, 4104, BF16, (128, 128, 2, 1)), ("dx", 8200, 4104, 520, BF16, (256, 128, 1, 1)),
+    ("dx", 2050, 264, 4104, BF16, (256, 256, 1, 1)), ("dx", 33, 2056, 72, BF16, (32, 128, 1, 14)),
+    ("dx", 130, 4104, 4104, BF16, (64, 128, 3, 7)), ("dx", 257, 4104, 4104, BF16, (128, 128, 2, 5)),
+    ("dx", 1030, 2056, 1032, BF16, (128, 128, 1, 3)), ("dx", 2050, 4104, 2056, BF16, (256, 256, 1, 3)),
+    ("dx", 4100, 72, 4104, F32, (128, 128, 1, 1)), ("dx", 4100, 71, 4103, F32, (128, 128, 1, 1)),
+    ("dx", 70, 1032, 72, F32, (64, 64, 1, 14)),
+    ("dw", 33, 72, 72, BF16, (32, 128, 1, 1)), ("dw", 33, 4104, 72, BF16, (64, 128, 1, 1)),
+    ("dw", 33, 4104, 200, BF16, (64, 128, 3, 1)), ("dw", 70, 4104, 200, BF16, (128, 128, 1, 1)),
+    ("dw", 130, 4104, 4104, BF16, (128, 128, 2, 1)), ("dw", 4100, 1032, 2056, BF16, (256, 128, 1, 1)),
+    ("dw", 1030, 2056, 2056, BF16, (256, 256, 1, 1)), ("dw", 8200, 72, 72, BF16, (32, 128, 1, 15)),
+    ("dw", 8200, 136, 4104, BF16, (128, 128, 2, 5)), ("dw", 8200, 1032, 2056, BF16, (256, 256, 1, 3)),
+    ("dw", 8200, 72, 4104, BF16, (64, 128, 3, 7)), ("dw", 70, 2056, 2056, F32, (128, 128, 1, 1)),
+    ("dw", 70, 2055, 2055, F32, (128, 128, 1, 1)), ("dw", 4100, 72, 72, F32, (64, 64, 1, 15))])
+def test_gated_gradients_on_every_tile(op, M, F, K, dtype, tile):
+    assert tile_of(2 if op == "dx" else 3, dtype, M, F, K) == tile
+    say(op, M, F, K, NAME[dtype], tile)
+    d, h = gated_case(M, F, K, dtype, False, 140)
+    pre, hp = rnd(141, (M, 2 * F), 1.5)
+    dout, hd = rnd(142, (M, F), 1.0, dtype)
+    got = t2i.gated_linear_backward(dout, d["x"], d["wg"], d["wu"], pre, act="gelu", need_dx=op == "dx",
+                                    need_dw=op == "dw")
+    i = some(M if op == "dx" else F, 3)
+    it = torch.from_numpy(i).to(DEV)
+    g, u = hp[:, :F], hp[:, F:]
+    if op == "dx":
+        g, u, hd = g[i], u[i], hd[i]
+    else:
+        g, u, hd = g[:, i], u[:, i], hd[:, i]
+    dg, du = hd * u * blocks.act_grad("gelu", g), hd * blocks.act("gelu", g)
+    fg, fu = 2.0 ** -20 * np.abs(hd * u) * (1 + np.abs(g)), 2.0 ** -20 * np.abs(hd * g)
+    eg, eu = fg + U[dtype] * (np.abs(dg) + fg), fu + U[dtype] * (np.abs(du) + fu)
+    if op == "dx":
+        cases = [(got[0], dg @ h["wg"] + du @ h["wu"], eg @ np.abs(h["wg"]) + eu @ np.abs(h["wu"]) +
+                  2 * F * E * (np.abs(dg) @ np.abs(h["wg"]) + np.abs(du) @ np.abs(h["wu"])))]
+    else:
+        ax = np.abs(h["x"])
+        cases = [(got[1], dg.T @ h["x"], eg.T @ ax + M * E * (np.abs(dg).T @ ax)),
+                 (got[2], du.T @ h["x"], eu.T @ ax + M * E * (np.abs(du).T @ ax))]
+    for t, ref, tol in cases:
+        within(t[it], ref, tol + U[dtype] * (np.abs(ref) + tol), op)
+        assert rel_l2(to_host(t[it]), ref) < (2.0 ** -7 if dtype == BF16 else 2.0 ** -17)
+
+
+def test_rows_far_apart():
+    """Offsets past 32 bits: rows just below 8 MiB apart in tensors of more than 2 GiB."""
+    M, F, K, wide = 300, 264, 72, 2 ** 22 - 8
+    d, _ = gated_case(M, F, K, BF16, False, 150)
+    dout, _ = rnd(151, (M, F), 1.0, BF16)
+    out, pre = t2i.gated_linear(*d.values(), save_pre=True)
+    want = t2i.gated_linear_backward(dout, d["x"], d["wg"], d["wu"], pre)
+    x = torch.empty((M, wide), dtype=BF16, device=DEV)[:, :K]
+    w = torch.empty((2 * F, wide), dtype=BF16, device=DEV)[:, :K]
+    x.copy_(d["x"])
+    w[:F], w[F:] = d["wg"], d["wu"]
+    got = t2i.gated_linear(x, w[:F], w[F:], save_pre=True)
+    assert torch.equal(got[0], out) and torch.equal(got[1], pre)
+    for a, b in zip(t2i.gated_linear_backward(dout, x, w[:F], w[F:], pre)[:3], want):
+        assert torch.equal(a, b)
+    q, s = t2i.quant_rows(x)
+    q0, s0 = t2i.quant_rows(d["x"])
+    assert torch.equal(q, q0) and torch.equal(s, s0)
+    del x, w, got
+    big = torch.zeros((M, 2 ** 23 - 16), dtype=torch.int8, device=DEV)
+    big[:, :128] = q
+    wq, ws = t2i.quant_rows(d["wg"])
+    assert torch.equal(t2i.linear_i8(big, s, wq, ws, K=K), t2i.linear_i8(q, s, wq, ws, K=K))
+    del big
+    heads = torch.empty((M, wide), dtype=BF16, device=DEV)[:, :K].unflatten(1, (1, 72))
+    heads.copy_(d["x"].unflatten(1, (1, 72)))
+    near = d["x"].unflatten(1, (1, 72))
+    assert torch.equal(t2i.qk_norm_rope(heads, near)[0], t2i.qk_norm_rope(near, near)[0])
+    for a, b in zip(t2i.qk_norm_rope_backward(heads, near, heads, near), t2i.qk_norm_rope_backward(near, near, near, near)):
+        assert a is b or torch.equal(a, b)
+
+
 # ------------------------------------------------------------------ query / key norm with rotation
 
 def qk_case(rows, hq, hk, d, dtype, pairing, seed=1, fused=True):
