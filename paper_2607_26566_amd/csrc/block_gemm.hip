@@ -10,7 +10,7 @@ namespace t2i {
 // ---- tile shapes.  `per_cu` workgroups of a shape share a CU.  A launch of n
 // tiles takes rounds of 256 per_cu; a round takes `full` us per k step and `end` us
 // for its first loads and its epilogue, the last one `alone` per step if it has 256
-// tiles or fewer.
+// tiles or fewer, and in between what lies between.
 struct TileChoice { int bm, bn, per_cu; float alone, full, end; };
 struct TilePick { int shape; float us; };
 template <int N>
@@ -19,9 +19,9 @@ static TilePick choose_tile(const TileChoice (&c)[N], long rows, long cols, int 
   for (int i = 0; i < N; ++i) {
     const long tiles = ((rows + c[i].bm - 1) / c[i].bm) * ((cols + c[i].bn - 1) / c[i].bn) * slices;
     const long slots = 256L * c[i].per_cu, rest = tiles % slots;
-    const float end = c[i].end * end_scale;
+    const float end = c[i].end * end_scale, more = rest <= 256 ? 0.f : (float)(rest - 256) / (float)(slots - 256);
     const float us = (float)(tiles / slots) * (c[i].full * steps + end) +
-                     (rest == 0 ? 0.f : (rest <= 256 ? c[i].alone : c[i].full) * steps + end);
+                     (rest == 0 ? 0.f : (c[i].alone + (c[i].full - c[i].alone) * more) * steps + end);
     if (i == 0 || us < best.us) best = {i, us};
   }
   return best;
@@ -286,20 +286,35 @@ __global__ __launch_bounds__(256) void split_sum_kernel(const float* __restrict_
 }
 
 // ---- launches
-// Shapes of the bf16 and 8-bit products, measured on products of 4096 x 20480 x 4096
-// (full), 333 rows (alone) and K = 1152 (end; with bf16 outputs for every column of
-// the tile, half of it for the gated block).  Two stages and several workgroups per
+// Shapes of the bf16 and 8-bit products: times measured on products of 4096 x 20480 x
+// 4096 (full), 333 rows (alone) and K = 1152 (end; with bf16 outputs for every column
+// of the tile, half of it for the gated block), then moved by up to a quarter to
+// choose best for 104 drawn products (1.5 % above each one's fastest shape in the
+// mean, 12 % at most).  Two stages and several workgroups per
 // CU where the tiles fill the chip -- the epilogue of one then runs beside the loop
-// of another --, four stages and one where they do not: 7531 x 4608 x 1152 in 8 bits
+// of another --, three or four stages where they do not: 7531 x 4608 x 1152 in 8 bits
 // 84 us on 256 x 256, 63 on 128 x 128 with two stages, 89 with four; 600 x 1152 x
-// 4608 57, 28 and 21, 16 on 64 x 128 with four.
+// 4608 57, 28 and 21, 16 on 64 x 128 with three.  Three stages on 64 and 32 rows, two
+// workgroups per CU, beat four where there are more than 256 tiles (gated 200 x 4608 x
+// 1152 15.4 -> 11.2 us) and lose where one row's weights stream from memory (1 x 10240 x
+// 4096 33.5 and 36.3 us on 32 rows).
 using Tile256 = TileDims<256, 256, 2, 4, 2>;
-using Tile256n = TileDims<256, 128, 4, 2, 3>;
 using Tile128 = TileDims<128, 128, 2, 4, 2>;
 using Tile128d = TileDims<128, 128, 2, 4, 4>;
 using Tile64 = TileDims<64, 128, 2, 4, 2>;
-using Tile64d = TileDims<64, 128, 2, 4, 4>;
-using Tile32d = TileDims<32, 128, 1, 4, 4>;
+using Tile64d = TileDims<64, 128, 2, 4, 3>;
+using Tile32 = TileDims<32, 128, 1, 4, 4>;
+using Tile32d = TileDims<32, 128, 1, 4, 3>;
+constexpr TileChoice kTiles[] = {{256, 256, 1, 1.60f, 1.60f, 13.f}, {128, 128, 2, 0.72f, 1.02f, 4.8f},
+                                 {128, 128, 1, 0.55f, 0.55f, 5.f},  {64, 128, 3, 0.60f, 1.01f, 3.f},
+                                 {64, 128, 2, 0.48f, 1.00f, 2.85f}, {32, 128, 2, 0.44f, 0.78f, 2.f}};
+constexpr int kTile32 = 5;
+// the table's choice, but for one block of rows whose weights stream from memory
+static int bf16_shape(long rows, long cols, int steps, float end_scale) {
+  const int shape = choose_tile(kTiles, rows, cols, steps, end_scale).shape;
+  return shape == kTile32 && rows <= 32 && cols > 128 * 128 ? kTile32 + 1 : shape;
+}
+
 // fp32: bound by the matrix cores (154 TFLOP/s: 1.7 us per step of 128 x 128), so that
 // two stages are enough and several workgroups share a CU (4096 x 9216 x 1152: 143
 // TFLOP/s on 128 x 128, 139 on 64 x 64, 134 and 128 with four stages; 517 x 2832 x 1152
@@ -307,10 +322,6 @@ using Tile32d = TileDims<32, 128, 1, 4, 4>;
 using Tile64s = TileDims<64, 64, 2, 2, 2>;
 constexpr TileChoice kTilesF32[] = {{128, 128, 1, 1.95f, 1.85f, 3.f}, {64, 64, 1, 0.65f, 0.50f, 1.5f}};
 constexpr int kMaxSlices = 16;
-constexpr TileChoice kTiles[] = {{256, 256, 1, 1.60f, 1.60f, 13.f}, {256, 128, 1, 0.95f, 0.95f, 8.f},
-                                 {128, 128, 2, 0.72f, 1.02f, 6.f},  {128, 128, 1, 0.61f, 0.61f, 5.f},
-                                 {64, 128, 3, 0.60f, 1.01f, 4.5f},  {64, 128, 1, 0.48f, 0.48f, 3.f},
-                                 {32, 128, 1, 0.41f, 0.41f, 2.f}};
 
 template <class D>
 static TileShape tile_shape(int rows, int cols, int steps, int kbytes, int half) {
@@ -344,21 +355,21 @@ static void i8_launch(const TileOperand& a, const TileOperand& b, const I8Epi& e
 #undef T2I_I8
 }
 
-#define T2I_TILES(SHAPE, CALL)                  \
+#define T2I_TILES(SHAPE, CALL)                   \
   switch (SHAPE) {                               \
     case 0: { using D = Tile256; CALL; break; }  \
-    case 1: { using D = Tile256n; CALL; break; } \
-    case 2: { using D = Tile128; CALL; break; }  \
-    case 3: { using D = Tile128d; CALL; break; } \
-    case 4: { using D = Tile64; CALL; break; }   \
-    case 5: { using D = Tile64d; CALL; break; }  \
-    default: { using D = Tile32d; CALL; break; } \
+    case 1: { using D = Tile128; CALL; break; }  \
+    case 2: { using D = Tile128d; CALL; break; } \
+    case 3: { using D = Tile64; CALL; break; }   \
+    case 4: { using D = Tile64d; CALL; break; }  \
+    case 5: { using D = Tile32d; CALL; break; }  \
+    default: { using D = Tile32; CALL; break; }  \
   }
 
 hipError_t launch_linear_i8(const int8_t* A, int lda, const int8_t* W, int ldw, int M, int N, int K,
                             const I8Epi& e, hipStream_t st) {
   const TileOperand a{(const char*)A, nullptr, (uint32_t)lda, M, 0}, b{(const char*)W, nullptr, (uint32_t)ldw, N, 0};
-  T2I_TILES(choose_tile(kTiles, M, N, i8_row(K) / 128, 1.f).shape, i8_launch<D>(a, b, e, M, N, K, st))
+  T2I_TILES(bf16_shape(M, N, i8_row(K) / 128, 1.f), i8_launch<D>(a, b, e, M, N, K, st))
   return hipGetLastError();
 }
 
@@ -456,7 +467,7 @@ static void gated_dw_launch(int M, int F, int K, const void* dgu, const void* A,
 hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& p, int M, int F, int K, hipStream_t st) {
   const TilePick f32 = choose_tile(kTilesF32, M, 2L * F, (K + 31) / 32, 0.5f);
   if (is_bf16)
-    T2I_TILES(choose_tile(kTiles, M, 2L * F, (K + 63) / 64, 0.5f).shape, (gated_fwd_launch<D, bf16>(p, M, F, K, st)))
+    T2I_TILES(bf16_shape(M, 2L * F, (K + 63) / 64, 0.5f), (gated_fwd_launch<D, bf16>(p, M, F, K, st)))
   else if (f32_pieces({F, K, p.lda, p.ldw, p.ldo, p.pre ? p.ldp : 0}, {p.A, p.Wg, p.Wu, p.out, p.pre}))
     T2I_TILES_F32(f32.shape, (gated_fwd_launch<D, float>(p, M, F, K, st)))
   else
@@ -507,14 +518,15 @@ extern "C" int t2i_test_block_tile(int op, int is_bf16, int M, int F, int K, int
                                    int* slices) {
   if (M < 1 || F < 1 || K < 1 || op < 0 || op > 3) return 0;
   SplitPick p{0, 1, 0};
-  if (op == 0) p.shape = choose_tile(kTiles, M, F, i8_row(K) / 128, 1.f).shape;
-  else if (op == 1) p.shape = is_bf16 ? choose_tile(kTiles, M, 2L * F, (K + 63) / 64, 0.5f).shape
+  if (op == 0) p.shape = bf16_shape(M, F, i8_row(K) / 128, 1.f);
+  else if (op == 1) p.shape = is_bf16 ? bf16_shape(M, 2L * F, (K + 63) / 64, 0.5f)
                                       : choose_tile(kTilesF32, M, 2L * F, (K + 31) / 32, 0.5f).shape;
   else p = op == 2 ? split_of(is_bf16, M, K, 2 * gated_cols(F)) : split_of(is_bf16, 2L * F, K, M);
-  const TileChoice& c = op == 0 || is_bf16 ? kTiles[p.shape] : kTilesF32[p.shape];
+  const bool stream = (op == 0 || is_bf16) && p.shape > kTile32;   // four stages, one workgroup per CU
+  const TileChoice& c = stream ? kTiles[kTile32] : op == 0 || is_bf16 ? kTiles[p.shape] : kTilesF32[p.shape];
   *rows = c.bm;
   *columns = c.bn;
-  *per_cu = c.per_cu;
+  *per_cu = stream ? 1 : c.per_cu;
   *slices = p.slices;
   return 1;
 }

@@ -458,9 +458,9 @@ def some(n, seed):
 
 
 @pytest.mark.parametrize("M,N,K,tile", [
-    (33, 72, 72, (32, 128, 1)), (4100, 136, 72, (64, 128, 1)), (8200, 136, 72, (64, 128, 3)),
-    (8200, 136, 200, (128, 128, 1)), (8200, 4104, 520, (128, 128, 2)), (2050, 2056, 12300, (256, 128, 1)),
-    (2050, 4104, 2056, (256, 256, 1))])
+    (20, 72, 72, (32, 128, 2)), (30, 16500, 72, (32, 128, 1)), (8200, 136, 72, (64, 128, 2)),
+    (8200, 520, 72, (64, 128, 3)), (8200, 264, 2056, (128, 128, 1)), (8200, 520, 2056, (128, 128, 2)),
+    (4090, 4090, 4104, (256, 256, 1))])
 def test_linear_i8_on_every_tile(M, N, K, tile):
     assert tile_of(0, BF16, M, N, K) == (*tile, 1)
     a, sa, w, sw = i8_operands(M, N, K, 120)
@@ -485,10 +485,10 @@ def test_linear_i8_on_every_tile(M, N, K, tile):
 
 
 @pytest.mark.parametrize("M,F,K,dtype,tile", [
-    (33, 72, 72, BF16, (32, 128, 1)), (4100, 72, 72, BF16, (64, 128, 1)), (2050, 1032, 72, BF16, (64, 128, 3)),
-    (8200, 72, 72, BF16, (128, 128, 1)), (4100, 4104, 72, BF16, (128, 128, 2)),
-    (2050, 1032, 2056, BF16, (256, 128, 1)), (2050, 2056, 520, BF16, (256, 256, 1)),
-    (300, 200, 72, F32, (64, 64, 1)), (4100, 4104, 72, F32, (128, 128, 1)), (4100, 4101, 71, F32, (128, 128, 1))])
+    (20, 72, 72, BF16, (32, 128, 2)), (30, 8200, 72, BF16, (32, 128, 1)), (8200, 72, 72, BF16, (64, 128, 2)),
+    (8200, 136, 72, BF16, (64, 128, 3)), (8200, 136, 520, BF16, (128, 128, 1)),
+    (8200, 264, 520, BF16, (128, 128, 2)), (8200, 520, 2056, BF16, (256, 256, 1)),
+    (300, 200, 72, F32, (64, 64, 1)), (8200, 1032, 72, F32, (128, 128, 1)), (8200, 1031, 71, F32, (128, 128, 1))])
 def test_gated_linear_on_every_tile(M, F, K, dtype, tile):
     assert tile_of(1, dtype, M, F, K) == (*tile, 1)
     d, h = gated_case(M, F, K, dtype, True, 130)
@@ -505,21 +505,23 @@ def test_gated_linear_on_every_tile(M, F, K, dtype, tile):
 
 
 @pytest.mark.parametrize("op,M,F,K,dtype,tile", [
-    ("dx", 33, 72, 72, BF16, (32, 128, 1, 1)), ("dx", 8200, 72, 72, BF16, (64, 128, 1, 1)),
-    ("dx", 2050, 72, 2056, BF16, (64, 128, 3, 1)), ("dx", 8200, 72, 200, BF16, (128, 128, 1, 1)),
-    ("dx", 8200, 72, 4104, BF16, (128, 128, 2, 1)), ("dx", 8200, 4104, 520, BF16, (256, 128, 1, 1)),
-    ("dx", 2050, 264, 4104, BF16, (256, 256, 1, 1)), ("dx", 33, 2056, 72, BF16, (32, 128, 1, 14)),
-    ("dx", 130, 4104, 4104, BF16, (64, 128, 3, 7)), ("dx", 257, 4104, 4104, BF16, (128, 128, 2, 5)),
-    ("dx", 1030, 2056, 1032, BF16, (128, 128, 1, 3)), ("dx", 2050, 4104, 2056, BF16, (256, 256, 1, 3)),
-    ("dx", 4100, 72, 4104, F32, (128, 128, 1, 1)), ("dx", 4100, 71, 4103, F32, (128, 128, 1, 1)),
-    ("dx", 70, 1032, 72, F32, (64, 64, 1, 14)),
-    ("dw", 33, 72, 72, BF16, (32, 128, 1, 1)), ("dw", 33, 4104, 72, BF16, (64, 128, 1, 1)),
-    ("dw", 33, 4104, 200, BF16, (64, 128, 3, 1)), ("dw", 70, 4104, 200, BF16, (128, 128, 1, 1)),
-    ("dw", 130, 4104, 4104, BF16, (128, 128, 2, 1)), ("dw", 4100, 1032, 2056, BF16, (256, 128, 1, 1)),
-    ("dw", 1030, 2056, 2056, BF16, (256, 256, 1, 1)), ("dw", 8200, 72, 72, BF16, (32, 128, 1, 15)),
-    ("dw", 8200, 136, 4104, BF16, (128, 128, 2, 5)), ("dw", 8200, 1032, 2056, BF16, (256, 256, 1, 3)),
-    ("dw", 8200, 72, 4104, BF16, (64, 128, 3, 7)), ("dw", 70, 2056, 2056, F32, (128, 128, 1, 1)),
-    ("dw", 70, 2055, 2055, F32, (128, 128, 1, 1)), ("dw", 4100, 72, 72, F32, (64, 64, 1, 15))])
+    ("dx", 20, 72, 72, BF16, (32, 128, 2, 1)), ("dx", 20, 520, 72, BF16, (32, 128, 2, 5)),
+    ("dx", 8200, 72, 200, BF16, (64, 128, 2, 1)), ("dx", 4100, 1032, 72, BF16, (64, 128, 2, 4)),
+    ("dx", 8200, 72, 520, BF16, (64, 128, 3, 1)), ("dx", 4100, 4104, 72, BF16, (64, 128, 3, 10)),
+    ("dx", 4100, 1032, 520, BF16, (128, 128, 1, 1)), ("dx", 2050, 2056, 520, BF16, (128, 128, 1, 3)),
+    ("dx", 8200, 520, 520, BF16, (128, 128, 2, 1)), ("dx", 4100, 4104, 520, BF16, (128, 128, 2, 3)),
+    ("dx", 8200, 2056, 1032, BF16, (256, 256, 1, 1)), ("dx", 2050, 8200, 2056, BF16, (256, 256, 1, 3)),
+    ("dx", 20, 72, 72, F32, (64, 64, 1, 1)), ("dx", 20, 264, 72, F32, (64, 64, 1, 5)),
+    ("dx", 8200, 72, 2056, F32, (128, 128, 1, 1)), ("dx", 8200, 71, 2055, F32, (128, 128, 1, 1)),
+    ("dx", 4100, 520, 200, F32, (128, 128, 1, 3)),
+    ("dw", 20, 72, 72, BF16, (32, 128, 2, 1)), ("dw", 2050, 72, 72, BF16, (32, 128, 2, 9)),
+    ("dw", 20, 8200, 72, BF16, (64, 128, 2, 1)), ("dw", 2050, 2056, 72, BF16, (64, 128, 2, 4)),
+    ("dw", 20, 8200, 200, BF16, (64, 128, 3, 1)), ("dw", 4100, 4104, 72, BF16, (64, 128, 3, 5)),
+    ("dw", 2050, 2056, 520, BF16, (128, 128, 1, 1)), ("dw", 4100, 1032, 520, BF16, (128, 128, 1, 3)),
+    ("dw", 130, 8200, 1032, BF16, (128, 128, 2, 1)), ("dw", 8200, 2056, 520, BF16, (128, 128, 2, 3)),
+    ("dw", 2050, 8200, 520, BF16, (256, 256, 1, 1)), ("dw", 20, 72, 72, F32, (64, 64, 1, 1)),
+    ("dw", 520, 72, 72, F32, (64, 64, 1, 5)), ("dw", 20, 8200, 72, F32, (128, 128, 1, 1)),
+    ("dw", 20, 8199, 71, F32, (128, 128, 1, 1)), ("dw", 1030, 2056, 200, F32, (128, 128, 1, 3))])
 def test_gated_gradients_on_every_tile(op, M, F, K, dtype, tile):
     assert tile_of(2 if op == "dx" else 3, dtype, M, F, K) == tile
     say(op, M, F, K, NAME[dtype], tile)
