@@ -173,7 +173,8 @@ t2i_status t2i_op_lora_merge_batch(int32_t dtype, int32_t n, int32_t n_out, int3
  *   its type (16-byte aligned rows are read in whole pieces: same results,
  *   less time); q [rows, ldq] with ldq % 16 == 0, ldq >= K rounded up to a
  *   multiple of 128, 16-byte aligned: columns K .. that multiple are written
- *   as zeros, columns behind it are left alone; scale [rows] fp32.
+ *   as zeros, columns behind it are left alone; scale [rows] fp32.  Fewer than
+ *   2^26 - 4 rows (K > 2048: 2^24 - 4).
  */
 t2i_status t2i_op_quant_rows(int32_t dtype, int32_t rows, int32_t K, const void* x, int32_t ldx,
                              int8_t* q, int32_t ldq, float* scale, void* stream);
@@ -185,10 +186,11 @@ t2i_status t2i_op_quant_rows(int32_t dtype, int32_t rows, int32_t K, const void*
  * The sum is exact (32-bit integers, K <= 131071); it is rounded once to fp32,
  * the rest is fp32.
  *   A [M, K], W [N, K] int8, 16-byte aligned, row strides lda, ldw multiples of
- *   16, at least K rounded up to a multiple of 128 and at most 8 MiB: both are
- *   read up to that multiple, and one of the two must hold zeros behind K (t2i_op_quant_rows
- *   writes them).  dtype is the type of bias [N] (or NULL: none) and out; the
- *   remaining arguments are those of t2i_op_linear.
+ *   16, at least K rounded up to a multiple of 128 and below 8 MiB: both are read
+ *   up to that multiple, and one of the two must hold zeros behind K
+ *   (t2i_op_quant_rows writes them).  dtype is the type of bias [N] (or NULL: none)
+ *   and out; the remaining arguments are those of t2i_op_linear.  Fewer than 2^23
+ *   pieces of 64 x 64 outputs.
  */
 t2i_status t2i_op_linear_i8(int32_t dtype, int32_t epilogue, int32_t M, int32_t N, int32_t K,
                             const int8_t* A, int32_t lda, const float* a_scale, const int8_t* W,
@@ -210,7 +212,8 @@ t2i_status t2i_op_linear_i8(int32_t dtype, int32_t epilogue, int32_t M, int32_t 
  *   bf16 they would add a quarter to the gradients' error).
  *   bf16: F, K and the strides % 8 == 0 (ldp % 4), every pointer 16-byte
  *   aligned.  fp32: any sizes (F, K, strides % 4 == 0 and 16-byte aligned
- *   pointers are faster).  Rows of A, Wg and Wu at most 8 MiB apart.
+ *   pointers are faster).  Rows of A, Wg and Wu less than 8 MiB apart, fewer than
+ *   2^23 pieces of 64 x 64 values in g | u (backward: dA, dWg | dWu as well).
  * No output may overlap an input.
  */
 t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,
@@ -228,7 +231,7 @@ t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F,
  * bias sums take them unrounded); products and sums are fp32.  dA (stride
  * ldda), dWg, dWu (common stride lddw) may each be NULL: not computed; dbg and
  * dbu both or neither.  Sizes, strides and alignment as in the forward pass
- * (F up to 2^20).
+ * (F below 2^20).
  * ws: device workspace of ws_bytes >= t2i_op_gated_linear_backward_ws_bytes,
  * 256-byte aligned, used by this call until it has finished on the stream;
  * the result does not depend on what it holds.  No output may overlap an
@@ -258,7 +261,8 @@ typedef enum {
  *   (stride ldk; the columns of one fused projection, or buffers of their
  *   own), wq, wk [head_dim] or NULL (ones), outputs q_out, k_out alike, all of
  *   dtype; the arithmetic is fp32, one rounding.  heads_q or heads_k may be 0
- *   (its pointers are then unused); rows * (heads_q + heads_k) < 2^31.
+ *   (its pointers are then unused); rows * (heads_q + heads_k) < 2^31, and head_dim
+ *   times that < 2^34.
  *   table fp32 [n_pos][head_dim / 2][2] of (cos, sin), or NULL: no rotation
  *   (one, two or more position axes: the table's rows say which pair turns by
  *   which angle).  Row r turns by table row pos[r] (device, [rows]), or r when

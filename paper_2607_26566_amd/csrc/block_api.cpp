@@ -10,9 +10,12 @@ namespace {
 
 bool bad_dtype(int32_t d) { return d != T2I_F32 && d != T2I_BF16; }
 bool off(const void* p, size_t n) { return (uintptr_t)p % n != 0; }
-// one workgroup per 16 x 16 outputs at the least: the grid stays below 2^31
-bool too_large(int32_t M, int32_t N) {
-  return ((int64_t)M / 16 + 1) * ((int64_t)N / 16 + 1) > 0x7fffffff || M > (1 << 30) || N > (1 << 30);
+// a launch holds fewer than 2^32 threads: the smallest tiles take 512 for 64 x 128
+// outputs, 256 for 64 x 64 or 32 x 128
+bool too_large(int64_t M, int64_t N) { return ((M + 63) / 64) * ((N + 63) / 64) >= 1 << 23; }
+// (fewer than 2^32 threads, of which a head takes less than a fourth of its elements)
+bool too_many_heads(int64_t rows, int64_t hq, int64_t hk, int64_t d) {
+  return rows * (hq + hk) > 0x7fffffff || rows * (hq + hk) * d >= 1LL << 34;
 }
 // the kernels address up to 256 rows of an operand with 32-bit byte offsets
 bool far_rows(int32_t ld, size_t elem) { return (int64_t)ld * (int64_t)elem * 256 > 0x7fffffff; }
@@ -31,7 +34,7 @@ t2i_status check_qk(int32_t dtype, int32_t rows, int32_t hq, int32_t hk, int32_t
   if (d < 8 || d > 256 || d % 8) return ops_fail(T2I_ERR_SHAPE, "head_dim must be a multiple of 8 in 8 .. 256");
   if (pairing == T2I_ROPE_HALVES && d % 16)
     return ops_fail(T2I_ERR_SHAPE, "halves need head_dim % 16 == 0");
-  if ((int64_t)rows * ((int64_t)hq + hk) > 0x7fffffff) return ops_fail(T2I_ERR_SHAPE, "rows * heads past 2^31");
+  if (too_many_heads(rows, hq, hk, d)) return ops_fail(T2I_ERR_SHAPE, "rows * heads past 2^31, or elements past 2^34");
   if ((hq && (!q || !oq)) || (hk && (!k || !ok))) return ops_fail(T2I_ERR_INVALID_ARG, "NULL pointer");
   if ((hq && (ldq < (int64_t)hq * d || ldoq < (int64_t)hq * d || ldq % 8 || ldoq % 8)) ||
       (hk && (ldk < (int64_t)hk * d || ldok < (int64_t)hk * d || ldk % 8 || ldok % 8)))
@@ -84,7 +87,9 @@ extern "C" {
 t2i_status t2i_op_quant_rows(int32_t dtype, int32_t rows, int32_t K, const void* x, int32_t ldx,
                              int8_t* q, int32_t ldq, float* scale, void* stream) {
   if (bad_dtype(dtype)) return ops_fail(T2I_ERR_INVALID_ARG, "bad dtype");
-  if (rows < 1 || K < 1 || K > (1 << 30)) return ops_fail(T2I_ERR_SHAPE, "bad shape");
+  // (fewer than 2^32 threads: a wave per row up to K = 2048, a workgroup for longer ones)
+  if (rows < 1 || K < 1 || K > (1 << 30) || rows >= (K <= 2048 ? 1 << 26 : 1 << 24) - 4)
+    return ops_fail(T2I_ERR_SHAPE, "bad shape");
   if (!x || !q || !scale) return ops_fail(T2I_ERR_INVALID_ARG, "NULL pointer");
   if (ldx < K) return ops_fail(T2I_ERR_SHAPE, "leading dimension < K");
   if (ldq < i8_row(K) || ldq % 16)
@@ -140,7 +145,7 @@ t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F,
   if (bad_dtype(dtype)) return ops_fail(T2I_ERR_INVALID_ARG, "bad dtype");
   if (act != T2I_EPI_GELU && act != T2I_EPI_SILU)
     return ops_fail(T2I_ERR_INVALID_ARG, "act must be T2I_EPI_GELU or T2I_EPI_SILU");
-  if (M < 1 || F < 1 || K < 1 || K > (1 << 30) || F > (1 << 28) || too_large(M, 2 * F))
+  if (M < 1 || F < 1 || K < 1 || K > (1 << 30) || F > (1 << 28) || too_large(M, 2LL * F))
     return ops_fail(T2I_ERR_SHAPE, "bad shape");
   if (!A || !Wg || !Wu || !out) return ops_fail(T2I_ERR_INVALID_ARG, "NULL operand");
   if (!bg != !bu) return ops_fail(T2I_ERR_INVALID_ARG, "bg and bu go together");
@@ -171,8 +176,8 @@ t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F,
 }
 
 size_t t2i_op_gated_linear_backward_ws_bytes(int32_t dtype, int32_t M, int32_t F, int32_t K) {
-  if (bad_dtype(dtype) || M < 1 || F < 1 || K < 1 || K > (1 << 30) || F > (1 << 28) || too_large(M, 2 * F) ||
-      too_large(M, K) || too_large(F, K))
+  if (bad_dtype(dtype) || M < 1 || F < 1 || K < 1 || K > (1 << 30) || F > (1 << 28) || too_large(M, 2LL * F) ||
+      too_large(M, K) || too_large(2LL * F, K))
     return 0;
   // dg | du, the bias gradients' column sums, the products' partial sums
   const size_t partial = ((size_t)gate_row_blocks(M, F) * 2 * gated_cols(F) * 4 + 255) / 256 * 256;
@@ -188,8 +193,8 @@ t2i_status t2i_op_gated_linear_backward(int32_t dtype, int32_t act, int32_t M, i
   if (bad_dtype(dtype)) return ops_fail(T2I_ERR_INVALID_ARG, "bad dtype");
   if (act != T2I_EPI_GELU && act != T2I_EPI_SILU)
     return ops_fail(T2I_ERR_INVALID_ARG, "act must be T2I_EPI_GELU or T2I_EPI_SILU");
-  if (M < 1 || F < 1 || K < 1 || K > (1 << 30) || F > (1 << 28) || too_large(M, 2 * F) || too_large(M, K) ||
-      too_large(F, K))
+  if (M < 1 || F < 1 || K < 1 || K > (1 << 30) || F > (1 << 28) || too_large(M, 2LL * F) || too_large(M, K) ||
+      too_large(2LL * F, K))
     return ops_fail(T2I_ERR_SHAPE, "bad shape");
   if (!A || !Wg || !Wu || !pre || !dout || !ws) return ops_fail(T2I_ERR_INVALID_ARG, "NULL operand");
   if (!dbg != !dbu) return ops_fail(T2I_ERR_INVALID_ARG, "dbg and dbu go together");
@@ -236,7 +241,7 @@ t2i_status t2i_op_qk_norm_rope(int32_t dtype, int32_t rows, int32_t heads_q, int
 size_t t2i_op_qk_norm_rope_backward_ws_bytes(int32_t rows, int32_t heads_q, int32_t heads_k,
                                              int32_t head_dim) {
   if (rows < 1 || heads_q < 0 || heads_k < 0 || (int64_t)heads_q + heads_k < 1 || head_dim < 8 ||
-      head_dim > 256 || head_dim % 8 || (int64_t)rows * ((int64_t)heads_q + heads_k) > 0x7fffffff)
+      head_dim > 256 || head_dim % 8 || too_many_heads(rows, heads_q, heads_k, head_dim))
     return 0;
   return (size_t)qk_bwd_blocks(rows, heads_q + heads_k, head_dim) * 2 * head_dim * 4;
 }

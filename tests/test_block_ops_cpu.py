@@ -216,6 +216,23 @@ def test_qk_norm_rope_backward_refuses():
     assert ws(0, 1, 1, 16) == 0 and ws(3, 0, 0, 16) == 0 and ws(3, 1, 1, 12) == 0 and ws(3, 1, 1, 264) == 0
 
 
+def test_launches_of_too_many_threads_are_refused():
+    """A launch holds fewer than 2^32 threads: sizes past that are refused here, not
+    by the launch (for the gradients: before the first of their kernels)."""
+    need = t2i.load().t2i_op_gated_linear_backward_ws_bytes
+    check_refusals("t2i_op_quant_rows", QUANT, [
+        (dict(rows=2 ** 26 - 4), SHAPE), (dict(rows=2 ** 24 - 4, K=2056, ldx=2056, ldq=2176), SHAPE)])
+    check_refusals("t2i_op_linear_i8", I8, [
+        (dict(M=2 ** 29, N=1), SHAPE), (dict(M=2 ** 18, N=2 ** 17, ldo=2 ** 17), SHAPE)])
+    check_refusals("t2i_op_gated_linear", GATED, [
+        (dict(M=2 ** 29, F=8, ldo=8, ldp=16), SHAPE), (dict(M=2 ** 18, F=2 ** 16, ldo=2 ** 16, ldp=2 ** 17), SHAPE)])
+    big = dict(M=2 ** 21, F=2 ** 13, ldp=2 ** 14, ldd=2 ** 13)
+    check_refusals("t2i_op_gated_linear_backward", GBWD, [(big, SHAPE)])
+    assert need(BF16, big["M"], big["F"], 16) == 0 and need(BF16, big["M"] // 2, big["F"], 16) > 0
+    wide = dict(rows=2 ** 26, heads_q=1, heads_k=0, head_dim=256, ldq=256, ldqo=256, pos=P)
+    check_refusals("t2i_op_qk_norm_rope", QK, [(wide, SHAPE)])
+
+
 # ------------------------------------------------------------------ refusals of the Python calls
 
 def test_python_calls_refuse_host_tensors():
