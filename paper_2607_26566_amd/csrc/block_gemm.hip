@@ -71,6 +71,11 @@ __device__ __forceinline__ float i8_value(int acc, float sa, float sw, float b, 
   return kind == EPI_GELU ? gelu_tanh(y) : kind == EPI_SILU ? silu(y) : y;
 }
 
+// The 8-bit linear layer: y = (sum of whole products) sa sw + b.  The sum is exact in
+// 32 bits whatever the tile, so a row's result does not depend on the rows beside it.
+// 7531 x 4608 x 1152 with GELU 63 us (1.27 POP/s): nine k steps per tile, of which the
+// waits and the epilogue (75 MB of stores, an exponential and a reciprocal per
+// output) take more than the products; 4096 x 4096 x 12288 168 us (2.45 POP/s).
 template <class D, typename T, bool RES>
 __global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a, TileOperand b, TileShape s,
                                                                   I8Epi e, int M, int N, int vec) {
@@ -133,6 +138,11 @@ __global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a,
 template <typename T>
 constexpr TileElem elem_of() { return sizeof(T) == 4 ? ELEM_F32 : ELEM_BF16; }
 
+// Both projections of the gated block on one tile of gate and up columns; a wave holds
+// the same columns of both, so activation and product happen in registers and g and u
+// go to memory only where the backward pass wants them.  8192 x 4608 x 1152 155 - 170
+// us (1.0 - 1.1 PFLOP/s: 4.5 rounds of tiles in 5, 18 k steps each), 4096 x 10240 x 4096
+// 515 - 530 us, one row of 10240 x 4096 33 us (the weights at 5.1 TB/s, a copy's rate).
 template <class D, typename T, bool P4>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand a, TileOperand b, TileShape s,
                                                                      GatedFwd p, int M, int F) {
@@ -183,10 +193,9 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
 }
 
 // The gradients' products.  b is a KR operand: a pair of fragments holds 8
-// neighbouring columns of a row, of which all or the first four exist (N % 4 == 0)
-// except with 4-byte loads.
-// Stored in the operands' type (row stride ldc), or as fp32 partial sums (row stride
-// N) where the contraction is split.
+// neighbouring columns of a row, of which all or the first four exist (N % 4 == 0,
+// except with 4-byte loads).  Stored in the operands' type (row stride ldc), or as
+// fp32 partial sums (row stride N) where the contraction is split.
 template <class D, class P, bool P4, typename T>
 __device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D::TN], T* C, int ldc, int m0,
                                            int n0, int M, int N) {
@@ -290,14 +299,14 @@ __global__ __launch_bounds__(256) void split_sum_kernel(const float* __restrict_
 // 4096 (full), 333 rows (alone) and K = 1152 (end; with bf16 outputs for every column
 // of the tile, half of it for the gated block), then moved by up to a quarter to
 // choose best for 104 drawn products (1.5 % above each one's fastest shape in the
-// mean, 12 % at most).  Two stages and several workgroups per
-// CU where the tiles fill the chip -- the epilogue of one then runs beside the loop
-// of another --, three or four stages where they do not: 7531 x 4608 x 1152 in 8 bits
-// 84 us on 256 x 256, 63 on 128 x 128 with two stages, 89 with four; 600 x 1152 x
-// 4608 57, 28 and 21, 16 on 64 x 128 with three.  Three stages on 64 and 32 rows, two
-// workgroups per CU, beat four where there are more than 256 tiles (gated 200 x 4608 x
-// 1152 15.4 -> 11.2 us) and lose where one row's weights stream from memory (1 x 10240 x
-// 4096 33.5 and 36.3 us on 32 rows).
+// mean, 12 % at most).  Two stages and several workgroups per CU where the tiles fill
+// the chip -- the epilogue of one then runs beside the loop of another --, three or
+// four stages where they do not: 7531 x 4608 x 1152 in 8 bits 84 us on 256 x 256, 63 on
+// 128 x 128 with two stages, 89 with four; 600 x 1152 x 4608 57, 28 and 21, 16 on 64 x
+// 128 with three.  Three stages on 64 and 32 rows, two workgroups per CU, beat four
+// where there are more than 256 tiles (gated 200 x 4608 x 1152 15.4 -> 11.2 us) and
+// lose where the weights of few rows stream from memory (1 x 10240 x 4096 33.5 and 36.3
+// us on 32 rows): Tile32 takes over there.
 using Tile256 = TileDims<256, 256, 2, 4, 2>;
 using Tile128 = TileDims<128, 128, 2, 4, 2>;
 using Tile128d = TileDims<128, 128, 2, 4, 4>;
@@ -309,8 +318,9 @@ constexpr TileChoice kTiles[] = {{256, 256, 1, 1.60f, 1.60f, 13.f}, {128, 128, 2
                                  {128, 128, 1, 0.55f, 0.55f, 5.f},  {64, 128, 3, 0.60f, 1.01f, 3.f},
                                  {64, 128, 2, 0.48f, 1.00f, 2.85f}, {32, 128, 2, 0.44f, 0.78f, 2.f}};
 constexpr int kTile32 = 5;
-// the table's choice, but for one block of rows whose weights stream from memory
-static int bf16_shape(long rows, long cols, int steps, float end_scale) {
+// the bf16 and 8-bit products' entry of T2I_TILES: the table's choice, but for one
+// block of rows whose weights stream from memory
+static int tile_index(long rows, long cols, int steps, float end_scale) {
   const int shape = choose_tile(kTiles, rows, cols, steps, end_scale).shape;
   return shape == kTile32 && rows <= 32 && cols > 128 * 128 ? kTile32 + 1 : shape;
 }
@@ -323,6 +333,7 @@ using Tile64s = TileDims<64, 64, 2, 2, 2>;
 constexpr TileChoice kTilesF32[] = {{128, 128, 1, 1.95f, 1.85f, 3.f}, {64, 64, 1, 0.65f, 0.50f, 1.5f}};
 constexpr int kMaxSlices = 16;
 
+// group_m 8: eight row blocks share a column block's operand in an XCD's L2
 template <class D>
 static TileShape tile_shape(int rows, int cols, int steps, int kbytes, int half) {
   TileShape s;
@@ -369,7 +380,7 @@ static void i8_launch(const TileOperand& a, const TileOperand& b, const I8Epi& e
 hipError_t launch_linear_i8(const int8_t* A, int lda, const int8_t* W, int ldw, int M, int N, int K,
                             const I8Epi& e, hipStream_t st) {
   const TileOperand a{(const char*)A, nullptr, (uint32_t)lda, M, 0}, b{(const char*)W, nullptr, (uint32_t)ldw, N, 0};
-  T2I_TILES(bf16_shape(M, N, i8_row(K) / 128, 1.f), i8_launch<D>(a, b, e, M, N, K, st))
+  T2I_TILES(tile_index(M, N, i8_row(K) / 128, 1.f), i8_launch<D>(a, b, e, M, N, K, st))
   return hipGetLastError();
 }
 
@@ -467,7 +478,7 @@ static void gated_dw_launch(int M, int F, int K, const void* dgu, const void* A,
 hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& p, int M, int F, int K, hipStream_t st) {
   const TilePick f32 = choose_tile(kTilesF32, M, 2L * F, (K + 31) / 32, 0.5f);
   if (is_bf16)
-    T2I_TILES(bf16_shape(M, 2L * F, (K + 63) / 64, 0.5f), (gated_fwd_launch<D, bf16>(p, M, F, K, st)))
+    T2I_TILES(tile_index(M, 2L * F, (K + 63) / 64, 0.5f), (gated_fwd_launch<D, bf16>(p, M, F, K, st)))
   else if (f32_pieces({F, K, p.lda, p.ldw, p.ldo, p.pre ? p.ldp : 0}, {p.A, p.Wg, p.Wu, p.out, p.pre}))
     T2I_TILES_F32(f32.shape, (gated_fwd_launch<D, float>(p, M, F, K, st)))
   else
@@ -518,8 +529,8 @@ extern "C" int t2i_test_block_tile(int op, int is_bf16, int M, int F, int K, int
                                    int* slices) {
   if (M < 1 || F < 1 || K < 1 || op < 0 || op > 3) return 0;
   SplitPick p{0, 1, 0};
-  if (op == 0) p.shape = bf16_shape(M, F, i8_row(K) / 128, 1.f);
-  else if (op == 1) p.shape = is_bf16 ? bf16_shape(M, 2L * F, (K + 63) / 64, 0.5f)
+  if (op == 0) p.shape = tile_index(M, F, i8_row(K) / 128, 1.f);
+  else if (op == 1) p.shape = is_bf16 ? tile_index(M, 2L * F, (K + 63) / 64, 0.5f)
                                       : choose_tile(kTilesF32, M, 2L * F, (K + 31) / 32, 0.5f).shape;
   else p = op == 2 ? split_of(is_bf16, M, K, 2 * gated_cols(F)) : split_of(is_bf16, 2L * F, K, M);
   const bool stream = (op == 0 || is_bf16) && p.shape > kTile32;   // four stages, one workgroup per CU

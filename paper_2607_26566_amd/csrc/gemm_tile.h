@@ -28,16 +28,27 @@
 // Loop over the steps (a step is two half-steps of one MFMA depth): the MFMAs of
 // half-step h run while the fragments of h + 1 are read -- the a fragments into
 // the other register set, each b fragment in place once its column is done --
-// and the workgroup meets once per step, a third of the way into half-step 1,
+// and the workgroup meets once per step, after the first of half-step 1's columns,
 // when every fragment of the stage is in registers; then the stage is refilled
-// and the next stage's fragments are read under the remaining columns.
+// and the next stage's fragments are read under the remaining columns.  (Meeting
+// before the first column or halfway, and raising the waves' priority around the
+// MFMAs, measured within 2 % of it.)
+//
+// Measured, operands of 4096 x 10240 x 4096 and so much work that the clock falls
+// to 1.7 GHz: both projections of the gated block 515 - 530 us (1.30 - 1.33 PFLOP/s,
+// MFMA busy in 68 % of the cycles; a library product of 8192^3 reaches 1.37), dx 510 -
+// 580 (1.18 - 1.35; the library with k across b's rows 1.21), dW 585 - 640 (1.07 -
+// 1.18; k across both 1.08); 8 bits at 4096 x 4096 x 12288 168 - 179 us (2.3 - 2.45
+// POP/s; 2.11); fp32 at 4096 x 9216 x 1152 608 us (143 TFLOP/s; 154).  At K = 1152 the
+// first loads and the epilogue take a fifth to a half of a tile's time, see kTiles.
 //
 // fp32 operands that do not lie in whole, aligned 16-byte pieces are loaded 4 bytes
 // per lane instead (P4), four times the load instructions into the same layout.
 //
-// Sizes: rows behind the operand are read as its last row (KC) or as zeros (KR,
-// by the buffer resource's bound), k behind the end as zeros (by an offset
-// behind the resource); what they add up to is not stored.
+// Sizes: tile rows behind the operand's last are read as that row (KC), columns as
+// its last ones (KR): what comes of them is not stored.  k behind the end is read as
+// zeros (KC: by an offset behind the resource, KR: by the resource's bound) and
+// adds nothing.
 #pragma once
 
 #include <type_traits>
@@ -126,10 +137,10 @@ struct TileDims {
 
 enum TileElem { ELEM_BF16, ELEM_I8, ELEM_F32 };
 
-// E: element type.  AKR, BKR: operand layouts.  DUAL: b is two
-// matrices side by side, p for the first half of the tile's columns and p2 for the
-// second, so that a wave holds both of an output.  SEGS (BKR): the contraction
-// runs over p's rows, then p2's.  P4: loads of 4 bytes (fp32).
+// E: element type.  AKR, BKR: operand layouts.  DUAL: b is two matrices side by side,
+// p for the first half of the tile's columns and p2 for the second, so that a wave
+// holds both of an output.  SEGS (BKR): the contraction runs over p's rows, then p2's.
+// P4: loads of 4 bytes (fp32).
 template <class D, TileElem E, bool AKR, bool BKR, bool DUAL, bool SEGS, bool P4 = false>
 struct TileProduct {
   static_assert(!P4 || E == ELEM_F32, "4-byte loads");
@@ -249,7 +260,8 @@ struct TileProduct {
       constexpr int LK = 16 / EB, DW = N * EB / 4;   // k of a lane, dwords of its read
       typedef int raw_t __attribute__((ext_vector_type(DW > 1 ? DW : 2)));
       const int o = (c0 + N * fr) * EB;
-      const char* at = smem + base + (kk * (KROWS / 2) + g * LK) * W * EB + (((o >> 6) ^ (kr_swap<N>(g) & MASK)) << 6) + (o & 63);
+      const char* at = smem + base + (kk * (KROWS / 2) + g * LK) * W * EB +
+                       (((o >> 6) ^ (kr_swap<N>(g) & MASK)) << 6) + (o & 63);
       int raw[LK][DW];
 #pragma unroll
       for (int k = 0; k < LK; ++k) {
@@ -321,7 +333,7 @@ struct TileProduct {
 
     // ---- loop
     constexpr int S = TN / 3;                                   // columns before the barrier
-    constexpr int LPC = (LOADS + TN - S - 1) / (TN - S);     // loads per column after it
+    constexpr int LPC = (LOADS + TN - S - 1) / (TN - S);        // loads per column after it
 #pragma unroll
     for (int t = 0; t < ST; ++t)
       if (t < KT) {

@@ -5,8 +5,10 @@ Argument marshalling only, as in the package's other calls.  Tensors are device
 tensors of one device whose last dimension is contiguous (rows may be strided);
 results are new tensors of that device.  The work runs on ``stream``, by default
 the device's current stream, and results and workspaces are allocated for that
-stream: a caller that uses another stream on either side orders the two itself.
-Wrong arguments raise :class:`T2IError` before anything is launched.
+stream: a caller that uses another stream on either side orders the two itself and
+keeps the operands until the work is done.  Nothing here is recorded for automatic
+differentiation; the ``_backward`` calls are the gradients.  Wrong arguments raise
+:class:`T2IError` before anything is launched.
 """
 from __future__ import annotations
 
