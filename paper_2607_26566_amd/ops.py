@@ -44,21 +44,27 @@ def _of(table: dict, key, what: str):
     return v
 
 
-def _device(first: torch.Tensor, *others) -> torch.device:
-    """The one device of all given tensors (None entries left out)."""
-    dev = first.device
-    if dev.type != "cuda":
+def _device(first: torch.Tensor, *others) -> int:
+    """Index of the one device of all given tensors (None entries left out)."""
+    dev = first.get_device()
+    if dev < 0:
         raise T2IError(1, "operands must be device tensors")
     for t in others:
-        if t is not None and t.device != dev:
+        if t is not None and t.get_device() != dev:
             raise T2IError(1, "operands must be device tensors of one device")
     return dev
 
 
+# A call's own work is a few microseconds, so the common case -- contiguous operands on
+# the current device, no stream given -- goes without strides, stream objects and
+# contexts.
+
 def _rows(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> int:
     """Row stride of a matrix of this shape and type (its columns contiguous)."""
-    if t.dtype != dtype or t.shape != (rows, cols):
+    if t.dtype is not dtype or t.shape != (rows, cols):
         raise T2IError(2, f"{what}: expected ({rows}, {cols}) {dtype}, got {tuple(t.shape)} {t.dtype}")
+    if t.is_contiguous():
+        return cols
     ld, step = t.stride()
     if cols != 1 and step != 1:
         raise T2IError(2, f"{what}: columns must be contiguous")
@@ -70,7 +76,7 @@ def _rows(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> int:
 
 
 def _vec(t: Optional[torch.Tensor], n: int, dtype, what: str):
-    if t is not None and (t.dtype != dtype or t.shape != (n,) or (n > 1 and t.stride(0) != 1)):
+    if t is not None and (t.dtype is not dtype or t.shape != (n,) or not t.is_contiguous()):
         raise T2IError(2, f"{what}: expected ({n},) {dtype}, contiguous")
 
 
@@ -78,26 +84,22 @@ def _p(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
-# A call's own work is a few microseconds, so the common case -- no stream given,
-# operands on the current device -- goes without stream objects and contexts.
-
-def _elsewhere(dev: torch.device, stream) -> bool:
-    return stream is not None or dev.index != torch.cuda.current_device()
+def _elsewhere(dev: int, stream) -> bool:
+    return stream is not None or dev != torch._C._cuda_getDevice()
 
 
 @contextlib.contextmanager
-def _switch(dev: torch.device, stream):
+def _switch(dev: int, stream):
     """The operands' device and the stream asked for (or that device's own) made current."""
     if stream is None:
         stream = torch.cuda.current_stream(dev)
-    elif stream.device != dev:
+    elif stream.device.index != dev:
         raise T2IError(1, "stream belongs to another device than the operands")
     with torch.cuda.device(dev), torch.cuda.stream(stream):
         yield
 
 
-def _stream(dev: torch.device) -> int:
-    return torch._C._cuda_getCurrentRawStream(dev.index)
+_stream = torch._C._cuda_getCurrentRawStream
 
 
 def quant_rows(x: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
@@ -226,14 +228,17 @@ def gated_linear_backward(dout: torch.Tensor, x: torch.Tensor, wg: torch.Tensor,
 def _heads(t: torch.Tensor, rows: int, d: int, dtype, what: str):
     """(heads, row stride) of a [rows, heads, d] tensor whose heads lie side by side."""
     shape = t.shape
-    if t.dtype != dtype or len(shape) != 3 or shape[0] != rows or shape[2] != d:
+    if t.dtype is not dtype or len(shape) != 3 or shape[0] != rows or shape[2] != d:
         raise T2IError(2, f"{what}: expected ({rows}, heads, {d}) {dtype}, got {tuple(shape)} {t.dtype}")
     h = shape[1]
-    ld, head, step = t.stride()
-    if step != 1 or (h > 1 and head != d):
-        raise T2IError(2, f"{what}: heads must be side by side")
-    if rows == 1:
+    if t.is_contiguous():
         ld = h * d
+    else:
+        ld, head, step = t.stride()
+        if step != 1 or (h > 1 and head != d):
+            raise T2IError(2, f"{what}: heads must be side by side")
+        if rows == 1:
+            ld = h * d
     if not h * d <= ld < 2 ** 31:
         raise T2IError(2, f"{what}: rows must not overlap")
     return h, ld
