@@ -226,11 +226,11 @@ __device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D
 }
 
 // A contraction split over gridDim.y slices of `per` steps: slice y writes fp32
-// partial sums [rows][cols] behind those of the slices before it, which
+// partial sums [rows][ld] behind those of the slices before it, which
 // split_sum_kernel adds up in order.
 struct Split {
   float* partial;   // NULL: not split
-  int per;
+  int per, ld;      // ld: the output's columns in whole 16-byte pieces
 };
 __device__ __forceinline__ void take_slice(const Split& sp, TileShape& s) {
   s.first = (int)blockIdx.y * sp.per;
@@ -248,7 +248,7 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, 
   typename P::Acc acc[D::TM][D::TN];
   P::run(smem, a, b, s, tm * D::BM, tn * D::BN, acc);
   if (sp.partial)
-    store_tile<D, P, P4>(acc, sp.partial + (size_t)blockIdx.y * M * K, K, tm * D::BM, tn * D::BN, M, K);
+    store_tile<D, P, false>(acc, sp.partial + (size_t)blockIdx.y * M * sp.ld, sp.ld, tm * D::BM, tn * D::BN, M, sp.ld);
   else
     store_tile<D, P, P4>(acc, dx, ldx, tm * D::BM, tn * D::BN, M, K);
 }
@@ -271,27 +271,27 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, 
   P::run(smem, a, b, s, m0, tn * D::BN, acc);
   if (sp.partial) {
     const size_t of = (size_t)blockIdx.y * (s.tiles_m / half) * F + (second ? F : 0);
-    store_tile<D, P, P4>(acc, sp.partial + of * K, K, m0, tn * D::BN, F, K);
+    store_tile<D, P, false>(acc, sp.partial + of * sp.ld, sp.ld, m0, tn * D::BN, F, sp.ld);
   } else {
     store_tile<D, P, P4>(acc, second ? d1 : d0, ldw, m0, tn * D::BN, F, K);
   }
 }
 
 // out (rows [0, half) to o0, the others to o1) = the sum of the slices' partials
-// [rows][cols], in ascending slice order; cols % 4 == 0, one thread per 4 columns
+// [rows][ldp], in ascending slice order; one thread per 4 columns
 template <typename T>
 __global__ __launch_bounds__(256) void split_sum_kernel(const float* __restrict__ partial, int slices, long rows,
-                                                        long half, int cols, T* o0, T* o1, int ld) {
-  const long x = blockIdx.x * 256L + threadIdx.x, n4 = cols / 4;
+                                                        long half, int cols, int ldp, T* o0, T* o1, int ld, int vec) {
+  const long x = blockIdx.x * 256L + threadIdx.x, n4 = ldp / 4;
   if (x >= rows * n4) return;
   const long r = x / n4;
   const int c = (int)(x - r * n4) * 4;
-  const float* p = partial + r * cols + c;
+  const float* p = partial + r * ldp + c;
   f32x4 a = *(const f32x4*)p;
 #pragma unroll 4
-  for (int i = 1; i < slices; ++i) a += *(const f32x4*)(p + i * rows * cols);
+  for (int i = 1; i < slices; ++i) a += *(const f32x4*)(p + i * rows * ldp);
   const float v[4] = {a[0], a[1], a[2], a[3]};
-  store4((r < half ? o0 + r * ld : o1 + (r - half) * ld) + c, 4, true, v);
+  store4((r < half ? o0 + r * ld : o1 + (r - half) * ld) + c, cols - c, vec, v);
 }
 
 // ---- launches
@@ -328,9 +328,10 @@ static int tile_index(long rows, long cols, int steps, float end_scale) {
 // fp32: bound by the matrix cores (154 TFLOP/s: 1.7 us per step of 128 x 128), so that
 // two stages are enough and several workgroups share a CU (4096 x 9216 x 1152: 143
 // TFLOP/s on 128 x 128, 139 on 64 x 64, 134 and 128 with four stages; 517 x 2832 x 1152
-// 71 and 39 us)
+// 71 and 39 us).  Costs from 36 to 9216 tiles of 36 steps: 22.7 us for up to 256 of 64 x
+// 64, 17.1 for every 256 more; 70.5 and 67 on 128 x 128.
 using Tile64s = TileDims<64, 64, 2, 2, 2>;
-constexpr TileChoice kTilesF32[] = {{128, 128, 1, 1.95f, 1.85f, 3.f}, {64, 64, 1, 0.65f, 0.50f, 1.5f}};
+constexpr TileChoice kTilesF32[] = {{128, 128, 1, 1.88f, 1.79f, 3.f}, {64, 64, 1, 0.605f, 0.455f, 0.9f}};
 constexpr int kMaxSlices = 16;
 
 // group_m 8: eight row blocks share a column block's operand in an XCD's L2
@@ -427,6 +428,7 @@ static SplitPick choose_split(const TileChoice (&tiles)[N], long rows, long cols
   return best;
 }
 
+static long whole4(long cols) { return (cols + 3) / 4 * 4; }
 static SplitPick split_of(bool is_bf16, long rows, long cols, int k) {
   return is_bf16 ? choose_split(kTiles, rows, cols, (k + 63) / 64) : choose_split(kTilesF32, rows, cols, (k + 31) / 32);
 }
@@ -434,16 +436,16 @@ static SplitPick split_of(bool is_bf16, long rows, long cols, int k) {
 size_t gated_split_floats(bool is_bf16, int M, int F, int K) {
   auto floats = [&](long rows, long cols, int k) -> size_t {
     const int n = split_of(is_bf16, rows, cols, k).slices;
-    return n > 1 ? (size_t)n * rows * cols : 0;
+    return n > 1 ? (size_t)n * rows * whole4(cols) : 0;
   };
   return std::max({floats(M, K, 2 * gated_cols(F)), floats(2L * F, K, M), floats(F, K, M)});
 }
 
 template <typename T>
-static void split_sum(const SplitPick& pick, const float* partial, long rows, long half, int cols, T* o0, T* o1,
-                      int ld, hipStream_t st) {
-  hipLaunchKernelGGL((split_sum_kernel<T>), dim3((unsigned)((rows * (cols / 4) + 255) / 256)), dim3(256), 0, st,
-                     partial, pick.slices, rows, half, cols, o0, o1, ld);
+static void split_sum(const Split& sp, int slices, long rows, long half, int cols, T* o0, T* o1, int ld, bool vec,
+                      hipStream_t st) {
+  hipLaunchKernelGGL((split_sum_kernel<T>), dim3((unsigned)((rows * (sp.ld / 4) + 255) / 256)), dim3(256), 0, st,
+                     sp.partial, slices, rows, half, cols, sp.ld, o0, o1, ld, vec);
 }
 
 template <class D, typename T, bool P4 = false>
@@ -456,7 +458,7 @@ static void gated_dx_launch(int M, int F, int K, const void* dgu, const void* Wg
   const TileShape s = tile_shape<D>(M, K, 2 * Fp / per, 2 * e * Fp, Fp / per);
   hipLaunchKernelGGL((gated_dx_kernel<D, T, P4>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
                      st, a, b, s, sp, dx, ldx, M, K);
-  if (sp.partial) split_sum(pick, sp.partial, M, M, K, dx, dx, ldx, st);
+  if (sp.partial) split_sum(sp, pick.slices, M, M, K, dx, dx, ldx, !P4, st);
 }
 
 template <class D, typename T, bool P4 = false>
@@ -472,7 +474,7 @@ static void gated_dw_launch(int M, int F, int K, const void* dgu, const void* A,
   s.tiles_m *= n;
   hipLaunchKernelGGL((gated_dw_kernel<D, T, P4>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
                      st, a, b, s, sp, half, e * Fp, first, dWu, lddw, F, K);
-  if (sp.partial) split_sum(pick, sp.partial, (long)n * F, F, K, first, dWu, lddw, st);
+  if (sp.partial) split_sum(sp, pick.slices, (long)n * F, F, K, first, dWu, lddw, !P4, st);
 }
 
 hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& p, int M, int F, int K, hipStream_t st) {
@@ -489,16 +491,14 @@ hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& p, int M, int F, in
 hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw,
                            void* dx, int ldx, float* partial, hipStream_t st) {
   const SplitPick pick = split_of(is_bf16, M, K, 2 * gated_cols(F));
-  const Split sp{pick.slices > 1 ? partial : nullptr, pick.per};
+  const Split sp{pick.slices > 1 ? partial : nullptr, pick.per, (int)whole4(K)};
   if (is_bf16) {
     T2I_TILES(pick.shape, (gated_dx_launch<D, bf16>(M, F, K, dgu, Wg, Wu, ldw, (bf16*)dx, ldx, pick, sp, st)))
   } else if (f32_pieces({K, ldw, ldx}, {Wg, Wu, dx})) {
     T2I_TILES_F32(pick.shape, (gated_dx_launch<D, float>(M, F, K, dgu, Wg, Wu, ldw, (float*)dx, ldx, pick, sp, st)))
   } else {
-    const int steps = 2 * gated_cols(F) / 32;   // (the slices' sum takes whole pieces: one slice)
-    T2I_TILES_F32(choose_tile(kTilesF32, M, K, steps, 1.f).shape,
-                  (gated_dx_launch<D, float, true>(M, F, K, dgu, Wg, Wu, ldw, (float*)dx, ldx, SplitPick{0, 1, steps},
-                                                   Split{nullptr, steps}, st)))
+    T2I_TILES_F32(pick.shape,
+                  (gated_dx_launch<D, float, true>(M, F, K, dgu, Wg, Wu, ldw, (float*)dx, ldx, pick, sp, st)))
   }
   return hipGetLastError();
 }
@@ -507,7 +507,7 @@ hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, c
                            void* dWu, int lddw, float* partial, hipStream_t st) {
   const long rows = (dWg && dWu ? 2L : 1L) * F;
   const SplitPick pick = split_of(is_bf16, rows, K, M);
-  const Split sp{pick.slices > 1 ? partial : nullptr, pick.per};
+  const Split sp{pick.slices > 1 ? partial : nullptr, pick.per, (int)whole4(K)};
   if (is_bf16) {
     T2I_TILES(pick.shape,
               (gated_dw_launch<D, bf16>(M, F, K, dgu, A, lda, (bf16*)dWg, (bf16*)dWu, lddw, pick, sp, st)))
@@ -515,10 +515,8 @@ hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, c
     T2I_TILES_F32(pick.shape,
                   (gated_dw_launch<D, float>(M, F, K, dgu, A, lda, (float*)dWg, (float*)dWu, lddw, pick, sp, st)))
   } else {
-    const int steps = (M + 31) / 32;
-    T2I_TILES_F32(choose_tile(kTilesF32, rows, K, steps, 1.f).shape,
-                  (gated_dw_launch<D, float, true>(M, F, K, dgu, A, lda, (float*)dWg, (float*)dWu, lddw,
-                                                   SplitPick{0, 1, steps}, Split{nullptr, steps}, st)))
+    T2I_TILES_F32(pick.shape, (gated_dw_launch<D, float, true>(M, F, K, dgu, A, lda, (float*)dWg, (float*)dWu, lddw,
+                                                               pick, sp, st)))
   }
   return hipGetLastError();
 }
