@@ -327,11 +327,18 @@ static int tile_index(long rows, long cols, int steps, float end_scale) {
 
 // fp32: bound by the matrix cores (154 TFLOP/s: 1.7 us per step of 128 x 128), so that
 // two stages are enough and several workgroups share a CU (4096 x 9216 x 1152: 143
-// TFLOP/s on 128 x 128, 139 on 64 x 64, 134 and 128 with four stages; 517 x 2832 x 1152
-// 71 and 39 us).  Costs from 36 to 9216 tiles of 36 steps: 22.7 us for up to 256 of 64 x
-// 64, 17.1 for every 256 more; 70.5 and 67 on 128 x 128.
+// TFLOP/s on 128 x 128, 139 on 64 x 64, 134 and 128 with four stages).  Costs from 36 to
+// 9216 tiles of 36 steps: 22.7 us for up to 256 of 64 x 64, 17.1 for every 256 more;
+// 70.5 and 67 on 128 x 128.  A wave's step is 32 MFMAs of 32 cycles on 64 x 64, 16 on 32
+// x 64, where a chain of steps is what takes the time: 33 x 2304 x 1152 22.3 and 14.9
+// us, 5 x 1634 x 3128 73 and 48 (three stages; two stages of 32 x 32 per wave 4 - 10 us
+// more, four stages 0.5 - 2); 517 x 2832 x 1152 38 and 32; 1024 x 9216 x 1152 160 and 174.
 using Tile64s = TileDims<64, 64, 2, 2, 2>;
-constexpr TileChoice kTilesF32[] = {{128, 128, 1, 1.88f, 1.79f, 3.f}, {64, 64, 1, 0.605f, 0.455f, 0.9f}};
+using Tile32s = TileDims<32, 64, 2, 2, 3>;
+#define T2I_F32_COSTS {128, 128, 1, 1.88f, 1.79f, 3.f}, {64, 64, 1, 0.605f, 0.455f, 0.9f}
+constexpr TileChoice kTilesF32[] = {T2I_F32_COSTS, {32, 64, 1, 0.404f, 0.25f, 0.7f}};
+// dW: a's fragments are turned in twos at least, which 16 rows per wave do not have
+constexpr TileChoice kTilesF32Dw[] = {T2I_F32_COSTS};
 constexpr int kMaxSlices = 16;
 
 // group_m 8: eight row blocks share a column block's operand in an XCD's L2
@@ -385,11 +392,14 @@ hipError_t launch_linear_i8(const int8_t* A, int lda, const int8_t* W, int ldw, 
   return hipGetLastError();
 }
 
-#define T2I_TILES_F32(SHAPE, CALL)              \
-  switch (SHAPE) {                              \
-    case 0: { using D = Tile128; CALL; break; } \
+#define T2I_TILES_F32_DW(SHAPE, CALL)            \
+  switch (SHAPE) {                               \
+    case 0: { using D = Tile128; CALL; break; }  \
     default: { using D = Tile64s; CALL; break; } \
   }
+#define T2I_TILES_F32(SHAPE, CALL)                \
+  if (SHAPE == 2) { using D = Tile32s; CALL; }    \
+  else { T2I_TILES_F32_DW(SHAPE, CALL) }
 
 template <class D, typename T, bool P4 = false>
 static void gated_fwd_launch(const GatedFwd& p, int M, int F, int K, hipStream_t st) {
@@ -429,16 +439,19 @@ static SplitPick choose_split(const TileChoice (&tiles)[N], long rows, long cols
 }
 
 static long whole4(long cols) { return (cols + 3) / 4 * 4; }
-static SplitPick split_of(bool is_bf16, long rows, long cols, int k) {
+static SplitPick split_dx(bool is_bf16, long rows, long cols, int k) {
   return is_bf16 ? choose_split(kTiles, rows, cols, (k + 63) / 64) : choose_split(kTilesF32, rows, cols, (k + 31) / 32);
+}
+static SplitPick split_dw(bool is_bf16, long rows, long cols, int k) {
+  return is_bf16 ? choose_split(kTiles, rows, cols, (k + 63) / 64) : choose_split(kTilesF32Dw, rows, cols, (k + 31) / 32);
 }
 
 size_t gated_split_floats(bool is_bf16, int M, int F, int K) {
-  auto floats = [&](long rows, long cols, int k) -> size_t {
-    const int n = split_of(is_bf16, rows, cols, k).slices;
-    return n > 1 ? (size_t)n * rows * whole4(cols) : 0;
+  auto floats = [](const SplitPick& p, long rows, long cols) -> size_t {
+    return p.slices > 1 ? (size_t)p.slices * rows * whole4(cols) : 0;
   };
-  return std::max({floats(M, K, 2 * gated_cols(F)), floats(2L * F, K, M), floats(F, K, M)});
+  return std::max({floats(split_dx(is_bf16, M, K, 2 * gated_cols(F)), M, K),
+                   floats(split_dw(is_bf16, 2L * F, K, M), 2L * F, K), floats(split_dw(is_bf16, F, K, M), F, K)});
 }
 
 template <typename T>
@@ -490,7 +503,7 @@ hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& p, int M, int F, in
 
 hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw,
                            void* dx, int ldx, float* partial, hipStream_t st) {
-  const SplitPick pick = split_of(is_bf16, M, K, 2 * gated_cols(F));
+  const SplitPick pick = split_dx(is_bf16, M, K, 2 * gated_cols(F));
   const Split sp{pick.slices > 1 ? partial : nullptr, pick.per, (int)whole4(K)};
   if (is_bf16) {
     T2I_TILES(pick.shape, (gated_dx_launch<D, bf16>(M, F, K, dgu, Wg, Wu, ldw, (bf16*)dx, ldx, pick, sp, st)))
@@ -506,16 +519,16 @@ hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, c
 hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, const void* A, int lda, void* dWg,
                            void* dWu, int lddw, float* partial, hipStream_t st) {
   const long rows = (dWg && dWu ? 2L : 1L) * F;
-  const SplitPick pick = split_of(is_bf16, rows, K, M);
+  const SplitPick pick = split_dw(is_bf16, rows, K, M);
   const Split sp{pick.slices > 1 ? partial : nullptr, pick.per, (int)whole4(K)};
   if (is_bf16) {
     T2I_TILES(pick.shape,
               (gated_dw_launch<D, bf16>(M, F, K, dgu, A, lda, (bf16*)dWg, (bf16*)dWu, lddw, pick, sp, st)))
   } else if (f32_pieces({F, K, lda, lddw}, {A, dWg, dWu})) {
-    T2I_TILES_F32(pick.shape,
+    T2I_TILES_F32_DW(pick.shape,
                   (gated_dw_launch<D, float>(M, F, K, dgu, A, lda, (float*)dWg, (float*)dWu, lddw, pick, sp, st)))
   } else {
-    T2I_TILES_F32(pick.shape, (gated_dw_launch<D, float, true>(M, F, K, dgu, A, lda, (float*)dWg, (float*)dWu, lddw,
+    T2I_TILES_F32_DW(pick.shape, (gated_dw_launch<D, float, true>(M, F, K, dgu, A, lda, (float*)dWg, (float*)dWu, lddw,
                                                                pick, sp, st)))
   }
   return hipGetLastError();
@@ -530,7 +543,7 @@ extern "C" int t2i_test_block_tile(int op, int is_bf16, int M, int F, int K, int
   if (op == 0) p.shape = tile_index(M, F, i8_row(K) / 128, 1.f);
   else if (op == 1) p.shape = is_bf16 ? tile_index(M, 2L * F, (K + 63) / 64, 0.5f)
                                       : choose_tile(kTilesF32, M, 2L * F, (K + 31) / 32, 0.5f).shape;
-  else p = op == 2 ? split_of(is_bf16, M, K, 2 * gated_cols(F)) : split_of(is_bf16, 2L * F, K, M);
+  else p = op == 2 ? split_dx(is_bf16, M, K, 2 * gated_cols(F)) : split_dw(is_bf16, 2L * F, K, M);
   const bool stream = (op == 0 || is_bf16) && p.shape > kTile32;   // four stages, one workgroup per CU
   const TileChoice& c = stream ? kTiles[kTile32] : op == 0 || is_bf16 ? kTiles[p.shape] : kTilesF32[p.shape];
   *rows = c.bm;

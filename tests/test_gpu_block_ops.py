@@ -488,7 +488,7 @@ def test_linear_i8_on_every_tile(M, N, K, tile):
     (20, 72, 72, BF16, (32, 128, 2)), (30, 8200, 72, BF16, (32, 128, 1)), (8200, 72, 72, BF16, (64, 128, 2)),
     (8200, 136, 72, BF16, (64, 128, 3)), (8200, 136, 520, BF16, (128, 128, 1)),
     (8200, 264, 520, BF16, (128, 128, 2)), (8200, 520, 2056, BF16, (256, 256, 1)),
-    (300, 200, 72, F32, (64, 64, 1)), (8200, 1032, 72, F32, (64, 64, 1)), (8200, 1031, 71, F32, (64, 64, 1)),
+    (300, 200, 72, F32, (32, 64, 1)), (300, 199, 71, F32, (32, 64, 1)), (8200, 1032, 72, F32, (64, 64, 1)), (8200, 1031, 71, F32, (64, 64, 1)),
     (1032, 1544, 72, F32, (128, 128, 1)), (1032, 1543, 71, F32, (128, 128, 1))])
 def test_gated_linear_on_every_tile(M, F, K, dtype, tile):
     assert tile_of(1, dtype, M, F, K) == (*tile, 1)
@@ -512,11 +512,13 @@ def test_gated_linear_on_every_tile(M, F, K, dtype, tile):
     ("dx", 4100, 1032, 520, BF16, (128, 128, 1, 1)), ("dx", 2050, 2056, 520, BF16, (128, 128, 1, 3)),
     ("dx", 8200, 520, 520, BF16, (128, 128, 2, 1)), ("dx", 4100, 4104, 520, BF16, (128, 128, 2, 3)),
     ("dx", 8200, 2056, 1032, BF16, (256, 256, 1, 1)), ("dx", 2050, 8200, 2056, BF16, (256, 256, 1, 3)),
-    ("dx", 20, 72, 72, F32, (64, 64, 1, 1)), ("dx", 20, 264, 72, F32, (64, 64, 1, 5)),
+    ("dx", 20, 72, 72, F32, (32, 64, 1, 1)), ("dx", 20, 264, 72, F32, (32, 64, 1, 5)),
     ("dx", 8200, 72, 2056, F32, (64, 64, 1, 1)), ("dx", 8200, 71, 2055, F32, (64, 64, 1, 1)),
     ("dx", 2056, 72, 1544, F32, (128, 128, 1, 1)), ("dx", 2056, 71, 1543, F32, (128, 128, 1, 1)),
-    ("dx", 4100, 520, 200, F32, (128, 128, 1, 3)), ("dx", 4100, 521, 203, F32, (128, 128, 1, 3)),
-    ("dx", 77, 1031, 333, F32, (64, 64, 1, 14)), ("dx", 70, 1031, 65, F32, (64, 64, 1, 14)),
+    ("dx", 4100, 520, 200, F32, (32, 64, 1, 1)), ("dx", 4100, 521, 203, F32, (32, 64, 1, 1)),
+    ("dx", 1032, 1032, 1032, F32, (128, 128, 1, 3)), ("dx", 1032, 1031, 1033, F32, (128, 128, 1, 3)),
+    ("dx", 520, 520, 200, F32, (64, 64, 1, 6)), ("dx", 520, 519, 201, F32, (64, 64, 1, 6)),
+    ("dx", 77, 1031, 333, F32, (32, 64, 1, 14)), ("dx", 70, 1031, 65, F32, (32, 64, 1, 14)),
     ("dw", 20, 72, 72, BF16, (32, 128, 2, 1)), ("dw", 2050, 72, 72, BF16, (32, 128, 2, 9)),
     ("dw", 20, 8200, 72, BF16, (64, 128, 2, 1)), ("dw", 2050, 2056, 72, BF16, (64, 128, 2, 4)),
     ("dw", 20, 8200, 200, BF16, (64, 128, 3, 1)), ("dw", 4100, 4104, 72, BF16, (64, 128, 3, 5)),
