@@ -145,7 +145,7 @@ constexpr TileElem elem_of() { return sizeof(T) == 4 ? ELEM_F32 : ELEM_BF16; }
 // 515 - 530 us, one row of 10240 x 4096 33 us (the weights at 5.1 TB/s, a copy's rate).
 template <class D, typename T, bool P4>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand a, TileOperand b, TileShape s,
-                                                                     GatedFwd p, int M, int F) {
+                                                                     GatedFwd p, int M, int F, int vec) {
   using P = TileProduct<D, elem_of<T>(), false, false, true, false, P4>;
   constexpr int THREADS = D::NW * 64, H = D::BN / 2, TH = D::TN / 2;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + D::BN * 4];
@@ -172,7 +172,8 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
 #pragma unroll
     for (int j = 0; j < TH; ++j) {
       const int fl = nw + j * 16 + g * 4, f = f0 + fl;
-      const int left = P4 ? F - f : 4;   // (else F % 4 == 0: four columns or none)
+      const int left = sizeof(T) == 4 ? F - f : 4;   // (bf16: F % 8 == 0, four columns or none)
+      const bool whole = sizeof(T) == 2 || vec;
       if (f >= F) continue;
       const f32x4 bg = *(const f32x4*)(ev + fl), bu = *(const f32x4*)(ev + H + fl);
       float gv[4], uv[4], y[4];
@@ -184,21 +185,21 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
       }
       if (p.pre) {
         float* q = p.pre + (size_t)m * p.ldp + f;
-        store4(q, left, !P4, gv);
-        store4(q + F, left, !P4, uv);
+        store4(q, left, whole, gv);
+        store4(q + F, left, whole, uv);
       }
-      store4((T*)p.out + (size_t)m * p.ldo + f, left, !P4, y);
+      store4((T*)p.out + (size_t)m * p.ldo + f, left, whole, y);
     }
   }
 }
 
 // The gradients' products.  b is a KR operand: a pair of fragments holds 8
-// neighbouring columns of a row, of which all or the first four exist (N % 4 == 0,
-// except with 4-byte loads).  Stored in the operands' type (row stride ldc), or as
-// fp32 partial sums (row stride N) where the contraction is split.
-template <class D, class P, bool P4, typename T>
+// neighbouring columns of a row (bf16: all of them exist).  Stored in the operands'
+// type (row stride ldc), or as fp32 partial sums (row stride Split::ld) where the
+// contraction is split; vec: fp32 rows lie in whole 16-byte pieces.
+template <class D, class P, typename T>
 __device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D::TN], T* C, int ldc, int m0,
-                                           int n0, int M, int N) {
+                                           int n0, int M, int N, bool vec) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
   const int mw = m0 + (wave / D::WGN) * D::WM, nw = n0 + (wave % D::WGN) * D::WN;
 #pragma unroll
@@ -218,8 +219,8 @@ __device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D
       } else {
         const float lo[4] = {acc[i][j][0], acc[i][j + 1][0], acc[i][j][1], acc[i][j + 1][1]};
         const float hi[4] = {acc[i][j][2], acc[i][j + 1][2], acc[i][j][3], acc[i][j + 1][3]};
-        store4(p, N - n, !P4, lo);
-        store4(p + 4, N - n - 4, !P4, hi);
+        store4(p, N - n, vec, lo);
+        store4(p + 4, N - n - 4, vec, hi);
       }
     }
   }
@@ -239,7 +240,7 @@ __device__ __forceinline__ void take_slice(const Split& sp, TileShape& s) {
 
 template <class D, typename T, bool P4>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
-                                                                 T* dx, int ldx, int M, int K) {
+                                                                 T* dx, int ldx, int M, int K, int vec) {
   using P = TileProduct<D, elem_of<T>(), false, true, false, true, P4>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
@@ -248,9 +249,9 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, 
   typename P::Acc acc[D::TM][D::TN];
   P::run(smem, a, b, s, tm * D::BM, tn * D::BN, acc);
   if (sp.partial)
-    store_tile<D, P, false>(acc, sp.partial + (size_t)blockIdx.y * M * sp.ld, sp.ld, tm * D::BM, tn * D::BN, M, sp.ld);
+    store_tile<D, P>(acc, sp.partial + (size_t)blockIdx.y * M * sp.ld, sp.ld, tm * D::BM, tn * D::BN, M, sp.ld, true);
   else
-    store_tile<D, P, P4>(acc, dx, ldx, tm * D::BM, tn * D::BN, M, K);
+    store_tile<D, P>(acc, dx, ldx, tm * D::BM, tn * D::BN, M, K, vec);
 }
 
 // row blocks [0, half) are the first output's, the others the second's (their
@@ -258,7 +259,7 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, 
 template <class D, typename T, bool P4>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
                                                                  int half, int shift, T* d0, T* d1, int ldw,
-                                                                 int F, int K) {
+                                                                 int F, int K, int vec) {
   using P = TileProduct<D, elem_of<T>(), true, true, false, false, P4>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
@@ -271,9 +272,9 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, 
   P::run(smem, a, b, s, m0, tn * D::BN, acc);
   if (sp.partial) {
     const size_t of = (size_t)blockIdx.y * (s.tiles_m / half) * F + (second ? F : 0);
-    store_tile<D, P, false>(acc, sp.partial + of * sp.ld, sp.ld, m0, tn * D::BN, F, sp.ld);
+    store_tile<D, P>(acc, sp.partial + of * sp.ld, sp.ld, m0, tn * D::BN, F, sp.ld, true);
   } else {
-    store_tile<D, P, P4>(acc, second ? d1 : d0, ldw, m0, tn * D::BN, F, K);
+    store_tile<D, P>(acc, second ? d1 : d0, ldw, m0, tn * D::BN, F, K, vec);
   }
 }
 
@@ -401,23 +402,23 @@ hipError_t launch_linear_i8(const int8_t* A, int lda, const int8_t* W, int ldw, 
   if (SHAPE == 2) { using D = Tile32s; CALL; }    \
   else { T2I_TILES_F32_DW(SHAPE, CALL) }
 
+// whether these sizes and strides of fp32 values, and pointers, are whole 16-byte pieces
+static bool f32_pieces(std::initializer_list<int> sizes, std::initializer_list<const void*> ptrs) {
+  uintptr_t bits = 0;
+  for (int n : sizes) bits |= (uintptr_t)n * 4;
+  for (const void* p : ptrs) bits |= (uintptr_t)p;
+  return bits % 16 == 0;
+}
+
 template <class D, typename T, bool P4 = false>
 static void gated_fwd_launch(const GatedFwd& p, int M, int F, int K, hipStream_t st) {
   constexpr int e = sizeof(T), per = 128 / e;
   const TileOperand a{(const char*)p.A, nullptr, (uint32_t)e * p.lda, M, 0},
       b{(const char*)p.Wg, (const char*)p.Wu, (uint32_t)e * p.ldw, F, 0};
   const TileShape s = tile_shape<D>(M, 2 * F, (K + per - 1) / per, e * K, 0);
+  const int vec = f32_pieces({F, p.ldo, p.pre ? p.ldp : 0}, {p.out, p.pre});
   hipLaunchKernelGGL((gated_linear_kernel<D, T, P4>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64), 0, st, a,
-                     b, s, p, M, F);
-}
-
-// whether fp32 operands lie in whole, aligned 16-byte pieces (sizes and strides, and
-// the bits of all pointers): then they go through the same tiles
-static bool f32_pieces(std::initializer_list<int> sizes, std::initializer_list<const void*> ptrs) {
-  uintptr_t bits = 0;
-  for (int n : sizes) bits |= (uintptr_t)n * 4;
-  for (const void* p : ptrs) bits |= (uintptr_t)p;
-  return bits % 16 == 0;
+                     b, s, p, M, F, vec);
 }
 
 // Tile shape and slices of a gradient's product: as few slices as keep the time
@@ -469,9 +470,10 @@ static void gated_dx_launch(int M, int F, int K, const void* dgu, const void* Wg
   const TileOperand a{(const char*)dgu, nullptr, 2u * e * Fp, M, 0},
       b{(const char*)Wg, (const char*)Wu, (uint32_t)e * ldw, F, K};
   const TileShape s = tile_shape<D>(M, K, 2 * Fp / per, 2 * e * Fp, Fp / per);
+  const bool vec = sizeof(T) == 2 || f32_pieces({K, ldx}, {dx});
   hipLaunchKernelGGL((gated_dx_kernel<D, T, P4>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
-                     st, a, b, s, sp, dx, ldx, M, K);
-  if (sp.partial) split_sum(sp, pick.slices, M, M, K, dx, dx, ldx, !P4, st);
+                     st, a, b, s, sp, dx, ldx, M, K, vec);
+  if (sp.partial) split_sum(sp, pick.slices, M, M, K, dx, dx, ldx, vec, st);
 }
 
 template <class D, typename T, bool P4 = false>
@@ -480,21 +482,22 @@ static void gated_dw_launch(int M, int F, int K, const void* dgu, const void* A,
   constexpr int e = sizeof(T), per = 128 / e;
   const int Fp = gated_cols(F), n = dWg && dWu ? 2 : 1;
   T* const first = dWg ? dWg : dWu;
-  const TileOperand a{(const char*)dgu + (dWg ? 0 : (size_t)e * Fp), nullptr, 2u * e * Fp, M, F},
+  const TileOperand a{(const char*)dgu + (dWg ? 0 : (size_t)e * Fp), nullptr, 2u * e * Fp, M, (F + 7) / 8 * 8},
       b{(const char*)A, nullptr, (uint32_t)e * lda, M, K};
   TileShape s = tile_shape<D>(F, K, (M + per - 1) / per, 0, 0);
   const int half = s.tiles_m;
   s.tiles_m *= n;
+  const bool vec = sizeof(T) == 2 || f32_pieces({K, lddw}, {dWg, dWu});
   hipLaunchKernelGGL((gated_dw_kernel<D, T, P4>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
-                     st, a, b, s, sp, half, e * Fp, first, dWu, lddw, F, K);
-  if (sp.partial) split_sum(sp, pick.slices, (long)n * F, F, K, first, dWu, lddw, !P4, st);
+                     st, a, b, s, sp, half, e * Fp, first, dWu, lddw, F, K, vec);
+  if (sp.partial) split_sum(sp, pick.slices, (long)n * F, F, K, first, dWu, lddw, vec, st);
 }
 
 hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& p, int M, int F, int K, hipStream_t st) {
   const TilePick f32 = choose_tile(kTilesF32, M, 2L * F, (K + 31) / 32, 0.5f);
   if (is_bf16)
     T2I_TILES(tile_index(M, 2L * F, (K + 63) / 64, 0.5f), (gated_fwd_launch<D, bf16>(p, M, F, K, st)))
-  else if (f32_pieces({F, K, p.lda, p.ldw, p.ldo, p.pre ? p.ldp : 0}, {p.A, p.Wg, p.Wu, p.out, p.pre}))
+  else if (f32_pieces({K, p.lda, p.ldw}, {p.A, p.Wg, p.Wu}))
     T2I_TILES_F32(f32.shape, (gated_fwd_launch<D, float>(p, M, F, K, st)))
   else
     T2I_TILES_F32(f32.shape, (gated_fwd_launch<D, float, true>(p, M, F, K, st)))
@@ -507,7 +510,7 @@ hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, c
   const Split sp{pick.slices > 1 ? partial : nullptr, pick.per, (int)whole4(K)};
   if (is_bf16) {
     T2I_TILES(pick.shape, (gated_dx_launch<D, bf16>(M, F, K, dgu, Wg, Wu, ldw, (bf16*)dx, ldx, pick, sp, st)))
-  } else if (f32_pieces({K, ldw, ldx}, {Wg, Wu, dx})) {
+  } else if (f32_pieces({K, ldw}, {Wg, Wu})) {
     T2I_TILES_F32(pick.shape, (gated_dx_launch<D, float>(M, F, K, dgu, Wg, Wu, ldw, (float*)dx, ldx, pick, sp, st)))
   } else {
     T2I_TILES_F32(pick.shape,
@@ -524,7 +527,7 @@ hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, c
   if (is_bf16) {
     T2I_TILES(pick.shape,
               (gated_dw_launch<D, bf16>(M, F, K, dgu, A, lda, (bf16*)dWg, (bf16*)dWu, lddw, pick, sp, st)))
-  } else if (f32_pieces({F, K, lda, lddw}, {A, dWg, dWu})) {
+  } else if (f32_pieces({K, lda}, {A})) {
     T2I_TILES_F32_DW(pick.shape,
                   (gated_dw_launch<D, float>(M, F, K, dgu, A, lda, (float*)dWg, (float*)dWu, lddw, pick, sp, st)))
   } else {

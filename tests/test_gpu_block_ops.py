@@ -264,7 +264,7 @@ def test_gated_linear(M, F, K, act, dtype):
 
 
 @pytest.mark.parametrize("M,F,K,extra", [(5, 1, 1, 0), (3, 7, 5, 0), (70, 33, 65, 0), (130, 131, 257, 0),
-                                         (130, 132, 260, 0), (70, 36, 68, 4), (70, 36, 68, 1), (300, 700, 333, 2),
+                                         (130, 132, 260, 0), (130, 131, 260, 0), (130, 132, 257, 0), (70, 36, 68, 4), (70, 36, 68, 1), (300, 700, 333, 2),
                                          (2100, 12, 20, 0)])
 def test_gated_linear_f32_any_width(M, F, K, extra):
     """Widths and strides that are no multiples of 16 bytes, and of 16 but not of 32."""
