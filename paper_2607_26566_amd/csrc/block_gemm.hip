@@ -143,10 +143,10 @@ constexpr TileElem elem_of() { return sizeof(T) == 4 ? ELEM_F32 : ELEM_BF16; }
 // go to memory only where the backward pass wants them.  8192 x 4608 x 1152 155 - 170
 // us (1.0 - 1.1 PFLOP/s: 4.5 rounds of tiles in 5, 18 k steps each), 4096 x 10240 x 4096
 // 515 - 530 us, one row of 10240 x 4096 33 us (the weights at 5.1 TB/s, a copy's rate).
-template <class D, typename T, bool P4>
+template <class D, typename T, bool U>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand a, TileOperand b, TileShape s,
                                                                      GatedFwd p, int M, int F, int vec) {
-  using P = TileProduct<D, elem_of<T>(), false, false, true, false, P4>;
+  using P = TileProduct<D, elem_of<T>(), false, false, true, false, U>;
   constexpr int THREADS = D::NW * 64, H = D::BN / 2, TH = D::TN / 2;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + D::BN * 4];
   int tm, tn;
@@ -226,6 +226,14 @@ __device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D
   }
 }
 
+// First column of column block tn.  U: the last block ends with the matrix (if that is
+// not narrower than a tile) and does some columns over again, the same sums in the
+// same order, so that no load reaches past a row's end.
+template <class D, bool U>
+__device__ __forceinline__ int first_column(int tn, int cols) {
+  return U && cols >= D::BN ? min(tn * D::BN, cols - D::BN) : tn * D::BN;
+}
+
 // A contraction split over gridDim.y slices of `per` steps: slice y writes fp32
 // partial sums [rows][ld] behind those of the slices before it, which
 // split_sum_kernel adds up in order.
@@ -238,29 +246,30 @@ __device__ __forceinline__ void take_slice(const Split& sp, TileShape& s) {
   s.steps = min(sp.per, s.steps - s.first);
 }
 
-template <class D, typename T, bool P4>
+template <class D, typename T, bool U>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
                                                                  T* dx, int ldx, int M, int K, int vec) {
-  using P = TileProduct<D, elem_of<T>(), false, true, false, true, P4>;
+  using P = TileProduct<D, elem_of<T>(), false, true, false, true, U>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
   if (sp.partial) take_slice(sp, s);
   typename P::Acc acc[D::TM][D::TN];
-  P::run(smem, a, b, s, tm * D::BM, tn * D::BN, acc);
+  const int m0 = tm * D::BM, n0 = first_column<D, U>(tn, K);
+  P::run(smem, a, b, s, m0, n0, acc);
   if (sp.partial)
-    store_tile<D, P>(acc, sp.partial + (size_t)blockIdx.y * M * sp.ld, sp.ld, tm * D::BM, tn * D::BN, M, sp.ld, true);
+    store_tile<D, P>(acc, sp.partial + (size_t)blockIdx.y * M * sp.ld, sp.ld, m0, n0, M, K, !U);
   else
-    store_tile<D, P>(acc, dx, ldx, tm * D::BM, tn * D::BN, M, K, vec);
+    store_tile<D, P>(acc, dx, ldx, m0, n0, M, K, vec);
 }
 
 // row blocks [0, half) are the first output's, the others the second's (their
 // operand lies `shift` bytes further)
-template <class D, typename T, bool P4>
+template <class D, typename T, bool U>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
                                                                  int half, int shift, T* d0, T* d1, int ldw,
                                                                  int F, int K, int vec) {
-  using P = TileProduct<D, elem_of<T>(), true, true, false, false, P4>;
+  using P = TileProduct<D, elem_of<T>(), true, true, false, false, U>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
@@ -269,12 +278,13 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, 
   const int m0 = (second ? tm - half : tm) * D::BM;
   if (second) a.p += shift;
   typename P::Acc acc[D::TM][D::TN];
-  P::run(smem, a, b, s, m0, tn * D::BN, acc);
+  const int n0 = first_column<D, U>(tn, K);
+  P::run(smem, a, b, s, m0, n0, acc);
   if (sp.partial) {
     const size_t of = (size_t)blockIdx.y * (s.tiles_m / half) * F + (second ? F : 0);
-    store_tile<D, P>(acc, sp.partial + of * sp.ld, sp.ld, m0, tn * D::BN, F, sp.ld, true);
+    store_tile<D, P>(acc, sp.partial + of * sp.ld, sp.ld, m0, n0, F, K, !U);
   } else {
-    store_tile<D, P>(acc, second ? d1 : d0, ldw, m0, tn * D::BN, F, K, vec);
+    store_tile<D, P>(acc, second ? d1 : d0, ldw, m0, n0, F, K, vec);
   }
 }
 
@@ -410,14 +420,14 @@ static bool f32_pieces(std::initializer_list<int> sizes, std::initializer_list<c
   return bits % 16 == 0;
 }
 
-template <class D, typename T, bool P4 = false>
+template <class D, typename T, bool U = false>
 static void gated_fwd_launch(const GatedFwd& p, int M, int F, int K, hipStream_t st) {
   constexpr int e = sizeof(T), per = 128 / e;
   const TileOperand a{(const char*)p.A, nullptr, (uint32_t)e * p.lda, M, 0},
       b{(const char*)p.Wg, (const char*)p.Wu, (uint32_t)e * p.ldw, F, 0};
   const TileShape s = tile_shape<D>(M, 2 * F, (K + per - 1) / per, e * K, 0);
   const int vec = f32_pieces({F, p.ldo, p.pre ? p.ldp : 0}, {p.out, p.pre});
-  hipLaunchKernelGGL((gated_linear_kernel<D, T, P4>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64), 0, st, a,
+  hipLaunchKernelGGL((gated_linear_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64), 0, st, a,
                      b, s, p, M, F, vec);
 }
 
@@ -462,7 +472,7 @@ static void split_sum(const Split& sp, int slices, long rows, long half, int col
                      sp.partial, slices, rows, half, cols, sp.ld, o0, o1, ld, vec);
 }
 
-template <class D, typename T, bool P4 = false>
+template <class D, typename T, bool U = false>
 static void gated_dx_launch(int M, int F, int K, const void* dgu, const void* Wg, const void* Wu, int ldw, T* dx,
                             int ldx, const SplitPick& pick, const Split& sp, hipStream_t st) {
   constexpr int e = sizeof(T), per = 128 / e;
@@ -471,12 +481,12 @@ static void gated_dx_launch(int M, int F, int K, const void* dgu, const void* Wg
       b{(const char*)Wg, (const char*)Wu, (uint32_t)e * ldw, F, K};
   const TileShape s = tile_shape<D>(M, K, 2 * Fp / per, 2 * e * Fp, Fp / per);
   const bool vec = sizeof(T) == 2 || f32_pieces({K, ldx}, {dx});
-  hipLaunchKernelGGL((gated_dx_kernel<D, T, P4>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
+  hipLaunchKernelGGL((gated_dx_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
                      st, a, b, s, sp, dx, ldx, M, K, vec);
   if (sp.partial) split_sum(sp, pick.slices, M, M, K, dx, dx, ldx, vec, st);
 }
 
-template <class D, typename T, bool P4 = false>
+template <class D, typename T, bool U = false>
 static void gated_dw_launch(int M, int F, int K, const void* dgu, const void* A, int lda, T* dWg, T* dWu, int lddw,
                             const SplitPick& pick, const Split& sp, hipStream_t st) {
   constexpr int e = sizeof(T), per = 128 / e;
@@ -488,7 +498,7 @@ static void gated_dw_launch(int M, int F, int K, const void* dgu, const void* A,
   const int half = s.tiles_m;
   s.tiles_m *= n;
   const bool vec = sizeof(T) == 2 || f32_pieces({K, lddw}, {dWg, dWu});
-  hipLaunchKernelGGL((gated_dw_kernel<D, T, P4>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
+  hipLaunchKernelGGL((gated_dw_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
                      st, a, b, s, sp, half, e * Fp, first, dWu, lddw, F, K, vec);
   if (sp.partial) split_sum(sp, pick.slices, (long)n * F, F, K, first, dWu, lddw, vec, st);
 }

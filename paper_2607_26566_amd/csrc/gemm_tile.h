@@ -42,8 +42,10 @@
 // POP/s; 2.11); fp32 at 4096 x 9216 x 1152 608 us (143 TFLOP/s; 154).  At K = 1152 the
 // first loads and the epilogue take a fifth to a half of a tile's time, see kTiles.
 //
-// fp32 operands that do not lie in whole, aligned 16-byte pieces are loaded 4 bytes
-// per lane instead (P4), four times the load instructions into the same layout.
+// fp32 operands whose rows do not lie in whole, aligned 16-byte pieces (U) are loaded
+// by the same 16 bytes per lane from addresses that are multiples of 4, and 4 bytes
+// per lane, four times the instructions, where a piece would reach past a row's end:
+// KC in the last step, KR in a tile that is wider than the matrix.
 //
 // Sizes: tile rows behind the operand's last are read as that row (KC), columns as
 // its last ones (KR): what comes of them is not stored.  k behind the end is read as
@@ -140,14 +142,11 @@ enum TileElem { ELEM_BF16, ELEM_I8, ELEM_F32 };
 // E: element type.  AKR, BKR: operand layouts.  DUAL: b is two matrices side by side,
 // p for the first half of the tile's columns and p2 for the second, so that a wave
 // holds both of an output.  SEGS (BKR): the contraction runs over p's rows, then p2's.
-// P4: loads of 4 bytes (fp32).
-template <class D, TileElem E, bool AKR, bool BKR, bool DUAL, bool SEGS, bool P4 = false>
+// U: operand rows anywhere (fp32).
+template <class D, TileElem E, bool AKR, bool BKR, bool DUAL, bool SEGS, bool U = false>
 struct TileProduct {
-  static_assert(!P4 || E == ELEM_F32, "4-byte loads");
-  static constexpr int Q = P4 ? 4 : 1;   // load instructions per KB
-  static constexpr int PB = 16 / Q;      // bytes per lane of one
-  static constexpr int LOADS = D::LOADS * Q;
-  static_assert((D::ST - 1) * LOADS < 64, "outstanding loads");
+  static_assert(!U || E == ELEM_F32, "rows off 16 bytes");
+  static constexpr int LOADS = D::LOADS;
   static constexpr bool I8 = E == ELEM_I8;
   static constexpr int EB = E == ELEM_F32 ? 4 : I8 ? 1 : 2;   // bytes of an element
   static constexpr int KROWS = 128 / EB;                      // k of a step
@@ -186,31 +185,30 @@ struct TileProduct {
     constexpr int LA = BM / 8 / D::NW;
     const int KT = s.steps;
 
-    // ---- sources: this lane's offset of each load.  Load i takes part i % Q of KB
-    // block wave + i / Q waves, a's blocks first; byte `at` of that operand's stage.
-    auto block_of = [&](int i) { return wave + (i / Q < LA ? i / Q : i / Q - LA) * D::NW; };
-    auto at_of = [&](int i) { return block_of(i) * 1024 + i % Q * 256 + lane * PB; };
+    // ---- sources: this lane's offset of each load.  Load i takes KB block wave + i
+    // waves of the stage, a's blocks first; byte `at` of that operand's stage.
+    auto block_of = [&](int i) { return wave + (i < LA ? i : i - LA) * D::NW; };
+    auto at_of = [&](int i) { return block_of(i) * 1024 + lane * 16; };
     // KC: row and byte of k (within the step) of a place in the stage
     auto kc_row = [](int at) { return at >> 7; };
     auto kc_byte = [](int at) { return ((((at >> 4) & 7) ^ ((at >> 8) & 7)) << 4) | (at & 15); };
-    uint32_t src[LOADS];
-#pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const bool is_a = i / Q < LA;
+    // offset of the `bytes` that belong at byte `at`
+    auto source = [&](bool is_a, int at, int bytes) -> uint32_t {
       const TileOperand& o = is_a ? a : b;
-      const int at = at_of(i);
       if (is_a ? AKR : BKR) {
         int row, col;
         if (is_a) kr_source<BM, NA>(at, row, col);
         else kr_source<BN, NB>(at, row, col);
-        src[i] = (uint32_t)row * o.ld + EB * (uint32_t)min((is_a ? m0 : n0) + col, o.cols - PB / EB);
-      } else {
-        // rows from the tile's first, not behind the last (DUAL: within the half)
-        const int r0 = is_a ? m0 : n0, lr = kc_row(at);
-        const int rr = !is_a && DUAL && lr >= BN / 2 ? lr - BN / 2 : lr;
-        src[i] = (uint32_t)min(rr, o.rows - 1 - r0) * o.ld + kc_byte(at);
+        return (uint32_t)row * o.ld + EB * (uint32_t)min((is_a ? m0 : n0) + col, o.cols - bytes / EB);
       }
-    }
+      // rows from the tile's first, not behind the last (DUAL: within the half)
+      const int r0 = is_a ? m0 : n0, lr = kc_row(at);
+      const int rr = !is_a && DUAL && lr >= BN / 2 ? lr - BN / 2 : lr;
+      return (uint32_t)min(rr, o.rows - 1 - r0) * o.ld + kc_byte(at);
+    };
+    uint32_t src[LOADS];
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) src[i] = source(i < LA, at_of(i), 16);
     const bool ragged_k = !I8 && s.kbytes % 128 != 0;   // KC: places of the last step lie behind k
     // KC: rows at fixed offsets from the tile's first, k as the scalar offset.
     // KR: the step's first row as the base, the resource ends with its last row.
@@ -231,18 +229,32 @@ struct TileProduct {
     const __amdgpu_buffer_rsrc_t rb2_kc = kc_res(DUAL ? b.p2 : b.p, BKR ? 0 : (size_t)n0 * b.ld + (size_t)s.first * 128);
     auto res_a = [&](int t) { return AKR ? kr_res(a, t, false) : ra_kc; };
     auto res_b = [&](int t) { return BKR ? kr_res(b, t, SEGS) : rb_kc; };
+    // U: whether a load of step t takes 4 bytes at a time (a KR operand a is the
+    // gradients' workspace: whole pieces)
+    auto fine = [&](bool is_a, int t) {
+      if (is_a ? AKR : BKR) return !is_a && n0 + BN > b.cols;
+      return ragged_k && t == KT - 1;
+    };
     auto issue = [&](int i, int t, uint32_t slot, const __amdgpu_buffer_rsrc_t& ra,
                      const __amdgpu_buffer_rsrc_t& rb) {
-      const bool is_a = i / Q < LA;
+      const bool is_a = i < LA;
       const int blk = block_of(i);
-      char* const dst = smem + slot + (is_a ? 0 : BM * 128) + blk * 1024 + i % Q * 256;
-      if (is_a ? AKR : BKR) {
-        tile_load<PB>(is_a ? ra : rb, dst, src[i], 0);
+      char* const dst = smem + slot + (is_a ? 0 : BM * 128) + blk * 1024;
+      const bool up = DUAL && !is_a && blk * 8 >= BN / 2;
+      const __amdgpu_buffer_rsrc_t& r = is_a ? ra : up ? rb2_kc : rb;
+      const bool kr = is_a ? AKR : BKR;
+      const int soff = kr ? 0 : t * 128;
+      auto behind = [&](int at) {   // KC: k behind the end
+        return !kr && ragged_k && t == KT - 1 && (s.first + t) * 128 + kc_byte(at) >= s.kbytes;
+      };
+      if (U && fine(is_a, t)) {
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int at = blk * 1024 + q * 256 + lane * 4;
+          tile_load<4>(r, dst + q * 256, behind(at) ? kTileOff : source(is_a, at, 4), soff);
+        }
       } else {
-        uint32_t v = src[i];
-        if (ragged_k && t == KT - 1 && (s.first + t) * 128 + kc_byte(at_of(i)) >= s.kbytes) v = kTileOff;
-        const bool up = DUAL && !is_a && blk * 8 >= BN / 2;
-        tile_load<PB>(is_a ? ra : up ? rb2_kc : rb, dst, v, t * 128);
+        tile_load<16>(r, dst, behind(at_of(i)) ? kTileOff : src[i], soff);
       }
     };
 
