@@ -52,12 +52,13 @@ struct Staged {
   }
 };
 
-// four consecutive values of a row, to memory as T
+// four consecutive values of a row, to memory as T: one store at any alignment of T
+// (odd widths: fp32 dW of 9238 x 2385 82 -> 36 us, 8 bits 4032 x 9343 x 632 90 -> 66)
 template <typename T>
-__device__ __forceinline__ void store4(T* p, int left, bool vec, const float (&v)[4]) {
-  if (vec && left >= 4) {
-    if constexpr (sizeof(T) == 2) *(bf16x4*)p = bf16x4{(bf16)v[0], (bf16)v[1], (bf16)v[2], (bf16)v[3]};
-    else *(f32x4*)p = f32x4{v[0], v[1], v[2], v[3]};
+__device__ __forceinline__ void store4(T* p, int left, const float (&v)[4]) {
+  typedef T any4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+  if (left >= 4) {
+    *(any4*)p = any4{(T)v[0], (T)v[1], (T)v[2], (T)v[3]};
   } else {
 #pragma unroll
     for (int r = 0; r < 4; ++r)
@@ -78,7 +79,7 @@ __device__ __forceinline__ float i8_value(int acc, float sa, float sw, float b, 
 // output) take more than the products; 4096 x 4096 x 12288 168 us (2.45 POP/s).
 template <class D, typename T, bool RES>
 __global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a, TileOperand b, TileShape s,
-                                                                  I8Epi e, int M, int N, int vec) {
+                                                                  I8Epi e, int M, int N) {
   using P = TileProduct<D, ELEM_I8, false, false, false, false>;
   constexpr int THREADS = D::NW * 64, NE = D::BM + (RES ? 3 : 2) * D::BN;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + NE * 4];
@@ -118,18 +119,19 @@ __global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a,
         float* x = e.x + (size_t)m * e.ldx + n;
         const f32x4 gt = *(const f32x4*)(ev + D::BM + 2 * D::BN + nl);
         float xv[4];
-        if (vec && left >= 4) {
-          const f32x4 x4 = *(const f32x4*)x;
+        if (left >= 4) {
+          typedef float any4 __attribute__((ext_vector_type(4), aligned(4)));
+          const any4 x4 = *(const any4*)x;
 #pragma unroll
           for (int r = 0; r < 4; ++r) xv[r] = x4[r] + gt[r] * y[r];
         } else {
 #pragma unroll
           for (int r = 0; r < 4; ++r) xv[r] = r < left ? x[r] + gt[r] * y[r] : 0.f;
         }
-        store4(x, left, vec, xv);
-        if (e.xb) store4(e.xb + (size_t)m * e.ldx + n, left, vec, xv);
+        store4(x, left, xv);
+        if (e.xb) store4(e.xb + (size_t)m * e.ldx + n, left, xv);
       } else {
-        store4((T*)e.out + (size_t)m * e.ldo + n, left, vec, y);
+        store4((T*)e.out + (size_t)m * e.ldo + n, left, y);
       }
     }
   }
@@ -145,7 +147,7 @@ constexpr TileElem elem_of() { return sizeof(T) == 4 ? ELEM_F32 : ELEM_BF16; }
 // 515 - 530 us, one row of 10240 x 4096 33 us (the weights at 5.1 TB/s, a copy's rate).
 template <class D, typename T, bool U>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand a, TileOperand b, TileShape s,
-                                                                     GatedFwd p, int M, int F, int vec) {
+                                                                     GatedFwd p, int M, int F) {
   using P = TileProduct<D, elem_of<T>(), false, false, true, false, U>;
   constexpr int THREADS = D::NW * 64, H = D::BN / 2, TH = D::TN / 2;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + D::BN * 4];
@@ -173,7 +175,6 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
     for (int j = 0; j < TH; ++j) {
       const int fl = nw + j * 16 + g * 4, f = f0 + fl;
       const int left = sizeof(T) == 4 ? F - f : 4;   // (bf16: F % 8 == 0, four columns or none)
-      const bool whole = sizeof(T) == 2 || vec;
       if (f >= F) continue;
       const f32x4 bg = *(const f32x4*)(ev + fl), bu = *(const f32x4*)(ev + H + fl);
       float gv[4], uv[4], y[4];
@@ -185,10 +186,10 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
       }
       if (p.pre) {
         float* q = p.pre + (size_t)m * p.ldp + f;
-        store4(q, left, whole, gv);
-        store4(q + F, left, whole, uv);
+        store4(q, left, gv);
+        store4(q + F, left, uv);
       }
-      store4((T*)p.out + (size_t)m * p.ldo + f, left, whole, y);
+      store4((T*)p.out + (size_t)m * p.ldo + f, left, y);
     }
   }
 }
@@ -196,10 +197,10 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
 // The gradients' products.  b is a KR operand: a pair of fragments holds 8
 // neighbouring columns of a row (bf16: all of them exist).  Stored in the operands'
 // type (row stride ldc), or as fp32 partial sums (row stride Split::ld) where the
-// contraction is split; vec: fp32 rows lie in whole 16-byte pieces.
+// contraction is split.
 template <class D, class P, typename T>
 __device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D::TN], T* C, int ldc, int m0,
-                                           int n0, int M, int N, bool vec) {
+                                           int n0, int M, int N) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
   const int mw = m0 + (wave / D::WGN) * D::WM, nw = n0 + (wave % D::WGN) * D::WN;
 #pragma unroll
@@ -219,8 +220,8 @@ __device__ __forceinline__ void store_tile(const typename P::Acc (&acc)[D::TM][D
       } else {
         const float lo[4] = {acc[i][j][0], acc[i][j + 1][0], acc[i][j][1], acc[i][j + 1][1]};
         const float hi[4] = {acc[i][j][2], acc[i][j + 1][2], acc[i][j][3], acc[i][j + 1][3]};
-        store4(p, N - n, vec, lo);
-        store4(p + 4, N - n - 4, vec, hi);
+        store4(p, N - n, lo);
+        store4(p + 4, N - n - 4, hi);
       }
     }
   }
@@ -248,7 +249,7 @@ __device__ __forceinline__ void take_slice(const Split& sp, TileShape& s) {
 
 template <class D, typename T, bool U>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
-                                                                 T* dx, int ldx, int M, int K, int vec) {
+                                                                 T* dx, int ldx, int M, int K) {
   using P = TileProduct<D, elem_of<T>(), false, true, false, true, U>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
@@ -258,9 +259,9 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, 
   const int m0 = tm * D::BM, n0 = first_column<D, U>(tn, K);
   P::run(smem, a, b, s, m0, n0, acc);
   if (sp.partial)
-    store_tile<D, P>(acc, sp.partial + (size_t)blockIdx.y * M * sp.ld, sp.ld, m0, n0, M, K, !U);
+    store_tile<D, P>(acc, sp.partial + (size_t)blockIdx.y * M * sp.ld, sp.ld, m0, n0, M, K);
   else
-    store_tile<D, P>(acc, dx, ldx, m0, n0, M, K, vec);
+    store_tile<D, P>(acc, dx, ldx, m0, n0, M, K);
 }
 
 // row blocks [0, half) are the first output's, the others the second's (their
@@ -268,7 +269,7 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, 
 template <class D, typename T, bool U>
 __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
                                                                  int half, int shift, T* d0, T* d1, int ldw,
-                                                                 int F, int K, int vec) {
+                                                                 int F, int K) {
   using P = TileProduct<D, elem_of<T>(), true, true, false, false, U>;
   __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
   int tm, tn;
@@ -282,9 +283,9 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, 
   P::run(smem, a, b, s, m0, n0, acc);
   if (sp.partial) {
     const size_t of = (size_t)blockIdx.y * (s.tiles_m / half) * F + (second ? F : 0);
-    store_tile<D, P>(acc, sp.partial + of * sp.ld, sp.ld, m0, n0, F, K, !U);
+    store_tile<D, P>(acc, sp.partial + of * sp.ld, sp.ld, m0, n0, F, K);
   } else {
-    store_tile<D, P>(acc, second ? d1 : d0, ldw, m0, n0, F, K, vec);
+    store_tile<D, P>(acc, second ? d1 : d0, ldw, m0, n0, F, K);
   }
 }
 
@@ -292,7 +293,7 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, 
 // [rows][ldp], in ascending slice order; one thread per 4 columns
 template <typename T>
 __global__ __launch_bounds__(256) void split_sum_kernel(const float* __restrict__ partial, int slices, long rows,
-                                                        long half, int cols, int ldp, T* o0, T* o1, int ld, int vec) {
+                                                        long half, int cols, int ldp, T* o0, T* o1, int ld) {
   const long x = blockIdx.x * 256L + threadIdx.x, n4 = ldp / 4;
   if (x >= rows * n4) return;
   const long r = x / n4;
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(256) void split_sum_kernel(const float* __restrict_
 #pragma unroll 4
   for (int i = 1; i < slices; ++i) a += *(const f32x4*)(p + i * rows * ldp);
   const float v[4] = {a[0], a[1], a[2], a[3]};
-  store4((r < half ? o0 + r * ld : o1 + (r - half) * ld) + c, cols - c, vec, v);
+  store4((r < half ? o0 + r * ld : o1 + (r - half) * ld) + c, cols - c, v);
 }
 
 // ---- launches
@@ -371,10 +372,8 @@ static void i8_launch(const TileOperand& a, const TileOperand& b, const I8Epi& e
   const TileShape s = tile_shape<D>(M, N, i8_row(K) / 128, i8_row(K), 0);
   const dim3 grid((unsigned)(s.tiles_m * s.tiles_n));
   const bool res = e.kind >= EPI_RESID;
-  const size_t align = res ? (size_t)e.x | (size_t)(e.ldx * 4) : (size_t)e.out | (size_t)(e.ldo * (e.bf16_out ? 2 : 4));
-  const int vec = align % (res || !e.bf16_out ? 16 : 8) == 0 && (size_t)e.xb % 8 == 0;
 #define T2I_I8(T, RES)                                                                                         \
-  hipLaunchKernelGGL((linear_i8_kernel<D, T, RES>), grid, dim3(D::NW * 64), 0, st, a, b, s, e, M, N, vec)
+  hipLaunchKernelGGL((linear_i8_kernel<D, T, RES>), grid, dim3(D::NW * 64), 0, st, a, b, s, e, M, N)
   if (e.bf16_out) {
     if (res) T2I_I8(bf16, true);
     else T2I_I8(bf16, false);
@@ -426,9 +425,8 @@ static void gated_fwd_launch(const GatedFwd& p, int M, int F, int K, hipStream_t
   const TileOperand a{(const char*)p.A, nullptr, (uint32_t)e * p.lda, M, 0},
       b{(const char*)p.Wg, (const char*)p.Wu, (uint32_t)e * p.ldw, F, 0};
   const TileShape s = tile_shape<D>(M, 2 * F, (K + per - 1) / per, e * K, 0);
-  const int vec = f32_pieces({F, p.ldo, p.pre ? p.ldp : 0}, {p.out, p.pre});
   hipLaunchKernelGGL((gated_linear_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64), 0, st, a,
-                     b, s, p, M, F, vec);
+                     b, s, p, M, F);
 }
 
 // Tile shape and slices of a gradient's product: as few slices as keep the time
@@ -466,10 +464,10 @@ size_t gated_split_floats(bool is_bf16, int M, int F, int K) {
 }
 
 template <typename T>
-static void split_sum(const Split& sp, int slices, long rows, long half, int cols, T* o0, T* o1, int ld, bool vec,
+static void split_sum(const Split& sp, int slices, long rows, long half, int cols, T* o0, T* o1, int ld,
                       hipStream_t st) {
   hipLaunchKernelGGL((split_sum_kernel<T>), dim3((unsigned)((rows * (sp.ld / 4) + 255) / 256)), dim3(256), 0, st,
-                     sp.partial, slices, rows, half, cols, sp.ld, o0, o1, ld, vec);
+                     sp.partial, slices, rows, half, cols, sp.ld, o0, o1, ld);
 }
 
 template <class D, typename T, bool U = false>
@@ -480,10 +478,9 @@ static void gated_dx_launch(int M, int F, int K, const void* dgu, const void* Wg
   const TileOperand a{(const char*)dgu, nullptr, 2u * e * Fp, M, 0},
       b{(const char*)Wg, (const char*)Wu, (uint32_t)e * ldw, F, K};
   const TileShape s = tile_shape<D>(M, K, 2 * Fp / per, 2 * e * Fp, Fp / per);
-  const bool vec = sizeof(T) == 2 || f32_pieces({K, ldx}, {dx});
   hipLaunchKernelGGL((gated_dx_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
-                     st, a, b, s, sp, dx, ldx, M, K, vec);
-  if (sp.partial) split_sum(sp, pick.slices, M, M, K, dx, dx, ldx, vec, st);
+                     st, a, b, s, sp, dx, ldx, M, K);
+  if (sp.partial) split_sum(sp, pick.slices, M, M, K, dx, dx, ldx, st);
 }
 
 template <class D, typename T, bool U = false>
@@ -497,10 +494,9 @@ static void gated_dw_launch(int M, int F, int K, const void* dgu, const void* A,
   TileShape s = tile_shape<D>(F, K, (M + per - 1) / per, 0, 0);
   const int half = s.tiles_m;
   s.tiles_m *= n;
-  const bool vec = sizeof(T) == 2 || f32_pieces({K, lddw}, {dWg, dWu});
   hipLaunchKernelGGL((gated_dw_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
-                     st, a, b, s, sp, half, e * Fp, first, dWu, lddw, F, K, vec);
-  if (sp.partial) split_sum(sp, pick.slices, (long)n * F, F, K, first, dWu, lddw, vec, st);
+                     st, a, b, s, sp, half, e * Fp, first, dWu, lddw, F, K);
+  if (sp.partial) split_sum(sp, pick.slices, (long)n * F, F, K, first, dWu, lddw, st);
 }
 
 hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& p, int M, int F, int K, hipStream_t st) {
