@@ -13,10 +13,10 @@ namespace t2i {
 // tiles or fewer, and in between what lies between.
 struct TileChoice { int bm, bn, per_cu; float alone, full, end; };
 struct TilePick { int shape; float us; };
-template <int N>
-static TilePick choose_tile(const TileChoice (&c)[N], long rows, long cols, int steps, float end_scale, int slices = 1) {
+static TilePick choose_tile(const TileChoice* c, int shapes, long rows, long cols, int steps, float end_scale,
+                            int slices = 1) {
   TilePick best{0, 0.f};
-  for (int i = 0; i < N; ++i) {
+  for (int i = 0; i < shapes; ++i) {
     const long tiles = ((rows + c[i].bm - 1) / c[i].bm) * ((cols + c[i].bn - 1) / c[i].bn) * slices;
     const long slots = 256L * c[i].per_cu, rest = tiles % slots;
     const float end = c[i].end * end_scale, more = rest <= 256 ? 0.f : (float)(rest - 256) / (float)(slots - 256);
@@ -78,11 +78,11 @@ __device__ __forceinline__ float i8_value(int acc, float sa, float sw, float b, 
 // waits and the epilogue (75 MB of stores, an exponential and a reciprocal per
 // output) take more than the products; 4096 x 4096 x 12288 168 us (2.45 POP/s).
 template <class D, typename T, bool RES>
-__global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a, TileOperand b, TileShape s,
+__global__ __launch_bounds__(D::THREADS, 1) void linear_i8_kernel(TileOperand a, TileOperand b, TileShape s,
                                                                   I8Epi e, int M, int N) {
   using P = TileProduct<D, ELEM_I8, false, false, false, false>;
-  constexpr int THREADS = D::NW * 64, NE = D::BM + (RES ? 3 : 2) * D::BN;
-  __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + NE * 4];
+  constexpr int THREADS = D::THREADS, NE = D::BM + (RES ? 3 : 2) * D::BN;
+  __shared__ __attribute__((aligned(1024))) char smem[D::KG * D::RING + NE * 4];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
   const int m0 = tm * D::BM, n0 = tn * D::BN;
@@ -96,10 +96,11 @@ __global__ __launch_bounds__(D::NW * 64, 1) void linear_i8_kernel(TileOperand a,
   Staged<NE, THREADS, decltype(value)> st;
   st.fetch(value);
   typename P::Acc acc[D::TM][D::TN];
-  P::run(smem, a, b, s, m0, n0, acc);
-  float* const ev = (float*)(smem + D::ST * D::STAGE);
+  const bool mine = P::run_groups(smem, a, b, s, m0, n0, acc);
+  float* const ev = (float*)(smem + D::KG * D::RING);
   st.put(ev);
   tile_barrier();
+  if (!mine) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
   const int mw = (wave / D::WGN) * D::WM, nw = (wave % D::WGN) * D::WN;
 #pragma unroll
@@ -146,11 +147,11 @@ constexpr TileElem elem_of() { return sizeof(T) == 4 ? ELEM_F32 : ELEM_BF16; }
 // us (1.0 - 1.1 PFLOP/s: 4.5 rounds of tiles in 5, 18 k steps each), 4096 x 10240 x 4096
 // 515 - 530 us, one row of 10240 x 4096 33 us (the weights at 5.1 TB/s, a copy's rate).
 template <class D, typename T, bool U>
-__global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand a, TileOperand b, TileShape s,
+__global__ __launch_bounds__(D::THREADS, 1) void gated_linear_kernel(TileOperand a, TileOperand b, TileShape s,
                                                                      GatedFwd p, int M, int F) {
   using P = TileProduct<D, elem_of<T>(), false, false, true, false, U>;
-  constexpr int THREADS = D::NW * 64, H = D::BN / 2, TH = D::TN / 2;
-  __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE + D::BN * 4];
+  constexpr int THREADS = D::THREADS, H = D::BN / 2, TH = D::TN / 2;
+  __shared__ __attribute__((aligned(1024))) char smem[D::KG * D::RING + D::BN * 4];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
   const int m0 = tm * D::BM, f0 = tn * H;
@@ -161,10 +162,11 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_linear_kernel(TileOperand
   Staged<D::BN, THREADS, decltype(value)> st;
   st.fetch(value);
   typename P::Acc acc[D::TM][D::TN];
-  P::run(smem, a, b, s, m0, f0, acc);
-  float* const ev = (float*)(smem + D::ST * D::STAGE);
+  const bool mine = P::run_groups(smem, a, b, s, m0, f0, acc);
+  float* const ev = (float*)(smem + D::KG * D::RING);
   st.put(ev);
   tile_barrier();
+  if (!mine) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
   const int mw = (wave / D::WGN) * D::WM, nw = (wave % D::WGN) * (D::WN / 2);
 #pragma unroll
@@ -248,10 +250,10 @@ __device__ __forceinline__ void take_slice(const Split& sp, TileShape& s) {
 }
 
 template <class D, typename T, bool U>
-__global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
+__global__ __launch_bounds__(D::THREADS, 1) void gated_dx_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
                                                                  T* dx, int ldx, int M, int K) {
   using P = TileProduct<D, elem_of<T>(), false, true, false, true, U>;
-  __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
+  __shared__ __attribute__((aligned(1024))) char smem[D::RING];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
   if (sp.partial) take_slice(sp, s);
@@ -267,11 +269,11 @@ __global__ __launch_bounds__(D::NW * 64, 1) void gated_dx_kernel(TileOperand a, 
 // row blocks [0, half) are the first output's, the others the second's (their
 // operand lies `shift` bytes further)
 template <class D, typename T, bool U>
-__global__ __launch_bounds__(D::NW * 64, 1) void gated_dw_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
+__global__ __launch_bounds__(D::THREADS, 1) void gated_dw_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
                                                                  int half, int shift, T* d0, T* d1, int ldw,
                                                                  int F, int K) {
   using P = TileProduct<D, elem_of<T>(), true, true, false, false, U>;
-  __shared__ __attribute__((aligned(1024))) char smem[D::ST * D::STAGE];
+  __shared__ __attribute__((aligned(1024))) char smem[D::RING];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
   if (sp.partial) take_slice(sp, s);
@@ -318,7 +320,7 @@ __global__ __launch_bounds__(256) void split_sum_kernel(const float* __restrict_
 // 128 with three.  Three stages on 64 and 32 rows, two workgroups per CU, beat four
 // where there are more than 256 tiles (gated 200 x 4608 x 1152 15.4 -> 11.2 us) and
 // lose where the weights of few rows stream from memory (1 x 10240 x 4096 33.5 and 36.3
-// us on 32 rows): Tile32 takes over there.
+// us on 32 rows).
 using Tile256 = TileDims<256, 256, 2, 4, 2>;
 using Tile128 = TileDims<128, 128, 2, 4, 2>;
 using Tile128d = TileDims<128, 128, 2, 4, 4>;
@@ -326,15 +328,22 @@ using Tile64 = TileDims<64, 128, 2, 4, 2>;
 using Tile64d = TileDims<64, 128, 2, 4, 3>;
 using Tile32 = TileDims<32, 128, 1, 4, 4>;
 using Tile32d = TileDims<32, 128, 1, 4, 3>;
+using Tile32k = TileDims<32, 64, 2, 2, 3, 2>;
+using Tile16k = TileDims<16, 32, 1, 1, 3, 4>;
 constexpr TileChoice kTiles[] = {{256, 256, 1, 1.60f, 1.60f, 13.f}, {128, 128, 2, 0.72f, 1.02f, 4.8f},
                                  {128, 128, 1, 0.55f, 0.55f, 5.f},  {64, 128, 3, 0.60f, 1.01f, 3.f},
-                                 {64, 128, 2, 0.48f, 1.00f, 2.85f}, {32, 128, 2, 0.44f, 0.78f, 2.f}};
-constexpr int kTile32 = 5;
-// the bf16 and 8-bit products' entry of T2I_TILES: the table's choice, but for one
-// block of rows whose weights stream from memory
+                                 {64, 128, 2, 0.48f, 1.00f, 2.85f}, {32, 128, 2, 0.44f, 0.78f, 2.f},
+                                 {32, 64, 2, 0.155f, 0.37f, 2.2f},  {16, 32, 2, 0.073f, 0.17f, 2.5f}};
+constexpr int kGradTiles = 6, kTile32 = 5, kTile32k = 6, kTile16k = 7, kStream = 8;
+// The products without slices (8-bit layer, gated forward) have two more shapes for few
+// tiles of a long contraction: groups of waves share the steps of a tile (us on Tile32
+// to Tile64d, Tile32k, Tile16k: 8 bits 4 x 775 x 7447 20.5, 10.9, 9; gated 5 x 976 x 8896
+// 35, 21, 11.7, 21 x 3984 x 6600 37, 23, -; 21 x 12976 x 2824 -, 13.4, 20.1.  Eight groups
+// of 16 x 32 leave no room for a second workgroup: 2464 columns 9.1 -> 8.2, 8512 17.0 ->
+// 18.9).  Tile32 takes one block of rows whose weights stream from memory.
 static int tile_index(long rows, long cols, int steps, float end_scale) {
-  const int shape = choose_tile(kTiles, rows, cols, steps, end_scale).shape;
-  return shape == kTile32 && rows <= 32 && cols > 128 * 128 ? kTile32 + 1 : shape;
+  const int shape = choose_tile(kTiles, steps < 4 ? kGradTiles : kGradTiles + 2, rows, cols, steps, end_scale).shape;
+  return shape >= kTile32 && rows <= 32 && cols > 128 * 128 ? kStream : shape;
 }
 
 // fp32: bound by the matrix cores (154 TFLOP/s: 1.7 us per step of 128 x 128), so that
@@ -347,10 +356,17 @@ static int tile_index(long rows, long cols, int steps, float end_scale) {
 // more, four stages 0.5 - 2); 517 x 2832 x 1152 38 and 32; 1024 x 9216 x 1152 160 and 174.
 using Tile64s = TileDims<64, 64, 2, 2, 2>;
 using Tile32s = TileDims<32, 64, 2, 2, 3>;
-#define T2I_F32_COSTS {128, 128, 1, 1.88f, 1.79f, 3.f}, {64, 64, 1, 0.605f, 0.455f, 0.9f}
-constexpr TileChoice kTilesF32[] = {T2I_F32_COSTS, {32, 64, 1, 0.404f, 0.25f, 0.7f}};
-// dW: a's fragments are turned in twos at least, which 16 rows per wave do not have
-constexpr TileChoice kTilesF32Dw[] = {T2I_F32_COSTS};
+constexpr TileChoice kTilesF32[] = {{128, 128, 1, 1.88f, 1.79f, 3.f}, {64, 64, 1, 0.605f, 0.455f, 0.9f},
+                                    {32, 64, 1, 0.404f, 0.25f, 0.7f}, {32, 64, 1, 0.32f, 0.25f, 1.2f},
+                                    {16, 32, 2, 0.10f, 0.18f, 3.f}};
+// dW: a's fragments are turned in twos at least, which 16 rows per wave do not have.
+// The last two, with groups of waves, for the gated forward: a step of 16 x 32 is 16
+// MFMAs instead of 64 of the CU (23 x 9238 x 2385 32.9 us on 32 x 64, 25.6 with two
+// groups; 1 x 4608 x 7496 80, 69 and 26 on 16 x 32; 82 x 4512 x 1792 22, 19, 23).
+constexpr int kF32DwTiles = 2, kF32DxTiles = 3, kF32Groups = 3;
+static int tile_index_f32(long rows, long cols, int steps) {
+  return choose_tile(kTilesF32, steps < 4 ? kF32Groups : kF32Groups + 2, rows, cols, steps, 0.5f).shape;
+}
 constexpr int kMaxSlices = 16;
 
 // group_m 8: eight row blocks share a column block's operand in an XCD's L2
@@ -373,7 +389,7 @@ static void i8_launch(const TileOperand& a, const TileOperand& b, const I8Epi& e
   const dim3 grid((unsigned)(s.tiles_m * s.tiles_n));
   const bool res = e.kind >= EPI_RESID;
 #define T2I_I8(T, RES)                                                                                         \
-  hipLaunchKernelGGL((linear_i8_kernel<D, T, RES>), grid, dim3(D::NW * 64), 0, st, a, b, s, e, M, N)
+  hipLaunchKernelGGL((linear_i8_kernel<D, T, RES>), grid, dim3(D::THREADS), 0, st, a, b, s, e, M, N)
   if (e.bf16_out) {
     if (res) T2I_I8(bf16, true);
     else T2I_I8(bf16, false);
@@ -384,21 +400,28 @@ static void i8_launch(const TileOperand& a, const TileOperand& b, const I8Epi& e
 #undef T2I_I8
 }
 
-#define T2I_TILES(SHAPE, CALL)                   \
-  switch (SHAPE) {                               \
-    case 0: { using D = Tile256; CALL; break; }  \
-    case 1: { using D = Tile128; CALL; break; }  \
-    case 2: { using D = Tile128d; CALL; break; } \
-    case 3: { using D = Tile64; CALL; break; }   \
-    case 4: { using D = Tile64d; CALL; break; }  \
-    case 5: { using D = Tile32d; CALL; break; }  \
-    default: { using D = Tile32; CALL; break; }  \
+#define T2I_TILES(SHAPE, CALL)                    \
+  switch (SHAPE) {                                \
+    case 0: { using D = Tile256; CALL; break; }   \
+    case 1: { using D = Tile128; CALL; break; }   \
+    case 2: { using D = Tile128d; CALL; break; }  \
+    case 3: { using D = Tile64; CALL; break; }    \
+    case 4: { using D = Tile64d; CALL; break; }   \
+    default: { using D = Tile32d; CALL; break; }  \
+  }
+#define T2I_TILES_FWD(SHAPE, CALL)                        \
+  switch (SHAPE) {                                        \
+    case kTile32k: { using D = Tile32k; CALL; break; }    \
+    case kTile16k: { using D = Tile16k; CALL; break; }    \
+    case kStream: { using D = Tile32; CALL; break; }      \
+    default: T2I_TILES(SHAPE, CALL)                       \
   }
 
 hipError_t launch_linear_i8(const int8_t* A, int lda, const int8_t* W, int ldw, int M, int N, int K,
                             const I8Epi& e, hipStream_t st) {
   const TileOperand a{(const char*)A, nullptr, (uint32_t)lda, M, 0}, b{(const char*)W, nullptr, (uint32_t)ldw, N, 0};
-  T2I_TILES(tile_index(M, N, i8_row(K) / 128, 1.f), i8_launch<D>(a, b, e, M, N, K, st))
+  const int shape = tile_index(M, N, i8_row(K) / 128, 1.f);
+  T2I_TILES_FWD(shape, i8_launch<D>(a, b, e, M, N, K, st))
   return hipGetLastError();
 }
 
@@ -407,9 +430,17 @@ hipError_t launch_linear_i8(const int8_t* A, int lda, const int8_t* W, int ldw, 
     case 0: { using D = Tile128; CALL; break; }  \
     default: { using D = Tile64s; CALL; break; } \
   }
-#define T2I_TILES_F32(SHAPE, CALL)                \
-  if (SHAPE == 2) { using D = Tile32s; CALL; }    \
-  else { T2I_TILES_F32_DW(SHAPE, CALL) }
+#define T2I_TILES_F32_DX(SHAPE, CALL)            \
+  switch (SHAPE) {                               \
+    case 2: { using D = Tile32s; CALL; break; }  \
+    default: T2I_TILES_F32_DW(SHAPE, CALL)       \
+  }
+#define T2I_TILES_F32_FWD(SHAPE, CALL)                       \
+  switch (SHAPE) {                                           \
+    case kF32Groups: { using D = Tile32k; CALL; break; }     \
+    case kF32Groups + 1: { using D = Tile16k; CALL; break; } \
+    default: T2I_TILES_F32_DX(SHAPE, CALL)                   \
+  }
 
 // whether these sizes and strides of fp32 values, and pointers, are whole 16-byte pieces
 static bool f32_pieces(std::initializer_list<int> sizes, std::initializer_list<const void*> ptrs) {
@@ -425,7 +456,7 @@ static void gated_fwd_launch(const GatedFwd& p, int M, int F, int K, hipStream_t
   const TileOperand a{(const char*)p.A, nullptr, (uint32_t)e * p.lda, M, 0},
       b{(const char*)p.Wg, (const char*)p.Wu, (uint32_t)e * p.ldw, F, 0};
   const TileShape s = tile_shape<D>(M, 2 * F, (K + per - 1) / per, e * K, 0);
-  hipLaunchKernelGGL((gated_linear_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::NW * 64), 0, st, a,
+  hipLaunchKernelGGL((gated_linear_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n)), dim3(D::THREADS), 0, st, a,
                      b, s, p, M, F);
 }
 
@@ -433,14 +464,13 @@ static void gated_fwd_launch(const GatedFwd& p, int M, int F, int K, hipStream_t
 // least, counting 4 us for the second launch and the partial sums' way out and back
 // at 4 TB/s (1024 x 9216 x 1152: 63 us on 144 64 x 128 tiles, 41 in slices).
 struct SplitPick { int shape, slices, per; };
-template <int N>
-static SplitPick choose_split(const TileChoice (&tiles)[N], long rows, long cols, int steps) {
+static SplitPick choose_split(const TileChoice* tiles, int shapes, long rows, long cols, int steps) {
   SplitPick best{0, 1, steps};
   float least = 0.f;
   for (int n = 1; n <= kMaxSlices; ++n) {
     const int per = (steps + n - 1) / n, slices = (steps + per - 1) / per;
     if (slices != n || (n > 1 && per < 4)) continue;
-    const TilePick p = choose_tile(tiles, rows, cols, per, n > 1 ? 2.f : 1.f, n);
+    const TilePick p = choose_tile(tiles, shapes, rows, cols, per, n > 1 ? 2.f : 1.f, n);
     const float us = p.us + (n > 1 ? 4.f + (float)n * rows * cols * 8 / 4e6f : 0.f);
     if (n == 1 || us < least) least = us, best = {p.shape, n, per};
   }
@@ -449,10 +479,12 @@ static SplitPick choose_split(const TileChoice (&tiles)[N], long rows, long cols
 
 static long whole4(long cols) { return (cols + 3) / 4 * 4; }
 static SplitPick split_dx(bool is_bf16, long rows, long cols, int k) {
-  return is_bf16 ? choose_split(kTiles, rows, cols, (k + 63) / 64) : choose_split(kTilesF32, rows, cols, (k + 31) / 32);
+  return is_bf16 ? choose_split(kTiles, kGradTiles, rows, cols, (k + 63) / 64)
+                 : choose_split(kTilesF32, kF32DxTiles, rows, cols, (k + 31) / 32);
 }
 static SplitPick split_dw(bool is_bf16, long rows, long cols, int k) {
-  return is_bf16 ? choose_split(kTiles, rows, cols, (k + 63) / 64) : choose_split(kTilesF32Dw, rows, cols, (k + 31) / 32);
+  return is_bf16 ? choose_split(kTiles, kGradTiles, rows, cols, (k + 63) / 64)
+                 : choose_split(kTilesF32, kF32DwTiles, rows, cols, (k + 31) / 32);
 }
 
 size_t gated_split_floats(bool is_bf16, int M, int F, int K) {
@@ -478,7 +510,7 @@ static void gated_dx_launch(int M, int F, int K, const void* dgu, const void* Wg
   const TileOperand a{(const char*)dgu, nullptr, 2u * e * Fp, M, 0},
       b{(const char*)Wg, (const char*)Wu, (uint32_t)e * ldw, F, K};
   const TileShape s = tile_shape<D>(M, K, 2 * Fp / per, 2 * e * Fp, Fp / per);
-  hipLaunchKernelGGL((gated_dx_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
+  hipLaunchKernelGGL((gated_dx_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::THREADS), 0,
                      st, a, b, s, sp, dx, ldx, M, K);
   if (sp.partial) split_sum(sp, pick.slices, M, M, K, dx, dx, ldx, st);
 }
@@ -494,19 +526,20 @@ static void gated_dw_launch(int M, int F, int K, const void* dgu, const void* A,
   TileShape s = tile_shape<D>(F, K, (M + per - 1) / per, 0, 0);
   const int half = s.tiles_m;
   s.tiles_m *= n;
-  hipLaunchKernelGGL((gated_dw_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::NW * 64), 0,
+  hipLaunchKernelGGL((gated_dw_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::THREADS), 0,
                      st, a, b, s, sp, half, e * Fp, first, dWu, lddw, F, K);
   if (sp.partial) split_sum(sp, pick.slices, (long)n * F, F, K, first, dWu, lddw, st);
 }
 
 hipError_t launch_gated_linear(bool is_bf16, const GatedFwd& p, int M, int F, int K, hipStream_t st) {
-  const TilePick f32 = choose_tile(kTilesF32, M, 2L * F, (K + 31) / 32, 0.5f);
-  if (is_bf16)
-    T2I_TILES(tile_index(M, 2L * F, (K + 63) / 64, 0.5f), (gated_fwd_launch<D, bf16>(p, M, F, K, st)))
-  else if (f32_pieces({K, p.lda, p.ldw}, {p.A, p.Wg, p.Wu}))
-    T2I_TILES_F32(f32.shape, (gated_fwd_launch<D, float>(p, M, F, K, st)))
-  else
-    T2I_TILES_F32(f32.shape, (gated_fwd_launch<D, float, true>(p, M, F, K, st)))
+  const int shape = is_bf16 ? tile_index(M, 2L * F, (K + 63) / 64, 0.5f) : tile_index_f32(M, 2L * F, (K + 31) / 32);
+  if (is_bf16) {
+    T2I_TILES_FWD(shape, (gated_fwd_launch<D, bf16>(p, M, F, K, st)))
+  } else if (f32_pieces({K, p.lda, p.ldw}, {p.A, p.Wg, p.Wu})) {
+    T2I_TILES_F32_FWD(shape, (gated_fwd_launch<D, float>(p, M, F, K, st)))
+  } else {
+    T2I_TILES_F32_FWD(shape, (gated_fwd_launch<D, float, true>(p, M, F, K, st)))
+  }
   return hipGetLastError();
 }
 
@@ -517,9 +550,9 @@ hipError_t launch_gated_dx(bool is_bf16, int M, int F, int K, const void* dgu, c
   if (is_bf16) {
     T2I_TILES(pick.shape, (gated_dx_launch<D, bf16>(M, F, K, dgu, Wg, Wu, ldw, (bf16*)dx, ldx, pick, sp, st)))
   } else if (f32_pieces({K, ldw}, {Wg, Wu})) {
-    T2I_TILES_F32(pick.shape, (gated_dx_launch<D, float>(M, F, K, dgu, Wg, Wu, ldw, (float*)dx, ldx, pick, sp, st)))
+    T2I_TILES_F32_DX(pick.shape, (gated_dx_launch<D, float>(M, F, K, dgu, Wg, Wu, ldw, (float*)dx, ldx, pick, sp, st)))
   } else {
-    T2I_TILES_F32(pick.shape,
+    T2I_TILES_F32_DX(pick.shape,
                   (gated_dx_launch<D, float, true>(M, F, K, dgu, Wg, Wu, ldw, (float*)dx, ldx, pick, sp, st)))
   }
   return hipGetLastError();
@@ -543,22 +576,23 @@ hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, c
   return hipGetLastError();
 }
 
-// The tile and the slices that a product takes (op 0: 8-bit layer with F columns, 1:
+// The tile and the slices (or groups of waves) that a product takes (op 0: 8-bit layer with F columns, 1:
 // gated forward, 2: dx, 3: dWg and dWu)
 extern "C" int t2i_test_block_tile(int op, int is_bf16, int M, int F, int K, int* rows, int* columns, int* per_cu,
                                    int* slices) {
   if (M < 1 || F < 1 || K < 1 || op < 0 || op > 3) return 0;
   SplitPick p{0, 1, 0};
+  const bool f32 = op != 0 && !is_bf16;
   if (op == 0) p.shape = tile_index(M, F, i8_row(K) / 128, 1.f);
-  else if (op == 1) p.shape = is_bf16 ? tile_index(M, 2L * F, (K + 63) / 64, 0.5f)
-                                      : choose_tile(kTilesF32, M, 2L * F, (K + 31) / 32, 0.5f).shape;
+  else if (op == 1) p.shape = f32 ? tile_index_f32(M, 2L * F, (K + 31) / 32) : tile_index(M, 2L * F, (K + 63) / 64, 0.5f);
   else p = op == 2 ? split_dx(is_bf16, M, K, 2 * gated_cols(F)) : split_dw(is_bf16, 2L * F, K, M);
-  const bool stream = (op == 0 || is_bf16) && p.shape > kTile32;   // four stages, one workgroup per CU
-  const TileChoice& c = stream ? kTiles[kTile32] : op == 0 || is_bf16 ? kTiles[p.shape] : kTilesF32[p.shape];
+  const bool stream = !f32 && p.shape == kStream;   // four stages, one workgroup per CU
+  const TileChoice& c = f32 ? kTilesF32[p.shape] : kTiles[stream ? kTile32 : p.shape];
   *rows = c.bm;
   *columns = c.bn;
   *per_cu = stream ? 1 : c.per_cu;
-  *slices = p.slices;
+  const int group = p.shape - (f32 ? kF32Groups : kTile32k);
+  *slices = op > 1 ? p.slices : group == 0 ? Tile32k::KG : group == 1 ? Tile16k::KG : 1;
   return 1;
 }
 

@@ -47,6 +47,10 @@
 // per lane, four times the instructions, where a piece would reach past a row's end:
 // KC in the last step, KR in a tile that is wider than the matrix.
 //
+// Few tiles of a long contraction leave most CUs idle and each busy one waiting for its
+// own loads: there KG groups of waves share a tile, each with a slice of the steps and
+// a ring of its own, and the groups' sums are added through LDS in a fixed order.
+//
 // Sizes: tile rows behind the operand's last are read as that row (KC), columns as
 // its last ones (KR): what comes of them is not stored.  k behind the end is read as
 // zeros (KC: by an offset behind the resource, KR: by the resource's bound) and
@@ -127,11 +131,13 @@ __device__ __forceinline__ void tile_place(const TileShape& s, int block, int bl
 
 constexpr uint32_t kTileOff = 0x80000000u;   // behind every resource: reads as zero
 
-template <int BM_, int BN_, int WGM_, int WGN_, int ST_>
+// KG groups of WGM x WGN waves share a tile, each with a slice of the contraction and
+// a ring of its own
+template <int BM_, int BN_, int WGM_, int WGN_, int ST_, int KG_ = 1>
 struct TileDims {
-  static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, ST = ST_;
+  static constexpr int BM = BM_, BN = BN_, WGM = WGM_, WGN = WGN_, ST = ST_, KG = KG_;
   static constexpr int NW = WGM * WGN, WM = BM / WGM, WN = BN / WGN, TM = WM / 16, TN = WN / 16;
-  static constexpr int STAGE = (BM + BN) * 128;
+  static constexpr int STAGE = (BM + BN) * 128, RING = ST * STAGE, THREADS = KG * NW * 64;
   static constexpr int LOADS = (BM + BN) / 8 / NW;   // load instructions per wave and step
   static_assert((BM + BN) / 8 % NW == 0 && BM / 8 % NW == 0, "whole load rounds per operand");
   static_assert(WM % 16 == 0 && WN % 16 == 0 && ST >= 2 && ST <= 5 && (ST - 1) * LOADS < 64, "tile shape");
@@ -180,7 +186,7 @@ struct TileProduct {
   static __device__ __forceinline__ void run(char* smem, const TileOperand& a, const TileOperand& b,
                                              const TileShape& s, int m0, int n0, Acc (&acc)[TM][TN]) {
     const int tid = threadIdx.x, lane = tid & 63;
-    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int wave = __builtin_amdgcn_readfirstlane((tid >> 6) % D::NW);
     const int wm = wave / D::WGN, wn = wave % D::WGN, fr = lane & 15, g = lane >> 4;
     constexpr int LA = BM / 8 / D::NW;
     const int KT = s.steps;
@@ -209,7 +215,7 @@ struct TileProduct {
     uint32_t src[LOADS];
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) src[i] = source(i < LA, at_of(i), 16);
-    const bool ragged_k = !I8 && s.kbytes % 128 != 0;   // KC: places of the last step lie behind k
+    const bool ragged_k = !I8 && (s.first + s.steps) * 128 > s.kbytes;   // KC: places of the last step lie behind k
     // KC: rows at fixed offsets from the tile's first, k as the scalar offset.
     // KR: the step's first row as the base, the resource ends with its last row.
     auto kc_res = [](const char* p, size_t off) {
@@ -399,6 +405,42 @@ struct TileProduct {
     half0(slot);
 #pragma unroll
     for (int j = S; j < TN; ++j) column(j, a1);
+  }
+
+  // the same by KG groups of waves; the sum, in ascending group order, is the first
+  // group's.  Returns whether this wave is of that group (the others have no outputs).
+  static __device__ __forceinline__ bool run_groups(char* smem, const TileOperand& a, const TileOperand& b, TileShape s,
+                                                    int m0, int n0, Acc (&acc)[TM][TN]) {
+    if constexpr (D::KG == 1) {
+      run(smem, a, b, s, m0, n0, acc);
+      return true;
+    } else {
+      const int kg = __builtin_amdgcn_readfirstlane((int)threadIdx.x / (D::NW * 64)), t = threadIdx.x % (D::NW * 64);
+      const int total = s.steps, per = (total + D::KG - 1) / D::KG;
+      s.first = kg * total / D::KG;
+      s.steps = (kg + 1) * total / D::KG - s.first;
+      run(smem + kg * D::RING, a, b, s, m0, n0, acc);
+      // (every group meets as often: slices differ by a step)
+      for (int x = s.steps; x < per; ++x) tile_barrier();
+      tile_barrier();
+      Acc* const part = (Acc*)smem + t;
+      if (kg > 0) {
+#pragma unroll
+        for (int i = 0; i < TM; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) part[(((kg - 1) * TM + i) * TN + j) * D::NW * 64] = acc[i][j];
+      }
+      tile_barrier();
+      if (kg == 0) {
+#pragma unroll
+        for (int x = 0; x < D::KG - 1; ++x)
+#pragma unroll
+          for (int i = 0; i < TM; ++i)
+#pragma unroll
+            for (int j = 0; j < TN; ++j) acc[i][j] += part[((x * TM + i) * TN + j) * D::NW * 64];
+      }
+      return kg == 0;
+    }
   }
 };
 

@@ -445,7 +445,7 @@ def test_gated_not_finite_values_stay_where_they_belong():
 # ------------------------------------------------------------------ every tile, long rows
 
 def tile_of(op, dtype, M, F, K):
-    """(rows, columns, workgroups per CU, slices) that a product takes"""
+    """(rows, columns, workgroups per CU, slices or groups of waves) that a product takes"""
     v = [C.c_int() for _ in range(4)]
     assert t2i.load().t2i_test_block_tile(op, int(dtype == BF16), M, F, K, *map(C.byref, v))
     return tuple(x.value for x in v)
@@ -460,9 +460,10 @@ def some(n, seed):
 @pytest.mark.parametrize("M,N,K,tile", [
     (20, 72, 72, (32, 128, 2)), (30, 16500, 72, (32, 128, 1)), (8200, 136, 72, (64, 128, 2)),
     (8200, 520, 72, (64, 128, 3)), (8200, 264, 2056, (128, 128, 1)), (8200, 520, 2056, (128, 128, 2)),
-    (4090, 4090, 4104, (256, 256, 1))])
+    (4090, 4090, 4104, (256, 256, 1)), (17, 72, 521, (16, 32, 2, 4)), (33, 3000, 650, (16, 32, 2, 4)),
+    (1, 41, 7447, (16, 32, 2, 4)), (200, 1033, 650, (32, 64, 2, 2)), (130, 2056, 1100, (32, 64, 2, 2))])
 def test_linear_i8_on_every_tile(M, N, K, tile):
-    assert tile_of(0, BF16, M, N, K) == (*tile, 1)
+    assert tile_of(0, BF16, M, N, K) == (*tile, 1)[:4]
     a, sa, w, sw = i8_operands(M, N, K, 120)
     d = [dev(v, torch.int8) if v.dtype == np.int8 else dev(v) for v in (a, sa, w, sw)]
     b, rb = rnd(121, (N,), 0.3, BF16)
@@ -489,9 +490,13 @@ def test_linear_i8_on_every_tile(M, N, K, tile):
     (8200, 136, 72, BF16, (64, 128, 3)), (8200, 136, 520, BF16, (128, 128, 1)),
     (8200, 264, 520, BF16, (128, 128, 2)), (8200, 520, 2056, BF16, (256, 256, 1)),
     (300, 200, 72, F32, (32, 64, 1)), (300, 199, 71, F32, (32, 64, 1)), (8200, 1032, 72, F32, (64, 64, 1)), (8200, 1031, 71, F32, (64, 64, 1)),
-    (1032, 1544, 72, F32, (128, 128, 1)), (1032, 1543, 71, F32, (128, 128, 1))])
+    (1032, 1544, 72, F32, (128, 128, 1)), (1032, 1543, 71, F32, (128, 128, 1)),
+    (17, 40, 264, BF16, (16, 32, 2, 4)), (1, 72, 2056, BF16, (16, 32, 2, 4)), (33, 520, 328, BF16, (16, 32, 2, 4)),
+    (200, 520, 264, BF16, (32, 64, 2, 2)), (70, 4104, 328, BF16, (32, 64, 2, 2)),
+    (5, 41, 131, F32, (16, 32, 2, 4)), (17, 40, 164, F32, (16, 32, 2, 4)), (40, 521, 2049, F32, (16, 32, 2, 4)),
+    (130, 1032, 264, F32, (32, 64, 1, 2)), (130, 1033, 299, F32, (32, 64, 1, 2))])
 def test_gated_linear_on_every_tile(M, F, K, dtype, tile):
-    assert tile_of(1, dtype, M, F, K) == (*tile, 1)
+    assert tile_of(1, dtype, M, F, K) == (*tile, 1)[:4]
     d, h = gated_case(M, F, K, dtype, True, 130)
     out, pre = t2i.gated_linear(*d.values(), act="silu", save_pre=True)
     i = some(M, 2)
