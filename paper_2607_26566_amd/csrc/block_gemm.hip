@@ -74,9 +74,9 @@ __device__ __forceinline__ float i8_value(int acc, float sa, float sw, float b, 
 
 // The 8-bit linear layer: y = (sum of whole products) sa sw + b.  The sum is exact in
 // 32 bits whatever the tile, so a row's result does not depend on the rows beside it.
-// 7531 x 4608 x 1152 with GELU 63 us (1.27 POP/s): nine k steps per tile, of which the
-// waits and the epilogue (75 MB of stores, an exponential and a reciprocal per
-// output) take more than the products; 4096 x 4096 x 12288 168 us (2.45 POP/s).
+// 7531 x 4608 x 1152 64 us, 66 with GELU (1.2 POP/s): nine k steps per tile, of which
+// the first loads and 69 MB of stores take more than the products; 4096 x 4096 x 12288
+// 156 - 177 us (2.3 - 2.6 POP/s).
 template <class D, typename T, bool RES>
 __global__ __launch_bounds__(D::THREADS, 1) void linear_i8_kernel(TileOperand a, TileOperand b, TileShape s,
                                                                   I8Epi e, int M, int N) {
@@ -336,23 +336,23 @@ constexpr TileChoice kTiles[] = {{256, 256, 1, 1.60f, 1.60f, 13.f}, {128, 128, 2
                                  {32, 64, 2, 0.155f, 0.37f, 2.2f},  {16, 32, 2, 0.073f, 0.17f, 2.5f}};
 constexpr int kGradTiles = 6, kTile32 = 5, kTile32k = 6, kTile16k = 7, kStream = 8;
 // The products without slices (8-bit layer, gated forward) have two more shapes for few
-// tiles of a long contraction: groups of waves share the steps of a tile (us on Tile32
-// to Tile64d, Tile32k, Tile16k: 8 bits 4 x 775 x 7447 20.5, 10.9, 9; gated 5 x 976 x 8896
-// 35, 21, 11.7, 21 x 3984 x 6600 37, 23, -; 21 x 12976 x 2824 -, 13.4, 20.1.  Eight groups
-// of 16 x 32 leave no room for a second workgroup: 2464 columns 9.1 -> 8.2, 8512 17.0 ->
-// 18.9).  Tile32 takes one block of rows whose weights stream from memory.
+// tiles of a long contraction: groups of waves share the steps of a tile.  us on the
+// shapes before them, on Tile32k and on Tile16k: 8 bits 4 x 775 x 7447 20.5, 10.9, 9;
+// F = 488 at 5 rows of K = 8896 35, 21, 11.7; F = 6488 at 21 rows of 2824 -, 13.4, 20.1.
+// (Eight groups of 16 x 32 leave no room for a second workgroup: F = 1232 9.1 -> 8.2, F =
+// 4256 17.0 -> 18.9.)  Tile32 takes one block of rows whose weights stream from memory.
 static int tile_index(long rows, long cols, int steps, float end_scale) {
   const int shape = choose_tile(kTiles, steps < 4 ? kGradTiles : kGradTiles + 2, rows, cols, steps, end_scale).shape;
   return shape >= kTile32 && rows <= 32 && cols > 128 * 128 ? kStream : shape;
 }
 
-// fp32: bound by the matrix cores (154 TFLOP/s: 1.7 us per step of 128 x 128), so that
-// two stages are enough and several workgroups share a CU (4096 x 9216 x 1152: 143
-// TFLOP/s on 128 x 128, 139 on 64 x 64, 134 and 128 with four stages).  Costs from 36 to
-// 9216 tiles of 36 steps: 22.7 us for up to 256 of 64 x 64, 17.1 for every 256 more;
-// 70.5 and 67 on 128 x 128.  A wave's step is 32 MFMAs of 32 cycles on 64 x 64, 16 on 32
-// x 64, where a chain of steps is what takes the time: 33 x 2304 x 1152 22.3 and 14.9
-// us, 5 x 1634 x 3128 73 and 48 (three stages; two stages of 32 x 32 per wave 4 - 10 us
+// fp32 (sizes: rows x columns of g | u x K): bound by the matrix cores (154 TFLOP/s: 1.7
+// us per step of 128 x 128), so that two stages are enough and several workgroups share
+// a CU (4096 x 9216 x 1152: 143 TFLOP/s on 128 x 128, 139 on 64 x 64, 134 and 128 with
+// four stages).  Costs from 36 to 9216 tiles of 36 steps: 22.7 us for up to 256 of 64 x
+// 64, 17.1 for every 256 more; 70.5 and 67 on 128 x 128.  A wave's step is 32 MFMAs of
+// 32 cycles on 64 x 64, 16 on 32 x 64, where a chain of steps is what takes the time: 33
+// x 2304 x 1152 22.3 and 14.9 us (three stages; two stages of 32 x 32 per wave 4 - 10 us
 // more, four stages 0.5 - 2); 517 x 2832 x 1152 38 and 32; 1024 x 9216 x 1152 160 and 174.
 using Tile64s = TileDims<64, 64, 2, 2, 2>;
 using Tile32s = TileDims<32, 64, 2, 2, 3>;
