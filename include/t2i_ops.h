@@ -211,9 +211,10 @@ t2i_status t2i_op_linear_i8(int32_t dtype, int32_t epilogue, int32_t M, int32_t 
  *   t2i_op_gated_linear_backward reads (fp32 for bf16 operands too: rounded to
  *   bf16 they would add a quarter to the gradients' error).
  *   bf16: F, K and the strides % 8 == 0 (ldp % 4), every pointer 16-byte
- *   aligned.  fp32: any sizes (F, K, strides % 4 == 0 and 16-byte aligned
- *   pointers are faster).  Rows of A, Wg and Wu less than 8 MiB apart, fewer than
- *   2^23 pieces of 64 x 64 values in g | u (backward: dA, dWg | dWu as well).
+ *   aligned.  fp32: any sizes, strides and alignment (A, Wg and Wu in whole 16-byte
+ *   rows are some percent faster, same results).  Rows of A, Wg and Wu less than 8
+ *   MiB apart, fewer than 2^23 pieces of 64 x 64 values in g | u (backward: dA, dWg |
+ *   dWu as well).
  * No output may overlap an input.
  */
 t2i_status t2i_op_gated_linear(int32_t dtype, int32_t act, int32_t M, int32_t F, int32_t K,

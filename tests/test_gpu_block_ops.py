@@ -564,6 +564,32 @@ def test_gated_gradients_on_every_tile(op, M, F, K, dtype, tile):
         assert rel_l2(to_host(t[it]), ref) < (2.0 ** -7 if dtype == BF16 else 2.0 ** -17)
 
 
+@pytest.mark.parametrize("M,F,K", [(5, 40, 37), (33, 130, 70), (70, 129, 132), (200, 1032, 264), (130, 72, 513),
+                                   (1030, 300, 203), (1032, 1544, 72)])
+@pytest.mark.parametrize("at", [1, 2, 3])
+def test_gated_f32_rows_at_any_address(M, F, K, at):
+    """Operands cut out of wider matrices of NaN, off 16 bytes: the contiguous operands'
+    results bit for bit (the same sums in the same order)."""
+    say("any address", M, F, K, at)
+    d, _ = gated_case(M, F, K, F32, True, 160)
+    dout, _ = rnd(161, (M, F))
+
+    def cut(t):
+        wide = torch.full((t.shape[0], t.shape[1] + 5), float("nan"), device=DEV)
+        v = wide[:, at:at + t.shape[1]]
+        v.copy_(t)
+        return v
+
+    def both(x, wg, wu, dh):
+        h, pre = t2i.gated_linear(x, wg, wu, d["bg"], d["bu"], act="gelu", save_pre=True)
+        return [h, pre, *t2i.gated_linear_backward(dh, x, wg, wu, pre, act="gelu", bias=True)]
+
+    a = both(d["x"], d["wg"], d["wu"], dout)
+    b = both(cut(d["x"]), cut(d["wg"]), cut(d["wu"]), cut(dout))
+    for n, u, v in zip(("h", "pre", "dx", "dwg", "dwu", "dbg", "dbu"), a, b):
+        assert torch.isfinite(u).all() and torch.equal(u, v), n
+
+
 def test_rows_far_apart():
     """Offsets past 32 bits: rows just below 8 MiB apart in tensors of more than 2 GiB."""
     M, F, K, wide = 300, 264, 72, 2 ** 22 - 8
