@@ -170,8 +170,7 @@ t2i_status t2i_op_lora_merge_batch(int32_t dtype, int32_t n, int32_t n_out, int3
  *              (of the exact quotient; -127 .. 127).
  * A row that holds a NaN or an infinity gets scale NaN and q = 0.
  *   x [rows, K] of dtype (bf16 or fp32), row stride ldx >= K, any alignment of
- *   its type (16-byte aligned rows are read in whole pieces: same results,
- *   less time); q [rows, ldq] with ldq % 16 == 0, ldq >= K rounded up to a
+ *   its type; q [rows, ldq] with ldq % 16 == 0, ldq >= K rounded up to a
  *   multiple of 128, 16-byte aligned: columns K .. that multiple are written
  *   as zeros, columns behind it are left alone; scale [rows] fp32.  Fewer than
  *   2^26 - 4 rows (K > 2048: 2^24 - 4).

@@ -68,16 +68,18 @@ __device__ __forceinline__ int quant1(float x, float s, float inv) {
   return (int)n;
 }
 
-// eight elements of a row as they lie in memory, and the largest of their
-// magnitudes' bits (which order as the magnitudes do, infinity and NaN above)
+// eight elements of a row as they lie in memory (at any address: one or two loads all
+// the same), and the largest of their magnitudes' bits (which order as the magnitudes
+// do, infinity and NaN above)
 template <typename T>
 struct Piece;
 template <>
 struct Piece<bf16> {
   uint32_t w[4];
   __device__ __forceinline__ void load(const bf16* p) {
-    const uint4 v = *(const uint4*)p;
-    w[0] = v.x, w[1] = v.y, w[2] = v.z, w[3] = v.w;
+    typedef uint32_t any4 __attribute__((ext_vector_type(4), aligned(2)));
+    const any4 v = *(const any4*)p;
+    w[0] = v[0], w[1] = v[1], w[2] = v[2], w[3] = v[3];
   }
   __device__ __forceinline__ void set(int i, bf16 v) {
     const uint32_t b = __builtin_bit_cast(uint16_t, v);
@@ -101,7 +103,12 @@ struct Piece<bf16> {
 template <>
 struct Piece<float> {
   float v[8];
-  __device__ __forceinline__ void load(const float* p) { load8(p, v); }
+  __device__ __forceinline__ void load(const float* p) {
+    typedef float any4 __attribute__((ext_vector_type(4), aligned(4)));
+    const any4 a = *(const any4*)p, b = *(const any4*)(p + 4);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) v[i] = a[i], v[4 + i] = b[i];
+  }
   __device__ __forceinline__ void set(int i, float x) { v[i] = x; }
   __device__ __forceinline__ void clear() {
 #pragma unroll
@@ -117,8 +124,8 @@ struct Piece<float> {
 };
 
 // TPR threads per row, NV pieces per thread in registers; longer rows read their
-// pieces again.  VEC: rows start at multiples of 16 bytes.
-template <typename T, int TPR, int NV, bool VEC>
+// pieces again.
+template <typename T, int TPR, int NV>
 __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x, int ldx, int rows,
                                                          int K, int8_t* __restrict__ q, int ldq,
                                                          float* __restrict__ scale) {
@@ -131,7 +138,7 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x
   Piece<T> v[NV];
   auto load = [&](int c, Piece<T>& p) {
     const int k = c * 8;
-    if (VEC && k + 8 <= K) {
+    if (k + 8 <= K) {
       p.load(xr + k);
     } else {
       p.clear();
@@ -200,26 +207,18 @@ __global__ __launch_bounds__(256) void quant_rows_kernel(const T* __restrict__ x
 
 template <typename T>
 static void quant_rows_any(int rows, int K, const T* x, int ldx, int8_t* q, int ldq, float* scale, hipStream_t st) {
-  const bool vec = (uintptr_t)x % 16 == 0 && ldx * sizeof(T) % 16 == 0;
-#define T2I_Q(TPR, NV)                                                                                          \
-  {                                                                                                            \
-    const dim3 grid((unsigned)((rows + 256L / TPR - 1) / (256 / TPR)));                                         \
-    if (vec)                                                                                                   \
-      hipLaunchKernelGGL((quant_rows_kernel<T, TPR, NV, true>), grid, dim3(256), 0, st, x, ldx, rows, K, q,     \
-                         ldq, scale);                                                                          \
-    else                                                                                                       \
-      hipLaunchKernelGGL((quant_rows_kernel<T, TPR, NV, false>), grid, dim3(256), 0, st, x, ldx, rows, K, q,    \
-                         ldq, scale);                                                                          \
-  }
+#define T2I_Q(TPR, NV)                                                                                      \
+  hipLaunchKernelGGL((quant_rows_kernel<T, TPR, NV>), dim3((unsigned)((rows + 256L / TPR - 1) / (256 / TPR))), \
+                     dim3(256), 0, st, x, ldx, rows, K, q, ldq, scale)
   // one wave per row up to 2048 elements, a workgroup for longer rows; just the
   // pieces that the row has, up to what registers hold
-  if (K <= 512) T2I_Q(64, 1)
-  else if (K <= 1024) T2I_Q(64, 2)
-  else if (K <= 1536) T2I_Q(64, 3)
-  else if (K <= 2048) T2I_Q(64, 4)
-  else if (K <= 4096) T2I_Q(256, 2)
-  else if (K <= 8192) T2I_Q(256, 4)
-  else T2I_Q(256, 8)
+  if (K <= 512) T2I_Q(64, 1);
+  else if (K <= 1024) T2I_Q(64, 2);
+  else if (K <= 1536) T2I_Q(64, 3);
+  else if (K <= 2048) T2I_Q(64, 4);
+  else if (K <= 4096) T2I_Q(256, 2);
+  else if (K <= 8192) T2I_Q(256, 4);
+  else T2I_Q(256, 8);
 #undef T2I_Q
 }
 
