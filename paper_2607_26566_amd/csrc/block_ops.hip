@@ -37,12 +37,34 @@ __device__ __forceinline__ void store8(T* p, const float (&v)[8]) {
   }
 }
 
+// Groups of G lanes in a workgroup of 256: powers of two, or nine lanes (heads of 72),
+// seven groups to a wave.
 template <int G>
-__device__ __forceinline__ float group_sum(float v) {
+struct Groups {
+  static constexpr int WAVE = 64 / G, ALL = 4 * WAVE;
+  int lane, group;   // of the group; of the workgroup
+  bool live;         // (nine: the 64th lane has no group)
+  __device__ __forceinline__ Groups() {
+    const int l = threadIdx.x & 63;
+    lane = l % G, group = (threadIdx.x >> 6) * WAVE + l / G, live = l < WAVE * G;
+  }
+  // sum over the group's lanes, the same in each of them
+  __device__ __forceinline__ float sum(float v) const {
+    if constexpr ((G & (G - 1)) == 0) {
 #pragma unroll
-  for (int o = G / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
-  return v;
-}
+      for (int o = G / 2; o >= 1; o >>= 1) v += __shfl_xor(v, o, kWave);
+      return v;
+    } else {
+      static_assert(G == 9, "lanes of a head");
+      const int base = (threadIdx.x & 63) - lane;
+      float s = v;
+#pragma unroll
+      for (int o = 1; o <= 4; o *= 2) s += __shfl(s, lane + o < G ? base + lane + o : base, kWave);
+      // (the first lane's: eight lanes from it on, and the ninth)
+      return __shfl(s, base, kWave) + __shfl(v, base + 8, kWave);
+    }
+  }
+};
 
 // ---------------------------------------------------------------------------
 // Quantising rows: s = max(max |x| / 127, 2^-126) in fp32, q = x / s to the
@@ -230,11 +252,12 @@ hipError_t launch_quant_rows(bool bf16_in, int rows, int K, const void* x, int l
 }
 
 // ---------------------------------------------------------------------------
-// Query / key norm with rotation.  G lanes hold one head, 8 elements each
-// (G = the power of two at or above head_dim / 8); a group keeps one row's
-// rotation and takes HPG of its heads, all of whose loads are under way before the
-// first norm.  9216 rows of 48 heads of 128 47 - 52 us (4.5 - 4.9 TB/s; a copy 5.1),
-// 4451 rows of 32 heads of 72 (9 of 16 lanes) 12.9 us (3.3 TB/s).
+// Query / key norm with rotation.  G lanes hold one head, 8 elements each (G = the
+// power of two at or above head_dim / 8, or nine); a group keeps one row's rotation and
+// takes HPG of its heads, all of whose loads are under way before the first norm.  9216
+// rows of 48 heads of 128 42 - 52 us (4.5 - 5.4 TB/s; a copy 5.1), 4451 rows of 32 heads
+// of 72 10.8 us (3.8 TB/s; with 16 lanes of which nine work 13.0, 20000 rows of 28 heads
+// 39.3 -> 31.9 and backward 75.2 -> 54.3).
 
 // The rotation of a lane's elements.  Pairs (2j, 2j + 1): four pairs in the lane.
 // Halves (j, j + d/2): eight elements whose partners sit in another lane.
@@ -301,11 +324,12 @@ __device__ __forceinline__ void load_weight(const void* w, int lg, int nl, float
 
 template <typename T, int G, bool HALVES, int HPG>
 __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNorm a, int upr) {
-  const int lg = threadIdx.x % G, nl = a.head_dim / 8, H = a.heads_q + a.heads_k;
-  const unsigned unit = blockIdx.x * (256 / G) + threadIdx.x / G;
+  const Groups<G> gr;
+  const int lg = gr.lane, nl = a.head_dim / 8, H = a.heads_q + a.heads_k;
+  const unsigned unit = blockIdx.x * Groups<G>::ALL + gr.group;
   const unsigned r = unit / (unsigned)upr;
   const int h0 = (int)(unit - r * (unsigned)upr);
-  const bool live = r < (unsigned)a.rows && lg < nl;
+  const bool live = r < (unsigned)a.rows && lg < nl && gr.live;
   const int row = r < (unsigned)a.rows ? (int)r : 0;
   float v[HPG][8];
 #pragma unroll
@@ -332,7 +356,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNorm a, int upr) {
     float ss = 0.f;
 #pragma unroll
     for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
-    const float rs = rsqrtf(fmaf(group_sum<G>(ss), rd, a.eps));
+    const float rs = rsqrtf(fmaf(gr.sum(ss), rd, a.eps));
     const bool isq = h < a.heads_q;
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[i][j] = v[i][j] * rs * (isq ? wq[j] : wk[j]);
@@ -345,12 +369,14 @@ __global__ __launch_bounds__(256) void qk_norm_rope_kernel(QkNorm a, int upr) {
   }
 }
 
-// lanes that hold one head
+// lanes that hold one head, and groups of them in a workgroup
 static int head_lanes(int head_dim) {
+  if (head_dim == 9 * 8) return 9;
   int g = 1;
   while (g * 8 < head_dim) g *= 2;
   return g;
 }
+static int head_groups(int head_dim) { return 64 / head_lanes(head_dim) * 4; }
 
 // heads per group of the forward kernel (two: 9216 rows of 48 heads of 128 54.3 us,
 // four 51.9, six 51.4 but 22.0 instead of 20.5 for 16384 of 20 heads of 64)
@@ -358,7 +384,7 @@ constexpr int kFwdHeads = 4;
 template <typename T, int G, bool HALVES>
 static void qk_launch(const QkNorm& a, hipStream_t st) {
   const int H = a.heads_q + a.heads_k;
-  const int gr = 256 / G;
+  const int gr = Groups<G>::ALL;
   // several heads of a row per group where that still leaves workgroups enough
   const int hpg = (long)a.rows * ((H + kFwdHeads - 1) / kFwdHeads) / gr >= 1024 ? kFwdHeads : 1;
   const int upr = (H + hpg - 1) / hpg;
@@ -372,15 +398,17 @@ static void qk_launch(const QkNorm& a, hipStream_t st) {
 // Backward.  With n = x r, r = (mean x^2 + eps)^-1/2, y = R (n w):
 //   dn = (R^T dy) w,  dx = r (dn - n mean(dn n)),  dw = sum over rows and heads
 //   of (R^T dy) n.
-// 9216 rows of 48 heads of 128 86 us (4.0 TB/s), 4451 of 32 heads of 72 21.4 us.
+// 9216 rows of 48 heads of 128 86 us (4.0 TB/s), 4451 of 32 heads of 72 20.6 us with
+// the second launch (16 lanes for a head of 72: 24.6).
 // A fixed number of workgroups walks the (row, heads) units; dw adds up in
 // registers, then over the workgroup in LDS, then (qk_weight_grad_kernel) over
 // the workgroups: a fixed order.
 template <typename T, int G, bool HALVES, int HPG>
 __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, int upr, float* __restrict__ partial) {
-  constexpr int GR = 256 / G;
+  constexpr int GR = Groups<G>::ALL;
   __shared__ float red[2][GR][G * 8];
-  const int lg = threadIdx.x % G, gi = threadIdx.x / G, nl = a.head_dim / 8;
+  const Groups<G> gr;
+  const int lg = gr.lane, gi = gr.group, nl = a.head_dim / 8;
   const int H = a.heads_q + a.heads_k;
   const unsigned units = (unsigned)a.rows * (unsigned)upr, stride = gridDim.x * GR;
   float wq[8], wk[8], aq[8], ak[8];
@@ -391,7 +419,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, int upr
   const float rd = 1.f / (float)a.head_dim;
   for (unsigned u0 = blockIdx.x * GR; u0 < units; u0 += stride) {
     const unsigned u = u0 + gi;
-    const bool in = u < units && lg < nl;
+    const bool in = u < units && lg < nl && gr.live;
     const int row = u < units ? (int)(u / (unsigned)upr) : 0;
     const int h0 = u < units ? (int)(u - (unsigned)row * (unsigned)upr) : 0;
     float x[HPG][8], dy[HPG][8];
@@ -422,7 +450,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, int upr
       float ss = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) ss = fmaf(n[j], n[j], ss);
-      const float r = rsqrtf(fmaf(group_sum<G>(ss), rd, a.eps));
+      const float r = rsqrtf(fmaf(gr.sum(ss), rd, a.eps));
       float dot = 0.f;
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
@@ -433,7 +461,7 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, int upr
         d[j] *= isq ? wq[j] : wk[j];
         dot = fmaf(d[j], n[j], dot);
       }
-      dot = group_sum<G>(dot) * rd;
+      dot = gr.sum(dot) * rd;
 #pragma unroll
       for (int j = 0; j < 8; ++j) d[j] = r * fmaf(-n[j], dot, d[j]);
       if (live)
@@ -442,11 +470,12 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, int upr
     }
   }
   if (!partial) return;
+  if (gr.live)
 #pragma unroll
-  for (int j = 0; j < 8; ++j) {
-    red[0][gi][lg * 8 + j] = aq[j];
-    red[1][gi][lg * 8 + j] = ak[j];
-  }
+    for (int j = 0; j < 8; ++j) {
+      red[0][gi][lg * 8 + j] = aq[j];
+      red[1][gi][lg * 8 + j] = ak[j];
+    }
   __syncthreads();
   for (int i = threadIdx.x; i < 2 * a.head_dim; i += 256) {
     const int w = i / a.head_dim, c = i - w * a.head_dim;
@@ -462,11 +491,11 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, int upr
 // halve the waves), 1024 workgroups (four per CU; 2048: 89 us, 768: 99)
 constexpr int kBwdHeads = 2, kBwdBlocks = 1024;
 static int qk_bwd_hpg(int rows, int heads, int head_dim) {
-  const int gr = 256 / head_lanes(head_dim);
+  const int gr = head_groups(head_dim);
   return (long)rows * ((heads + kBwdHeads - 1) / kBwdHeads) / gr >= kBwdBlocks ? kBwdHeads : 1;
 }
 int qk_bwd_blocks(int rows, int heads, int head_dim) {
-  const int gr = 256 / head_lanes(head_dim), hpg = qk_bwd_hpg(rows, heads, head_dim);
+  const int gr = head_groups(head_dim), hpg = qk_bwd_hpg(rows, heads, head_dim);
   return (int)std::min<long>(kBwdBlocks, ((long)rows * ((heads + hpg - 1) / hpg) + gr - 1) / gr);
 }
 
@@ -486,6 +515,7 @@ static void qk_bwd_launch(const QkNorm& a, float* partial, hipStream_t st) {
     case 2: FN<T, 2, HALVES>(__VA_ARGS__); break;                                   \
     case 4: FN<T, 4, HALVES>(__VA_ARGS__); break;                                   \
     case 8: FN<T, 8, HALVES>(__VA_ARGS__); break;                                   \
+    case 9: FN<T, 9, HALVES>(__VA_ARGS__); break;                                   \
     case 16: FN<T, 16, HALVES>(__VA_ARGS__); break;                                 \
     default: FN<T, 32, HALVES>(__VA_ARGS__); break;                                 \
   }
