@@ -99,7 +99,9 @@ def _switch(dev: int, stream):
         yield
 
 
-_stream = torch._C._cuda_getCurrentRawStream
+def _stream(dev: int) -> int:
+    # (looked up here, not at import: a torch without a GPU back end has no such name)
+    return torch._C._cuda_getCurrentRawStream(dev)
 
 
 def quant_rows(x: torch.Tensor, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:

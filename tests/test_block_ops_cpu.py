@@ -2,6 +2,8 @@
 and every refusal of the entry points (nothing here reaches a GPU: each call
 fails its argument checks)."""
 import ctypes as C
+import subprocess
+import sys
 
 import numpy as np
 import pytest
@@ -9,6 +11,7 @@ import torch
 
 import paper_2607_26566_amd as t2i
 from paper_2607_26566_amd import _lib
+from conftest import ROOT
 from oracle import blocks
 
 F32, BF16 = _lib.T2I_F32, _lib.T2I_BF16
@@ -245,3 +248,24 @@ def test_python_calls_refuse_host_tensors():
         with pytest.raises(t2i.T2IError) as e:
             f()
         assert e.value.status == INVALID
+
+
+def test_the_package_imports_with_a_torch_that_has_no_gpu():
+    """Such a torch lacks the names behind the current device and stream; the calls still
+    refuse host tensors."""
+    code = """
+import torch
+for name in ("_cuda_getCurrentRawStream", "_cuda_getDevice"):
+    if hasattr(torch._C, name):
+        delattr(torch._C, name)
+import paper_2607_26566_amd as t2i
+x = torch.zeros(4, 128)
+try:
+    t2i.quant_rows(x)
+except t2i.T2IError as e:
+    assert e.status == 1
+else:
+    raise SystemExit("not refused")
+"""
+    r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
+    assert r.returncode == 0, r.stderr
