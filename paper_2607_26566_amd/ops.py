@@ -59,10 +59,15 @@ def _device(first: torch.Tensor, *others) -> int:
 # the current device, no stream given -- goes without strides, stream objects and
 # contexts.
 
+_INT = 2 ** 31   # the library's sizes are 32-bit integers, and ctypes drops what lies above
+
+
 def _rows(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> int:
     """Row stride of a matrix of this shape and type (its columns contiguous)."""
     if t.dtype is not dtype or t.shape != (rows, cols):
         raise T2IError(2, f"{what}: expected ({rows}, {cols}) {dtype}, got {tuple(t.shape)} {t.dtype}")
+    if rows >= _INT or cols >= _INT:
+        raise T2IError(2, f"{what}: 2^31 rows or columns, or more")
     if t.is_contiguous():
         return cols
     ld, step = t.stride()
@@ -70,7 +75,7 @@ def _rows(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> int:
         raise T2IError(2, f"{what}: columns must be contiguous")
     if rows == 1:       # a single row may come with any stride
         ld = cols
-    if not cols <= ld < 2 ** 31:
+    if not cols <= ld < _INT:
         raise T2IError(2, f"{what}: rows must not overlap")
     return ld
 
@@ -241,7 +246,9 @@ def _heads(t: torch.Tensor, rows: int, d: int, dtype, what: str):
             raise T2IError(2, f"{what}: heads must be side by side")
         if rows == 1:
             ld = h * d
-    if not h * d <= ld < 2 ** 31:
+    if rows >= _INT:
+        raise T2IError(2, f"{what}: 2^31 rows or more")
+    if not h * d <= ld < _INT:
         raise T2IError(2, f"{what}: rows must not overlap")
     return h, ld
 
@@ -260,6 +267,7 @@ def _qk_args(q, k, wq, wk, table, pos, pairing):
         n_pos = table.shape[0] if table.dim() == 3 else -1
         if table.dtype != torch.float32 or table.shape != (n_pos, d // 2, 2) or not table.is_contiguous():
             raise T2IError(2, f"table must be fp32 [n_pos, {d // 2}, 2], contiguous")
+        _need(n_pos < _INT, "table: 2^31 positions or more")
     _need(pos is None or table is not None, "pos goes with a table", 1)
     _vec(pos, rows, torch.int32, "pos")
     return dt, pr, rows, hq, hk, d, ldq, ldk, n_pos

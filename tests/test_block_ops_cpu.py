@@ -269,3 +269,28 @@ else:
 """
     r = subprocess.run([sys.executable, "-c", code], cwd=ROOT, capture_output=True, text=True)
     assert r.returncode == 0, r.stderr
+
+
+def test_python_calls_refuse_sizes_past_32_bits(monkeypatch):
+    """2^32 + 8 of anything would reach the library as 8."""
+    from paper_2607_26566_amd import ops
+    monkeypatch.setattr(ops, "_device", lambda *a: 0)
+    monkeypatch.setattr(ops, "_elsewhere", lambda *a: False)
+    monkeypatch.setattr(ops, "_stream", lambda dev: 0)
+    big = 2 ** 32 + 8
+
+    def of(*shape, dtype=torch.bfloat16):   # (no memory behind it)
+        return torch.empty(shape, dtype=dtype, device="meta")
+    x, w, h = of(big, 8), of(8, 8), of(big, 1, 8)
+    q8, s8 = of(big, 128, dtype=torch.int8), of(big, dtype=torch.float32)
+    w8, ws = of(8, 128, dtype=torch.int8), of(8, dtype=torch.float32)
+    pre, few, table = of(big, 16, dtype=torch.float32), of(8, 1, 8), of(big, 4, 2, dtype=torch.float32)
+    for f in (lambda: t2i.quant_rows(x), lambda: t2i.quant_rows(of(1, big)),
+              lambda: t2i.linear_i8(q8, s8, w8, ws, K=8), lambda: t2i.linear_i8(w8, ws, q8, s8, K=8),
+              lambda: t2i.linear_i8(of(8, 2 ** 32 + 128, dtype=torch.int8), ws, w8, ws, K=8),
+              lambda: t2i.gated_linear(x, w, w), lambda: t2i.gated_linear(w, x, x),
+              lambda: t2i.gated_linear_backward(x, x, w, w, pre), lambda: t2i.qk_norm_rope(h, h),
+              lambda: t2i.qk_norm_rope(few, few, table=table), lambda: t2i.qk_norm_rope_backward(h, h, h, h)):
+        with pytest.raises(t2i.T2IError, match=r"2\^31") as e:
+            f()
+        assert e.value.status == SHAPE
