@@ -10,8 +10,8 @@ namespace {
 
 bool bad_dtype(int32_t d) { return d != T2I_F32 && d != T2I_BF16; }
 bool off(const void* p, size_t n) { return (uintptr_t)p % n != 0; }
-// a launch holds fewer than 2^32 threads: the smallest tiles take 512 for 64 x 128
-// outputs, 256 for 64 x 64 or 32 x 128
+// a launch holds fewer than 2^32 threads: the tiles that many outputs may take have at most
+// 512 for 64 x 64 of them
 bool too_large(int64_t M, int64_t N) { return ((M + 63) / 64) * ((N + 63) / 64) >= 1 << 23; }
 // (fewer than 2^32 threads, of which a head takes less than a fourth of its elements)
 bool too_many_heads(int64_t rows, int64_t hq, int64_t hk, int64_t d) {

@@ -334,6 +334,9 @@ constexpr TileChoice kTiles[] = {{256, 256, 1, 1.60f, 1.60f, 13.f}, {128, 128, 2
                                  {128, 128, 1, 0.55f, 0.55f, 5.f},  {64, 128, 3, 0.60f, 1.01f, 3.f},
                                  {64, 128, 2, 0.48f, 1.00f, 2.85f}, {32, 128, 2, 0.44f, 0.78f, 2.f},
                                  {32, 64, 2, 0.155f, 0.37f, 2.2f},  {16, 32, 2, 0.073f, 0.17f, 2.5f}};
+// Shapes with groups of waves, for few tiles: their launch takes up to 2048 threads for 64
+// x 64 outputs (the others at most 512), so that it stays below 2^32 only up to here.
+static bool few_tiles(long rows, long cols) { return ((rows + 63) / 64) * ((cols + 63) / 64) < 1 << 21; }
 constexpr int kGradTiles = 6, kTile32 = 5, kTile32k = 6, kTile16k = 7, kStream = 8;
 // The products without slices (8-bit layer, gated forward) have two more shapes for few
 // tiles of a long contraction: groups of waves share the steps of a tile.  us on the
@@ -342,7 +345,8 @@ constexpr int kGradTiles = 6, kTile32 = 5, kTile32k = 6, kTile16k = 7, kStream =
 // (Eight groups of 16 x 32 leave no room for a second workgroup: F = 1232 9.1 -> 8.2, F =
 // 4256 17.0 -> 18.9.)  Tile32 takes one block of rows whose weights stream from memory.
 static int tile_index(long rows, long cols, int steps, float end_scale) {
-  const int shape = choose_tile(kTiles, steps < 4 ? kGradTiles : kGradTiles + 2, rows, cols, steps, end_scale).shape;
+  const bool groups = steps >= 4 && few_tiles(rows, cols);
+  const int shape = choose_tile(kTiles, groups ? kGradTiles + 2 : kGradTiles, rows, cols, steps, end_scale).shape;
   return shape >= kTile32 && rows <= 32 && cols > 128 * 128 ? kStream : shape;
 }
 
@@ -365,7 +369,8 @@ constexpr TileChoice kTilesF32[] = {{128, 128, 1, 1.88f, 1.79f, 3.f}, {64, 64, 1
 // groups; 1 x 4608 x 7496 80, 69 and 26 on 16 x 32; 82 x 4512 x 1792 22, 19, 23).
 constexpr int kF32DwTiles = 2, kF32DxTiles = 3, kF32Groups = 3;
 static int tile_index_f32(long rows, long cols, int steps) {
-  return choose_tile(kTilesF32, steps < 4 ? kF32Groups : kF32Groups + 2, rows, cols, steps, 0.5f).shape;
+  const bool groups = steps >= 4 && few_tiles(rows, cols);
+  return choose_tile(kTilesF32, groups ? kF32Groups + 2 : kF32Groups, rows, cols, steps, 0.5f).shape;
 }
 constexpr int kMaxSlices = 16;
 

@@ -294,3 +294,41 @@ def test_python_calls_refuse_sizes_past_32_bits(monkeypatch):
         with pytest.raises(t2i.T2IError, match=r"2\^31") as e:
             f()
         assert e.value.status == SHAPE
+
+
+def launched_threads(op, dtype, M, F, K):
+    """Threads of the launch that a product takes (op as in t2i_test_block_tile)."""
+    v = [C.c_int() for _ in range(4)]
+    assert t2i.load().t2i_test_block_tile(op, int(dtype == BF16), M, F, K, *map(C.byref, v))
+    bm, bn, _, slices = (x.value for x in v)
+    rows, cols = {0: (M, F), 1: (M, 2 * F), 2: (M, K), 3: (F, K)}[op]
+    tiles = -(-rows // bm) * -(-cols // bn) * (2 if op == 3 else 1)
+    waves = {(256, 256): 8, (128, 128): 8, (64, 128): 8, (32, 128): 4, (64, 64): 4, (32, 64): 4, (16, 32): 1}
+    return tiles * waves[bm, bn] * 64 * slices
+
+
+@pytest.mark.parametrize("op,dtype", [(0, BF16), (1, BF16), (1, F32), (2, BF16), (2, F32), (3, BF16), (3, F32)])
+def test_no_allowed_product_launches_too_many_threads(op, dtype):
+    """Sizes just inside the limit of 2^23 pieces of 64 x 64 outputs, of every form."""
+    r, most = rng(5 + op), 2 ** 23 - 1
+    cases = 0
+    for i in range(4000):
+        short = int(2 ** r.uniform(0, 20)) if i % 4 else int(r.integers(1, 65))
+        long = most // -(-short // 64) * 64 - int(r.integers(0, 200))
+        deep = int(2 ** r.uniform(0, 14))
+        rows, cols = (long, short) if r.random() < 0.5 else (short, long)
+        if op == 0:
+            sizes = rows, cols, deep
+        elif op == 1:
+            sizes = rows, max(1, cols // 2), deep
+        elif op == 2:
+            sizes = rows, deep, cols
+        else:
+            sizes = deep, max(1, rows // 2), cols
+        M, F, K = sizes
+        # (an operand's rows lie less than 8 MiB apart)
+        if F > 2 ** 28 or op > 1 and F >= 2 ** 20 or op and K * (2 if dtype == BF16 else 4) >= 2 ** 23:
+            continue
+        cases += 1
+        assert launched_threads(op, dtype, M, F, K) < 2 ** 32, sizes
+    assert cases > 500
