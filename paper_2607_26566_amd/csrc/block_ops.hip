@@ -509,13 +509,14 @@ static void qk_bwd_launch(const QkNorm& a, float* partial, hipStream_t st) {
     hipLaunchKernelGGL((qk_norm_rope_bwd_kernel<T, G, HALVES, 1>), grid, dim3(256), 0, st, a, upr, partial);
 }
 
+// (halves: head_dim % 16 == 0, so neither one lane nor nine)
 #define T2I_QK(FN, ...)                                                             \
   switch (head_lanes(a.head_dim)) {                                                 \
-    case 1: FN<T, 1, HALVES>(__VA_ARGS__); break;                                   \
+    case 1: if constexpr (!HALVES) FN<T, 1, HALVES>(__VA_ARGS__); break;            \
     case 2: FN<T, 2, HALVES>(__VA_ARGS__); break;                                   \
     case 4: FN<T, 4, HALVES>(__VA_ARGS__); break;                                   \
     case 8: FN<T, 8, HALVES>(__VA_ARGS__); break;                                   \
-    case 9: FN<T, 9, HALVES>(__VA_ARGS__); break;                                   \
+    case 9: if constexpr (!HALVES) FN<T, 9, HALVES>(__VA_ARGS__); break;            \
     case 16: FN<T, 16, HALVES>(__VA_ARGS__); break;                                 \
     default: FN<T, 32, HALVES>(__VA_ARGS__); break;                                 \
   }

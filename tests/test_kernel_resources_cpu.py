@@ -58,3 +58,12 @@ def test_conditioning_rows_keep_five_waves_per_simd(kernels):
 def test_cache_signal_does_not_spill(kernels):
     for k, v in find(kernels, "cache_signal_kernel").items():
         assert v["vgpr_spill_count"] == 0 and v["private_segment_fixed_size"] == 0, (k, v)
+
+
+def test_no_head_norm_kernel_that_no_call_reaches(kernels):
+    """Halves need head_dim % 16 == 0: no head of 8 (one lane) or 72 (nine lanes)."""
+    forms = {k: re.search(r"kernelI(f|DF16b)Li(\d+)ELb([01])ELi\d+E", k)
+             for k in {**find(kernels, "qk_norm_rope_kernel"), **find(kernels, "qk_norm_rope_bwd_kernel")}}
+    assert all(forms.values())
+    assert {int(m[2]) for m in forms.values() if m[3] == "1"} == {2, 4, 8, 16, 32}
+    assert {int(m[2]) for m in forms.values() if m[3] == "0"} == {1, 2, 4, 8, 9, 16, 32}
