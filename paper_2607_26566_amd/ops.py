@@ -7,8 +7,10 @@ results are new tensors of that device.  The work runs on ``stream``, by default
 the device's current stream, and results and workspaces are allocated for that
 stream: a caller that uses another stream on either side orders the two itself and
 keeps the operands until the work is done.  Nothing here is recorded for automatic
-differentiation; the ``_backward`` calls are the gradients.  Wrong arguments raise
-:class:`T2IError` before anything is launched.
+differentiation: the ``_backward`` calls are the gradients, and an operand that requires a
+gradient while gradients are recorded (outside ``torch.no_grad()`` and the passes of a
+``torch.autograd.Function``), or that carries a tangent, is refused, as the result would
+lose it.  Wrong arguments raise :class:`T2IError` before anything is launched.
 """
 from __future__ import annotations
 
@@ -16,6 +18,7 @@ import contextlib
 from typing import Optional, Tuple
 
 import torch
+from torch.autograd import forward_ad
 
 from . import _lib
 from ._lib import T2I_BF16, T2I_F32, T2IError, load
@@ -45,13 +48,23 @@ def _of(table: dict, key, what: str):
 
 
 def _device(first: torch.Tensor, *others) -> int:
-    """Index of the one device of all given tensors (None entries left out)."""
+    """Index of the one device of all given tensors (None entries left out), none of
+    which automatic differentiation follows."""
     dev = first.get_device()
     if dev < 0:
         raise T2IError(1, "operands must be device tensors")
     for t in others:
         if t is not None and t.get_device() != dev:
             raise T2IError(1, "operands must be device tensors of one device")
+    if torch.is_grad_enabled():
+        for t in (first, *others):
+            if t is not None and t.requires_grad:
+                raise T2IError(1, "an operand requires a gradient, which this call does not record: "
+                                  "detach it or call under torch.no_grad()")
+    if getattr(forward_ad, "_current_level", 0) >= 0:   # (within a dual level)
+        for t in (first, *others):
+            if t is not None and forward_ad.unpack_dual(t).tangent is not None:
+                raise T2IError(1, "an operand carries a tangent, which this call does not pass on")
     return dev
 
 

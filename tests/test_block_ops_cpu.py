@@ -296,6 +296,62 @@ def test_python_calls_refuse_sizes_past_32_bits(monkeypatch):
         assert e.value.status == SHAPE
 
 
+class OnDevice(torch.Tensor):
+    """A host tensor that says it lies on device 0."""
+
+    def get_device(self):
+        return 0
+
+
+def block_calls(mk):
+    """(call, its floating operands) of every Python call, on operands that mk makes."""
+    x, wg, wu, b, dout, pre, g = mk(4, 64), mk(8, 64), mk(8, 64), mk(8), mk(4, 8), mk(4, 16), mk(8)
+    q8, w8 = torch.zeros(4, 128, dtype=torch.int8).as_subclass(OnDevice), torch.zeros(8, 128, dtype=torch.int8)
+    w8, sa, sw, r, c = w8.as_subclass(OnDevice), mk(4), mk(8), mk(4, 8), mk(4, 8)
+    q, k, dq, dk, nq, nk, t = mk(4, 2, 16), mk(4, 1, 16), mk(4, 2, 16), mk(4, 1, 16), mk(16), mk(16), mk(4, 8, 2)
+    return [
+        (lambda x: t2i.quant_rows(x), [x]),
+        (lambda sa, sw, b, r, c, g: t2i.linear_i8(q8, sa, w8, sw, b, K=64, epilogue="resid_gated", resid=r,
+                                                  resid_copy=c, gate=g), [sa, sw, b, r, c, g]),
+        (lambda x, wg, wu, b, c: t2i.gated_linear(x, wg, wu, b, c), [x, wg, wu, b, g]),
+        (lambda *a: t2i.gated_linear_backward(*a), [dout, x, wg, wu, pre]),
+        (lambda q, k, nq, nk, t: t2i.qk_norm_rope(q, k, nq, nk, table=t), [q, k, nq, nk, t]),
+        (lambda dq, dk, q, k, nq, nk, t: t2i.qk_norm_rope_backward(dq, dk, q, k, nq, nk, table=t),
+         [dq, dk, q, k, nq, nk, t])]
+
+
+def test_python_calls_refuse_what_differentiation_follows(monkeypatch):
+    from torch.autograd import forward_ad
+    from paper_2607_26566_amd import ops
+
+    class Through(Exception):
+        pass
+
+    def through(*a):
+        raise Through
+    monkeypatch.setattr(ops, "_elsewhere", through)   # what follows the checks of the operands
+    for call, operands in block_calls(lambda *s: torch.ones(s).as_subclass(OnDevice)):
+        with pytest.raises(Through):
+            call(*operands)
+        for i, t in enumerate(operands):
+            leaf = t.clone().requires_grad_()
+            for v in (leaf, leaf * 1):
+                args = [*operands[:i], v, *operands[i + 1:]]
+                with pytest.raises(t2i.T2IError, match="requires a gradient") as e:
+                    call(*args)
+                assert e.value.status == INVALID
+                with torch.no_grad(), pytest.raises(Through):
+                    call(*args)
+                with pytest.raises(Through):
+                    call(*(a.detach() for a in args))
+            with forward_ad.dual_level():
+                dual = forward_ad.make_dual(t, torch.ones_like(t))
+                with pytest.raises(t2i.T2IError, match="tangent"):
+                    call(*operands[:i], dual, *operands[i + 1:])
+                with pytest.raises(Through):
+                    call(*operands)
+
+
 def launched_threads(op, dtype, M, F, K):
     """Threads of the launch that a product takes (op as in t2i_test_block_tile)."""
     v = [C.c_int() for _ in range(4)]
