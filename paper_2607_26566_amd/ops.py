@@ -102,6 +102,14 @@ def _p(t: Optional[torch.Tensor]):
     return None if t is None else t.data_ptr()
 
 
+def _written(*tensors):
+    """Operands that were written to: differentiation that has saved one of them finds out
+    (as with torch's own operations in place) instead of using the new values."""
+    for t in tensors:
+        if t is not None:
+            torch.autograd.graph.increment_version(t)
+
+
 def _elsewhere(dev: int, stream) -> bool:
     return stream is not None or dev != torch._C._cuda_getDevice()
 
@@ -184,7 +192,10 @@ def linear_i8(a: torch.Tensor, a_scale: torch.Tensor, w: torch.Tensor, w_scale: 
     _check(load().t2i_op_linear_i8(dt, epi, M, N, K, a.data_ptr(), lda, a_scale.data_ptr(), w.data_ptr(),
                                    ldw, w_scale.data_ptr(), _p(bias), _p(out), N, _p(resid), ldr,
                                    _p(resid_copy), _p(gate), _stream(dev)))
-    return resid if out is None else out
+    if out is not None:
+        return out
+    _written(resid, resid_copy)
+    return resid
 
 
 def _gated_args(x, wg, wu):
@@ -307,6 +318,8 @@ def qk_norm_rope(q: torch.Tensor, k: torch.Tensor, wq: Optional[torch.Tensor] = 
     _check(load().t2i_op_qk_norm_rope(
         dt, rows, hq, hk, d, q.data_ptr(), ldq, k.data_ptr(), ldk, _p(wq), _p(wk), eps, pr, _p(table), n_pos,
         _p(pos), oq.data_ptr(), ldoq, ok.data_ptr(), ldok, _stream(dev)))
+    if inplace:
+        _written(q, k)
     return oq, ok
 
 

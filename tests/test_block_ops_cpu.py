@@ -352,6 +352,43 @@ def test_python_calls_refuse_what_differentiation_follows(monkeypatch):
                     call(*operands)
 
 
+def test_operands_written_in_place_are_marked(monkeypatch):
+    """Differentiation that saved them has to find out that their values are gone."""
+    from paper_2607_26566_amd import ops
+
+    class Done:   # (a library whose calls succeed)
+        t2i_op_linear_i8 = t2i_op_qk_norm_rope = staticmethod(lambda *a: 0)
+    monkeypatch.setattr(ops, "load", Done)
+    monkeypatch.setattr(ops, "_elsewhere", lambda *a: False)
+    monkeypatch.setattr(ops, "_stream", lambda dev: 0)
+
+    def mk(*s, dtype=torch.float32):
+        return torch.ones(s, dtype=dtype).as_subclass(OnDevice)
+    weight = torch.ones(4, 16, requires_grad=True)
+    q8, s8 = mk(4, 128, dtype=torch.int8), mk(4)
+
+    def spoiled(t, call):
+        """Whether the gradient of weight * t fails once the call has written t."""
+        y = (weight * t.as_subclass(torch.Tensor).reshape(4, 16)).sum()
+        call()
+        try:
+            y.backward()
+        except RuntimeError as e:
+            assert "inplace" in str(e)
+            return True
+        return False
+    q, k, r, c = mk(4, 1, 16), mk(4, 1, 16), mk(4, 4), mk(4, 4, dtype=torch.bfloat16)
+    for t in (q, k):
+        assert spoiled(t, lambda: t2i.qk_norm_rope(q, k, inplace=True))
+        assert not spoiled(t, lambda: t2i.qk_norm_rope(q, k))
+    before = r._version, c._version
+    t2i.linear_i8(q8, s8, q8, s8, K=128, epilogue="resid", resid=r, resid_copy=c)
+    assert (r._version, c._version) == (before[0] + 1, before[1] + 1)
+    with torch.inference_mode():
+        q, k = mk(4, 1, 16), mk(4, 1, 16)
+        t2i.qk_norm_rope(q, k, inplace=True)
+
+
 def launched_threads(op, dtype, M, F, K):
     """Threads of the launch that a product takes (op as in t2i_test_block_tile)."""
     v = [C.c_int() for _ in range(4)]
