@@ -75,6 +75,10 @@ hipError_t launch_gated_dw(bool is_bf16, int M, int F, int K, const void* dgu, c
 // arithmetic only): the tile of a product, its workgroups per CU and slices.
 extern "C" int t2i_test_block_tile(int op, int is_bf16, int M, int F, int K, int* rows, int* columns, int* per_cu,
                                    int* slices);
+// also for the tests: heads that a group takes in the head norm's kernels, rows that a
+// workgroup takes in the gate gradients'
+extern "C" int t2i_test_head_norm_heads(int rows, int heads, int head_dim, int backward);
+extern "C" int t2i_test_gate_rows(int M, int F);
 
 // ---- query / key norm with rotation
 

@@ -381,12 +381,15 @@ static int head_groups(int head_dim) { return 64 / head_lanes(head_dim) * 4; }
 // heads per group of the forward kernel (two: 9216 rows of 48 heads of 128 54.3 us,
 // four 51.9, six 51.4 but 22.0 instead of 20.5 for 16384 of 20 heads of 64)
 constexpr int kFwdHeads = 4;
+// several heads of a row per group where that still leaves workgroups enough
+static int qk_fwd_hpg(int rows, int heads, int head_dim) {
+  return (long)rows * ((heads + kFwdHeads - 1) / kFwdHeads) / head_groups(head_dim) >= 1024 ? kFwdHeads : 1;
+}
 template <typename T, int G, bool HALVES>
 static void qk_launch(const QkNorm& a, hipStream_t st) {
   const int H = a.heads_q + a.heads_k;
   const int gr = Groups<G>::ALL;
-  // several heads of a row per group where that still leaves workgroups enough
-  const int hpg = (long)a.rows * ((H + kFwdHeads - 1) / kFwdHeads) / gr >= 1024 ? kFwdHeads : 1;
+  const int hpg = qk_fwd_hpg(a.rows, H, a.head_dim);
   const int upr = (H + hpg - 1) / hpg;
   const dim3 grid((unsigned)(((long)a.rows * upr + gr - 1) / gr));
   if (hpg > 1)
@@ -497,6 +500,11 @@ static int qk_bwd_hpg(int rows, int heads, int head_dim) {
 int qk_bwd_blocks(int rows, int heads, int head_dim) {
   const int gr = head_groups(head_dim), hpg = qk_bwd_hpg(rows, heads, head_dim);
   return (int)std::min<long>(kBwdBlocks, ((long)rows * ((heads + hpg - 1) / hpg) + gr - 1) / gr);
+}
+
+extern "C" int t2i_test_head_norm_heads(int rows, int heads, int head_dim, int backward) {
+  if (rows < 1 || heads < 1 || head_dim < 8 || head_dim > 256 || head_dim % 8) return 0;
+  return backward ? qk_bwd_hpg(rows, heads, head_dim) : qk_fwd_hpg(rows, heads, head_dim);
 }
 
 template <typename T, int G, bool HALVES>
@@ -623,6 +631,8 @@ int gate_row_blocks(int M, int F) {
   const int rows = gate_rows(M, F);
   return (M + rows - 1) / rows;
 }
+
+extern "C" int t2i_test_gate_rows(int M, int F) { return M < 1 || F < 1 ? 0 : gate_rows(M, F); }
 
 // V columns per thread (8 where rows are whole 16-byte pieces, else 1): 32
 // threads side by side, 8 rows at a time

@@ -934,3 +934,125 @@ def test_python_calls_refuse(bad):
     x, _ = rnd(430, (8, 256), 1.0, BF16)
     with pytest.raises(t2i.T2IError):
         bad(x, *t2i.quant_rows(x))
+
+
+# ------------------------------------------------------------------ forms that large inputs take
+
+MANY_HEADS = [(1400, 24, 24, 128, "pairs"), (17000, 2, 1, 128, "halves"), (6000, 16, 5, 64, "halves"),
+              (33000, 5, 1, 32, "pairs"), (4200, 4, 2, 256, "halves"), (14400, 1, 4, 72, "pairs"),
+              (8400, 3, 4, 80, "halves"), (131100, 2, 1, 16, "halves"), (132000, 6, 1, 8, "pairs")]
+
+
+@pytest.mark.parametrize("rows,hq,hk,d,pairing", MANY_HEADS)
+@DTYPES
+def test_qk_norm_rope_of_several_heads_per_group(rows, hq, hk, d, pairing, dtype):
+    """Four heads of a row per group of lanes (backward: two), numbers of heads that they
+    divide and that they do not, q and k within one group's heads."""
+    say("qk, several heads", rows, hq, hk, d, pairing, NAME[dtype])
+    heads = t2i.load().t2i_test_head_norm_heads
+    assert heads(rows, hq + hk, d, 0) == 4 and heads(rows, hq + hk, d, 1) == 2
+    q, k, wq, wk, rot = qk_case(rows, hq, hk, d, dtype, pairing, 21)
+    dq, hdq = rnd(22, (rows, hq, d), 1.0, dtype)
+    dk, hdk = rnd(23, (rows, hk, d), 1.0, dtype)
+    eps, hr = 1e-3, host_rot(rot)
+    out = t2i.qk_norm_rope(q, k, wq, wk, eps=eps, **rot)
+    got = t2i.qk_norm_rope_backward(dq, dk, q, k, wq, wk, eps=eps, **rot)
+    i = some(rows, 4)
+    it, ri = torch.from_numpy(i).to(DEV), dict(hr, pos=hr["pos"][i])
+    for x, w, dy, y, dx, dw in ((q, wq, hdq, out[0], got[0], got[2]), (k, wk, hdk, out[1], got[1], got[3])):
+        hx, hw = to_host(x), to_host(w)
+        # the bounds of the smaller cases' tests
+        ref = blocks.qk_norm_rope(hx[i], hw, eps, **ri)
+        mix = np.sqrt(pair_energy(blocks.head_norm(hx[i], hw, eps), pairing))
+        tol = (d / 16 + 12) * E * 2 * np.maximum(mix, np.abs(ref))
+        within(y[it], ref, tol + U[dtype] * (np.abs(ref) + tol))
+        ref, _ = blocks.qk_norm_rope_grads(dy[i], hx[i], hw, eps, **ri)
+        r = 1 / np.sqrt((hx * hx).mean(-1, keepdims=True) + eps)
+        n, mix = hx * r, np.sqrt(pair_energy(dy, pairing))
+        size = mix[i] * np.abs(hw)
+        tol = 2 * (d / 16 + 16) * E * r[i] * (size + np.abs(n[i]) * (size * np.abs(n[i])).mean(-1, keepdims=True))
+        within(dx[it], ref, tol + U[dtype] * (np.abs(ref) + tol), "dx")
+        ref = (blocks.rotate(dy, hr["table"], hr["pos"], pairing, inverse=True) * n).sum((0, 1))
+        # a term: rotation, root, product (d / 16 + 12 roundings); a lane's run of at most
+        # rows heads / (1024 groups) terms, at least two heads per step; then wider sums
+        tol = (rows * (hq + hk) / 1024 + 64 + d / 16) * E * (mix * np.abs(n)).sum((0, 1))
+        within(dw, ref, tol + U[dtype] * (np.abs(ref) + tol), "dw")
+
+
+@pytest.mark.parametrize("M,F,dtype,rows", [
+    (333, 2048, BF16, 8), (1030, 2048, BF16, 16), (2101, 2048, BF16, 32), (4133, 2048, BF16, 64),
+    (5001, 1608, BF16, 64), (301, 2055, F32, 8), (927, 2055, F32, 16), (1851, 2055, F32, 32), (3710, 2055, F32, 64)])
+def test_bias_gradients_of_every_row_block(M, F, dtype, rows):
+    """8 to 64 rows per workgroup, up to 8 of them per thread, a last block that is not full."""
+    say("bias gradients", M, F, NAME[dtype], rows)
+    assert t2i.load().t2i_test_gate_rows(M, F) == rows and M % rows
+    d, _ = gated_case(M, F, 8, dtype, False, 170)
+    pre, hp = rnd(171, (M, 2 * F), 1.5)
+    dout, hd = rnd(172, (M, F), 1.0, dtype)
+    got = t2i.gated_linear_backward(dout, d["x"], d["wg"], d["wu"], pre, act="gelu", bias=True, need_dx=False,
+                                    need_dw=False)
+    assert got[0] is None and got[1] is None and got[2] is None
+    g, u = hp[:, :F], hp[:, F:]
+    # per value as in the other gradients' tests; 8 rows in a thread, 8 threads, one
+    # rounding of the block's sum, the rest wider
+    for t, ref, each in ((got[3], hd * u * blocks.act_grad("gelu", g), np.abs(hd * u) * (1 + np.abs(g))),
+                         (got[4], hd * blocks.act("gelu", g), np.abs(hd * g))):
+        f = 2.0 ** -20 * each
+        tol = f.sum(0) + 17 * E * (np.abs(ref) + f).sum(0)
+        ref = ref.sum(0)
+        within(t, ref, tol + U[dtype] * (np.abs(ref) + tol))
+
+
+@pytest.mark.parametrize("M,N,K", [(1, 70, 300), (5, 128, 128), (33, 3000, 650), (70, 1152, 1152), (300, 260, 700),
+                                   (200, 1033, 650), (2050, 1152, 256), (4090, 4090, 640)])
+def test_linear_i8_residual_updates_with_fp32_biases(M, N, K):
+    a, sa, w, sw = i8_operands(M, N, K, 3)
+    d = [dev(v, torch.int8) if v.dtype == np.int8 else dev(v) for v in (a, sa, w, sw)]
+    b, rb = rnd(10, (N,), 0.3, F32)
+    gate, rg = rnd(11, (N,), 0.5)
+    x0, rx = rnd(12, (M, N), 2.0)
+    i = some(M, 5)
+    it = torch.from_numpy(i).to(DEV)
+    y = (a[i, :K].astype(np.float64) @ w[:, :K].astype(np.float64).T) * sa[i, None].astype(np.float64) * sw + rb
+    for epi, g in (("resid", np.ones(N)), ("resid_gated", rg)):
+        x, buf = padded(x0, 3)
+        cp, cbuf = padded(x0.to(BF16), 3)
+        out = t2i.linear_i8(*d, b, K=K, epilogue=epi, dtype=F32, resid=x, resid_copy=cp,
+                            gate=gate if epi == "resid_gated" else None)
+        assert out is x
+        ref = rx[i] + g * y
+        tol = np.abs(g) * i8_bound(y - rb, rb, y, F32, "store") + 2 * E * (np.abs(g * y) + np.abs(ref))
+        within(x[it], ref, tol, epi)
+        assert torch.equal(cp, x.to(BF16)) and (cbuf[:-1, N:] == 7).all()
+        assert (buf[:-1, N:] == 7).all() and (buf[-1] == 7).all()
+
+
+# ------------------------------------------------------------------ sums that cancel
+
+@pytest.mark.parametrize("d", [8, 64, 72, 128])
+@DTYPES
+def test_head_weight_gradients_that_cancel(d, dtype):
+    """One head per group: 2^24, ones, -2^24.  In fp32 the groups' sum loses every one."""
+    groups = {8: 256, 64: 32, 72: 28, 128: 16}[d]
+    one = torch.ones((groups, 1, d), dtype=dtype, device=DEV)
+    dy = one.clone()
+    dy[0], dy[-1] = 2.0 ** 24, -2.0 ** 24
+    w = torch.ones(d, dtype=dtype, device=DEV)
+    # (mean 1, eps 0: every normed value is the root's reciprocal, the same for all)
+    norm = t2i.qk_norm_rope(one, one[:, :0], w, w, eps=0.0)[0][0, 0].double()
+    dw = t2i.qk_norm_rope_backward(dy, one[:, :0], one, one[:, :0], w, w, eps=0.0)[2].double()
+    want = (groups - 2) * norm
+    assert ((dw - want).abs() <= 2 * U[dtype] * want).all(), dw
+
+
+@DTYPES
+def test_bias_gradients_that_cancel(dtype):
+    """One row per thread: 2^24, ones, -2^24, times an activation of 64 (exact)."""
+    M, F = 8, 16
+    dout = torch.ones((M, F), dtype=dtype, device=DEV)
+    dout[0], dout[-1] = 2.0 ** 24, -2.0 ** 24
+    x, w = torch.ones((M, 8), dtype=dtype, device=DEV), torch.ones((F, 8), dtype=dtype, device=DEV)
+    pre = torch.full((M, 2 * F), 64.0, device=DEV)
+    for act in ("silu", "gelu"):
+        dbu = t2i.gated_linear_backward(dout, x, w, w, pre, act=act, bias=True)[4]
+        assert (dbu == 64.0 * (M - 2)).all(), (act, dbu)
