@@ -403,9 +403,10 @@ static void qk_launch(const QkNorm& a, hipStream_t st) {
 //   of (R^T dy) n.
 // 9216 rows of 48 heads of 128 86 us (4.0 TB/s), 4451 of 32 heads of 72 20.6 us with
 // the second launch (16 lanes for a head of 72: 24.6).
-// A fixed number of workgroups walks the (row, heads) units; dw adds up in
-// registers, then over the workgroup in LDS, then (qk_weight_grad_kernel) over
-// the workgroups: a fixed order.
+// A fixed number of workgroups walks the (row, heads) units; dw adds up in fp32
+// registers (a lane's own units: up to 28 of them at 9216 rows of 48 heads of 128), then
+// in fp64 over the workgroup in LDS, whose sum is kept in fp32, and
+// (qk_weight_grad_kernel) over the workgroups: a fixed order.
 template <typename T, int G, bool HALVES, int HPG>
 __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, int upr, float* __restrict__ partial) {
   constexpr int GR = Groups<G>::ALL;
@@ -482,10 +483,10 @@ __global__ __launch_bounds__(256) void qk_norm_rope_bwd_kernel(QkNorm a, int upr
   __syncthreads();
   for (int i = threadIdx.x; i < 2 * a.head_dim; i += 256) {
     const int w = i / a.head_dim, c = i - w * a.head_dim;
-    float s = 0.f;
+    double s = 0.;
 #pragma unroll 4
-    for (int g = 0; g < GR; ++g) s += red[w][g][c];
-    partial[(size_t)blockIdx.x * 2 * a.head_dim + i] = s;
+    for (int g = 0; g < GR; ++g) s += (double)red[w][g][c];
+    partial[(size_t)blockIdx.x * 2 * a.head_dim + i] = (float)s;
   }
 }
 
