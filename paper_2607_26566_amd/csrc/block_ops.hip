@@ -600,7 +600,8 @@ hipError_t launch_qk_weight_grad(bool is_bf16, int blocks, int head_dim, const f
 // Gated feed-forward, elementwise gradients: with a = act(g),
 //   dg = dh u act'(g),  du = dh a,
 // rounded once to the operands' type for the products that follow (the matrix cores
-// take nothing wider); the bias gradients' column sums take the unrounded values.
+// take nothing wider); the bias gradients' column sums take the unrounded values: up to
+// 8 of a thread's rows in fp32, 8 threads in fp64, a workgroup's sum in fp32, these in fp64.
 // 4096 x 10240 120 us (4.9 TB/s of a copy's 5.1), with the column sums 121.
 
 struct ActGrad { float a, d; };   // act(g), act'(g)
@@ -694,10 +695,10 @@ __global__ __launch_bounds__(256) void gate_grad_kernel(int act, int M, int F, i
   for (int i = threadIdx.x; i < 2 * 32 * V; i += 256) {
     const int w = i / (32 * V), c = i - w * 32 * V, col = blockIdx.y * 32 * V + c;
     if (col >= Fp) continue;
-    float s = 0.f;
+    double s = 0.;
 #pragma unroll
-    for (int y = 0; y < 8; ++y) s += red[w][y][c];
-    partial[(size_t)blockIdx.x * 2 * Fp + w * Fp + col] = s;
+    for (int y = 0; y < 8; ++y) s += (double)red[w][y][c];
+    partial[(size_t)blockIdx.x * 2 * Fp + w * Fp + col] = (float)s;
   }
 }
 
