@@ -183,7 +183,7 @@ t2i_status t2i_op_quant_rows(int32_t dtype, int32_t rows, int32_t K, const void*
  * every row of W (output channel), with the epilogues of t2i_op_linear:
  *   y[m, n] = a_scale[m] * w_scale[n] * sum_k A[m, k] W[n, k] + bias[n].
  * The sum is exact (32-bit integers, K <= 131071); it is rounded once to fp32,
- * the rest is fp32.
+ * the rest is fp32 (a_scale times the sum first).
  *   A [M, K], W [N, K] int8, 16-byte aligned, row strides lda, ldw multiples of
  *   16, at least K rounded up to a multiple of 128 and below 8 MiB: both are read
  *   up to that multiple, and one of the two must hold zeros behind K
@@ -260,7 +260,8 @@ typedef enum {
  *   q [rows, heads_q * head_dim] (stride ldq), k [rows, heads_k * head_dim]
  *   (stride ldk; the columns of one fused projection, or buffers of their
  *   own), wq, wk [head_dim] or NULL (ones), outputs q_out, k_out alike, all of
- *   dtype; the arithmetic is fp32, one rounding.  heads_q or heads_k may be 0
+ *   dtype; the arithmetic is fp32, one rounding (squares past fp32 make a head's
+ *   outputs 0; with eps 0 a head of zeros gives NaN).  heads_q or heads_k may be 0
  *   (its pointers are then unused); rows * (heads_q + heads_k) < 2^31, and head_dim
  *   times that < 2^34.
  *   table fp32 [n_pos][head_dim / 2][2] of (cos, sin), or NULL: no rotation
@@ -285,7 +286,8 @@ t2i_status t2i_op_qk_norm_rope(int32_t dtype, int32_t rows, int32_t heads_q, int
  * Gradients of t2i_op_qk_norm_rope: dq, dk the gradients of q_out, k_out; q, k
  * and the other arguments the forward pass's inputs; dq_in, dk_in receive the
  * gradients of q, k, dwq, dwk [head_dim] (or NULL) those of the weights, summed
- * over rows and heads in a fixed order, all of dtype.  dq_in may be dq itself
+ * over rows and heads in a fixed order, all of dtype (a row with pos[r] >= n_pos
+ * makes its own gradients and dwq, dwk NaN).  dq_in may be dq itself
  * (same stride), dk_in dk.  ws as in t2i_op_gated_linear_backward (may be NULL
  * when dwq and dwk are).
  */

@@ -1,8 +1,8 @@
 // Row-wise block operators (gfx950): quantising rows to 8 bits, the gated
 // feed-forward's elementwise gradients, RMS norm of query and key heads with
 // the position rotation, and its gradients.  All of them are bound by HBM:
-// each input is read once, 16 bytes per lane, held in registers, and each
-// output written once.
+// each input is read once, 16 bytes per lane (the gate gradients in fp32: 4), held in
+// registers, and each output written once.
 #include <algorithm>
 
 #include "block_ops.h"
@@ -254,10 +254,16 @@ hipError_t launch_quant_rows(bool bf16_in, int rows, int K, const void* x, int l
 // ---------------------------------------------------------------------------
 // Query / key norm with rotation.  G lanes hold one head, 8 elements each (G = the
 // power of two at or above head_dim / 8, or nine); a group keeps one row's rotation and
-// takes HPG of its heads, all of whose loads are under way before the first norm.  9216
+// takes HPG of its heads, all of whose loads are under way before the first norm.  The
+// position, its table row and the two weights are loaded one after the other behind them,
+// and two of the rotation's values pass through scratch memory (the branches of
+// Rotor::load meet in one store): 12.6 of the 125.8 MB written below.  9216
 // rows of 48 heads of 128 42 - 52 us (4.5 - 5.4 TB/s; a copy 5.1), 4451 rows of 32 heads
 // of 72 10.8 us (3.8 TB/s; with 16 lanes of which nine work 13.0, 20000 rows of 28 heads
-// 39.3 -> 31.9 and backward 75.2 -> 54.3).
+// 39.3 -> 31.9 and backward 75.2 -> 54.3).  72, the cross-attention models' head size, has
+// the most to gain of the sizes between powers of two (7 heads to a wave instead of 4; 40
+// would have 12 instead of 8, 80 6 instead of 4, 96 5 instead of 4, 160 3 instead of 2);
+// those keep the power of two, and no other count was built or measured for them.
 
 // The rotation of a lane's elements.  Pairs (2j, 2j + 1): four pairs in the lane.
 // Halves (j, j + d/2): eight elements whose partners sit in another lane.
@@ -636,8 +642,8 @@ int gate_row_blocks(int M, int F) {
 
 extern "C" int t2i_test_gate_rows(int M, int F) { return M < 1 || F < 1 ? 0 : gate_rows(M, F); }
 
-// V columns per thread (8 where rows are whole 16-byte pieces, else 1): 32
-// threads side by side, 8 rows at a time
+// V columns per thread (bf16: 8, whose rows are whole 16-byte pieces; fp32, whose rows may
+// lie anywhere: 1): 32 threads side by side, 8 rows at a time
 template <typename T, int V>
 __global__ __launch_bounds__(256) void gate_grad_kernel(int act, int M, int F, int Fp, int rows,
                                                         const float* __restrict__ pre, int ldp,

@@ -67,3 +67,15 @@ def test_no_head_norm_kernel_that_no_call_reaches(kernels):
     assert all(forms.values())
     assert {int(m[2]) for m in forms.values() if m[3] == "1"} == {2, 4, 8, 16, 32}
     assert {int(m[2]) for m in forms.values() if m[3] == "0"} == {1, 2, 4, 8, 9, 16, 32}
+
+
+def test_block_operators_keep_their_registers(kernels):
+    """No spills but two registers of the widest dW tile, no scratch memory but that and
+    the head norms' three dwords (part of the rotation)."""
+    for name in ("linear_i8_kernel", "gated_linear_kernel", "gated_dx_kernel", "gated_dw_kernel", "split_sum_kernel",
+                 "quant_rows_kernel", "gate_grad_kernel", "gate_bias_grad_kernel", "qk_norm_rope_kernel",
+                 "qk_norm_rope_bwd_kernel", "qk_weight_grad_kernel"):
+        for k, v in find(kernels, name).items():
+            wide = name == "gated_dw_kernel" and "TileDimsILi256E" in k
+            assert v["vgpr_spill_count"] <= (2 if wide else 0), (k, v)
+            assert v["private_segment_fixed_size"] <= (12 if wide or "qk_norm_rope" in name else 0), (k, v)
