@@ -28,6 +28,7 @@ EPILOGUES = {"store": _lib.T2I_EPI_STORE, "gelu": _lib.T2I_EPI_GELU, "silu": _li
 ACTS = {"gelu": _lib.T2I_EPI_GELU, "silu": _lib.T2I_EPI_SILU}
 PAIRINGS = {"pairs": _lib.T2I_ROPE_PAIRS, "halves": _lib.T2I_ROPE_HALVES}
 _DTYPES = {torch.bfloat16: T2I_BF16, torch.float32: T2I_F32}
+_INT = 2 ** 31   # the library's sizes are 32-bit integers, and ctypes drops what lies above
 
 
 def _check(status: int):
@@ -53,12 +54,12 @@ def _device(first: torch.Tensor, *others) -> int:
     dev = first.get_device()
     if dev < 0:
         raise T2IError(1, "operands must be device tensors")
-    for t in others:
-        if t is not None and t.get_device() != dev:
-            raise T2IError(1, "operands must be device tensors of one device")
-    if torch.is_grad_enabled():
-        for t in (first, *others):
-            if t is not None and t.requires_grad:
+    followed = torch.is_grad_enabled()
+    for t in (first, *others):
+        if t is not None:
+            if t.get_device() != dev:
+                raise T2IError(1, "operands must be device tensors of one device")
+            if followed and t.requires_grad:
                 raise T2IError(1, "an operand requires a gradient, which this call does not record: "
                                   "detach it or call under torch.no_grad()")
     if getattr(forward_ad, "_current_level", 0) >= 0:   # (within a dual level)
@@ -71,9 +72,6 @@ def _device(first: torch.Tensor, *others) -> int:
 # A call's own work is a few microseconds, so the common case -- contiguous operands on
 # the current device, no stream given -- goes without strides, stream objects and
 # contexts.
-
-_INT = 2 ** 31   # the library's sizes are 32-bit integers, and ctypes drops what lies above
-
 
 def _rows(t: torch.Tensor, rows: int, cols: int, dtype, what: str) -> int:
     """Row stride of a matrix of this shape and type (its columns contiguous)."""
