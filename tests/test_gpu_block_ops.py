@@ -1056,3 +1056,44 @@ def test_bias_gradients_that_cancel(dtype):
     for act in ("silu", "gelu"):
         dbu = t2i.gated_linear_backward(dout, x, w, w, pre, act=act, bias=True)[4]
         assert (dbu == 64.0 * (M - 2)).all(), (act, dbu)
+
+
+# ------------------------------------------------------------------ beside automatic differentiation
+
+class Gated(torch.autograd.Function):
+    """The gated block as a program would record it: the calls in passes that record nothing."""
+
+    @staticmethod
+    def forward(ctx, x, wg, wu):
+        out, pre = t2i.gated_linear(x, wg, wu, act="gelu", save_pre=True)
+        ctx.save_for_backward(x, wg, wu, pre)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        return t2i.gated_linear_backward(dout, *ctx.saved_tensors, act="gelu")[:3]
+
+
+def test_calls_inside_an_autograd_function():
+    d, _ = gated_case(70, 72, 136, BF16, False, 180)
+    dout, _ = rnd(181, (70, 72), 1.0, BF16)
+    out, pre = t2i.gated_linear(d["x"], d["wg"], d["wu"], act="gelu", save_pre=True)
+    want = t2i.gated_linear_backward(dout, d["x"], d["wg"], d["wu"], pre, act="gelu")[:3]
+    leaves = [d[n].clone().requires_grad_() for n in ("x", "wg", "wu")]
+    with pytest.raises(t2i.T2IError):
+        t2i.gated_linear(*leaves, act="gelu")
+    y = Gated.apply(*leaves)
+    assert torch.equal(y, out)
+    y.backward(dout)
+    assert all(torch.equal(t.grad, g) for t, g in zip(leaves, want))
+    with torch.no_grad():
+        assert torch.equal(t2i.gated_linear(*leaves, act="gelu"), out)
+
+
+def test_a_saved_operand_overwritten_in_place_is_found():
+    q, k, wq, wk, rot = qk_case(37, 4, 2, 64, F32, "halves", 24, fused=False)
+    weight = torch.ones_like(q).requires_grad_()
+    y = (weight * q).sum()
+    t2i.qk_norm_rope(q, k, wq, wk, inplace=True, **rot)
+    with pytest.raises(RuntimeError, match="inplace"):
+        y.backward()
