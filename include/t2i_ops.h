@@ -304,6 +304,62 @@ t2i_status t2i_op_qk_norm_rope_backward(int32_t dtype, int32_t rows, int32_t hea
                                         void* stream);
 
 /*
+ * The residual's addition and an RMS norm in one pass:
+ *   h = resid + x,  r = 1 / sqrt(mean_k(h^2) + eps),  y = h r w,
+ * h rounded once to resid's type, which the norm takes then; statistics and
+ * products in fp32, y rounded once.
+ *   x [rows, K] (stride ldx), w [K] or NULL (ones), y [rows, K] (stride ldy) of
+ *   dtype; resid, h [rows, K] (strides ldr, ldh) of resid_dtype: dtype, or
+ *   T2I_F32 beside bf16 operands (a residual stream in fp32).  resid NULL: the
+ *   norm of x (h unused, resid_dtype must be dtype).  Any alignment and strides
+ *   of their types, K <= 2^20; fewer than 2^26 - 4 rows (K > 2048: 2^22).
+ *   h may be resid itself (same stride), y may be x; no other overlap of an
+ *   output with an input or another output.
+ * A row's results do not depend on the rows beside it.  Squares past fp32 make a
+ * row's y 0 (an infinity or a NaN in h: NaN); with eps 0 a row of zeros gives NaN.
+ */
+t2i_status t2i_op_add_rms_norm(int32_t dtype, int32_t resid_dtype, int32_t rows, int32_t K,
+                               const void* x, int32_t ldx, const void* resid, int32_t ldr,
+                               const void* w, float eps, void* h, int32_t ldh, void* y,
+                               int32_t ldy, void* stream);
+
+/*
+ * The same with y in 8 bits and a scale for every row, the input of
+ * t2i_op_linear_i8: with t = h w (exact) and T = max_k |t|,
+ *   scale = T r / 127 (fp32),
+ *   q[k] = 127 t[k] / T to the nearest whole number, ties to even, of the exact
+ *          quotient (-127 .. 127; zeros for T = 0): the norm's factor r is in
+ *          both and leaves it alone,
+ * so that q scale stands for y.  q [rows, ldq] as in t2i_op_quant_rows (16-byte
+ * aligned, ldq % 16 == 0, columns K .. K rounded up to 128 written as zeros).  A row
+ * whose h or products h w are not finite in fp32 gets scale NaN and q = 0.
+ */
+t2i_status t2i_op_add_rms_norm_i8(int32_t dtype, int32_t resid_dtype, int32_t rows, int32_t K,
+                                  const void* x, int32_t ldx, const void* resid, int32_t ldr,
+                                  const void* w, float eps, void* h, int32_t ldh, int8_t* q,
+                                  int32_t ldq, float* scale, void* stream);
+
+/*
+ * Gradients of t2i_op_add_rms_norm: dy [rows, K] (stride lddy) of dtype the
+ * gradient of y, h (stride ldh; without a residual x) and dh (stride lddh, or
+ * NULL: none), of resid_dtype, the sum and its gradient from elsewhere.  With
+ * n = h r, d = dy w:
+ *   dsum = dh + r (d - n mean_k(d n)), the gradient of x and of resid alike:
+ *   dx [rows, K] (stride lddx) of dtype, dresid (stride lddr) of resid_dtype, or
+ *   NULL where one type serves both;
+ *   dw [K] of dtype (or NULL) = sum over rows of dy n, in a fixed order.
+ * Sizes and alignment as forward.  dx may lie over dy or (of its type) dh,
+ * dresid over dh, same stride, if K <= 16384; no other overlap.  ws (with dw, else
+ * it may be NULL) as in t2i_op_gated_linear_backward.
+ */
+size_t t2i_op_add_rms_norm_backward_ws_bytes(int32_t rows, int32_t K);
+t2i_status t2i_op_add_rms_norm_backward(int32_t dtype, int32_t resid_dtype, int32_t rows, int32_t K,
+                                        const void* dy, int32_t lddy, const void* h, int32_t ldh,
+                                        const void* w, float eps, const void* dh, int32_t lddh,
+                                        void* dx, int32_t lddx, void* dresid, int32_t lddr,
+                                        void* dw, void* ws, size_t ws_bytes, void* stream);
+
+/*
  * Memory-counter calibration (not part of the denoising step): reads `bytes`
  * of src (device, 16-byte aligned; a multiple of 1024 below 2 GiB) exactly
  * once through the direct HBM -> LDS load path that the GEMM and attention

@@ -90,3 +90,39 @@ def qk_norm_rope_grads(dy, x, w, eps, table=None, pos=None, pairing="pairs"):
     dw = (dn * n).sum((0, 1))
     dn = dn * w
     return r * (dn - n * (dn * n).mean(-1, keepdims=True)), dw
+
+
+def add_rms_norm(h, w, eps):
+    """y of the sum h [rows, K]"""
+    return head_norm(h, 1.0 if w is None else w, eps)
+
+
+def add_rms_norm_i8(h, w, eps):
+    """(q int8, scale float64): t = h w, T = max|t|, scale = T / sqrt(mean h^2 + eps) / 127, q
+    the nearest whole number to 127 t / T, ties to even.  h and w are fp32 values, so that the
+    products fit float64 and 127 times them the 64 bits of a long double: exact."""
+    t = np.asarray(h, F64) * (1.0 if w is None else np.asarray(w, F64))
+    with np.errstate(over="ignore", invalid="ignore"):
+        ok = np.isfinite(np.asarray(h, F64)).all(1) & np.isfinite(t.astype(np.float32)).all(1)
+    ts = np.where(ok[:, None], t, 0.0)
+    top = np.abs(ts).max(1, keepdims=True)
+    L = np.longdouble
+    assert np.finfo(L).nmant >= 63
+    p, T = L(127) * np.abs(ts).astype(L), np.where(top > 0, top, 1.0).astype(L)
+    n = np.rint(p / T)
+    for side in (1, -1):
+        edge = (n + L(side) / 2) * T
+        over = (p > edge) | ((p == edge) & (n % 2 == 1)) if side > 0 else (p < edge) | ((p == edge) & (n % 2 == 1))
+        n = np.where(over, n + side, n)
+    q = np.where(top > 0, np.sign(ts) * n.astype(F64), 0.0).astype(np.int8)
+    with np.errstate(divide="ignore", invalid="ignore"):
+        s = top[:, 0] / np.sqrt((np.asarray(h, F64) ** 2).mean(1) + eps) / 127
+    return q, np.where(ok, s, np.nan)
+
+
+def add_rms_norm_grads(dy, h, w, dh, eps):
+    """(gradient of the sum, dw)"""
+    r = 1 / np.sqrt((h * h).mean(-1, keepdims=True) + eps)
+    n = h * r
+    d = dy * (1.0 if w is None else w)
+    return (0.0 if dh is None else dh) + r * (d - n * (d * n).mean(-1, keepdims=True)), (dy * n).sum(0)

@@ -124,6 +124,12 @@ SIGNATURES = {
     "t2i_op_qk_norm_rope_backward": (i32, [i32, i32, i32, i32, i32, vp, i32, vp, i32, vp, i32, vp,
                                            i32, vp, vp, f32, i32, vp, i32, vp, vp, i32, vp, i32,
                                            vp, vp, vp, sz, vp]),
+    "t2i_op_add_rms_norm": (i32, [i32, i32, i32, i32, vp, i32, vp, i32, vp, f32, vp, i32, vp, i32, vp]),
+    "t2i_op_add_rms_norm_i8": (i32, [i32, i32, i32, i32, vp, i32, vp, i32, vp, f32, vp, i32, vp, i32,
+                                     vp, vp]),
+    "t2i_op_add_rms_norm_backward_ws_bytes": (sz, [i32, i32]),
+    "t2i_op_add_rms_norm_backward": (i32, [i32, i32, i32, i32, vp, i32, vp, i32, vp, f32, vp, i32, vp,
+                                           i32, vp, i32, vp, vp, sz, vp]),
     "t2i_sched_create": (i32, [f64, C.POINTER(vp)]),
     "t2i_sched_destroy": (None, [vp]),
     "t2i_sched_submit": (i32, [vp, i32, C.c_int64, f64, f64, f64]),

@@ -103,4 +103,44 @@ hipError_t launch_qk_norm_rope_bwd(bool is_bf16, const QkNorm& a, float* partial
 hipError_t launch_qk_weight_grad(bool is_bf16, int blocks, int head_dim, const float* partial,
                                  void* dwq, void* dwk, hipStream_t st);
 
+// ---- the residual's addition with an RMS norm
+
+struct NormFwd {
+  int rows, K;
+  const void* x;
+  int ldx;
+  const void* resid;                 // or NULL: the norm of x
+  int ldr;
+  const void* w;                     // or NULL: ones
+  float eps;
+  void* h;                           // with resid
+  int ldh;
+  void* y;                           // or the codes
+  int ldy;
+  float* scale;                      // 8 bits
+};
+hipError_t launch_add_rms_norm(bool is_bf16, bool resid_bf16, bool to_i8, const NormFwd& a, hipStream_t st);
+
+struct NormBwd {
+  int rows, K;
+  const void* dy;
+  int lddy;
+  const void* h;
+  int ldh;
+  const void* w;                     // or NULL
+  float eps;
+  const void* dh;                    // or NULL
+  int lddh;
+  void* dx;
+  int lddx;
+  void* dresid;                      // or NULL
+  int lddr;
+  void* dw;                          // or NULL
+};
+// workgroups of the kernel that walks the rows: rows of its partial sums [blocks][K]
+int norm_bwd_blocks(int rows, int K);
+size_t norm_bwd_ws_bytes(int rows, int K);
+// ws: only with dw
+hipError_t launch_add_rms_norm_bwd(bool is_bf16, bool resid_bf16, const NormBwd& a, float* ws, hipStream_t st);
+
 }  // namespace t2i

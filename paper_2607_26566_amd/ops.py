@@ -348,3 +348,96 @@ def qk_norm_rope_backward(dq: torch.Tensor, dk: torch.Tensor, q: torch.Tensor, k
         _p(wq), _p(wk), eps, pr, _p(table), n_pos, _p(pos), oq.data_ptr(), hq * d, ok.data_ptr(), hk * d,
         _p(dwq), _p(dwk), _p(ws), n, _stream(dev)))
     return oq, ok, dwq, dwk
+
+
+def _norm_args(x, w, resid, what="x"):
+    dt = _of(_DTYPES, x.dtype, "dtype")
+    _need(x.dim() == 2, f"{what} must be [rows, K]")
+    rows, K = x.shape
+    ldx = _rows(x, rows, K, x.dtype, what)
+    _vec(w, K, x.dtype, "w")
+    if resid is None:
+        return dt, dt, rows, K, ldx, K
+    rt = _of(_DTYPES, resid.dtype, "the residual's dtype")
+    _need(rt in (dt, T2I_F32), "the residual must have the operands' dtype or be fp32", 1)
+    return dt, rt, rows, K, ldx, _rows(resid, rows, K, resid.dtype, "the residual")
+
+
+def _norm_sum(resid, rows, K, ldr, inplace):
+    """(tensor, pointer, stride) of the sum"""
+    if resid is None:
+        _need(not inplace, "inplace goes with a residual", 1)
+        return None, None, K
+    if inplace:
+        return resid, resid.data_ptr(), ldr
+    h = resid.new_empty((rows, K))
+    return h, h.data_ptr(), K
+
+
+def add_rms_norm(x: torch.Tensor, w: Optional[torch.Tensor] = None, resid: Optional[torch.Tensor] = None, *,
+                 eps: float = 1e-6, inplace: bool = False, stream=None) -> Tuple[torch.Tensor, torch.Tensor]:
+    """The residual's addition and an RMS norm (``t2i_op_add_rms_norm``): ``h = resid + x``,
+    ``y = h / sqrt(mean(h^2) + eps) * w`` for ``x [rows, K]``, ``w [K]`` (or None: ones) of
+    bf16 or fp32 and ``resid [rows, K]`` of that type or fp32.  Returns ``(y, h)``; with
+    ``inplace`` h is written over ``resid``; without a residual h is ``x``."""
+    dev = _device(x, w, resid)
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return add_rms_norm(x, w, resid, eps=eps, inplace=inplace)
+    dt, rt, rows, K, ldx, ldr = _norm_args(x, w, resid)
+    h, hp, ldh = _norm_sum(resid, rows, K, ldr, inplace)
+    y = x.new_empty((rows, K))
+    _check(load().t2i_op_add_rms_norm(dt, rt, rows, K, x.data_ptr(), ldx, _p(resid), ldr, _p(w), eps, hp, ldh,
+                                      y.data_ptr(), K, _stream(dev)))
+    if inplace:
+        _written(resid)
+    return y, (x if h is None else h)
+
+
+def add_rms_norm_i8(x: torch.Tensor, w: Optional[torch.Tensor] = None, resid: Optional[torch.Tensor] = None, *,
+                    eps: float = 1e-6, inplace: bool = False,
+                    stream=None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """:func:`add_rms_norm` with y in 8 bits (``t2i_op_add_rms_norm_i8``): ``(q int8 [rows, K
+    rounded up to 128], scale fp32 [rows], h)``, what :func:`linear_i8` takes."""
+    dev = _device(x, w, resid)
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return add_rms_norm_i8(x, w, resid, eps=eps, inplace=inplace)
+    dt, rt, rows, K, ldx, ldr = _norm_args(x, w, resid)
+    h, hp, ldh = _norm_sum(resid, rows, K, ldr, inplace)
+    ldq = (K + 127) // 128 * 128
+    q = x.new_empty((rows, ldq), dtype=torch.int8)
+    scale = x.new_empty(rows, dtype=torch.float32)
+    _check(load().t2i_op_add_rms_norm_i8(dt, rt, rows, K, x.data_ptr(), ldx, _p(resid), ldr, _p(w), eps, hp, ldh,
+                                         q.data_ptr(), ldq, scale.data_ptr(), _stream(dev)))
+    if inplace:
+        _written(resid)
+    return q, scale, (x if h is None else h)
+
+
+def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, w: Optional[torch.Tensor] = None,
+                          dh: Optional[torch.Tensor] = None, *, eps: float = 1e-6,
+                          stream=None) -> Tuple[torch.Tensor, Optional[torch.Tensor], Optional[torch.Tensor]]:
+    """Gradients of :func:`add_rms_norm` (``t2i_op_add_rms_norm_backward``) from y's, ``dy``,
+    the sum ``h`` that it returned and the gradient ``dh`` that reaches the sum from elsewhere
+    (or None): ``(dx, dresid, dw)``.  dx, of dy's type, is the gradient of x and of the
+    residual alike; where the residual is fp32 beside bf16 operands it comes in both types,
+    else dresid is None.  dw is None without a weight."""
+    dev = _device(dy, h, w, dh)
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return add_rms_norm_backward(dy, h, w, dh, eps=eps)
+    dt, rt, rows, K, lddy, ldh = _norm_args(dy, w, h, "dy")
+    lddh = K if dh is None else _rows(dh, rows, K, h.dtype, "dh")
+    lib = load()
+    dx = dy.new_empty((rows, K))
+    dresid = h.new_empty((rows, K)) if rt != dt else None
+    dw, n, ws = None, 0, None
+    if w is not None:
+        dw = w.new_empty(K)
+        n = lib.t2i_op_add_rms_norm_backward_ws_bytes(rows, K)
+        ws = dy.new_empty(n, dtype=torch.uint8)
+    _check(lib.t2i_op_add_rms_norm_backward(dt, rt, rows, K, dy.data_ptr(), lddy, h.data_ptr(), ldh, _p(w), eps,
+                                            _p(dh), lddh, dx.data_ptr(), K, _p(dresid), K, _p(dw), _p(ws), n,
+                                            _stream(dev)))
+    return dx, dresid, dw
