@@ -360,6 +360,57 @@ t2i_status t2i_op_add_rms_norm_backward(int32_t dtype, int32_t resid_dtype, int3
                                         void* dw, void* ws, size_t ws_bytes, void* stream);
 
 /*
+ * A linear layer shared by the rows of many requests, each with a low-rank adapter of
+ * its own or none (t2i_op_lora_merge changes W for everybody instead):
+ *   t[m] = s_i A_i x[m],  y[m] = W x[m] + bias + B_i t[m],  i = index[m],
+ * then the epilogues of t2i_op_linear.
+ *   x [M, K] (stride ldx), w [N, K] (stride ldw), bias [N] or NULL, a
+ *   [n][rank][K] and b [n][N][rank] (contiguous; adapters of smaller rank: zeros),
+ *   out [M, N] (stride ldo), t [M] rows (stride ldt), all of dtype; scale fp32 [n]
+ *   or NULL (ones); index (device, [M]) or NULL: every row takes adapter 0.  A row
+ *   whose index is not in 0 .. n - 1 takes no adapter.  The rest as t2i_op_linear.
+ *   Products and sums in fp32; t is rounded to dtype once (the second product's
+ *   operand), y once.  t receives rank columns and zeros up to rank rounded up to 32
+ *   (ldt at least that, % 8 == 0, 16-byte aligned): scratch memory, or kept for
+ *   t2i_op_adapter_linear_backward.
+ *   bf16: N, K, ldx, ldw % 8 == 0, x, w, a 16-byte aligned.  fp32: any sizes, strides
+ *   and alignment.  1 <= rank <= 128, n <= 32767, n max(N, K) rank < 2^33; M <= 2^24,
+ *   fewer than 2^23 pieces of 64 x 64 outputs; rows of x and w less than 8 MiB apart.
+ * Any order of the index; rows of one adapter next to each other are faster.  Nothing
+ * of another row's adapter enters a row's sums, not even as zeros.  No output may
+ * overlap an input or another output.
+ */
+t2i_status t2i_op_adapter_linear(int32_t dtype, int32_t epilogue, int32_t M, int32_t N, int32_t K,
+                                 const void* x, int32_t ldx, const void* w, int32_t ldw,
+                                 const void* bias, int32_t n, int32_t rank, const void* a,
+                                 const void* b, const float* scale, const int32_t* index, void* t,
+                                 int32_t ldt, void* out, int32_t ldo, float* resid, int32_t ldr,
+                                 void* resid_copy, const float* gate, void* stream);
+
+/*
+ * Gradients of t2i_op_adapter_linear (T2I_EPI_STORE) for adapters trained beside a frozen
+ * layer: with dy [M, N] (stride lddy) the gradient of y and t the forward pass's,
+ *   u[m] = s_i B_i^T dy[m],
+ *   dx[m] = W^T dy[m] + A_i^T u[m]   [M, K] (stride lddx),
+ *   da_i = sum over the rows of adapter i of u[m] x[m]^T   [n][rank][K],
+ *   db_i = sum of dy[m] t[m]^T   [n][N][rank],
+ * all of dtype; zeros for an adapter that no row takes.  u is rounded to dtype once;
+ * products and sums are fp32 or more, in a fixed order.  dx, da, db may each be NULL:
+ * not computed.  Sizes and alignment as forward (dy as x); b 16-byte aligned; the
+ * slices of the sums must fit a launch (T2I_ERR_SHAPE).  ws as in
+ * t2i_op_gated_linear_backward.  No output may overlap an input.
+ */
+size_t t2i_op_adapter_linear_backward_ws_bytes(int32_t dtype, int32_t M, int32_t N, int32_t K,
+                                               int32_t n, int32_t rank);
+t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, int32_t K,
+                                          const void* dy, int32_t lddy, const void* x, int32_t ldx,
+                                          const void* w, int32_t ldw, int32_t n, int32_t rank,
+                                          const void* a, const void* b, const float* scale,
+                                          const int32_t* index, const void* t, int32_t ldt,
+                                          void* dx, int32_t lddx, void* da, void* db, void* ws,
+                                          size_t ws_bytes, void* stream);
+
+/*
  * Memory-counter calibration (not part of the denoising step): reads `bytes`
  * of src (device, 16-byte aligned; a multiple of 1024 below 2 GiB) exactly
  * once through the direct HBM -> LDS load path that the GEMM and attention

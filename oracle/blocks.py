@@ -126,3 +126,32 @@ def add_rms_norm_grads(dy, h, w, dh, eps):
     n = h * r
     d = dy * (1.0 if w is None else w)
     return (0.0 if dh is None else dh) + r * (d - n * (d * n).mean(-1, keepdims=True)), (dy * n).sum(0)
+
+
+def adapter_rows(index, n, M):
+    """For every adapter the rows that take it (index None: all rows adapter 0's)"""
+    index = np.zeros(M, np.int64) if index is None else np.asarray(index)
+    return [np.nonzero(index == i)[0] for i in range(n)]
+
+
+def adapter_linear(x, w, a, b, bias=None, index=None, scale=None):
+    """(y, t): y = x w^T + bias + t b_i^T, t = s_i x a_i^T, i the row's adapter (t 0 without one)"""
+    y, t = x @ w.T, np.zeros((x.shape[0], a.shape[1]))
+    if bias is not None:
+        y = y + bias
+    for i, rows in enumerate(adapter_rows(index, a.shape[0], x.shape[0])):
+        t[rows] = (1.0 if scale is None else scale[i]) * x[rows] @ a[i].T
+        y[rows] += t[rows] @ b[i].T
+    return y, t
+
+
+def adapter_linear_grads(dy, x, w, a, b, index=None, scale=None):
+    """dict of dx, da, db, and u = s_i dy b_i"""
+    _, t = adapter_linear(x, w, a, b, None, index, scale)
+    dx, u = dy @ w, np.zeros_like(t)
+    da, db = np.zeros_like(a), np.zeros_like(b)
+    for i, rows in enumerate(adapter_rows(index, a.shape[0], x.shape[0])):
+        u[rows] = (1.0 if scale is None else scale[i]) * dy[rows] @ b[i]
+        dx[rows] += u[rows] @ a[i]
+        da[i], db[i] = u[rows].T @ x[rows], dy[rows].T @ t[rows]
+    return dict(dx=dx, da=da, db=db, u=u)

@@ -1,0 +1,716 @@
+// Low-rank adapters of many requests beside a shared linear layer, and the gradients of
+// both (gfx950).  Row m takes adapter i = index[m], or none:
+//   t = s_i x A_i^T,  y = x W^T + bias + t B_i^T.
+// Three kinds of kernels: the narrow products with A (and, for the gradients, B) that make
+// t, one row of 16 ranks per 16 x 16 MFMA tile or per wave; the shared product on the
+// tiles of gemm_tile.h, whose accumulators take t B^T before the epilogue; and the
+// adapters' own gradients, sums over the rows of each.
+//
+// Adapters never meet: a row's sums hold nothing of another row's adapter, not even
+// times zero (a NaN in one tenant's adapter stays in that tenant's rows).
+#include <algorithm>
+
+#include "block_gemm.h"
+#include "row_ops.h"
+
+namespace t2i {
+
+// the adapter of a row, -1: none (an index out of range takes none)
+__device__ __forceinline__ int adapter_of(const int32_t* index, int n, int row) {
+  const int i = index ? index[row] : 0;
+  return (unsigned)i < (unsigned)n ? i : -1;
+}
+
+// elements of a lane's 16 bytes: consecutive k of an MFMA operand
+template <typename T>
+constexpr int kLaneK = 16 / (int)sizeof(T);
+
+// 16 bytes at k of a row of `len` elements, `row` bytes behind base, 0 behind its end;
+// whole: len is a multiple of a piece
+template <typename T>
+__device__ __forceinline__ i32x4 load_k(const void* base, uint32_t row, int k, int len, bool whole) {
+  constexpr int L = kLaneK<T>;
+  typedef T piece __attribute__((ext_vector_type(kLaneK<T>), aligned(sizeof(T))));
+  const char* const p = (const char*)base;
+  const uint32_t at = row + (uint32_t)k * (uint32_t)sizeof(T);
+  i32x4 v = {0, 0, 0, 0};
+  if (whole ? k < len : k + L <= len) {
+    v = __builtin_bit_cast(i32x4, *(const piece*)(p + at));
+  } else if (!whole) {
+#pragma unroll
+    for (int i = 0; i < L; ++i)
+      if (k + i < len) {
+        const T e = *(const T*)(p + at + i * sizeof(T));
+        if constexpr (sizeof(T) == 2) v[i / 2] |= (int)((uint32_t)__builtin_bit_cast(uint16_t, e) << (16 * (i & 1)));
+        else v[i] = __float_as_int(e);
+      }
+  }
+  return v;
+}
+template <typename T>
+__device__ __forceinline__ float element(const i32x4& v, int i) {
+  if constexpr (sizeof(T) == 2)
+    return __uint_as_float(i & 1 ? (uint32_t)v[i / 2] & 0xffff0000u : (uint32_t)v[i / 2] << 16);
+  else
+    return __int_as_float(v[i]);
+}
+// c[j][m] += sum_k a[j][k] b[m][k], 32 (fp32: 16) of k: lane (x = lane & 15, g = lane >> 4)
+// gives k = L g .. of row x of both; it holds c[4 g + r][x]
+template <typename T>
+__device__ __forceinline__ f32x4 narrow_mfma(const i32x4& a, const i32x4& b, f32x4 c) {
+  if constexpr (sizeof(T) == 2) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0,
+                                                   0, 0);
+  } else {
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+      c = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(a[k]), __int_as_float(b[k]), c, 0, 0, 0);
+    return c;
+  }
+}
+
+// ---------------------------------------------------------------------------
+// t = s x A^T.  Few rows: a workgroup takes one row and four ranks, each wave a fourth of
+// k.
+template <typename T>
+__global__ __launch_bounds__(256) void adapter_down_rows_kernel(AdapterDown p) {
+  constexpr int RJ = 4;
+  __shared__ float red[4][RJ];
+  const int m = blockIdx.x, j0 = blockIdx.y * RJ, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int ad = adapter_of(p.index, p.n, m);
+  float s[RJ] = {0.f, 0.f, 0.f, 0.f};
+  if (ad >= 0 && j0 < p.rank) {
+    const T* const x = (const T*)p.x + (size_t)m * p.ldx;
+    const T* const a = (const T*)p.a + (size_t)ad * p.rank * p.K;
+#pragma unroll 2
+    for (int k = (wave * 64 + lane) * 8; k < p.K; k += 2048) {
+      Piece<T> px, pa[RJ];
+      load_piece(x, k, p.K, px);
+#pragma unroll
+      for (int j = 0; j < RJ; ++j) load_piece(a + (size_t)min(j0 + j, p.rank - 1) * p.K, k, p.K, pa[j]);
+#pragma unroll
+      for (int j = 0; j < RJ; ++j)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) s[j] = fmaf(px.get(e), pa[j].get(e), s[j]);
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < RJ; ++j) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) s[j] += __shfl_xor(s[j], o, kWave);
+    if (lane == 0) red[wave][j] = s[j];
+  }
+  __syncthreads();
+  const int j = threadIdx.x;
+  if (j >= RJ) return;
+  const float v = (red[0][j] + red[1][j]) + (red[2][j] + red[3][j]);
+  const float scale = ad >= 0 ? (p.scale ? p.scale[ad] : 1.f) : 0.f;
+  ((T*)p.t)[(size_t)m * p.ldt + j0 + j] = from_f32<T>(ad >= 0 && j0 + j < p.rank ? v * scale : 0.f);
+}
+
+// Many rows: a workgroup takes 16 rows and RT times 16 ranks, its waves a share of k each,
+// in blocks of 128 bytes: a lane's two pieces of a block are neighbours, so that the 16
+// rows' reads are whole lines; the order of k is the same for both operands.  Rows of
+// several adapters: one after the other.
+constexpr int kDownWaves = 8;
+template <typename T, int RT>
+__global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterDown p) {
+  constexpr int L = kLaneK<T>;
+  __shared__ f32x4 red[kDownWaves][RT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
+  const int m = blockIdx.x * 16 + fr, j0 = blockIdx.y * RT * 16, K = p.K;
+  const bool whole = K % L == 0;
+  const int ad = m < p.M ? adapter_of(p.index, p.n, m) : -1;
+  const T* const x = (const T*)p.x + (size_t)min(m, p.M - 1) * p.ldx;
+  // columns of t that this workgroup writes; rows without an adapter: zeros
+  auto store = [&](int jt, const f32x4& v) {
+    const int j = j0 + jt * 16 + g * 4;
+    float o[4];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) o[r] = j + r < p.rank ? v[r] : 0.f;
+    if (j < adapter_cols(p.rank)) store4((T*)p.t + (size_t)m * p.ldt + j, 4, o);
+  };
+  const bool behind = j0 >= p.rank;   // the zeros behind the ranks
+  if (wave == 0 && m < p.M && (ad < 0 || behind))
+    for (int jt = 0; jt < RT; ++jt) store(jt, f32x4{0.f, 0.f, 0.f, 0.f});
+  if (behind) return;
+  uint32_t left = (uint32_t)__ballot(ad >= 0) & 0xffffu;
+  while (left) {
+    const int now = __builtin_amdgcn_readlane(ad, __builtin_ctz(left));
+    const uint32_t mine = (uint32_t)__ballot(ad == now) & 0xffffu;
+    left &= ~mine;
+    const T* a[RT];
+#pragma unroll
+    for (int jt = 0; jt < RT; ++jt)
+      a[jt] = (const T*)p.a + ((size_t)now * p.rank + min(j0 + jt * 16 + fr, p.rank - 1)) * K;
+    f32x4 acc[RT];
+#pragma unroll
+    for (int jt = 0; jt < RT; ++jt) acc[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int k0 = wave * 8 * L; k0 < K; k0 += kDownWaves * 8 * L) {
+      const int k = k0 + 2 * g * L;
+      const i32x4 x0 = load_k<T>(x, 0, k, K, whole), x1 = load_k<T>(x, 0, k + L, K, whole);
+#pragma unroll
+      for (int jt = 0; jt < RT; ++jt) {
+        const i32x4 a0 = load_k<T>(a[jt], 0, k, K, whole), a1 = load_k<T>(a[jt], 0, k + L, K, whole);
+        acc[jt] = narrow_mfma<T>(a0, x0, acc[jt]);
+        acc[jt] = narrow_mfma<T>(a1, x1, acc[jt]);
+      }
+    }
+#pragma unroll
+    for (int jt = 0; jt < RT; ++jt) red[wave][jt][lane] = acc[jt];
+    __syncthreads();
+    if (wave < RT && ((mine >> fr) & 1)) {
+      f32x4 v = red[0][wave][lane];
+#pragma unroll
+      for (int w = 1; w < kDownWaves; ++w) v += red[w][wave][lane];
+      const float scale = p.scale ? p.scale[now] : 1.f;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) v[r] *= scale;
+      store(wave, v);
+    }
+    __syncthreads();
+  }
+}
+
+// rows up to which the first kernel takes them
+constexpr int kDownRows = 64;
+template <typename T>
+static void down_any(const AdapterDown& p, hipStream_t st) {
+  if (p.M <= kDownRows) {
+    hipLaunchKernelGGL((adapter_down_rows_kernel<T>), dim3((unsigned)p.M, (unsigned)(adapter_cols(p.rank) / 4)),
+                       dim3(256), 0, st, p);
+    return;
+  }
+  // all ranks in one workgroup where that leaves two for every CU: x is read once
+  const int mt = (p.M + 15) / 16, rt = adapter_cols(p.rank) / 16;
+#define T2I_DOWN(RT)                                                                                              \
+  hipLaunchKernelGGL((adapter_down_kernel<T, RT>), dim3((unsigned)mt, (unsigned)((rt + RT - 1) / RT)),            \
+                     dim3(64 * kDownWaves), 0, st, p)
+  if (p.rank <= 16 || mt < 256) T2I_DOWN(1);
+  else if (p.rank <= 32 || mt < 512) T2I_DOWN(2);
+  else T2I_DOWN(4);
+#undef T2I_DOWN
+}
+hipError_t launch_adapter_down(bool is_bf16, const AdapterDown& p, hipStream_t st) {
+  if (is_bf16) down_any<bf16>(p, st);
+  else down_any<float>(p, st);
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// acc += t P_i^T for the tile's rows, P_i [columns][stride] the adapter's second matrix
+// (forward: B; gradients: A transposed), both operands straight from memory.  A wave whose
+// rows have one adapter takes the matrix cores for all of them.  Rows of several: in the
+// largest tile, whose accumulators leave few registers, 16 rows at a time by the matrix
+// cores once for every adapter of theirs, of which each row takes its own, by way of
+// LDS; in the others a lane sums up its own row's products, all of whose loads are under
+// way at once.  smem: the tile's ring, which no wave reads any more.
+template <class P, class D, typename T>
+__device__ __forceinline__ void add_adapters(f32x4 (&acc)[D::TM][D::TN], char* smem, const AdapterUp& u, int m0, int n0,
+                                             int M, int N) {
+  constexpr int TM = D::TM, TN = D::TN, L = kLaneK<T>;
+  const int lane = threadIdx.x & 63, fr = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % D::NW);
+  const int mw = m0 + (wave / D::WGN) * D::WM, nw = n0 + (wave % D::WGN) * D::WN;
+  if (mw >= M || nw >= N) return;
+  const T* const t = (const T*)u.t + (size_t)mw * u.ldt;
+  const T* const p = (const T*)u.p + (size_t)nw * u.stride;
+  const bool whole = u.rank % L == 0;
+  // a row's adapter, -2 (any) behind the last row
+  auto id_of = [&](int i) {
+    const int m = mw + P::row_of(i, fr);
+    return m < M ? adapter_of(u.index, u.n, m) : -2;
+  };
+  // (t's and a matrix's rows of a wave span less than 2^31 bytes)
+  auto t_at = [&](int i, int k) {
+    return load_k<T>(t, (uint32_t)(min(P::row_of(i, fr), M - 1 - mw) * u.ldt) * (uint32_t)sizeof(T), k, u.ldt, true);
+  };
+  auto p_at = [&](const T* q, int j, int x, int k) {
+    return load_k<T>(q, (uint32_t)(min(P::col_of(j, x), N - 1 - nw) * u.stride) * (uint32_t)sizeof(T), k, u.rank, whole);
+  };
+  const size_t matrix = (size_t)N * u.stride;
+  const int first = __builtin_amdgcn_readfirstlane(id_of(0));   // (row mw exists)
+  bool same = true;
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int id = id_of(i);
+    same = same && (id == first || id == -2);
+  }
+  if (__all(same)) {
+    if (first < 0) return;
+    const T* const q = p + first * matrix;
+#pragma unroll 1
+    for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
+      i32x4 tv[TM];
+#pragma unroll
+      for (int i = 0; i < TM; ++i) tv[i] = t_at(i, k0 + g * L);
+#pragma unroll
+      for (int j = 0; j < TN; ++j) {
+        const i32x4 pv = p_at(q, j, fr, k0 + g * L);
+#pragma unroll
+        for (int i = 0; i < TM; ++i) acc[i][j] = narrow_mfma<T>(pv, tv[i], acc[i][j]);
+      }
+    }
+  } else if constexpr (TM * TN > 8) {
+    constexpr int HALF = TM / 2;
+    static_assert(D::NW * HALF * TN * 1024 <= D::RING, "room for half of the results");
+    f32x4* const part = (f32x4*)(smem + wave * HALF * TN * 1024) + lane;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll 1
+      for (int i = 0; i < HALF; ++i) {
+        const int id = id_of(h * HALF + i);
+        uint32_t left = (uint32_t)__ballot(id >= 0) & 0xffffu;
+        f32x4 sum[TN];
+#pragma unroll
+        for (int j = 0; j < TN; ++j) sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+        while (left) {
+          const int now = __builtin_amdgcn_readlane(id, __builtin_ctz(left));
+          left &= ~(uint32_t)__ballot(id == now);
+          const T* const q = p + now * matrix;
+          f32x4 add[TN];
+#pragma unroll
+          for (int j = 0; j < TN; ++j) add[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+          for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
+            const i32x4 tv = t_at(h * HALF + i, k0 + g * L);
+#pragma unroll
+            for (int j = 0; j < TN; ++j) add[j] = narrow_mfma<T>(p_at(q, j, fr, k0 + g * L), tv, add[j]);
+          }
+#pragma unroll
+          for (int j = 0; j < TN; ++j)
+#pragma unroll
+            for (int r = 0; r < 4; ++r) sum[j][r] = id == now ? add[j][r] : sum[j][r];
+        }
+#pragma unroll
+        for (int j = 0; j < TN; ++j) part[(i * TN + j) * 64] = sum[j];
+      }
+#pragma unroll
+      for (int i = 0; i < HALF; ++i)
+#pragma unroll
+        for (int j = 0; j < TN; ++j) acc[h * HALF + i][j] += part[(i * TN + j) * 64];
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      const int id = id_of(i);
+      if (id < 0) continue;
+      const T* const q = p + id * matrix;
+#pragma unroll 1
+      for (int k = 0; k < u.rank; k += L) {
+        const i32x4 tv = t_at(i, k);
+#pragma unroll
+        for (int j = 0; j < TN; ++j)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const i32x4 pv = p_at(q, j, g * 4 + r, k);
+#pragma unroll
+            for (int e = 0; e < L; ++e) acc[i][j][r] = fmaf(element<T>(tv, e), element<T>(pv, e), acc[i][j][r]);
+          }
+      }
+    }
+  }
+}
+
+// y = x W^T + t B^T + bias, then the linear layer's epilogues
+template <class D, typename T, bool RES, bool U>
+__global__ __launch_bounds__(D::THREADS, 1) void adapter_linear_kernel(TileOperand a, TileOperand b, TileShape s,
+                                                                       AdapterUp up, LinearEpi e, int M, int N) {
+  using P = TileProduct<D, elem_of<T>(), false, false, false, false, U>;
+  constexpr int THREADS = D::THREADS, NE = (RES ? 2 : 1) * D::BN;
+  __shared__ __attribute__((aligned(1024))) char smem[D::KG * D::RING + NE * 4];
+  int tm, tn;
+  tile_place(s, blockIdx.x, gridDim.x, tm, tn);
+  const int m0 = tm * D::BM, n0 = tn * D::BN;
+  auto value = [&](int x) -> float {
+    const int n = min(n0 + x % D::BN, N - 1);
+    if (x < D::BN) return e.bias ? to_f32(((const T*)e.bias)[n]) : 0.f;
+    return e.kind == EPI_RESID_GATED ? e.gate[n] : 1.f;
+  };
+  Staged<NE, THREADS, decltype(value)> st;
+  st.fetch(value);
+  typename P::Acc acc[D::TM][D::TN];
+  const bool mine = P::run_groups(smem, a, b, s, m0, n0, acc);
+  float* const ev = (float*)(smem + D::KG * D::RING);
+  st.put(ev);
+  tile_barrier();
+  if (!mine) return;
+  add_adapters<P, D, T>(acc, smem, up, m0, n0, M, N);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
+  const int mw = (wave / D::WGN) * D::WM, nw = (wave % D::WGN) * D::WN;
+#pragma unroll
+  for (int i = 0; i < D::TM; ++i) {
+    const int m = m0 + mw + i * 16 + fr;
+    if (m >= M) continue;
+#pragma unroll
+    for (int j = 0; j < D::TN; ++j) {
+      const int nl = nw + j * 16 + g * 4, n = n0 + nl, left = N - n;
+      if (left <= 0) continue;
+      const f32x4 bb = *(const f32x4*)(ev + nl);
+      float y[4];
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        y[r] = acc[i][j][r] + bb[r];
+        if (!RES) y[r] = e.kind == EPI_GELU ? gelu_tanh(y[r]) : e.kind == EPI_SILU ? silu(y[r]) : y[r];
+      }
+      if constexpr (RES) {
+        float* x = e.x + (size_t)m * e.ldx + n;
+        const f32x4 gt = *(const f32x4*)(ev + D::BN + nl);
+        float xv[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) xv[r] = r < left ? x[r] + gt[r] * y[r] : 0.f;
+        store4(x, left, xv);
+        if (e.xb) store4(e.xb + (size_t)m * e.ldx + n, left, xv);
+      } else {
+        store4((T*)e.out + (size_t)m * e.ldo + n, left, y);
+      }
+    }
+  }
+}
+
+// dx = dy W + u A; where the contraction is split, the first slice takes the adapters
+template <class D, typename T, bool U>
+__global__ __launch_bounds__(D::THREADS, 1) void adapter_dx_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
+                                                                   AdapterUp up, T* dx, int ldx, int M, int K) {
+  using P = TileProduct<D, elem_of<T>(), false, true, false, false, U>;
+  __shared__ __attribute__((aligned(1024))) char smem[D::RING];
+  int tm, tn;
+  tile_place(s, blockIdx.x, gridDim.x, tm, tn);
+  if (sp.partial) take_slice(sp, s);
+  typename P::Acc acc[D::TM][D::TN];
+  const int m0 = tm * D::BM, n0 = first_column<D, U>(tn, K);
+  P::run(smem, a, b, s, m0, n0, acc);
+  if (blockIdx.y == 0) {
+    tile_barrier();
+    add_adapters<P, D, T>(acc, smem, up, m0, n0, M, K);
+  }
+  if (sp.partial)
+    store_tile<D, P>(acc, sp.partial + (size_t)blockIdx.y * M * sp.ld, sp.ld, m0, n0, M, K);
+  else
+    store_tile<D, P>(acc, dx, ldx, m0, n0, M, K);
+}
+
+template <class D, typename T, bool U = false>
+static void adapter_linear_launch(const void* x, int ldx, const void* w, int ldw, int M, int N, int K,
+                                  const AdapterUp& up, const LinearEpi& e, hipStream_t st) {
+  constexpr int eb = sizeof(T), per = 128 / eb;
+  const TileOperand a{(const char*)x, nullptr, (uint32_t)eb * ldx, M, 0}, b{(const char*)w, nullptr, (uint32_t)eb * ldw, N, 0};
+  const TileShape s = tile_shape<D>(M, N, (K + per - 1) / per, eb * K, 0);
+  const dim3 grid((unsigned)(s.tiles_m * s.tiles_n));
+  if (e.kind >= EPI_RESID)
+    hipLaunchKernelGGL((adapter_linear_kernel<D, T, true, U>), grid, dim3(D::THREADS), 0, st, a, b, s, up, e, M, N);
+  else
+    hipLaunchKernelGGL((adapter_linear_kernel<D, T, false, U>), grid, dim3(D::THREADS), 0, st, a, b, s, up, e, M, N);
+}
+
+hipError_t launch_adapter_linear(bool is_bf16, const void* x, int ldx, const void* w, int ldw, int M, int N, int K,
+                                 const AdapterUp& up, const LinearEpi& e, hipStream_t st) {
+  const int shape = is_bf16 ? tile_index(M, N, (K + 63) / 64, 1.f) : tile_index_f32(M, N, (K + 31) / 32);
+  if (is_bf16) {
+    T2I_TILES_FWD(shape, (adapter_linear_launch<D, bf16>(x, ldx, w, ldw, M, N, K, up, e, st)))
+  } else if (f32_pieces({K, ldx, ldw}, {x, w})) {
+    T2I_TILES_F32_FWD(shape, (adapter_linear_launch<D, float>(x, ldx, w, ldw, M, N, K, up, e, st)))
+  } else {
+    T2I_TILES_F32_FWD(shape, (adapter_linear_launch<D, float, true>(x, ldx, w, ldw, M, N, K, up, e, st)))
+  }
+  return hipGetLastError();
+}
+
+size_t adapter_dx_floats(bool is_bf16, int M, int N, int K) {
+  const SplitPick p = split_dx(is_bf16, M, K, N);
+  return p.slices > 1 ? (size_t)p.slices * M * whole4(K) : 0;
+}
+
+template <class D, typename T, bool U = false>
+static void adapter_dx_launch(const void* dy, int lddy, const void* w, int ldw, int M, int N, int K, const AdapterUp& up,
+                              T* dx, int ldx, const SplitPick& pick, const Split& sp, hipStream_t st) {
+  constexpr int eb = sizeof(T), per = 128 / eb;
+  const TileOperand a{(const char*)dy, nullptr, (uint32_t)eb * lddy, M, 0}, b{(const char*)w, nullptr, (uint32_t)eb * ldw, N, K};
+  const TileShape s = tile_shape<D>(M, K, (N + per - 1) / per, eb * N, 0);
+  hipLaunchKernelGGL((adapter_dx_kernel<D, T, U>), dim3((unsigned)(s.tiles_m * s.tiles_n), pick.slices), dim3(D::THREADS), 0,
+                     st, a, b, s, sp, up, dx, ldx, M, K);
+  if (sp.partial) split_sum(sp, pick.slices, M, M, K, dx, dx, ldx, st);
+}
+
+hipError_t launch_adapter_dx(bool is_bf16, const void* dy, int lddy, const void* w, int ldw, int M, int N, int K,
+                             const AdapterUp& up, void* dx, int ldx, float* partial, hipStream_t st) {
+  const SplitPick pick = split_dx(is_bf16, M, K, N);
+  const Split sp{pick.slices > 1 ? partial : nullptr, pick.per, (int)whole4(K)};
+  if (is_bf16) {
+    T2I_TILES(pick.shape, (adapter_dx_launch<D, bf16>(dy, lddy, w, ldw, M, N, K, up, (bf16*)dx, ldx, pick, sp, st)))
+  } else if (f32_pieces({N, K, lddy, ldw}, {dy, w})) {
+    T2I_TILES_F32_DX(pick.shape,
+                     (adapter_dx_launch<D, float>(dy, lddy, w, ldw, M, N, K, up, (float*)dx, ldx, pick, sp, st)))
+  } else {
+    T2I_TILES_F32_DX(pick.shape,
+                     (adapter_dx_launch<D, float, true>(dy, lddy, w, ldw, M, N, K, up, (float*)dx, ldx, pick, sp, st)))
+  }
+  return hipGetLastError();
+}
+
+// ---------------------------------------------------------------------------
+// The adapters' matrices turned for the gradients: out[i][c][r] = in[i][r][c] for rows r <
+// R, 0 for R <= r < stride; a thread writes 8 values of a row of out.
+template <typename T>
+__global__ __launch_bounds__(256) void adapter_turn_kernel(const T* __restrict__ in, T* __restrict__ out, int R, int C,
+                                                           int stride) {
+  const long chunks = (stride + 7) / 8, x = blockIdx.x * 256L + threadIdx.x;
+  if (x >= chunks * C) return;
+  const int c = (int)(x % C), r0 = (int)(x / C) * 8;
+  const T* const p = in + (size_t)blockIdx.y * R * C + c;
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = r0 + i < R ? to_f32(p[(size_t)(r0 + i) * C]) : 0.f;
+  store_piece(out + ((size_t)blockIdx.y * C + c) * stride + r0, stride - r0, v);
+}
+template <typename T>
+static void turn_any(const T* in, T* out, int n, int R, int C, int stride, hipStream_t st) {
+  const long x = (long)((stride + 7) / 8) * C;
+  hipLaunchKernelGGL((adapter_turn_kernel<T>), dim3((unsigned)((x + 255) / 256), (unsigned)n), dim3(256), 0, st, in, out,
+                     R, C, stride);
+}
+hipError_t launch_adapter_turn(bool is_bf16, const void* in, void* out, int n, int R, int C, int stride,
+                               hipStream_t st) {
+  if (is_bf16) turn_any((const bf16*)in, (bf16*)out, n, R, C, stride, st);
+  else turn_any((const float*)in, (float*)out, n, R, C, stride, st);
+  return hipGetLastError();
+}
+
+// The rows of every adapter, in ascending order: adapter i's are order[start .. start +
+// count), (start, count) = span[i].  Cut at every multiple of `per` these are the slices of
+// the gradients' sums; slice b of adapter i has number b + i in `slices` (adapter, first,
+// rows), so that each number up to M / per + n is written by one workgroup, empty ones
+// too.  A workgroup per adapter reads the whole index twice.
+__global__ __launch_bounds__(1024) void adapter_group_kernel(const int32_t* __restrict__ index, int M, int n, int per,
+                                                             int32_t* __restrict__ order, int2* __restrict__ span,
+                                                             int4* __restrict__ slices) {
+  __shared__ int red[2][16];
+  const int ad = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  int before = 0, mine = 0;
+  for (int m = threadIdx.x; m < M; m += 1024) {
+    const int i = adapter_of(index, n, m);
+    before += i >= 0 && i < ad;
+    mine += i == ad;
+  }
+#pragma unroll
+  for (int o = 32; o >= 1; o >>= 1) {
+    before += __shfl_xor(before, o, kWave);
+    mine += __shfl_xor(mine, o, kWave);
+  }
+  if (lane == 0) red[0][wave] = before, red[1][wave] = mine;
+  __syncthreads();
+  int start = 0, count = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) start += red[0][w], count += red[1][w];
+  if (threadIdx.x == 0) span[ad] = int2{start, count};
+  // (the last adapter's also write the numbers that rows without an adapter leave over)
+  const int end = start + count, last = ad == n - 1 ? M / per : end / per;
+  for (int b = start / per + (int)threadIdx.x; b <= last; b += 1024) {
+    const int lo = max(start, b * per), hi = min(end, (b + 1) * per);
+    slices[b + ad] = int4{ad, lo, max(hi - lo, 0), 0};
+  }
+  int at = start;
+  for (int m0 = 0; m0 < M; m0 += 1024) {
+    const int m = m0 + (int)threadIdx.x;
+    const bool hit = m < M && adapter_of(index, n, m) == ad;
+    const uint64_t all = __ballot(hit);
+    __syncthreads();   // (the counts of the round before, or of the sums, are read)
+    if (lane == 0) red[0][wave] = __popcll(all);
+    __syncthreads();
+    int skip = 0, sum = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) {
+      skip += w < wave ? red[0][w] : 0;
+      sum += red[0][w];
+    }
+    if (hit) order[at + skip + __popcll(all & ((1ULL << lane) - 1))] = m;
+    at += sum;
+  }
+}
+
+hipError_t launch_adapter_group(const int32_t* index, int M, int n, int per, int32_t* order, int2* span, int4* slices,
+                                hipStream_t st) {
+  hipLaunchKernelGGL(adapter_group_kernel, dim3((unsigned)n), dim3(1024), 0, st, index, M, n, per, order, span, slices);
+  return hipGetLastError();
+}
+
+// rows of a slice: as many as leave two workgroups for every CU, at least a step of four
+// waves and at most 1024
+int adapter_slice_rows(bool is_bf16, int M, int N, int K, int rank) {
+  const int cols = is_bf16 ? 128 : 64;
+  const long wide = (long)((K + cols - 1) / cols + (N + cols - 1) / cols) * ((rank + 31) / 32);
+  int per = 1024;
+  while (per > 128 && (M + per - 1) / per * wide < 1024) per /= 2;
+  return per;
+}
+
+// One slice's part of the gradients: partial[slice][j][c] = sum over its rows of v[m, j]
+// z[m, c], with (z, v) = (x, u) for dA and (dy, t) for dB, side by side in the grid.  A
+// wave takes every fourth step of 32 (fp32: 16) of the slice's rows and 128 (64)
+// columns: a lane reads 16 bytes of each of its 8 (4) rows and joins the halves of
+// their dwords by v_perm, which gives it 8 (4) k of 8 (4) neighbouring columns, the
+// operands of as many MFMAs; z is read once for 32 ranks.
+template <typename T, int RT>
+__global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterOuter p) {
+  constexpr int L = kLaneK<T>, STEP = 4 * L, COLS = 16 * L;
+  __shared__ f32x4 red[3][RT][64];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
+  const bool second = (int)blockIdx.x >= p.blocks0;
+  const AdapterSide& d = second ? p.side[1] : p.side[0];
+  const int c0 = ((int)blockIdx.x - (second ? p.blocks0 : 0)) * COLS + fr * L, C = d.cols, j0 = blockIdx.z * RT * 16;
+  int first, rows;
+  if (p.slices) {
+    const int4 sl = p.slices[blockIdx.y];
+    first = sl.y, rows = sl.z;
+  } else {
+    first = blockIdx.y * p.per, rows = min(p.per, p.M - first);
+  }
+  if (rows <= 0) return;
+  const T* const z = (const T*)d.z;
+  const T* const v = (const T*)d.v;
+  const bool in = c0 < C, part = c0 + L > C;
+  f32x4 acc[L][RT];
+#pragma unroll
+  for (int q = 0; q < L; ++q)
+#pragma unroll
+    for (int jt = 0; jt < RT; ++jt) acc[q][jt] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+  for (int r0 = wave * STEP; r0 < rows; r0 += 4 * STEP) {
+    i32x4 raw[L], vv[RT];
+    int row[L];
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      const int at = r0 + g * L + i;
+      row[i] = at < rows ? (p.order ? p.order[first + at] : first + at) : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < L; ++i) {
+      raw[i] = i32x4{0, 0, 0, 0};
+      if (row[i] >= 0 && in) raw[i] = load_k<T>(z + (size_t)row[i] * d.ldz, 0, c0, C, !part);
+    }
+#pragma unroll
+    for (int jt = 0; jt < RT; ++jt) {
+      vv[jt] = i32x4{0, 0, 0, 0};
+      const int j = min(j0 + jt * 16 + fr, d.ldv - 1);
+#pragma unroll
+      for (int i = 0; i < L; ++i)
+        if (row[i] >= 0) {
+          const T e = v[(size_t)row[i] * d.ldv + j];
+          if constexpr (sizeof(T) == 2) vv[jt][i / 2] |= (int)((uint32_t)__builtin_bit_cast(uint16_t, e) << (16 * (i & 1)));
+          else vv[jt][i] = __float_as_int(e);
+        }
+    }
+#pragma unroll
+    for (int q = 0; q < L; ++q) {
+      i32x4 f;
+      if constexpr (sizeof(T) == 2) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          f[w] = __builtin_amdgcn_perm(raw[2 * w + 1][q / 2], raw[2 * w][q / 2], q & 1 ? 0x07060302 : 0x05040100);
+      } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) f[w] = raw[w][q];
+      }
+#pragma unroll
+      for (int jt = 0; jt < RT; ++jt) acc[q][jt] = narrow_mfma<T>(vv[jt], f, acc[q][jt]);
+    }
+  }
+  // lane (fr, g) holds ranks 4 g + r of column c0 + q: the other waves' sums by way of LDS,
+  // in ascending order
+#pragma unroll
+  for (int q = 0; q < L; ++q) {
+    __syncthreads();
+    if (wave > 0) {
+#pragma unroll
+      for (int jt = 0; jt < RT; ++jt) red[wave - 1][jt][lane] = acc[q][jt];
+    }
+    __syncthreads();
+    if (wave == 0) {
+#pragma unroll
+      for (int w = 0; w < 3; ++w)
+#pragma unroll
+        for (int jt = 0; jt < RT; ++jt) acc[q][jt] += red[w][jt][lane];
+    }
+  }
+  if (wave > 0 || !in) return;
+  float* const out = d.partial + (size_t)blockIdx.y * p.ranks * d.ldp + c0;
+#pragma unroll
+  for (int jt = 0; jt < RT; ++jt)
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      const int j = j0 + jt * 16 + g * 4 + r;
+      if (j >= p.ranks) continue;
+#pragma unroll
+      for (int q = 0; q < L; q += 4)   // (rows of ldp columns, a multiple of a lane's)
+        *(f32x4*)(out + (size_t)j * d.ldp + q) = f32x4{acc[q][jt][r], acc[q + 1][jt][r], acc[q + 2][jt][r], acc[q + 3][jt][r]};
+    }
+}
+
+// dA [n][rank][K] and dB [n][N][rank]: the slices' parts of every adapter, added up in
+// fp64 in ascending order; zeros for an adapter without rows.  A thread takes four
+// columns of one rank (dA), or of four (dB).
+template <typename T>
+__global__ __launch_bounds__(256) void adapter_sum_kernel(AdapterOuter p, T* dA, T* dB, int per_a, int per_b) {
+  const int ad = blockIdx.y;
+  const int2 span = p.span ? p.span[ad] : int2{0, ad == 0 ? p.M : 0};
+  const int b0 = span.x / p.per, b1 = span.y > 0 ? (span.x + span.y - 1) / p.per + 1 : b0;
+  const bool is_b = (int)blockIdx.x >= per_a;
+  const long x = ((int)blockIdx.x - (is_b ? per_a : 0)) * 256L + threadIdx.x;
+  const AdapterSide& d = is_b ? p.side[1] : p.side[0];
+  const int c4 = (d.cols + 3) / 4;
+  const int c = (int)(x % c4) * 4, jn = is_b ? 4 : 1, j0 = (int)(x / c4) * jn;
+  if (j0 >= p.rank) return;
+  double s[4][4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) s[j][e] = 0.;
+  for (int b = b0; b < b1; ++b) {
+    const float* const at = d.partial + ((size_t)(b + ad) * p.ranks + j0) * d.ldp + c;
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      if (j < jn) {
+        const f32x4 v = *(const f32x4*)(at + (size_t)j * d.ldp);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) s[j][e] += (double)v[e];
+      }
+  }
+  if (!is_b) {
+    const float v[4] = {(float)s[0][0], (float)s[0][1], (float)s[0][2], (float)s[0][3]};
+    store4(dA + ((size_t)ad * p.rank + j0) * d.cols + c, d.cols - c, v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (c + e >= d.cols) break;
+      const float v[4] = {(float)s[0][e], (float)s[1][e], (float)s[2][e], (float)s[3][e]};
+      store4(dB + ((size_t)ad * d.cols + c + e) * p.rank + j0, p.rank - j0, v);
+    }
+  }
+}
+
+template <typename T>
+static void outer_any(AdapterOuter p, int n, int slices, T* dA, T* dB, hipStream_t st) {
+  constexpr int COLS = 16 * kLaneK<T>;
+  const int blocks1 = dB ? (p.side[1].cols + COLS - 1) / COLS : 0;
+  p.blocks0 = dA ? (p.side[0].cols + COLS - 1) / COLS : 0;
+  if (p.rank <= 16)
+    hipLaunchKernelGGL((adapter_outer_kernel<T, 1>), dim3((unsigned)(p.blocks0 + blocks1), (unsigned)slices, 1), dim3(256),
+                       0, st, p);
+  else
+    hipLaunchKernelGGL((adapter_outer_kernel<T, 2>),
+                       dim3((unsigned)(p.blocks0 + blocks1), (unsigned)slices, (unsigned)((p.rank + 31) / 32)), dim3(256), 0,
+                       st, p);
+  auto blocks = [&](int cols, int per) { return (int)(((long)((cols + 3) / 4) * ((p.rank + per - 1) / per) + 255) / 256); };
+  const int a = dA ? blocks(p.side[0].cols, 1) : 0, b = dB ? blocks(p.side[1].cols, 4) : 0;
+  hipLaunchKernelGGL((adapter_sum_kernel<T>), dim3((unsigned)(a + b), (unsigned)n), dim3(256), 0, st, p, dA, dB, a, b);
+}
+hipError_t launch_adapter_outer(bool is_bf16, const AdapterOuter& p, int n, int slices, void* dA, void* dB,
+                                hipStream_t st) {
+  if (is_bf16) outer_any(p, n, slices, (bf16*)dA, (bf16*)dB, st);
+  else outer_any(p, n, slices, (float*)dA, (float*)dB, st);
+  return hipGetLastError();
+}
+
+}  // namespace t2i

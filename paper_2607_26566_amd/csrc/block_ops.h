@@ -143,4 +143,72 @@ size_t norm_bwd_ws_bytes(int rows, int K);
 // ws: only with dw
 hipError_t launch_add_rms_norm_bwd(bool is_bf16, bool resid_bf16, const NormBwd& a, float* ws, hipStream_t st);
 
+// ---- low-rank adapters of many requests beside a shared linear layer
+
+// columns of t and of the gradients' u: rank rounded up, zeros behind it
+__host__ __device__ inline int adapter_cols(int rank) { return (rank + 31) / 32 * 32; }
+
+// t = s x a^T: x [M, K], a [n][rank][K], t [M][ldt], ldt >= adapter_cols(rank)
+struct AdapterDown {
+  int M, K, n, rank;
+  const void* x;
+  int ldx;
+  const void* a;
+  const float* scale;                // [n] or NULL: ones
+  const int32_t* index;              // [M] or NULL: adapter 0
+  void* t;
+  int ldt;
+};
+hipError_t launch_adapter_down(bool is_bf16, const AdapterDown& p, hipStream_t st);
+
+// the product with the adapters' second matrices p [n][columns][stride], `rank` of which
+// count
+struct AdapterUp {
+  const int32_t* index;
+  int n, rank, stride;
+  const void* p;
+  const void* t;
+  int ldt;
+};
+struct LinearEpi {
+  int kind;                          // EPI_STORE .. EPI_RESID_GATED
+  const void* bias;                  // or NULL
+  void* out;
+  int ldo;
+  float* x;                          // residual
+  int ldx;
+  bf16* xb;                          // or NULL
+  const float* gate;
+};
+hipError_t launch_adapter_linear(bool is_bf16, const void* x, int ldx, const void* w, int ldw, int M, int N, int K,
+                                 const AdapterUp& up, const LinearEpi& e, hipStream_t st);
+// dx = dy W + u A; fp32 room that it needs at `partial`
+size_t adapter_dx_floats(bool is_bf16, int M, int N, int K);
+hipError_t launch_adapter_dx(bool is_bf16, const void* dy, int lddy, const void* w, int ldw, int M, int N, int K,
+                             const AdapterUp& up, void* dx, int ldx, float* partial, hipStream_t st);
+// out [n][C][stride] = in [n][R][C] turned, zeros behind R
+hipError_t launch_adapter_turn(bool is_bf16, const void* in, void* out, int n, int R, int C, int stride,
+                               hipStream_t st);
+// the rows of every adapter, and slices of them of at most `per` rows
+int adapter_slice_rows(bool is_bf16, int M, int N, int K, int rank);
+hipError_t launch_adapter_group(const int32_t* index, int M, int n, int per, int32_t* order, int2* span, int4* slices,
+                                hipStream_t st);
+// dA, dB (either may be NULL)
+struct AdapterSide {
+  const void *z, *v;                 // [M, cols], [M, ldv]
+  int ldz, ldv, cols;
+  float* partial;                    // [slices][ranks][ldp]
+  int ldp;                           // cols in whole pieces of eight
+};
+struct AdapterOuter {
+  AdapterSide side[2];               // dA: (x, u), dB: (dy, t)
+  int M, per, rank, ranks;           // ranks: rank in whole pieces of four
+  int blocks0;
+  const int32_t* order;              // NULL: all rows are adapter 0's
+  const int2* span;
+  const int4* slices;
+};
+hipError_t launch_adapter_outer(bool is_bf16, const AdapterOuter& p, int n, int slices, void* dA, void* dB,
+                                hipStream_t st);
+
 }  // namespace t2i

@@ -441,3 +441,86 @@ def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, w: Optional[torch.T
                                             _p(dh), lddh, dx.data_ptr(), K, _p(dresid), K, _p(dw), _p(ws), n,
                                             _stream(dev)))
     return dx, dresid, dw
+
+
+def _adapter_args(x, w, a, b, index, scale):
+    dt = _of(_DTYPES, x.dtype, "dtype")
+    _need(x.dim() == 2 and w.dim() == 2 and a.dim() == 3, "x and w must be matrices, a [n, rank, K]")
+    (M, K), N, (n, r, _) = x.shape, w.shape[0], a.shape
+    ldx, ldw = _rows(x, M, K, x.dtype, "x"), _rows(w, N, K, x.dtype, "w")
+    for t, shape, what in ((a, (n, r, K), "a"), (b, (n, N, r), "b")):
+        if t.dtype is not x.dtype or t.shape != shape or not t.is_contiguous():
+            raise T2IError(2, f"{what}: expected {shape} {x.dtype}, contiguous")
+    _need(n < _INT and r < _INT, "2^31 adapters or ranks, or more")
+    _vec(index, M, torch.int32, "index")
+    _vec(scale, n, torch.float32, "scale")
+    return dt, M, N, K, n, r, ldx, ldw
+
+
+def adapter_linear(x: torch.Tensor, w: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
+                   bias: Optional[torch.Tensor] = None, *, index: Optional[torch.Tensor] = None,
+                   scale: Optional[torch.Tensor] = None, epilogue: str = "store",
+                   resid: Optional[torch.Tensor] = None, resid_copy: Optional[torch.Tensor] = None,
+                   gate: Optional[torch.Tensor] = None, save_t: bool = False, stream=None):
+    """A linear layer shared by rows with low-rank adapters of their own
+    (``t2i_op_adapter_linear``): ``y = x w^T + bias + s_i (x a_i^T) b_i^T`` with ``i =
+    index[row]`` (int32 ``[M]``; outside ``0 .. n-1``: no adapter; None: adapter 0 for all) for
+    ``x [M, K]``, ``w [N, K]``, ``a [n, rank, K]``, ``b [n, N, rank]`` of one dtype (bf16 or
+    fp32) and ``scale`` fp32 ``[n]`` (None: ones), with the epilogues of :func:`linear_i8`.
+    With ``save_t`` also ``t = s_i x a_i^T`` (``[M, rank rounded up to 32]``) that
+    :func:`adapter_linear_backward` takes."""
+    dev = _device(x, w, a, b, bias, index, scale, resid, resid_copy, gate)
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return adapter_linear(x, w, a, b, bias, index=index, scale=scale, epilogue=epilogue, resid=resid,
+                                  resid_copy=resid_copy, gate=gate, save_t=save_t)
+    dt, M, N, K, n, r, ldx, ldw = _adapter_args(x, w, a, b, index, scale)
+    epi = _of(EPILOGUES, epilogue, "epilogue")
+    _vec(bias, N, x.dtype, "bias")
+    _vec(gate, N, torch.float32, "gate")
+    ldr, out = N, None
+    if epi >= _lib.T2I_EPI_RESID:
+        _need(resid is not None, "the resid epilogues need resid", 1)
+        ldr = _rows(resid, M, N, torch.float32, "resid")
+        if resid_copy is not None:
+            ldc = _rows(resid_copy, M, N, torch.bfloat16, "resid_copy")
+            _need(M == 1 or ldc == ldr, "resid_copy must have resid's row stride")
+    else:
+        _need(resid is None and resid_copy is None, "resid goes with the resid epilogues", 1)
+        out = x.new_empty((M, N))
+    _need((gate is not None) == (epilogue == "resid_gated"), "gate goes with resid_gated", 1)
+    ldt = (r + 31) // 32 * 32
+    t = x.new_empty((M, ldt))
+    _check(load().t2i_op_adapter_linear(dt, epi, M, N, K, x.data_ptr(), ldx, w.data_ptr(), ldw, _p(bias), n, r,
+                                        a.data_ptr(), b.data_ptr(), _p(scale), _p(index), t.data_ptr(), ldt, _p(out),
+                                        N, _p(resid), ldr, _p(resid_copy), _p(gate), _stream(dev)))
+    if out is None:
+        _written(resid, resid_copy)
+        out = resid
+    return (out, t) if save_t else out
+
+
+def adapter_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, a: torch.Tensor, b: torch.Tensor,
+                            t: torch.Tensor, *, index: Optional[torch.Tensor] = None,
+                            scale: Optional[torch.Tensor] = None, need_dx: bool = True, need_dab: bool = True,
+                            stream=None):
+    """Gradients of :func:`adapter_linear` (epilogue ``store``) for adapters trained beside a
+    frozen layer (``t2i_op_adapter_linear_backward``): ``(dx, da, db)`` from y's gradient ``dy
+    [M, N]``, the forward pass's operands and its ``t``; None for those not asked for."""
+    dev = _device(dy, x, w, a, b, t, index, scale)
+    if _elsewhere(dev, stream):
+        with _switch(dev, stream):
+            return adapter_linear_backward(dy, x, w, a, b, t, index=index, scale=scale, need_dx=need_dx,
+                                           need_dab=need_dab)
+    dt, M, N, K, n, r, ldx, ldw = _adapter_args(x, w, a, b, index, scale)
+    lddy = _rows(dy, M, N, x.dtype, "dy")
+    ldt = _rows(t, M, (r + 31) // 32 * 32, x.dtype, "t")
+    lib = load()
+    dx = x.new_empty((M, K)) if need_dx else None
+    da, db = (a.new_empty(a.shape), b.new_empty(b.shape)) if need_dab else (None, None)
+    nb = lib.t2i_op_adapter_linear_backward_ws_bytes(dt, M, N, K, n, r)
+    ws = x.new_empty(nb, dtype=torch.uint8)
+    _check(lib.t2i_op_adapter_linear_backward(
+        dt, M, N, K, dy.data_ptr(), lddy, x.data_ptr(), ldx, w.data_ptr(), ldw, n, r, a.data_ptr(), b.data_ptr(),
+        _p(scale), _p(index), t.data_ptr(), ldt, _p(dx), K, _p(da), _p(db), ws.data_ptr(), nb, _stream(dev)))
+    return dx, da, db
