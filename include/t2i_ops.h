@@ -411,6 +411,30 @@ t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, i
                                           size_t ws_bytes, void* stream);
 
 /*
+ * One AdamW step over n tensors (64 a launch).  For tensor i of numel[i] elements, with
+ * g' = grad_scale g:
+ *   m = beta1 m + (1 - beta1) g',  v = beta2 v + (1 - beta2) g'^2,
+ *   p -= lr (m / (1 - beta1^step) / (sqrt(v / (1 - beta2^step)) + eps) + weight_decay p),
+ * in place, fp32 arithmetic.
+ *   params[i] of param_dtype, grads[i] of grad_dtype (T2I_F32 or T2I_BF16 each),
+ *   moments exp_avg[i], exp_avg_sq[i] fp32; masters[i] fp32 for bf16 params, which
+ *   then receive the rounded masters (NULL for fp32 ones).  Host arrays of device
+ *   pointers to contiguous elements at any alignment of their type; read during the
+ *   call.  numel[i] 0 .. 2^33 (0: its pointers are not used).
+ *   step counts from 1.  lr_device, step_device (then lr, step are not used) and
+ *   grad_scale (NULL: 1) are device scalars that the kernel reads: a captured call
+ *   follows them from replay to replay.
+ * No tensor that is written may overlap another tensor.
+ */
+t2i_status t2i_op_adamw_step(int32_t param_dtype, int32_t grad_dtype, int32_t n,
+                             const int64_t* numel, void* const* params, const void* const* grads,
+                             float* const* exp_avg, float* const* exp_avg_sq,
+                             float* const* masters, double lr, double beta1, double beta2,
+                             double eps, double weight_decay, int64_t step,
+                             const float* lr_device, const int32_t* step_device,
+                             const float* grad_scale, void* stream);
+
+/*
  * Memory-counter calibration (not part of the denoising step): reads `bytes`
  * of src (device, 16-byte aligned; a multiple of 1024 below 2 GiB) exactly
  * once through the direct HBM -> LDS load path that the GEMM and attention

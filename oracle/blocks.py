@@ -155,3 +155,13 @@ def adapter_linear_grads(dy, x, w, a, b, index=None, scale=None):
         dx[rows] += u[rows] @ a[i]
         da[i], db[i] = u[rows].T @ x[rows], dy[rows].T @ t[rows]
     return dict(dx=dx, da=da, db=db, u=u)
+
+
+def adamw(p, g, m, v, step, lr, betas, eps, weight_decay, grad_scale=1.0):
+    """(p, m, v) after one step"""
+    b1, b2 = betas
+    g = g * grad_scale
+    m = b1 * m + (1 - b1) * g
+    v = b2 * v + (1 - b2) * g * g
+    way = m / (1 - b1 ** step) / (np.sqrt(v / (1 - b2 ** step)) + eps)
+    return p - lr * (way + weight_decay * p), m, v

@@ -27,6 +27,7 @@ from ._lib import (T2I_F32, T2I_BF16, T2I_ARCH_CROSS_DIT, T2I_ARCH_MMDIT,
 from .ops import (adapter_linear, adapter_linear_backward, add_rms_norm, add_rms_norm_backward,
                   add_rms_norm_i8, gated_linear, gated_linear_backward, linear_i8, qk_norm_rope,
                   qk_norm_rope_backward, quant_rows)
+from .optim import AdamW
 
 __all__ = ["Config", "DiT", "t2i_dit_init", "t2i_dit_init_static", "t2i_dit_step", "t2i_dit_sample",
            "t2i_cache_check", "weight_table", "upload", "T2IError", "load",
@@ -34,7 +35,7 @@ __all__ = ["Config", "DiT", "t2i_dit_init", "t2i_dit_init_static", "t2i_dit_step
            "t2i_dit_load_async", "t2i_dit_block_state", "t2i_first_layers",
            "quant_rows", "linear_i8", "gated_linear", "gated_linear_backward", "qk_norm_rope",
            "qk_norm_rope_backward", "add_rms_norm", "add_rms_norm_i8", "add_rms_norm_backward", "adapter_linear",
-           "adapter_linear_backward"]
+           "adapter_linear_backward", "AdamW"]
 
 
 def _stream(stream=None) -> int:

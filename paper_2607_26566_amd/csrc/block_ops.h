@@ -211,4 +211,28 @@ struct AdapterOuter {
 hipError_t launch_adapter_outer(bool is_bf16, const AdapterOuter& p, int n, int slices, void* dA, void* dB,
                                 hipStream_t st);
 
+// ---- AdamW over many tensors
+
+constexpr int kAdamTensors = 64;       // of a launch, by value
+struct AdamGroup {
+  void* p[kAdamTensors];
+  const void* g[kAdamTensors];
+  float *m[kAdamTensors], *v[kAdamTensors], *master[kAdamTensors];
+  int64_t numel[kAdamTensors];
+  int32_t first[kAdamTensors + 1];     // a tensor's first workgroup
+  int32_t n;
+};
+struct AdamScalars {
+  double beta1, beta2;
+  float b1, b2, c1, c2;                // c = 1 - b
+  float r1, r2;                        // 1 / (1 - beta^step), unless step is given
+  float lr, eps, wd;
+  const float* lr_dev;                 // or NULL
+  const int32_t* step;                 // or NULL
+  const float* grad_scale;             // or NULL
+};
+static_assert(sizeof(AdamGroup) + sizeof(AdamScalars) <= 4096, "kernel arguments");
+// low: bf16 weights with masters
+hipError_t launch_adamw(bool low, bool grad_bf16, const AdamGroup& a, const AdamScalars& s, hipStream_t st);
+
 }  // namespace t2i
