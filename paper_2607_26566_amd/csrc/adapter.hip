@@ -115,13 +115,18 @@ __global__ __launch_bounds__(256) void adapter_down_rows_kernel(AdapterDown p) {
 constexpr int kDownWaves = 8;
 template <typename T, int RT>
 __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterDown p) {
-  constexpr int L = kLaneK<T>;
+  constexpr int L = kLaneK<T>, EB = sizeof(T), U = RT == 1 ? 4 : 2;
   __shared__ f32x4 red[kDownWaves][RT][64];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
   const int m = blockIdx.x * 16 + fr, j0 = blockIdx.y * RT * 16, K = p.K;
-  const bool whole = K % L == 0;
   const int ad = m < p.M ? adapter_of(p.index, p.n, m) : -1;
-  const T* const x = (const T*)p.x + (size_t)min(m, p.M - 1) * p.ldx;
+  // (16 rows of x, 64 of A span less than 2^31 bytes)
+  const T* const x = (const T*)p.x + (size_t)blockIdx.x * 16 * p.ldx;
+  const uint32_t xoff = (uint32_t)(min(fr, p.M - 1 - (int)blockIdx.x * 16) * p.ldx) * EB;
+  const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)x, 0, 0x7fffffff, 0x00020000);
+  auto load = [](const __amdgpu_buffer_rsrc_t& r, uint32_t at) {
+    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
+  };
   // columns of t that this workgroup writes; rows without an adapter: zeros
   auto store = [&](int jt, const f32x4& v) {
     const int j = j0 + jt * 16 + g * 4;
@@ -139,23 +144,40 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterDo
     const int now = __builtin_amdgcn_readlane(ad, __builtin_ctz(left));
     const uint32_t mine = (uint32_t)__ballot(ad == now) & 0xffffu;
     left &= ~mine;
-    const T* a[RT];
+    const T* const a = (const T*)p.a + ((size_t)now * p.rank + j0) * K;
+    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)a, 0, 0x7fffffff, 0x00020000);
+    uint32_t aoff[RT];
 #pragma unroll
-    for (int jt = 0; jt < RT; ++jt)
-      a[jt] = (const T*)p.a + ((size_t)now * p.rank + min(j0 + jt * 16 + fr, p.rank - 1)) * K;
+    for (int jt = 0; jt < RT; ++jt) aoff[jt] = (uint32_t)(min(jt * 16 + fr, p.rank - 1 - j0) * K) * EB;
     f32x4 acc[RT];
 #pragma unroll
     for (int jt = 0; jt < RT; ++jt) acc[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int k0 = wave * 8 * L; k0 < K; k0 += kDownWaves * 8 * L) {
-      const int k = k0 + 2 * g * L;
-      const i32x4 x0 = load_k<T>(x, 0, k, K, whole), x1 = load_k<T>(x, 0, k + L, K, whole);
+#pragma unroll 1
+    for (int k0 = wave * 8 * L; k0 < K; k0 += U * kDownWaves * 8 * L) {
+      i32x4 xv[U][2], av[U][2][RT];
 #pragma unroll
-      for (int jt = 0; jt < RT; ++jt) {
-        const i32x4 a0 = load_k<T>(a[jt], 0, k, K, whole), a1 = load_k<T>(a[jt], 0, k + L, K, whole);
-        acc[jt] = narrow_mfma<T>(a0, x0, acc[jt]);
-        acc[jt] = narrow_mfma<T>(a1, x1, acc[jt]);
-      }
+      for (int q = 0; q < U; ++q)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const int k = k0 + q * kDownWaves * 8 * L + (2 * g + h) * L;
+          // (behind the resource: zeros)
+          const uint32_t at = k + L <= K ? (uint32_t)k * EB : kTileOff;
+          xv[q][h] = load(rx, at == kTileOff ? at : xoff + at);
+#pragma unroll
+          for (int jt = 0; jt < RT; ++jt) av[q][h][jt] = load(ra, at == kTileOff ? at : aoff[jt] + at);
+        }
+#pragma unroll
+      for (int q = 0; q < U; ++q)
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+          for (int jt = 0; jt < RT; ++jt) acc[jt] = narrow_mfma<T>(av[q][h][jt], xv[q][h], acc[jt]);
+    }
+    if (K % L && wave == 0) {   // the last elements of fp32 rows, in one group's lanes
+      const int k = g == 0 ? K / L * L : K;
+      const i32x4 xv = load_k<T>((const char*)x, xoff, k, K, false);
+#pragma unroll
+      for (int jt = 0; jt < RT; ++jt) acc[jt] = narrow_mfma<T>(load_k<T>(a, aoff[jt], k, K, false), xv, acc[jt]);
     }
 #pragma unroll
     for (int jt = 0; jt < RT; ++jt) red[wave][jt][lane] = acc[jt];
@@ -200,119 +222,159 @@ hipError_t launch_adapter_down(bool is_bf16, const AdapterDown& p, hipStream_t s
 
 // ---------------------------------------------------------------------------
 // acc += t P_i^T for the tile's rows, P_i [columns][stride] the adapter's second matrix
-// (forward: B; gradients: A transposed), both operands straight from memory.  A wave whose
-// rows have one adapter takes the matrix cores for all of them.  Rows of several: in the
-// largest tile, whose accumulators leave few registers, 16 rows at a time by the matrix
-// cores once for every adapter of theirs, of which each row takes its own, by way of
-// LDS; in the others a lane sums up its own row's products, all of whose loads are under
-// way at once.  smem: the tile's ring, which no wave reads any more.
+// (forward: B; gradients: A transposed), both operands straight from memory, while the
+// ring's first loads are under way.  A wave whose rows have one adapter takes the matrix
+// cores for all of them; rows of several take them once for every adapter, of whose
+// results each row takes its own (the largest tile, whose accumulators leave few
+// registers, after the last step, 16 rows at a time by way of LDS); in tiles of 16 rows,
+// which are for few rows with an adapter each, a lane sums up its own row's products, all
+// of whose loads are under way at once.
 template <class P, class D, typename T>
-__device__ __forceinline__ void add_adapters(f32x4 (&acc)[D::TM][D::TN], char* smem, const AdapterUp& u, int m0, int n0,
-                                             int M, int N) {
-  constexpr int TM = D::TM, TN = D::TN, L = kLaneK<T>;
-  const int lane = threadIdx.x & 63, fr = lane & 15, g = lane >> 4;
-  const int wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % D::NW);
-  const int mw = m0 + (wave / D::WGN) * D::WM, nw = n0 + (wave % D::WGN) * D::WN;
-  if (mw >= M || nw >= N) return;
-  const T* const t = (const T*)u.t + (size_t)mw * u.ldt;
-  const T* const p = (const T*)u.p + (size_t)nw * u.stride;
-  const bool whole = u.rank % L == 0;
-  // a row's adapter, -2 (any) behind the last row
-  auto id_of = [&](int i) {
-    const int m = mw + P::row_of(i, fr);
-    return m < M ? adapter_of(u.index, u.n, m) : -2;
-  };
-  // (t's and a matrix's rows of a wave span less than 2^31 bytes)
-  auto t_at = [&](int i, int k) {
-    return load_k<T>(t, (uint32_t)(min(P::row_of(i, fr), M - 1 - mw) * u.ldt) * (uint32_t)sizeof(T), k, u.ldt, true);
-  };
-  auto p_at = [&](const T* q, int j, int x, int k) {
-    return load_k<T>(q, (uint32_t)(min(P::col_of(j, x), N - 1 - nw) * u.stride) * (uint32_t)sizeof(T), k, u.rank, whole);
-  };
-  const size_t matrix = (size_t)N * u.stride;
-  const int first = __builtin_amdgcn_readfirstlane(id_of(0));   // (row mw exists)
-  bool same = true;
-#pragma unroll
-  for (int i = 0; i < TM; ++i) {
-    const int id = id_of(i);
-    same = same && (id == first || id == -2);
-  }
-  if (__all(same)) {
-    if (first < 0) return;
-    const T* const q = p + first * matrix;
-#pragma unroll 1
-    for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
-      i32x4 tv[TM];
-#pragma unroll
-      for (int i = 0; i < TM; ++i) tv[i] = t_at(i, k0 + g * L);
-#pragma unroll
-      for (int j = 0; j < TN; ++j) {
-        const i32x4 pv = p_at(q, j, fr, k0 + g * L);
-#pragma unroll
-        for (int i = 0; i < TM; ++i) acc[i][j] = narrow_mfma<T>(pv, tv[i], acc[i][j]);
-      }
-    }
-  } else if constexpr (TM * TN > 8) {
-    constexpr int HALF = TM / 2;
-    static_assert(D::NW * HALF * TN * 1024 <= D::RING, "room for half of the results");
-    f32x4* const part = (f32x4*)(smem + wave * HALF * TN * 1024) + lane;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-#pragma unroll 1
-      for (int i = 0; i < HALF; ++i) {
-        const int id = id_of(h * HALF + i);
-        uint32_t left = (uint32_t)__ballot(id >= 0) & 0xffffu;
-        f32x4 sum[TN];
-#pragma unroll
-        for (int j = 0; j < TN; ++j) sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-        while (left) {
-          const int now = __builtin_amdgcn_readlane(id, __builtin_ctz(left));
-          left &= ~(uint32_t)__ballot(id == now);
-          const T* const q = p + now * matrix;
-          f32x4 add[TN];
-#pragma unroll
-          for (int j = 0; j < TN; ++j) add[j] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-          for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
-            const i32x4 tv = t_at(h * HALF + i, k0 + g * L);
-#pragma unroll
-            for (int j = 0; j < TN; ++j) add[j] = narrow_mfma<T>(p_at(q, j, fr, k0 + g * L), tv, add[j]);
-          }
-#pragma unroll
-          for (int j = 0; j < TN; ++j)
-#pragma unroll
-            for (int r = 0; r < 4; ++r) sum[j][r] = id == now ? add[j][r] : sum[j][r];
-        }
-#pragma unroll
-        for (int j = 0; j < TN; ++j) part[(i * TN + j) * 64] = sum[j];
-      }
-#pragma unroll
-      for (int i = 0; i < HALF; ++i)
-#pragma unroll
-        for (int j = 0; j < TN; ++j) acc[h * HALF + i][j] += part[(i * TN + j) * 64];
-    }
-  } else {
+struct Adapters {
+  static constexpr int TM = D::TM, TN = D::TN, L = kLaneK<T>;
+  const AdapterUp& u;
+  int M, N, mw, nw, fr, g;
+  static constexpr bool LATE = TM * TN > 16;
+  int id[TM];   // a row's adapter, -2 (any) behind the last row
+
+  __device__ __forceinline__ Adapters(const AdapterUp& up, int m0, int n0, int M_, int N_) : u(up), M(M_), N(N_) {
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % D::NW);
+    fr = lane & 15, g = lane >> 4;
+    mw = m0 + (wave / D::WGN) * D::WM, nw = n0 + (wave % D::WGN) * D::WN;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
-      const int id = id_of(i);
-      if (id < 0) continue;
-      const T* const q = p + id * matrix;
+      const int m = mw + P::row_of(i, fr);
+      const int a = adapter_of(u.index, u.n, min(m, M - 1));
+      id[i] = m < M ? a : -2;
+    }
+  }
+  // (t's and a matrix's rows of a wave span less than 2^31 bytes)
+  __device__ __forceinline__ i32x4 t_at(int i, int k) const {
+    const T* const t = (const T*)u.t + (size_t)mw * u.ldt;
+    return load_k<T>(t, (uint32_t)(min(P::row_of(i, fr), M - 1 - mw) * u.ldt) * (uint32_t)sizeof(T), k, u.ldt, true);
+  }
+  __device__ __forceinline__ i32x4 p_at(int ad, int j, int x, int k) const {
+    const T* const p = (const T*)u.p + ((size_t)ad * N + nw) * u.stride;
+    return load_k<T>(p, (uint32_t)(min(P::col_of(j, x), N - 1 - nw) * u.stride) * (uint32_t)sizeof(T), k, u.rank,
+                     u.rank % L == 0);
+  }
+  __device__ __forceinline__ bool one_adapter() const {
+    const int first = __builtin_amdgcn_readfirstlane(id[0]);
+    bool same = true;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) same = same && (id[i] == first || id[i] == -2);
+    return __all(same);
+  }
+  __device__ __forceinline__ void operator()(f32x4 (&acc)[TM][TN]) const {
+    if (mw >= M || nw >= N) return;
+    if (one_adapter()) {
+      const int first = __builtin_amdgcn_readfirstlane(id[0]);   // (row mw exists)
+      if (first < 0) return;
+#pragma unroll 1
+      for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
+        i32x4 tv[TM];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) tv[i] = t_at(i, k0 + g * L);
+#pragma unroll
+        for (int j = 0; j < TN; ++j) {
+          const i32x4 pv = p_at(first, j, fr, k0 + g * L);
+#pragma unroll
+          for (int i = 0; i < TM; ++i) acc[i][j] = narrow_mfma<T>(pv, tv[i], acc[i][j]);
+        }
+      }
+    } else if constexpr (LATE) {
+    } else if constexpr (TM > 1) {
+#pragma unroll 1
+      for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
+        i32x4 tv[TM];
+#pragma unroll
+        for (int i = 0; i < TM; ++i) tv[i] = t_at(i, k0 + g * L);
+        int now = -1;
+#pragma unroll 1
+        for (;;) {   // the adapters in ascending order
+          int next = 0x7fffffff;
+#pragma unroll
+          for (int i = 0; i < TM; ++i) next = min(next, id[i] > now ? id[i] : 0x7fffffff);
+#pragma unroll
+          for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, kWave));
+          now = __builtin_amdgcn_readfirstlane(next);
+          if (now == 0x7fffffff) break;
+          i32x4 pv[TN];
+#pragma unroll
+          for (int j = 0; j < TN; ++j) pv[j] = p_at(now, j, fr, k0 + g * L);
+#pragma unroll
+          for (int i = 0; i < TM; ++i) {
+#pragma unroll
+            for (int j = 0; j < TN; ++j) {
+              const f32x4 add = narrow_mfma<T>(pv[j], tv[i], f32x4{0.f, 0.f, 0.f, 0.f});
+#pragma unroll
+              for (int r = 0; r < 4; ++r) acc[i][j][r] += id[i] == now ? add[r] : 0.f;
+            }
+          }
+        }
+      }
+    } else if (id[0] >= 0) {
 #pragma unroll 1
       for (int k = 0; k < u.rank; k += L) {
-        const i32x4 tv = t_at(i, k);
+        const i32x4 tv = t_at(0, k);
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
-            const i32x4 pv = p_at(q, j, g * 4 + r, k);
+            const i32x4 pv = p_at(id[0], j, g * 4 + r, k);
 #pragma unroll
-            for (int e = 0; e < L; ++e) acc[i][j][r] = fmaf(element<T>(tv, e), element<T>(pv, e), acc[i][j][r]);
+            for (int e = 0; e < L; ++e) acc[0][j][r] = fmaf(element<T>(tv, e), element<T>(pv, e), acc[0][j][r]);
           }
       }
     }
   }
-}
+  // what the largest tile has left; smem: its ring, which no wave reads any more
+  __device__ __forceinline__ void finish(char* smem, f32x4 (&acc)[TM][TN]) const {
+    if constexpr (LATE) {
+      if (mw >= M || nw >= N || one_adapter()) return;
+      constexpr int HALF = TM / 2;
+      static_assert(D::NW * HALF * TN * 1024 <= D::RING, "room for half of the results");
+      const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((threadIdx.x >> 6) % D::NW);
+      f32x4* const part = (f32x4*)(smem + wave * HALF * TN * 1024) + lane;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+#pragma unroll 1
+        for (int i = 0; i < HALF; ++i) {
+          const int m = mw + P::row_of(h * HALF + i, fr);
+          const int mine = m < M ? adapter_of(u.index, u.n, m) : -2;
+          uint32_t left = (uint32_t)__ballot(mine >= 0) & 0xffffu;
+          f32x4 sum[TN];
+#pragma unroll
+          for (int j = 0; j < TN; ++j) sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+          while (left) {
+            const int now = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
+            left &= ~(uint32_t)__ballot(mine == now);
+            f32x4 add[TN];
+#pragma unroll
+            for (int j = 0; j < TN; ++j) add[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 1
+            for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
+              const i32x4 tv = t_at(h * HALF + i, k0 + g * L);
+#pragma unroll
+              for (int j = 0; j < TN; ++j) add[j] = narrow_mfma<T>(p_at(now, j, fr, k0 + g * L), tv, add[j]);
+            }
+#pragma unroll
+            for (int j = 0; j < TN; ++j)
+#pragma unroll
+              for (int r = 0; r < 4; ++r) sum[j][r] = mine == now ? add[j][r] : sum[j][r];
+          }
+#pragma unroll
+          for (int j = 0; j < TN; ++j) part[(i * TN + j) * 64] = sum[j];
+        }
+#pragma unroll
+        for (int i = 0; i < HALF; ++i)
+#pragma unroll
+          for (int j = 0; j < TN; ++j) acc[h * HALF + i][j] += part[(i * TN + j) * 64];
+      }
+    }
+  }
+};
 
 // y = x W^T + t B^T + bias, then the linear layer's epilogues
 template <class D, typename T, bool RES, bool U>
@@ -332,12 +394,13 @@ __global__ __launch_bounds__(D::THREADS, 1) void adapter_linear_kernel(TileOpera
   Staged<NE, THREADS, decltype(value)> st;
   st.fetch(value);
   typename P::Acc acc[D::TM][D::TN];
-  const bool mine = P::run_groups(smem, a, b, s, m0, n0, acc);
+  const Adapters<P, D, T> from(up, m0, n0, M, N);
+  const bool mine = P::run_groups(smem, a, b, s, m0, n0, acc, from);
   float* const ev = (float*)(smem + D::KG * D::RING);
   st.put(ev);
   tile_barrier();
   if (!mine) return;
-  add_adapters<P, D, T>(acc, smem, up, m0, n0, M, N);
+  from.finish(smem, acc);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
   const int mw = (wave / D::WGN) * D::WM, nw = (wave % D::WGN) * D::WN;
 #pragma unroll
@@ -381,10 +444,13 @@ __global__ __launch_bounds__(D::THREADS, 1) void adapter_dx_kernel(TileOperand a
   if (sp.partial) take_slice(sp, s);
   typename P::Acc acc[D::TM][D::TN];
   const int m0 = tm * D::BM, n0 = first_column<D, U>(tn, K);
-  P::run(smem, a, b, s, m0, n0, acc);
-  if (blockIdx.y == 0) {
+  const Adapters<P, D, T> from(up, m0, n0, M, K);
+  P::run(smem, a, b, s, m0, n0, acc, [&](f32x4 (&c)[D::TM][D::TN]) {
+    if (blockIdx.y == 0) from(c);
+  });
+  if (from.LATE && blockIdx.y == 0) {
     tile_barrier();
-    add_adapters<P, D, T>(acc, smem, up, m0, n0, M, K);
+    from.finish(smem, acc);
   }
   if (sp.partial)
     store_tile<D, P>(acc, sp.partial + (size_t)blockIdx.y * M * sp.ld, sp.ld, m0, n0, M, K);

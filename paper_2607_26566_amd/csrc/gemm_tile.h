@@ -145,6 +145,12 @@ struct TileDims {
 
 enum TileElem { ELEM_BF16, ELEM_I8, ELEM_F32 };
 
+// what a product's accumulators start from: zeros
+struct FromZero {
+  template <class A>
+  __device__ __forceinline__ void operator()(A&) const {}
+};
+
 // E: element type.  AKR, BKR: operand layouts.  DUAL: b is two matrices side by side,
 // p for the first half of the tile's columns and p2 for the second, so that a wave
 // holds both of an output.  SEGS (BKR): the contraction runs over p's rows, then p2's.
@@ -182,9 +188,11 @@ struct TileProduct {
   static __device__ __forceinline__ int col_of(int j, int x) { return j / NB * NB * 16 + x * NB + j % NB; }
 
   // the tile product: acc[i][j][r] belongs to the wave's row row_of(i, lane & 15)
-  // and column col_of(j, 4 (lane >> 4) + r)
-  static __device__ __forceinline__ void run(char* smem, const TileOperand& a, const TileOperand& b,
-                                             const TileShape& s, int m0, int n0, Acc (&acc)[TM][TN]) {
+  // and column col_of(j, 4 (lane >> 4) + r).  `from` may add to the accumulators before the
+  // first step, while the ring's first loads are under way.
+  template <class F = FromZero>
+  static __device__ __forceinline__ void run(char* smem, const TileOperand& a, const TileOperand& b, const TileShape& s,
+                                             int m0, int n0, Acc (&acc)[TM][TN], const F& from = F()) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane((tid >> 6) % D::NW);
     const int wm = wave / D::WGN, wn = wave % D::WGN, fr = lane & 15, g = lane >> 4;
@@ -359,6 +367,7 @@ struct TileProduct {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) issue(i, t, t * D::STAGE, ra, rb);
       }
+    from(acc);
     tile_wait<LOADS>(min(ST, KT) - 1);
     tile_barrier();
     read_a(0, 0, a0);
@@ -408,18 +417,22 @@ struct TileProduct {
   }
 
   // the same by KG groups of waves; the sum, in ascending group order, is the first
-  // group's.  Returns whether this wave is of that group (the others have no outputs).
+  // group's, whose accumulators `from` adds to.  Returns whether this wave is of that group
+  // (the others have no outputs).
+  template <class F = FromZero>
   static __device__ __forceinline__ bool run_groups(char* smem, const TileOperand& a, const TileOperand& b, TileShape s,
-                                                    int m0, int n0, Acc (&acc)[TM][TN]) {
+                                                    int m0, int n0, Acc (&acc)[TM][TN], const F& from = F()) {
     if constexpr (D::KG == 1) {
-      run(smem, a, b, s, m0, n0, acc);
+      run(smem, a, b, s, m0, n0, acc, from);
       return true;
     } else {
       const int kg = __builtin_amdgcn_readfirstlane((int)threadIdx.x / (D::NW * 64)), t = threadIdx.x % (D::NW * 64);
       const int total = s.steps, per = (total + D::KG - 1) / D::KG;
       s.first = kg * total / D::KG;
       s.steps = (kg + 1) * total / D::KG - s.first;
-      run(smem + kg * D::RING, a, b, s, m0, n0, acc);
+      run(smem + kg * D::RING, a, b, s, m0, n0, acc, [&](Acc (&c)[TM][TN]) {
+        if (kg == 0) from(c);
+      });
       // (every group meets as often: slices differ by a step)
       for (int x = s.steps; x < per; ++x) tile_barrier();
       tile_barrier();
