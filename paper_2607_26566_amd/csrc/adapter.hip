@@ -108,111 +108,94 @@ __global__ __launch_bounds__(256) void adapter_down_rows_kernel(AdapterDown p) {
   ((T*)p.t)[(size_t)m * p.ldt + j0 + j] = from_f32<T>(ad >= 0 && j0 + j < p.rank ? v * scale : 0.f);
 }
 
-// Many rows: a workgroup takes 16 rows and RT times 16 ranks, its waves a share of k each,
-// in blocks of 128 bytes: a lane's two pieces of a block are neighbours, so that the 16
-// rows' reads are whole lines; the order of k is the same for both operands.  Rows of
-// several adapters: one after the other.
-constexpr int kDownWaves = 8;
-template <typename T, int RT>
-__global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterDown p) {
-  constexpr int L = kLaneK<T>, EB = sizeof(T), U = RT == 1 ? 4 : 2;
-  __shared__ f32x4 red[kDownWaves][RT][64];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
-  const int m = blockIdx.x * 16 + fr, j0 = blockIdx.y * RT * 16, K = p.K;
-  const int ad = m < p.M ? adapter_of(p.index, p.n, m) : -1;
-  // (16 rows of x, 64 of A span less than 2^31 bytes)
-  const T* const x = (const T*)p.x + (size_t)blockIdx.x * 16 * p.ldx;
-  const uint32_t xoff = (uint32_t)(min(fr, p.M - 1 - (int)blockIdx.x * 16) * p.ldx) * EB;
-  const __amdgpu_buffer_rsrc_t rx = __builtin_amdgcn_make_buffer_rsrc((void*)x, 0, 0x7fffffff, 0x00020000);
-  auto load = [](const __amdgpu_buffer_rsrc_t& r, uint32_t at) {
-    return __builtin_bit_cast(i32x4, __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, 0));
-  };
-  // columns of t that this workgroup writes; rows without an adapter: zeros
-  auto store = [&](int jt, const f32x4& v) {
-    const int j = j0 + jt * 16 + g * 4;
+// Many rows: a tile of rows and all ranks (up to 64), whose groups of waves share k as
+// in the products of few tiles; both operands come through LDS in whole lines (fragments
+// straight from memory, 16 rows to an instruction, 19 us for 4096 rows of 4096 and 16
+// ranks).  Rows of several adapters: the tile's product once for each of them.
+template <class D, typename T, bool U>
+__global__ __launch_bounds__(D::THREADS, 1) void adapter_down_kernel(AdapterDown p) {
+  using P = TileProduct<D, elem_of<T>(), false, false, false, false, U>;
+  __shared__ __attribute__((aligned(1024))) char smem[D::KG * D::RING];
+  constexpr int EB = sizeof(T), TM = D::TM, TN = D::TN;
+  const int lane = threadIdx.x & 63, fr = lane & 15, g = lane >> 4;
+  const int m0 = blockIdx.x * D::BM, j0 = blockIdx.y * D::BN, cols = adapter_cols(p.rank);
+  const TileOperand a{(const char*)p.x, nullptr, (uint32_t)(EB * p.ldx), p.M, 0};
+  TileShape s;
+  s.tiles_m = s.tiles_n = s.group_m = 1;
+  s.kbytes = EB * p.K;
+  s.steps = (s.kbytes + 127) / 128;
+  s.half = s.first = 0;
+  int ad[TM];
+#pragma unroll
+  for (int i = 0; i < TM; ++i) {
+    const int m = m0 + i * 16 + fr;
+    ad[i] = m < p.M ? adapter_of(p.index, p.n, m) : -2;
+  }
+  auto store = [&](int i, int j, const f32x4& v) {
+    const int m = m0 + i * 16 + fr, c = j0 + j * 16 + g * 4;
     float o[4];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) o[r] = j + r < p.rank ? v[r] : 0.f;
-    if (j < adapter_cols(p.rank)) store4((T*)p.t + (size_t)m * p.ldt + j, 4, o);
+    for (int r = 0; r < 4; ++r) o[r] = c + r < p.rank ? v[r] : 0.f;
+    if (c < cols) store4((T*)p.t + (size_t)m * p.ldt + c, 4, o);
   };
   const bool behind = j0 >= p.rank;   // the zeros behind the ranks
-  if (wave == 0 && m < p.M && (ad < 0 || behind))
-    for (int jt = 0; jt < RT; ++jt) store(jt, f32x4{0.f, 0.f, 0.f, 0.f});
+  if (threadIdx.x < 64) {
+#pragma unroll
+    for (int i = 0; i < TM; ++i)
+      if (ad[i] == -1 || (behind && ad[i] >= 0))
+#pragma unroll
+        for (int j = 0; j < TN; ++j) store(i, j, f32x4{0.f, 0.f, 0.f, 0.f});
+  }
   if (behind) return;
-  uint32_t left = (uint32_t)__ballot(ad >= 0) & 0xffffu;
-  while (left) {
-    const int now = __builtin_amdgcn_readlane(ad, __builtin_ctz(left));
-    const uint32_t mine = (uint32_t)__ballot(ad == now) & 0xffffu;
-    left &= ~mine;
-    const T* const a = (const T*)p.a + ((size_t)now * p.rank + j0) * K;
-    const __amdgpu_buffer_rsrc_t ra = __builtin_amdgcn_make_buffer_rsrc((void*)a, 0, 0x7fffffff, 0x00020000);
-    uint32_t aoff[RT];
+  int now = -1;
+  for (;;) {   // the adapters in ascending order, the same for every wave
+    int next = 0x7fffffff;
 #pragma unroll
-    for (int jt = 0; jt < RT; ++jt) aoff[jt] = (uint32_t)(min(jt * 16 + fr, p.rank - 1 - j0) * K) * EB;
-    f32x4 acc[RT];
+    for (int i = 0; i < TM; ++i) next = min(next, ad[i] > now ? ad[i] : 0x7fffffff);
 #pragma unroll
-    for (int jt = 0; jt < RT; ++jt) acc[jt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-    for (int k0 = wave * 8 * L; k0 < K; k0 += U * kDownWaves * 8 * L) {
-      i32x4 xv[U][2], av[U][2][RT];
+    for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, kWave));
+    next = __builtin_amdgcn_readfirstlane(next);
+    if (next == 0x7fffffff) return;
+    if (now >= 0) tile_barrier();   // (the sums of the adapter before are read)
+    now = next;
+    const TileOperand b{(const char*)p.a + (size_t)now * p.rank * p.K * EB, nullptr, (uint32_t)(EB * p.K), p.rank, 0};
+    typename P::Acc acc[TM][TN];
+    if (!P::run_groups(smem, a, b, s, m0, j0, acc)) continue;
+    const float scale = p.scale ? p.scale[now] : 1.f;
 #pragma unroll
-      for (int q = 0; q < U; ++q)
+    for (int i = 0; i < TM; ++i) {
+      if (ad[i] != now) continue;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          const int k = k0 + q * kDownWaves * 8 * L + (2 * g + h) * L;
-          // (behind the resource: zeros)
-          const uint32_t at = k + L <= K ? (uint32_t)k * EB : kTileOff;
-          xv[q][h] = load(rx, at == kTileOff ? at : xoff + at);
-#pragma unroll
-          for (int jt = 0; jt < RT; ++jt) av[q][h][jt] = load(ra, at == kTileOff ? at : aoff[jt] + at);
-        }
-#pragma unroll
-      for (int q = 0; q < U; ++q)
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-          for (int jt = 0; jt < RT; ++jt) acc[jt] = narrow_mfma<T>(av[q][h][jt], xv[q][h], acc[jt]);
+      for (int j = 0; j < TN; ++j) store(i, j, acc[i][j] * scale);
     }
-    if (K % L && wave == 0) {   // the last elements of fp32 rows, in one group's lanes
-      const int k = g == 0 ? K / L * L : K;
-      const i32x4 xv = load_k<T>((const char*)x, xoff, k, K, false);
-#pragma unroll
-      for (int jt = 0; jt < RT; ++jt) acc[jt] = narrow_mfma<T>(load_k<T>(a, aoff[jt], k, K, false), xv, acc[jt]);
-    }
-#pragma unroll
-    for (int jt = 0; jt < RT; ++jt) red[wave][jt][lane] = acc[jt];
-    __syncthreads();
-    if (wave < RT && ((mine >> fr) & 1)) {
-      f32x4 v = red[0][wave][lane];
-#pragma unroll
-      for (int w = 1; w < kDownWaves; ++w) v += red[w][wave][lane];
-      const float scale = p.scale ? p.scale[now] : 1.f;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) v[r] *= scale;
-      store(wave, v);
-    }
-    __syncthreads();
   }
 }
 
 // rows up to which the first kernel takes them
 constexpr int kDownRows = 64;
+template <class D, typename T, bool U>
+static void down_launch(const AdapterDown& p, hipStream_t st) {
+  hipLaunchKernelGGL((adapter_down_kernel<D, T, U>),
+                     dim3((unsigned)((p.M + D::BM - 1) / D::BM), (unsigned)((adapter_cols(p.rank) + D::BN - 1) / D::BN)),
+                     dim3(D::THREADS), 0, st, p);
+}
+template <typename T, bool U>
+static void down_tiles(const AdapterDown& p, hipStream_t st) {
+  const long steps = ((long)p.K * (int)sizeof(T) + 127) / 128;
+  // groups of waves have a step each at least
+  if (steps < 8) down_launch<TileDims<16, 32, 1, 1, 4>, T, U>(p, st);
+  else if (p.rank <= 16) down_launch<TileDims<16, 16, 1, 1, 4, 8>, T, U>(p, st);
+  else if (p.rank <= 32) down_launch<TileDims<16, 32, 1, 1, 3, 8>, T, U>(p, st);
+  else down_launch<TileDims<16, 64, 1, 1, 3, 4>, T, U>(p, st);
+}
 template <typename T>
 static void down_any(const AdapterDown& p, hipStream_t st) {
-  if (p.M <= kDownRows) {
+  if (p.M <= kDownRows)
     hipLaunchKernelGGL((adapter_down_rows_kernel<T>), dim3((unsigned)p.M, (unsigned)(adapter_cols(p.rank) / 4)),
                        dim3(256), 0, st, p);
-    return;
-  }
-  // all ranks in one workgroup where that leaves two for every CU: x is read once
-  const int mt = (p.M + 15) / 16, rt = adapter_cols(p.rank) / 16;
-#define T2I_DOWN(RT)                                                                                              \
-  hipLaunchKernelGGL((adapter_down_kernel<T, RT>), dim3((unsigned)mt, (unsigned)((rt + RT - 1) / RT)),            \
-                     dim3(64 * kDownWaves), 0, st, p)
-  if (p.rank <= 16 || mt < 256) T2I_DOWN(1);
-  else if (p.rank <= 32 || mt < 512) T2I_DOWN(2);
-  else T2I_DOWN(4);
-#undef T2I_DOWN
+  else if constexpr (sizeof(T) == 2) down_tiles<T, false>(p, st);
+  else if (f32_pieces({p.K, p.ldx}, {p.x, p.a})) down_tiles<T, false>(p, st);
+  else down_tiles<T, true>(p, st);
 }
 hipError_t launch_adapter_down(bool is_bf16, const AdapterDown& p, hipStream_t st) {
   if (is_bf16) down_any<bf16>(p, st);
@@ -517,46 +500,21 @@ hipError_t launch_adapter_dx(bool is_bf16, const void* dy, int lddy, const void*
 }
 
 // ---------------------------------------------------------------------------
-// The adapters' matrices turned for the gradients: out[i][c][r] = in[i][r][c] for rows r <
-// R, 0 for R <= r < stride; a thread writes 8 values of a row of out.
-template <typename T>
-__global__ __launch_bounds__(256) void adapter_turn_kernel(const T* __restrict__ in, T* __restrict__ out, int R, int C,
-                                                           int stride) {
-  const long chunks = (stride + 7) / 8, x = blockIdx.x * 256L + threadIdx.x;
-  if (x >= chunks * C) return;
-  const int c = (int)(x % C), r0 = (int)(x / C) * 8;
-  const T* const p = in + (size_t)blockIdx.y * R * C + c;
-  float v[8];
-#pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = r0 + i < R ? to_f32(p[(size_t)(r0 + i) * C]) : 0.f;
-  store_piece(out + ((size_t)blockIdx.y * C + c) * stride + r0, stride - r0, v);
-}
-template <typename T>
-static void turn_any(const T* in, T* out, int n, int R, int C, int stride, hipStream_t st) {
-  const long x = (long)((stride + 7) / 8) * C;
-  hipLaunchKernelGGL((adapter_turn_kernel<T>), dim3((unsigned)((x + 255) / 256), (unsigned)n), dim3(256), 0, st, in, out,
-                     R, C, stride);
-}
-hipError_t launch_adapter_turn(bool is_bf16, const void* in, void* out, int n, int R, int C, int stride,
-                               hipStream_t st) {
-  if (is_bf16) turn_any((const bf16*)in, (bf16*)out, n, R, C, stride, st);
-  else turn_any((const float*)in, (float*)out, n, R, C, stride, st);
-  return hipGetLastError();
-}
-
-// The rows of every adapter, in ascending order: adapter i's are order[start .. start +
-// count), (start, count) = span[i].  Cut at every multiple of `per` these are the slices of
-// the gradients' sums; slice b of adapter i has number b + i in `slices` (adapter, first,
-// rows), so that each number up to M / per + n is written by one workgroup, empty ones
-// too.  A workgroup per adapter reads the whole index twice.
-__global__ __launch_bounds__(1024) void adapter_group_kernel(const int32_t* __restrict__ index, int M, int n, int per,
-                                                             int32_t* __restrict__ order, int2* __restrict__ span,
-                                                             int4* __restrict__ slices) {
+// What the gradients need first, in one launch: the rows of every adapter, and the
+// adapters' matrices turned.
+//
+// Adapter i's rows, in ascending order, are order[start .. start + count), (start, count) =
+// span[i].  Cut at every multiple of `per` they are the slices of the gradients' sums;
+// slice b of adapter i has number b + i in `slices` (adapter, first, rows), so that each
+// number below M / per + n is written by one workgroup, empty ones too.  A workgroup per
+// adapter reads the whole index twice.
+__device__ __forceinline__ void group_rows(const AdapterPrepare& p, int ad) {
   __shared__ int red[2][16];
-  const int ad = blockIdx.x, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, M = p.M;
   int before = 0, mine = 0;
+#pragma unroll 4
   for (int m = threadIdx.x; m < M; m += 1024) {
-    const int i = adapter_of(index, n, m);
+    const int i = adapter_of(p.index, p.n, m);
     before += i >= 0 && i < ad;
     mine += i == ad;
   }
@@ -570,17 +528,20 @@ __global__ __launch_bounds__(1024) void adapter_group_kernel(const int32_t* __re
   int start = 0, count = 0;
 #pragma unroll
   for (int w = 0; w < 16; ++w) start += red[0][w], count += red[1][w];
-  if (threadIdx.x == 0) span[ad] = int2{start, count};
+  if (threadIdx.x == 0) p.span[ad] = int2{start, count};
   // (the last adapter's also write the numbers that rows without an adapter leave over)
-  const int end = start + count, last = ad == n - 1 ? M / per : end / per;
-  for (int b = start / per + (int)threadIdx.x; b <= last; b += 1024) {
-    const int lo = max(start, b * per), hi = min(end, (b + 1) * per);
-    slices[b + ad] = int4{ad, lo, max(hi - lo, 0), 0};
+  const int end = start + count, last = ad == p.n - 1 ? M / p.per : end / p.per;
+  for (int b = start / p.per + (int)threadIdx.x; b <= last; b += 1024) {
+    const int lo = max(start, b * p.per), hi = min(end, (b + 1) * p.per);
+    p.slices[b + ad] = int4{ad, lo, max(hi - lo, 0), 0};
   }
+  if (count == 0) return;
   int at = start;
+  int next = (int)threadIdx.x < M ? adapter_of(p.index, p.n, threadIdx.x) : -1;
   for (int m0 = 0; m0 < M; m0 += 1024) {
     const int m = m0 + (int)threadIdx.x;
-    const bool hit = m < M && adapter_of(index, n, m) == ad;
+    const bool hit = next == ad;
+    next = m + 1024 < M ? adapter_of(p.index, p.n, m + 1024) : -1;
     const uint64_t all = __ballot(hit);
     __syncthreads();   // (the counts of the round before, or of the sums, are read)
     if (lane == 0) red[0][wave] = __popcll(all);
@@ -591,14 +552,54 @@ __global__ __launch_bounds__(1024) void adapter_group_kernel(const int32_t* __re
       skip += w < wave ? red[0][w] : 0;
       sum += red[0][w];
     }
-    if (hit) order[at + skip + __popcll(all & ((1ULL << lane) - 1))] = m;
+    if (hit) p.order[at + skip + __popcll(all & ((1ULL << lane) - 1))] = m;
     at += sum;
   }
 }
 
-hipError_t launch_adapter_group(const int32_t* index, int M, int n, int per, int32_t* order, int2* span, int4* slices,
-                                hipStream_t st) {
-  hipLaunchKernelGGL(adapter_group_kernel, dim3((unsigned)n), dim3(1024), 0, st, index, M, n, per, order, span, slices);
+// out[i][c][r] = in[i][r][c] for rows r < R, 0 for R <= r < stride, thread x of all: 8
+// values of a row of out
+template <typename T>
+__device__ __forceinline__ void turn_rows(const AdapterTurn& d, long x) {
+  const long chunks = (d.stride + 7) / 8, per = chunks * d.C;
+  const int ad = (int)(x / per);
+  x -= ad * per;
+  const int c = (int)(x % d.C), r0 = (int)(x / d.C) * 8;
+  const T* const p = (const T*)d.in + (size_t)ad * d.R * d.C + c;
+  float v[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = r0 + i < d.R ? to_f32(p[(size_t)(r0 + i) * d.C]) : 0.f;
+  store_piece((T*)d.out + ((size_t)ad * d.C + c) * d.stride + r0, d.stride - r0, v);
+}
+
+template <typename T>
+__global__ __launch_bounds__(1024) void adapter_prepare_kernel(AdapterPrepare p) {
+  int block = blockIdx.x;
+  if (block < p.groups) {
+    group_rows(p, block);
+    return;
+  }
+  block -= p.groups;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const AdapterTurn& d = p.turn[i];
+    if (block < d.blocks) {
+      const long x = block * 1024L + threadIdx.x;
+      if (x < (long)((d.stride + 7) / 8) * d.C * p.n) turn_rows<T>(d, x);
+      return;
+    }
+    block -= d.blocks;
+  }
+}
+hipError_t launch_adapter_prepare(bool is_bf16, AdapterPrepare p, hipStream_t st) {
+  long blocks = p.groups;
+  for (AdapterTurn& d : p.turn) {
+    d.blocks = d.in ? (int)(((long)((d.stride + 7) / 8) * d.C * p.n + 1023) / 1024) : 0;
+    blocks += d.blocks;
+  }
+  if (blocks == 0) return hipSuccess;
+  if (is_bf16) hipLaunchKernelGGL((adapter_prepare_kernel<bf16>), dim3((unsigned)blocks), dim3(1024), 0, st, p);
+  else hipLaunchKernelGGL((adapter_prepare_kernel<float>), dim3((unsigned)blocks), dim3(1024), 0, st, p);
   return hipGetLastError();
 }
 
@@ -716,44 +717,37 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterOuter p) {
 
 // dA [n][rank][K] and dB [n][N][rank]: the slices' parts of every adapter, added up in
 // fp64 in ascending order; zeros for an adapter without rows.  A thread takes four
-// columns of one rank (dA), or of four (dB).
+// columns of one rank (dA), or one column of four (dB).
 template <typename T>
-__global__ __launch_bounds__(256) void adapter_sum_kernel(AdapterOuter p, T* dA, T* dB, int per_a, int per_b) {
+__global__ __launch_bounds__(256) void adapter_sum_kernel(AdapterOuter p, T* dA, T* dB, int per_a) {
   const int ad = blockIdx.y;
   const int2 span = p.span ? p.span[ad] : int2{0, ad == 0 ? p.M : 0};
   const int b0 = span.x / p.per, b1 = span.y > 0 ? (span.x + span.y - 1) / p.per + 1 : b0;
   const bool is_b = (int)blockIdx.x >= per_a;
   const long x = ((int)blockIdx.x - (is_b ? per_a : 0)) * 256L + threadIdx.x;
   const AdapterSide& d = is_b ? p.side[1] : p.side[0];
-  const int c4 = (d.cols + 3) / 4;
-  const int c = (int)(x % c4) * 4, jn = is_b ? 4 : 1, j0 = (int)(x / c4) * jn;
+  const int per_row = is_b ? d.cols : (d.cols + 3) / 4;
+  const int c = (int)(x % per_row) * (is_b ? 1 : 4), j0 = (int)(x / per_row) * (is_b ? 4 : 1);
   if (j0 >= p.rank) return;
-  double s[4][4];
-#pragma unroll
-  for (int j = 0; j < 4; ++j)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) s[j][e] = 0.;
-  for (int b = b0; b < b1; ++b) {
-    const float* const at = d.partial + ((size_t)(b + ad) * p.ranks + j0) * d.ldp + c;
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (j < jn) {
-        const f32x4 v = *(const f32x4*)(at + (size_t)j * d.ldp);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) s[j][e] += (double)v[e];
-      }
-  }
+  const float* at = d.partial + ((size_t)(b0 + ad) * p.ranks + j0) * d.ldp + c;
+  const size_t slice = (size_t)p.ranks * d.ldp;
+  double s[4] = {0., 0., 0., 0.};
   if (!is_b) {
-    const float v[4] = {(float)s[0][0], (float)s[0][1], (float)s[0][2], (float)s[0][3]};
-    store4(dA + ((size_t)ad * p.rank + j0) * d.cols + c, d.cols - c, v);
-  } else {
+#pragma unroll 4
+    for (int b = b0; b < b1; ++b, at += slice) {
+      const f32x4 v = *(const f32x4*)at;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (c + e >= d.cols) break;
-      const float v[4] = {(float)s[0][e], (float)s[1][e], (float)s[2][e], (float)s[3][e]};
-      store4(dB + ((size_t)ad * d.cols + c + e) * p.rank + j0, p.rank - j0, v);
+      for (int e = 0; e < 4; ++e) s[e] += (double)v[e];
     }
+  } else {
+#pragma unroll 4
+    for (int b = b0; b < b1; ++b, at += slice)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) s[e] += (double)at[(size_t)e * d.ldp];
   }
+  const float v[4] = {(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
+  if (!is_b) store4(dA + ((size_t)ad * p.rank + j0) * d.cols + c, d.cols - c, v);
+  else store4(dB + ((size_t)ad * d.cols + c) * p.rank + j0, p.rank - j0, v);
 }
 
 template <typename T>
@@ -768,9 +762,9 @@ static void outer_any(AdapterOuter p, int n, int slices, T* dA, T* dB, hipStream
     hipLaunchKernelGGL((adapter_outer_kernel<T, 2>),
                        dim3((unsigned)(p.blocks0 + blocks1), (unsigned)slices, (unsigned)((p.rank + 31) / 32)), dim3(256), 0,
                        st, p);
-  auto blocks = [&](int cols, int per) { return (int)(((long)((cols + 3) / 4) * ((p.rank + per - 1) / per) + 255) / 256); };
-  const int a = dA ? blocks(p.side[0].cols, 1) : 0, b = dB ? blocks(p.side[1].cols, 4) : 0;
-  hipLaunchKernelGGL((adapter_sum_kernel<T>), dim3((unsigned)(a + b), (unsigned)n), dim3(256), 0, st, p, dA, dB, a, b);
+  const int a = dA ? (int)(((long)((p.side[0].cols + 3) / 4) * p.rank + 255) / 256) : 0;
+  const int b = dB ? (int)(((long)p.side[1].cols * ((p.rank + 3) / 4) + 255) / 256) : 0;
+  hipLaunchKernelGGL((adapter_sum_kernel<T>), dim3((unsigned)(a + b), (unsigned)n), dim3(256), 0, st, p, dA, dB, a);
 }
 hipError_t launch_adapter_outer(bool is_bf16, const AdapterOuter& p, int n, int slices, void* dA, void* dB,
                                 hipStream_t st) {

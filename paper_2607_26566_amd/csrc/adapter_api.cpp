@@ -152,9 +152,21 @@ t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, i
   hipStream_t st = (hipStream_t)stream;
   char* const at = (char*)ws;
   const int32_t ldu = adapter_cols(rank);
-  hipError_t err = hipSuccess;
-  if (dx || da) {   // u = s dy B
-    err = launch_adapter_turn(bf, b, at + r.bt, n, N, rank, N, st);
+  const bool sums = da || db;
+  AdapterPrepare pre;
+  std::memset(&pre, 0, sizeof(pre));
+  pre.index = index;
+  pre.M = M;
+  pre.n = n;
+  pre.per = r.per;
+  pre.groups = sums && index ? n : 0;
+  pre.order = (int32_t*)(at + r.order);
+  pre.span = (int2*)(at + r.span);
+  pre.slices = (int4*)(at + r.table);
+  if (dx || da) pre.turn[0] = AdapterTurn{b, at + r.bt, N, rank, N, 0};
+  if (dx) pre.turn[1] = AdapterTurn{a, at + r.at, rank, K, whole8(rank), 0};
+  hipError_t err = launch_adapter_prepare(bf, pre, st);
+  if (err == hipSuccess && (dx || da)) {   // u = s dy B
     AdapterDown d;
     std::memset(&d, 0, sizeof(d));
     d.M = M;
@@ -168,20 +180,14 @@ t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, i
     d.index = index;
     d.t = at + r.u;
     d.ldt = ldu;
-    if (err == hipSuccess) err = launch_adapter_down(bf, d, st);
+    err = launch_adapter_down(bf, d, st);
   }
   if (err == hipSuccess && dx) {
-    err = launch_adapter_turn(bf, a, at + r.at, n, rank, K, whole8(rank), st);
     const AdapterUp up{index, n, whole8(rank), whole8(rank), at + r.at, at + r.u, ldu};
-    if (err == hipSuccess) err = launch_adapter_dx(bf, dy, lddy, w, ldw, M, N, K, up, dx, lddx, (float*)(at + r.dx), st);
+    err = launch_adapter_dx(bf, dy, lddy, w, ldw, M, N, K, up, dx, lddx, (float*)(at + r.dx), st);
   }
-  if (err == hipSuccess && (da || db)) {
-    int slices = (M + r.per - 1) / r.per;
-    if (index) {
-      slices = r.slices;
-      err = launch_adapter_group(index, M, n, r.per, (int32_t*)(at + r.order), (int2*)(at + r.span),
-                                 (int4*)(at + r.table), st);
-    }
+  if (err == hipSuccess && sums) {
+    const int slices = index ? r.slices : (M + r.per - 1) / r.per;
     AdapterOuter o;
     std::memset(&o, 0, sizeof(o));
     o.side[0] = AdapterSide{x, at + r.u, ldx, ldu, K, (float*)(at + r.part_a), whole8(K)};
@@ -196,7 +202,7 @@ t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, i
       o.slices = (const int4*)(at + r.table);
     }
     // (without an index only adapter 0 has rows)
-    if (err == hipSuccess) err = launch_adapter_outer(bf, o, n, slices, da, db, st);
+    err = launch_adapter_outer(bf, o, n, slices, da, db, st);
   }
   return done(err);
 }

@@ -186,13 +186,24 @@ hipError_t launch_adapter_linear(bool is_bf16, const void* x, int ldx, const voi
 size_t adapter_dx_floats(bool is_bf16, int M, int N, int K);
 hipError_t launch_adapter_dx(bool is_bf16, const void* dy, int lddy, const void* w, int ldw, int M, int N, int K,
                              const AdapterUp& up, void* dx, int ldx, float* partial, hipStream_t st);
-// out [n][C][stride] = in [n][R][C] turned, zeros behind R
-hipError_t launch_adapter_turn(bool is_bf16, const void* in, void* out, int n, int R, int C, int stride,
-                               hipStream_t st);
-// the rows of every adapter, and slices of them of at most `per` rows
+// the gradients' first launch: the rows of every adapter, slices of at most `per` of them
+// (groups = n, or 0 without an index), and matrices turned: out [n][C][stride] = in
+// [n][R][C], zeros behind R (in NULL: none)
 int adapter_slice_rows(bool is_bf16, int M, int N, int K, int rank);
-hipError_t launch_adapter_group(const int32_t* index, int M, int n, int per, int32_t* order, int2* span, int4* slices,
-                                hipStream_t st);
+struct AdapterTurn {
+  const void* in;
+  void* out;
+  int R, C, stride, blocks;
+};
+struct AdapterPrepare {
+  const int32_t* index;
+  int M, n, per, groups;
+  int32_t* order;
+  int2* span;
+  int4* slices;
+  AdapterTurn turn[2];
+};
+hipError_t launch_adapter_prepare(bool is_bf16, AdapterPrepare p, hipStream_t st);
 // dA, dB (either may be NULL)
 struct AdapterSide {
   const void *z, *v;                 // [M, cols], [M, ldv]
