@@ -135,8 +135,8 @@ SIGNATURES = {
     "t2i_op_adapter_linear_backward_ws_bytes": (sz, [i32, i32, i32, i32, i32, i32]),
     "t2i_op_adapter_linear_backward": (i32, [i32, i32, i32, i32, vp, i32, vp, i32, vp, i32, i32, i32, vp,
                                              vp, vp, vp, vp, i32, vp, i32, vp, vp, vp, sz, vp]),
-    "t2i_op_adamw_step": (i32, [i32, i32, i32, C.POINTER(i64), C.POINTER(vp), C.POINTER(vp), C.POINTER(vp),
-                                C.POINTER(vp), C.POINTER(vp), f64, f64, f64, f64, f64, i64, vp, vp, vp, vp]),
+    "t2i_op_adamw_step": (i32, [i32, i32, i32, C.POINTER(i64), vp, vp, vp, vp, vp, f64, f64, f64, f64,
+                                f64, i64, vp, vp, vp, vp]),
     "t2i_sched_create": (i32, [f64, C.POINTER(vp)]),
     "t2i_sched_destroy": (None, [vp]),
     "t2i_sched_submit": (i32, [vp, i32, C.c_int64, f64, f64, f64]),

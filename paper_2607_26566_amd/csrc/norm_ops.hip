@@ -34,24 +34,30 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
 // division: m = fma(t, 127 / T, 1.5 2^23) leaves the nearest whole number n in its low
 // bits; the factor, t and the product are off by 2^-24 of themselves each, so that n may
 // be wrong only where the quotient is within 127 3 2^-24 < 2^-15 of a half.  Pieces that
-// hold such a value (an element in 2^14) are settled in fp64, exactly.
+// hold such a value (an element in 2^14) are settled by the sign of 127 t - (n +- 1/2) T:
+// of bf16 factors r = fma(-n, T, 127 t) is exact (127 t has 23 bits, r, at most about T /
+// 2, no more than 24 above the last place of t), of fp32 ones fp64 products with what their
+// rounding leaves are.  (Settled by an fp64 division, one element after the other, 333 rows
+// of 1051 took 11.2 us instead of 8.1, 8192 of 4096 53 instead of 48.)
 
 constexpr float kMagic = 12582912.f;   // 1.5 2^23
 
-// the nearest whole number to 127 t / T (t >= 0, T > 0 products of two fp32 values, n
-// near it): the sign of 127 t - (n +- 1/2) T, whose products are taken with what their
-// rounding leaves
-__device__ __forceinline__ int code_of(double t, double T) {
-  double n = rint(127. * t / T);
-  auto side = [&](double c) {
-    const double p = 127. * t, q = c * T;
-    return (p - q) + (fma(127., t, -p) - fma(c, T, -q));
+// the nearest whole number to 127 t / T, ties to even, from an n that is it or next to it
+__device__ __forceinline__ float settle(float n, float t, float T) {
+  const float r2 = 2.f * fmaf(-n, T, 127.f * t);
+  const bool odd = ((int)n & 1) != 0;
+  return r2 > T || (r2 == T && odd) ? n + 1.f : r2 < -T || (r2 == -T && odd) ? n - 1.f : n;
+}
+// the same where neither 127 t nor the products with T need be exact
+__device__ __forceinline__ double settle(double n, double t, double T) {
+  const double p = 127. * t, pe = fma(127., t, -p);
+  auto beside = [&](double c) {
+    const double q = c * T;
+    return (p - q) + (pe - fma(c, T, -q));
   };
   const bool odd = ((int)n & 1) != 0;
-  const double up = side(n + 0.5), down = side(n - 0.5);
-  if (up > 0. || (up == 0. && odd)) n += 1.;
-  else if (down < 0. || (down == 0. && odd)) n -= 1.;
-  return (int)n;
+  const double up = beside(n + 0.5), down = beside(n - 0.5);
+  return up > 0. || (up == 0. && odd) ? n + 1. : down < 0. || (down == 0. && odd) ? n - 1. : n;
 }
 
 // T: x, w and y; R: resid and h.  TPR threads per row, NV pieces per thread in
@@ -205,11 +211,15 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(Nor
             b[j] = __float_as_uint(m);
           }
           if (far >= 0.5f - 0x1p-14f || !plain) {
-#pragma unroll 1
+#pragma unroll
             for (int j = 0; j < 8; ++j) {
-              const double p = (double)v[i][j] * (double)wv[j];
-              const int n = code_of(fabs(p), exact);
-              b[j] = (uint32_t)(p < 0. ? -n : n);
+              const float n = __uint_as_float(b[j]) - kMagic;
+              if (!WIDE && plain) {
+                b[j] = (uint32_t)(int)settle(n, v[i][j] * wv[j], most);
+              } else {
+                const double p = (double)v[i][j] * (double)wv[j];
+                b[j] = (uint32_t)(int)settle(plain ? (double)n : rint(127. * p / exact), p, exact);
+              }
             }
           }
         }
@@ -446,12 +456,16 @@ __global__ __launch_bounds__(1024) void norm_weight_grad_kernel(const float* __r
 }
 
 constexpr int kNormRegisters = 16384;   // elements of a row that a workgroup holds
-// (a wave per row up to 2048 elements: four rows at a time)
-static int norm_rows_at_once(int K) { return K <= 2048 ? 4 : 1; }
+// a wave per row, four rows at a time, up to 1024 elements (longer: 4451 rows of 1152 22
+// us, 18.4 with a workgroup per row)
+static int norm_rows_at_once(int K) { return K <= 1024 ? 4 : 1; }
+// Workgroups: as few as keep the memory busy, for their sums of columns go out and back
+// (4451 x 1152 19.2 us with 512, 18.5 with 768; 8192 x 4096 51.6, 54; 4096 x 10240 73 with
+// 256, 80 with 512; 2000 x 8192 52.5, 57.8).
 int norm_bwd_blocks(int rows, int K) {
   const int per = norm_rows_at_once(K);
   const long units = ((long)rows + per - 1) / per;
-  return (int)std::max(std::min<long>(units, K <= 2048 ? 1024 : 512), (units + kChain - 1) / kChain);
+  return (int)std::max(std::min<long>(units, K <= 1024 ? 512 : K <= 2048 ? 768 : K <= 4096 ? 512 : 256), (units + kChain - 1) / kChain);
 }
 
 template <typename T, typename R>
@@ -462,8 +476,7 @@ static void norm_bwd_any(const NormBwd& a, float* partial, float* rstd, hipStrea
                      dim3(TPR > 256 ? TPR : 256), 0, st, a, partial)
   if (a.K <= 512) T2I_N(64, 1);
   else if (a.K <= 1024) T2I_N(64, 2);
-  else if (a.K <= 1536) T2I_N(64, 3);
-  else if (a.K <= 2048) T2I_N(64, 4);
+  else if (a.K <= 2048) T2I_N(256, 1);
   else if (a.K <= 4096) T2I_N(256, 2);
   else if (a.K <= 8192) T2I_N(512, 2);
   else if (a.K <= 12288) T2I_N(512, 3);

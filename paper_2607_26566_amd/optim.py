@@ -7,6 +7,8 @@ from __future__ import annotations
 
 import ctypes as C
 import math
+from array import array
+from operator import attrgetter
 from typing import Optional, Sequence, Union
 
 import torch
@@ -18,8 +20,9 @@ from .ops import _check, _elsewhere, _need, _stream, _switch
 _DTYPES = {torch.bfloat16: T2I_BF16, torch.float32: T2I_F32}
 
 
-def _array(pointers):
-    return (C.c_void_p * len(pointers))(*pointers)
+_shape, _dtype, _requires_grad = attrgetter("shape"), attrgetter("dtype"), attrgetter("requires_grad")
+_pointer, _device_of, _whole = torch.Tensor.data_ptr, torch.Tensor.get_device, torch.Tensor.is_contiguous
+assert array("Q").itemsize == C.sizeof(C.c_void_p)
 
 
 def _scalar(t: Optional[torch.Tensor], dev: int, what: str):
@@ -38,7 +41,8 @@ class AdamW:
     are fp32: zeros, or the given ``exp_avg`` and ``exp_avg_sq`` with the number of ``step`` s
     behind them.  bf16 weights have fp32 ``masters`` -- the given ones, or copies -- whose
     rounded values they receive.  All of these are kept (attributes of the same names), to be
-    saved and passed in again by a program that resumes.
+    saved and passed in again by a program that resumes.  A weight's storage may be exchanged
+    between steps, the moments' and masters' may not.
 
     With ``capturable`` the number of steps is counted on the device, so that a captured
     :meth:`step` counts on from replay to replay; without it a step is refused while a graph
@@ -88,14 +92,12 @@ class AdamW:
         """The library's arrays of the tensors' addresses"""
         for what, tensors, dtype in self._state:
             self._listed(tensors, dtype, what)
-        self._at = [t.data_ptr() for t in self._written]
+        self._held = [t.detach() for t in self._written]   # (the addresses stay valid)
         spans = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in self._written if t.numel())
         for (at, size), (nxt, _) in zip(spans, spans[1:]):
             _need(at + size <= nxt, "weights, moments and masters must not overlap", 1)
-        n = len(self.params)
-        self._arrays = [_array(self._at[i:i + n]) for i in range(0, len(self._at), n)]
-        if len(self._arrays) == 3:
-            self._arrays.append(None)
+        self._arrays = [array("Q", map(_pointer, tensors)) for _, tensors, _ in self._state]
+        self._at = [a.buffer_info()[0] for a in self._arrays] + [None] * (4 - len(self._arrays))
 
     def _new(self, make):
         """fp32 tensors of the weights' shapes in one buffer, each at 256 bytes"""
@@ -129,14 +131,14 @@ class AdamW:
                 return self.step(grads, lr=lr, grad_scale=grad_scale)
         kind = _DTYPES.get(grads[0].dtype) if len(grads) else None
         _need(kind is not None, "gradients of all weights, bf16 or fp32", 1)
-        # (lists and sets: a hundred tensors' checks one by one take longer than the step)
-        if ([g.shape for g in grads] != self._shapes or {g.get_device() for g in grads} != {dev}
-                or {g.dtype for g in grads} != {grads[0].dtype} or False in [g.is_contiguous() for g in grads]):
+        # (as lists and sets: the checks of a hundred tensors one by one take longer than the step)
+        if (list(map(_shape, grads)) != self._shapes or set(map(_device_of, grads)) != {dev}
+                or set(map(_dtype, grads)) != {grads[0].dtype} or not all(map(_whole, grads))):
             self._listed(grads, grads[0].dtype, "grads")
-        if [t.data_ptr() for t in self._written] != self._at:   # (a weight's storage was exchanged)
+        if array("Q", map(_pointer, self.params)) != self._arrays[0]:
             self._lay_out()
         if torch.is_grad_enabled():
-            _need(True not in [t.requires_grad for t in self.params] and True not in [g.requires_grad for g in grads],
+            _need(True not in map(_requires_grad, self.params) and True not in map(_requires_grad, grads),
                   "a tensor requires a gradient, which this call does not record: call under torch.no_grad()", 1)
         if getattr(forward_ad, "_current_level", 0) >= 0:   # (within a dual level)
             _need(all(forward_ad.unpack_dual(t).tangent is None for t in (*self._written, *grads)),
@@ -154,9 +156,10 @@ class AdamW:
         else:
             _need(not torch.cuda.is_current_stream_capturing(),
                   "a captured step needs capturable=True: its count would stand still in the graph", 1)
-        p, m, v, masters = self._arrays
+        p, m, v, masters = self._at
+        at = array("Q", map(_pointer, grads))
         _check(load().t2i_op_adamw_step(
-            self._type, kind, len(self.params), self._numel, p, _array([g.data_ptr() for g in grads]), m, v, masters, rate,
+            self._type, kind, len(self.params), self._numel, p, at.buffer_info()[0], m, v, masters, rate,
             self.betas[0], self.betas[1], self.eps, self.weight_decay, self._steps + 1, lr_at, count, scale_at,
             _stream(dev)))
         self._steps += 1
