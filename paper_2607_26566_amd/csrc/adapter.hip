@@ -421,16 +421,17 @@ template <class D, typename T, bool U>
 __global__ __launch_bounds__(D::THREADS, 1) void adapter_dx_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
                                                                    AdapterUp up, T* dx, int ldx, int M, int K) {
   using P = TileProduct<D, elem_of<T>(), false, true, false, false, U>;
-  __shared__ __attribute__((aligned(1024))) char smem[D::RING];
+  __shared__ __attribute__((aligned(1024))) char smem[D::KG * D::RING];
   int tm, tn;
   tile_place(s, blockIdx.x, gridDim.x, tm, tn);
   if (sp.partial) take_slice(sp, s);
   typename P::Acc acc[D::TM][D::TN];
   const int m0 = tm * D::BM, n0 = first_column<D, U>(tn, K);
   const Adapters<P, D, T> from(up, m0, n0, M, K);
-  P::run(smem, a, b, s, m0, n0, acc, [&](f32x4 (&c)[D::TM][D::TN]) {
+  const bool mine = P::run_groups(smem, a, b, s, m0, n0, acc, [&](f32x4 (&c)[D::TM][D::TN]) {
     if (blockIdx.y == 0) from(c);
   });
+  if (!mine) return;
   if (from.LATE && blockIdx.y == 0) {
     tile_barrier();
     from.finish(smem, acc);
@@ -467,10 +468,29 @@ hipError_t launch_adapter_linear(bool is_bf16, const void* x, int ldx, const voi
   return hipGetLastError();
 }
 
-size_t adapter_dx_floats(bool is_bf16, int M, int N, int K) {
+// dx has the shapes with groups of waves, too, which need no second launch: taken where
+// they are estimated to beat the best number of slices (fp32 333 x 1155 x 1153 @@ us)
+SplitPick adapter_dx_pick(bool is_bf16, int M, int N, int K) {
   const SplitPick p = split_dx(is_bf16, M, K, N);
+  const int steps = is_bf16 ? (N + 63) / 64 : (N + 31) / 32;
+  if (steps < 4 || !few_tiles(M, K)) return p;
+  const TileChoice* const tiles = is_bf16 ? kTiles : kTilesF32;
+  const int first = is_bf16 ? kTile32k : kF32Groups;
+  const TilePick g = choose_tile(tiles + first, 2, M, K, steps, 1.f);
+  const TilePick split = choose_tile(tiles + p.shape, 1, M, K, p.per, p.slices > 1 ? 2.f : 1.f, p.slices);
+  const float us = split.us + (p.slices > 1 ? 4.f + (float)p.slices * M * K * 8 / 4e6f : 0.f);
+  return g.us < us ? SplitPick{first + g.shape, 1, steps} : p;
+}
+size_t adapter_dx_floats(bool is_bf16, int M, int N, int K) {
+  const SplitPick p = adapter_dx_pick(is_bf16, M, N, K);
   return p.slices > 1 ? (size_t)p.slices * M * whole4(K) : 0;
 }
+#define T2I_TILES_GRAD(SHAPE, CALL)                    \
+  switch (SHAPE) {                                     \
+    case kTile32k: { using D = Tile32k; CALL; break; } \
+    case kTile16k: { using D = Tile16k; CALL; break; } \
+    default: T2I_TILES(SHAPE, CALL)                    \
+  }
 
 template <class D, typename T, bool U = false>
 static void adapter_dx_launch(const void* dy, int lddy, const void* w, int ldw, int M, int N, int K, const AdapterUp& up,
@@ -485,16 +505,16 @@ static void adapter_dx_launch(const void* dy, int lddy, const void* w, int ldw, 
 
 hipError_t launch_adapter_dx(bool is_bf16, const void* dy, int lddy, const void* w, int ldw, int M, int N, int K,
                              const AdapterUp& up, void* dx, int ldx, float* partial, hipStream_t st) {
-  const SplitPick pick = split_dx(is_bf16, M, K, N);
+  const SplitPick pick = adapter_dx_pick(is_bf16, M, N, K);
   const Split sp{pick.slices > 1 ? partial : nullptr, pick.per, (int)whole4(K)};
   if (is_bf16) {
-    T2I_TILES(pick.shape, (adapter_dx_launch<D, bf16>(dy, lddy, w, ldw, M, N, K, up, (bf16*)dx, ldx, pick, sp, st)))
+    T2I_TILES_GRAD(pick.shape, (adapter_dx_launch<D, bf16>(dy, lddy, w, ldw, M, N, K, up, (bf16*)dx, ldx, pick, sp, st)))
   } else if (f32_pieces({N, K, lddy, ldw}, {dy, w})) {
-    T2I_TILES_F32_DX(pick.shape,
-                     (adapter_dx_launch<D, float>(dy, lddy, w, ldw, M, N, K, up, (float*)dx, ldx, pick, sp, st)))
+    T2I_TILES_F32_FWD(pick.shape,
+                      (adapter_dx_launch<D, float>(dy, lddy, w, ldw, M, N, K, up, (float*)dx, ldx, pick, sp, st)))
   } else {
-    T2I_TILES_F32_DX(pick.shape,
-                     (adapter_dx_launch<D, float, true>(dy, lddy, w, ldw, M, N, K, up, (float*)dx, ldx, pick, sp, st)))
+    T2I_TILES_F32_FWD(pick.shape,
+                      (adapter_dx_launch<D, float, true>(dy, lddy, w, ldw, M, N, K, up, (float*)dx, ldx, pick, sp, st)))
   }
   return hipGetLastError();
 }

@@ -277,6 +277,9 @@ inline SplitPick choose_split(const TileChoice* tiles, int shapes, long rows, lo
   return best;
 }
 
+// (adapter.hip: dx beside adapters)
+SplitPick adapter_dx_pick(bool is_bf16, int M, int N, int K);
+
 inline long whole4(long cols) { return (cols + 3) / 4 * 4; }
 inline SplitPick split_dx(bool is_bf16, long rows, long cols, int k) {
   return is_bf16 ? choose_split(kTiles, kGradTiles, rows, cols, (k + 63) / 64)

@@ -303,7 +303,7 @@ extern "C" int t2i_test_block_tile(int op, int is_bf16, int M, int F, int K, int
   SplitPick p{0, 1, 0};
   const bool f32 = op != 0 && !is_bf16;
   if (op == 4) p.shape = f32 ? tile_index_f32(M, F, (K + 31) / 32) : tile_index(M, F, (K + 63) / 64, 1.f);
-  else if (op == 5) p = split_dx(is_bf16, M, K, F);
+  else if (op == 5) p = adapter_dx_pick(is_bf16, M, F, K);
   else if (op == 0) p.shape = tile_index(M, F, i8_row(K) / 128, 1.f);
   else if (op == 1) p.shape = f32 ? tile_index_f32(M, 2L * F, (K + 31) / 32) : tile_index(M, 2L * F, (K + 63) / 64, 0.5f);
   else p = op == 2 ? split_dx(is_bf16, M, K, 2 * gated_cols(F)) : split_dw(is_bf16, 2L * F, K, M);
@@ -313,7 +313,7 @@ extern "C" int t2i_test_block_tile(int op, int is_bf16, int M, int F, int K, int
   *columns = c.bn;
   *per_cu = stream ? 1 : c.per_cu;
   const int group = p.shape - (f32 ? kF32Groups : kTile32k);
-  *slices = op > 1 && op != 4 ? p.slices : group == 0 ? Tile32k::KG : group == 1 ? Tile16k::KG : 1;
+  *slices = p.slices > 1 || op == 2 || op == 3 ? p.slices : group == 0 ? Tile32k::KG : group == 1 ? Tile16k::KG : 1;
   return 1;
 }
 
