@@ -374,7 +374,8 @@ t2i_status t2i_op_add_rms_norm_backward(int32_t dtype, int32_t resid_dtype, int3
  *   (ldt at least that, % 8 == 0, 16-byte aligned): scratch memory, or kept for
  *   t2i_op_adapter_linear_backward.
  *   bf16: N, K, ldx, ldw % 8 == 0, x, w, a 16-byte aligned.  fp32: any sizes, strides
- *   and alignment.  1 <= rank <= 128, n <= 32767, n max(N, K) rank < 2^33; M <= 2^24,
+ *   and alignment.  1 <= rank <= 128, n <= 32767, n max(N, K) times
+ *   rank rounded up to 8 below 2^32; M <= 2^24,
  *   fewer than 2^23 pieces of 64 x 64 outputs; rows of x and w less than 8 MiB apart.
  * Any order of the index; rows of one adapter next to each other are faster.  Nothing
  * of another row's adapter enters a row's sums, not even as zeros.  No output may

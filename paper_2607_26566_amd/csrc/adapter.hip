@@ -182,11 +182,19 @@ static void down_launch(const AdapterDown& p, hipStream_t st) {
 template <typename T, bool U>
 static void down_tiles(const AdapterDown& p, hipStream_t st) {
   const long steps = ((long)p.K * (int)sizeof(T) + 127) / 128;
-  // groups of waves have a step each at least
+  // Groups of waves have a step each at least.  Eight, one workgroup to a CU, while there
+  // are no more tiles than CUs, else four and two (with a product of 8 columns behind it:
+  // 7531 rows of 1152, rank 32 19.2 and 16.7 us, 16000 of 640, rank 8 19.7 and 14.3; 300 of
+  // 4096, rank 16 16.5 and 17.6), and 32 rows to read the adapter half as often for many
+  // ranks (8192 rows of 4608, rank 64 45 and 35.6).
+  const bool many = p.M > 16 * 256;
   if (steps < 8) down_launch<TileDims<16, 32, 1, 1, 4>, T, U>(p, st);
-  else if (p.rank <= 16) down_launch<TileDims<16, 16, 1, 1, 4, 8>, T, U>(p, st);
-  else if (p.rank <= 32) down_launch<TileDims<16, 32, 1, 1, 3, 8>, T, U>(p, st);
-  else down_launch<TileDims<16, 64, 1, 1, 3, 4>, T, U>(p, st);
+  else if (p.rank <= 16 && !many) down_launch<TileDims<16, 16, 1, 1, 4, 8>, T, U>(p, st);
+  else if (p.rank <= 16) down_launch<TileDims<16, 16, 1, 1, 3, 4>, T, U>(p, st);
+  else if (p.rank <= 32 && !many) down_launch<TileDims<16, 32, 1, 1, 3, 8>, T, U>(p, st);
+  else if (p.rank <= 32) down_launch<TileDims<16, 32, 1, 1, 3, 4>, T, U>(p, st);
+  else if (!many) down_launch<TileDims<16, 64, 1, 1, 3, 4>, T, U>(p, st);
+  else down_launch<TileDims<32, 64, 1, 1, 3, 4>, T, U>(p, st);
 }
 template <typename T>
 static void down_any(const AdapterDown& p, hipStream_t st) {

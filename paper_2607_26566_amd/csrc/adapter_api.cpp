@@ -23,7 +23,7 @@ t2i_status done(hipError_t e) {
 
 bool bad_sizes(int32_t M, int32_t N, int32_t K, int32_t n, int32_t rank) {
   return M < 1 || N < 1 || K < 1 || n < 1 || rank < 1 || M > 1 << 24 || N > 1 << 28 || K > 1 << 28 || n > 32767 ||
-         rank > 128 || too_large(M, N) || (int64_t)n * std::max(N, K) * rank >= 1LL << 33;
+         rank > 128 || too_large(M, N) || (int64_t)n * std::max(N, K) * whole8(rank) >= 1LL << 32;
 }
 
 // the gradients' workspace

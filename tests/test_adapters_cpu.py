@@ -85,7 +85,9 @@ def test_adapter_linear_backward_refuses():
         (dict(lddy=2 ** 22), SHAPE), (dict(dy=P + 8), INVALID), (dict(dx=P + 8), INVALID), (dict(da=P + 1), INVALID),
         (dict(db=P + 1), INVALID), (dict(ws=P + 128), INVALID), (dict(ws_bytes=need - 1), WORKSPACE),
         # more slices of the sums than a launch holds
-        (dict(n=32767, M=2 ** 23, K=8192, N=8192, ldx=8192, ldw=8192, lddy=8192, lddx=8192, rank=16), SHAPE)])
+        (dict(dtype=F32, n=32767, M=2 ** 16, K=2 ** 14, N=2 ** 14, ldx=2 ** 14, ldw=2 ** 14, lddy=2 ** 14, lddx=2 ** 14,
+              rank=8), SHAPE)])
+    assert b"launch" in lib.t2i_ops_last_error()
 
 
 def test_python_calls_refuse_what_differentiation_follows(monkeypatch):

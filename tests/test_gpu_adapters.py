@@ -91,6 +91,28 @@ def test_adapter_linear(M, N, K, n, rank, order, dtype):
     within(out, y, U[dtype] * (A(y) + err) + err, "y")
 
 
+@pytest.mark.parametrize("order", [None, "runs", "scattered"])
+@pytest.mark.parametrize("K,rank", [(72, 9), (520, 16), (520, 20), (523, 50), (264, 100)])
+@DTYPES
+def test_narrow_products_of_more_tiles_than_cus(K, rank, order, dtype):
+    """More than 4096 rows, with the gradients of both kinds."""
+    M, N = 4200, 64
+    if dtype == BF16:
+        K = K // 8 * 8
+    o, kw = operands(M, N, K, 1 if order is None else 5, rank, order, dtype, 23)
+    h = host(o, kw)
+    y, err, t, t_err = forward_bounds(h, None, dtype)
+    out, got = t2i.adapter_linear(**o, **kw, save_t=True)
+    within(got[:, :rank], t, t_err, "t")
+    assert not got[:, rank:].any()
+    within(out, y, U[dtype] * (A(y) + err) + err, "y")
+    dy, hdy = rnd(24, (M, N), 1.0, dtype)
+    grads = t2i.adapter_linear_backward(dy, **o, t=got, **kw)
+    ref, bounds = backward_bounds(h, hdy, dtype)
+    for v, name in zip(grads, ("dx", "da", "db")):
+        within(v, ref[name], U[dtype] * (A(ref[name]) + bounds[name]) + bounds[name], name)
+
+
 def test_the_largest_tiles_are_reached():
     v = [C.c_int() for _ in range(4)]
     for op, M, N, K in ((4, 4000, 4096, 640), (4, 2100, 4608, 1152), (5, 4000, 640, 4096)):
