@@ -366,13 +366,12 @@ t2i_status t2i_op_add_rms_norm_backward(int32_t dtype, int32_t resid_dtype, int3
  * then the epilogues of t2i_op_linear.
  *   x [M, K] (stride ldx), w [N, K] (stride ldw), bias [N] or NULL, a
  *   [n][rank][K] and b [n][N][rank] (contiguous; adapters of smaller rank: zeros),
- *   out [M, N] (stride ldo), t [M] rows (stride ldt), all of dtype; scale fp32 [n]
+ *   out [M, N] (stride ldo), all of dtype; scale fp32 [n]
  *   or NULL (ones); index (device, [M]) or NULL: every row takes adapter 0.  A row
  *   whose index is not in 0 .. n - 1 takes no adapter.  The rest as t2i_op_linear.
- *   Products and sums in fp32; t is rounded to dtype once (the second product's
- *   operand), y once.  t receives rank columns and zeros up to rank rounded up to 32
- *   (ldt at least that, % 8 == 0, 16-byte aligned): scratch memory, or kept for
- *   t2i_op_adapter_linear_backward.
+ *   Products and sums in fp32, one rounding.  t fp32 receives rank columns and zeros up
+ *   to rank rounded up to 32 (ldt at least that, % 8 == 0, 16-byte aligned): scratch
+ *   memory, or kept for t2i_op_adapter_linear_backward.
  *   bf16: N, K, ldx, ldw % 8 == 0, x, w, a 16-byte aligned.  fp32: any sizes, strides
  *   and alignment.  1 <= rank <= 128, n <= 32767, n max(N, K) times
  *   rank rounded up to 8 below 2^32; M <= 2^24,
@@ -384,7 +383,7 @@ t2i_status t2i_op_add_rms_norm_backward(int32_t dtype, int32_t resid_dtype, int3
 t2i_status t2i_op_adapter_linear(int32_t dtype, int32_t epilogue, int32_t M, int32_t N, int32_t K,
                                  const void* x, int32_t ldx, const void* w, int32_t ldw,
                                  const void* bias, int32_t n, int32_t rank, const void* a,
-                                 const void* b, const float* scale, const int32_t* index, void* t,
+                                 const void* b, const float* scale, const int32_t* index, float* t,
                                  int32_t ldt, void* out, int32_t ldo, float* resid, int32_t ldr,
                                  void* resid_copy, const float* gate, void* stream);
 
@@ -395,8 +394,8 @@ t2i_status t2i_op_adapter_linear(int32_t dtype, int32_t epilogue, int32_t M, int
  *   dx[m] = W^T dy[m] + A_i^T u[m]   [M, K] (stride lddx),
  *   da_i = sum over the rows of adapter i of u[m] x[m]^T   [n][rank][K],
  *   db_i = sum of dy[m] t[m]^T   [n][N][rank],
- * all of dtype; zeros for an adapter that no row takes.  u is rounded to dtype once;
- * products and sums are fp32 or more, in a fixed order.  dx, da, db may each be NULL:
+ * all of dtype; zeros for an adapter that no row takes.  Products and sums are fp32 or
+ * more, in a fixed order.  dx, da, db may each be NULL:
  * not computed.  Sizes and alignment as forward (dy as x); b 16-byte aligned; the
  * slices of the sums must fit a launch (T2I_ERR_SHAPE).  ws as in
  * t2i_op_gated_linear_backward.  No output may overlap an input.
@@ -407,7 +406,7 @@ t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, i
                                           const void* dy, int32_t lddy, const void* x, int32_t ldx,
                                           const void* w, int32_t ldw, int32_t n, int32_t rank,
                                           const void* a, const void* b, const float* scale,
-                                          const int32_t* index, const void* t, int32_t ldt,
+                                          const int32_t* index, const float* t, int32_t ldt,
                                           void* dx, int32_t lddx, void* da, void* db, void* ws,
                                           size_t ws_bytes, void* stream);
 

@@ -6,6 +6,10 @@
 // tiles of gemm_tile.h, whose accumulators take t B^T before the epilogue; and the
 // adapters' own gradients, sums over the rows of each.
 //
+// t (and the gradients' u) is fp32.  The matrix cores take it as two bf16 values, the
+// rounded one and what rounding leaves, 2^-17 of it short: rounded once it would raise the
+// error of dA and dB, whose operand it is, from 0.0017 to 0.0024.
+//
 // Adapters never meet: a row's sums hold nothing of another row's adapter, not even
 // times zero (a NaN in one tenant's adapter stays in that tenant's rows).
 #include <algorithm>
@@ -54,6 +58,25 @@ __device__ __forceinline__ float element(const i32x4& v, int i) {
   else
     return __int_as_float(v[i]);
 }
+// a lane's operand of t: L consecutive values, bf16 in two parts
+template <typename T>
+struct Exact {
+  i32x4 hi, lo;
+  __device__ __forceinline__ void set(const float (&v)[kLaneK<T>]) {
+    if constexpr (sizeof(T) == 2) {
+      bf16x8 h, l;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        h[i] = (bf16)v[i];
+        const float f = (float)h[i];
+        l[i] = (bf16)(__builtin_isinf(f) ? 0.f : v[i] - f);
+      }
+      hi = __builtin_bit_cast(i32x4, h), lo = __builtin_bit_cast(i32x4, l);
+    } else {
+      hi = i32x4{__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
+    }
+  }
+};
 // c[j][m] += sum_k a[j][k] b[m][k], 32 (fp32: 16) of k: lane (x = lane & 15, g = lane >> 4)
 // gives k = L g .. of row x of both; it holds c[4 g + r][x]
 template <typename T>
@@ -67,6 +90,19 @@ __device__ __forceinline__ f32x4 narrow_mfma(const i32x4& a, const i32x4& b, f32
       c = __builtin_amdgcn_mfma_f32_16x16x4f32(__int_as_float(a[k]), __int_as_float(b[k]), c, 0, 0, 0);
     return c;
   }
+}
+
+template <typename T>
+__device__ __forceinline__ f32x4 narrow_mfma(const i32x4& a, const Exact<T>& b, f32x4 c) {
+  c = narrow_mfma<T>(a, b.hi, c);
+  if constexpr (sizeof(T) == 2) c = narrow_mfma<T>(a, b.lo, c);
+  return c;
+}
+template <typename T>
+__device__ __forceinline__ f32x4 narrow_mfma(const Exact<T>& a, const i32x4& b, f32x4 c) {
+  c = narrow_mfma<T>(a.hi, b, c);
+  if constexpr (sizeof(T) == 2) c = narrow_mfma<T>(a.lo, b, c);
+  return c;
 }
 
 // ---------------------------------------------------------------------------
@@ -105,7 +141,7 @@ __global__ __launch_bounds__(256) void adapter_down_rows_kernel(AdapterDown p) {
   if (j >= RJ) return;
   const float v = (red[0][j] + red[1][j]) + (red[2][j] + red[3][j]);
   const float scale = ad >= 0 ? (p.scale ? p.scale[ad] : 1.f) : 0.f;
-  ((T*)p.t)[(size_t)m * p.ldt + j0 + j] = from_f32<T>(ad >= 0 && j0 + j < p.rank ? v * scale : 0.f);
+  p.t[(size_t)m * p.ldt + j0 + j] = ad >= 0 && j0 + j < p.rank ? v * scale : 0.f;
 }
 
 // Many rows: a tile of rows and all ranks (up to 64), whose groups of waves share k as
@@ -133,10 +169,10 @@ __global__ __launch_bounds__(D::THREADS, 1) void adapter_down_kernel(AdapterDown
   }
   auto store = [&](int i, int j, const f32x4& v) {
     const int m = m0 + i * 16 + fr, c = j0 + j * 16 + g * 4;
-    float o[4];
+    f32x4 o;
 #pragma unroll
     for (int r = 0; r < 4; ++r) o[r] = c + r < p.rank ? v[r] : 0.f;
-    if (c < cols) store4((T*)p.t + (size_t)m * p.ldt + c, 4, o);
+    if (c < cols) *(f32x4*)(p.t + (size_t)m * p.ldt + c) = o;
   };
   const bool behind = j0 >= p.rank;   // the zeros behind the ranks
   if (threadIdx.x < 64) {
@@ -239,10 +275,23 @@ struct Adapters {
       id[i] = m < M ? a : -2;
     }
   }
-  // (t's and a matrix's rows of a wave span less than 2^31 bytes)
-  __device__ __forceinline__ i32x4 t_at(int i, int k) const {
-    const T* const t = (const T*)u.t + (size_t)mw * u.ldt;
-    return load_k<T>(t, (uint32_t)(min(P::row_of(i, fr), M - 1 - mw) * u.ldt) * (uint32_t)sizeof(T), k, u.ldt, true);
+  // (t's and a matrix's rows of a wave span less than 2^31 bytes; t has whole steps)
+  __device__ __forceinline__ void t_at(int i, int k, float (&v)[L]) const {
+    const float* const t = u.t + (size_t)mw * u.ldt;
+    const float* const p = t + (uint32_t)(min(P::row_of(i, fr), M - 1 - mw) * u.ldt + k);
+#pragma unroll
+    for (int q = 0; q < L / 4; ++q) {
+      const f32x4 w = *(const f32x4*)(p + 4 * q);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[4 * q + e] = w[e];
+    }
+  }
+  __device__ __forceinline__ Exact<T> exact_t(int i, int k) const {
+    float v[L];
+    t_at(i, k, v);
+    Exact<T> x;
+    x.set(v);
+    return x;
   }
   __device__ __forceinline__ i32x4 p_at(int ad, int j, int x, int k) const {
     const T* const p = (const T*)u.p + ((size_t)ad * N + nw) * u.stride;
@@ -263,23 +312,23 @@ struct Adapters {
       if (first < 0) return;
 #pragma unroll 1
       for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
-        i32x4 tv[TM];
+        i32x4 pv[TN];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) tv[i] = t_at(i, k0 + g * L);
+        for (int j = 0; j < TN; ++j) pv[j] = p_at(first, j, fr, k0 + g * L);
 #pragma unroll
-        for (int j = 0; j < TN; ++j) {
-          const i32x4 pv = p_at(first, j, fr, k0 + g * L);
+        for (int i = 0; i < TM; ++i) {
+          const Exact<T> tv = exact_t(i, k0 + g * L);
 #pragma unroll
-          for (int i = 0; i < TM; ++i) acc[i][j] = narrow_mfma<T>(pv, tv[i], acc[i][j]);
+          for (int j = 0; j < TN; ++j) acc[i][j] = narrow_mfma<T>(pv[j], tv, acc[i][j]);
         }
       }
     } else if constexpr (LATE) {
     } else if constexpr (TM > 1) {
 #pragma unroll 1
       for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
-        i32x4 tv[TM];
+        Exact<T> tv[TM];
 #pragma unroll
-        for (int i = 0; i < TM; ++i) tv[i] = t_at(i, k0 + g * L);
+        for (int i = 0; i < TM; ++i) tv[i] = exact_t(i, k0 + g * L);
         int now = -1;
 #pragma unroll 1
         for (;;) {   // the adapters in ascending order
@@ -307,14 +356,15 @@ struct Adapters {
     } else if (id[0] >= 0) {
 #pragma unroll 1
       for (int k = 0; k < u.rank; k += L) {
-        const i32x4 tv = t_at(0, k);
+        float tv[L];
+        t_at(0, k, tv);
 #pragma unroll
         for (int j = 0; j < TN; ++j)
 #pragma unroll
           for (int r = 0; r < 4; ++r) {
             const i32x4 pv = p_at(id[0], j, g * 4 + r, k);
 #pragma unroll
-            for (int e = 0; e < L; ++e) acc[0][j][r] = fmaf(element<T>(tv, e), element<T>(pv, e), acc[0][j][r]);
+            for (int e = 0; e < L; ++e) acc[0][j][r] = fmaf(tv[e], element<T>(pv, e), acc[0][j][r]);
           }
       }
     }
@@ -346,7 +396,7 @@ struct Adapters {
             for (int j = 0; j < TN; ++j) add[j] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
             for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
-              const i32x4 tv = t_at(h * HALF + i, k0 + g * L);
+              const Exact<T> tv = exact_t(h * HALF + i, k0 + g * L);
 #pragma unroll
               for (int j = 0; j < TN; ++j) add[j] = narrow_mfma<T>(p_at(now, j, fr, k0 + g * L), tv, add[j]);
             }
@@ -367,9 +417,16 @@ struct Adapters {
   }
 };
 
+// waves per SIMD that a tile's LDS leaves room for, which the registers should, too (128 x
+// 128 with 134 instead of 128 of them: 7531 x 4608 x 1152 148 instead of 105 us)
+template <class D>
+constexpr int waves_per_simd() {
+  return (160 * 1024) / (D::KG * D::RING + 8 * D::BN) * D::THREADS / 256;
+}
+
 // y = x W^T + t B^T + bias, then the linear layer's epilogues
 template <class D, typename T, bool RES, bool U>
-__global__ __launch_bounds__(D::THREADS, 1) void adapter_linear_kernel(TileOperand a, TileOperand b, TileShape s,
+__global__ __launch_bounds__(D::THREADS, waves_per_simd<D>()) void adapter_linear_kernel(TileOperand a, TileOperand b, TileShape s,
                                                                        AdapterUp up, LinearEpi e, int M, int N) {
   using P = TileProduct<D, elem_of<T>(), false, false, false, false, U>;
   constexpr int THREADS = D::THREADS, NE = (RES ? 2 : 1) * D::BN;
@@ -426,7 +483,7 @@ __global__ __launch_bounds__(D::THREADS, 1) void adapter_linear_kernel(TileOpera
 
 // dx = dy W + u A; where the contraction is split, the first slice takes the adapters
 template <class D, typename T, bool U>
-__global__ __launch_bounds__(D::THREADS, 1) void adapter_dx_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
+__global__ __launch_bounds__(D::THREADS, waves_per_simd<D>()) void adapter_dx_kernel(TileOperand a, TileOperand b, TileShape s, Split sp,
                                                                    AdapterUp up, T* dx, int ldx, int M, int K) {
   using P = TileProduct<D, elem_of<T>(), false, true, false, false, U>;
   __shared__ __attribute__((aligned(1024))) char smem[D::KG * D::RING];
@@ -664,7 +721,7 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterOuter p) {
   }
   if (rows <= 0) return;
   const T* const z = (const T*)d.z;
-  const T* const v = (const T*)d.v;
+  const float* const v = d.v;
   const bool in = c0 < C, part = c0 + L > C;
   f32x4 acc[L][RT];
 #pragma unroll
@@ -673,7 +730,8 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterOuter p) {
     for (int jt = 0; jt < RT; ++jt) acc[q][jt] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 1
   for (int r0 = wave * STEP; r0 < rows; r0 += 4 * STEP) {
-    i32x4 raw[L], vv[RT];
+    i32x4 raw[L];
+    Exact<T> vv[RT];
     int row[L];
 #pragma unroll
     for (int i = 0; i < L; ++i) {
@@ -687,15 +745,11 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterOuter p) {
     }
 #pragma unroll
     for (int jt = 0; jt < RT; ++jt) {
-      vv[jt] = i32x4{0, 0, 0, 0};
       const int j = min(j0 + jt * 16 + fr, d.ldv - 1);
+      float e[L];
 #pragma unroll
-      for (int i = 0; i < L; ++i)
-        if (row[i] >= 0) {
-          const T e = v[(size_t)row[i] * d.ldv + j];
-          if constexpr (sizeof(T) == 2) vv[jt][i / 2] |= (int)((uint32_t)__builtin_bit_cast(uint16_t, e) << (16 * (i & 1)));
-          else vv[jt][i] = __float_as_int(e);
-        }
+      for (int i = 0; i < L; ++i) e[i] = row[i] >= 0 ? v[(size_t)row[i] * d.ldv + j] : 0.f;
+      vv[jt].set(e);
     }
 #pragma unroll
     for (int q = 0; q < L; ++q) {

@@ -43,7 +43,7 @@ Room room_of(bool bf, int32_t M, int32_t N, int32_t K, int32_t n, int32_t rank) 
     return here;
   };
   const size_t ranks = (rank + 3) / 4 * 4;
-  r.u = take((size_t)M * adapter_cols(rank) * e);
+  r.u = take((size_t)M * adapter_cols(rank) * 4);
   r.at = take((size_t)n * K * whole8(rank) * e);
   r.bt = take((size_t)n * rank * N * e);
   r.order = take((size_t)M * 4);
@@ -63,7 +63,7 @@ bool too_many_slices(bool bf, const Room& r, int32_t N, int32_t K, int32_t rank)
 
 t2i_status check_operands(int32_t dtype, int32_t M, int32_t N, int32_t K, const void* x, int32_t ldx, const void* w,
                           int32_t ldw, int32_t n, int32_t rank, const void* a, const void* b, const float* scale,
-                          const int32_t* index, const void* t, int32_t ldt) {
+                          const int32_t* index, const float* t, int32_t ldt) {
   if (bad_dtype(dtype)) return ops_fail(T2I_ERR_INVALID_ARG, "bad dtype");
   if (bad_sizes(M, N, K, n, rank)) return ops_fail(T2I_ERR_SHAPE, "bad shape");
   if (!x || !w || !a || !b || !t) return ops_fail(T2I_ERR_INVALID_ARG, "NULL operand");
@@ -86,7 +86,7 @@ extern "C" {
 
 t2i_status t2i_op_adapter_linear(int32_t dtype, int32_t epilogue, int32_t M, int32_t N, int32_t K, const void* x,
                                  int32_t ldx, const void* w, int32_t ldw, const void* bias, int32_t n, int32_t rank,
-                                 const void* a, const void* b, const float* scale, const int32_t* index, void* t,
+                                 const void* a, const void* b, const float* scale, const int32_t* index, float* t,
                                  int32_t ldt, void* out, int32_t ldo, float* resid, int32_t ldr, void* resid_copy,
                                  const float* gate, void* stream) {
   if (epilogue < T2I_EPI_STORE || epilogue > T2I_EPI_RESID_GATED)
@@ -132,7 +132,7 @@ size_t t2i_op_adapter_linear_backward_ws_bytes(int32_t dtype, int32_t M, int32_t
 t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, int32_t K, const void* dy, int32_t lddy,
                                           const void* x, int32_t ldx, const void* w, int32_t ldw, int32_t n,
                                           int32_t rank, const void* a, const void* b, const float* scale,
-                                          const int32_t* index, const void* t, int32_t ldt, void* dx, int32_t lddx,
+                                          const int32_t* index, const float* t, int32_t ldt, void* dx, int32_t lddx,
                                           void* da, void* db, void* ws, size_t ws_bytes, void* stream) {
   const t2i_status s = check_operands(dtype, M, N, K, x, ldx, w, ldw, n, rank, a, b, scale, index, t, ldt);
   if (s != T2I_OK) return s;
@@ -178,19 +178,19 @@ t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, i
     d.a = at + r.bt;
     d.scale = scale;
     d.index = index;
-    d.t = at + r.u;
+    d.t = (float*)(at + r.u);
     d.ldt = ldu;
     err = launch_adapter_down(bf, d, st);
   }
   if (err == hipSuccess && dx) {
-    const AdapterUp up{index, n, whole8(rank), whole8(rank), at + r.at, at + r.u, ldu};
+    const AdapterUp up{index, n, whole8(rank), whole8(rank), at + r.at, (const float*)(at + r.u), ldu};
     err = launch_adapter_dx(bf, dy, lddy, w, ldw, M, N, K, up, dx, lddx, (float*)(at + r.dx), st);
   }
   if (err == hipSuccess && sums) {
     const int slices = index ? r.slices : (M + r.per - 1) / r.per;
     AdapterOuter o;
     std::memset(&o, 0, sizeof(o));
-    o.side[0] = AdapterSide{x, at + r.u, ldx, ldu, K, (float*)(at + r.part_a), whole8(K)};
+    o.side[0] = AdapterSide{x, (const float*)(at + r.u), ldx, ldu, K, (float*)(at + r.part_a), whole8(K)};
     o.side[1] = AdapterSide{dy, t, lddy, ldt, N, (float*)(at + r.part_b), whole8(N)};
     o.M = M;
     o.per = r.per;

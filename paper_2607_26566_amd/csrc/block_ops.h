@@ -148,7 +148,7 @@ hipError_t launch_add_rms_norm_bwd(bool is_bf16, bool resid_bf16, const NormBwd&
 // columns of t and of the gradients' u: rank rounded up, zeros behind it
 __host__ __device__ inline int adapter_cols(int rank) { return (rank + 31) / 32 * 32; }
 
-// t = s x a^T: x [M, K], a [n][rank][K], t [M][ldt], ldt >= adapter_cols(rank)
+// t = s x a^T: x [M, K], a [n][rank][K], t fp32 [M][ldt], ldt >= adapter_cols(rank)
 struct AdapterDown {
   int M, K, n, rank;
   const void* x;
@@ -156,7 +156,7 @@ struct AdapterDown {
   const void* a;
   const float* scale;                // [n] or NULL: ones
   const int32_t* index;              // [M] or NULL: adapter 0
-  void* t;
+  float* t;
   int ldt;
 };
 hipError_t launch_adapter_down(bool is_bf16, const AdapterDown& p, hipStream_t st);
@@ -167,7 +167,7 @@ struct AdapterUp {
   const int32_t* index;
   int n, rank, stride;
   const void* p;
-  const void* t;
+  const float* t;
   int ldt;
 };
 struct LinearEpi {
@@ -206,7 +206,8 @@ struct AdapterPrepare {
 hipError_t launch_adapter_prepare(bool is_bf16, AdapterPrepare p, hipStream_t st);
 // dA, dB (either may be NULL)
 struct AdapterSide {
-  const void *z, *v;                 // [M, cols], [M, ldv]
+  const void* z;                     // [M, cols]
+  const float* v;                    // [M, ldv]
   int ldz, ldv, cols;
   float* partial;                    // [slices][ranks][ldp]
   int ldp;                           // cols in whole pieces of eight

@@ -467,7 +467,7 @@ def adapter_linear(x: torch.Tensor, w: torch.Tensor, a: torch.Tensor, b: torch.T
     index[row]`` (int32 ``[M]``; outside ``0 .. n-1``: no adapter; None: adapter 0 for all) for
     ``x [M, K]``, ``w [N, K]``, ``a [n, rank, K]``, ``b [n, N, rank]`` of one dtype (bf16 or
     fp32) and ``scale`` fp32 ``[n]`` (None: ones), with the epilogues of :func:`linear_i8`.
-    With ``save_t`` also ``t = s_i x a_i^T`` (``[M, rank rounded up to 32]``) that
+    With ``save_t`` also ``t = s_i x a_i^T`` (fp32 ``[M, rank rounded up to 32]``) that
     :func:`adapter_linear_backward` takes."""
     dev = _device(x, w, a, b, bias, index, scale, resid, resid_copy, gate)
     if _elsewhere(dev, stream):
@@ -490,7 +490,7 @@ def adapter_linear(x: torch.Tensor, w: torch.Tensor, a: torch.Tensor, b: torch.T
         out = x.new_empty((M, N))
     _need((gate is not None) == (epilogue == "resid_gated"), "gate goes with resid_gated", 1)
     ldt = (r + 31) // 32 * 32
-    t = x.new_empty((M, ldt))
+    t = x.new_empty((M, ldt), dtype=torch.float32)
     _check(load().t2i_op_adapter_linear(dt, epi, M, N, K, x.data_ptr(), ldx, w.data_ptr(), ldw, _p(bias), n, r,
                                         a.data_ptr(), b.data_ptr(), _p(scale), _p(index), t.data_ptr(), ldt, _p(out),
                                         N, _p(resid), ldr, _p(resid_copy), _p(gate), _stream(dev)))
@@ -514,7 +514,7 @@ def adapter_linear_backward(dy: torch.Tensor, x: torch.Tensor, w: torch.Tensor, 
                                            need_dab=need_dab)
     dt, M, N, K, n, r, ldx, ldw = _adapter_args(x, w, a, b, index, scale)
     lddy = _rows(dy, M, N, x.dtype, "dy")
-    ldt = _rows(t, M, (r + 31) // 32 * 32, x.dtype, "t")
+    ldt = _rows(t, M, (r + 31) // 32 * 32, torch.float32, "t")
     lib = load()
     dx = x.new_empty((M, K)) if need_dx else None
     da, db = (a.new_empty(a.shape), b.new_empty(b.shape)) if need_dab else (None, None)

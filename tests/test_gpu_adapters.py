@@ -3,8 +3,8 @@ definitions (``oracle/blocks.py``).
 
 Bounds count roundings.  U is half a step of the operands' type relative to the value, E =
 2^-24; a sum of n products in fp32 is off by at most n E times the sum of the products'
-sizes.  t (and the gradients' u) is such a sum, scaled and rounded to the operands' type;
-what it is off by goes through the second product."""
+sizes.  t (and the gradients' u) is such a sum, scaled, in fp32; the products take bf16
+operands' as two bf16 values, 2^-16 of it short.  What it is off by goes through them."""
 import ctypes as C
 
 import numpy as np
@@ -57,11 +57,12 @@ def forward_bounds(h, bias, dtype):
     y, t = blocks.adapter_linear(**h, bias=bias)
     mag = {**h, **{k: A(h[k]) for k in "xwab"}}
     _, tm = blocks.adapter_linear(**mag)
-    t_err = (h["x"].shape[1] + 2) * E * tm + U[dtype] * A(t)
+    t_err = (h["x"].shape[1] + 2) * E * tm
+    left = t_err + (2.0 ** -16 * A(t) if dtype == BF16 else 0)   # as the products take it
     K, rank = h["x"].shape[1], h["a"].shape[1]
     err = (K + 2) * E * (A(h["x"]) @ A(h["w"]).T) + 4 * E * A(y) + (0 if bias is None else 2 * E * A(bias))
     for i, rows in enumerate(blocks.adapter_rows(h["index"], h["a"].shape[0], y.shape[0])):
-        err[rows] += (t_err[rows] + (rank + 2) * E * A(t[rows])) @ A(h["b"][i]).T
+        err[rows] += (left[rows] + (2 * rank + 2) * E * A(t[rows])) @ A(h["b"][i]).T
     return y, err, t, t_err
 
 
@@ -235,7 +236,7 @@ def test_rows_without_an_adapter_are_the_layers(dtype):
     assert A(r).max() < 0.05
     lib, st = t2i.load(), C.c_void_p(torch.cuda.current_stream().cuda_stream)
     for rows in (M, 40):
-        t = torch.full((rows + 1, 72), float("nan"), dtype=dtype, device=DEV)
+        t = torch.full((rows + 1, 72), float("nan"), device=DEV)
         out = torch.full((rows + 1, N + 5), 7.0, dtype=dtype, device=DEV)
         _lib.check(lib.t2i_op_adapter_linear(
             int(dtype == BF16), 0, rows, N, K, o["x"].data_ptr(), K, o["w"].data_ptr(), K, None, 3, 9, o["a"].data_ptr(),
@@ -255,14 +256,15 @@ def backward_bounds(h, dy, dtype):
     big = blocks.adapter_linear_grads(A(dy), **mag)
     _, _, t, t_err = forward_bounds(h, None, dtype)
     M, N, K, rank = dy.shape[0], dy.shape[1], h["x"].shape[1], h["a"].shape[1]
-    u_err = (N + 2) * E * big["u"] + U[dtype] * A(ref["u"])
+    short = 2.0 ** -16 if dtype == BF16 else 0
+    u_err, t_err = (N + 2) * E * big["u"] + short * A(ref["u"]), t_err + short * A(t)
     err = dict(dx=(N + 2) * E * (A(dy) @ A(h["w"])) + 4 * E * A(ref["dx"]), da=np.zeros_like(ref["da"]),
                db=np.zeros_like(ref["db"]))
     for i, rows in enumerate(blocks.adapter_rows(h["index"], h["a"].shape[0], M)):
         u = A(ref["u"][rows])
-        err["dx"][rows] += (u_err[rows] + (rank + 2) * E * u) @ A(h["a"][i])
-        err["da"][i] = (u_err[rows] + (len(rows) + 2) * E * u).T @ A(h["x"][rows])
-        err["db"][i] = A(dy[rows]).T @ (t_err[rows] + (len(rows) + 2) * E * A(t[rows]))
+        err["dx"][rows] += (u_err[rows] + (2 * rank + 2) * E * u) @ A(h["a"][i])
+        err["da"][i] = (u_err[rows] + (2 * len(rows) + 2) * E * u).T @ A(h["x"][rows])
+        err["db"][i] = A(dy[rows]).T @ (t_err[rows] + (2 * len(rows) + 2) * E * A(t[rows]))
     return ref, err
 
 
@@ -370,7 +372,7 @@ def test_adapters_on_another_stream_and_in_graphs():
 def test_python_adapter_calls_refuse(bad):
     o, kw = operands(8, 16, 24, 2, 4, "scattered", BF16)
     dy = rnd(3, (8, 16), 1.0, BF16)[0]
-    t = torch.zeros((8, 32), dtype=BF16, device=DEV)
+    t = torch.zeros((8, 32), device=DEV)
     both = True
     if bad == "a":
         o["a"] = o["a"][:, :, :16]
@@ -392,7 +394,7 @@ def test_python_adapter_calls_refuse(bad):
         o["a"] = o["a"].cpu()
     elif bad == "rank":
         o["a"], o["b"] = torch.zeros((2, 129, 24), dtype=BF16, device=DEV), torch.zeros((2, 16, 129), dtype=BF16, device=DEV)
-        t = torch.zeros((8, 160), dtype=BF16, device=DEV)
+        t = torch.zeros((8, 160), device=DEV)
     else:
         both = False
     if both:
@@ -401,7 +403,7 @@ def test_python_adapter_calls_refuse(bad):
         with pytest.raises(t2i.T2IError):
             t2i.adapter_linear_backward(dy, **o, t=t, **kw)
     elif bad == "t":
-        for wrong in (t[:, :4], t.float(), t[:7]):
+        for wrong in (t[:, :4], t.to(BF16), t[:7]):
             with pytest.raises(t2i.T2IError):
                 t2i.adapter_linear_backward(dy, **o, t=wrong, **kw)
     else:
