@@ -585,8 +585,8 @@ hipError_t launch_adapter_dx(bool is_bf16, const void* dy, int lddy, const void*
 }
 
 // ---------------------------------------------------------------------------
-// What the gradients need first, in one launch: the rows of every adapter, and the
-// adapters' matrices turned.
+// What the gradients need first, in one launch: the rows of every adapter, the adapters'
+// matrices turned, and, of few rows, u = s dy B straight from B.
 //
 // Adapter i's rows, in ascending order, are order[start .. start + count), (start, count) =
 // span[i].  Cut at every multiple of `per` they are the slices of the gradients' sums;
@@ -657,6 +657,48 @@ __device__ __forceinline__ void turn_rows(const AdapterTurn& d, long x) {
   store_piece((T*)d.out + ((size_t)ad * d.C + c) * d.stride + r0, d.stride - r0, v);
 }
 
+// u of few rows: four waves take one row and four ranks, a lane every 256th column
+template <typename T>
+__device__ __forceinline__ void up_rows(const AdapterPrepare& p, int block) {
+  __shared__ float red[16][4];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = adapter_cols(p.rank) / 4;
+  const long item = block * 4L + (wave >> 2);
+  const int m = (int)(item / per), j0 = (int)(item % per) * 4;
+  const int ad = m < p.M ? adapter_of(p.index, p.n, m) : -1;
+  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  if (ad >= 0 && j0 < p.rank) {
+    const T* const dy = (const T*)p.dy + (size_t)m * p.lddy;
+    const T* const b = (const T*)p.b + (size_t)ad * p.N * p.rank + j0;
+    typedef T any4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
+    const bool four = j0 + 4 <= p.rank;
+#pragma unroll 4
+    for (int c = (wave & 3) * 64 + lane; c < p.N; c += 256) {
+      const float d = to_f32(dy[c]);
+      const T* const q = b + (size_t)c * p.rank;
+      if (four) {
+        const any4 v = *(const any4*)q;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) s[j] = fmaf(d, (float)v[j], s[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (j0 + j < p.rank) s[j] = fmaf(d, to_f32(q[j]), s[j]);
+      }
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) s[j] += __shfl_xor(s[j], o, kWave);
+    if (lane == 0) red[wave][j] = s[j];
+  }
+  __syncthreads();
+  if ((wave & 3) != 0 || lane >= 4 || m >= p.M) return;
+  const float v = (red[wave][lane] + red[wave + 1][lane]) + (red[wave + 2][lane] + red[wave + 3][lane]);
+  const float scale = ad >= 0 ? (p.scale ? p.scale[ad] : 1.f) : 0.f;
+  p.u[(size_t)m * adapter_cols(p.rank) + j0 + lane] = ad >= 0 && j0 + lane < p.rank ? v * scale : 0.f;
+}
+
 template <typename T>
 __global__ __launch_bounds__(1024) void adapter_prepare_kernel(AdapterPrepare p) {
   int block = blockIdx.x;
@@ -665,6 +707,11 @@ __global__ __launch_bounds__(1024) void adapter_prepare_kernel(AdapterPrepare p)
     return;
   }
   block -= p.groups;
+  if (block < p.rows) {
+    up_rows<T>(p, block);
+    return;
+  }
+  block -= p.rows;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     const AdapterTurn& d = p.turn[i];
@@ -677,7 +724,8 @@ __global__ __launch_bounds__(1024) void adapter_prepare_kernel(AdapterPrepare p)
   }
 }
 hipError_t launch_adapter_prepare(bool is_bf16, AdapterPrepare p, hipStream_t st) {
-  long blocks = p.groups;
+  p.rows = p.dy ? (int)(((long)p.M * (adapter_cols(p.rank) / 4) + 3) / 4) : 0;
+  long blocks = p.groups + p.rows;
   for (AdapterTurn& d : p.turn) {
     d.blocks = d.in ? (int)(((long)((d.stride + 7) / 8) * d.C * p.n + 1023) / 1024) : 0;
     blocks += d.blocks;
@@ -688,9 +736,15 @@ hipError_t launch_adapter_prepare(bool is_bf16, AdapterPrepare p, hipStream_t st
   return hipGetLastError();
 }
 
-// rows of a slice: as many as leave two workgroups for every CU, at least a step of four
-// waves and at most 1024
+// u of up to so many products in the first launch: no second one, and B need not be
+// turned (fp32 333 x 1155, rank 5 @@)
+bool adapter_few_rows(int M, int N, int rank) { return M <= 1024 && (int64_t)M * N * rank <= 1 << 23; }
+
+// rows of a slice: all of up to 512, whose sums are then done without a second launch;
+// else as many as leave two workgroups for every CU, at least a step of four waves and at
+// most 1024
 int adapter_slice_rows(bool is_bf16, int M, int N, int K, int rank) {
+  if (M <= 512) return 1024;
   const int cols = is_bf16 ? 128 : 64;
   const long wide = (long)((K + cols - 1) / cols + (N + cols - 1) / cols) * ((rank + 31) / 32);
   int per = 1024;
@@ -717,9 +771,10 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterOuter p) {
     const int4 sl = p.slices[blockIdx.y];
     first = sl.y, rows = sl.z;
   } else {
-    first = blockIdx.y * p.per, rows = min(p.per, p.M - first);
+    first = blockIdx.y * p.per, rows = max(0, min(p.per, p.M - first));
   }
-  if (rows <= 0) return;
+  T* const done = (T*)d.grad;   // (one slice to an adapter: the gradient itself)
+  if (rows <= 0 && !done) return;
   const T* const z = (const T*)d.z;
   const float* const v = d.v;
   const bool in = c0 < C, part = c0 + L > C;
@@ -784,6 +839,31 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterOuter p) {
     }
   }
   if (wave > 0 || !in) return;
+  if (done) {
+    const int ad = p.slices ? p.slices[blockIdx.y].x : blockIdx.y, left = C - c0;
+#pragma unroll
+    for (int jt = 0; jt < RT; ++jt) {
+      const int j = j0 + jt * 16 + g * 4, ranks = p.rank - j;
+      if (ranks <= 0) continue;
+      if (second) {   // dB [N][rank]: four ranks of a column
+#pragma unroll
+        for (int q = 0; q < L; ++q) {
+          const float w[4] = {acc[q][jt][0], acc[q][jt][1], acc[q][jt][2], acc[q][jt][3]};
+          if (q < left) store4(done + ((size_t)ad * C + c0 + q) * p.rank + j, ranks, w);
+        }
+      } else {        // dA [rank][K]: neighbouring columns of a rank
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          if (r < ranks)
+#pragma unroll
+            for (int q = 0; q < L; q += 4) {
+              const float w[4] = {acc[q][jt][r], acc[q + 1][jt][r], acc[q + 2][jt][r], acc[q + 3][jt][r]};
+              if (q < left) store4(done + ((size_t)ad * p.rank + j + r) * C + c0 + q, left - q, w);
+            }
+      }
+    }
+    return;
+  }
   float* const out = d.partial + (size_t)blockIdx.y * p.ranks * d.ldp + c0;
 #pragma unroll
   for (int jt = 0; jt < RT; ++jt)
@@ -835,6 +915,12 @@ __global__ __launch_bounds__(256) void adapter_sum_kernel(AdapterOuter p, T* dA,
 template <typename T>
 static void outer_any(AdapterOuter p, int n, int slices, T* dA, T* dB, hipStream_t st) {
   constexpr int COLS = 16 * kLaneK<T>;
+  // up to one slice of rows: slice i is adapter i's, empty ones too
+  const bool direct = p.M < p.per;
+  if (direct) {
+    p.side[0].grad = dA, p.side[1].grad = dB;
+    slices = n;
+  }
   const int blocks1 = dB ? (p.side[1].cols + COLS - 1) / COLS : 0;
   p.blocks0 = dA ? (p.side[0].cols + COLS - 1) / COLS : 0;
   if (p.rank <= 16)
@@ -844,6 +930,7 @@ static void outer_any(AdapterOuter p, int n, int slices, T* dA, T* dB, hipStream
     hipLaunchKernelGGL((adapter_outer_kernel<T, 2>),
                        dim3((unsigned)(p.blocks0 + blocks1), (unsigned)slices, (unsigned)((p.rank + 31) / 32)), dim3(256), 0,
                        st, p);
+  if (direct) return;
   const int a = dA ? (int)(((long)((p.side[0].cols + 3) / 4) * p.rank + 255) / 256) : 0;
   const int b = dB ? (int)(((long)p.side[1].cols * ((p.rank + 3) / 4) + 255) / 256) : 0;
   hipLaunchKernelGGL((adapter_sum_kernel<T>), dim3((unsigned)(a + b), (unsigned)n), dim3(256), 0, st, p, dA, dB, a);

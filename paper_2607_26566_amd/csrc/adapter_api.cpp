@@ -163,10 +163,21 @@ t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, i
   pre.order = (int32_t*)(at + r.order);
   pre.span = (int2*)(at + r.span);
   pre.slices = (int4*)(at + r.table);
-  if (dx || da) pre.turn[0] = AdapterTurn{b, at + r.bt, N, rank, N, 0};
+  const bool need_u = dx || da, few = adapter_few_rows(M, N, rank);
+  pre.rank = rank;
+  if (need_u && few) {
+    pre.dy = dy;
+    pre.lddy = lddy;
+    pre.b = b;
+    pre.N = N;
+    pre.scale = scale;
+    pre.u = (float*)(at + r.u);
+  } else if (need_u) {
+    pre.turn[0] = AdapterTurn{b, at + r.bt, N, rank, N, 0};
+  }
   if (dx) pre.turn[1] = AdapterTurn{a, at + r.at, rank, K, whole8(rank), 0};
   hipError_t err = launch_adapter_prepare(bf, pre, st);
-  if (err == hipSuccess && (dx || da)) {   // u = s dy B
+  if (err == hipSuccess && need_u && !few) {   // u = s dy B
     AdapterDown d;
     std::memset(&d, 0, sizeof(d));
     d.M = M;
@@ -190,8 +201,8 @@ t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, i
     const int slices = index ? r.slices : (M + r.per - 1) / r.per;
     AdapterOuter o;
     std::memset(&o, 0, sizeof(o));
-    o.side[0] = AdapterSide{x, (const float*)(at + r.u), ldx, ldu, K, (float*)(at + r.part_a), whole8(K)};
-    o.side[1] = AdapterSide{dy, t, lddy, ldt, N, (float*)(at + r.part_b), whole8(N)};
+    o.side[0] = AdapterSide{x, (const float*)(at + r.u), ldx, ldu, K, (float*)(at + r.part_a), whole8(K), nullptr};
+    o.side[1] = AdapterSide{dy, t, lddy, ldt, N, (float*)(at + r.part_b), whole8(N), nullptr};
     o.M = M;
     o.per = r.per;
     o.rank = rank;

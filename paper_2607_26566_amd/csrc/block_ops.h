@@ -187,8 +187,9 @@ size_t adapter_dx_floats(bool is_bf16, int M, int N, int K);
 hipError_t launch_adapter_dx(bool is_bf16, const void* dy, int lddy, const void* w, int ldw, int M, int N, int K,
                              const AdapterUp& up, void* dx, int ldx, float* partial, hipStream_t st);
 // the gradients' first launch: the rows of every adapter, slices of at most `per` of them
-// (groups = n, or 0 without an index), and matrices turned: out [n][C][stride] = in
-// [n][R][C], zeros behind R (in NULL: none)
+// (groups = n, or 0 without an index), matrices turned: out [n][C][stride] = in
+// [n][R][C], zeros behind R (in NULL: none), and u [M][adapter_cols(rank)] = s dy b (dy
+// NULL: not)
 int adapter_slice_rows(bool is_bf16, int M, int N, int K, int rank);
 struct AdapterTurn {
   const void* in;
@@ -202,7 +203,12 @@ struct AdapterPrepare {
   int2* span;
   int4* slices;
   AdapterTurn turn[2];
+  const void *dy, *b;
+  const float* scale;
+  float* u;
+  int lddy, N, rank, rows;
 };
+bool adapter_few_rows(int M, int N, int rank);
 hipError_t launch_adapter_prepare(bool is_bf16, AdapterPrepare p, hipStream_t st);
 // dA, dB (either may be NULL)
 struct AdapterSide {
@@ -211,6 +217,7 @@ struct AdapterSide {
   int ldz, ldv, cols;
   float* partial;                    // [slices][ranks][ldp]
   int ldp;                           // cols in whole pieces of eight
+  void* grad;                        // set by the launch: dA, dB if they need no partial sums
 };
 struct AdapterOuter {
   AdapterSide side[2];               // dA: (x, u), dB: (dy, t)
