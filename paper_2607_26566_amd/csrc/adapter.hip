@@ -147,32 +147,132 @@ __global__ __launch_bounds__(256) void adapter_down_rows_kernel(AdapterDown p) {
 // Many rows: a tile of rows and all ranks (up to 64), whose groups of waves share k as
 // in the products of few tiles; both operands come through LDS in whole lines (fragments
 // straight from memory, 16 rows to an instruction, 19 us for 4096 rows of 4096 and 16
-// ranks).  Rows of several adapters: the tile's product once for each of them.
+// ranks).
+//
+// A tile whose rows take several adapters does its product once for each of them.  Tiles of
+// more than three in a window of rows share those rows anew instead, in the order of their
+// adapters: each of them works out the same order from the window's index, which takes it
+// about 5 us, and takes the part that is its turn (512 rows of 4096 with one of 32 adapters
+// each, rank 16: 59 -> 25 us).
+constexpr int kWindow = 4096, kSorted = 512, kOwn = 3;   // rows; adapters for that; adapters a tile takes as it is
+
+template <int BM, int THREADS>
+struct SharedRows {
+  static constexpr int TILES = kWindow / BM, PER = kWindow / THREADS, NW = THREADS / 64;
+  int16_t* ids;      // [kWindow] in LDS, as the others
+  int* hist;         // [kSorted]
+  uint8_t* several;  // [TILES] whether a tile's rows take more than kOwn adapters
+  int* scratch;      // [NW + 4]
+  int* row;          // [BM] the rows of this tile, counted from the window's first, -1: none
+  int* adapter;      // [BM]
+
+  // sum of v over the threads before this one; all of them in `sum`
+  __device__ __forceinline__ int before(int v, int& sum) const {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    int x = v;
+#pragma unroll
+    for (int o = 1; o < 64; o *= 2) {
+      const int y = __shfl_up(x, o, kWave);
+      if (lane >= o) x += y;
+    }
+    __syncthreads();
+    if (lane == 63) scratch[wave] = x;
+    __syncthreads();
+    int base = 0;
+    sum = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      base += w < wave ? scratch[w] : 0;
+      sum += scratch[w];
+    }
+    return base + x - v;
+  }
+  __device__ __forceinline__ void take(const AdapterDown& p, int first, int tile) const {
+    const int t = threadIdx.x, rows = min(kWindow, p.M - first);
+    for (int r = t; r < kWindow; r += THREADS) ids[r] = (int16_t)(r < rows ? adapter_of(p.index, p.n, first + r) : -1);
+    for (int i = t; i < p.n; i += THREADS) hist[i] = 0;
+    if (t < BM) row[t] = adapter[t] = -1;
+    __syncthreads();
+    for (int i = t; i < TILES; i += THREADS) {
+      int seen[kOwn] = {-1, -1, -1}, count = 0;   // the first ones
+      for (int r = 0; r < BM; ++r) {
+        const int a = ids[i * BM + r];
+        if (a < 0 || a == seen[0] || a == seen[1] || a == seen[2]) continue;
+        if (count < kOwn) seen[count == 0 ? 0 : count == 1 ? 1 : 2] = a;
+        ++count;
+      }
+      several[i] = count > kOwn;
+    }
+    __syncthreads();
+    // this thread's rows, next to each other; those of no interest become -1
+    int mine[PER];
+#pragma unroll
+    for (int i = 0; i < PER; ++i) {
+      const int r = t * PER + i;
+      mine[i] = several[r / BM] ? ids[r] : -1;
+      if (mine[i] >= 0) atomicAdd(&hist[mine[i]], 1);   // (counts: any order)
+    }
+    int turn = 0;
+    for (int i = t & 63; i < tile; i += 64) turn += several[i];
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) turn += __shfl_xor(turn, o, kWave);
+    __syncthreads();
+    // the adapter of the first row whose turn it is, and how many of its rows come before;
+    // then row after row of it and the next ones
+    int skip = turn * BM, got = 0;
+    for (int a = 0; a < p.n && got < BM; ++a) {
+      const int count = hist[a];
+      if (count <= skip) {
+        skip -= count;
+        continue;
+      }
+      int here = 0, sum;
+#pragma unroll
+      for (int i = 0; i < PER; ++i) here += mine[i] == a;
+      int at = before(here, sum) - skip + got;
+#pragma unroll
+      for (int i = 0; i < PER; ++i)
+        if (mine[i] == a) {
+          if (at >= got && at < BM) row[at] = t * PER + i, adapter[at] = a;
+          ++at;
+        }
+      got = min(BM, got + count - skip);
+      skip = 0;
+    }
+    __syncthreads();
+  }
+};
+
 template <class D, typename T, bool U>
 __global__ __launch_bounds__(D::THREADS, 1) void adapter_down_kernel(AdapterDown p) {
   using P = TileProduct<D, elem_of<T>(), false, false, false, false, U>;
-  __shared__ __attribute__((aligned(1024))) char smem[D::KG * D::RING];
+  using S = SharedRows<D::BM, D::THREADS>;
+  constexpr int RING = D::KG * D::RING;
+  static_assert(kWindow * 2 + kSorted * 4 + S::TILES + (S::NW + 4) * 4 <= RING, "room for a window's index");
+  __shared__ __attribute__((aligned(1024))) char smem[RING];
+  __shared__ int rows[2][D::BM];
   constexpr int EB = sizeof(T), TM = D::TM, TN = D::TN;
   const int lane = threadIdx.x & 63, fr = lane & 15, g = lane >> 4;
-  const int m0 = blockIdx.x * D::BM, j0 = blockIdx.y * D::BN, cols = adapter_cols(p.rank);
+  int m0 = blockIdx.x * D::BM;
+  const int j0 = blockIdx.y * D::BN, cols = adapter_cols(p.rank);
   const TileOperand a{(const char*)p.x, nullptr, (uint32_t)(EB * p.ldx), p.M, 0};
   TileShape s;
   s.tiles_m = s.tiles_n = s.group_m = 1;
   s.kbytes = EB * p.K;
   s.steps = (s.kbytes + 127) / 128;
   s.half = s.first = 0;
-  int ad[TM];
+  int ad[TM], row[TM];   // adapter (-2: no row), row from m0
 #pragma unroll
   for (int i = 0; i < TM; ++i) {
-    const int m = m0 + i * 16 + fr;
-    ad[i] = m < p.M ? adapter_of(p.index, p.n, m) : -2;
+    row[i] = i * 16 + fr;
+    ad[i] = m0 + row[i] < p.M ? adapter_of(p.index, p.n, m0 + row[i]) : -2;
   }
   auto store = [&](int i, int j, const f32x4& v) {
-    const int m = m0 + i * 16 + fr, c = j0 + j * 16 + g * 4;
+    const int c = j0 + j * 16 + g * 4;
     f32x4 o;
 #pragma unroll
     for (int r = 0; r < 4; ++r) o[r] = c + r < p.rank ? v[r] : 0.f;
-    if (c < cols) *(f32x4*)(p.t + (size_t)m * p.ldt + c) = o;
+    if (c < cols) *(f32x4*)(p.t + (size_t)(m0 + row[i]) * p.ldt + c) = o;
   };
   const bool behind = j0 >= p.rank;   // the zeros behind the ranks
   if (threadIdx.x < 64) {
@@ -183,20 +283,47 @@ __global__ __launch_bounds__(D::THREADS, 1) void adapter_down_kernel(AdapterDown
         for (int j = 0; j < TN; ++j) store(i, j, f32x4{0.f, 0.f, 0.f, 0.f});
   }
   if (behind) return;
-  int now = -1;
-  for (;;) {   // the adapters in ascending order, the same for every wave
+  // the least adapter above `now`
+  auto above = [&](int now) {
     int next = 0x7fffffff;
 #pragma unroll
     for (int i = 0; i < TM; ++i) next = min(next, ad[i] > now ? ad[i] : 0x7fffffff);
 #pragma unroll
     for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, kWave));
-    next = __builtin_amdgcn_readfirstlane(next);
+    return __builtin_amdgcn_readfirstlane(next);
+  };
+  int next = above(-1);
+  int last = next;
+#pragma unroll
+  for (int i = 0; i < kOwn; ++i) last = last == 0x7fffffff ? last : above(last);
+  const bool several = last != 0x7fffffff;   // more than kOwn
+  if (several && p.n <= kSorted && (int64_t)kWindow * p.ldx * EB < 0x7fffffff) {
+    const int first = m0 / kWindow * kWindow, tile = (m0 - first) / D::BM;
+    const S sh{(int16_t*)smem, (int*)(smem + kWindow * 2), (uint8_t*)(smem + kWindow * 2 + kSorted * 4),
+               (int*)(smem + kWindow * 2 + kSorted * 4 + S::TILES), rows[0], rows[1]};
+    sh.take(p, first, tile);
+    m0 = first;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) {
+      row[i] = max(rows[0][i * 16 + fr], 0);
+      ad[i] = rows[0][i * 16 + fr] < 0 ? -2 : rows[1][i * 16 + fr];
+    }
+    next = above(-1);
+  } else {
+    if (threadIdx.x < D::BM) rows[0][threadIdx.x] = min((int)threadIdx.x, p.M - 1 - m0);
+    __syncthreads();
+  }
+  int now = -1;
+  for (;;) {   // the adapters in ascending order, the same for every wave
     if (next == 0x7fffffff) return;
     if (now >= 0) tile_barrier();   // (the sums of the adapter before are read)
     now = next;
+    next = above(now);
     const TileOperand b{(const char*)p.a + (size_t)now * p.rank * p.K * EB, nullptr, (uint32_t)(EB * p.K), p.rank, 0};
     typename P::Acc acc[TM][TN];
-    if (!P::run_groups(smem, a, b, s, m0, j0, acc)) continue;
+    if (!P::run_groups(smem, a, b, s, m0, j0, acc, FromZero(),
+                       [&](int r, int, int) { return max(rows[0][r], 0); }))
+      continue;
     const float scale = p.scale ? p.scale[now] : 1.f;
 #pragma unroll
     for (int i = 0; i < TM; ++i) {
@@ -207,8 +334,9 @@ __global__ __launch_bounds__(D::THREADS, 1) void adapter_down_kernel(AdapterDown
   }
 }
 
-// rows up to which the first kernel takes them
-constexpr int kDownRows = 64;
+// rows up to which the first kernel takes them (with a product of 8 columns behind it: 256
+// of 4096, rank 16, 32 adapters 16 us, tiles 15.5; 512 18 and 13)
+constexpr int kDownRows = 256;
 template <class D, typename T, bool U>
 static void down_launch(const AdapterDown& p, hipStream_t st) {
   hipLaunchKernelGGL((adapter_down_kernel<D, T, U>),
@@ -298,6 +426,16 @@ struct Adapters {
     return load_k<T>(p, (uint32_t)(min(P::col_of(j, x), N - 1 - nw) * u.stride) * (uint32_t)sizeof(T), k, u.rank,
                      u.rank % L == 0);
   }
+  // the least adapter of the wave's rows above `now`, or kNone
+  static constexpr int kNone = 0x7fffffff;
+  __device__ __forceinline__ int above(int now) const {
+    int next = kNone;
+#pragma unroll
+    for (int i = 0; i < TM; ++i) next = min(next, id[i] > now ? id[i] : kNone);
+#pragma unroll
+    for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, kWave));
+    return __builtin_amdgcn_readfirstlane(next);
+  }
   __device__ __forceinline__ bool one_adapter() const {
     const int first = __builtin_amdgcn_readfirstlane(id[0]);
     bool same = true;
@@ -329,28 +467,20 @@ struct Adapters {
         Exact<T> tv[TM];
 #pragma unroll
         for (int i = 0; i < TM; ++i) tv[i] = exact_t(i, k0 + g * L);
-        int now = -1;
+        // (one after the other: two at a time spill the accumulators of 128 x 128)
 #pragma unroll 1
-        for (;;) {   // the adapters in ascending order
-          int next = 0x7fffffff;
-#pragma unroll
-          for (int i = 0; i < TM; ++i) next = min(next, id[i] > now ? id[i] : 0x7fffffff);
-#pragma unroll
-          for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, kWave));
-          now = __builtin_amdgcn_readfirstlane(next);
-          if (now == 0x7fffffff) break;
+        for (int now = above(-1); now != kNone; now = above(now)) {
           i32x4 pv[TN];
 #pragma unroll
           for (int j = 0; j < TN; ++j) pv[j] = p_at(now, j, fr, k0 + g * L);
 #pragma unroll
-          for (int i = 0; i < TM; ++i) {
+          for (int i = 0; i < TM; ++i)
 #pragma unroll
             for (int j = 0; j < TN; ++j) {
               const f32x4 add = narrow_mfma<T>(pv[j], tv[i], f32x4{0.f, 0.f, 0.f, 0.f});
 #pragma unroll
               for (int r = 0; r < 4; ++r) acc[i][j][r] += id[i] == now ? add[r] : 0.f;
             }
-          }
         }
       }
     } else if (id[0] >= 0) {
@@ -379,34 +509,39 @@ struct Adapters {
       f32x4* const part = (f32x4*)(smem + wave * HALF * TN * 1024) + lane;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
-#pragma unroll 1
+        int mine[HALF];
+#pragma unroll
         for (int i = 0; i < HALF; ++i) {
           const int m = mw + P::row_of(h * HALF + i, fr);
-          const int mine = m < M ? adapter_of(u.index, u.n, m) : -2;
-          uint32_t left = (uint32_t)__ballot(mine >= 0) & 0xffffu;
-          f32x4 sum[TN];
+          mine[i] = m < M ? adapter_of(u.index, u.n, m) : -2;
 #pragma unroll
-          for (int j = 0; j < TN; ++j) sum[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int j = 0; j < TN; ++j) part[(i * TN + j) * 64] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
 #pragma unroll 1
-          while (left) {
-            const int now = __builtin_amdgcn_readlane(mine, __builtin_ctz(left));
-            left &= ~(uint32_t)__ballot(mine == now);
-            f32x4 add[TN];
+        for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
+          Exact<T> tv[HALF];
 #pragma unroll
-            for (int j = 0; j < TN; ++j) add[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+          for (int i = 0; i < HALF; ++i) tv[i] = exact_t(h * HALF + i, k0 + g * L);
 #pragma unroll 1
-            for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
-              const Exact<T> tv = exact_t(h * HALF + i, k0 + g * L);
+          for (int now = -1;;) {
+            int next = kNone;
 #pragma unroll
-              for (int j = 0; j < TN; ++j) add[j] = narrow_mfma<T>(p_at(now, j, fr, k0 + g * L), tv, add[j]);
-            }
+            for (int i = 0; i < HALF; ++i) next = min(next, mine[i] > now ? mine[i] : kNone);
 #pragma unroll
-            for (int j = 0; j < TN; ++j)
+            for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, kWave));
+            now = __builtin_amdgcn_readfirstlane(next);
+            if (now == kNone) break;
+            i32x4 pv[TN];
 #pragma unroll
-              for (int r = 0; r < 4; ++r) sum[j][r] = mine == now ? add[j][r] : sum[j][r];
+            for (int j = 0; j < TN; ++j) pv[j] = p_at(now, j, fr, k0 + g * L);
+#pragma unroll
+            for (int i = 0; i < HALF; ++i)
+#pragma unroll
+              for (int j = 0; j < TN; ++j) {
+                const f32x4 add = narrow_mfma<T>(pv[j], tv[i], f32x4{0.f, 0.f, 0.f, 0.f});
+                if (mine[i] == now) part[(i * TN + j) * 64] += add;
+              }
           }
-#pragma unroll
-          for (int j = 0; j < TN; ++j) part[(i * TN + j) * 64] = sum[j];
         }
 #pragma unroll
         for (int i = 0; i < HALF; ++i)

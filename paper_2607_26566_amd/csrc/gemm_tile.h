@@ -145,6 +145,10 @@ struct TileDims {
 
 enum TileElem { ELEM_BF16, ELEM_I8, ELEM_F32 };
 
+// the row of operand a (a KC one) that a tile's row is: the next ones from the first
+struct NextRows {
+  __device__ __forceinline__ int operator()(int row, int rows, int first) const { return min(row, rows - 1 - first); }
+};
 // what a product's accumulators start from: zeros
 struct FromZero {
   template <class A>
@@ -189,10 +193,12 @@ struct TileProduct {
 
   // the tile product: acc[i][j][r] belongs to the wave's row row_of(i, lane & 15)
   // and column col_of(j, 4 (lane >> 4) + r).  `from` may add to the accumulators before the
-  // first step, while the ring's first loads are under way.
-  template <class F = FromZero>
+  // first step, while the ring's first loads are under way; `pick` says which rows of a the
+  // tile's are, counted from m0.
+  template <class F = FromZero, class R = NextRows>
   static __device__ __forceinline__ void run(char* smem, const TileOperand& a, const TileOperand& b, const TileShape& s,
-                                             int m0, int n0, Acc (&acc)[TM][TN], const F& from = F()) {
+                                             int m0, int n0, Acc (&acc)[TM][TN], const F& from = F(),
+                                             const R& pick = R()) {
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane((tid >> 6) % D::NW);
     const int wm = wave / D::WGN, wn = wave % D::WGN, fr = lane & 15, g = lane >> 4;
@@ -218,7 +224,7 @@ struct TileProduct {
       // rows from the tile's first, not behind the last (DUAL: within the half)
       const int r0 = is_a ? m0 : n0, lr = kc_row(at);
       const int rr = !is_a && DUAL && lr >= BN / 2 ? lr - BN / 2 : lr;
-      return (uint32_t)min(rr, o.rows - 1 - r0) * o.ld + kc_byte(at);
+      return (uint32_t)(is_a ? pick(rr, o.rows, r0) : min(rr, o.rows - 1 - r0)) * o.ld + kc_byte(at);
     };
     uint32_t src[LOADS];
 #pragma unroll
@@ -419,11 +425,12 @@ struct TileProduct {
   // the same by KG groups of waves; the sum, in ascending group order, is the first
   // group's, whose accumulators `from` adds to.  Returns whether this wave is of that group
   // (the others have no outputs).
-  template <class F = FromZero>
+  template <class F = FromZero, class R = NextRows>
   static __device__ __forceinline__ bool run_groups(char* smem, const TileOperand& a, const TileOperand& b, TileShape s,
-                                                    int m0, int n0, Acc (&acc)[TM][TN], const F& from = F()) {
+                                                    int m0, int n0, Acc (&acc)[TM][TN], const F& from = F(),
+                                                    const R& pick = R()) {
     if constexpr (D::KG == 1) {
-      run(smem, a, b, s, m0, n0, acc, from);
+      run(smem, a, b, s, m0, n0, acc, from, pick);
       return true;
     } else {
       const int kg = __builtin_amdgcn_readfirstlane((int)threadIdx.x / (D::NW * 64)), t = threadIdx.x % (D::NW * 64);
@@ -432,7 +439,7 @@ struct TileProduct {
       s.steps = (kg + 1) * total / D::KG - s.first;
       run(smem + kg * D::RING, a, b, s, m0, n0, acc, [&](Acc (&c)[TM][TN]) {
         if (kg == 0) from(c);
-      });
+      }, pick);
       // (every group meets as often: slices differ by a step)
       for (int x = s.steps; x < per; ++x) tile_barrier();
       tile_barrier();
