@@ -114,6 +114,44 @@ def test_narrow_products_of_more_tiles_than_cus(K, rank, order, dtype):
         within(v, ref[name], U[dtype] * (A(ref[name]) + bounds[name]) + bounds[name], name)
 
 
+def check_all(o, kw, M, N, dtype, seed):
+    h = host(o, kw)
+    y, err, t, t_err = forward_bounds(h, None, dtype)
+    out, got = t2i.adapter_linear(**o, **kw, save_t=True)
+    within(got[:, :t.shape[1]], t, t_err, "t")
+    within(out, y, U[dtype] * (A(y) + err) + err, "y")
+    dy, hdy = rnd(seed, (M, N), 1.0, dtype)
+    ref, bounds = backward_bounds(h, hdy, dtype)
+    for v, name in zip(t2i.adapter_linear_backward(dy, **o, t=got, **kw), ("dx", "da", "db")):
+        within(v, ref[name], U[dtype] * (A(ref[name]) + bounds[name]) + bounds[name], name)
+
+
+@pytest.mark.parametrize("M,n", [(300, 1), (300, 2), (300, 4), (300, 300), (700, 512), (700, 600), (4100, 30), (8200, 3)])
+@DTYPES
+def test_rows_of_many_adapters(M, n, dtype):
+    """Rows shared anew between tiles (more than three adapters to a tile, up to 512 in all), in one
+    window and in two, and the other ways."""
+    N, K = 16, 520
+    o, kw = operands(M, N, K, n, 8, "scattered", dtype, 25)
+    check_all(o, kw, M, N, dtype, 26)
+    # single tiles of several adapters among tiles of one
+    kw["index"] = torch.arange(M, device=DEV, dtype=torch.int32) // 48 % n
+    kw["index"][33:61] = torch.arange(28, device=DEV, dtype=torch.int32) % n
+    kw["index"][M - 9:] = torch.arange(9, device=DEV, dtype=torch.int32) % n
+    check_all(o, kw, M, N, dtype, 27)
+
+
+def test_rows_of_many_adapters_far_apart():
+    """Rows of x that a window's 32-bit offsets do not reach."""
+    M, N, K, ld = 300, 64, 72, 2 ** 18 + 8
+    o, kw = operands(M, N, K, 9, 8, "scattered", BF16, 29)
+    wide = torch.zeros((M - 1) * ld + K, dtype=BF16, device=DEV).as_strided((M, K), (ld, 1))
+    wide.copy_(o["x"])
+    y, t = t2i.adapter_linear(**o, **kw, save_t=True)
+    y2, t2 = t2i.adapter_linear(**{**o, "x": wide}, **kw, save_t=True)
+    assert torch.equal(t, t2) and torch.equal(y, y2)
+
+
 def test_the_largest_tiles_are_reached():
     v = [C.c_int() for _ in range(4)]
     for op, M, N, K in ((4, 4000, 4096, 640), (4, 2100, 4608, 1152), (5, 4000, 640, 4096)):
