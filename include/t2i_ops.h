@@ -349,8 +349,8 @@ t2i_status t2i_op_add_rms_norm_i8(int32_t dtype, int32_t resid_dtype, int32_t ro
  *   NULL where one type serves both;
  *   dw [K] of dtype (or NULL) = sum over rows of dy n, in a fixed order.
  * Sizes and alignment as forward.  dx may lie over dy or (of its type) dh,
- * dresid over dh, same stride, if K <= 16384; no other overlap.  ws (with dw, else
- * it may be NULL) as in t2i_op_gated_linear_backward.
+ * dresid over dh, same stride, if K <= 16384; no other overlap.  ws as in
+ * t2i_op_gated_linear_backward (NULL without dw, or where it takes no bytes).
  */
 size_t t2i_op_add_rms_norm_backward_ws_bytes(int32_t rows, int32_t K);
 t2i_status t2i_op_add_rms_norm_backward(int32_t dtype, int32_t resid_dtype, int32_t rows, int32_t K,

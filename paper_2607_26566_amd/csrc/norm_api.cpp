@@ -107,7 +107,8 @@ t2i_status t2i_op_add_rms_norm_backward(int32_t dtype, int32_t resid_dtype, int3
       (dw && off(ws, 256)))
     return ops_fail(T2I_ERR_INVALID_ARG, "operands need the alignment of their type, ws 256 bytes");
   if (!(eps >= 0.f) || !std::isfinite(eps)) return ops_fail(T2I_ERR_INVALID_ARG, "eps must be finite, >= 0");
-  if (dw && (!ws || ws_bytes < norm_bwd_ws_bytes(rows, K))) return ops_fail(T2I_ERR_WORKSPACE, "workspace too small");
+  const size_t need = dw ? norm_bwd_ws_bytes(rows, K) : 0;
+  if (need && (!ws || ws_bytes < need)) return ops_fail(T2I_ERR_WORKSPACE, "workspace too small");
   NormBwd a;
   std::memset(&a, 0, sizeof(a));
   a.rows = rows;

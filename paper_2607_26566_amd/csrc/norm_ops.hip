@@ -353,7 +353,9 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel
       }
     }
   }
-  if (!partial) return;
+  // (one workgroup: its sums are dw)
+  T* const whole = gridDim.x == 1 ? (T*)a.dw : nullptr;
+  if (!partial && !whole) return;
   float* const p = partial + (size_t)blockIdx.x * K;
   if constexpr (RPB > 1) {
 #pragma unroll
@@ -365,13 +367,16 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel
       double s = 0.;
 #pragma unroll
       for (int g = 0; g < RPB; ++g) s += (double)cols[g][k];
-      p[k] = (float)s;
+      if (whole) whole[k] = from_f32<T>((float)s);
+      else p[k] = (float)s;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int k = (i * TPR + t) * 8;
-      if (k < K) store_piece(p + k, K - k, dw[i]);
+      if (k >= K) continue;
+      if (whole) store_piece(whole + k, K - k, dw[i]);
+      else store_piece(p + k, K - k, dw[i]);
     }
   }
 }
@@ -465,6 +470,8 @@ static int norm_rows_at_once(int K) { return K <= 1024 ? 4 : 1; }
 int norm_bwd_blocks(int rows, int K) {
   const int per = norm_rows_at_once(K);
   const long units = ((long)rows + per - 1) / per;
+  // few rows: one workgroup, whose sums need no second launch
+  if (units <= 4 && K <= kNormRegisters) return 1;
   return (int)std::max(std::min<long>(units, K <= 1024 ? 512 : K <= 2048 ? 768 : K <= 4096 ? 512 : 256), (units + kChain - 1) / kChain);
 }
 
@@ -492,12 +499,13 @@ static void norm_bwd_any(const NormBwd& a, float* partial, float* rstd, hipStrea
 
 hipError_t launch_add_rms_norm_bwd(bool is_bf16, bool resid_bf16, const NormBwd& a, float* ws, hipStream_t st) {
   const int blocks = norm_bwd_blocks(a.rows, a.K);
+  if (norm_bwd_ws_bytes(a.rows, a.K) == 0) ws = nullptr;
   // rows' factors first, then the workgroups' sums of columns
   float* const partial = ws ? ws + ((size_t)a.rows + 63) / 64 * 64 : nullptr;
   if (is_bf16 && resid_bf16) norm_bwd_any<bf16, bf16>(a, partial, ws, st);
   else if (is_bf16) norm_bwd_any<bf16, float>(a, partial, ws, st);
   else norm_bwd_any<float, float>(a, partial, ws, st);
-  if (a.dw) {
+  if (partial) {
     const dim3 grid((unsigned)((a.K + 15) / 16));
     if (is_bf16)
       hipLaunchKernelGGL((norm_weight_grad_kernel<bf16>), grid, dim3(1024), 0, st, partial, blocks, a.K, (bf16*)a.dw);
@@ -508,6 +516,7 @@ hipError_t launch_add_rms_norm_bwd(bool is_bf16, bool resid_bf16, const NormBwd&
 }
 
 size_t norm_bwd_ws_bytes(int rows, int K) {
+  if (norm_bwd_blocks(rows, K) == 1 && K <= kNormRegisters) return 0;
   return (((size_t)rows + 63) / 64 * 64 + (size_t)norm_bwd_blocks(rows, K) * K) * 4;
 }
 

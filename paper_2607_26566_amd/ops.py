@@ -436,7 +436,7 @@ def add_rms_norm_backward(dy: torch.Tensor, h: torch.Tensor, w: Optional[torch.T
     if w is not None:
         dw = w.new_empty(K)
         n = lib.t2i_op_add_rms_norm_backward_ws_bytes(rows, K)
-        ws = dy.new_empty(n, dtype=torch.uint8)
+        ws = dy.new_empty(n, dtype=torch.uint8) if n else None
     _check(lib.t2i_op_add_rms_norm_backward(dt, rt, rows, K, dy.data_ptr(), lddy, h.data_ptr(), ldh, _p(w), eps,
                                             _p(dh), lddh, dx.data_ptr(), K, _p(dresid), K, _p(dw), _p(ws), n,
                                             _stream(dev)))

@@ -75,12 +75,15 @@ SHAPES = [(1, 8, 8, 1, 1), (1, 4096, 1152, 1, 16), (2, 72, 136, 3, 5), (5, 128, 
           (4000, 4096, 640, 5, 40)]
 
 
-@pytest.mark.parametrize("order", [None, "runs", "scattered", "one"])
-@pytest.mark.parametrize("M,N,K,n,rank", SHAPES)
-@DTYPES
+# (fp32 takes the same tiles for more rows as for fewer)
+CASES = pytest.mark.parametrize("M,N,K,n,rank,dtype", [(*s, d) for s in SHAPES for d in (BF16, F32)
+                                                       if s[0] <= 1500 or d == BF16])
+ORDERS = pytest.mark.parametrize("order", [None, "runs", "scattered", "one"])
+
+
+@ORDERS
+@CASES
 def test_adapter_linear(M, N, K, n, rank, order, dtype):
-    if M > 1500 and dtype == F32:
-        pytest.skip("the same tiles as smaller ones")
     n = 1 if order is None else n
     say("adapter", M, N, K, n, rank, order, NAME[dtype])
     o, kw = operands(M, N, K, n, rank, order, dtype)
@@ -215,13 +218,11 @@ def test_adapter_epilogues(M, N, K):
                     assert torch.equal(cp, r.to(BF16)) and (cbuf[:-1, N:] == 7).all()
 
 
-@pytest.mark.parametrize("M,N,K", [(9, 64, 128), (40, 128, 72), (200, 264, 200), (4000, 4096, 640)])
-@DTYPES
+@pytest.mark.parametrize("M,N,K,dtype", [(9, 64, 128, BF16), (40, 128, 72, BF16), (300, 264, 200, BF16),
+                                         (4000, 4096, 640, BF16), (9, 64, 128, F32), (300, 264, 200, F32)])
 def test_one_tenants_nan_stays_with_it(M, N, K, dtype):
     """A NaN or an infinity in an adapter, in its scale or in one row of x reaches the rows that
     take it and no other; the gradients of other adapters neither."""
-    if M > 1000 and dtype == F32:
-        return
     for order in ("runs", "scattered"):
         o, kw = operands(M, N, K, 4, 16, order, dtype, 6)
         ix = kw["index"].clone()
@@ -306,12 +307,9 @@ def backward_bounds(h, dy, dtype):
     return ref, err
 
 
-@pytest.mark.parametrize("order", [None, "runs", "scattered", "one"])
-@pytest.mark.parametrize("M,N,K,n,rank", SHAPES)
-@DTYPES
+@ORDERS
+@CASES
 def test_adapter_linear_backward(M, N, K, n, rank, order, dtype):
-    if M > 1500 and (dtype == F32 or order == "one"):
-        pytest.skip("the same kernels as smaller ones")
     n = 1 if order is None else n
     say("adapter bwd", M, N, K, n, rank, order, NAME[dtype])
     o, kw = operands(M, N, K, n, rank, order, dtype, 11)

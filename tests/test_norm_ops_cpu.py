@@ -85,11 +85,11 @@ def test_add_rms_norm_i8_refuses():
 
 def test_add_rms_norm_backward_refuses():
     lib = t2i.load()
-    n = lib.t2i_op_add_rms_norm_backward_ws_bytes(3, 130)
-    assert n > 0 and n % 4 == 0
+    n = lib.t2i_op_add_rms_norm_backward_ws_bytes(30, 130)
+    assert n > 0 and n % 4 == 0 and lib.t2i_op_add_rms_norm_backward_ws_bytes(16, 130) == 0
     for rows, K in ((0, 5), (5, 0), (5, 2 ** 20 + 1), (2 ** 26, 5)):
         assert lib.t2i_op_add_rms_norm_backward_ws_bytes(rows, K) == 0
-    spec = dict(dtype=BF16, resid_dtype=F32, rows=3, K=130, dy=P, lddy=130, h=P, ldh=130, w=P, eps=1e-6, dh=P,
+    spec = dict(dtype=BF16, resid_dtype=F32, rows=30, K=130, dy=P, lddy=130, h=P, ldh=130, w=P, eps=1e-6, dh=P,
                 lddh=130, dx=P, lddx=130, dresid=P, lddr=130, dw=P, ws=P, ws_bytes=n, stream=None)
     check_refusals("t2i_op_add_rms_norm_backward", spec, [
         (dict(dtype=2), INVALID), (dict(resid_dtype=-1), INVALID), (dict(dtype=F32, resid_dtype=BF16), INVALID),
