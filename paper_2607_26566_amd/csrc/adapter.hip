@@ -655,11 +655,34 @@ static void adapter_linear_launch(const void* x, int ldx, const void* w, int ldw
     hipLaunchKernelGGL((adapter_linear_kernel<D, T, false, U>), grid, dim3(D::THREADS), 0, st, a, b, s, up, e, M, N);
 }
 
+// Two more shapes of bf16 products, for sizes that 256 x 256 divides into too few tiles for
+// the CUs: 8192 x 1152 x 4608 99 us on 256 x 256 (160 tiles), 83 on 256 x 192 (192); 2100 x
+// 4608 x 4608 115 (162), 97 on 192 x 256 (198); 6000 x 2048 x 2048 68 and 60; 5000 x 4096 x
+// 1152 59 on 128 x 128, 81.  Costs for choose_tile from these, as those of kTiles.
+using Tile192 = TileDims<192, 256, 2, 4, 2>;
+using Tile256n = TileDims<256, 192, 2, 4, 2>;
+constexpr TileChoice kWideTiles[] = {{192, 256, 1, 1.30f, 1.30f, 14.f}, {256, 192, 1, 1.28f, 1.28f, 14.f}};
+static int with_wide(int shape, float us, int wide, long rows, long cols, int steps) {
+  const TilePick w = choose_tile(kWideTiles, wide, rows, cols, steps, 1.f);
+  return w.us < us ? kTile192 + w.shape : shape;
+}
+int adapter_tile(bool is_bf16, int M, int N, int K) {
+  if (!is_bf16) return tile_index_f32(M, N, (K + 31) / 32);
+  const int steps = (K + 63) / 64, shape = tile_index(M, N, steps, 1.f);
+  return shape < kGradTiles ? with_wide(shape, choose_tile(kTiles + shape, 1, M, N, steps, 1.f).us, 2, M, N, steps) : shape;
+}
+#define T2I_TILES_ADAPTER(SHAPE, CALL)                      \
+  switch (SHAPE) {                                          \
+    case kTile192: { using D = Tile192; CALL; break; }      \
+    case kTile192 + 1: { using D = Tile256n; CALL; break; } \
+    default: T2I_TILES_FWD(SHAPE, CALL)                     \
+  }
+
 hipError_t launch_adapter_linear(bool is_bf16, const void* x, int ldx, const void* w, int ldw, int M, int N, int K,
                                  const AdapterUp& up, const LinearEpi& e, hipStream_t st) {
-  const int shape = is_bf16 ? tile_index(M, N, (K + 63) / 64, 1.f) : tile_index_f32(M, N, (K + 31) / 32);
+  const int shape = adapter_tile(is_bf16, M, N, K);
   if (is_bf16) {
-    T2I_TILES_FWD(shape, (adapter_linear_launch<D, bf16>(x, ldx, w, ldw, M, N, K, up, e, st)))
+    T2I_TILES_ADAPTER(shape, (adapter_linear_launch<D, bf16>(x, ldx, w, ldw, M, N, K, up, e, st)))
   } else if (f32_pieces({K, ldx, ldw}, {x, w})) {
     T2I_TILES_F32_FWD(shape, (adapter_linear_launch<D, float>(x, ldx, w, ldw, M, N, K, up, e, st)))
   } else {
@@ -669,17 +692,20 @@ hipError_t launch_adapter_linear(bool is_bf16, const void* x, int ldx, const voi
 }
 
 // dx has the shapes with groups of waves, too, which need no second launch: taken where
-// they are estimated to beat the best number of slices (fp32 333 x 1155 x 1153 @@ us)
+// they are estimated to beat the best number of slices (fp32 333 x 1155 x 1153 20.5 -> 17.2
+// us), and the wider of the two shapes above
 SplitPick adapter_dx_pick(bool is_bf16, int M, int N, int K) {
   const SplitPick p = split_dx(is_bf16, M, K, N);
   const int steps = is_bf16 ? (N + 63) / 64 : (N + 31) / 32;
-  if (steps < 4 || !few_tiles(M, K)) return p;
   const TileChoice* const tiles = is_bf16 ? kTiles : kTilesF32;
   const int first = is_bf16 ? kTile32k : kF32Groups;
-  const TilePick g = choose_tile(tiles + first, 2, M, K, steps, 1.f);
   const TilePick split = choose_tile(tiles + p.shape, 1, M, K, p.per, p.slices > 1 ? 2.f : 1.f, p.slices);
   const float us = split.us + (p.slices > 1 ? 4.f + (float)p.slices * M * K * 8 / 4e6f : 0.f);
-  return g.us < us ? SplitPick{first + g.shape, 1, steps} : p;
+  if (steps >= 4 && few_tiles(M, K)) {
+    const TilePick g = choose_tile(tiles + first, 2, M, K, steps, 1.f);
+    if (g.us < us) return {first + g.shape, 1, steps};
+  }
+  return is_bf16 && with_wide(0, us, 1, M, K, steps) ? SplitPick{kTile192, 1, steps} : p;
 }
 size_t adapter_dx_floats(bool is_bf16, int M, int N, int K) {
   const SplitPick p = adapter_dx_pick(is_bf16, M, N, K);
@@ -689,6 +715,7 @@ size_t adapter_dx_floats(bool is_bf16, int M, int N, int K) {
   switch (SHAPE) {                                     \
     case kTile32k: { using D = Tile32k; CALL; break; } \
     case kTile16k: { using D = Tile16k; CALL; break; } \
+    case kTile192: { using D = Tile192; CALL; break; } \
     default: T2I_TILES(SHAPE, CALL)                    \
   }
 
@@ -872,7 +899,7 @@ hipError_t launch_adapter_prepare(bool is_bf16, AdapterPrepare p, hipStream_t st
 }
 
 // u of up to so many products in the first launch: no second one, and B need not be
-// turned (fp32 333 x 1155, rank 5 @@)
+// turned (fp32 333 x 1155 x 1153, rank 5: 4.2 + 6.3 us in two launches, 7.9 in one)
 bool adapter_few_rows(int M, int N, int rank) { return M <= 1024 && (int64_t)M * N * rank <= 1 << 23; }
 
 // rows of a slice: all of up to 512, whose sums are then done without a second launch;

@@ -277,7 +277,9 @@ inline SplitPick choose_split(const TileChoice* tiles, int shapes, long rows, lo
   return best;
 }
 
-// (adapter.hip: dx beside adapters)
+// (adapter.hip: shapes of the layer beside adapters, of which two are its own, and of dx)
+constexpr int kTile192 = 9;
+int adapter_tile(bool is_bf16, int M, int N, int K);
 SplitPick adapter_dx_pick(bool is_bf16, int M, int N, int K);
 
 inline long whole4(long cols) { return (cols + 3) / 4 * 4; }

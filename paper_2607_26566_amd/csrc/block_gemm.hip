@@ -302,11 +302,17 @@ extern "C" int t2i_test_block_tile(int op, int is_bf16, int M, int F, int K, int
   if (M < 1 || F < 1 || K < 1 || op < 0 || op > 5) return 0;
   SplitPick p{0, 1, 0};
   const bool f32 = op != 0 && !is_bf16;
-  if (op == 4) p.shape = f32 ? tile_index_f32(M, F, (K + 31) / 32) : tile_index(M, F, (K + 63) / 64, 1.f);
+  if (op == 4) p.shape = adapter_tile(is_bf16, M, F, K);
   else if (op == 5) p = adapter_dx_pick(is_bf16, M, F, K);
   else if (op == 0) p.shape = tile_index(M, F, i8_row(K) / 128, 1.f);
   else if (op == 1) p.shape = f32 ? tile_index_f32(M, 2L * F, (K + 31) / 32) : tile_index(M, 2L * F, (K + 63) / 64, 0.5f);
   else p = op == 2 ? split_dx(is_bf16, M, K, 2 * gated_cols(F)) : split_dw(is_bf16, 2L * F, K, M);
+  if (!f32 && p.shape >= kTile192) {
+    *rows = p.shape == kTile192 ? 192 : 256;
+    *columns = p.shape == kTile192 ? 256 : 192;
+    *per_cu = *slices = 1;
+    return 1;
+  }
   const bool stream = !f32 && p.shape == kStream;   // four stages, one workgroup per CU
   const TileChoice& c = f32 ? kTilesF32[p.shape] : kTiles[stream ? kTile32 : p.shape];
   *rows = c.bm;
