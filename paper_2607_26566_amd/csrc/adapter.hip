@@ -702,7 +702,8 @@ SplitPick adapter_dx_pick(bool is_bf16, int M, int N, int K) {
   const TilePick split = choose_tile(tiles + p.shape, 1, M, K, p.per, p.slices > 1 ? 2.f : 1.f, p.slices);
   const float us = split.us + (p.slices > 1 ? 4.f + (float)p.slices * M * K * 8 / 4e6f : 0.f);
   if (steps >= 4 && few_tiles(M, K)) {
-    const TilePick g = choose_tile(tiles + first, 2, M, K, steps, 1.f);
+    // (bf16 with k across b's rows: a step takes twice as long as the forward product's)
+    const TilePick g = choose_tile(tiles + first, 2, M, K, is_bf16 ? 2 * steps : steps, 1.f);
     if (g.us < us) return {first + g.shape, 1, steps};
   }
   return is_bf16 && with_wide(0, us, 1, M, K, steps) ? SplitPick{kTile192, 1, steps} : p;
@@ -819,46 +820,45 @@ __device__ __forceinline__ void turn_rows(const AdapterTurn& d, long x) {
   store_piece((T*)d.out + ((size_t)ad * d.C + c) * d.stride + r0, d.stride - r0, v);
 }
 
-// u of few rows: four waves take one row and four ranks, a lane every 256th column
+// u of few rows: a workgroup takes one row and 32 ranks, G lanes eight ranks each of a row of
+// B, 64 / G rows side by side
 template <typename T>
 __device__ __forceinline__ void up_rows(const AdapterPrepare& p, int block) {
-  __shared__ float red[16][4];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, per = adapter_cols(p.rank) / 4;
-  const long item = block * 4L + (wave >> 2);
-  const int m = (int)(item / per), j0 = (int)(item % per) * 4;
-  const int ad = m < p.M ? adapter_of(p.index, p.n, m) : -1;
-  float s[4] = {0.f, 0.f, 0.f, 0.f};
+  __shared__ float red[16][32];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, cols = adapter_cols(p.rank), per = cols / 32;
+  const int m = block / per, first = block % per * 32;
+  const int ranks = min(p.rank - first, 32), G = ranks <= 8 ? 1 : ranks <= 16 ? 2 : 4;
+  const int ad = adapter_of(p.index, p.n, m), j0 = first + (lane & (G - 1)) * 8;
+  float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
   if (ad >= 0 && j0 < p.rank) {
     const T* const dy = (const T*)p.dy + (size_t)m * p.lddy;
-    const T* const b = (const T*)p.b + (size_t)ad * p.N * p.rank + j0;
-    typedef T any4 __attribute__((ext_vector_type(4), aligned(sizeof(T))));
-    const bool four = j0 + 4 <= p.rank;
+    const T* const b = (const T*)p.b + (size_t)ad * p.N * p.rank;
+    const int step = 64 / G;
 #pragma unroll 4
-    for (int c = (wave & 3) * 64 + lane; c < p.N; c += 256) {
+    for (int c = wave * step + lane / G; c < p.N; c += 16 * step) {
+      Piece<T> v;
+      load_piece(b + (size_t)c * p.rank, j0, p.rank, v);
       const float d = to_f32(dy[c]);
-      const T* const q = b + (size_t)c * p.rank;
-      if (four) {
-        const any4 v = *(const any4*)q;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) s[j] = fmaf(d, (float)v[j], s[j]);
-      } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (j0 + j < p.rank) s[j] = fmaf(d, to_f32(q[j]), s[j]);
-      }
+      for (int j = 0; j < 8; ++j) s[j] = fmaf(d, v.get(j), s[j]);
     }
   }
 #pragma unroll
-  for (int j = 0; j < 4; ++j) {
+  for (int j = 0; j < 8; ++j) {
 #pragma unroll
-    for (int o = 32; o >= 1; o >>= 1) s[j] += __shfl_xor(s[j], o, kWave);
-    if (lane == 0) red[wave][j] = s[j];
+    for (int o = 32; o >= 1; o >>= 1) {
+      const float y = __shfl_xor(s[j], o, kWave);
+      s[j] += o >= G ? y : 0.f;
+    }
+    if (lane < 4) red[wave][lane * 8 + j] = lane < G ? s[j] : 0.f;
   }
   __syncthreads();
-  if ((wave & 3) != 0 || lane >= 4 || m >= p.M) return;
-  const float v = (red[wave][lane] + red[wave + 1][lane]) + (red[wave + 2][lane] + red[wave + 3][lane]);
+  if (threadIdx.x >= 32) return;
+  float v = 0.f;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) v += red[w][lane];
   const float scale = ad >= 0 ? (p.scale ? p.scale[ad] : 1.f) : 0.f;
-  p.u[(size_t)m * adapter_cols(p.rank) + j0 + lane] = ad >= 0 && j0 + lane < p.rank ? v * scale : 0.f;
+  p.u[(size_t)m * cols + first + lane] = ad >= 0 && first + lane < p.rank ? v * scale : 0.f;
 }
 
 template <typename T>
@@ -886,7 +886,7 @@ __global__ __launch_bounds__(1024) void adapter_prepare_kernel(AdapterPrepare p)
   }
 }
 hipError_t launch_adapter_prepare(bool is_bf16, AdapterPrepare p, hipStream_t st) {
-  p.rows = p.dy ? (int)(((long)p.M * (adapter_cols(p.rank) / 4) + 3) / 4) : 0;
+  p.rows = p.dy ? p.M * (adapter_cols(p.rank) / 32) : 0;
   long blocks = p.groups + p.rows;
   for (AdapterTurn& d : p.turn) {
     d.blocks = d.in ? (int)(((long)((d.stride + 7) / 8) * d.C * p.n + 1023) / 1024) : 0;
@@ -902,15 +902,18 @@ hipError_t launch_adapter_prepare(bool is_bf16, AdapterPrepare p, hipStream_t st
 // turned (fp32 333 x 1155 x 1153, rank 5: 4.2 + 6.3 us in two launches, 7.9 in one)
 bool adapter_few_rows(int M, int N, int rank) { return M <= 1024 && (int64_t)M * N * rank <= 1 << 23; }
 
-// rows of a slice: all of up to 512, whose sums are then done without a second launch;
-// else as many as leave two workgroups for every CU, at least a step of four waves and at
-// most 1024
-int adapter_slice_rows(bool is_bf16, int M, int N, int K, int rank) {
-  if (M <= 512) return 1024;
+constexpr int kSliceRows = 1024;
+// rows of a slice: all of up to 768, whose sums are then done without a second launch;
+// else the most, up to kSliceRows, that leave 384 workgroups (adapters cut the slices, too),
+// at least a step of four waves.  t to dB and dA alone, 7531 x 4608 x 1152, rank 32, 8
+// adapters 67 us with 1024 rows, 71 with 512, 87 with 128; 3320 x 224 x 4256, rank 32 36, 30,
+// 36.
+int adapter_slice_rows(bool is_bf16, int M, int N, int K, int n, int rank) {
+  if (M <= 768) return kSliceRows;
   const int cols = is_bf16 ? 128 : 64;
   const long wide = (long)((K + cols - 1) / cols + (N + cols - 1) / cols) * ((rank + 31) / 32);
-  int per = 1024;
-  while (per > 128 && (M + per - 1) / per * wide < 1024) per /= 2;
+  int per = kSliceRows;
+  while (per > 128 && ((M + per - 1) / per + n / 2) * wide < 384) per /= 2;
   return per;
 }
 
@@ -924,6 +927,7 @@ template <typename T, int RT>
 __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterOuter p) {
   constexpr int L = kLaneK<T>, STEP = 4 * L, COLS = 16 * L;
   __shared__ f32x4 red[3][RT][64];
+  __shared__ int order[kSliceRows];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, fr = lane & 15, g = lane >> 4;
   const bool second = (int)blockIdx.x >= p.blocks0;
   const AdapterSide& d = second ? p.side[1] : p.side[0];
@@ -945,48 +949,68 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterOuter p) {
   for (int q = 0; q < L; ++q)
 #pragma unroll
     for (int jt = 0; jt < RT; ++jt) acc[q][jt] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 1
-  for (int r0 = wave * STEP; r0 < rows; r0 += 4 * STEP) {
+  for (int r = threadIdx.x; r < rows; r += 256) order[r] = p.order ? p.order[first + r] : first + r;
+  __syncthreads();
+  // a step's operands, zeros behind the last row; the next step's are under way while one is
+  // multiplied
+  struct Step {
     i32x4 raw[L];
-    Exact<T> vv[RT];
+    float e[RT][L];
+  };
+  auto load = [&](int r0, Step& x) {
     int row[L];
 #pragma unroll
     for (int i = 0; i < L; ++i) {
       const int at = r0 + g * L + i;
-      row[i] = at < rows ? (p.order ? p.order[first + at] : first + at) : -1;
+      row[i] = at < rows ? order[at] : -1;
     }
 #pragma unroll
     for (int i = 0; i < L; ++i) {
-      raw[i] = i32x4{0, 0, 0, 0};
-      if (row[i] >= 0 && in) raw[i] = load_k<T>(z + (size_t)row[i] * d.ldz, 0, c0, C, !part);
+      x.raw[i] = i32x4{0, 0, 0, 0};
+      if (row[i] >= 0 && in) x.raw[i] = load_k<T>(z + (size_t)row[i] * d.ldz, 0, c0, C, !part);
     }
 #pragma unroll
     for (int jt = 0; jt < RT; ++jt) {
       const int j = min(j0 + jt * 16 + fr, d.ldv - 1);
-      float e[L];
 #pragma unroll
-      for (int i = 0; i < L; ++i) e[i] = row[i] >= 0 ? v[(size_t)row[i] * d.ldv + j] : 0.f;
-      vv[jt].set(e);
+      for (int i = 0; i < L; ++i) x.e[jt][i] = row[i] >= 0 ? v[(size_t)row[i] * d.ldv + j] : 0.f;
     }
+  };
+  auto multiply = [&](const Step& x) {
+    Exact<T> vv[RT];
+#pragma unroll
+    for (int jt = 0; jt < RT; ++jt) vv[jt].set(x.e[jt]);
 #pragma unroll
     for (int q = 0; q < L; ++q) {
       i32x4 f;
       if constexpr (sizeof(T) == 2) {
 #pragma unroll
         for (int w = 0; w < 4; ++w)
-          f[w] = __builtin_amdgcn_perm(raw[2 * w + 1][q / 2], raw[2 * w][q / 2], q & 1 ? 0x07060302 : 0x05040100);
+          f[w] = __builtin_amdgcn_perm(x.raw[2 * w + 1][q / 2], x.raw[2 * w][q / 2], q & 1 ? 0x07060302 : 0x05040100);
       } else {
 #pragma unroll
-        for (int w = 0; w < 4; ++w) f[w] = raw[w][q];
+        for (int w = 0; w < 4; ++w) f[w] = x.raw[w][q];
       }
 #pragma unroll
       for (int jt = 0; jt < RT; ++jt) acc[q][jt] = narrow_mfma<T>(vv[jt], f, acc[q][jt]);
     }
+  };
+  Step even, odd;
+  int r0 = wave * STEP;
+  load(r0, even);
+#pragma unroll 1
+  for (; r0 < rows; r0 += 8 * STEP) {
+    load(r0 + 4 * STEP, odd);   // (behind the last row: zeros)
+    multiply(even);
+    if (r0 + 4 * STEP >= rows) break;
+    load(r0 + 8 * STEP, even);
+    multiply(odd);
   }
   // lane (fr, g) holds ranks 4 g + r of column c0 + q: the other waves' sums by way of LDS,
-  // in ascending order
+  // in ascending order (of one step only the first has any)
 #pragma unroll
   for (int q = 0; q < L; ++q) {
+    if (rows <= STEP) break;
     __syncthreads();
     if (wave > 0) {
 #pragma unroll

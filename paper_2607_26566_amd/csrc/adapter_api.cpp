@@ -34,7 +34,7 @@ struct Room {
 Room room_of(bool bf, int32_t M, int32_t N, int32_t K, int32_t n, int32_t rank) {
   Room r;
   const size_t e = bf ? 2 : 4;
-  r.per = adapter_slice_rows(bf, M, N, K, rank);
+  r.per = adapter_slice_rows(bf, M, N, K, n, rank);
   r.slices = M / r.per + n;
   size_t o = 0;
   auto take = [&](size_t bytes) {

@@ -190,7 +190,7 @@ hipError_t launch_adapter_dx(bool is_bf16, const void* dy, int lddy, const void*
 // (groups = n, or 0 without an index), matrices turned: out [n][C][stride] = in
 // [n][R][C], zeros behind R (in NULL: none), and u [M][adapter_cols(rank)] = s dy b (dy
 // NULL: not)
-int adapter_slice_rows(bool is_bf16, int M, int N, int K, int rank);
+int adapter_slice_rows(bool is_bf16, int M, int N, int K, int n, int rank);
 struct AdapterTurn {
   const void* in;
   void* out;
