@@ -904,16 +904,17 @@ bool adapter_few_rows(int M, int N, int rank) { return M <= 1024 && (int64_t)M *
 
 constexpr int kSliceRows = 1024;
 // rows of a slice: all of up to 768, whose sums are then done without a second launch;
-// else the most, up to kSliceRows, that leave 384 workgroups (adapters cut the slices, too),
-// at least a step of four waves.  t to dB and dA alone, 7531 x 4608 x 1152, rank 32, 8
-// adapters 67 us with 1024 rows, 71 with 512, 87 with 128; 3320 x 224 x 4256, rank 32 36, 30,
-// 36.
+// else the most, up to kSliceRows, that leave 384 workgroups (adapters cut the slices, too;
+// up to 16 ranks, where a wave has one step's loads under way instead of two: 1024), at
+// least a step of four waves.  dA and dB alone, 7531 x 4608 x 1152, rank 32, 8 adapters 67
+// us with 1024 rows, 71 with 512, 87 with 128; 3320 x 224 x 4256, rank 32 36, 30, 36; 4096 x
+// 4096 x 4096, rank 16 41, 35, 38, 34 with 256.
 int adapter_slice_rows(bool is_bf16, int M, int N, int K, int n, int rank) {
   if (M <= 768) return kSliceRows;
   const int cols = is_bf16 ? 128 : 64;
   const long wide = (long)((K + cols - 1) / cols + (N + cols - 1) / cols) * ((rank + 31) / 32);
   int per = kSliceRows;
-  while (per > 128 && ((M + per - 1) / per + n / 2) * wide < 384) per /= 2;
+  while (per > 128 && ((M + per - 1) / per + n / 2) * wide < (rank <= 16 ? 1024 : 384)) per /= 2;
   return per;
 }
 
@@ -924,7 +925,7 @@ int adapter_slice_rows(bool is_bf16, int M, int N, int K, int n, int rank) {
 // their dwords by v_perm, which gives it 8 (4) k of 8 (4) neighbouring columns, the
 // operands of as many MFMAs; z is read once for 32 ranks.
 template <typename T, int RT>
-__global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterOuter p) {
+__global__ __launch_bounds__(256, RT == 1 ? 4 : 2) void adapter_outer_kernel(AdapterOuter p) {
   constexpr int L = kLaneK<T>, STEP = 4 * L, COLS = 16 * L;
   __shared__ f32x4 red[3][RT][64];
   __shared__ int order[kSliceRows];
@@ -951,8 +952,8 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterOuter p) {
     for (int jt = 0; jt < RT; ++jt) acc[q][jt] = f32x4{0.f, 0.f, 0.f, 0.f};
   for (int r = threadIdx.x; r < rows; r += 256) order[r] = p.order ? p.order[first + r] : first + r;
   __syncthreads();
-  // a step's operands, zeros behind the last row; the next step's are under way while one is
-  // multiplied
+  // a step's operands, zeros behind the last row; of 32 ranks the next step's are under way
+  // while one is multiplied
   struct Step {
     i32x4 raw[L];
     float e[RT][L];
@@ -997,14 +998,22 @@ __global__ __launch_bounds__(256) void adapter_outer_kernel(AdapterOuter p) {
   };
   Step even, odd;
   int r0 = wave * STEP;
-  load(r0, even);
+  if constexpr (RT == 1) {   // (more waves instead)
 #pragma unroll 1
-  for (; r0 < rows; r0 += 8 * STEP) {
-    load(r0 + 4 * STEP, odd);   // (behind the last row: zeros)
-    multiply(even);
-    if (r0 + 4 * STEP >= rows) break;
-    load(r0 + 8 * STEP, even);
-    multiply(odd);
+    for (; r0 < rows; r0 += 4 * STEP) {
+      load(r0, even);
+      multiply(even);
+    }
+  } else {
+    load(r0, even);
+#pragma unroll 1
+    for (; r0 < rows; r0 += 8 * STEP) {
+      load(r0 + 4 * STEP, odd);   // (behind the last row: zeros)
+      multiply(even);
+      if (r0 + 4 * STEP >= rows) break;
+      load(r0 + 8 * STEP, even);
+      multiply(odd);
+    }
   }
   // lane (fr, g) holds ranks 4 g + r of column c0 + q: the other waves' sums by way of LDS,
   // in ascending order (of one step only the first has any)
