@@ -158,9 +158,14 @@ class AdamW:
                   "a captured step needs capturable=True: its count would stand still in the graph", 1)
         p, m, v, masters = self._at
         at = array("Q", map(_pointer, grads))
-        _check(load().t2i_op_adamw_step(
-            self._type, kind, len(self.params), self._numel, p, at.buffer_info()[0], m, v, masters, rate,
-            self.betas[0], self.betas[1], self.eps, self.weight_decay, self._steps + 1, lr_at, count, scale_at,
-            _stream(dev)))
+        try:
+            _check(load().t2i_op_adamw_step(
+                self._type, kind, len(self.params), self._numel, p, at.buffer_info()[0], m, v, masters, rate,
+                self.betas[0], self.betas[1], self.eps, self.weight_decay, self._steps + 1, lr_at, count, scale_at,
+                _stream(dev)))
+        except T2IError:
+            if self._count is not None:   # (no step was taken)
+                self._count -= 1
+            raise
         self._steps += 1
         torch.autograd.graph.increment_version(self._written)

@@ -153,6 +153,23 @@ def test_adamw_captured_steps_count_on():
             eager.step(g)
 
 
+@pytest.mark.parametrize("capturable", [False, True])
+def test_adamw_refused_steps_do_not_count(capturable):
+    say("refused step", capturable)
+    (p,), (g,) = tensors(5, [(300,)], 1.0), tensors(6, [(300,)], 1.0)
+    opt = t2i.AdamW([p.clone()], capturable=capturable, **HYPER)
+    opt.eps = -1.0
+    with pytest.raises(t2i.T2IError, match="eps"):
+        opt.step([g])
+    assert opt.steps == 0 and torch.equal(opt.params[0], p)
+    opt.eps = HYPER["eps"]
+    opt.step([g])
+    assert opt.steps == 1
+    zero = np.zeros(300)
+    check_step((to_host(p), zero, zero), [to_host(t[0]) for t in (opt.params, opt.exp_avg, opt.exp_avg_sq)],
+               to_host(g), 1)
+
+
 def test_adamw_resumed_on_another_stream_and_exchanged_weights():
     shapes = [(30, 7), (2049,)]
     p, g = tensors(1, shapes, 1.0), tensors(50, shapes, 0.1)
