@@ -5,7 +5,9 @@
  * be checked against its definition in isolation, and operators of transformer
  * blocks that the models above do not have: an 8-bit linear layer, a gated
  * feed-forward with its gradients, query / key norm with rotation and its
- * gradients.  Conventions are those of
+ * gradients, the residual's addition with an RMS norm and its gradients, a linear
+ * layer with a low-rank adapter per row and their gradients, an AdamW step.
+ * Conventions are those of
  * t2i_dit.h: device pointers are caller-owned HIP memory, `stream` is a
  * hipStream_t as void*, launches are asynchronous, arguments are validated
  * before any launch, errors come back as t2i_status (text in

@@ -1,5 +1,7 @@
 """Block operators in float64: the 8-bit linear layer, the gated feed-forward and
-its gradients, query / key norm with rotation and its gradients.
+its gradients, query / key norm with rotation and its gradients, the residual's addition
+with an RMS norm and its gradients, a linear layer with a low-rank adapter per row and
+their gradients, the AdamW step.
 
 The 8-bit scales are fp32 by definition; everything else is float64 throughout.
 """

@@ -10,6 +10,11 @@
 // rounded one and what rounding leaves, 2^-17 of it short: rounded once it would raise the
 // error of dA and dB, whose operand it is, from 0.0017 to 0.0024.
 //
+// What bounds them: the layer is its tile product's (7531 x 4608 x 1152, rank 32, adapters
+// in runs 100 - 118 us of 82.7 GFLOP, 4096 x 4096 x 4096, rank 16 105 of 137, dx 112), for
+// few rows HBM and the ring's first loads (24 x 4096 x 4096 10.5 us); t and the gradients'
+// sums are bound by reading x or dy once (33.6 MB: t 12.8 us, both sums 13.9).
+//
 // Adapters never meet: a row's sums hold nothing of another row's adapter, not even
 // times zero (a NaN in one tenant's adapter stays in that tenant's rows).
 #include <algorithm>

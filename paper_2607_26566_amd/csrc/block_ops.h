@@ -1,6 +1,7 @@
 // Block operators: 8-bit linear layer, gated feed-forward, query / key norm
-// with rotation.  Launchers (asynchronous on `st`; arguments checked by the
-// entry points in block_api.cpp).
+// with rotation; the residual's addition with an RMS norm, low-rank adapters beside
+// a shared layer, AdamW.  Launchers (asynchronous on `st`; arguments checked by the
+// entry points in block_api.cpp; norm_api.cpp, adapter_api.cpp, adamw_api.cpp).
 #pragma once
 
 #include "t2i_internal.h"

@@ -1,7 +1,9 @@
 // The residual's addition with an RMS norm, its output in the operands' type or in 8
 // bits, and the gradients (gfx950).  All of them are bound by HBM: a row's pieces are
 // read once, 16 bytes per lane, held in registers while its sum is taken, and each
-// output is written once.
+// output is written once.  With a large copy at 4.84 TB/s: 7531 rows of 1152 with an fp32
+// residual 18.4 us (104 MB, 5.7 TB/s, part of it in the cache), 8192 of 4096 43 in bf16, 49
+// to 8 bits (4.8), gradients of 4096 of 10240 69 + 5 (4.9).
 #include <algorithm>
 
 #include "row_ops.h"
@@ -240,7 +242,11 @@ static void norm_any(const NormFwd& a, hipStream_t st) {
   hipLaunchKernelGGL((add_rms_norm_kernel<T, R, TPR, NV, I8>),                                               \
                      dim3((unsigned)((a.rows + (TPR > 64 ? 0L : 3L)) / (TPR > 64 ? 1 : 4))),                 \
                      dim3(TPR > 64 ? TPR : 256), 0, st, a)
-  // one wave per row up to 2048 elements, a workgroup for longer rows
+  // One wave per row up to 2048 elements, whose sums need no LDS, a workgroup for longer
+  // rows, as few threads as hold theirs in two or three pieces each.  34 million elements, to
+  // bf16 and to 8 bits: rows of 1152 45 and 55 us, 51 and 72 with 256 threads; 2048 45 and
+  // 52, 44 and 51; 2560 44 and 52, 49 and 66 with 512; 5000 45 and 57, 54 and 71 with 1024;
+  // 16384 46 and 54, 46 and 58 with 512 of four pieces.
   if (a.K <= 512) T2I_N(64, 1);
   else if (a.K <= 1024) T2I_N(64, 2);
   else if (a.K <= 1536) T2I_N(64, 3);

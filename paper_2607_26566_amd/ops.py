@@ -1,5 +1,6 @@
 """Block operators (``include/t2i_ops.h``): 8-bit linear layer, gated
-feed-forward, query / key norm with rotation, and their gradients.
+feed-forward, query / key norm with rotation, the residual's addition with an RMS norm, a
+linear layer with a low-rank adapter per row, and their gradients.
 
 Argument marshalling only, as in the package's other calls.  Tensors are device
 tensors of one device whose last dimension is contiguous (rows may be strided);
