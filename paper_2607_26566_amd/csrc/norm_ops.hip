@@ -25,6 +25,30 @@ __device__ __forceinline__ float row_sum(float v, float* red) {
   return v;
 }
 
+// the same of NV values per thread, each wave's sums of one after the other in the order of
+// the row: the same result for any TPR NV; `red` [NV TPR / 64]
+template <int TPR, int NV>
+__device__ __forceinline__ float row_sum_in_order(float (&v)[NV], float* red) {
+#pragma unroll
+  for (int i = 0; i < NV; ++i)
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) v[i] += __shfl_xor(v[i], o, kWave);
+  float s = 0.f;
+  if constexpr (TPR > 64) {
+    constexpr int NW = TPR / 64;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) red[i * NW + ((threadIdx.x % TPR) >> 6)] = v[i];
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < NV * NW; ++i) s += red[i];
+  } else {
+#pragma unroll
+    for (int i = 0; i < NV; ++i) s += v[i];
+  }
+  return s;
+}
+
 // ---------------------------------------------------------------------------
 // Forward: h = resid + x, rounded to resid's type R, which the norm then takes:
 //   r = (mean h^2 + eps)^-1/2,  y = h r w.
@@ -68,7 +92,7 @@ template <typename T, typename R, int TPR, int NV, bool I8>
 __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(NormFwd a) {
   constexpr int RPB = TPR > 256 ? 1 : 256 / TPR, NW = TPR / 64;
   constexpr bool WIDE = I8 && sizeof(R) == 4;   // products past fp32
-  __shared__ float red_s[RPB][NW];
+  __shared__ float red_s[RPB][NV * NW];
   __shared__ uint32_t red_m[RPB][NW];
   __shared__ double red_d[RPB][NW];
   const int t = threadIdx.x % TPR, rl = threadIdx.x / TPR;
@@ -124,16 +148,16 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(Nor
   };
 
   double total = 0.;   // (over rounds; a round's squares in fp32)
-  float ss = 0.f;
+  float ss[NV];        // a piece's each
   uint32_t top = 0;    // bits of the largest |h w|, which order as it does, infinity and NaN above
   double topd = 0.;
   for (int r = 0; r < rounds; ++r) {
     load(r, true);
-    ss = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
+      ss[i] = 0.f;
 #pragma unroll
-      for (int j = 0; j < 8; ++j) ss = fmaf(v[i][j], v[i][j], ss);
+      for (int j = 0; j < 8; ++j) ss[i] = fmaf(v[i][j], v[i][j], ss[i]);
       if constexpr (I8) {
         float wv[8];
         weight(((r * NV + i) * TPR + t) * 8, wv);
@@ -144,9 +168,13 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(Nor
         }
       }
     }
-    if (rounds > 1) total += (double)ss;
+    if (rounds > 1)
+#pragma unroll
+      for (int i = 0; i < NV; ++i) total += (double)ss[i];
   }
-  if (rounds > 1) ss = (float)total;
+  if (rounds > 1)
+#pragma unroll
+    for (int i = 0; i < NV; ++i) ss[i] = i == 0 ? (float)total : 0.f;
   if constexpr (I8) {
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) {
@@ -160,7 +188,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(Nor
       }
     }
   }
-  ss = row_sum<TPR>(ss, red_s[rl]);
+  const float squares = row_sum_in_order<TPR, NV>(ss, red_s[rl]);
   if constexpr (I8 && TPR > 64) {
 #pragma unroll
     for (int i = 0; i < NW; ++i) {
@@ -168,7 +196,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(Nor
       if constexpr (WIDE) topd = fmax(topd, red_d[rl][i]);
     }
   }
-  const float rs = rsqrtf(fmaf(ss, 1.f / (float)K, a.eps));
+  const float rs = rsqrtf(fmaf(squares, 1.f / (float)K, a.eps));
   if (!live) return;
 
   if constexpr (!I8) {
@@ -247,13 +275,21 @@ static void norm_any(const NormFwd& a, hipStream_t st) {
   // bf16 and to 8 bits: rows of 1152 45 and 55 us, 51 and 72 with 256 threads; 2048 45 and
   // 52, 44 and 51; 2560 44 and 52, 49 and 66 with 512; 5000 45 and 57, 54 and 71 with 1024;
   // 16384 46 and 54, 46 and 58 with 512 of four pieces.
+  // Few rows, which leave CUs idle: a piece per thread (two of the longest).  16 rows of 1152
+  // 4.0 and 7.5 us, 2.9 and 4.2 with 256 threads; 333 of 1051 5.4 and 8.6, 4.1 and 5.1; 1500 of
+  // 1000 4.3 and 6.5, 4.7 and 6.4, of 1152 5.0 and 8.0, 4.9 and 6.7, of 2048 6.5 and 10.2, 5.6
+  // and 7.4; 700 of 4096 5.8 and 7.8, 5.5 and 7.1 with 512; 100 of 8192
+  // 4.1 and 6.5, 4.1 and 5.8 with 1024, 333 5.9 and 8.3, 6.2 and 8.2.
   if (a.K <= 512) T2I_N(64, 1);
+  else if (a.K <= 2048 && a.rows <= (a.K <= 1024 ? 1024 : 2048)) T2I_N(256, 1);
   else if (a.K <= 1024) T2I_N(64, 2);
   else if (a.K <= 1536) T2I_N(64, 3);
   else if (a.K <= 2048) T2I_N(64, 4);
+  else if (a.K <= 4096 && a.rows <= 1024) T2I_N(512, 1);
   else if (a.K <= 4096) T2I_N(256, 2);
+  else if (a.K <= 8192 && a.rows <= 256) T2I_N(1024, 1);
   else if (a.K <= 8192) T2I_N(512, 2);
-  else if (a.K <= 12288) T2I_N(512, 3);
+  else if (a.K <= 12288 && a.rows > 256) T2I_N(512, 3);
   else T2I_N(1024, 2);
 #undef T2I_N
 }

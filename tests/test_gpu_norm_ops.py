@@ -171,6 +171,22 @@ def test_norm_strides_surroundings_and_in_place(dtype, rtype):
                     assert (buf[:-1, K:] == 7).all() and (buf[-1] == 7).all()
 
 
+@pytest.mark.parametrize("K", [513, 1051, 1152, 2048, 3001, 4096, 8192, 10007])
+def test_norm_rows_do_not_depend_on_the_number_of_rows(K):
+    """few rows have more threads each, and the same sums"""
+    say("few and many rows", K)
+    x, _ = rnd(81, (2100, K), 1.0, BF16)
+    resid, _ = rnd(82, (2100, K), 2.0, F32)
+    w, _ = rnd(83, (K,), 1.0, BF16)
+    y, h = t2i.add_rms_norm(x, w, resid, eps=EPS)
+    q, s, _ = t2i.add_rms_norm_i8(x, w, resid, eps=EPS)
+    for rows in (1, 200, 300, 1024, 2048):
+        fy, fh = t2i.add_rms_norm(x[:rows], w, resid[:rows], eps=EPS)
+        fq, fs, _ = t2i.add_rms_norm_i8(x[:rows], w, resid[:rows], eps=EPS)
+        assert torch.equal(fy, y[:rows]) and torch.equal(fh, h[:rows])
+        assert torch.equal(fq, q[:rows]) and torch.equal(fs, s[:rows])
+
+
 def test_norm_rows_do_not_depend_on_the_batch():
     x, w, resid, _ = operands(3000, 1152, BF16, F32, 17)
     y, _ = t2i.add_rms_norm(x, w, resid)
