@@ -671,15 +671,22 @@ static int with_wide(int shape, float us, int wide, long rows, long cols, int st
   const TilePick w = choose_tile(kWideTiles, wide, rows, cols, steps, 1.f);
   return w.us < us ? kTile192 + w.shape : shape;
 }
+// And one for few rows, whose weights stream from memory: 16 x 16 with eight groups of
+// waves, one tile to a CU, where 16 x 32 leaves half of the CUs without one.  With t, 16 rows
+// x 4096 x 4096 15.0 us instead of 17.5, x 10240 26.8 and 35.5, 64 x 1024 x 1024 8.0 and
+// 9.4; more tiles than CUs take two rounds of it: 24 x 4096 x 4096 20.3 and 17.2.
+using Tile16n = TileDims<16, 16, 1, 1, 4, 8>;
 int adapter_tile(bool is_bf16, int M, int N, int K) {
   if (!is_bf16) return tile_index_f32(M, N, (K + 31) / 32);
   const int steps = (K + 63) / 64, shape = tile_index(M, N, steps, 1.f);
+  if (steps >= Tile16n::KG && (M + 15L) / 16 * ((N + 15L) / 16) <= 256) return kTile16n;
   return shape < kGradTiles ? with_wide(shape, choose_tile(kTiles + shape, 1, M, N, steps, 1.f).us, 2, M, N, steps) : shape;
 }
 #define T2I_TILES_ADAPTER(SHAPE, CALL)                      \
   switch (SHAPE) {                                          \
     case kTile192: { using D = Tile192; CALL; break; }      \
     case kTile192 + 1: { using D = Tile256n; CALL; break; } \
+    case kTile16n: { using D = Tile16n; CALL; break; }      \
     default: T2I_TILES_FWD(SHAPE, CALL)                     \
   }
 

@@ -277,8 +277,8 @@ inline SplitPick choose_split(const TileChoice* tiles, int shapes, long rows, lo
   return best;
 }
 
-// (adapter.hip: shapes of the layer beside adapters, of which two are its own, and of dx)
-constexpr int kTile192 = 9;
+// (adapter.hip: shapes of the layer beside adapters, of which three are its own, and of dx)
+constexpr int kTile192 = 9, kTile16n = 11;
 int adapter_tile(bool is_bf16, int M, int N, int K);
 SplitPick adapter_dx_pick(bool is_bf16, int M, int N, int K);
 

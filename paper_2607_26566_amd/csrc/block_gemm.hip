@@ -307,6 +307,12 @@ extern "C" int t2i_test_block_tile(int op, int is_bf16, int M, int F, int K, int
   else if (op == 0) p.shape = tile_index(M, F, i8_row(K) / 128, 1.f);
   else if (op == 1) p.shape = f32 ? tile_index_f32(M, 2L * F, (K + 31) / 32) : tile_index(M, 2L * F, (K + 63) / 64, 0.5f);
   else p = op == 2 ? split_dx(is_bf16, M, K, 2 * gated_cols(F)) : split_dw(is_bf16, 2L * F, K, M);
+  if (!f32 && p.shape == kTile16n) {
+    *rows = *columns = 16;
+    *per_cu = 1;
+    *slices = 8;
+    return 1;
+  }
   if (!f32 && p.shape >= kTile192) {
     *rows = p.shape == kTile192 ? 192 : 256;
     *columns = p.shape == kTile192 ? 256 : 192;

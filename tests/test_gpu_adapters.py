@@ -156,6 +156,28 @@ def test_rows_of_many_adapters_far_apart():
     assert torch.equal(t, t2) and torch.equal(y, y2)
 
 
+@pytest.mark.parametrize("M,N,K,rank", [(1, 4096, 456, 16), (16, 4096, 1160, 9), (17, 2048, 520, 33), (17, 2056, 520, 8),
+                                        (64, 1000, 456, 128), (64, 1032, 448, 16), (250, 256, 2056, 4), (15, 8, 5000, 1)])
+def test_few_tiles_of_the_second_product(M, N, K, rank):
+    """Up to one 16 x 16 tile to a CU, and a few more; groups of waves with a step and more each."""
+    for order in (None, "runs", "scattered"):
+        o, kw = operands(M, N, K, 1 if order is None else 4, rank, order, BF16, 31)
+        check_all(o, kw, M, N, BF16, 32)
+        bias, hb = rnd(33, (N,), 0.3, BF16)
+        gate, hg = rnd(34, (N,), 0.5)
+        y, err, _, _ = forward_bounds(host(o, kw), hb, BF16)
+        silu = blocks.act("silu", y)
+        lin = 1.13 * err + 2.0 ** -20 * (A(y) + err)   # (the activation's slope, its exponential and reciprocal)
+        within(t2i.adapter_linear(**o, bias=bias, **kw, epilogue="silu"), silu, U[BF16] * (A(silu) + lin) + lin, "silu")
+        resid, hr = rnd(35, (M, N), 2.0)
+        buf = torch.full((M + 1, N + 3), 7.0, device=DEV)
+        buf[:-1, :N] = resid
+        t2i.adapter_linear(**o, bias=bias, **kw, epilogue="resid_gated", resid=buf[:-1, :N], gate=gate)
+        ref = hr + hg * y
+        within(buf[:-1, :N], ref, A(hg) * err + 3 * E * (A(hg * y) + A(ref)), "resid_gated")
+        assert (buf[:-1, N:] == 7).all() and (buf[-1] == 7).all()
+
+
 def test_the_largest_tiles_are_reached():
     v = [C.c_int() for _ in range(4)]
     tiles = set()
