@@ -371,9 +371,11 @@ t2i_status t2i_op_add_rms_norm_backward(int32_t dtype, int32_t resid_dtype, int3
  *   out [M, N] (stride ldo), all of dtype; scale fp32 [n]
  *   or NULL (ones); index (device, [M]) or NULL: every row takes adapter 0.  A row
  *   whose index is not in 0 .. n - 1 takes no adapter.  The rest as t2i_op_linear.
- *   Products and sums in fp32, one rounding.  t fp32 receives rank columns and zeros up
- *   to rank rounded up to 32 (ldt at least that, % 8 == 0, 16-byte aligned): scratch
- *   memory, or kept for t2i_op_adapter_linear_backward.
+ *   Products and sums in fp32, one rounding; bf16 operands meet all of t's bits, and an
+ *   infinity among them makes infinities and NaN as in fp32 (of t and the gradients' u
+ *   from 2^-86).  t fp32 receives rank columns and zeros up to rank rounded up to 32
+ *   (ldt at least that, % 8 == 0, 16-byte aligned): scratch memory, or kept for
+ *   t2i_op_adapter_linear_backward.
  *   bf16: N, K, ldx, ldw % 8 == 0, x, w, a 16-byte aligned.  fp32: any sizes, strides
  *   and alignment.  1 <= rank <= 128, n <= 32767, n max(N, K) times
  *   rank rounded up to 8 below 2^32; M <= 2^24,

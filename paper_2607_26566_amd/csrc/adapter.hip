@@ -2,13 +2,14 @@
 // both (gfx950).  Row m takes adapter i = index[m], or none:
 //   t = s_i x A_i^T,  y = x W^T + bias + t B_i^T.
 // Three kinds of kernels: the narrow products with A (and, for the gradients, B) that make
-// t, one row of 16 ranks per 16 x 16 MFMA tile or per wave; the shared product on the
-// tiles of gemm_tile.h, whose accumulators take t B^T before the epilogue; and the
-// adapters' own gradients, sums over the rows of each.
+// t, on tiles of 16 or 32 rows or, for few rows, one row and four ranks to a workgroup; the
+// shared product on the tiles of gemm_tile.h, whose accumulators take t B^T before the
+// epilogue; and the adapters' own gradients, sums over the rows of each.
 //
-// t (and the gradients' u) is fp32.  The matrix cores take it as two bf16 values, the
-// rounded one and what rounding leaves, 2^-17 of it short: rounded once it would raise the
-// error of dA and dB, whose operand it is, from 0.0017 to 0.0024.
+// t (and the gradients' u) is fp32.  The matrix cores take it as three bf16 values, 8 of its
+// 24 bits each and all of its sign: rounded once it would raise the error of dA and dB, whose
+// operand it is, from 0.0017 to 0.0024, and parts of both signs would make a NaN of their
+// products with an infinity.
 //
 // What bounds them: the layer is its tile product's (7531 x 4608 x 1152, rank 32, adapters
 // in runs 100 - 118 us of 82.7 GFLOP, 4096 x 4096 x 4096, rank 16 105 of 137, dx 112), for
@@ -28,6 +29,23 @@ namespace t2i {
 __device__ __forceinline__ int adapter_of(const int32_t* index, int n, int row) {
   const int i = index ? index[row] : 0;
   return (unsigned)i < (unsigned)n ? i : -1;
+}
+
+// the least adapter above `now` of the rows of 16 neighbouring lanes (negative: none), or kNone:
+// unsigned differences put those up to `now` last; ds_swizzle (lanes xor 8, 4, 2, 1) takes no
+// registers for addresses
+constexpr int kNone = 0x7fffffff;
+template <int N>
+__device__ __forceinline__ int least_above(int now, const int (&ids)[N]) {
+  uint32_t v = ~0u;
+#pragma unroll
+  for (int i = 0; i < N; ++i) v = min(v, (uint32_t)(ids[i] - now - 1));
+  v = min(v, (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x201f));
+  v = min(v, (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x101f));
+  v = min(v, (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x081f));
+  v = min(v, (uint32_t)__builtin_amdgcn_ds_swizzle((int)v, 0x041f));
+  v = (uint32_t)__builtin_amdgcn_readfirstlane((int)v);
+  return v < 0x80000000u - (uint32_t)(now + 1) ? now + 1 + (int)v : kNone;
 }
 
 // elements of a lane's 16 bytes: consecutive k of an MFMA operand
@@ -63,22 +81,36 @@ __device__ __forceinline__ float element(const i32x4& v, int i) {
   else
     return __int_as_float(v[i]);
 }
-// a lane's operand of t: L consecutive values, bf16 in two parts
+// a lane's operand of t: L consecutive values, bf16 in three parts of t's sign, each the upper
+// half of what the ones before it leave.  A part that would be 0 is 2^-40 t instead (t is off
+// by 2^-39 of itself at most), so that an infinite factor makes an infinity of every part as it
+// does of t, unless t is below 2^-86; t = 0 and infinities have equal parts.
 template <typename T>
 struct Exact {
-  i32x4 hi, lo;
+  static constexpr int PARTS = sizeof(T) == 2 ? 3 : 1;
+  i32x4 part[PARTS];
   __device__ __forceinline__ void set(const float (&v)[kLaneK<T>]) {
     if constexpr (sizeof(T) == 2) {
-      bf16x8 h, l;
+      auto top = [](float x) { return __uint_as_float(__float_as_uint(x) & 0xffff0000u); };
+      // the upper halves of two values, with these signs
+      auto pair = [](float x, float y) { return __builtin_amdgcn_perm(__float_as_uint(y), __float_as_uint(x), 0x07060302); };
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        h[i] = (bf16)v[i];
-        const float f = (float)h[i];
-        l[i] = (bf16)(__builtin_isinf(f) ? 0.f : v[i] - f);
+      for (int i = 0; i < 4; ++i) {
+        float mid[2], low[2];
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const float x = v[2 * i + e], least = fabsf(x) * 0x1p-40f;
+          // (an infinity less itself is a NaN, which fmaxf leaves out)
+          mid[e] = fmaxf(fabsf(x - top(x)), least);
+          low[e] = fmaxf(mid[e] - top(mid[e]), least);
+        }
+        const uint32_t hi = pair(v[2 * i], v[2 * i + 1]), sign = hi & 0x80008000u;
+        part[0][i] = (int)hi;
+        part[1][i] = (int)(pair(mid[0], mid[1]) | sign);
+        part[2][i] = (int)(pair(low[0], low[1]) | sign);
       }
-      hi = __builtin_bit_cast(i32x4, h), lo = __builtin_bit_cast(i32x4, l);
     } else {
-      hi = i32x4{__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
+      part[0] = i32x4{__float_as_int(v[0]), __float_as_int(v[1]), __float_as_int(v[2]), __float_as_int(v[3])};
     }
   }
 };
@@ -99,14 +131,14 @@ __device__ __forceinline__ f32x4 narrow_mfma(const i32x4& a, const i32x4& b, f32
 
 template <typename T>
 __device__ __forceinline__ f32x4 narrow_mfma(const i32x4& a, const Exact<T>& b, f32x4 c) {
-  c = narrow_mfma<T>(a, b.hi, c);
-  if constexpr (sizeof(T) == 2) c = narrow_mfma<T>(a, b.lo, c);
+#pragma unroll
+  for (int i = 0; i < Exact<T>::PARTS; ++i) c = narrow_mfma<T>(a, b.part[i], c);
   return c;
 }
 template <typename T>
 __device__ __forceinline__ f32x4 narrow_mfma(const Exact<T>& a, const i32x4& b, f32x4 c) {
-  c = narrow_mfma<T>(a.hi, b, c);
-  if constexpr (sizeof(T) == 2) c = narrow_mfma<T>(a.lo, b, c);
+#pragma unroll
+  for (int i = 0; i < Exact<T>::PARTS; ++i) c = narrow_mfma<T>(a.part[i], b, c);
   return c;
 }
 
@@ -288,20 +320,11 @@ __global__ __launch_bounds__(D::THREADS, 1) void adapter_down_kernel(AdapterDown
         for (int j = 0; j < TN; ++j) store(i, j, f32x4{0.f, 0.f, 0.f, 0.f});
   }
   if (behind) return;
-  // the least adapter above `now`
-  auto above = [&](int now) {
-    int next = 0x7fffffff;
-#pragma unroll
-    for (int i = 0; i < TM; ++i) next = min(next, ad[i] > now ? ad[i] : 0x7fffffff);
-#pragma unroll
-    for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, kWave));
-    return __builtin_amdgcn_readfirstlane(next);
-  };
-  int next = above(-1);
+  int next = least_above(-1, ad);
   int last = next;
 #pragma unroll
-  for (int i = 0; i < kOwn; ++i) last = last == 0x7fffffff ? last : above(last);
-  const bool several = last != 0x7fffffff;   // more than kOwn
+  for (int i = 0; i < kOwn; ++i) last = last == kNone ? last : least_above(last, ad);
+  const bool several = last != kNone;   // more than kOwn
   if (several && p.n <= kSorted && (int64_t)kWindow * p.ldx * EB < 0x7fffffff) {
     const int first = m0 / kWindow * kWindow, tile = (m0 - first) / D::BM;
     const S sh{(int16_t*)smem, (int*)(smem + kWindow * 2), (uint8_t*)(smem + kWindow * 2 + kSorted * 4),
@@ -313,17 +336,17 @@ __global__ __launch_bounds__(D::THREADS, 1) void adapter_down_kernel(AdapterDown
       row[i] = max(rows[0][i * 16 + fr], 0);
       ad[i] = rows[0][i * 16 + fr] < 0 ? -2 : rows[1][i * 16 + fr];
     }
-    next = above(-1);
+    next = least_above(-1, ad);
   } else {
     if (threadIdx.x < D::BM) rows[0][threadIdx.x] = min((int)threadIdx.x, p.M - 1 - m0);
     __syncthreads();
   }
   int now = -1;
   for (;;) {   // the adapters in ascending order, the same for every wave
-    if (next == 0x7fffffff) return;
+    if (next == kNone) return;
     if (now >= 0) tile_barrier();   // (the sums of the adapter before are read)
     now = next;
-    next = above(now);
+    next = least_above(now, ad);
     const TileOperand b{(const char*)p.a + (size_t)now * p.rank * p.K * EB, nullptr, (uint32_t)(EB * p.K), p.rank, 0};
     typename P::Acc acc[TM][TN];
     if (!P::run_groups(smem, a, b, s, m0, j0, acc, FromZero(),
@@ -431,16 +454,6 @@ struct Adapters {
     return load_k<T>(p, (uint32_t)(min(P::col_of(j, x), N - 1 - nw) * u.stride) * (uint32_t)sizeof(T), k, u.rank,
                      u.rank % L == 0);
   }
-  // the least adapter of the wave's rows above `now`, or kNone
-  static constexpr int kNone = 0x7fffffff;
-  __device__ __forceinline__ int above(int now) const {
-    int next = kNone;
-#pragma unroll
-    for (int i = 0; i < TM; ++i) next = min(next, id[i] > now ? id[i] : kNone);
-#pragma unroll
-    for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, kWave));
-    return __builtin_amdgcn_readfirstlane(next);
-  }
   __device__ __forceinline__ bool one_adapter() const {
     const int first = __builtin_amdgcn_readfirstlane(id[0]);
     bool same = true;
@@ -474,7 +487,7 @@ struct Adapters {
         for (int i = 0; i < TM; ++i) tv[i] = exact_t(i, k0 + g * L);
         // (one after the other: two at a time spill the accumulators of 128 x 128)
 #pragma unroll 1
-        for (int now = above(-1); now != kNone; now = above(now)) {
+        for (int now = least_above(-1, id); now != kNone; now = least_above(now, id)) {
           i32x4 pv[TN];
 #pragma unroll
           for (int j = 0; j < TN; ++j) pv[j] = p_at(now, j, fr, k0 + g * L);
@@ -526,26 +539,24 @@ struct Adapters {
         for (int k0 = 0; k0 < u.rank; k0 += 4 * L) {
           Exact<T> tv[HALF];
 #pragma unroll
-          for (int i = 0; i < HALF; ++i) tv[i] = exact_t(h * HALF + i, k0 + g * L);
+          for (int i = 0; i < HALF; ++i) {
+            tv[i] = exact_t(h * HALF + i, k0 + g * L);
+            __builtin_amdgcn_sched_barrier(0);
+          }
 #pragma unroll 1
-          for (int now = -1;;) {
-            int next = kNone;
+          for (int now = least_above(-1, mine); now != kNone; now = least_above(now, mine)) {
+            // (two fragments of P_i, and t's one after the other: all at once spill 20 registers more)
+            i32x4 pv[2] = {p_at(now, 0, fr, k0 + g * L)};
 #pragma unroll
-            for (int i = 0; i < HALF; ++i) next = min(next, mine[i] > now ? mine[i] : kNone);
+            for (int j = 0; j < TN; ++j) {
+              if (j + 1 < TN) pv[(j + 1) % 2] = p_at(now, j + 1, fr, k0 + g * L);
 #pragma unroll
-            for (int o = 8; o >= 1; o >>= 1) next = min(next, __shfl_xor(next, o, kWave));
-            now = __builtin_amdgcn_readfirstlane(next);
-            if (now == kNone) break;
-            i32x4 pv[TN];
-#pragma unroll
-            for (int j = 0; j < TN; ++j) pv[j] = p_at(now, j, fr, k0 + g * L);
-#pragma unroll
-            for (int i = 0; i < HALF; ++i)
-#pragma unroll
-              for (int j = 0; j < TN; ++j) {
-                const f32x4 add = narrow_mfma<T>(pv[j], tv[i], f32x4{0.f, 0.f, 0.f, 0.f});
+              for (int i = 0; i < HALF; ++i) {
+                const f32x4 add = narrow_mfma<T>(pv[j % 2], tv[i], f32x4{0.f, 0.f, 0.f, 0.f});
                 if (mine[i] == now) part[(i * TN + j) * 64] += add;
               }
+              __builtin_amdgcn_sched_barrier(0);
+            }
           }
         }
 #pragma unroll
