@@ -56,7 +56,7 @@ __device__ __forceinline__ float row_sum_in_order(float (&v)[NV], float* red) {
 // the scale s = T r / 127 and an element alone: q = 127 t / T to the nearest whole
 // number, ties to even, of the exact quotient.
 //
-// t of bf16 factors is exact in fp32, that of fp32 ones in fp64.  127 t / T takes no
+// t of bf16 factors is exact in fp32 (but for its smallest values), that of fp32 ones in fp64.  127 t / T takes no
 // division: m = fma(t, 127 / T, 1.5 2^23) leaves the nearest whole number n in its low
 // bits; the factor, t and the product are off by 2^-24 of themselves each, so that n may
 // be wrong only where the quotient is within 127 3 2^-24 < 2^-15 of a half.  Pieces that
@@ -95,6 +95,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(Nor
   __shared__ float red_s[RPB][NV * NW];
   __shared__ uint32_t red_m[RPB][NW];
   __shared__ double red_d[RPB][NW];
+  __shared__ float red_l[RPB][NW];
   const int t = threadIdx.x % TPR, rl = threadIdx.x / TPR;
   const int row = blockIdx.x * RPB + rl, K = a.K;
   const bool live = row < a.rows;
@@ -217,12 +218,59 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_kernel(Nor
   } else {
     const bool finite = top < 0x7f800000u && rs == rs;
     const float most = __uint_as_float(top);
+    int8_t* const q = (int8_t*)a.y + at * a.ldy;
+    if constexpr (!WIDE) {
+      // Products of bf16 factors up to 2^-90 may have lost bits in fp32, which holds 2^160 times
+      // them (from 2^-266): codes by division, settled as below.  (Apart, from memory once more,
+      // so that other rows keep their registers.)
+      if (most <= 0x1p-90f) {   // (the same for all threads of the row)
+        const R* const from = resid ? (const R*)h : (const R*)x;
+        auto products = [&](int c, float (&p)[8]) {
+          Piece<R> hv;
+          float wv[8];
+          load_piece(from, c * 8, K, hv);
+          weight(c * 8, wv);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) p[j] = (float)((double)hv.get(j) * (double)wv[j] * 0x1p160);
+        };
+        float large = 0.f;
+#pragma unroll 1
+        for (int c = t; c < pieces; c += TPR) {
+          float p[8];
+          products(c, p);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) large = fmaxf(large, fabsf(p[j]));
+        }
+#pragma unroll
+        for (int o = 32; o >= 1; o >>= 1) large = fmaxf(large, __shfl_xor(large, o, kWave));
+        if constexpr (TPR > 64) {
+          if ((t & 63) == 0) red_l[rl][t >> 6] = large;
+          __syncthreads();
+#pragma unroll
+          for (int i = 0; i < NW; ++i) large = fmaxf(large, red_l[rl][i]);
+        }
+        if (t == 0) a.scale[at] = (float)((double)large * 0x1p-160 * (double)rs / 127.);
+#pragma unroll 1
+        for (int c = t; c < all; c += TPR) {
+          uint64_t codes = 0;
+          if (c < pieces && large > 0.f) {
+            float p[8];
+            products(c, p);
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+              codes |= (uint64_t)(uint8_t)(int)settle(rintf(127.f * p[j] / large), p[j], large) << (8 * j);
+          }
+          *(uint64_t*)(q + (size_t)c * 8) = codes;
+        }
+        return;
+      }
+    }
     // (factors past fp32's range, or products that have lost bits there: in fp64)
     const bool plain = most > 0x1p-90f && most < 0x1p120f;
     const float inv = plain ? 127.f / most : 0.f;
     const double exact = WIDE ? topd : (double)most;
-    if (t == 0) a.scale[at] = finite ? most * rs / 127.f : __uint_as_float(0x7fc00000u);
-    int8_t* const q = (int8_t*)a.y + at * a.ldy;
+    if (t == 0)
+      a.scale[at] = !finite ? __uint_as_float(0x7fc00000u) : plain ? most * rs / 127.f : (float)(exact * (double)rs / 127.);
     const int qrounds = (all + TPR * NV - 1) / (TPR * NV);
     for (int r = 0; r < qrounds; ++r) {
       if (rounds > 1) load(r, false);
