@@ -139,7 +139,7 @@ struct NormBwd {
   void* dw;                          // or NULL
 };
 // workgroups of the kernel that walks the rows: rows of its partial sums [blocks][K]
-int norm_bwd_blocks(int rows, int K);
+int norm_bwd_blocks(bool is_bf16, int rows, int K);
 size_t norm_bwd_ws_bytes(int rows, int K);
 // ws: only with dw
 hipError_t launch_add_rms_norm_bwd(bool is_bf16, bool resid_bf16, const NormBwd& a, float* ws, hipStream_t st);

@@ -5,6 +5,7 @@
 // residual 18.4 us (104 MB, 5.7 TB/s, part of it in the cache), 8192 of 4096 43 in bf16, 49
 // to 8 bits (4.8), gradients of 4096 of 10240 69 + 5 (4.9).
 #include <algorithm>
+#include <type_traits>
 
 #include "row_ops.h"
 
@@ -353,18 +354,36 @@ hipError_t launch_add_rms_norm(bool is_bf16, bool resid_bf16, bool to_i8, const 
 // Backward, with d = dy w, n = h r:
 //   dsum = dh + r (d - n mean(d n)),  dw = sum over rows of dy n.
 // A fixed number of workgroups walks the rows; a thread keeps its columns of w and of
-// dw, which adds up in fp32 over the thread's own rows (at most kChain), in fp64 over the
-// waves of a workgroup that have the same columns, whose sum is kept in fp32, and in fp64
-// over the workgroups (norm_weight_grad_kernel): a fixed order.
+// dw, which adds up over the thread's own rows (at most kChain), in fp64 over the waves of a
+// workgroup that have the same columns and in fp64 over the workgroups
+// (norm_weight_grad_kernel): a fixed order.  A thread's and a workgroup's sums are fp32 where
+// the result is bf16, fp64 where it is fp32 (16000 rows of 512: error of dw 8.9e-8 with sums
+// in fp32, 200000 of 64 1.6e-7; a result's own rounding and its products' are 5 to 6e-8), from
+// three pieces per thread in LDS, for registers hold no more.
 constexpr int kChain = 64;
+template <typename T>
+using ColumnSum = std::conditional_t<sizeof(T) == 4, double, float>;
+__device__ __forceinline__ void store_sums(float* p, int n, const float (&v)[8]) { store_piece(p, n, v); }
+__device__ __forceinline__ void store_sums(double* p, int n, const double (&v)[8]) {
+  typedef double any2 __attribute__((ext_vector_type(2), aligned(8)));
+#pragma unroll
+  for (int i = 0; i < 8; i += 2) {
+    if (i + 2 <= n) *(any2*)(p + i) = any2{v[i], v[i + 1]};
+    else if (i < n) p[i] = v[i];
+  }
+}
 
 template <typename T, typename R, int TPR, int NV>
-__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel(NormBwd a, float* __restrict__ partial) {
+__global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel(
+    NormBwd a, ColumnSum<T>* __restrict__ partial) {
+  using S = ColumnSum<T>;
   constexpr int RPB = TPR > 256 ? 1 : 256 / TPR, NW = TPR / 64;
+  constexpr bool IN_LDS = sizeof(S) == 8 && NV >= 3;
   __shared__ float red[2][2][RPB][NW];
-  __shared__ float cols[RPB > 1 ? RPB : 1][RPB > 1 ? TPR * NV * 8 : 1];
+  __shared__ S cols[RPB > 1 ? RPB : 1][RPB > 1 ? TPR * NV * 8 : 1];
+  __shared__ S kept[IN_LDS ? NV : 1][IN_LDS ? 8 : 1][IN_LDS ? TPR : 1];   // a thread's own each
   const int t = threadIdx.x % TPR, rl = threadIdx.x / TPR, K = a.K;
-  float dw[NV][8];
+  S dw[IN_LDS ? 1 : NV][8];
   Piece<T> w[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) {
@@ -377,7 +396,9 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel
         for (int j = 0; j < 8; ++j) w[i].set(j, (T)1.f);
     }
 #pragma unroll
-    for (int j = 0; j < 8; ++j) dw[i][j] = 0.f;
+    for (int j = 0; j < 8; ++j)
+      if constexpr (IN_LDS) kept[i][j][t] = 0;
+      else dw[i][j] = 0;
   }
   int parity = 0;
   for (int r0 = blockIdx.x * RPB; r0 < a.rows; r0 += gridDim.x * RPB, parity ^= 1) {
@@ -435,7 +456,9 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           const float n = h[i].get(j) * r, d = dy[i].get(j);
-          dw[i][j] = fmaf(d, n, dw[i][j]);
+          if constexpr (IN_LDS) kept[i][j][t] += (S)(d * n);
+          else if constexpr (sizeof(S) == 8) dw[i][j] += (S)(d * n);
+          else dw[i][j] = fmaf(d, n, dw[i][j]);
           o[j] = fmaf(r, fmaf(-n, c, d * w[i].get(j)), dh[i].get(j));
         }
         store_piece((T*)a.dx + at * a.lddx + k, K - k, o);
@@ -446,7 +469,7 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel
   // (one workgroup: its sums are dw)
   T* const whole = gridDim.x == 1 ? (T*)a.dw : nullptr;
   if (!partial && !whole) return;
-  float* const p = partial + (size_t)blockIdx.x * K;
+  S* const p = partial + (size_t)blockIdx.x * K;
   if constexpr (RPB > 1) {
 #pragma unroll
     for (int i = 0; i < NV; ++i)
@@ -458,15 +481,24 @@ __global__ __launch_bounds__(TPR > 256 ? TPR : 256) void add_rms_norm_bwd_kernel
 #pragma unroll
       for (int g = 0; g < RPB; ++g) s += (double)cols[g][k];
       if (whole) whole[k] = from_f32<T>((float)s);
-      else p[k] = (float)s;
+      else p[k] = (S)s;
     }
   } else {
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
       const int k = (i * TPR + t) * 8;
       if (k >= K) continue;
-      if (whole) store_piece(whole + k, K - k, dw[i]);
-      else store_piece(p + k, K - k, dw[i]);
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if constexpr (IN_LDS) dw[0][j] = kept[i][j][t];
+      const S(&o)[8] = dw[IN_LDS ? 0 : i];
+      if (whole) {
+        const float v[8] = {(float)o[0], (float)o[1], (float)o[2], (float)o[3],
+                            (float)o[4], (float)o[5], (float)o[6], (float)o[7]};
+        store_piece(whole + k, K - k, v);
+      } else {
+        store_sums(p + k, K - k, o);
+      }
     }
   }
 }
@@ -526,10 +558,11 @@ __global__ __launch_bounds__(1024) void add_rms_norm_bwd_long_kernel(NormBwd a, 
 // (after the rows': dx may not lie over dy or h)
 template <typename T, typename R>
 __global__ __launch_bounds__(256) void add_rms_norm_dw_long_kernel(NormBwd a, const float* __restrict__ rstd,
-                                                                   float* __restrict__ partial) {
+                                                                   ColumnSum<T>* __restrict__ partial) {
+  using S = ColumnSum<T>;
   const int k = (blockIdx.y * 256 + threadIdx.x) * 8, K = a.K;
   if (k >= K) return;
-  float dw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+  S dw[8] = {0, 0, 0, 0, 0, 0, 0, 0};
   for (int row = blockIdx.x; row < a.rows; row += gridDim.x) {
     Piece<T> pd;
     Piece<R> ph;
@@ -537,14 +570,16 @@ __global__ __launch_bounds__(256) void add_rms_norm_dw_long_kernel(NormBwd a, co
     load_piece((const R*)a.h + (size_t)row * a.ldh, k, K, ph);
     const float r = rstd[row];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) dw[j] = fmaf(pd.get(j), ph.get(j) * r, dw[j]);
+    for (int j = 0; j < 8; ++j)
+      if constexpr (sizeof(S) == 8) dw[j] += (S)(pd.get(j) * (ph.get(j) * r));
+      else dw[j] = fmaf(pd.get(j), ph.get(j) * r, dw[j]);
   }
-  store_piece(partial + (size_t)blockIdx.x * K + k, K - k, dw);
+  store_sums(partial + (size_t)blockIdx.x * K + k, K - k, dw);
 }
 
 template <typename T>
-__global__ __launch_bounds__(1024) void norm_weight_grad_kernel(const float* __restrict__ partial, int blocks, int K,
-                                                                T* __restrict__ dw) {
+__global__ __launch_bounds__(1024) void norm_weight_grad_kernel(const ColumnSum<T>* __restrict__ partial,
+                                                                int blocks, int K, T* __restrict__ dw) {
   const int c = blockIdx.x * 16 + threadIdx.x % 16;
   const double v = column_sum(partial, blocks, (size_t)K, c, c < K);
   if (threadIdx.x < 16 && c < K) dw[c] = from_f32<T>((float)v);
@@ -556,18 +591,25 @@ constexpr int kNormRegisters = 16384;   // elements of a row that a workgroup ho
 static int norm_rows_at_once(int K) { return K <= 1024 ? 4 : 1; }
 // Workgroups: as few as keep the memory busy, for their sums of columns go out and back
 // (4451 x 1152 19.2 us with 512, 18.5 with 768; 8192 x 4096 51.6, 54; 4096 x 10240 73 with
-// 256, 80 with 512; 2000 x 8192 52.5, 57.8).
-int norm_bwd_blocks(int rows, int K) {
+// 256, 80 with 512; 2000 x 8192 52.5, 57.8).  fp64 sums of the longest rows, whose kernel has
+// several workgroups to a row, from 64 (600 x 20000 in fp32 61 us, 76 with 256).
+int norm_bwd_blocks(bool is_bf16, int rows, int K) {
   const int per = norm_rows_at_once(K);
   const long units = ((long)rows + per - 1) / per;
   // few rows: one workgroup, whose sums need no second launch
   if (units <= 4 && K <= kNormRegisters) return 1;
-  return (int)std::max(std::min<long>(units, K <= 1024 ? 512 : K <= 2048 ? 768 : K <= 4096 ? 512 : 256), (units + kChain - 1) / kChain);
+  const int most = K <= 1024 ? 512 : K <= 2048 ? 768 : K <= 4096 ? 512 : K <= kNormRegisters || is_bf16 ? 256 : 64;
+  return (int)std::max(std::min<long>(units, most), (units + kChain - 1) / kChain);
 }
 
 template <typename T, typename R>
-static void norm_bwd_any(const NormBwd& a, float* partial, float* rstd, hipStream_t st) {
-  const int blocks = norm_bwd_blocks(a.rows, a.K);
+static void norm_bwd_any(const NormBwd& a, float* ws, hipStream_t st) {
+  const int blocks = norm_bwd_blocks(sizeof(T) == 2, a.rows, a.K);
+  if (norm_bwd_ws_bytes(a.rows, a.K) == 0) ws = nullptr;
+  // rows' factors first, then the workgroups' sums of columns
+  float* const rstd = ws;
+  using S = ColumnSum<T>;
+  S* const partial = ws ? (S*)(ws + ((size_t)a.rows + 63) / 64 * 64) : nullptr;
 #define T2I_N(TPR, NV)                                                                                  \
   hipLaunchKernelGGL((add_rms_norm_bwd_kernel<T, R, TPR, NV>), dim3((unsigned)blocks),                  \
                      dim3(TPR > 256 ? TPR : 256), 0, st, a, partial)
@@ -585,29 +627,22 @@ static void norm_bwd_any(const NormBwd& a, float* partial, float* rstd, hipStrea
                          dim3(256), 0, st, a, rstd, partial);
   }
 #undef T2I_N
+  if (partial)
+    hipLaunchKernelGGL((norm_weight_grad_kernel<T>), dim3((unsigned)((a.K + 15) / 16)), dim3(1024), 0, st, partial, blocks,
+                       a.K, (T*)a.dw);
 }
 
 hipError_t launch_add_rms_norm_bwd(bool is_bf16, bool resid_bf16, const NormBwd& a, float* ws, hipStream_t st) {
-  const int blocks = norm_bwd_blocks(a.rows, a.K);
-  if (norm_bwd_ws_bytes(a.rows, a.K) == 0) ws = nullptr;
-  // rows' factors first, then the workgroups' sums of columns
-  float* const partial = ws ? ws + ((size_t)a.rows + 63) / 64 * 64 : nullptr;
-  if (is_bf16 && resid_bf16) norm_bwd_any<bf16, bf16>(a, partial, ws, st);
-  else if (is_bf16) norm_bwd_any<bf16, float>(a, partial, ws, st);
-  else norm_bwd_any<float, float>(a, partial, ws, st);
-  if (partial) {
-    const dim3 grid((unsigned)((a.K + 15) / 16));
-    if (is_bf16)
-      hipLaunchKernelGGL((norm_weight_grad_kernel<bf16>), grid, dim3(1024), 0, st, partial, blocks, a.K, (bf16*)a.dw);
-    else
-      hipLaunchKernelGGL((norm_weight_grad_kernel<float>), grid, dim3(1024), 0, st, partial, blocks, a.K, (float*)a.dw);
-  }
+  if (is_bf16 && resid_bf16) norm_bwd_any<bf16, bf16>(a, ws, st);
+  else if (is_bf16) norm_bwd_any<bf16, float>(a, ws, st);
+  else norm_bwd_any<float, float>(a, ws, st);
   return hipGetLastError();
 }
 
 size_t norm_bwd_ws_bytes(int rows, int K) {
-  if (norm_bwd_blocks(rows, K) == 1 && K <= kNormRegisters) return 0;
-  return (((size_t)rows + 63) / 64 * 64 + (size_t)norm_bwd_blocks(rows, K) * K) * 4;
+  const size_t low = norm_bwd_blocks(true, rows, K), full = norm_bwd_blocks(false, rows, K);
+  if (low == 1 && K <= kNormRegisters) return 0;
+  return (((size_t)rows + 63) / 64 * 64 + std::max(low, 2 * full) * K) * 4;   // (for either type)
 }
 
 }  // namespace t2i

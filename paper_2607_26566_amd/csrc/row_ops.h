@@ -121,10 +121,11 @@ __device__ __forceinline__ void load_piece(const T* row, int k, int K, Piece<T>&
   }
 }
 
-// Column sums of n rows of fp32 partials (row stride ld) in fp64: 16 columns
+// Column sums of n rows of fp32 or fp64 partials (row stride ld) in fp64: 16 columns
 // per workgroup of 1024, each by 64 threads that take every 64th row (so that a
 // sum's reads are all under way at once), joined in a fixed order.
-__device__ __forceinline__ double column_sum(const float* p, int n, size_t ld, int c, bool in) {
+template <typename S>
+__device__ __forceinline__ double column_sum(const S* p, int n, size_t ld, int c, bool in) {
   __shared__ double red[64][16];
   const int s = threadIdx.x / 16, l = threadIdx.x % 16;
   double v = 0.;

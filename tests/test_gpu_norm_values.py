@@ -57,3 +57,20 @@ def test_scales_of_small_weights_and_of_large_ones(dtype):
             rq, rs = blocks.add_rms_norm_i8(to_host(h)[:2] if big > 1 else to_host(h), to_host(w), 0.0)
             assert np.array_equal(q.cpu().numpy()[:, :K], rq)
             within(s, rs, 42 * E * rs + 2.0 ** -149)
+
+
+# rows of one wave, of a workgroup of one to four pieces per thread, longer ones
+@pytest.mark.parametrize("rows,K", [(13, 64), (40000, 64), (20000, 512), (9000, 1000), (6000, 1152), (3000, 4096),
+                                    (1400, 8192), (1300, 10000), (900, 16384), (700, 20000)])
+def test_weight_gradients_in_fp32_are_sums_in_more(rows, K):
+    """With h = +-1 and eps = 0 r is 1 but for its own rounding and that of 1 / K, 2 E and E, the same
+    in all rows, and dy n is exact otherwise: dw is off by that and by its last rounding, E, whatever
+    it is beside the sizes of what it sums up (fp64: 2^-53 of them for each of the rows)."""
+    say("dw", rows, K)
+    dy, hdy = rnd(rows, (rows, K), 1.0, F32)
+    h = torch.where(rnd(K, (rows, K), 1.0, F32)[0] < 0, -1.0, 1.0)
+    w, _ = rnd(K + 1, (K,), 0.3, F32)
+    _, _, dw = t2i.add_rms_norm_backward(dy, h, w, eps=0.0)
+    terms = hdy * to_host(h)
+    ref = terms.sum(0)
+    within(dw, ref, 4 * E * np.abs(ref) + 2.0 ** -53 * rows * np.abs(terms).sum(0))
