@@ -8,8 +8,8 @@ from __future__ import annotations
 import ctypes as C
 import math
 from array import array
-from operator import attrgetter
-from typing import Optional, Sequence, Union
+from operator import attrgetter, is_
+from typing import Iterable, Optional, Sequence, Union
 
 import torch
 from torch.autograd import forward_ad
@@ -41,8 +41,8 @@ class AdamW:
     are fp32: zeros, or the given ``exp_avg`` and ``exp_avg_sq`` with the number of ``step`` s
     behind them.  bf16 weights have fp32 ``masters`` -- the given ones, or copies -- whose
     rounded values they receive.  All of these are kept (attributes of the same names), to be
-    saved and passed in again by a program that resumes.  A weight's storage may be exchanged
-    between steps, the moments' and masters' may not.
+    saved and passed in again by a program that resumes.  A weight's storage, or its tensor in
+    ``params``, may be exchanged between steps, the moments' and masters' may not.
 
     With ``capturable`` the number of steps is counted on the device, so that a captured
     :meth:`step` counts on from replay to replay; without it a step is refused while a graph
@@ -82,9 +82,9 @@ class AdamW:
                        ("exp_avg_sq", self.exp_avg_sq, torch.float32)]
         if low:
             self._state.append(("masters", self.masters, torch.float32))
-        self._written = [t for _, tensors, _ in self._state for t in tensors]
+        self._kept = [t for _, tensors, _ in self._state[1:] for t in tensors]
         self._lay_out()
-        _need(not any(t.requires_grad for t in self._written[len(self.params):]), "moments and masters take no gradients", 1)
+        _need(not any(t.requires_grad for t in self._kept), "moments and masters take no gradients", 1)
         self._count = torch.tensor([int(step)], dtype=torch.int32, device=first.device) if capturable else None
         self._steps = int(step)
 
@@ -92,12 +92,19 @@ class AdamW:
         """The library's arrays of the tensors' addresses"""
         for what, tensors, dtype in self._state:
             self._listed(tensors, dtype, what)
-        self._held = [t.detach() for t in self._written]   # (the addresses stay valid)
-        spans = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in self._written if t.numel())
+        written = self._written()
+        held = [t.detach() for t in written]
+        spans = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in written if t.numel())
         for (at, size), (nxt, _) in zip(spans, spans[1:]):
             _need(at + size <= nxt, "weights, moments and masters must not overlap", 1)
+        self._seen, self._held = list(self.params), held   # (the addresses stay valid)
         self._arrays = [array("Q", map(_pointer, tensors)) for _, tensors, _ in self._state]
         self._at = [a.buffer_info()[0] for a in self._arrays] + [None] * (4 - len(self._arrays))
+
+    def _written(self):
+        """What a step writes: the weights as they are now (a program may have put others into
+        the list), moments and masters"""
+        return self.params + self._kept
 
     def _new(self, make):
         """fp32 tensors of the weights' shapes in one buffer, each at 256 bytes"""
@@ -107,7 +114,9 @@ class AdamW:
 
     def _listed(self, tensors, dtype, what: str):
         _need(len(tensors) == len(self._shapes), f"{what}: {len(self._shapes)} tensors expected, {len(tensors)} given")
-        for t, shape in zip(tensors, self._shapes):
+        for i, (t, shape) in enumerate(zip(tensors, self._shapes)):
+            if not isinstance(t, torch.Tensor):
+                raise T2IError(1, f"{what}: entry {i} is no tensor, but {type(t).__name__}")
             if t.get_device() != self._dev:
                 raise T2IError(1, f"{what}: tensors must be on the first weight's device")
             if t.dtype is not dtype or t.shape != shape or not t.is_contiguous():
@@ -121,27 +130,41 @@ class AdamW:
     def step(self, grads: Sequence[torch.Tensor], *, lr: Union[float, torch.Tensor, None] = None,
              grad_scale: Optional[torch.Tensor] = None, stream=None) -> None:
         """One step with the gradients of all weights, of one type (bf16 or fp32) and the weights'
-        shapes.  ``lr``: instead of the constructor's, a number or one fp32 value on the device;
-        ``grad_scale``: one fp32 value on the device that the gradients are multiplied by (the
-        factor of a clipped norm).  Refused while gradients of a weight are recorded, like any
-        operation in place on a leaf: call it under ``torch.no_grad()``."""
+        shapes (a weight that took no part has a gradient of zeros, not None).  ``lr``: instead of
+        the constructor's, a number or one fp32 value on the device; ``grad_scale``: one fp32 value
+        on the device that the gradients are multiplied by (the factor of a clipped norm).  Refused
+        while gradients of a weight are recorded, like any operation in place on a leaf: call it
+        under ``torch.no_grad()``."""
         dev = self._dev
         if _elsewhere(dev, stream):
             with _switch(dev, stream):
                 return self.step(grads, lr=lr, grad_scale=grad_scale)
-        kind = _DTYPES.get(grads[0].dtype) if len(grads) else None
+        if not isinstance(grads, (list, tuple)):
+            _need(isinstance(grads, Iterable) and not isinstance(grads, torch.Tensor), "gradients must be a sequence", 1)
+            grads = list(grads)
+        first = grads[0] if len(grads) else None
+        kind = _DTYPES.get(first.dtype) if isinstance(first, torch.Tensor) else None
         _need(kind is not None, "gradients of all weights, bf16 or fp32", 1)
         # (as lists and sets: the checks of a hundred tensors one by one take longer than the step)
-        if (list(map(_shape, grads)) != self._shapes or set(map(_device_of, grads)) != {dev}
-                or set(map(_dtype, grads)) != {grads[0].dtype} or not all(map(_whole, grads))):
-            self._listed(grads, grads[0].dtype, "grads")
-        if array("Q", map(_pointer, self.params)) != self._arrays[0]:
+        try:
+            fit = (list(map(_shape, grads)) == self._shapes and set(map(_device_of, grads)) == {dev}
+                   and set(map(_dtype, grads)) == {first.dtype} and all(map(_whole, grads)))
+        except (AttributeError, TypeError):   # (no tensor)
+            fit = False
+        if not fit:
+            self._listed(grads, first.dtype, "grads")
+        try:
+            at_rest = (len(self.params) == len(self._seen) and all(map(is_, self.params, self._seen))
+                       and array("Q", map(_pointer, self.params)) == self._arrays[0])
+        except TypeError:
+            at_rest = False
+        if not at_rest:
             self._lay_out()
         if torch.is_grad_enabled():
             _need(True not in map(_requires_grad, self.params) and True not in map(_requires_grad, grads),
                   "a tensor requires a gradient, which this call does not record: call under torch.no_grad()", 1)
         if getattr(forward_ad, "_current_level", 0) >= 0:   # (within a dual level)
-            _need(all(forward_ad.unpack_dual(t).tangent is None for t in (*self._written, *grads)),
+            _need(all(forward_ad.unpack_dual(t).tangent is None for t in (*self._written(), *grads)),
                   "a tensor carries a tangent, which this call does not pass on", 1)
         on_device = isinstance(lr, torch.Tensor)
         lr_at = _scalar(lr if on_device else None, dev, "lr")
@@ -168,4 +191,4 @@ class AdamW:
                 self._count -= 1
             raise
         self._steps += 1
-        torch.autograd.graph.increment_version(self._written)
+        torch.autograd.graph.increment_version(self._written())
