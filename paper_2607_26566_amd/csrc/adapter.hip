@@ -776,9 +776,17 @@ hipError_t launch_adapter_dx(bool is_bf16, const void* dy, int lddy, const void*
 //
 // Adapter i's rows, in ascending order, are order[start .. start + count), (start, count) =
 // span[i].  Cut at every multiple of `per` they are the slices of the gradients' sums;
-// slice b of adapter i has number b + i in `slices` (adapter, first, rows), so that each
-// number below M / per + n is written by one workgroup, empty ones too.  A workgroup per
-// adapter reads the whole index twice.
+// slice b of adapter i has number b + i in `slices` (adapter, first, rows, place), so that
+// each number below M / per + n is written by one workgroup, empty ones too.  An adapter's
+// only slice, or its first if it has no rows, goes to the gradients (kWhole), a further empty
+// one nowhere (kNowhere).  Of slices b at most one goes on from b - 1 and at most one begins
+// and goes on to b + 1: their places among the partial sums are 2 b and 2 b + 1, however many
+// adapters there are.  A workgroup per adapter reads the whole index twice.
+constexpr int kWhole = -1, kNowhere = -2;
+__device__ __forceinline__ int place_of(int b, int start, int count, int per) {
+  const int b0 = start / per, b1 = count > 0 ? (start + count - 1) / per : b0;
+  return b > b1 ? kNowhere : b0 == b1 ? kWhole : b == b0 ? 2 * b + 1 : 2 * b;
+}
 __device__ __forceinline__ void group_rows(const AdapterPrepare& p, int ad) {
   __shared__ int red[2][16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, M = p.M;
@@ -804,7 +812,7 @@ __device__ __forceinline__ void group_rows(const AdapterPrepare& p, int ad) {
   const int end = start + count, last = ad == p.n - 1 ? M / p.per : end / p.per;
   for (int b = start / p.per + (int)threadIdx.x; b <= last; b += 1024) {
     const int lo = max(start, b * p.per), hi = min(end, (b + 1) * p.per);
-    p.slices[b + ad] = int4{ad, lo, max(hi - lo, 0), 0};
+    p.slices[b + ad] = int4{ad, lo, max(hi - lo, 0), place_of(b, start, count, p.per)};
   }
   if (count == 0) return;
   int at = start;
@@ -941,7 +949,7 @@ int adapter_slice_rows(bool is_bf16, int M, int N, int K, int n, int rank) {
   return per;
 }
 
-// One slice's part of the gradients: partial[slice][j][c] = sum over its rows of v[m, j]
+// One slice's part of the gradients: partial[place][j][c] = sum over its rows of v[m, j]
 // z[m, c], with (z, v) = (x, u) for dA and (dy, t) for dB, side by side in the grid.  A
 // wave takes every fourth step of 32 (fp32: 16) of the slice's rows and 128 (64)
 // columns: a lane reads 16 bytes of each of its 8 (4) rows and joins the halves of
@@ -956,15 +964,16 @@ __global__ __launch_bounds__(256, RT == 1 ? 4 : 2) void adapter_outer_kernel(Ada
   const bool second = (int)blockIdx.x >= p.blocks0;
   const AdapterSide& d = second ? p.side[1] : p.side[0];
   const int c0 = ((int)blockIdx.x - (second ? p.blocks0 : 0)) * COLS + fr * L, C = d.cols, j0 = blockIdx.z * RT * 16;
-  int first, rows;
+  int ad, first, rows, place;
   if (p.slices) {
     const int4 sl = p.slices[blockIdx.y];
-    first = sl.y, rows = sl.z;
-  } else {
+    ad = sl.x, first = sl.y, rows = sl.z, place = sl.w;
+  } else {   // (all rows are adapter 0's; if they are one slice, slice i is adapter i's)
+    ad = p.M <= p.per ? blockIdx.y : 0;
     first = blockIdx.y * p.per, rows = max(0, min(p.per, p.M - first));
+    place = p.M <= p.per ? kWhole : place_of(blockIdx.y, 0, p.M, p.per);
   }
-  T* const done = (T*)d.grad;   // (one slice to an adapter: the gradient itself)
-  if (rows <= 0 && !done) return;
+  if (place == kNowhere) return;
   const T* const z = (const T*)d.z;
   const float* const v = d.v;
   const bool in = c0 < C, part = c0 + L > C;
@@ -1057,8 +1066,9 @@ __global__ __launch_bounds__(256, RT == 1 ? 4 : 2) void adapter_outer_kernel(Ada
     }
   }
   if (wave > 0 || !in) return;
-  if (done) {
-    const int ad = p.slices ? p.slices[blockIdx.y].x : blockIdx.y, left = C - c0;
+  if (place == kWhole) {
+    T* const done = (T*)d.grad;
+    const int left = C - c0;
 #pragma unroll
     for (int jt = 0; jt < RT; ++jt) {
       const int j = j0 + jt * 16 + g * 4, ranks = p.rank - j;
@@ -1082,7 +1092,7 @@ __global__ __launch_bounds__(256, RT == 1 ? 4 : 2) void adapter_outer_kernel(Ada
     }
     return;
   }
-  float* const out = d.partial + (size_t)blockIdx.y * p.ranks * d.ldp + c0;
+  float* const out = d.partial + (size_t)place * p.ranks * d.ldp + c0;
 #pragma unroll
   for (int jt = 0; jt < RT; ++jt)
 #pragma unroll
@@ -1095,50 +1105,59 @@ __global__ __launch_bounds__(256, RT == 1 ? 4 : 2) void adapter_outer_kernel(Ada
     }
 }
 
-// dA [n][rank][K] and dB [n][N][rank]: the slices' parts of every adapter, added up in
-// fp64 in ascending order; zeros for an adapter without rows.  A thread takes four
-// columns of one rank (dA), or one column of four (dB).
+// dA [n][rank][K] and dB [n][N][rank] of adapters of several slices: their parts, added up
+// in fp64 in ascending order; zeros for the adapters that rows without an index do not take.
+// A thread takes four columns of one rank (dA), or one column of four (dB).
 template <typename T>
 __global__ __launch_bounds__(256) void adapter_sum_kernel(AdapterOuter p, T* dA, T* dB, int per_a) {
   const int ad = blockIdx.y;
   const int2 span = p.span ? p.span[ad] : int2{0, ad == 0 ? p.M : 0};
   const int b0 = span.x / p.per, b1 = span.y > 0 ? (span.x + span.y - 1) / p.per + 1 : b0;
+  if (p.span && b1 <= b0 + 1) return;
   const bool is_b = (int)blockIdx.x >= per_a;
   const long x = ((int)blockIdx.x - (is_b ? per_a : 0)) * 256L + threadIdx.x;
   const AdapterSide& d = is_b ? p.side[1] : p.side[0];
   const int per_row = is_b ? d.cols : (d.cols + 3) / 4;
   const int c = (int)(x % per_row) * (is_b ? 1 : 4), j0 = (int)(x / per_row) * (is_b ? 4 : 1);
   if (j0 >= p.rank) return;
-  const float* at = d.partial + ((size_t)(b0 + ad) * p.ranks + j0) * d.ldp + c;
   const size_t slice = (size_t)p.ranks * d.ldp;
+  const float* const parts = d.partial + (size_t)j0 * d.ldp + c;
+  auto part = [&](int b) { return parts + (size_t)(b == b0 ? 2 * b + 1 : 2 * b) * slice; };
   double s[4] = {0., 0., 0., 0.};
   if (!is_b) {
 #pragma unroll 4
-    for (int b = b0; b < b1; ++b, at += slice) {
-      const f32x4 v = *(const f32x4*)at;
+    for (int b = b0; b < b1; ++b) {
+      const f32x4 v = *(const f32x4*)part(b);
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[e] += (double)v[e];
     }
   } else {
 #pragma unroll 4
-    for (int b = b0; b < b1; ++b, at += slice)
+    for (int b = b0; b < b1; ++b) {
+      const float* const at = part(b);
 #pragma unroll
       for (int e = 0; e < 4; ++e) s[e] += (double)at[(size_t)e * d.ldp];
+    }
   }
   const float v[4] = {(float)s[0], (float)s[1], (float)s[2], (float)s[3]};
   if (!is_b) store4(dA + ((size_t)ad * p.rank + j0) * d.cols + c, d.cols - c, v);
   else store4(dB + ((size_t)ad * d.cols + c) * p.rank + j0, p.rank - j0, v);
 }
 
+// slices of the launch: with an index M / per + n numbers; of up to one slice of rows one
+// for every adapter, which need no sums
+int adapter_slices(bool indexed, int M, int n, int per) {
+  return (indexed ? M < per : M <= per) ? n : indexed ? M / per + n : (M + per - 1) / per;
+}
+// places of the partial sums
+int adapter_places(int M, int per) { return M < per ? 0 : 2 * ((M - 1) / per + 1); }
+
 template <typename T>
-static void outer_any(AdapterOuter p, int n, int slices, T* dA, T* dB, hipStream_t st) {
+static void outer_any(AdapterOuter p, int n, T* dA, T* dB, hipStream_t st) {
   constexpr int COLS = 16 * kLaneK<T>;
-  // up to one slice of rows: slice i is adapter i's, empty ones too
-  const bool direct = p.M < p.per;
-  if (direct) {
-    p.side[0].grad = dA, p.side[1].grad = dB;
-    slices = n;
-  }
+  const int slices = adapter_slices(p.slices != nullptr, p.M, n, p.per);
+  const bool direct = p.slices ? p.M < p.per : p.M <= p.per;
+  p.side[0].grad = dA, p.side[1].grad = dB;
   const int blocks1 = dB ? (p.side[1].cols + COLS - 1) / COLS : 0;
   p.blocks0 = dA ? (p.side[0].cols + COLS - 1) / COLS : 0;
   if (p.rank <= 16)
@@ -1153,10 +1172,9 @@ static void outer_any(AdapterOuter p, int n, int slices, T* dA, T* dB, hipStream
   const int b = dB ? (int)(((long)p.side[1].cols * ((p.rank + 3) / 4) + 255) / 256) : 0;
   hipLaunchKernelGGL((adapter_sum_kernel<T>), dim3((unsigned)(a + b), (unsigned)n), dim3(256), 0, st, p, dA, dB, a);
 }
-hipError_t launch_adapter_outer(bool is_bf16, const AdapterOuter& p, int n, int slices, void* dA, void* dB,
-                                hipStream_t st) {
-  if (is_bf16) outer_any(p, n, slices, (bf16*)dA, (bf16*)dB, st);
-  else outer_any(p, n, slices, (float*)dA, (float*)dB, st);
+hipError_t launch_adapter_outer(bool is_bf16, const AdapterOuter& p, int n, void* dA, void* dB, hipStream_t st) {
+  if (is_bf16) outer_any(p, n, (bf16*)dA, (bf16*)dB, st);
+  else outer_any(p, n, (float*)dA, (float*)dB, st);
   return hipGetLastError();
 }
 

@@ -28,37 +28,36 @@ bool bad_sizes(int32_t M, int32_t N, int32_t K, int32_t n, int32_t rank) {
 
 // the gradients' workspace
 struct Room {
-  int per, slices;                       // rows of a slice, slices
+  int per;                               // rows of a slice
   size_t u, at, bt, order, span, table, part_a, part_b, dx, all;   // offsets
 };
 Room room_of(bool bf, int32_t M, int32_t N, int32_t K, int32_t n, int32_t rank) {
   Room r;
   const size_t e = bf ? 2 : 4;
   r.per = adapter_slice_rows(bf, M, N, K, n, rank);
-  r.slices = M / r.per + n;
   size_t o = 0;
   auto take = [&](size_t bytes) {
     const size_t here = o;
     o += whole(bytes);
     return here;
   };
-  const size_t ranks = (rank + 3) / 4 * 4;
+  const size_t ranks = (rank + 3) / 4 * 4, places = adapter_places(M, r.per);
   r.u = take((size_t)M * adapter_cols(rank) * 4);
   r.at = take((size_t)n * K * whole8(rank) * e);
-  r.bt = take((size_t)n * rank * N * e);
+  r.bt = take(adapter_few_rows(M, N, rank) ? 0 : (size_t)n * rank * N * e);
   r.order = take((size_t)M * 4);
   r.span = take((size_t)n * 8);
-  r.table = take((size_t)r.slices * 16);
-  r.part_a = take((size_t)r.slices * ranks * whole8(K) * 4);
-  r.part_b = take((size_t)r.slices * ranks * whole8(N) * 4);
+  r.table = take((size_t)(M / r.per + n) * 16);
+  r.part_a = take(places * ranks * whole8(K) * 4);
+  r.part_b = take(places * ranks * whole8(N) * 4);
   r.dx = take(adapter_dx_floats(bf, M, N, K) * 4);
   r.all = o;
   return r;
 }
-// whether the sums' slices pass a launch
-bool too_many_slices(bool bf, const Room& r, int32_t N, int32_t K, int32_t rank) {
-  const int64_t cols = bf ? 128 : 64, blocks = (K + cols - 1) / cols + (N + cols - 1) / cols;
-  return blocks * r.slices * ((rank + 31) / 32) >= 1 << 24 || r.slices > 65535;
+// whether the slices of the sums of so many columns pass a launch
+bool too_many_slices(bool bf, int64_t slices, int64_t da_columns, int64_t db_columns, int32_t rank) {
+  const int64_t cols = bf ? 128 : 64, blocks = (da_columns + cols - 1) / cols + (db_columns + cols - 1) / cols;
+  return blocks * slices * ((rank + 31) / 32) >= 1 << 24 || slices > 65535;
 }
 
 t2i_status check_operands(int32_t dtype, int32_t M, int32_t N, int32_t K, const void* x, int32_t ldx, const void* w,
@@ -147,7 +146,8 @@ t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, i
   if (off(dy, al) || off(dx, al) || off(da, bytes_of(dtype)) || off(db, bytes_of(dtype)) || off(ws, 256))
     return ops_fail(T2I_ERR_INVALID_ARG, "pointers need 16-byte (bf16) or 4-byte (fp32) alignment, ws 256-byte");
   const Room r = room_of(bf, M, N, K, n, rank);
-  if (too_many_slices(bf, r, N, K, rank)) return ops_fail(T2I_ERR_SHAPE, "too many adapters for a launch");
+  if (too_many_slices(bf, adapter_slices(index != nullptr, M, n, r.per), da ? K : 0, db ? N : 0, rank))
+    return ops_fail(T2I_ERR_SHAPE, "too many adapters for a launch");
   if (ws_bytes < r.all) return ops_fail(T2I_ERR_WORKSPACE, "workspace too small");
   hipStream_t st = (hipStream_t)stream;
   char* const at = (char*)ws;
@@ -198,7 +198,6 @@ t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, i
     err = launch_adapter_dx(bf, dy, lddy, w, ldw, M, N, K, up, dx, lddx, (float*)(at + r.dx), st);
   }
   if (err == hipSuccess && sums) {
-    const int slices = index ? r.slices : (M + r.per - 1) / r.per;
     AdapterOuter o;
     std::memset(&o, 0, sizeof(o));
     o.side[0] = AdapterSide{x, (const float*)(at + r.u), ldx, ldu, K, (float*)(at + r.part_a), whole8(K), nullptr};
@@ -213,7 +212,7 @@ t2i_status t2i_op_adapter_linear_backward(int32_t dtype, int32_t M, int32_t N, i
       o.slices = (const int4*)(at + r.table);
     }
     // (without an index only adapter 0 has rows)
-    err = launch_adapter_outer(bf, o, n, slices, da, db, st);
+    err = launch_adapter_outer(bf, o, n, da, db, st);
   }
   return done(err);
 }

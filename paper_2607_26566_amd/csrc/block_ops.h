@@ -216,9 +216,9 @@ struct AdapterSide {
   const void* z;                     // [M, cols]
   const float* v;                    // [M, ldv]
   int ldz, ldv, cols;
-  float* partial;                    // [slices][ranks][ldp]
+  float* partial;                    // [places][ranks][ldp]
   int ldp;                           // cols in whole pieces of eight
-  void* grad;                        // set by the launch: dA, dB if they need no partial sums
+  void* grad;                        // set by the launch: dA, dB
 };
 struct AdapterOuter {
   AdapterSide side[2];               // dA: (x, u), dB: (dy, t)
@@ -228,8 +228,9 @@ struct AdapterOuter {
   const int2* span;
   const int4* slices;
 };
-hipError_t launch_adapter_outer(bool is_bf16, const AdapterOuter& p, int n, int slices, void* dA, void* dB,
-                                hipStream_t st);
+int adapter_slices(bool indexed, int M, int n, int per);
+int adapter_places(int M, int per);
+hipError_t launch_adapter_outer(bool is_bf16, const AdapterOuter& p, int n, void* dA, void* dB, hipStream_t st);
 
 // ---- AdamW over many tensors
 
