@@ -89,22 +89,18 @@ class AdamW:
         self._steps = int(step)
 
     def _lay_out(self):
-        """The library's arrays of the tensors' addresses"""
+        """The library's arrays of the tensors' addresses: the weights as they are now (a program
+        may have put others into the list), moments and masters"""
         for what, tensors, dtype in self._state:
             self._listed(tensors, dtype, what)
-        written = self._written()
+        written = self.params + self._kept
         held = [t.detach() for t in written]
         spans = sorted((t.data_ptr(), t.numel() * t.element_size()) for t in written if t.numel())
         for (at, size), (nxt, _) in zip(spans, spans[1:]):
             _need(at + size <= nxt, "weights, moments and masters must not overlap", 1)
-        self._seen, self._held = list(self.params), held   # (the addresses stay valid)
+        self._seen, self._written, self._held = list(self.params), written, held   # (the addresses stay valid)
         self._arrays = [array("Q", map(_pointer, tensors)) for _, tensors, _ in self._state]
         self._at = [a.buffer_info()[0] for a in self._arrays] + [None] * (4 - len(self._arrays))
-
-    def _written(self):
-        """What a step writes: the weights as they are now (a program may have put others into
-        the list), moments and masters"""
-        return self.params + self._kept
 
     def _new(self, make):
         """fp32 tensors of the weights' shapes in one buffer, each at 256 bytes"""
@@ -164,7 +160,7 @@ class AdamW:
             _need(True not in map(_requires_grad, self.params) and True not in map(_requires_grad, grads),
                   "a tensor requires a gradient, which this call does not record: call under torch.no_grad()", 1)
         if getattr(forward_ad, "_current_level", 0) >= 0:   # (within a dual level)
-            _need(all(forward_ad.unpack_dual(t).tangent is None for t in (*self._written(), *grads)),
+            _need(all(forward_ad.unpack_dual(t).tangent is None for t in (*self._written, *grads)),
                   "a tensor carries a tangent, which this call does not pass on", 1)
         on_device = isinstance(lr, torch.Tensor)
         lr_at = _scalar(lr if on_device else None, dev, "lr")
@@ -191,4 +187,4 @@ class AdamW:
                 self._count -= 1
             raise
         self._steps += 1
-        torch.autograd.graph.increment_version(self._written())
+        torch.autograd.graph.increment_version(self._written)
