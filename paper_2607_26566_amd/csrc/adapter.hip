@@ -14,7 +14,7 @@
 // What bounds them: the layer is its tile product's (7531 x 4608 x 1152, rank 32, adapters
 // in runs 100 - 118 us of 82.7 GFLOP, 4096 x 4096 x 4096, rank 16 105 of 137, dx 112), for
 // few rows HBM and the ring's first loads (24 x 4096 x 4096 10.5 us); t and the gradients'
-// sums are bound by reading x or dy once (33.6 MB: t 12.8 us, both sums 13.9).
+// sums are bound by reading x or dy once (33.6 MB: t 12.8 us, both sums 16.5).
 //
 // Adapters never meet: a row's sums hold nothing of another row's adapter, not even
 // times zero (a NaN in one tenant's adapter stays in that tenant's rows).
@@ -939,7 +939,7 @@ constexpr int kSliceRows = 1024;
 // up to 16 ranks, where a wave has one step's loads under way instead of two: 1024), at
 // least a step of four waves.  dA and dB alone, 7531 x 4608 x 1152, rank 32, 8 adapters 67
 // us with 1024 rows, 71 with 512, 87 with 128; 3320 x 224 x 4256, rank 32 36, 30, 36; 4096 x
-// 4096 x 4096, rank 16 41, 35, 38, 34 with 256.
+// 4096 x 4096, rank 16 41, 35, 38, 34 with 256 (t in two bf16 parts; in three 35.5).
 int adapter_slice_rows(bool is_bf16, int M, int N, int K, int n, int rank) {
   if (M <= 768) return kSliceRows;
   const int cols = is_bf16 ? 128 : 64;
